@@ -299,6 +299,94 @@ int vgg_softmax_xent_bwd(int N, int K, const float *p, const int32_t *labels, fl
 /* theta[i] -= lr * grad[i], i < n. */
 int vgg_sgd_update(size_t n, float *theta, const float *grad, float lr, void *stream);
 
+/* ------------------------------------------------- answers: log probabilities */
+
+/* Class scores to log probabilities.  z [N] rows of K scores in `dtype`, a row
+ * every ldz elements (ldz >= K, any alignment of a row); everything that is
+ * written is fp32 (classes int32):
+ *   logp[n]    = z[n,y] - log sum_j exp(z[n,j]), y = labels[n]; 0 where y is
+ *                not in [0,K) (as in vgg_softmax_xent_bwd);
+ *   entropy[n] = -sum_j p log p of the row's probabilities;
+ *   top_logp[n][top], top_idx[n][top]: the `top` most likely classes and their
+ *                log probabilities, best first, the lower class first among
+ *                equal scores; 0 <= top <= min(K, VGG_MAX_TOP);
+ *   stats[n][2]: the row's largest score and the log of the sum of the
+ *                exponentials of what the scores are above it, which
+ *                vgg_log_probs_bwd takes.
+ * Each may be NULL (labels and logp together; top_logp and top_idx exactly
+ * when top is 0).  A score of -inf masks its class: probability 0, never an
+ * alternative.  Missing alternatives are -inf at class -1; a row without a
+ * class left has logp -inf and entropy 0.  A NaN or +inf among a row's scores
+ * makes the row's results NaN (alternatives: at class -1).  N <= 2^23.
+ * The scores are read once; sums are fp32.  Rows too few to fill the chip are
+ * cut into parts that a second kernel joins in a fixed order (workspace). */
+#define VGG_MAX_TOP 64
+size_t vgg_log_probs_workspace_bytes(int dtype, int N, int K, int top);
+int vgg_log_probs(int dtype, int N, int K, size_t ldz, const void *z, const int32_t *labels, int top, float *logp,
+                  float *entropy, float *top_logp, int32_t *top_idx, float *stats, void *ws, size_t ws_bytes,
+                  void *stream);
+/* The gradient of logp and entropy with respect to the scores, p = exp(log p):
+ *   dz[n,j] = g_logp[n] (1[j = labels[n]] - p_j) - g_entropy[n] p_j (log p_j + entropy[n])
+ * with the first term absent where the label is not in [0,K).  stats and
+ * entropy are vgg_log_probs' of the same scores; g_logp (then labels) or
+ * g_entropy (then entropy) may be NULL, not both.  dz in `dtype`, a row every
+ * lddz elements; dz may be z itself (lddz = ldz).  Masked classes, rows
+ * without a class and rows whose two upstream gradients are zero get zeros,
+ * whatever the scores of the latter. */
+int vgg_log_probs_bwd(int dtype, int N, int K, size_t ldz, const void *z, const int32_t *labels, const float *stats,
+                      const float *entropy, const float *g_logp, const float *g_entropy, void *dz, size_t lddz,
+                      void *stream);
+
+/* ------------------------------------------------ dense layers from 4-bit weights */
+
+/* A 4-bit weight is a code's value times its group's scale.  Codes: bit 3 the
+ * sign, bits 0..2 one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (E2M1).  A group is
+ * `group` (32, 64 or 128) consecutive inputs of one output, the last of a row
+ * what is left.  codes [Out][ceil(In/32)*16] bytes: two codes a byte, the even
+ * input in the low half, rows padded to 32 codes (padding is never used).
+ * scales [Out][ceil(In/group)] bf16.
+ *
+ * Rounding fp32 weights w [Out][In]: the scale is the group's largest
+ * magnitude times fp32(1/6), rounded to bf16; a code is that of the value
+ * nearest to w / scale, the even code at ties (padding codes are 0).  A group
+ * with a NaN or an infinity gets the scale NaN.  Padding, where a row has it,
+ * is written.  w must be 16-byte aligned, and codes and scales. */
+int vgg_fc_w4_quantize(int In, int Out, int group, const float *w, uint8_t *codes, uint16_t *scales, void *stream);
+/* The fp32 values w [Out][In] that codes and scales stand for. */
+int vgg_fc_w4_dequantize(int In, int Out, int group, const uint8_t *codes, const uint16_t *scales, float *w, void *stream);
+/* vgg_fc with such weights: z[n,o] = f(bias[o] + sum_i w[o,i] a[n,i]), a
+ * [N][In] in `dtype` (rows densely packed), z [N][Out] in z_dtype, bias fp32
+ * or NULL.  Any N, In, Out > 0.  Weights are never rounded further: products
+ * of code values and activations (fp32 ones to 2^-24) are summed in fp32
+ * group by group, and a group's sum is multiplied by its scale. */
+size_t vgg_fc_w4_workspace_bytes(int dtype, int N, int In, int Out, int group);
+int vgg_fc_w4(int dtype, int N, int In, int Out, int group, const void *a, const uint8_t *codes, const uint16_t *scales,
+              const float *bias, void *z, int z_dtype, int relu, void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------------ orthogonalised updates */
+
+/* y = NS(x) for each of `batch` matrices x [rows][cols] in `dtype`, one after
+ * the other in memory: x / (|x|_F + 1e-7), then `steps` (1..20) times
+ *   G = X X^T,  X <- 3.4445 X + (-4.7750 G + 2.0315 G G) X
+ * (with X^T in X's place where rows > cols: the same values), which takes the
+ * singular values towards 1.  VGG_F32: products as exact as fp32 ones (two
+ * f16 parts per value, fp32 sums).  VGG_BF16: x and y are bf16, operands of a
+ * product hold 11 bits, sums and the iterate are fp32.  y may be x.  A matrix
+ * with a NaN or an infinity comes out NaN.  min(rows, cols) <= 32768, both
+ * <= 2^22, batch <= 65535. */
+size_t vgg_orthogonalize_workspace_bytes(int dtype, int batch, int rows, int cols);
+int vgg_orthogonalize(int dtype, int batch, int rows, int cols, int steps, const void *x, void *y, void *ws,
+                      size_t ws_bytes, void *stream);
+/* One optimiser step on fp32 matrices [batch][rows][cols] (a dense layer's
+ * weights, or a convolution's [Cout][Cin*9]):
+ *   momentum <- mu momentum + grad,  u = grad + mu momentum (nesterov != 0)
+ *                                    or momentum,
+ *   theta <- (1 - lr weight_decay) theta - lr sqrt(max(1, rows/cols)) NS(u).
+ * dtype says how exact the products of NS are, as above (all buffers fp32). */
+size_t vgg_muon_workspace_bytes(int dtype, int batch, int rows, int cols);
+int vgg_muon_update(int dtype, int batch, int rows, int cols, int steps, float *theta, const float *grad, float *momentum,
+                    float lr, float mu, int nesterov, float weight_decay, void *ws, size_t ws_bytes, void *stream);
+
 /* ------------------------------------------------------------- whole model */
 
 /* Size in bytes of the packed parameter block for cfg, and of the

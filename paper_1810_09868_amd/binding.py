@@ -30,6 +30,9 @@ EXPORTS = [
     "vgg19_pack_params", "vgg19_unpack_params", "vgg19_forward", "vgg19_train_step", "vgg19_plan",
     "vgg19_timed", "vgg_mfma_probe_sink_bytes", "vgg_mfma_probe", "vgg_conv3x3_plan",
     "vgg_fc_static",
+    "vgg_log_probs_workspace_bytes", "vgg_log_probs", "vgg_log_probs_bwd",
+    "vgg_fc_w4_quantize", "vgg_fc_w4_dequantize", "vgg_fc_w4_workspace_bytes", "vgg_fc_w4",
+    "vgg_orthogonalize_workspace_bytes", "vgg_orthogonalize", "vgg_muon_workspace_bytes", "vgg_muon_update",
 ]
 
 
@@ -92,6 +95,20 @@ def lib() -> C.CDLL:
         L.vgg_softmax.argtypes = [_i, _i, _vp, _vp, _vp]
         L.vgg_softmax_xent_bwd.argtypes = [_i, _i, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
         L.vgg_sgd_update.argtypes = [_sz, _vp, _vp, C.c_float, _vp]
+        L.vgg_log_probs_workspace_bytes.restype = _sz
+        L.vgg_log_probs_workspace_bytes.argtypes = [_i] * 4
+        L.vgg_log_probs.argtypes = [_i, _i, _i, _sz, _vp, _vp, _i] + [_vp] * 6 + [_sz, _vp]
+        L.vgg_log_probs_bwd.argtypes = [_i, _i, _i, _sz] + [_vp] * 7 + [_sz, _vp]
+        L.vgg_fc_w4_quantize.argtypes = [_i] * 3 + [_vp] * 4
+        L.vgg_fc_w4_dequantize.argtypes = [_i] * 3 + [_vp] * 4
+        L.vgg_fc_w4_workspace_bytes.restype = _sz
+        L.vgg_fc_w4_workspace_bytes.argtypes = [_i] * 5
+        L.vgg_fc_w4.argtypes = [_i] * 5 + [_vp] * 5 + [_i, _i, _vp, _sz, _vp]
+        for n in ("vgg_orthogonalize_workspace_bytes", "vgg_muon_workspace_bytes"):
+            getattr(L, n).restype = _sz
+            getattr(L, n).argtypes = [_i] * 4
+        L.vgg_orthogonalize.argtypes = [_i] * 5 + [_vp, _vp, _vp, _sz, _vp]
+        L.vgg_muon_update.argtypes = [_i] * 5 + [_vp] * 3 + [C.c_float, C.c_float, _i, C.c_float, _vp, _sz, _vp]
         cfgp = C.POINTER(VggConfig)
         prmp = C.POINTER(Vgg19Params)
         for n in ("vgg19_packed_bytes", "vgg19_forward_workspace_bytes", "vgg19_train_workspace_bytes"):
@@ -282,6 +299,60 @@ def vgg_softmax_xent_bwd(N, K, p, labels, loss, dz, ws):
 
 def vgg_sgd_update(n, theta, grad, lr):
     _chk(lib().vgg_sgd_update(n, _ptr(theta), _ptr(grad), float(lr), _stream()), "vgg_sgd_update")
+
+
+# -------------------------------------------- answers, 4-bit weights, orthogonalised updates
+MAX_TOP = 64  # VGG_MAX_TOP
+
+
+def vgg_log_probs_workspace_bytes(dtype, N, K, top=0) -> int:
+    return lib().vgg_log_probs_workspace_bytes(dtype, N, K, top)
+
+
+def vgg_log_probs(dtype, N, K, z, labels, top, logp, entropy, top_logp, top_idx, stats, ws=None, ldz=None):
+    _chk(lib().vgg_log_probs(dtype, N, K, K if ldz is None else ldz, _ptr(z), _ptr(labels), top, _ptr(logp), _ptr(entropy),
+                             _ptr(top_logp), _ptr(top_idx), _ptr(stats), _ptr(ws), _nbytes(ws), _stream()), "vgg_log_probs")
+
+
+def vgg_log_probs_bwd(dtype, N, K, z, labels, stats, entropy, g_logp, g_entropy, dz, ldz=None, lddz=None):
+    _chk(lib().vgg_log_probs_bwd(dtype, N, K, K if ldz is None else ldz, _ptr(z), _ptr(labels), _ptr(stats), _ptr(entropy),
+                                 _ptr(g_logp), _ptr(g_entropy), _ptr(dz), K if lddz is None else lddz, _stream()),
+         "vgg_log_probs_bwd")
+
+
+def vgg_fc_w4_quantize(In, Out, group, w, codes, scales):
+    _chk(lib().vgg_fc_w4_quantize(In, Out, group, _ptr(w), _ptr(codes), _ptr(scales), _stream()), "vgg_fc_w4_quantize")
+
+
+def vgg_fc_w4_dequantize(In, Out, group, codes, scales, w):
+    _chk(lib().vgg_fc_w4_dequantize(In, Out, group, _ptr(codes), _ptr(scales), _ptr(w), _stream()), "vgg_fc_w4_dequantize")
+
+
+def vgg_fc_w4_workspace_bytes(dtype, N, In, Out, group) -> int:
+    return lib().vgg_fc_w4_workspace_bytes(dtype, N, In, Out, group)
+
+
+def vgg_fc_w4(dtype, N, In, Out, group, a, codes, scales, bias, z, z_dtype, relu, ws=None):
+    _chk(lib().vgg_fc_w4(dtype, N, In, Out, group, _ptr(a), _ptr(codes), _ptr(scales), _ptr(bias), _ptr(z), z_dtype, int(relu),
+                         _ptr(ws), _nbytes(ws), _stream()), "vgg_fc_w4")
+
+
+def vgg_orthogonalize_workspace_bytes(dtype, batch, rows, cols) -> int:
+    return lib().vgg_orthogonalize_workspace_bytes(dtype, batch, rows, cols)
+
+
+def vgg_orthogonalize(dtype, batch, rows, cols, steps, x, y, ws):
+    _chk(lib().vgg_orthogonalize(dtype, batch, rows, cols, steps, _ptr(x), _ptr(y), _ptr(ws), _nbytes(ws), _stream()),
+         "vgg_orthogonalize")
+
+
+def vgg_muon_workspace_bytes(dtype, batch, rows, cols) -> int:
+    return lib().vgg_muon_workspace_bytes(dtype, batch, rows, cols)
+
+
+def vgg_muon_update(dtype, batch, rows, cols, steps, theta, grad, momentum, lr, mu, nesterov, weight_decay, ws):
+    _chk(lib().vgg_muon_update(dtype, batch, rows, cols, steps, _ptr(theta), _ptr(grad), _ptr(momentum), float(lr), float(mu),
+                               int(nesterov), float(weight_decay), _ptr(ws), _nbytes(ws), _stream()), "vgg_muon_update")
 
 
 # ------------------------------------------------------------- whole model

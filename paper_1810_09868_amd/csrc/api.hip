@@ -74,6 +74,21 @@ size_t fc_bwd_bf16_workspace(int N, int In, int Out);
 int fc_backward_bf16(int N, int In, int Out, const bf16_t *a, const bf16_t *w, const float *dz, float *dw, float *db, float *da,
                      int relu_mask, void *ws, hipStream_t s, float lr = 0.f, bf16_t *copy = nullptr);
 
+int log_probs(int dtype, int N, int K, size_t ldz, const void *z, const int32_t *labels, int top, float *logp, float *entropy,
+              float *top_logp, int32_t *top_idx, float *stats, void *ws, hipStream_t s);
+size_t log_probs_workspace(int N, int K, int top);
+int log_probs_bwd(int dtype, int N, int K, size_t ldz, const void *z, const int32_t *labels, const float *stats, const float *entropy,
+                  const float *g_logp, const float *g_entropy, void *dz, size_t lddz, hipStream_t s);
+int w4_quantize(int In, int Out, int group, const float *w, uint8_t *codes, bf16_t *scales, hipStream_t s);
+int w4_dequantize(int In, int Out, int group, const uint8_t *codes, const bf16_t *scales, float *w, hipStream_t s);
+size_t fc_w4_workspace(int dtype, int N, int In, int Out, int group);
+int fc_w4(int dtype, int N, int In, int Out, int group, const void *a, const uint8_t *codes, const bf16_t *scales, const float *bias, void *z,
+          int z_dtype, int relu, void *ws, hipStream_t s);
+size_t muon_workspace(int dtype, int batch, int rows, int cols);
+int orthogonalize(int dtype, int batch, int rows, int cols, int steps, const void *x, void *y, void *ws, hipStream_t s);
+int muon_update(int dtype, int batch, int rows, int cols, int steps, float *theta, const float *grad, float *momentum, float lr, float mu,
+                int nesterov, float weight_decay, void *ws, hipStream_t s);
+
 namespace {
 
 const int kConvCh[VGG19_NUM_CONV][2] = {{3, 64},    {64, 64},   {64, 128},  {128, 128}, {128, 256}, {256, 256},
@@ -486,6 +501,24 @@ bool params_aligned(const vgg19_params *p)
     return true;
 }
 
+bool scores_shape_ok(int N, int K, size_t ld) { return N > 0 && N <= (1 << 23) && K > 0 && ld >= (size_t)K; }
+bool w4_shape_ok(int In, int Out, int group)
+{
+    return In > 0 && Out > 0 && In <= (1 << 24) && (long)In * Out <= (1L << 33) && (group == 32 || group == 64 || group == 128);
+}
+bool muon_shape_ok(int batch, int rows, int cols)
+{
+    return batch > 0 && batch <= 65535 && rows > 0 && cols > 0 && rows <= (1 << 22) && cols <= (1 << 22) && (rows <= 32768 || cols <= 32768);
+}
+// What the two entry points around the Newton-Schulz products ask of their arguments in common.
+int muon_refusal(int dtype, int batch, int rows, int cols, int steps, const void *ws, size_t ws_bytes)
+{
+    if (!dtype_ok(dtype)) return VGG_ERR_DTYPE;
+    if (!muon_shape_ok(batch, rows, cols) || steps < 1 || steps > 20) return VGG_ERR_SHAPE;
+    if (!ws || ws_bytes < muon_workspace(dtype, batch, rows, cols)) return VGG_ERR_WORKSPACE;
+    return aligned16(ws) ? VGG_OK : VGG_ERR_ALIGN;
+}
+
 bool conv_shape_ok(int N, int H, int W, int Cin, int Cout)
 {
     return N > 0 && H > 0 && W > 0 && Cin > 0 && Cout > 0 && (long)N * H * W <= (1L << 27) &&
@@ -830,6 +863,94 @@ int vgg_sgd_update(size_t n, float *theta, const float *grad, float lr, void *st
     if (n == 0) return VGG_ERR_SHAPE;
     if (!aligned16(theta) || !aligned16(grad)) return VGG_ERR_ALIGN;
     return sgd_update(n, theta, grad, lr, (hipStream_t)stream);
+}
+
+size_t vgg_log_probs_workspace_bytes(int dtype, int N, int K, int top)
+{
+    if (!dtype_ok(dtype) || !scores_shape_ok(N, K, K) || top < 0 || top > VGG_MAX_TOP || top > K) return 0;
+    return log_probs_workspace(N, K, top);
+}
+
+int vgg_log_probs(int dtype, int N, int K, size_t ldz, const void *z, const int32_t *labels, int top, float *logp, float *entropy,
+                  float *top_logp, int32_t *top_idx, float *stats, void *ws, size_t ws_bytes, void *stream)
+{
+    if (!z || !labels != !logp || (top > 0) != !!top_logp || (top > 0) != !!top_idx || (!logp && !entropy && !top_logp && !stats)) return VGG_ERR_NULL;
+    if (!dtype_ok(dtype)) return VGG_ERR_DTYPE;
+    if (!scores_shape_ok(N, K, ldz) || top < 0 || top > VGG_MAX_TOP || top > K) return VGG_ERR_SHAPE;
+    if (!aligned16(z) || !aligned16(labels) || !aligned16(logp) || !aligned16(entropy) || !aligned16(top_logp) || !aligned16(top_idx) || !aligned16(stats) || !aligned16(ws))
+        return VGG_ERR_ALIGN;
+    const size_t need = log_probs_workspace(N, K, top);
+    if (need && (!ws || ws_bytes < need)) return VGG_ERR_WORKSPACE;
+    return log_probs(dtype, N, K, ldz, z, labels, top, logp, entropy, top_logp, top_idx, stats, ws, (hipStream_t)stream);
+}
+
+int vgg_log_probs_bwd(int dtype, int N, int K, size_t ldz, const void *z, const int32_t *labels, const float *stats, const float *entropy,
+                      const float *g_logp, const float *g_entropy, void *dz, size_t lddz, void *stream)
+{
+    if (!z || !stats || !dz || (!g_logp && !g_entropy) || (g_logp && !labels) || (g_entropy && !entropy)) return VGG_ERR_NULL;
+    if (!dtype_ok(dtype)) return VGG_ERR_DTYPE;
+    if (!scores_shape_ok(N, K, ldz) || lddz < (size_t)K || (z == dz && ldz != lddz)) return VGG_ERR_SHAPE;
+    if (!aligned16(z) || !aligned16(labels) || !aligned16(stats) || !aligned16(entropy) || !aligned16(g_logp) || !aligned16(g_entropy) || !aligned16(dz))
+        return VGG_ERR_ALIGN;
+    return log_probs_bwd(dtype, N, K, ldz, z, labels, stats, entropy, g_logp, g_entropy, dz, lddz, (hipStream_t)stream);
+}
+
+int vgg_fc_w4_quantize(int In, int Out, int group, const float *w, uint8_t *codes, uint16_t *scales, void *stream)
+{
+    if (!w || !codes || !scales) return VGG_ERR_NULL;
+    if (!w4_shape_ok(In, Out, group)) return VGG_ERR_SHAPE;
+    if (!aligned16(w) || !aligned16(codes) || !aligned16(scales)) return VGG_ERR_ALIGN;
+    return w4_quantize(In, Out, group, w, codes, scales, (hipStream_t)stream);
+}
+
+int vgg_fc_w4_dequantize(int In, int Out, int group, const uint8_t *codes, const uint16_t *scales, float *w, void *stream)
+{
+    if (!w || !codes || !scales) return VGG_ERR_NULL;
+    if (!w4_shape_ok(In, Out, group)) return VGG_ERR_SHAPE;
+    if (!aligned16(w) || !aligned16(codes) || !aligned16(scales)) return VGG_ERR_ALIGN;
+    return w4_dequantize(In, Out, group, codes, scales, w, (hipStream_t)stream);
+}
+
+size_t vgg_fc_w4_workspace_bytes(int dtype, int N, int In, int Out, int group)
+{
+    if (!dtype_ok(dtype) || N <= 0 || !w4_shape_ok(In, Out, group)) return 0;
+    return fc_w4_workspace(dtype, N, In, Out, group);
+}
+
+int vgg_fc_w4(int dtype, int N, int In, int Out, int group, const void *a, const uint8_t *codes, const uint16_t *scales, const float *bias,
+              void *z, int z_dtype, int relu, void *ws, size_t ws_bytes, void *stream)
+{
+    if (!a || !codes || !scales || !z) return VGG_ERR_NULL;
+    if (!dtype_ok(dtype) || !dtype_ok(z_dtype)) return VGG_ERR_DTYPE;
+    if (N <= 0 || !w4_shape_ok(In, Out, group) || (long)N * In > (1L << 33) || (long)N * Out > (1L << 33)) return VGG_ERR_SHAPE;
+    if (!aligned16(a) || !aligned16(codes) || !aligned16(scales) || !aligned16(bias) || !aligned16(z) || !aligned16(ws)) return VGG_ERR_ALIGN;
+    const size_t need = fc_w4_workspace(dtype, N, In, Out, group);
+    if (need && (!ws || ws_bytes < need)) return VGG_ERR_WORKSPACE;
+    return fc_w4(dtype, N, In, Out, group, a, codes, scales, bias, z, z_dtype, relu ? 1 : 0, ws, (hipStream_t)stream);
+}
+
+size_t vgg_orthogonalize_workspace_bytes(int dtype, int batch, int rows, int cols)
+{
+    return dtype_ok(dtype) && muon_shape_ok(batch, rows, cols) ? muon_workspace(dtype, batch, rows, cols) : 0;
+}
+
+int vgg_orthogonalize(int dtype, int batch, int rows, int cols, int steps, const void *x, void *y, void *ws, size_t ws_bytes, void *stream)
+{
+    if (!x || !y) return VGG_ERR_NULL;
+    if (const int rc = muon_refusal(dtype, batch, rows, cols, steps, ws, ws_bytes)) return rc;
+    if (!aligned16(x) || !aligned16(y)) return VGG_ERR_ALIGN;
+    return orthogonalize(dtype, batch, rows, cols, steps, x, y, ws, (hipStream_t)stream);
+}
+
+size_t vgg_muon_workspace_bytes(int dtype, int batch, int rows, int cols) { return vgg_orthogonalize_workspace_bytes(dtype, batch, rows, cols); }
+
+int vgg_muon_update(int dtype, int batch, int rows, int cols, int steps, float *theta, const float *grad, float *momentum, float lr, float mu,
+                    int nesterov, float weight_decay, void *ws, size_t ws_bytes, void *stream)
+{
+    if (!theta || !grad || !momentum) return VGG_ERR_NULL;
+    if (const int rc = muon_refusal(dtype, batch, rows, cols, steps, ws, ws_bytes)) return rc;
+    if (!aligned16(theta) || !aligned16(grad) || !aligned16(momentum)) return VGG_ERR_ALIGN;
+    return muon_update(dtype, batch, rows, cols, steps, theta, grad, momentum, lr, mu, nesterov ? 1 : 0, weight_decay, ws, (hipStream_t)stream);
 }
 
 size_t vgg19_packed_bytes(const vgg_config *cfg) { return cfg_ok(cfg) ? packed_total(cfg) : 0; }
