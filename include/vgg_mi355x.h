@@ -356,7 +356,7 @@ int vgg_fc_w4_quantize(int In, int Out, int group, const float *w, uint8_t *code
 int vgg_fc_w4_dequantize(int In, int Out, int group, const uint8_t *codes, const uint16_t *scales, float *w, void *stream);
 /* vgg_fc with such weights: z[n,o] = f(bias[o] + sum_i w[o,i] a[n,i]), a
  * [N][In] in `dtype` (rows densely packed), z [N][Out] in z_dtype, bias fp32
- * or NULL.  Any N, In, Out > 0.  Weights are never rounded further: products
+ * or NULL.  Any N, Out > 0, 0 < In <= 2^22.  Weights are never rounded further: products
  * of code values and activations (fp32 ones to 2^-24) are summed in fp32
  * group by group, and a group's sum is multiplied by its scale. */
 size_t vgg_fc_w4_workspace_bytes(int dtype, int N, int In, int Out, int group);
