@@ -504,7 +504,7 @@ bool params_aligned(const vgg19_params *p)
 bool scores_shape_ok(int N, int K, size_t ld) { return N > 0 && N <= (1 << 23) && K > 0 && ld >= (size_t)K; }
 bool w4_shape_ok(int In, int Out, int group)
 {
-    return In > 0 && Out > 0 && In <= (1 << 22) && (long)In * Out <= (1L << 33) && (group == 32 || group == 64 || group == 128);
+    return In > 0 && Out > 0 && In <= (1 << 22) && (long)((In + 127) / 128 * 128) * Out <= (1L << 33) && (group == 32 || group == 64 || group == 128);
 }
 bool muon_shape_ok(int batch, int rows, int cols)
 {

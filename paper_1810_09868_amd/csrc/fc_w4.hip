@@ -24,61 +24,7 @@ __device__ __forceinline__ unsigned code_of(float w, float s)
     return c | (w < 0.f ? 8u : 0u);
 }
 
-// A lane takes 32 inputs of a group (or what the row has of them): G lanes to a group.
-template <int G>
-__global__ __launch_bounds__(256) void w4_quantize_kernel(const float *__restrict__ w, uint8_t *__restrict__ codes, bf16_t *__restrict__ scales,
-                                                          int In, int Out, int blocks, int groups, size_t units)
-{
-    const size_t u = (size_t)blockIdx.x * 256 + threadIdx.x;
-    const size_t row = u / (unsigned)(groups * G);
-    const int b = (int)(u - row * (unsigned)(groups * G)), i0 = b * 32;
-    const bool there = u < units && i0 < In;
-    const int n = !there ? 0 : In - i0 < 32 ? In - i0 : 32;
-    const float *src = w + row * In + i0;
-    float v[32];
-    float most = 0.f;
-    bool bad = false;
-#pragma unroll
-    for (int j = 0; j < 32; ++j) {
-        v[j] = j < n ? src[j] : 0.f;
-        most = fmaxf(most, __builtin_fabsf(v[j]));
-        bad = bad || !(__builtin_fabsf(v[j]) < INFINITY);
-    }
-    if (bad) most = INFINITY;
-#pragma unroll
-    for (int o = 1; o < G; o <<= 1) most = fmaxf(most, __shfl_xor(most, o));
-    const bf16_t sb = most < INFINITY ? f32_to_bf16(most * (1.f / 6.f)) : (bf16_t)0x7fc0;
-    const float s = bf16_to_f32(sb);
-    if (!there) return;
-    u32x4 q;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        unsigned x = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x |= code_of(v[8 * k + j], s) << (4 * j);
-        q[k] = x;
-    }
-    reinterpret_cast<u32x4 *>(codes)[row * blocks + b] = q;
-    if (b % G == 0) scales[row * groups + b / G] = sb;
-}
-
-__device__ __forceinline__ float value_of(unsigned code)
-{
-    const float mag = code & 4u ? (float)(2u + (code & 1u)) * (code & 2u ? 2.f : 1.f) : 0.5f * (float)(code & 3u);
-    return code & 8u ? -mag : mag;
-}
-__global__ __launch_bounds__(256) void w4_dequantize_kernel(const uint8_t *__restrict__ codes, const bf16_t *__restrict__ scales, float *__restrict__ w,
-                                                            int In, int ld, int shift, int groups, int chunks)
-{
-    const size_t row = blockIdx.x / (unsigned)chunks;
-    const int i = (int)(blockIdx.x - row * (unsigned)chunks) * 256 + threadIdx.x;
-    if (i >= In) return;
-    const unsigned byte = codes[row * ld + i / 2];
-    w[row * In + i] = value_of(i & 1 ? byte >> 4 : byte & 15u) * bf16_to_f32(scales[row * groups + (i >> shift)]);
-}
-
-// ------------------------------------------------------------------------------------------------- product
-// 16 bytes from an address that is a multiple of an element's size only.
+// 16 bytes from or to an address that is a multiple of an element's size only.
 struct __attribute__((packed, aligned(2))) Loose16 { unsigned v[4]; };
 __device__ __forceinline__ u32x4 loose16(const void *p)
 {
@@ -86,6 +32,74 @@ __device__ __forceinline__ u32x4 loose16(const void *p)
     return u32x4{l.v[0], l.v[1], l.v[2], l.v[3]};
 }
 
+// A lane takes eight inputs: two loads of 16 bytes, one store of its eight codes.  2^shift / 8 lanes share a group, all in one wave.
+// `units`: lanes of a row, whole groups.
+__global__ __launch_bounds__(256) void w4_quantize_kernel(const float *__restrict__ w, uint8_t *__restrict__ codes, bf16_t *__restrict__ scales,
+                                                          int In, int blocks, int groups, int shift, unsigned units, unsigned all)
+{
+    const unsigned u = blockIdx.x * 256 + threadIdx.x;
+    if (u >= all) return;                              // (whole groups: no lane of one that goes on)
+    const unsigned row = u / units, i0 = (u - row * units) * 8;
+    const float *src = w + (size_t)row * In + i0;
+    const int n = In - (int)i0;
+    float v[8];
+    if (n >= 8) {
+        const u32x4 lo = loose16(src), hi = loose16(src + 4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { const unsigned a = lo[j], b = hi[j]; v[j] = __uint_as_float(a); v[4 + j] = __uint_as_float(b); }
+    } else
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = j < n ? src[j] : 0.f;
+    float most = 0.f;
+    bool bad = false;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        most = fmaxf(most, __builtin_fabsf(v[j]));
+        bad = bad || !(__builtin_fabsf(v[j]) < INFINITY);
+    }
+    if (bad) most = INFINITY;
+    most = fmaxf(most, __shfl_xor(most, 1));
+    most = fmaxf(most, __shfl_xor(most, 2));
+    if (shift > 5) most = fmaxf(most, __shfl_xor(most, 4));
+    if (shift > 6) most = fmaxf(most, __shfl_xor(most, 8));
+    const bf16_t sb = most < INFINITY ? f32_to_bf16(most * (1.f / 6.f)) : (bf16_t)0x7fc0;
+    const float s = bf16_to_f32(sb);
+    unsigned x = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x |= code_of(v[j], s) << (4 * j);
+    if ((int)(i0 >> 5) < blocks) reinterpret_cast<unsigned *>(codes)[(size_t)row * blocks * 4 + (i0 >> 3)] = x;
+    if ((i0 & ((1u << shift) - 1)) == 0) scales[(size_t)row * groups + (i0 >> shift)] = sb;
+}
+
+// A lane: eight codes to 32 bytes of values.
+__global__ __launch_bounds__(256) void w4_dequantize_kernel(const uint8_t *__restrict__ codes, const bf16_t *__restrict__ scales, float *__restrict__ w,
+                                                            int In, int blocks, int groups, int shift, unsigned units, unsigned all)
+{
+    const unsigned u = blockIdx.x * 256 + threadIdx.x;
+    if (u >= all) return;
+    const unsigned row = u / units, i0 = (u - row * units) * 8;
+    const int n = In - (int)i0;
+    if (n <= 0) return;
+    const unsigned q = reinterpret_cast<const unsigned *>(codes)[(size_t)row * blocks * 4 + (i0 >> 3)];
+    const float s = bf16_to_f32(scales[(size_t)row * groups + (i0 >> shift)]);
+    const f32x2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.f, 1),
+                        __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, 1.f, 3)};
+    float *to = w + (size_t)row * In + i0;
+    if (n >= 8) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            Loose16 o;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o.v[j] = __float_as_uint(s * v[2 * k + j / 2][j & 1]);
+            *reinterpret_cast<Loose16 *>(to + 4 * k) = o;
+        }
+    } else
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < n) to[j] = s * v[j / 2][j & 1];
+}
+
+// ------------------------------------------------------------------------------------------------- product
 // Codes stand for 2^-10 of their values in products, so that no sum of 128 of them with activations overflows where the result,
 // which the scales bring down, does not.
 constexpr float kSmall = 1.f / 1024.f, kLarge = 1024.f;
@@ -118,114 +132,142 @@ __device__ __forceinline__ void store_z(const W4Args &p, int n, int o, float v)
     else static_cast<float *>(p.z)[at] = v;
 }
 
-// A few rows of a.  A lane keeps 32 consecutive inputs of each row of a in registers and meets them with R outputs' codes, 16
-// bytes a load, 2^logl lanes side by side along an output's row; the waves of a workgroup take the row's further slices, and LDS
-// adds up what they find.  Every code is read once and nothing else is read more than once a workgroup.
-template <int NV> constexpr int kRowWaves = NV == 1 ? 16 : 8;   // of a workgroup at most: registers
-template <typename T, int NV, int R>
-__global__ __launch_bounds__(kRowWaves<NV> * 64) void fc_w4_rows_kernel(const T *__restrict__ a, W4Args p, int logl)
+// Sums of 16 lanes, in each of them.
+__device__ __forceinline__ float row16_sum(float v)
 {
-    extern __shared__ __align__(16) float sums[];     // [waves][outputs][NV]
+    auto ror = [](float x, auto n) __attribute__((always_inline)) {
+        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + decltype(n)::value, 0xf, 0xf, true));
+    };
+    v += ror(v, std::integral_constant<int, 8>{});
+    v += ror(v, std::integral_constant<int, 4>{});
+    v += ror(v, std::integral_constant<int, 2>{});
+    return v + ror(v, std::integral_constant<int, 1>{});
+}
+// Sums of 64 lanes each of four values, value i in the lanes 16 i...  (Halves and quarters of two values change places and are
+// added, so that every addition works on all lanes.)
+__device__ __forceinline__ float sum_lanes4(const float (&v)[4])
+{
+    float h[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[k]), __float_as_uint(v[k + 2]), false, false);
+        h[k] = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+    }
+    const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(h[0]), __float_as_uint(h[1]), false, false);
+    return row16_sum(__uint_as_float(s[0]) + __uint_as_float(s[1]));
+}
+
+// One row of a.  A lane keeps 32 consecutive inputs in registers and meets them with the codes of four outputs at a time (one or
+// 64 / 2^logl of them a load, 16 bytes a lane), while the next four's are on their way; the waves of a workgroup take the row's
+// further slices, and LDS adds up what they find.  Every code is read once, in runs of up to 1 KB.
+constexpr int kBatch = 4, kRowWaves = 16;
+template <typename T>
+__global__ __launch_bounds__(kRowWaves * 64) void fc_w4_row_kernel(const T *__restrict__ a_rows, W4Args p, int logl, int batches)
+{
+    extern __shared__ __align__(16) float sums[];     // [batches][waves][outputs of a batch]
+    const T *a = a_rows + (size_t)blockIdx.y * p.In;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     const int L = 1 << logl, per = 64 >> logl, mine = lane & (L - 1), sub = lane >> logl;
-    const int n0 = blockIdx.y * NV, o0 = blockIdx.x * (R * per);
-    float acc[R][NV] = {};
-    for (int b = wave * L + mine; b - mine < p.blocks; b += waves * L) {
-        const bool there = b < p.blocks;
-        u32x4 q[R];
-        bf16_t sc[R];
+    const int some = kBatch * per, o0 = blockIdx.x * batches * some;
+    const int slices = (p.blocks + waves * L - 1) / (waves * L);
+    if (batches > (p.Out - o0 + some - 1) / some) batches = (p.Out - o0 + some - 1) / some;
+    const char *qbase = reinterpret_cast<const char *>(p.codes) + (size_t)o0 * p.blocks * 16;
+    const char *sbase = reinterpret_cast<const char *>(p.scales) + (size_t)o0 * p.groups * 2;
+
+    for (int slice = 0; slice < slices; ++slice) {
+        const int b = (slice * waves + wave) * L + mine, left = p.In - b * 32, bc = left > 0 ? b : p.blocks - 1;
+        const unsigned grp = (unsigned)(bc * 32) >> p.shift;
+        struct Weights { u32x4 q[kBatch]; bf16_t sc[kBatch]; };
+        auto fetch = [&](int batch, Weights &w) __attribute__((always_inline)) {
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const int o = o0 + r * per + sub;
-            const bool ok = there && o < p.Out;
-            q[r] = ok ? reinterpret_cast<const u32x4 *>(p.codes)[(size_t)o * p.blocks + b] : u32x4{0, 0, 0, 0};
-            sc[r] = ok ? p.scales[(size_t)o * p.groups + (b * 32 >> p.shift)] : (bf16_t)0;
-        }
-        const int left = there ? p.In - b * 32 : 0;
-        if constexpr (sizeof(T) == 2) {
-            u32x4 x[NV][4];
-#pragma unroll
-            for (int n = 0; n < NV; ++n) {
-                const T *xr = a + (size_t)(n0 + n < p.N ? n0 + n : p.N - 1) * p.In + (size_t)b * 32;
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if (left >= 8 * k + 8) x[n][k] = loose16(xr + 8 * k);
-                    else {
-                        unsigned short e[8];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) e[j] = 8 * k + j < left ? xr[8 * k + j] : (unsigned short)0;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) x[n][k][j] = e[2 * j] | (unsigned)e[2 * j + 1] << 16;
-                    }
-                }
+            for (int r = 0; r < kBatch; ++r) {
+                int o = batch * some + r * per + sub;
+                if (o >= p.Out - o0) o = p.Out - 1 - o0;
+                w.q[r] = *reinterpret_cast<const u32x4 *>(qbase + ((unsigned)o * p.blocks + bc) * 16u);
+                w.sc[r] = *reinterpret_cast<const bf16_t *>(sbase + ((unsigned)o * p.groups + grp) * 2u);
             }
+        };
+        Weights w0;
+        fetch(0, w0);
+        constexpr int X = sizeof(T) == 2 ? 4 : 8, E = 16 / (int)sizeof(T);   // 16-byte pieces of 32 inputs, inputs of a piece
+        u32x4 x[X];
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                float part[NV] = {};
+        for (int k = 0; k < X; ++k) {
+            const T *xr = a + (size_t)b * 32 + E * k;
+            if (left >= E * k + E) x[k] = loose16(xr);
+            else {
+                T e[E];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const u32x4 w = bf16_values(q[r][k]);
+                for (int j = 0; j < E; ++j) e[j] = E * k + j < left ? xr[j] : (T)0;
+                u32x4 v;
+                __builtin_memcpy(&v, e, sizeof v);
+                x[k] = v;
+            }
+        }
+        auto multiply = [&](const Weights &w, int batch) __attribute__((always_inline)) {
+            float acc[kBatch];
 #pragma unroll
-                    for (int n = 0; n < NV; ++n)
+            for (int r = 0; r < kBatch; ++r) {
+                float part[2] = {};
+                if constexpr (sizeof(T) == 2) {
+                    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const u32x4 c = bf16_values(w.q[r][k]);
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-                            const unsigned wj = w[j], xj = x[n][k][j];   // (a vector's element is not to be reinterpreted in place)
-                            part[n] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, wj), __builtin_bit_cast(bf16x2, xj), part[n], false);
+                            const unsigned cj = c[j], xj = x[k][j];   // (a vector's element is not to be reinterpreted in place)
+                            part[j & 1] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, cj), __builtin_bit_cast(bf16x2, xj), part[j & 1], false);
                         }
+                    }
+                } else {
+                    auto pair = [&](f32x2 c, int at) __attribute__((always_inline)) {
+                        const unsigned x0 = x[at >> 2][at & 3], x1 = x[at >> 2][(at & 3) + 1];
+                        part[0] = __builtin_fmaf(c[0], __uint_as_float(x0), part[0]);
+                        part[1] = __builtin_fmaf(c[1], __uint_as_float(x1), part[1]);
+                    };
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        pair(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.q[r][k], kSmall, 0), 8 * k);
+                        pair(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.q[r][k], kSmall, 1), 8 * k + 2);
+                        pair(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.q[r][k], kSmall, 2), 8 * k + 4);
+                        pair(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w.q[r][k], kSmall, 3), 8 * k + 6);
+                    }
                 }
-#pragma unroll
-                for (int n = 0; n < NV; ++n) acc[r][n] = __builtin_fmaf(bf16_to_f32(sc[r]), part[n], acc[r][n]);
+                acc[r] = (left > 0 ? bf16_to_f32(w.sc[r]) : 0.f) * (part[0] + part[1]);
             }
-        } else {
-            float x[NV][32];
+            float *to = sums + (batch * waves + wave) * some;
+            if (logl == 6) {
+                const float v = sum_lanes4(acc);
+                if ((lane & 15) == 0) to[lane >> 4] = slice ? to[lane >> 4] + v : v;
+            } else {
 #pragma unroll
-            for (int n = 0; n < NV; ++n) {
-                const T *xr = a + (size_t)(n0 + n < p.N ? n0 + n : p.N - 1) * p.In + (size_t)b * 32;
+                for (int o = 16; o > 0; o >>= 1)
+                    if (o < L)
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    if (left >= 4 * k + 4) {
-                        const u32x4 v = loose16(xr + 4 * k);
+                        for (int r = 0; r < kBatch; ++r) acc[r] += __shfl_xor(acc[r], o, kWave);
+                if (mine == 0)
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) x[n][4 * k + j] = __uint_as_float(v[j]);
-                    } else
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) x[n][4 * k + j] = 4 * k + j < left ? (float)xr[4 * k + j] : 0.f;
-                }
+                    for (int r = 0; r < kBatch; ++r) to[r * per + sub] = slice ? to[r * per + sub] + acc[r] : acc[r];
             }
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                float part[NV] = {};
-                auto pair = [&](f32x2 w, int at) __attribute__((always_inline)) {
-#pragma unroll
-                    for (int n = 0; n < NV; ++n) part[n] = __builtin_fmaf(w[1], x[n][at + 1], __builtin_fmaf(w[0], x[n][at], part[n]));
-                };
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    pair(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q[r][k], kSmall, 0), 8 * k);
-                    pair(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q[r][k], kSmall, 1), 8 * k + 2);
-                    pair(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q[r][k], kSmall, 2), 8 * k + 4);
-                    pair(__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q[r][k], kSmall, 3), 8 * k + 6);
-                }
-#pragma unroll
-                for (int n = 0; n < NV; ++n) acc[r][n] = __builtin_fmaf(bf16_to_f32(sc[r]), part[n], acc[r][n]);
-            }
+        };
+        Weights w1;
+        for (int batch = 0; batch < batches; batch += 2) {
+            if (batch + 1 < batches) fetch(batch + 1, w1);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(w0, batch);
+            if (batch + 1 == batches) break;
+            if (batch + 2 < batches) fetch(batch + 2, w0);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(w1, batch + 1);
         }
     }
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int n = 0; n < NV; ++n) {
-            float v = acc[r][n];
-            for (int o = L >> 1; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
-            if (mine == 0) sums[(wave * (R * per) + r * per + sub) * NV + n] = v;
-        }
     __syncthreads();
-    for (int i = threadIdx.x; i < R * per * NV; i += blockDim.x) {
+    for (int i = threadIdx.x; i < batches * some; i += blockDim.x) {
+        const int batch = i / some, at = i - batch * some;
         float v = 0.f;
-        for (int w = 0; w < waves; ++w) v += sums[w * (R * per * NV) + i];
-        const int o = o0 + i / NV, n = n0 + i % NV;
-        if (o < p.Out && n < p.N) store_z(p, n, o, v);
+        for (int w = 0; w < waves; ++w) v += sums[(batch * waves + w) * some + at];
+        if (o0 + i < p.Out) store_z(p, blockIdx.y, o0 + i, v);
     }
 }
 
@@ -266,138 +308,244 @@ __device__ __forceinline__ Parts8 parts_of_any(const float (&x)[8])
     return o;
 }
 
-// Many rows of a, on the matrix unit (16 x 16 x 32, bf16): rows of a times 16 RT outputs a wave, NT tiles of 16 rows; the waves of
-// a workgroup take every W-th 128 inputs and LDS adds them up.  A lane loads 32 codes of one output; the four lanes of an output
-// then exchange them (permlane swaps), so that one instruction's 32 inputs are of one group and its sum can take the group's
-// scale: an output is a column of the result, so that a lane's four sums share it.
-template <typename T, int RT, int NT, int W, int G>
-__global__ __launch_bounds__(W * 64) void fc_w4_tiles_kernel(const T *__restrict__ a, W4Args p)
+// More rows, on the matrix unit (16 x 16 x 32, bf16): rows of a times outputs, an output a column of the result, so that a lane's
+// four sums share its scales.  A lane loads 32 codes of one output; the four lanes of an output then exchange them (permlane
+// swaps), so that one instruction's 32 inputs are of one group: dword j of lane group g, codes 8j.. of block g, becomes codes 8g..
+// of block j.
+__device__ __forceinline__ void spread_codes(const u32x4 &q, u32x4 (&w)[4])
+{
+    const auto s02 = __builtin_amdgcn_permlane32_swap(q[0], q[2], false, false);
+    const auto s13 = __builtin_amdgcn_permlane32_swap(q[1], q[3], false, false);
+    const auto s01 = __builtin_amdgcn_permlane16_swap(s02[0], s13[0], false, false);
+    const auto s23 = __builtin_amdgcn_permlane16_swap(s02[1], s13[1], false, false);
+    w[0] = bf16_values(s01[0]);
+    w[1] = bf16_values(s01[1]);
+    w[2] = bf16_values(s23[0]);
+    w[3] = bf16_values(s23[1]);
+}
+// The scales of 128 inputs of one output, S of them, as loaded.
+template <int S> struct Scales { unsigned v[(S + 1) / 2]; };
+template <int S> __device__ __forceinline__ Scales<S> load_scales(const bf16_t *src, int left)
+{
+    Scales<S> o;
+    struct __attribute__((packed, aligned(2))) Loose { unsigned v[(S + 1) / 2]; };
+    if (S == 1) o.v[0] = src[0];
+    else if (left >= S) {
+        const Loose l = *reinterpret_cast<const Loose *>(src);
+#pragma unroll
+        for (int i = 0; i < (S + 1) / 2; ++i) o.v[i] = l.v[i];
+    } else
+#pragma unroll
+        for (int i = 0; i < (S + 1) / 2; ++i) o.v[i] = (2 * i < left ? src[2 * i] : 0u) | (2 * i + 1 < left ? (unsigned)src[2 * i + 1] << 16 : 0u);
+    return o;
+}
+template <int S> __device__ __forceinline__ float scale_of(const Scales<S> &s, int i) { return bf16_to_f32((bf16_t)(s.v[i >> 1] >> 16 * (i & 1))); }
+__device__ __forceinline__ f32x4 mfma(const u32x4 &x, const u32x4 &w, f32x4 acc)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, w), acc, 0, 0, 0);
+}
+
+// Up to 16 rows: 16 outputs to a workgroup, whose W waves take every W-th 128 inputs, the next ones' codes, scales and activations
+// on their way, and add up in LDS.
+template <typename T, int W, int G>
+__global__ __launch_bounds__(W * 64) void fc_w4_tile_kernel(const T *__restrict__ a, W4Args p)
+{
+    extern __shared__ __align__(16) f32x4 red[];      // [W][64]
+    constexpr int S = 4 / G;                           // groups of 128 inputs
+    constexpr int Q = sizeof(T) / 2;                   // 16-byte loads of 8 inputs
+    constexpr int P = Q == 1 ? 1 : 3;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
+    const int o0 = blockIdx.x * 16, o = o0 + col < p.Out ? o0 + col : p.Out - 1;
+    const int KB = (p.In + 127) / 128, whole = p.In / 128;
+    const T *xr = a + (size_t)(col < p.N ? col : p.N - 1) * p.In + g * 8;
+    const u32x4 *qr = reinterpret_cast<const u32x4 *>(p.codes) + (size_t)o * p.blocks + g;
+    const bf16_t *sr = p.scales + (size_t)o * p.groups;
+    struct Step { u32x4 q; Scales<S> sc; u32x4 x[4][Q]; };
+    auto fetch = [&](int kb, Step &f) __attribute__((always_inline)) {
+        if (kb < whole) {
+            f.q = qr[(size_t)kb * 4];
+            f.sc = load_scales<S>(sr + (size_t)kb * S, S);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int h = 0; h < Q; ++h) f.x[j][h] = loose16(xr + (size_t)kb * 128 + j * 32 + h * (16 / (int)sizeof(T)));
+            return;
+        }
+        f.q = kb * 4 + g < p.blocks ? qr[(size_t)kb * 4] : u32x4{0, 0, 0, 0};
+        f.sc = load_scales<S>(sr + (size_t)kb * S, p.groups - kb * S);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int left = p.In - (kb * 128 + j * 32 + g * 8);
+            T e[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e[i] = i < left ? xr[(size_t)kb * 128 + j * 32 + i] : (T)0;
+            __builtin_memcpy(f.x[j], e, sizeof e);
+        }
+    };
+    f32x4 total = {0.f, 0.f, 0.f, 0.f};
+    auto multiply = [&](const Step &f) __attribute__((always_inline)) {
+        u32x4 w[4];
+        spread_codes(f.q, w);
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            u32x4 part[P];
+            if constexpr (P == 1) part[0] = f.x[j][0];
+            else {
+                float e[8];
+                __builtin_memcpy(e, f.x[j], sizeof e);
+                const Parts8 o8 = parts_of_any(e);
+#pragma unroll
+                for (int k = 0; k < 3; ++k) part[k] = o8.p[k];
+            }
+#pragma unroll
+            for (int k = P - 1; k >= 0; --k) acc = mfma(part[k], w[j], acc);
+            if ((j + 1) % G == 0) {
+                const float sc = scale_of<S>(f.sc, j / G);
+#pragma unroll
+                for (int v = 0; v < 4; ++v) total[v] = __builtin_fmaf(sc, acc[v], total[v]);
+                acc = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+        }
+    };
+    Step f0, f1;
+    int kb = wave;
+    if (kb < KB) fetch(kb, f0);
+    for (; kb < KB; kb += 2 * W) {
+        if (kb + W < KB) fetch(kb + W, f1);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(f0);
+        if (kb + W >= KB) break;
+        if (kb + 2 * W < KB) fetch(kb + 2 * W, f0);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(f1);
+    }
+    // value v of a lane: row 4 g + v of a, output col
+    red[wave * 64 + lane] = total;
+    __syncthreads();
+    const float *all = reinterpret_cast<const float *>(red);
+    for (int i = threadIdx.x; i < 256; i += W * 64) {
+        const int c = i & 15, row = i >> 4, at = ((row >> 2) * 16 + c) * 4 + (row & 3);   // sixteen threads: outputs of one row
+        float v = 0.f;
+#pragma unroll
+        for (int k = 0; k < W; ++k) v += all[k * 256 + at];
+        if (row < p.N && o0 + c < p.Out) store_z(p, row, o0 + c, v);
+    }
+}
+
+// Activations as the matrix unit takes them: [128 inputs][16 rows][32 inputs][part], 1 KB each, lane l's 16 bytes at 16 l: row
+// l % 16, inputs 8 (l / 16)..; zeros past the last row and input.  fp32 ones in their three parts.
+template <typename T>
+__global__ __launch_bounds__(256) void fc_w4_lay_kernel(const T *__restrict__ a, u32x4 *__restrict__ x, int N, int In, int tiles, unsigned units)
+{
+    const unsigned u = blockIdx.x * 4 + (threadIdx.x >> 6);     // (128 inputs, tile of rows, 32 inputs)
+    if (u >= units) return;
+    const int lane = threadIdx.x & 63, j = u & 3, tile = (u >> 2) % tiles, kb = (u >> 2) / tiles;
+    const int n = tile * 16 + (lane & 15), k = kb * 128 + j * 32 + (lane >> 4) * 8, left = n < N ? In - k : 0;
+    const T *src = a + (size_t)n * In + k;
+    T e[8];
+    if (left >= 8) {
+#pragma unroll
+        for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+            const u32x4 v = loose16(src + h * (16 / (int)sizeof(T)));
+            __builtin_memcpy(e + h * (16 / (int)sizeof(T)), &v, 16);
+        }
+    } else
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = i < left ? src[i] : (T)0;
+    if constexpr (sizeof(T) == 2) {
+        u32x4 v;
+        __builtin_memcpy(&v, e, 16);
+        x[(size_t)u * 64 + lane] = v;
+    } else {
+        const Parts8 o = parts_of_any(e);
+#pragma unroll
+        for (int k3 = 0; k3 < 3; ++k3) x[((size_t)u * 3 + k3) * 64 + lane] = o.p[k3];
+    }
+}
+
+// 16 RT outputs and 16 NT rows to a workgroup, whose eight waves take every eighth 128 inputs of its share and add up in LDS.
+// The next 128 inputs' codes and scales and the next few blocks of activations are on their way.
+template <int P, int RT, int NT, int G>
+__global__ __launch_bounds__(512) void fc_w4_tiles_kernel(const u32x4 *__restrict__ x, W4Args p)
 {
     extern __shared__ __align__(16) f32x4 red[];      // [W][NT][64]
+    constexpr int W = 8, S = 4 / G, F = NT * 4;        // F: blocks of 16 rows x 32 inputs of a step
+    constexpr int AHEAD = P == 1 ? 4 : 2;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
     const int split = blockIdx.x / p.row_tiles, o0 = (blockIdx.x - split * p.row_tiles) * (16 * RT), n0 = blockIdx.y * (16 * NT);
-    const int KB = (p.In + 127) / 128;
+    const int KB = (p.In + 127) / 128, whole = p.In / 128;
     const int kb0 = (int)((long)KB * split / p.splits), kb1 = (int)((long)KB * (split + 1) / p.splits);
+    const int tiles = (p.N + 16 * NT - 1) / (16 * NT) * NT;
     f32x4 total[RT][NT] = {};
 
-    // (32-bit offsets from a base that the wave shares)
-    unsigned xoff[NT], qoff[RT], soff[RT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int n = n0 + t * 16 + col < p.N ? t * 16 + col : p.N - 1 - n0;
-        xoff[t] = ((unsigned)n * (unsigned)p.In + g * 8) * (unsigned)sizeof(T);
-    }
+    unsigned qoff[RT], soff[RT];                       // 32-bit offsets from bases that the wave shares
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         const int o = o0 + r * 16 + col < p.Out ? r * 16 + col : p.Out - 1 - o0;
         qoff[r] = ((unsigned)o * p.blocks + g) * 16u;
         soff[r] = (unsigned)o * p.groups * 2u;
     }
-    const char *xbase = reinterpret_cast<const char *>(a + (size_t)n0 * p.In);
     const char *qbase = reinterpret_cast<const char *>(p.codes) + (size_t)o0 * p.blocks * 16;
     const char *sbase = reinterpret_cast<const char *>(p.scales) + (size_t)o0 * p.groups * 2;
-    constexpr int S = 4 / G;                           // groups of 128 inputs
-    constexpr int Q = sizeof(T) / 2;                   // 16-byte loads of 8 inputs
-    constexpr int P = Q == 1 ? 1 : 3;
-
-    // 128 inputs; FULL: all of them are there
-    auto step = [&](int kb, auto FULL) __attribute__((always_inline)) {
-        constexpr bool full = decltype(FULL)::value;
-        const char *xk = xbase + (size_t)kb * (128 * sizeof(T)), *qk = qbase + (size_t)kb * 64, *sk = sbase + (size_t)kb * (2 * S);
-        u32x4 q[RT];
+    struct Weights { u32x4 q[RT]; Scales<S> sc[RT]; };
+    auto fetch = [&](int kb, Weights &f) __attribute__((always_inline)) {
+        const char *qk = qbase + (size_t)kb * 64, *sk = sbase + (size_t)kb * (2 * S);
+        const bool all = kb < whole;
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            f.q[r] = all || kb * 4 + g < p.blocks ? *reinterpret_cast<const u32x4 *>(qk + qoff[r]) : u32x4{0, 0, 0, 0};
+            f.sc[r] = load_scales<S>(reinterpret_cast<const bf16_t *>(sk + soff[r]), all ? S : p.groups - kb * S);
+        }
+    };
+    // block i of a step (or of the wave's next one)
+    u32x4 ring[AHEAD][P];
+    auto fetch_x = [&](int kb, int i, u32x4 (&f)[P]) __attribute__((always_inline)) {
+        if (i >= F) { i -= F; kb = kb + W < kb1 ? kb + W : kb; }
+        const u32x4 *src = x + ((((size_t)kb * tiles + blockIdx.y * NT) * 4 + i) * P) * 64;
+#pragma unroll
+        for (int k = 0; k < P; ++k) f[k] = src[k * 64 + lane];
+    };
+    Weights f;
+    int kb = kb0 + wave;
+    if (kb < kb1) {
+        fetch(kb, f);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) fetch_x(kb, i, ring[i]);
+    }
+    for (; kb < kb1; kb += W) {
+        u32x4 w[RT][4];
         float sc[RT][S];
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
-            q[r] = full || kb * 4 + g < p.blocks ? *reinterpret_cast<const u32x4 *>(qk + qoff[r]) : u32x4{0, 0, 0, 0};
-            if constexpr (full && S == 4) {
-                struct __attribute__((packed, aligned(2))) L8 { unsigned v[2]; };
-                const L8 v = *reinterpret_cast<const L8 *>(sk + soff[r]);
+            spread_codes(f.q[r], w[r]);
 #pragma unroll
-                for (int i = 0; i < S; ++i) sc[r][i] = bf16_to_f32((bf16_t)(v.v[i >> 1] >> 16 * (i & 1)));
-            } else if constexpr (full && S == 2) {
-                struct __attribute__((packed, aligned(2))) L4 { unsigned v; };
-                const L4 v = *reinterpret_cast<const L4 *>(sk + soff[r]);
-#pragma unroll
-                for (int i = 0; i < S; ++i) sc[r][i] = bf16_to_f32((bf16_t)(v.v >> 16 * (i & 1)));
-            } else
-#pragma unroll
-                for (int i = 0; i < S; ++i) sc[r][i] = kb * S + i < p.groups ? bf16_to_f32(reinterpret_cast<const bf16_t *>(sk + soff[r])[i]) : 0.f;
+            for (int i = 0; i < S; ++i) sc[r][i] = scale_of<S>(f.sc[r], i);
         }
-        // what a tile of 16 rows needs, as loaded: 8 inputs of each of the four blocks
-        auto load_x = [&](int t, u32x4 (&x)[4][Q]) __attribute__((always_inline)) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (kb + W < kb1) fetch(kb + W, f);
+        f32x4 acc[RT];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const T *xr = reinterpret_cast<const T *>(xk + xoff[t]) + j * 32;
-                if constexpr (full) {
+        for (int i = 0; i < F; ++i) {
+            const int j = i & 3, t = i >> 2;
+            u32x4 now[P];
 #pragma unroll
-                    for (int h = 0; h < Q; ++h) x[j][h] = loose16(xr + h * (16 / (int)sizeof(T)));
-                } else {
-                    const int left = p.In - (kb * 128 + j * 32 + g * 8);
-                    T e[8];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) e[i] = i < left ? xr[i] : (T)0;
-                    __builtin_memcpy(x[j], e, sizeof e);
-                }
-            }
-        };
-        u32x4 x[4][Q], next[4][Q];
-        load_x(0, x);
-        u32x4 w[RT][4];
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            // dword j of lane group g: codes 8j.. of block g  ->  codes 8g.. of block j
-            const auto s02 = __builtin_amdgcn_permlane32_swap(q[r][0], q[r][2], false, false);
-            const auto s13 = __builtin_amdgcn_permlane32_swap(q[r][1], q[r][3], false, false);
-            const auto s01 = __builtin_amdgcn_permlane16_swap(s02[0], s13[0], false, false);
-            const auto s23 = __builtin_amdgcn_permlane16_swap(s02[1], s13[1], false, false);
-            w[r][0] = bf16_values(s01[0]);
-            w[r][1] = bf16_values(s01[1]);
-            w[r][2] = bf16_values(s23[0]);
-            w[r][3] = bf16_values(s23[1]);
-        }
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            if (t + 1 < NT) load_x(t + 1, next);
-            if (NT > 1) __builtin_amdgcn_sched_barrier(0);         // (one tile ahead, not all: registers)
-            u32x4 part[4][P];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                if constexpr (P == 1) part[j][0] = x[j][0];
-                else {
-                    float e[8];
-                    __builtin_memcpy(e, x[j], sizeof e);
-                    const Parts8 o = parts_of_any(e);
-#pragma unroll
-                    for (int k = 0; k < 3; ++k) part[j][k] = o.p[k];
-                }
-            }
+            for (int k = 0; k < P; ++k) now[k] = ring[i % AHEAD][k];
+            fetch_x(kb, i + AHEAD, ring[i % AHEAD]);
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+                if (j % G == 0) acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-#pragma unroll
-                    for (int k = P - 1; k >= 0; --k)
-                        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, part[j][k]), __builtin_bit_cast(bf16x8, w[r][j]), acc, 0, 0, 0);
-                    if ((j + 1) % G == 0) {
-#pragma unroll
-                        for (int v = 0; v < 4; ++v) total[r][t][v] = __builtin_fmaf(sc[r][j / G], acc[v], total[r][t][v]);
-                        acc = f32x4{0.f, 0.f, 0.f, 0.f};
-                    }
-                }
-                if (RT > 1 && G < 4) __builtin_amdgcn_sched_barrier(0);   // (every group's sum apart would take its registers)
+                for (int k = P - 1; k >= 0; --k) acc[r] = mfma(now[k], w[r][j], acc[r]);
             }
-            if (NT > 1) __builtin_amdgcn_sched_barrier(0);
+            if ((j + 1) % G == 0)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+                for (int r = 0; r < RT; ++r)
 #pragma unroll
-                for (int h = 0; h < Q; ++h) x[j][h] = next[j][h];
+                    for (int v = 0; v < 4; ++v) total[r][t][v] = __builtin_fmaf(sc[r][j / G], acc[r][v], total[r][t][v]);
+            __builtin_amdgcn_sched_barrier(0);          // (the loads stay where they are issued, and no more of them: registers)
         }
-    };
-    const int whole = p.In / 128;
-    int kb = kb0 + wave;
-    for (; kb < kb1 && kb < whole; kb += W) step(kb, std::true_type{});
-    if (kb < kb1) step(kb, std::false_type{});
+    }
 
     // value v of a lane: row 4 g + v of its tile of a, output col
 #pragma unroll
@@ -438,85 +586,98 @@ inline int shift_of(int group) { return group == 32 ? 5 : group == 64 ? 6 : 7; }
 
 int w4_quantize(int In, int Out, int group, const float *w, uint8_t *codes, bf16_t *scales, hipStream_t s)
 {
-    const int groups = (In + group - 1) / group, blocks = (In + 31) / 32, G = group / 32;
-    const size_t units = (size_t)Out * groups * G;
-    const dim3 grid((unsigned)((units + 255) / 256)), block(256);
-    if (G == 1) hipLaunchKernelGGL(w4_quantize_kernel<1>, grid, block, 0, s, w, codes, scales, In, Out, blocks, groups, units);
-    else if (G == 2) hipLaunchKernelGGL(w4_quantize_kernel<2>, grid, block, 0, s, w, codes, scales, In, Out, blocks, groups, units);
-    else hipLaunchKernelGGL(w4_quantize_kernel<4>, grid, block, 0, s, w, codes, scales, In, Out, blocks, groups, units);
+    const int groups = (In + group - 1) / group;
+    const unsigned units = (unsigned)groups * (group / 8), all = units * (unsigned)Out;
+    hipLaunchKernelGGL(w4_quantize_kernel, dim3((all + 255) / 256), dim3(256), 0, s, w, codes, scales, In, (In + 31) / 32, groups, shift_of(group), units, all);
     return launch_status();
 }
 
 int w4_dequantize(int In, int Out, int group, const uint8_t *codes, const bf16_t *scales, float *w, hipStream_t s)
 {
-    const int chunks = (In + 255) / 256;
-    hipLaunchKernelGGL(w4_dequantize_kernel, dim3((unsigned)chunks * (unsigned)Out), dim3(256), 0, s, codes, scales, w, In, (In + 31) / 32 * 16,
-                       shift_of(group), (In + group - 1) / group, chunks);
+    const unsigned units = (unsigned)(In + 7) / 8, all = units * (unsigned)Out;
+    hipLaunchKernelGGL(w4_dequantize_kernel, dim3((all + 255) / 256), dim3(256), 0, s, codes, scales, w, In, (In + 31) / 32, (In + group - 1) / group,
+                       shift_of(group), units, all);
     return launch_status();
 }
 
 namespace {
 
-constexpr int kFewRows = 4;    // rows of a up to which the first kernel runs
+constexpr int kFewRows = 1;    // rows of a up to which the first kernel runs
 
-struct W4Plan { int rt, nt, splits, row_tiles; };
+// ... and the second: its workgroups of 16 outputs read all of a each, in pieces scattered over its rows, so that long rows are
+// worth laying out first (25088 inputs, bf16: 5 rows 18.2 against 20.7 us, 10 rows 23.5 against 20.8; 4096 inputs, fp32, 16 rows:
+// 11.5 against 11.7).
+constexpr int kTileRows = 16;
+constexpr size_t kTileBytes = 300000;
+
+bool one_tile(int dtype, int N, int In) { return N <= kTileRows && (size_t)N * In * dtype_size(dtype) <= kTileBytes; }
+
+struct W4Plan { int nt, tiles, splits, row_tiles; size_t lay_bytes; };
 W4Plan tiles_plan(int dtype, int N, int In, int Out)
 {
     W4Plan t;
     t.nt = N <= 16 ? 1 : N <= 32 ? 2 : 4;
-    t.rt = t.nt <= 2 ? 1 : dtype == VGG_BF16 ? 4 : 2;
-    t.row_tiles = (Out + 16 * t.rt - 1) / (16 * t.rt);
-    t.splits = 1;
-    if (t.rt > 1) {
-        const int kb = (In + 127) / 128, most = (kb + 7) / 8;
-        const long units = (long)t.row_tiles * ((N + 16 * t.nt - 1) / (16 * t.nt));
-        t.splits = (int)(units >= 256 ? 1 : (256 + units - 1) / units);
-        if (t.splits > most) t.splits = most;
-    }
+    t.tiles = (N + 16 * t.nt - 1) / (16 * t.nt) * t.nt;
+    t.row_tiles = (Out + 63) / 64;
+    const int kb = (In + 127) / 128, most = (kb + 7) / 8;
+    const long units = (long)t.row_tiles * (t.tiles / t.nt);
+    t.splits = (int)(units >= 256 ? 1 : (256 + units - 1) / units);
+    if (t.splits > most) t.splits = most;
+    t.lay_bytes = round_up((size_t)kb * t.tiles * 4 * (dtype == VGG_BF16 ? 1 : 3) * 1024, 256);
     return t;
 }
 
-template <typename T, int RT, int NT, int W, int G>
-int launch_tiles_of(const T *a, const W4Args &p, hipStream_t s)
+template <typename T, int NT, int G>
+int launch_tiles_of(const T *a, W4Args p, const W4Plan &t, void *ws, hipStream_t s)
 {
-    auto kern = fc_w4_tiles_kernel<T, RT, NT, W, G>;
-    const size_t lds = (size_t)W * NT * 1024;
-    hipLaunchKernelGGL(kern, dim3((unsigned)(p.row_tiles * p.splits), (unsigned)((p.N + 16 * NT - 1) / (16 * NT))), dim3(W * 64), lds, s, a, p);
-    if (p.splits > 1) hipLaunchKernelGGL(fc_w4_join_kernel, dim3((unsigned)(((size_t)p.N * p.Out + 255) / 256)), dim3(256), 0, s, p);
+    constexpr int P = sizeof(T) == 2 ? 1 : 3;
+    u32x4 *x = static_cast<u32x4 *>(ws);
+    p.part = reinterpret_cast<float *>(static_cast<char *>(ws) + t.lay_bytes);
+    p.splits = t.splits;
+    p.row_tiles = t.row_tiles;
+    const unsigned units = (unsigned)((p.In + 127) / 128) * t.tiles * 4;
+    hipLaunchKernelGGL(fc_w4_lay_kernel<T>, dim3((units + 3) / 4), dim3(256), 0, s, a, x, p.N, p.In, t.tiles, units);
+    hipLaunchKernelGGL((fc_w4_tiles_kernel<P, 4, NT, G>), dim3((unsigned)(t.row_tiles * t.splits), (unsigned)(t.tiles / NT)), dim3(512), (size_t)8 * NT * 1024, s, x, p);
+    if (t.splits > 1) hipLaunchKernelGGL(fc_w4_join_kernel, dim3((unsigned)(((size_t)p.N * p.Out + 255) / 256)), dim3(256), 0, s, p);
     return launch_status();
 }
-template <typename T, int RT, int NT, int W>
-int launch_tiles(const T *a, const W4Args &p, hipStream_t s)
+template <typename T, int NT>
+int launch_tiles(const T *a, const W4Args &p, const W4Plan &t, void *ws, hipStream_t s)
 {
-    if (p.shift == 5) return launch_tiles_of<T, RT, NT, W, 1>(a, p, s);
-    if (p.shift == 6) return launch_tiles_of<T, RT, NT, W, 2>(a, p, s);
-    return launch_tiles_of<T, RT, NT, W, 4>(a, p, s);
+    if (p.shift == 5) return launch_tiles_of<T, NT, 1>(a, p, t, ws, s);
+    if (p.shift == 6) return launch_tiles_of<T, NT, 2>(a, p, t, ws, s);
+    return launch_tiles_of<T, NT, 4>(a, p, t, ws, s);
 }
-template <typename T, int NV, int R>
+template <typename T, int G>
+int launch_tile(const T *a, const W4Args &p, hipStream_t s)
+{
+    constexpr int W = 16;
+    hipLaunchKernelGGL((fc_w4_tile_kernel<T, W, G>), dim3((unsigned)((p.Out + 15) / 16)), dim3(W * 64), W * 1024, s, a, p);
+    return launch_status();
+}
+template <typename T>
 int launch_rows(const T *a, const W4Args &p, hipStream_t s)
 {
     int logl = 6;
     while (logl > 0 && (1 << (logl - 1)) >= p.blocks) --logl;
-    const int per = R * (64 >> logl);
-    int waves = (p.blocks + (1 << logl) - 1) >> logl;
-    if (waves > kRowWaves<NV>) waves = kRowWaves<NV>;
-    hipLaunchKernelGGL((fc_w4_rows_kernel<T, NV, R>), dim3((unsigned)((p.Out + per - 1) / per), (unsigned)((p.N + NV - 1) / NV)), dim3(64 * waves),
-                       (size_t)waves * per * NV * 4, s, a, p, logl);
+    const int some = kBatch * (64 >> logl), pieces = (p.blocks + (1 << logl) - 1) >> logl;
+    const int slices = (pieces + kRowWaves - 1) / kRowWaves, waves = (pieces + slices - 1) / slices;
+    // as many batches to a workgroup as leave the chip 16 waves a compute unit
+    const long sets = (p.Out + some - 1) / some, load = sets * waves * p.N;
+    int batches = (int)((load + 4095) / 4096);
+    if (batches > 64) batches = 64;
+    if (batches > sets) batches = (int)sets;
+    hipLaunchKernelGGL((fc_w4_row_kernel<T>), dim3((unsigned)((sets + batches - 1) / batches), (unsigned)p.N), dim3(64 * waves),
+                       (size_t)batches * waves * some * 4, s, a, p, logl, batches);
     return launch_status();
 }
 template <typename T>
-int fc_w4_of(const T *a, W4Args p, hipStream_t s)
+int fc_w4_of(const T *a, const W4Args &p, void *ws, hipStream_t s)
 {
-    if (p.N == 1) return launch_rows<T, 1, 8>(a, p, s);
-    if (p.N == 2) return launch_rows<T, 2, 8>(a, p, s);
-    if (p.N <= kFewRows) return launch_rows<T, 4, 8>(a, p, s);
+    if (p.N <= kFewRows) return launch_rows(a, p, s);
+    if (one_tile(sizeof(T) == 2 ? VGG_BF16 : VGG_F32, p.N, p.In)) return p.shift == 5 ? launch_tile<T, 1>(a, p, s) : p.shift == 6 ? launch_tile<T, 2>(a, p, s) : launch_tile<T, 4>(a, p, s);
     const W4Plan t = tiles_plan(sizeof(T) == 2 ? VGG_BF16 : VGG_F32, p.N, p.In, p.Out);
-    p.splits = t.splits;
-    p.row_tiles = t.row_tiles;
-    if (t.nt == 1) return launch_tiles<T, 1, 1, 16>(a, p, s);
-    if (t.nt == 2) return launch_tiles<T, 1, 2, sizeof(T) == 2 ? 16 : 8>(a, p, s);
-    constexpr int RT = sizeof(T) == 2 ? 4 : 2;
-    return launch_tiles<T, RT, 4, 8>(a, p, s);
+    return t.nt == 1 ? launch_tiles<T, 1>(a, p, t, ws, s) : t.nt == 2 ? launch_tiles<T, 2>(a, p, t, ws, s) : launch_tiles<T, 4>(a, p, t, ws, s);
 }
 
 }  // namespace
@@ -524,18 +685,18 @@ int fc_w4_of(const T *a, W4Args p, hipStream_t s)
 size_t fc_w4_workspace(int dtype, int N, int In, int Out, int group)
 {
     (void)group;
-    if (N <= kFewRows) return 0;
+    if (N <= kFewRows || one_tile(dtype, N, In)) return 0;
     const W4Plan t = tiles_plan(dtype, N, In, Out);
-    return t.splits > 1 ? round_up((size_t)t.splits * N * Out * 4, 256) : 0;
+    return t.lay_bytes + (t.splits > 1 ? round_up((size_t)t.splits * N * Out * 4, 256) : 0);
 }
 
 int fc_w4(int dtype, int N, int In, int Out, int group, const void *a, const uint8_t *codes, const bf16_t *scales, const float *bias, void *z,
           int z_dtype, int relu, void *ws, hipStream_t s)
 {
-    const W4Args p = {codes, scales, bias, z, static_cast<float *>(ws), z_dtype == VGG_BF16, relu, N, In, Out, (In + 31) / 32, (In + group - 1) / group,
+    const W4Args p = {codes, scales, bias, z, nullptr, z_dtype == VGG_BF16, relu, N, In, Out, (In + 31) / 32, (In + group - 1) / group,
                       shift_of(group), 1, 0};
-    if (dtype == VGG_BF16) return fc_w4_of(static_cast<const bf16_t *>(a), p, s);
-    return fc_w4_of(static_cast<const float *>(a), p, s);
+    if (dtype == VGG_BF16) return fc_w4_of(static_cast<const bf16_t *>(a), p, ws, s);
+    return fc_w4_of(static_cast<const float *>(a), p, ws, s);
 }
 
 }  // namespace vgg
