@@ -35,19 +35,38 @@ __device__ __forceinline__ Sums joined(Sums a, Sums b)
     rebase(b, M);
     return {M, a.s + b.s, a.t + b.t};
 }
+// Sums and maxima over a wave without LDS: rotations within 16 lanes, then quarters and halves that change places.
+template <int N> __device__ __forceinline__ float row_ror(float x)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + N, 0xf, 0xf, true));
+}
+template <typename F> __device__ __forceinline__ float wave_all(float v, F f)
+{
+    v = f(v, row_ror<8>(v));
+    v = f(v, row_ror<4>(v));
+    v = f(v, row_ror<2>(v));
+    v = f(v, row_ror<1>(v));
+    const auto q = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    const unsigned q0 = q[0], q1 = q[1];
+    v = f(__uint_as_float(q0), __uint_as_float(q1));
+    const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    const unsigned h0 = h[0], h1 = h[1];
+    return f(__uint_as_float(h0), __uint_as_float(h1));
+}
+__device__ __forceinline__ float all_max(float v) { return wave_all(v, [](float a, float b) { return fmaxf(a, b); }); }
+__device__ __forceinline__ float all_min(float v) { return wave_all(v, [](float a, float b) { return fminf(a, b); }); }
+__device__ __forceinline__ float all_sum(float v) { return wave_all(v, [](float a, float b) { return a + b; }); }
 __device__ __forceinline__ Sums wave_joined(Sums a)
 {
-    const float M = wave_max(a.m);
+    const float M = all_max(a.m);
     rebase(a, M);
-    return {M, wave_sum(a.s), wave_sum(a.t)};
+    return {M, all_sum(a.s), all_sum(a.t)};
 }
 
-// V scores into a thread's sums.
-template <int V> __device__ __forceinline__ void add_scores(Sums &a, const float (&z)[V])
+// V scores, `most` the largest, into a thread's sums.
+template <int V> __device__ __forceinline__ void add_scores(Sums &a, const float (&z)[V], float most)
 {
-    float M = a.m;
-#pragma unroll
-    for (int j = 0; j < V; ++j) M = fmaxf(M, z[j]);
+    const float M = fmaxf(a.m, most);
     if (M > a.m) rebase(a, M);
     const float base = M == -INFINITY ? 0.f : M;
 #pragma unroll
@@ -58,34 +77,103 @@ template <int V> __device__ __forceinline__ void add_scores(Sums &a, const float
     }
 }
 
-// The best scores that a wave has seen, one to a lane, best first; empty places are -inf at class -1.  Equal scores: the lower
-// class is better.
+// A score and its class as one number: the better, the larger; equal scores: the lower class.  0: none.
+typedef unsigned long long Key;
+__device__ __forceinline__ Key key_of(float v, int id)
+{
+    const unsigned b = __float_as_uint(v + 0.f);         // (-0 is 0)
+    return (Key)(b ^ ((unsigned)((int)b >> 31) | 0x80000000u)) << 32 | (unsigned)~id;
+}
+__device__ __forceinline__ float score_of(Key k)
+{
+    const unsigned b = (unsigned)(k >> 32);
+    return __uint_as_float(b & 0x80000000u ? b ^ 0x80000000u : ~b);
+}
+__device__ __forceinline__ int class_of(Key k) { return (int)~(unsigned)k; }
+
+// The best scores that a wave has seen.  Those that may be among them are put into a list in LDS, which, when it is nearly full
+// and at the end, is cut down to the best `top` by counting for each how many are better.  What is not better than the last of
+// them (or, before that, than the top-th of the lanes' first scores) is passed over without more than a comparison.
+constexpr int kList = 256;
 struct Best {
-    float v;
-    int id;
-    float worst_v;   // of the last of `top` places
+    Key *list;         // [kList], this wave's
+    int count, top;
+    float worst_v;
     int worst_id;
 };
-__device__ __forceinline__ float lane_of(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
-__device__ __forceinline__ bool better(float v, int id, float w, int wid) { return v > w || (v == w && id < wid); }
-// Takes what the lanes offer (one score each) into the list, best of the wave or not.
-__device__ __forceinline__ void offer(Best &b, float v, int id, int top, int lane)
+__device__ __forceinline__ bool may_enter(const Best &b, float v, int id) { return v > b.worst_v || (v == b.worst_v && id < b.worst_id); }
+
+// What the wave's lanes have written to LDS is there for all of them.
+__device__ __forceinline__ void wave_sync()
 {
-    unsigned long long rest = __ballot(better(v, id, b.worst_v, b.worst_id));
-    while (rest) {
-        const int l = __builtin_ctzll(rest);
-        const float nv = lane_of(v, l);
-        const int ni = __builtin_amdgcn_readlane(id, l);
-        const int at = __builtin_popcountll(__ballot(better(b.v, b.id, nv, ni)));
-        const float pv = __shfl_up(b.v, 1);
-        const int pi = __shfl_up(b.id, 1);
-        if (lane > at) { b.v = pv; b.id = pi; }
-        else if (lane == at) { b.v = nv; b.id = ni; }
-        b.worst_v = lane_of(b.v, top - 1);
-        b.worst_id = __builtin_amdgcn_readlane(b.id, top - 1);
-        rest &= rest - 1;
-        rest &= __ballot(better(v, id, b.worst_v, b.worst_id));
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+template <int I> __device__ __forceinline__ void cut_list(Key *list, int count, int top, int lane)
+{
+    Key mine[I];
+    int rank[I];
+#pragma unroll
+    for (int i = 0; i < I; ++i) {
+        mine[i] = lane + 64 * i < count ? list[lane + 64 * i] : 0;
+        rank[i] = 0;
     }
+    int q = 0;
+    for (; q + 4 <= count; q += 4) {
+        Key k[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) k[j] = list[q + j];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int i = 0; i < I; ++i) rank[i] += k[j] > mine[i];
+    }
+    for (; q < count; ++q) {
+        const Key k = list[q];
+#pragma unroll
+        for (int i = 0; i < I; ++i) rank[i] += k > mine[i];
+    }
+    wave_sync();
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+        if (mine[i] && rank[i] < top) list[rank[i]] = mine[i];
+    wave_sync();
+}
+__device__ __noinline__ void cut_lists(Key *list, int count, int top, int lane)
+{
+    if (count <= 64) cut_list<1>(list, count, top, lane);
+    else if (count <= 128) cut_list<2>(list, count, top, lane);
+    else cut_list<4>(list, count, top, lane);
+}
+__device__ __forceinline__ void cut(Best &b, int lane)
+{
+    wave_sync();
+    cut_lists(b.list, b.count, b.top, lane);
+    if (b.count >= b.top) {
+        b.count = b.top;
+        const Key last = b.list[b.top - 1];
+        b.worst_v = score_of(last);
+        b.worst_id = class_of(last);
+    }
+}
+__device__ __forceinline__ void offer(Best &b, float v, int id, int lane)
+{
+    const Key mask = __ballot(may_enter(b, v, id));
+    if (!mask) return;
+    const int at = b.count + __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0));
+    if (mask >> lane & 1) b.list[at] = key_of(v, id);
+    b.count += __builtin_popcountll(mask);
+    if (b.count > kList - 64) cut(b, lane);
+}
+// From each lane's best of a first lot: at least `top` of all scores are as good as the top-th of these.
+__device__ __forceinline__ void expect(Best &b, float most)
+{
+    int rank = 0;
+#pragma unroll
+    for (int l = 0; l < 64; ++l) rank += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(most), l)) > most;
+    const float t = all_min(rank < b.top ? most : INFINITY);
+    if (t > -INFINITY) { b.worst_v = t; b.worst_id = 0x7fffffff; }
 }
 
 template <typename T> constexpr int kVec = 16 / (int)sizeof(T);   // scores of a 16-byte load
@@ -113,119 +201,137 @@ struct ScoreArgs {
     float *logp, *entropy, *top_logp, *stats;
     int32_t *top_idx;
     float *part_sums;             // [N][parts][3]
-    float *part_v;                // [N][parts][top]
-    int *part_id;
+    Key *part_best;               // [N][parts][top], best first, 0 where there are fewer
 };
 
-// What a row's waves leave in LDS (or parts in the workspace) becomes the row's outputs: `count` list entries at v, id.
-__device__ void finish_row(const ScoreArgs &a, const Sums &r, float z_label, int row, const float *v, const int *id, int count, int tid, int threads)
+// Log of a row's sum; -inf where it has no class.
+__device__ __forceinline__ float log_sum(const Sums &r) { return r.m == -INFINITY && r.s == 0.f ? -INFINITY : logf(r.s); }
+__device__ __forceinline__ void write_row(const ScoreArgs &a, const Sums &r, float z_label, int y, int row)
 {
-    const float log_s = r.m == -INFINITY && r.s == 0.f ? -INFINITY : logf(r.s);
+    const float log_s = log_sum(r);
     const bool empty = log_s == -INFINITY;
-    if (tid == 0) {
-        if (a.logp) {
-            const int y = a.labels[row];
-            a.logp[row] = y < 0 || y >= a.K ? 0.f : empty ? -INFINITY : (z_label - r.m) - log_s;
+    if (a.logp) a.logp[row] = y < 0 || y >= a.K ? 0.f : empty ? -INFINITY : (z_label - r.m) - log_s;
+    if (a.entropy) a.entropy[row] = empty ? 0.f : log_s - r.t / r.s;
+    if (a.stats) { a.stats[2 * (size_t)row] = r.m; a.stats[2 * (size_t)row + 1] = log_s; }
+}
+// Alternative i of a row: `k`, or none.
+__device__ __forceinline__ void write_best(const ScoreArgs &a, const Sums &r, int row, int i, Key k)
+{
+    const bool fine = r.s > 0.f;         // neither without a class nor NaN
+    const size_t at = (size_t)row * a.top + i;
+    a.top_logp[at] = k && fine ? (score_of(k) - r.m) - log_sum(r) : fine || r.s == 0.f ? -INFINITY : r.s;
+    a.top_idx[at] = k && fine ? class_of(k) : -1;
+}
+// The best of the waves' lists, `top` places each with `count` keys together: to each thread's key its place.
+template <int W, typename F> __device__ __forceinline__ void merge_lists(const Key (*lists)[kList], const int *counts, int top, F write)
+{
+    const int i = threadIdx.x, w = i / top, at = i - w * top;
+    int all = 0;
+#pragma unroll
+    for (int k = 0; k < W; ++k) all += counts[k];
+    if (w < W && at < counts[w]) {
+        const Key mine = lists[w][at];
+        int rank = at;                   // (its own list is in order)
+#pragma unroll
+        for (int k = 0; k < W; ++k) {
+            if (k == w) continue;
+            int lo = 0, hi = counts[k];  // better ones in list k
+            while (lo < hi) {
+                const int mid = (lo + hi) / 2;
+                if (lists[k][mid] > mine) lo = mid + 1;
+                else hi = mid;
+            }
+            rank += lo;
         }
-        if (a.entropy) a.entropy[row] = empty ? 0.f : log_s - r.t / r.s;
-        if (a.stats) { a.stats[2 * (size_t)row] = r.m; a.stats[2 * (size_t)row + 1] = log_s; }
+        if (rank < top) write(rank, mine);
     }
-    if (!a.top) return;
-    float *tv = a.top_logp + (size_t)row * a.top;
-    int32_t *ti = a.top_idx + (size_t)row * a.top;
-    const bool none = !(r.s > 0.f);   // no class left, or a NaN
-    int real = 0;
-    for (int i = 0; i < count; ++i) real += id[i] >= 0;
-    for (int i = tid; i < count; i += threads) {
-        if (id[i] < 0 || none) continue;
-        int rank = 0;
-        for (int j = 0; j < count; ++j) rank += id[j] >= 0 && better(v[j], id[j], v[i], id[i]);
-        if (rank < a.top) { tv[rank] = (v[i] - r.m) - log_s; ti[rank] = id[i]; }
-    }
-    for (int i = tid; i < a.top; i += threads)
-        if (none || i >= real) { tv[i] = empty ? -INFINITY : none ? r.s : -INFINITY; ti[i] = -1; }
+    if (i < top && i >= all) write(i, (Key)0);
 }
 
 // W waves to a row or to a part of one; W == 1: four rows to a workgroup.
 template <typename T, int W, bool TOP>
-__global__ __launch_bounds__(W == 1 ? 256 : W * 64) void log_probs_kernel(const T *__restrict__ z, ScoreArgs a)
+__global__ __launch_bounds__(256) void log_probs_kernel(const T *__restrict__ z, ScoreArgs a)
 {
-    constexpr int V = kVec<T>;
-    constexpr int R = W == 1 ? 4 : 1;    // rows of a workgroup
-    __shared__ Sums sums[W];
-    __shared__ float best_v[R * (W == 1 ? 1 : W) * kMaxTop];
-    __shared__ int best_id[R * (W == 1 ? 1 : W) * kMaxTop];
+    constexpr int V = kVec<T>, U = 4;    // U loads at a time
+    __shared__ Sums sums[4];
+    __shared__ Key lists[TOP ? 4 : 1][kList];
+    __shared__ int counts[4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int unit = W == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
-    const int row = unit / a.parts, part = unit - row * a.parts;
+    const int row = a.parts == 1 ? unit : unit / a.parts, part = unit - row * a.parts;
     if (row >= a.N) return;              // (W == 1 only: there is no barrier there)
     const T *zr = z + (size_t)row * a.ldz;
+    const int y = a.logp ? a.labels[row] : -1;
+    const float z_label = y >= 0 && y < a.K ? Elem<T>::load(zr + y) : 0.f;
     const int k0 = part * a.span, k1 = a.K - k0 < a.span ? a.K : k0 + a.span;
     // whole 16-byte vectors between a head and a tail of fewer scores
     const int off = (int)((reinterpret_cast<uintptr_t>(zr + k0) & 15) / sizeof(T));
     int head = off ? V - off : 0;
     if (head > k1 - k0) head = k1 - k0;
     const int v0 = k0 + head, nvec = (k1 - v0) / V, tail0 = v0 + nvec * V;
-    const int ti = W == 1 ? lane : threadIdx.x, tn = W == 1 ? 64 : W * 64;
+    const int ti = W == 1 ? lane : threadIdx.x, tn = W * 64;
 
     Sums mine = {-INFINITY, 0.f, 0.f};
-    Best b = {-INFINITY, -1, -INFINITY, -1};
-    for (int i0 = 0; i0 < nvec; i0 += tn) {
-        const int i = i0 + ti;
-        float x[V];
-        if (i < nvec) load_scores(zr + v0 + (size_t)i * V, x);
-        else
+    Best b = {lists[TOP ? wave : 0], 0, a.top, -INFINITY, -1};
+    // head and tail: fewer than 2 V scores, one to a lane of the first wave
+    float ends = -INFINITY;
+    const int end_k = lane < head ? k0 + lane : tail0 + lane - head;
+    if ((W == 1 || wave == 0) && (lane < head || end_k < k1)) ends = Elem<T>::load(zr + end_k);
+    for (int i0 = ti; i0 - ti < nvec; i0 += U * tn) {
+        float x[U][V];
 #pragma unroll
-            for (int j = 0; j < V; ++j) x[j] = -INFINITY;
-        add_scores<V>(mine, x);
-        if constexpr (TOP) {
-            float most = x[0];
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u * tn;
+            if (i < nvec) load_scores(zr + v0 + (size_t)i * V, x[u]);
+            else
 #pragma unroll
-            for (int j = 1; j < V; ++j) most = fmaxf(most, x[j]);
-            if (__ballot(most >= b.worst_v && most > -INFINITY))
+                for (int j = 0; j < V; ++j) x[u][j] = -INFINITY;
+        }
+        float most[U];
 #pragma unroll
-                for (int j = 0; j < V; ++j) offer(b, x[j], v0 + i * V + j, a.top, lane);
+        for (int u = 0; u < U; ++u) {
+            most[u] = x[u][0];
+#pragma unroll
+            for (int j = 1; j < V; ++j) most[u] = fmaxf(most[u], x[u][j]);
+        }
+        if constexpr (TOP)
+            if (i0 == ti) expect(b, fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])));
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            add_scores<V>(mine, x[u], most[u]);
+            if constexpr (TOP)
+                if (__ballot(most[u] >= b.worst_v && most[u] > -INFINITY))
+#pragma unroll
+                    for (int j = 0; j < V; ++j) offer(b, x[u][j], v0 + (i0 + u * tn) * V + j, lane);
         }
     }
-    if (W == 1 || wave == 0) {           // head and tail: fewer than 2 V scores, one to a lane
-        const int k = lane < head ? k0 + lane : tail0 + lane - head;
-        float x[1] = {lane < head || k < k1 ? Elem<T>::load(zr + k) : -INFINITY};
-        add_scores<1>(mine, x);
-        if constexpr (TOP) offer(b, x[0], k, a.top, lane);
+    {
+        const float x[1] = {ends};
+        add_scores<1>(mine, x, ends);
+        if constexpr (TOP) offer(b, ends, end_k, lane);
     }
     mine = wave_joined(mine);
+    if constexpr (TOP) cut(b, lane);
 
-    const int y = a.logp ? a.labels[row] : -1;
-    const float z_label = y >= 0 && y < a.K ? Elem<T>::load(zr + y) : 0.f;
     if constexpr (W == 1) {
-        // the list is in order already
-        if (a.parts == 1) {
-            float *bv = best_v + wave * kMaxTop;
-            int *bi = best_id + wave * kMaxTop;
-            if (TOP && lane < a.top) { bv[lane] = b.v; bi[lane] = b.id; }
-            __builtin_amdgcn_wave_barrier();
-            finish_row(a, mine, z_label, row, bv, bi, TOP ? a.top : 0, lane, 64);
-        }
+        if (lane == 0) write_row(a, mine, z_label, y, row);
+        if (TOP && lane < a.top) write_best(a, mine, row, lane, lane < b.count ? b.list[lane] : 0);
     } else {
-        if (lane == 0) sums[wave] = mine;
-        if (TOP && lane < a.top) { best_v[wave * a.top + lane] = b.v; best_id[wave * a.top + lane] = b.id; }
+        if (lane == 0) {
+            sums[wave] = mine;
+            counts[wave] = b.count;
+        }
         __syncthreads();
         mine = sums[0];
         for (int w = 1; w < W; ++w) mine = joined(mine, sums[w]);
-        const int count = TOP ? W * a.top : 0;
-        if (a.parts == 1) { finish_row(a, mine, z_label, row, best_v, best_id, count, threadIdx.x, W * 64); return; }
+        if (a.parts == 1) {
+            if (threadIdx.x == 0) write_row(a, mine, z_label, y, row);
+            if constexpr (TOP) merge_lists<W>(lists, counts, a.top, [&](int i, Key k) { write_best(a, mine, row, i, k); });
+            return;
+        }
         const size_t at = (size_t)row * a.parts + part;
         if (threadIdx.x == 0) { a.part_sums[at * 3] = mine.m; a.part_sums[at * 3 + 1] = mine.s; a.part_sums[at * 3 + 2] = mine.t; }
-        // the part's own best, in order
-        int real = 0;
-        for (int i = 0; i < count; ++i) real += best_id[i] >= 0;
-        for (int i = threadIdx.x; i < count; i += W * 64) {
-            if (best_id[i] < 0) continue;
-            int rank = 0;
-            for (int j = 0; j < count; ++j) rank += best_id[j] >= 0 && better(best_v[j], best_id[j], best_v[i], best_id[i]);
-            if (rank < a.top) { a.part_v[at * a.top + rank] = best_v[i]; a.part_id[at * a.top + rank] = best_id[i]; }
-        }
-        for (int i = real + threadIdx.x; i < a.top && TOP; i += W * 64) { a.part_v[at * a.top + i] = -INFINITY; a.part_id[at * a.top + i] = -1; }
+        if constexpr (TOP) merge_lists<W>(lists, counts, a.top, [&](int i, Key k) { a.part_best[at * a.top + i] = k; });
     }
 }
 
@@ -234,32 +340,38 @@ template <typename T, bool TOP>
 __global__ __launch_bounds__(256) void log_probs_join_kernel(const T *__restrict__ z, ScoreArgs a)
 {
     __shared__ Sums sums[4];
-    __shared__ float best_v[4 * kMaxTop];
-    __shared__ int best_id[4 * kMaxTop];
+    __shared__ Key lists[TOP ? 4 : 1][kList];
+    __shared__ int counts[4];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = blockIdx.x;
+    const int y = a.logp ? a.labels[row] : -1;
+    const float z_label = y >= 0 && y < a.K ? Elem<T>::load(z + (size_t)row * a.ldz + y) : 0.f;
     Sums mine = {-INFINITY, 0.f, 0.f};
     for (int p = threadIdx.x; p < a.parts; p += 256) {
         const float *s = a.part_sums + ((size_t)row * a.parts + p) * 3;
         mine = joined(mine, {s[0], s[1], s[2]});
     }
     mine = wave_joined(mine);
+    Best b = {lists[TOP ? wave : 0], 0, a.top, -INFINITY, -1};
     if constexpr (TOP) {
-        Best b = {-INFINITY, -1, -INFINITY, -1};
         const int n = a.parts * a.top;
-        const size_t at = (size_t)row * n;
-        for (int i0 = 0; i0 < n; i0 += 256) {
-            const int i = i0 + threadIdx.x;
-            offer(b, i < n ? a.part_v[at + i] : -INFINITY, i < n ? a.part_id[at + i] : 0, a.top, lane);
+        const Key *keys = a.part_best + (size_t)row * n;
+        for (int i0 = wave * 64; i0 < n; i0 += 256) {
+            const Key k = i0 + lane < n ? keys[i0 + lane] : 0;
+            const float v = k ? score_of(k) : -INFINITY;
+            if (i0 == wave * 64) expect(b, v);
+            offer(b, v, class_of(k), lane);
         }
-        if (lane < a.top) { best_v[wave * a.top + lane] = b.v; best_id[wave * a.top + lane] = b.id; }
+        cut(b, lane);
     }
-    if (lane == 0) sums[wave] = mine;
+    if (lane == 0) {
+        sums[wave] = mine;
+        counts[wave] = b.count;
+    }
     __syncthreads();
     mine = sums[0];
     for (int w = 1; w < 4; ++w) mine = joined(mine, sums[w]);
-    const int y = a.logp ? a.labels[row] : -1;
-    const float z_label = y >= 0 && y < a.K ? Elem<T>::load(z + (size_t)row * a.ldz + y) : 0.f;
-    finish_row(a, mine, z_label, row, best_v, best_id, TOP ? 4 * a.top : 0, threadIdx.x, 256);
+    if (threadIdx.x == 0) write_row(a, mine, z_label, y, row);
+    if constexpr (TOP) merge_lists<4>(lists, counts, a.top, [&](int i, Key k) { write_best(a, mine, row, i, k); });
 }
 
 // dz_j = g (1[j = y] - p_j) - h p_j (log p_j + entropy).
@@ -269,11 +381,14 @@ struct GradArgs {
     const int32_t *labels;
     const float *stats, *entropy, *g_logp, *g_entropy;
 };
-template <typename T>
+// W waves to a row or to a part of one.
+template <typename T, int W>
 __global__ __launch_bounds__(256) void log_probs_bwd_kernel(const T *z, T *dz, GradArgs a)
 {
-    constexpr int V = kVec<T>;
-    const int row = blockIdx.x / a.parts, part = blockIdx.x - row * a.parts;
+    constexpr int V = kVec<T>, TN = W * 64;
+    const int tid = threadIdx.x % TN, unit = blockIdx.x * (4 / W) + threadIdx.x / TN;
+    const int row = a.parts == 1 ? unit : unit / a.parts, part = unit - row * a.parts;
+    if (row >= a.N) return;
     const T *zr = z + (size_t)row * a.ldz;
     T *dr = dz + (size_t)row * a.lddz;
     const int k0 = part * a.span, k1 = a.K - k0 < a.span ? a.K : k0 + a.span;
@@ -295,7 +410,7 @@ __global__ __launch_bounds__(256) void log_probs_bwd_kernel(const T *z, T *dz, G
     int head = together ? (off ? V - off : 0) : k1 - k0;   // scores before the first 16-byte vector; all, where dz has none there
     if (head > k1 - k0) head = k1 - k0;
     const int v0 = k0 + head, nvec = (k1 - v0) / V, tail0 = v0 + nvec * V;
-    for (int i = threadIdx.x; i < nvec; i += 256) {
+    for (int i = tid; i < nvec; i += TN) {
         float x[V] = {};
         if (!zero) {
             load_scores(zr + v0 + (size_t)i * V, x);
@@ -305,7 +420,7 @@ __global__ __launch_bounds__(256) void log_probs_bwd_kernel(const T *z, T *dz, G
 #pragma unroll
         for (int j = 0; j < V; j += 4) store4(dr + v0 + (size_t)i * V + j, x[j], x[j + 1], x[j + 2], x[j + 3]);
     }
-    for (int i = threadIdx.x; i < head + (k1 - tail0); i += 256) {
+    for (int i = tid; i < head + (k1 - tail0); i += TN) {
         const int k = i < head ? k0 + i : tail0 + i - head;
         Elem<T>::store(dr + k, zero ? 0.f : grad(Elem<T>::load(zr + k), k));
     }
@@ -328,7 +443,7 @@ size_t log_probs_workspace(int N, int K, int top)
 {
     const Split s = split_rows(N, K);
     if (s.parts == 1) return 0;
-    return round_up((size_t)N * s.parts * (3 + 2 * top) * 4, 256);
+    return round_up((size_t)N * s.parts * (3 * sizeof(float) + top * sizeof(Key)) + sizeof(Key), 256);
 }
 
 template <typename T>
@@ -351,15 +466,24 @@ int log_probs(int dtype, int N, int K, size_t ldz, const void *z, const int32_t 
               float *top_logp, int32_t *top_idx, float *stats, void *ws, hipStream_t s)
 {
     const Split c = split_rows(N, K);
-    ScoreArgs a = {N, K, top, c.parts, c.span, ldz, labels, logp, entropy, top_logp, stats, top_idx, nullptr, nullptr, nullptr};
+    ScoreArgs a = {N, K, top, c.parts, c.span, ldz, labels, logp, entropy, top_logp, stats, top_idx, nullptr, nullptr};
     if (c.parts > 1) {
         const size_t n = (size_t)N * c.parts;
         a.part_sums = static_cast<float *>(ws);
-        a.part_v = a.part_sums + n * 3;
-        a.part_id = reinterpret_cast<int *>(a.part_v + n * top);
+        a.part_best = static_cast<Key *>(ws);
+        a.part_sums = reinterpret_cast<float *>(a.part_best + n * top);
     }
     if (dtype == VGG_BF16) return log_probs_of(static_cast<const bf16_t *>(z), a, s);
     return log_probs_of(static_cast<const float *>(z), a, s);
+}
+
+template <typename T>
+static int log_probs_bwd_of(const T *z, T *dz, const GradArgs &a, hipStream_t s)
+{
+    const unsigned units = (unsigned)a.N * a.parts;
+    if (a.K <= 512) hipLaunchKernelGGL((log_probs_bwd_kernel<T, 1>), dim3((units + 3) / 4), dim3(256), 0, s, z, dz, a);
+    else hipLaunchKernelGGL((log_probs_bwd_kernel<T, 4>), dim3(units), dim3(256), 0, s, z, dz, a);
+    return launch_status();
 }
 
 int log_probs_bwd(int dtype, int N, int K, size_t ldz, const void *z, const int32_t *labels, const float *stats, const float *entropy,
@@ -367,10 +491,8 @@ int log_probs_bwd(int dtype, int N, int K, size_t ldz, const void *z, const int3
 {
     const Split c = split_rows(N, K);
     const GradArgs a = {N, K, c.span, c.parts, ldz, lddz, labels, stats, entropy, g_logp, g_entropy};
-    const dim3 grid((unsigned)N * c.parts), block(256);
-    if (dtype == VGG_BF16) hipLaunchKernelGGL(log_probs_bwd_kernel<bf16_t>, grid, block, 0, s, static_cast<const bf16_t *>(z), static_cast<bf16_t *>(dz), a);
-    else hipLaunchKernelGGL(log_probs_bwd_kernel<float>, grid, block, 0, s, static_cast<const float *>(z), static_cast<float *>(dz), a);
-    return launch_status();
+    if (dtype == VGG_BF16) return log_probs_bwd_of(static_cast<const bf16_t *>(z), static_cast<bf16_t *>(dz), a, s);
+    return log_probs_bwd_of(static_cast<const float *>(z), static_cast<float *>(dz), a, s);
 }
 
 }  // namespace vgg

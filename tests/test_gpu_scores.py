@@ -1,0 +1,310 @@
+"""Log probabilities with entropy, alternatives and gradient against the definition in 64 bits: one class to many, rows of every
+alignment, ties, masks that leave nothing, infinities and NaN, rows in parts, another stream, a graph."""
+import numpy as np
+import pytest
+import torch
+
+from paper_1810_09868_amd import binding as B
+
+from gpu_util import TDT, ws_bytes
+
+pytestmark = pytest.mark.gpu
+
+
+def reference(z, labels, top):
+    """logp, entropy, top_logp, top_idx of fp64 scores by the definition (rows that are finite or -inf)."""
+    N, K = z.shape
+    out = [np.zeros(N), np.zeros(N), np.full((N, top), -np.inf), np.full((N, top), -1)]
+    for n in range(N):
+        row, there = z[n], z[n] > -np.inf
+        if not there.any():
+            out[0][n] = -np.inf if 0 <= labels[n] < K else 0
+            continue
+        m = row.max()
+        with np.errstate(under="ignore"):
+            log_s = np.log(np.exp(row[there] - m).sum())
+            lp = np.where(there, (row - m) - log_s, -np.inf)     # (m + log s would lose log s beside the lowest value)
+            p = np.exp(lp[there])
+        out[0][n] = lp[labels[n]] if 0 <= labels[n] < K else 0
+        out[1][n] = -(p * np.where(p > 0, lp[there], 0)).sum()
+        best = np.lexsort((np.arange(K), -row))[:top]
+        best = best[row[best] > -np.inf]
+        out[2][n, : len(best)], out[3][n, : len(best)] = lp[best], best
+    return out
+
+
+def gradient64(z, labels, g, h):
+    N, K = z.shape
+    dz = np.zeros((N, K))
+    for n in range(N):
+        there = z[n] > -np.inf
+        if not there.any():
+            continue
+        m = z[n].max()
+        lp = z[n][there] - m - np.log(np.exp(z[n][there] - m).sum())
+        p = np.exp(lp)
+        d = np.zeros(K)
+        gn = g[n] if 0 <= labels[n] < K else 0.0
+        H = -(p * np.where(p > 0, lp, 0)).sum()
+        d[there] = -gn * p - h[n] * p * (np.where(p > 0, lp, 0) + H)
+        if 0 <= labels[n] < K and there[labels[n]]:
+            d[labels[n]] += gn
+        dz[n] = d
+    return dz
+
+
+class Call:
+    def __init__(self, dtype, z, labels, top, ldz=None):
+        """z: a float tensor [N][K] already rounded to the type's values."""
+        N, K = z.shape
+        ld = K if ldz is None else ldz
+        self.dtype, self.N, self.K, self.ld = dtype, N, K, ld
+        buf = torch.full((N, ld), 7.0e4, dtype=TDT[dtype])     # what lies between rows must not count
+        buf[:, :K] = z
+        self.z = buf.cuda()
+        self.labels = torch.tensor(labels, dtype=torch.int32, device="cuda")
+        self.logp, self.entropy = (torch.full((N,), 9.0, device="cuda") for _ in range(2))
+        self.stats = torch.full((N, 2), 9.0, device="cuda")
+        self.top = top
+        self.top_logp = torch.full((N, max(top, 1)), 9.0, device="cuda")
+        self.top_idx = torch.full((N, max(top, 1)), 99, dtype=torch.int32, device="cuda")
+        self.ws = ws_bytes(B.vgg_log_probs_workspace_bytes(dtype, N, K, top))
+        self.ws.fill_(0xFF)
+
+    def run(self):
+        B.vgg_log_probs(self.dtype, self.N, self.K, self.z, self.labels, self.top, self.logp, self.entropy,
+                        self.top_logp if self.top else None, self.top_idx if self.top else None, self.stats, self.ws, ldz=self.ld)
+        return self
+
+    def grad(self, g, h, lddz=None, in_place=False):
+        lddz = self.ld if lddz is None else lddz
+        dz = self.z if in_place else torch.full((self.N, lddz), 5.0, dtype=TDT[self.dtype], device="cuda")
+        dev = lambda a: None if a is None else torch.tensor(a, dtype=torch.float32, device="cuda")  # noqa: E731
+        B.vgg_log_probs_bwd(self.dtype, self.N, self.K, self.z, None if g is None else self.labels, self.stats,
+                            None if h is None else self.entropy, dev(g), dev(h), dz, ldz=self.ld, lddz=lddz)
+        return dz
+
+
+def scores(dtype, N, K, seed, masked=0.0, std=3.0):
+    rng = np.random.default_rng(seed)
+    z = torch.from_numpy((rng.standard_normal((N, K)) * std).astype(np.float32)).to(TDT[dtype]).float()
+    if masked:
+        z[torch.from_numpy(rng.random((N, K)) < masked)] = -np.inf
+    return z, rng.integers(-1, K + 1, N).astype(np.int32)      # labels outside on both sides among them
+
+
+# A log probability is z - m (exact to 2^-24 |z - m|) less log S: S sums K terms of relative error about 2^-22 (their exponents'
+# rounding at |z - m| up to 20) and log adds 2^-24 of itself: below 4e-6 (1 + |value|) in all; entropy the same.
+def close(got, want, tol=4e-6):
+    got, want = np.asarray(got, np.float64), np.asarray(want, np.float64)
+    want = np.where(np.abs(want) > 3.4028236e38, np.sign(want) * np.inf, want)      # past fp32's range
+    assert np.array_equal(np.isinf(got), np.isinf(want)) and not np.isnan(got).any()
+    f = np.isfinite(want)
+    assert np.array_equal(got[~f], want[~f])
+    err = np.abs(got[f] - want[f]) / (1 + np.abs(want[f]))
+    assert err.size == 0 or err.max() <= tol, err.max()
+
+
+def check(c, z, labels):
+    torch.cuda.synchronize()
+    logp, entropy, tl, ti = reference(z.double().numpy(), labels, c.top)
+    close(c.logp.cpu(), logp)
+    close(c.entropy.cpu(), entropy)
+    if c.top:
+        assert np.array_equal(c.top_idx.cpu().numpy(), ti)
+        close(c.top_logp.cpu(), tl)
+
+
+SIZES = [(1, 1), (3, 2), (1, 7), (5, 10), (2, 63), (9, 64), (3, 65), (4, 255), (100, 1000), (3, 2048), (2, 2049), (7, 4099), (2, 16384), (1, 33333), (3, 70001)]
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("top", [0, 1, 5, 20, 64])
+def test_forward_against_64_bits(dtype, top):
+    for k, (N, K) in enumerate(SIZES):
+        z, labels = scores(dtype, N, K, 31 * k + top, masked=0.3 if k % 3 == 0 else 0.0)
+        ld = K if k % 2 else K + (k % 5) + 1
+        check(Call(dtype, z, labels, min(top, K), ld).run(), z, labels)
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+def test_backward_against_64_bits(dtype):
+    for k, (N, K) in enumerate(SIZES):
+        z, labels = scores(dtype, N, K, 17 * k, masked=0.2 if k % 2 == 0 else 0.0)
+        rng = np.random.default_rng(k)
+        g, h = rng.standard_normal(N).astype(np.float32), rng.standard_normal(N).astype(np.float32)
+        if N > 2:
+            h[1] = 0.0
+        ld = K + k % 4
+        for lddz, use_g, use_h, inplace in ((ld, True, True, False), (ld + 3, True, False, False), (ld, False, True, False), (ld, True, True, True)):
+            c = Call(dtype, z, labels, 0, ld).run()
+            dz = c.grad(g if use_g else None, h if use_h else None, lddz, inplace)
+            torch.cuda.synchronize()
+            want = gradient64(z.double().numpy(), labels, g if use_g else 0 * g, h if use_h else 0 * h)
+            got = dz.float().cpu().double().numpy()
+            # p to 4e-6 of itself, times g, and times h (log p + H) whose two terms are below 25 in size; bf16 adds half of 2^-8
+            size = np.abs(g)[:, None] + np.abs(h)[:, None] * 25
+            p = np.exp(np.where(z > -np.inf, z.double().numpy() - c.stats.double().sum(1, keepdim=True).cpu().numpy(), -np.inf))
+            allow = 8e-6 * size * (p + 1e-30) + 1e-6 * np.abs(want) + (2.0 ** -8 * np.abs(want) if dtype == B.BF16 else 0) + 1e-37
+            assert (np.abs(got[:, :K] - want) <= allow).all(), (N, K, use_g, use_h)
+            assert (got[:, K:] == (7.0e4 if inplace else 5.0)).all() or dtype == B.BF16 and inplace
+
+
+def test_gradient_against_differences():
+    rng = np.random.default_rng(3)
+    z = rng.standard_normal((2, 12)) * 2
+    labels = np.array([3, 11], np.int32)
+    g, h = np.array([0.7, -1.2], np.float32), np.array([0.4, 1.1], np.float32)
+
+    def value(x):
+        logp, entropy, _, _ = reference(x, labels, 0)
+        return (g * logp + h * entropy).sum()
+
+    want = np.zeros_like(z)
+    for n in range(2):
+        for j in range(12):
+            d = np.zeros_like(z)
+            d[n, j] = 1e-5
+            want[n, j] = (value(z + d) - value(z - d)) / 2e-5
+    c = Call(B.F32, torch.from_numpy(z).float(), labels, 0).run()
+    assert np.abs(c.grad(g, h).cpu().numpy() - want).max() < 2e-6
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("K", [5, 300, 3000, 50000])
+def test_equal_scores_go_to_the_lowest_class(dtype, K):
+    z = torch.zeros((3, K))
+    z[1] = torch.arange(K) % 3                    # a third of the classes share each score
+    z[2, : K // 2] = -0.0                         # -0 and 0 are equal
+    labels = np.array([0, K - 1, 1], np.int32)
+    check(Call(dtype, z, labels, min(K, 40)).run(), z, labels)
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("order", ["rising", "falling"])
+def test_alternatives_of_sorted_rows(dtype, order):
+    K = 40000
+    z = torch.linspace(-20, 20, K)[None].to(TDT[dtype]).float()
+    z = z if order == "rising" else z.flip(1)
+    check(Call(dtype, z.contiguous(), np.array([7], np.int32), 64).run(), z, np.array([7], np.int32))
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("K", [40, 1000, 20011])
+def test_rows_that_a_mask_empties(dtype, K):
+    low = float(torch.finfo(TDT[dtype]).min)
+    z = torch.full((6, K), -np.inf)
+    z[1, K - 2] = 3.0                             # one class left
+    z[2, 1:4] = torch.tensor([1.0, 2.0, 1.0])     # three
+    z[3] = low                                    # a mask of the type's lowest value: every class is as likely
+    z[4] = low
+    z[4, 5] = 2.0
+    z[5, 0], z[5, 1] = -low, low                  # as far apart as they get
+    labels = np.array([2, 0, 3, 1, 5, 1], np.int32)
+    c = Call(dtype, z, labels, min(K, 8)).run()
+    check(c, z, labels)
+    one = np.ones(6, np.float32)
+    dz = c.grad(one, one).float().cpu().double().numpy()
+    want = gradient64(z.double().numpy(), labels, one, one)
+    assert np.isfinite(dz).all() and np.abs(dz - want).max() <= (1e-2 if dtype == B.BF16 else 1e-5)
+    assert not dz[0].any() and not dz[1, : K - 2].any()
+
+
+@pytest.mark.parametrize("K", [30, 5000, 20011])
+def test_nans_and_infinities_keep_to_their_rows(K):
+    z, labels = scores(B.F32, 6, K, 5)
+    labels[:] = 3
+    z[1, K - 1], z[3, 2], z[4, 3] = np.nan, np.inf, -np.inf
+    c = Call(B.F32, z, labels, 6).run()
+    torch.cuda.synchronize()
+    for n in (1, 3):
+        assert torch.isnan(c.logp[n]) and torch.isnan(c.entropy[n]) and torch.isnan(c.top_logp[n]).all() and (c.top_idx[n] == -1).all()
+    keep = [0, 2, 4, 5]
+    logp, entropy, tl, ti = reference(z[keep].double().numpy(), labels[keep], 6)
+    close(c.logp[keep].cpu(), logp)
+    close(c.entropy[keep].cpu(), entropy)
+    assert np.array_equal(c.top_idx[keep].cpu().numpy(), ti)
+    g = np.ones(6, np.float32)
+    dz = c.grad(g, None).cpu()
+    assert torch.isnan(dz[1]).all() and torch.isnan(dz[3]).all() and torch.isfinite(dz[keep]).all() and dz[4, 3] == 0
+    g[1] = g[3] = 0                               # a row without an upstream gradient: zeros, whatever it holds
+    dz = c.grad(g, 0 * g).cpu()
+    assert torch.isfinite(dz).all() and not dz[1].any() and not dz[3].any()
+
+
+def test_offsets_scores_by_thousands_without_loss():
+    z, labels = scores(B.F32, 4, 3000, 9)
+    z = (z * 64).round() / 64 + 8192              # exact in fp32
+    c = Call(B.F32, z, labels, 3).run()
+    check(c, z, labels)
+    g = np.ones(4, np.float32)
+    dz = c.grad(g, g).cpu().double().numpy()
+    want = gradient64(z.double().numpy(), labels, g, g)
+    assert np.abs(dz - want).max() <= 3e-6
+
+
+def test_results_that_are_not_wanted_are_not_needed():
+    z, labels = scores(B.BF16, 5, 777, 2)
+    c = Call(B.BF16, z, labels, 4).run()
+    logp, top = torch.zeros(5, device="cuda"), torch.zeros((5, 4), device="cuda")
+    idx = torch.zeros((5, 4), dtype=torch.int32, device="cuda")
+    B.vgg_log_probs(B.BF16, 5, 777, c.z, c.labels, 0, logp, None, None, None, None)
+    B.vgg_log_probs(B.BF16, 5, 777, c.z, None, 4, None, None, top, idx, None)
+    torch.cuda.synchronize()
+    assert torch.equal(logp, c.logp) and torch.equal(top, c.top_logp) and torch.equal(idx, c.top_idx)
+
+
+def test_softmax_and_cross_entropy_of_the_training_step_agree():
+    z, _ = scores(B.F32, 100, 1000, 4)
+    labels = np.arange(100, dtype=np.int32) * 9
+    c = Call(B.F32, z, labels, 0).run()
+    p, dz, loss = torch.empty((100, 1000), device="cuda"), torch.empty((100, 1000), device="cuda"), torch.empty(1, device="cuda")
+    B.vgg_softmax(100, 1000, c.z, p)
+    B.vgg_softmax_xent_bwd(100, 1000, p, c.labels, loss, dz, ws_bytes(400))
+    mine = c.grad(np.full(100, -0.01, np.float32), None)
+    torch.cuda.synchronize()
+    assert abs(float(loss) + float(c.logp.double().mean())) < 1e-5
+    assert float((mine - dz).abs().max()) < 1e-8
+
+
+def test_refusals():
+    a, i = torch.zeros((4096,), device="cuda"), torch.zeros((64,), dtype=torch.int32, device="cuda")
+    ok = dict(dtype=B.F32, N=2, K=10, z=a, labels=i, top=2, logp=a, entropy=a, top_logp=a, top_idx=i, stats=a)
+    for change, status in [(dict(z=None), -1), (dict(labels=None), -1), (dict(logp=None), -1), (dict(top=0), -1), (dict(top_idx=None), -1),
+                           (dict(dtype=4), -3), (dict(N=0), -2), (dict(K=0), -2), (dict(top=11), -2), (dict(top=-1, top_logp=None, top_idx=None), -2),
+                           (dict(ldz=9), -2), (dict(z=a[1:]), -4), (dict(stats=a[1:]), -4), (dict(N=1, K=200000), -5), (dict(N=1 << 24), -2)]:
+        with pytest.raises(B.VggError) as e:
+            B.vgg_log_probs(**{**ok, **change})
+        assert e.value.status == status, change
+    with pytest.raises(B.VggError):
+        B.vgg_log_probs(**{**ok, "K": 200, "top": 65})
+    ok = dict(dtype=B.F32, N=2, K=10, z=a, labels=i, stats=a, entropy=a, g_logp=a, g_entropy=a, dz=a[1024:])
+    for change, status in [(dict(stats=None), -1), (dict(g_logp=None, g_entropy=None), -1), (dict(labels=None), -1), (dict(entropy=None), -1),
+                           (dict(dtype=-1), -3), (dict(lddz=9), -2), (dict(dz=a, lddz=12), -2), (dict(dz=a[2:]), -4)]:
+        with pytest.raises(B.VggError) as e:
+            B.vgg_log_probs_bwd(**{**ok, **change})
+        assert e.value.status == status, change
+
+
+def test_on_another_stream_and_in_a_graph():
+    z, labels = scores(B.BF16, 3, 30011, 8)
+    c, d = Call(B.BF16, z, labels, 10).run(), Call(B.BF16, z, labels, 10)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        d.run()
+    torch.cuda.synchronize()
+    same = lambda: torch.equal(c.top_idx, d.top_idx) and torch.equal(c.logp, d.logp) and torch.equal(c.entropy, d.entropy)  # noqa: E731
+    assert same()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        d.run()
+    for k in range(3):
+        fresh, _ = scores(B.BF16, 3, 30011, 20 + k)
+        c.z.copy_(fresh.to(torch.bfloat16))
+        d.z.copy_(c.z)
+        c.run()
+        d.ws.fill_(0xFF)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert same(), k
