@@ -8,8 +8,10 @@
 // that they are held times 2^14, below f16's largest, and need no other scale; f16 then keeps 11 bits of everything down to
 // 2^-28.  PLANES = 2 (VGG_F32): a value is two f16 numbers, the nearest and what that leaves, 22 bits; hi hi + hi lo + lo hi
 // leaves out 2^-22 of a product at most.  PLANES = 1 (VGG_BF16): operands are rounded to 11 bits.  In both the term a X adds an
-// fp32 copy of X: a rounding of X there would grow 3.4-fold in every later step where X has no (or small) singular values, while
-// what the products' rounding adds lies in the space that X spans.
+// fp32 copy of X, since a rounding of X there would grow 3.4-fold in every later step where X has no (or small) singular values;
+// and the diagonals of G and P, which hold most of them, are kept apart in fp32 (zeros in the planes): with G = D + E,
+//     (G G)_ij = (E E)_ij + (d_i + d_j) e_ij,   (G G)_ii = (E E)_ii + d_i^2,   (P X)_i = p_i X_i + (the rest of P) X.
+// One plane is then 3e-4 to 1e-3 off in all, against 1.3e-3 to 2.4e-3 with the diagonals rounded (bf16's own rounding: 1.7e-3).
 //
 // All products are "row times row": C[i][j] = sum_k A[i][k] B[j][k].  G: rows of X; G G: rows of the symmetric G; P X: rows of P
 // and of X^T, for which X is also kept transposed.  An operand's row holds, for every 32 contraction indices, 64 bytes of the
@@ -91,7 +93,8 @@ struct Layout {
     int rows, cols, m, n, mp, np, tall;
     float *x32;            // [batch][mp][np]
     half_t *x, *xt[2];     // [batch][mp][np], [batch][np][mp], PLANES each
-    half_t *g, *p;         // [batch][mp][mp], PLANES each
+    half_t *g, *p;         // [batch][mp][mp], PLANES each, zero diagonals
+    float *gd, *pd;        // [batch][mp], the diagonals
     double *part;          // [batch][kParts]
 };
 template <typename T, int PL>
@@ -215,17 +218,21 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(Layout L, int from
                 const int i = ti * 128 + wi + x * 32 + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3), j = tj * 128 + wj + y * 32 + (lane & 31);
                 const float c = acc[x][y][v];
                 if constexpr (MODE == kGram) {
-                    half_t *g = L.g + b * mm * PL;
-                    put<PL>(g + (size_t)i * L.mp * PL, j, c * kDown);
-                    if (ti != tj) put<PL>(g + (size_t)j * L.mp * PL, i, c * kDown);
+                    half_t *gm = L.g + b * mm * PL;
+                    if (i == j) L.gd[(size_t)b * L.mp + i] = c * (kDown * kDown);
+                    put<PL>(gm + (size_t)i * L.mp * PL, j, i == j ? 0.f : c * kDown);
+                    if (ti != tj) put<PL>(gm + (size_t)j * L.mp * PL, i, c * kDown);
                 } else if constexpr (MODE == kPoly) {
-                    const float w = kB * get<PL>(L.g + b * mm * PL + (size_t)i * L.mp * PL, j) + kC * (c * kDown);
-                    half_t *p = L.p + b * mm * PL;
-                    put<PL>(p + (size_t)i * L.mp * PL, j, w);
-                    if (ti != tj) put<PL>(p + (size_t)j * L.mp * PL, i, w);
+                    const float *gd = L.gd + (size_t)b * L.mp;
+                    const float di = gd[i], dj = gd[j];
+                    const float w = __builtin_fmaf(kC, c * kDown, __builtin_fmaf(kC, di + dj, kB) * get<PL>(L.g + b * mm * PL + (size_t)i * L.mp * PL, j));
+                    half_t *pm = L.p + b * mm * PL;
+                    if (i == j) L.pd[(size_t)b * L.mp + i] = __builtin_fmaf(kC, __builtin_fmaf(di, di, c * (kDown * kDown)), kB * di);
+                    put<PL>(pm + (size_t)i * L.mp * PL, j, i == j ? 0.f : w);
+                    if (ti != tj) put<PL>(pm + (size_t)j * L.mp * PL, i, w);
                 } else {
                     float *x32 = L.x32 + b * mn + (size_t)i * L.np + j;
-                    const float w = __builtin_fmaf(kA, *x32, c * (kDown * kDown));
+                    const float w = __builtin_fmaf(kA + L.pd[(size_t)b * L.mp + i], *x32, c * (kDown * kDown));
                     if constexpr (MODE == kApply) {
                         *x32 = w;
                         put<PL>(L.x + b * mn * PL + (size_t)i * L.np * PL, j, w * kUp);
@@ -254,6 +261,8 @@ Layout layout_of(int planes, int batch, int rows, int cols, char *ws, size_t &to
     for (int k = 0; k < 2; ++k) L.xt[k] = reinterpret_cast<half_t *>(take(mn * 2 * planes));
     L.g = reinterpret_cast<half_t *>(take(mm * 2 * planes));
     L.p = reinterpret_cast<half_t *>(take(mm * 2 * planes));
+    L.gd = reinterpret_cast<float *>(take((size_t)batch * L.mp * 4));
+    L.pd = reinterpret_cast<float *>(take((size_t)batch * L.mp * 4));
     total = off;
     return L;
 }

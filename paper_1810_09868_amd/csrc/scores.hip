@@ -1,12 +1,13 @@
 // Class scores to log probabilities: of given classes, with every row's entropy and most likely alternatives, and the
 // gradient of the first two with respect to the scores.
 //
-// One pass over a row keeps, with d = z - m and m the largest score so far, the sums S = sum exp(d) and T = sum d exp(d); a
-// larger score rescales both (S' = r S, T' = r (T + (m - m') S), r = exp(m - m')).  Then
-//     log p_j = (z_j - m) - log S,   entropy = log S - T / S.
-// m and log S are kept apart (stats): their sum would round what the gradient takes the exponential of.
+// One pass over a row keeps, with d = z - m and m the largest score so far, E = sum exp(d) over all scores but one of the largest,
+// and T = sum d exp(d); a larger score rescales both (S = 1 + E; E' = r S, T' = r (T + (m - m') S), r = exp(m - m')).  Then
+//     log p_j = (z_j - m) - log S,   log S = log1p(E),   entropy = log S - T / S,
+// E without the largest's own 1, so that the log probability of a class that is all but certain, -E, keeps its digits.  m and
+// log S are kept apart (stats): their sum would round what the gradient takes the exponential of.
 // All sums are fp32.  A score of -inf has d = -inf and exp(d) = 0; only its product d exp(d) has to be kept from NaN.
-// A NaN, or a +inf (whose d is NaN), makes S and with it everything of its row NaN.
+// A NaN makes E, and it or a +inf everything of its row NaN.
 #include "common.h"
 
 namespace vgg {
@@ -17,28 +18,39 @@ constexpr float kLowest = -3.402823466e38f;
 constexpr float kNothing = -1e4f;   // exp of it is 0, and no product with it overflows
 constexpr int kMaxTop = 64;   // one alternative to a lane
 
-struct Sums { float m, s, t; };   // of no scores: -inf, 0, 0
+struct Sums { float m, e, t; };   // of no scores: -inf, 0, 0
 
-// The factor and shift that bring sums over to a larger maximum M.
+// E and T of sums that are not the largest's (or are, but count its 1), brought over to the maximum M.
 __device__ __forceinline__ void rebase(Sums &a, float M)
 {
-    const float d = fmaxf(a.m - M, kNothing);
-    const float r = a.m == M ? 1.f : expf(d);
-    a.t = r * (a.t + (a.s > 0.f && a.m != M ? d * a.s : 0.f));
-    a.s *= r;
+    const float d = a.m == M ? 0.f : fmaxf(a.m - M, kNothing), r = expf(d), s = a.e + (a.m > -INFINITY ? 1.f : 0.f);
+    a.t = r * __builtin_fmaf(d, s, a.t);
+    a.e = r * s;
     a.m = M;
 }
 __device__ __forceinline__ Sums joined(Sums a, Sums b)
 {
-    const float M = fmaxf(a.m, b.m);
-    rebase(a, M);
-    rebase(b, M);
-    return {M, a.s + b.s, a.t + b.t};
+    if (b.m > a.m) { const Sums c = a; a = b; b = c; }
+    rebase(b, a.m);
+    return {a.m, a.e + b.e, a.t + b.t};
 }
+
 // Sums and maxima over a wave without LDS: rotations within 16 lanes, then quarters and halves that change places.
 template <int N> __device__ __forceinline__ float row_ror(float x)
 {
     return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + N, 0xf, 0xf, true));
+}
+template <typename F> __device__ __forceinline__ float quarters(float v, F f)
+{
+    const auto q = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    const unsigned q0 = q[0], q1 = q[1];
+    return f(__uint_as_float(q0), __uint_as_float(q1));
+}
+template <typename F> __device__ __forceinline__ float halves(float v, F f)
+{
+    const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    const unsigned h0 = h[0], h1 = h[1];
+    return f(__uint_as_float(h0), __uint_as_float(h1));
 }
 template <typename F> __device__ __forceinline__ float wave_all(float v, F f)
 {
@@ -46,35 +58,40 @@ template <typename F> __device__ __forceinline__ float wave_all(float v, F f)
     v = f(v, row_ror<4>(v));
     v = f(v, row_ror<2>(v));
     v = f(v, row_ror<1>(v));
-    const auto q = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    const unsigned q0 = q[0], q1 = q[1];
-    v = f(__uint_as_float(q0), __uint_as_float(q1));
-    const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    const unsigned h0 = h[0], h1 = h[1];
-    return f(__uint_as_float(h0), __uint_as_float(h1));
+    return halves(quarters(v, f), f);
 }
 __device__ __forceinline__ float all_max(float v) { return wave_all(v, [](float a, float b) { return fmaxf(a, b); }); }
 __device__ __forceinline__ float all_min(float v) { return wave_all(v, [](float a, float b) { return fminf(a, b); }); }
 __device__ __forceinline__ float all_sum(float v) { return wave_all(v, [](float a, float b) { return a + b; }); }
-__device__ __forceinline__ Sums wave_joined(Sums a)
+__device__ __forceinline__ Sums wave_joined(Sums a, int lane)
 {
     const float M = all_max(a.m);
-    rebase(a, M);
-    return {M, all_sum(a.s), all_sum(a.t)};
+    if (lane != __builtin_ctzll(__ballot(a.m == M) | 1ull << 63)) rebase(a, M);   // (the first with the largest keeps its E)
+    return {M, all_sum(a.e), all_sum(a.t)};
 }
 
 // V scores, `most` the largest, into a thread's sums.
 template <int V> __device__ __forceinline__ void add_scores(Sums &a, const float (&z)[V], float most)
 {
-    const float M = fmaxf(a.m, most);
-    if (M > a.m) rebase(a, M);
-    const float base = M == -INFINITY ? 0.f : M;
+    bool fresh = most > a.m;
+    if (fresh) rebase(a, most);
+    const float base = a.m == -INFINITY ? 0.f : a.m;
+    float e[V];
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        const float d = z[j] - base, e = __expf(d);
-        a.s += e;
-        a.t = __builtin_fmaf(fmaxf(d, kLowest), e, a.t);
+        const float d = z[j] - base;
+        e[j] = __expf(d);
+        a.t = __builtin_fmaf(fmaxf(d, kLowest), e[j], a.t);
     }
+    if (__any(fresh))
+#pragma unroll
+        for (int j = 0; j < V; ++j) {       // one of the new largest does not count
+            const bool it = fresh && z[j] == a.m;
+            e[j] = it ? 0.f : e[j];
+            fresh = fresh && !it;
+        }
+#pragma unroll
+    for (int j = 0; j < V; ++j) a.e += e[j];
 }
 
 // A score and its class as one number: the better, the larger; equal scores: the lower class.  0: none.
@@ -159,6 +176,7 @@ __device__ __forceinline__ void cut(Best &b, int lane)
 }
 __device__ __forceinline__ void offer(Best &b, float v, int id, int lane)
 {
+    if (!__any(v >= b.worst_v)) return;
     const Key mask = __ballot(may_enter(b, v, id));
     if (!mask) return;
     const int at = b.count + __builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, 0));
@@ -204,45 +222,46 @@ struct ScoreArgs {
     Key *part_best;               // [N][parts][top], best first, 0 where there are fewer
 };
 
-// Log of a row's sum; -inf where it has no class.
-__device__ __forceinline__ float log_sum(const Sums &r) { return r.m == -INFINITY && r.s == 0.f ? -INFINITY : logf(r.s); }
+// Log of a row's sum: -inf where it has no class, NaN with a NaN or +inf.
+__device__ __forceinline__ float log_sum(const Sums &r) { return r.m == -INFINITY && r.e == 0.f ? -INFINITY : r.m < INFINITY ? log1pf(r.e) : NAN; }
 __device__ __forceinline__ void write_row(const ScoreArgs &a, const Sums &r, float z_label, int y, int row)
 {
     const float log_s = log_sum(r);
     const bool empty = log_s == -INFINITY;
     if (a.logp) a.logp[row] = y < 0 || y >= a.K ? 0.f : empty ? -INFINITY : (z_label - r.m) - log_s;
-    if (a.entropy) a.entropy[row] = empty ? 0.f : log_s - r.t / r.s;
+    if (a.entropy) a.entropy[row] = empty ? 0.f : log_s - r.t / (1.f + r.e);
     if (a.stats) { a.stats[2 * (size_t)row] = r.m; a.stats[2 * (size_t)row + 1] = log_s; }
 }
 // Alternative i of a row: `k`, or none.
 __device__ __forceinline__ void write_best(const ScoreArgs &a, const Sums &r, int row, int i, Key k)
 {
-    const bool fine = r.s > 0.f;         // neither without a class nor NaN
+    const float log_s = log_sum(r);
+    const bool there = k && log_s > -INFINITY;       // (not with a NaN either)
     const size_t at = (size_t)row * a.top + i;
-    a.top_logp[at] = k && fine ? (score_of(k) - r.m) - log_sum(r) : fine || r.s == 0.f ? -INFINITY : r.s;
-    a.top_idx[at] = k && fine ? class_of(k) : -1;
+    a.top_logp[at] = there ? (score_of(k) - r.m) - log_s : log_s == log_s ? -INFINITY : log_s;
+    a.top_idx[at] = there ? class_of(k) : -1;
 }
-// The best of the waves' lists, `top` places each with `count` keys together: to each thread's key its place.
+// The best of W waves' lists, each in order: a thread finds its key's place among all by halving, in every list at a time.
 template <int W, typename F> __device__ __forceinline__ void merge_lists(const Key (*lists)[kList], const int *counts, int top, F write)
 {
     const int i = threadIdx.x, w = i / top, at = i - w * top;
-    int all = 0;
+    int count[W], all = 0;
 #pragma unroll
-    for (int k = 0; k < W; ++k) all += counts[k];
+    for (int k = 0; k < W; ++k) all += count[k] = counts[k];
     if (w < W && at < counts[w]) {
         const Key mine = lists[w][at];
-        int rank = at;                   // (its own list is in order)
+        int before[W] = {};
+        for (int step = 64; step > 0; step >>= 1) {
+            if (step > top) continue;
 #pragma unroll
-        for (int k = 0; k < W; ++k) {
-            if (k == w) continue;
-            int lo = 0, hi = counts[k];  // better ones in list k
-            while (lo < hi) {
-                const int mid = (lo + hi) / 2;
-                if (lists[k][mid] > mine) lo = mid + 1;
-                else hi = mid;
+            for (int k = 0; k < W; ++k) {
+                const int next = before[k] + step;
+                if (next <= count[k] && lists[k][next - 1] > mine) before[k] = next;
             }
-            rank += lo;
         }
+        int rank = 0;
+#pragma unroll
+        for (int k = 0; k < W; ++k) rank += before[k];
         if (rank < top) write(rank, mine);
     }
     if (i < top && i >= all) write(i, (Key)0);
@@ -297,12 +316,17 @@ __global__ __launch_bounds__(256) void log_probs_kernel(const T *__restrict__ z,
         if constexpr (TOP)
             if (i0 == ti) expect(b, fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])));
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            add_scores<V>(mine, x[u], most[u]);
-            if constexpr (TOP)
-                if (__ballot(most[u] >= b.worst_v && most[u] > -INFINITY))
+        for (int u = 0; u < U; ++u) add_scores<V>(mine, x[u], most[u]);
+        if constexpr (TOP) {
+            const float lot = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
+            if (__ballot(lot >= b.worst_v && lot > -INFINITY)) {
 #pragma unroll
-                    for (int j = 0; j < V; ++j) offer(b, x[u][j], v0 + (i0 + u * tn) * V + j, lane);
+                for (int u = 0; u < U; ++u)
+                    if (__ballot(most[u] >= b.worst_v))
+#pragma unroll
+                        for (int j = 0; j < V; ++j) offer(b, x[u][j], v0 + (i0 + u * tn) * V + j, lane);
+                if (b.count > b.top + 24 && i0 - ti + U * tn < nvec) cut(b, lane);   // (what follows meets a higher bar)
+            }
         }
     }
     {
@@ -310,7 +334,7 @@ __global__ __launch_bounds__(256) void log_probs_kernel(const T *__restrict__ z,
         add_scores<1>(mine, x, ends);
         if constexpr (TOP) offer(b, ends, end_k, lane);
     }
-    mine = wave_joined(mine);
+    mine = wave_joined(mine, lane);
     if constexpr (TOP) cut(b, lane);
 
     if constexpr (W == 1) {
@@ -330,7 +354,7 @@ __global__ __launch_bounds__(256) void log_probs_kernel(const T *__restrict__ z,
             return;
         }
         const size_t at = (size_t)row * a.parts + part;
-        if (threadIdx.x == 0) { a.part_sums[at * 3] = mine.m; a.part_sums[at * 3 + 1] = mine.s; a.part_sums[at * 3 + 2] = mine.t; }
+        if (threadIdx.x == 0) { a.part_sums[at * 3] = mine.m; a.part_sums[at * 3 + 1] = mine.e; a.part_sums[at * 3 + 2] = mine.t; }
         if constexpr (TOP) merge_lists<W>(lists, counts, a.top, [&](int i, Key k) { a.part_best[at * a.top + i] = k; });
     }
 }
@@ -350,7 +374,7 @@ __global__ __launch_bounds__(256) void log_probs_join_kernel(const T *__restrict
         const float *s = a.part_sums + ((size_t)row * a.parts + p) * 3;
         mine = joined(mine, {s[0], s[1], s[2]});
     }
-    mine = wave_joined(mine);
+    mine = wave_joined(mine, lane);
     Best b = {lists[TOP ? wave : 0], 0, a.top, -INFINITY, -1};
     if constexpr (TOP) {
         const int n = a.parts * a.top;
@@ -426,6 +450,7 @@ __global__ __launch_bounds__(256) void log_probs_bwd_kernel(const T *z, T *dz, G
     }
 }
 
+constexpr int kOneWave = 1024;   // scores that one wave takes by itself (16 x 2048, top 5: 9.9 us so, 7.1 us with four waves)
 struct Split { int parts, span; };
 // Rows that are too few to fill the chip are cut into parts of at least 4096 scores.
 Split split_rows(int N, int K)
@@ -446,19 +471,13 @@ size_t log_probs_workspace(int N, int K, int top)
     return round_up((size_t)N * s.parts * (3 * sizeof(float) + top * sizeof(Key)) + sizeof(Key), 256);
 }
 
-template <typename T>
-static int log_probs_of(const T *z, ScoreArgs a, hipStream_t s)
+template <typename T, bool TOP>
+static int log_probs_of(const T *z, const ScoreArgs &a, hipStream_t s)
 {
-    const dim3 one((unsigned)(((size_t)a.N + 3) / 4));
-    const bool small = a.K <= 2048;
-    if (small && a.top) hipLaunchKernelGGL((log_probs_kernel<T, 1, true>), one, dim3(256), 0, s, z, a);
-    else if (small) hipLaunchKernelGGL((log_probs_kernel<T, 1, false>), one, dim3(256), 0, s, z, a);
-    else if (a.top) hipLaunchKernelGGL((log_probs_kernel<T, 4, true>), dim3((unsigned)a.N * a.parts), dim3(256), 0, s, z, a);
-    else hipLaunchKernelGGL((log_probs_kernel<T, 4, false>), dim3((unsigned)a.N * a.parts), dim3(256), 0, s, z, a);
-    if (a.parts > 1) {
-        if (a.top) hipLaunchKernelGGL((log_probs_join_kernel<T, true>), dim3(a.N), dim3(256), 0, s, z, a);
-        else hipLaunchKernelGGL((log_probs_join_kernel<T, false>), dim3(a.N), dim3(256), 0, s, z, a);
-    }
+    const unsigned units = (unsigned)a.N * a.parts;
+    if (a.K <= kOneWave) hipLaunchKernelGGL((log_probs_kernel<T, 1, TOP>), dim3((units + 3) / 4), dim3(256), 0, s, z, a);
+    else hipLaunchKernelGGL((log_probs_kernel<T, 4, TOP>), dim3(units), dim3(256), 0, s, z, a);
+    if (a.parts > 1) hipLaunchKernelGGL((log_probs_join_kernel<T, TOP>), dim3(a.N), dim3(256), 0, s, z, a);
     return launch_status();
 }
 
@@ -473,8 +492,12 @@ int log_probs(int dtype, int N, int K, size_t ldz, const void *z, const int32_t 
         a.part_best = static_cast<Key *>(ws);
         a.part_sums = reinterpret_cast<float *>(a.part_best + n * top);
     }
-    if (dtype == VGG_BF16) return log_probs_of(static_cast<const bf16_t *>(z), a, s);
-    return log_probs_of(static_cast<const float *>(z), a, s);
+    if (dtype == VGG_BF16) {
+        const bf16_t *zb = static_cast<const bf16_t *>(z);
+        return top ? log_probs_of<bf16_t, true>(zb, a, s) : log_probs_of<bf16_t, false>(zb, a, s);
+    }
+    const float *zf = static_cast<const float *>(z);
+    return top ? log_probs_of<float, true>(zf, a, s) : log_probs_of<float, false>(zf, a, s);
 }
 
 template <typename T>

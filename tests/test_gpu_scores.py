@@ -243,6 +243,21 @@ def test_offsets_scores_by_thousands_without_loss():
     assert np.abs(dz - want).max() <= 3e-6
 
 
+@pytest.mark.parametrize("K", [2, 1000, 5000, 70001])
+def test_a_class_that_is_all_but_certain_keeps_its_digits(K):
+    # log p of the best class is -log1p(E), E the other classes' sum (here 1e-5 to 1e-9): relative to it, not to 1
+    z = torch.zeros((3, K))
+    for n in range(3):
+        z[n, K // 2 + n - 1 if K > 4 else 0] = float(np.log(K)) + 12 + 4 * n
+    labels = z.argmax(1).int().numpy()
+    c = Call(B.F32, z, labels, 1).run()
+    torch.cuda.synchronize()
+    E = (K - 1) * np.exp(-z.double().max(1).values.numpy())
+    want_h = np.log1p(E) + z.double().max(1).values.numpy() * E / (1 + E)
+    for got, want in ((c.logp, -np.log1p(E)), (c.top_logp[:, 0], -np.log1p(E)), (c.entropy, want_h)):
+        assert np.abs(got.double().cpu().numpy() / want - 1).max() < 4e-6
+
+
 def test_results_that_are_not_wanted_are_not_needed():
     z, labels = scores(B.BF16, 5, 777, 2)
     c = Call(B.BF16, z, labels, 4).run()
