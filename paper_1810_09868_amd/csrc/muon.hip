@@ -13,9 +13,10 @@
 //     (G G)_ij = (E E)_ij + (d_i + d_j) e_ij,   (G G)_ii = (E E)_ii + d_i^2,   (P X)_i = p_i X_i + (the rest of P) X.
 // One plane is then 3e-4 to 1e-3 off in all, against 1.3e-3 to 2.4e-3 with the diagonals rounded (bf16's own rounding: 1.7e-3).
 //
-// All products are "row times row": C[i][j] = sum_k A[i][k] B[j][k].  G: rows of X; G G: rows of the symmetric G; P X: rows of P
-// and of X^T, for which X is also kept transposed.  An operand's row holds, for every 32 contraction indices, 64 bytes of the
-// first plane and then of the second.
+// X, G and P lie by rows, a row's every 32 elements 64 bytes of the first plane and then of the second.  G and G G contract along
+// rows of both operands; P X takes X's columns, which LDS hands out transposed (ds_read_b64_tr_b16), so that X is kept once.  X is
+// padded with zeros to whole tiles.  G and P are symmetric: the tiles on and below the diagonal are formed, over a few ranges of
+// the contraction where they are too few to fill the chip, and a second kernel adds the ranges in order and mirrors them.
 #include "common.h"
 
 namespace vgg {
@@ -27,10 +28,7 @@ typedef _Float16 half_t;
 
 constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f, kEps = 1e-7f;
 constexpr float kUp = 16384.f, kDown = 1.f / 16384.f;   // 2^14
-constexpr int kTile = 128;                              // every padded size is a multiple of it
-constexpr int kParts = 256;                             // partial sums of squares of a matrix
-
-__host__ __device__ inline int padded(int v) { return (v + kTile - 1) / kTile * kTile; }
+constexpr int kParts = 1024;                            // partial sums of squares of a matrix
 
 // Element k of a row of K-blocks of 32 with PL planes.
 template <int PL> __device__ __forceinline__ size_t at_plane(int k, int plane) { return (size_t)(k >> 5) * (32 * PL) + plane * 32 + (k & 31); }
@@ -77,48 +75,78 @@ template <typename T> __device__ __forceinline__ float source_at(const Source &s
 template <typename T>
 __global__ __launch_bounds__(256) void muon_norm_kernel(Source s, double *__restrict__ part, size_t count)
 {
-    const size_t base = (size_t)blockIdx.y * count;
+    constexpr int U = 8;                                // loads in flight
+    const size_t base = (size_t)blockIdx.y * count, step = (size_t)gridDim.x * 256;
+    const T *x = static_cast<const T *>(s.x) + base;
+    float *mom = s.momentum ? s.momentum + base : nullptr;
     double sum = 0;
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < count; i += (size_t)kParts * 256) {
-        if (s.momentum) s.momentum[base + i] = __builtin_fmaf(s.mu, s.momentum[base + i], Elem<T>::load(static_cast<const T *>(s.x) + base + i));
-        const float u = source_at<T>(s, base + i);
-        sum += (double)u * u;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < count; i += U * step) {
+        float u[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) u[k] = i + k * step < count ? Elem<T>::load(x + i + k * step) : 0.f;
+        if (mom) {
+            float m[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) m[k] = i + k * step < count ? mom[i + k * step] : 0.f;
+#pragma unroll
+            for (int k = 0; k < U; ++k) {
+                m[k] = __builtin_fmaf(s.mu, m[k], u[k]);
+                if (i + k * step < count) mom[i + k * step] = m[k];
+                u[k] = s.nesterov ? __builtin_fmaf(s.mu, m[k], u[k]) : m[k];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < U; ++k) sum = __builtin_fma((double)u[k], (double)u[k], sum);
     }
     sum = block_sum(sum);
     if (threadIdx.x == 0) part[blockIdx.y * kParts + blockIdx.x] = sum;
 }
 
-// X_0 in all its layouts, zeros where they are padded.  A workgroup: 64 x 64 of the padded X.
+// What a call works on.
 struct Layout {
-    int rows, cols, m, n, mp, np, tall;
+    int rows, cols, m, n, mp, np, tall, tile, parts, batch;   // tile: of the products, 128 or 256, which mp and np are multiples of
+    int splits[2];         // of the Gram matrix and its square
     float *x32;            // [batch][mp][np]
-    half_t *x, *xt[2];     // [batch][mp][np], [batch][np][mp], PLANES each
+    half_t *x[2];          // [batch][mp][np], PLANES each
     half_t *g, *p;         // [batch][mp][mp], PLANES each, zero diagonals
     float *gd, *pd;        // [batch][mp], the diagonals
+    float *sums;           // [batch][tiles][splits][tile][tile]
     double *part;          // [batch][kParts]
 };
+
+// X_0 in all its forms, zeros where they are padded.  A workgroup: 64 x 64 of the padded X.
 template <typename T, int PL>
 __global__ __launch_bounds__(256) void muon_start_kernel(Source s, Layout L)
 {
     __shared__ float tile[64][65];
     const int b = blockIdx.z, i0 = blockIdx.y * 64, j0 = blockIdx.x * 64, tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
-    const double norm2 = block_sum(L.part[b * kParts + threadIdx.x]);
-    const float by = norm2 < (double)INFINITY ? 1.f / ((float)sqrt(norm2) + kEps) : NAN;
     const size_t base = (size_t)b * L.rows * L.cols;
     // the source is read along its own rows
-    for (int y = ty; y < 64; y += 4) {
-        const int i = L.tall ? i0 + tx : i0 + y, j = L.tall ? j0 + y : j0 + tx;      // of X
-        const float v = i < L.m && j < L.n ? source_at<T>(s, base + (L.tall ? (size_t)j * L.cols + i : (size_t)i * L.cols + j)) * by : 0.f;
-        if (L.tall) tile[tx][y] = v;
-        else tile[y][tx] = v;
+    float v[16];
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        const int y = ty + 4 * k, i = L.tall ? i0 + tx : i0 + y, j = L.tall ? j0 + y : j0 + tx;      // of X
+        v[k] = i < L.m && j < L.n ? source_at<T>(s, base + (L.tall ? (size_t)j * L.cols + i : (size_t)i * L.cols + j)) : 0.f;
     }
-    __syncthreads();
+    double norm2 = 0;
+    for (int k = threadIdx.x; k < L.parts; k += 256) norm2 += L.part[b * kParts + k];
+    norm2 = block_sum(norm2);
+    const double by = norm2 < (double)INFINITY ? 1. / (sqrt(norm2) + (double)kEps) : (double)NAN;   // (its product with fp32's largest is none of fp32's zeros)
     float *x32 = L.x32 + (size_t)b * L.mp * L.np;
-    half_t *x = L.x + (size_t)b * L.mp * L.np * PL, *xt = L.xt[0] + (size_t)b * L.mp * L.np * PL;
-    for (int y = ty; y < 64; y += 4) {
-        x32[(size_t)(i0 + y) * L.np + j0 + tx] = tile[y][tx];
-        put<PL>(x + (size_t)(i0 + y) * L.np * PL, j0 + tx, tile[y][tx] * kUp);
-        put<PL>(xt + (size_t)(j0 + y) * L.mp * PL, i0 + tx, tile[tx][y] * kUp);
+    half_t *x = L.x[0] + (size_t)b * L.mp * L.np * PL;
+    if (L.tall) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) tile[tx][ty + 4 * k] = v[k];
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 16; ++k) v[k] = tile[ty + 4 * k][tx];
+    }
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        const int y = ty + 4 * k;
+        const float w = (float)(v[k] * by);
+        x32[(size_t)(i0 + y) * L.np + j0 + tx] = w;
+        put<PL>(x + (size_t)(i0 + y) * L.np * PL, j0 + tx, w * kUp);
     }
 }
 
@@ -134,71 +162,126 @@ struct Target {
 
 __device__ __forceinline__ void copy16(unsigned lds, const void *src)   // 16 bytes a lane to lds + 16 lane
 {
-    const unsigned at = __builtin_amdgcn_readfirstlane(lds);
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(at), "v"(src) : "m0", "memory");
+    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds), "v"(src) : "m0", "memory");
+}
+typedef __attribute__((address_space(3))) char lds_char;
+
+// Workgroups go round the eight XCDs; each takes a run of the work, so that neighbours share their operands in its L2.
+__device__ __forceinline__ int spread(int id, int count)
+{
+    const int per = count >> 3, more = count & 7, xcd = id & 7, at = id >> 3;
+    return xcd * per + (xcd < more ? xcd : more) + at;
 }
 
-// A workgroup of four waves: 128 x 128 of C, 64 x 64 to a wave.  128 bytes of each operand row a stage (64 contraction indices,
-// or 32 in two planes), two stages in LDS; 16-byte segment s of row r lies at s ^ (r & 7), so that eight rows of one segment are
-// in different banks.
-template <typename T, int PL, int MODE>
-__global__ __launch_bounds__(256, 2) void muon_product_kernel(Layout L, int from, Target out)
+// A workgroup of eight waves (2 x 4): TILE x TILE of C = A B^T (kGram, kPoly) or A B (kApply, kLast).  A stage is 128 bytes of
+// every row of A (64 contraction indices, or 32 in two planes), and as many rows or bytes of B; STAGES of them in LDS, all but one
+// on their way (128 KB, one workgroup to a compute unit).  A 16-byte segment s of a row r of A lies at s ^ (r & 7), so that eight
+// rows of one segment are in different banks; a 64-byte block c of a row r of B that is read transposed at c ^ (r & 3), for the
+// four rows that sixteen lanes read.  256 x 256 tiles take 2/3 of the LDS traffic of 128 x 128 ones, and four times the work.
+template <typename T, int PL, int MODE, int TILE>
+__global__ __launch_bounds__(512) void muon_product_kernel(Layout L, int from, Target out)
 {
-    extern __shared__ __align__(16) char lds[];   // [2][A 16 KB, B 16 KB]
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = blockIdx.z;
-    int ti = blockIdx.y, tj = blockIdx.x;
-    if constexpr (MODE == kGram || MODE == kPoly) {   // tiles on and below the diagonal, counted row by row
-        const int t = blockIdx.x;
+    extern __shared__ __align__(16) char lds[];   // [STAGES][A, B: TILE x 128 bytes each]
+    constexpr bool TR = MODE == kApply || MODE == kLast;
+    constexpr int STAGES = TILE == 256 ? 2 : 4, HALF = TILE * 128, BX = TILE / 64, BY = TILE / 128, COPIES = TILE / 64, KS = 64 / PL;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = blockIdx.y;
+    const int mt = L.mp / TILE, nt = L.np / TILE;
+    int ti, tj, split = 0;
+    const int unit = spread(blockIdx.x, gridDim.x);
+    if constexpr (TR) {                           // eight tiles down, then one to the right
+        const int wide = 8 * nt, group = unit / wide, in = unit - group * wide, rows = mt - group * 8 < 8 ? mt - group * 8 : 8;
+        ti = group * 8 + in % rows;
+        tj = in / rows;
+    } else {                                      // tiles on and below the diagonal, row by row
+        const int tiles = mt * (mt + 1) / 2;
+        split = unit / tiles;
+        const int t = unit - split * tiles;
         ti = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
         while ((ti + 1) * (ti + 2) / 2 <= t) ++ti;
         while (ti * (ti + 1) / 2 > t) --ti;
         tj = t - ti * (ti + 1) / 2;
     }
     const size_t mm = (size_t)L.mp * L.mp, mn = (size_t)L.mp * L.np;
-    const int K = MODE == kGram ? L.np : L.mp;
-    const size_t row_bytes = (size_t)K * PL * 2;
-    const half_t *pa = MODE == kGram ? L.x + b * mn * PL : MODE == kPoly ? L.g + b * mm * PL : L.p + b * mm * PL;
-    const half_t *pb = MODE == kGram ? pa : MODE == kPoly ? pa : L.xt[from] + b * mn * PL;
-    const char *ga = reinterpret_cast<const char *>(pa) + (size_t)ti * 128 * row_bytes;
-    const char *gb = reinterpret_cast<const char *>(pb) + (size_t)tj * 128 * row_bytes;
-    const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
-    const int stages = (int)(row_bytes / 128);
+    const int K = MODE == kGram ? L.np : L.mp, all = K / KS;
+    const int splits = TR ? 1 : L.splits[MODE];
+    const int s0 = (int)((long)all * split / splits), stages = (int)((long)all * (split + 1) / splits) - s0;
+    const size_t row_bytes = (size_t)K * PL * 2, x_bytes = (size_t)L.np * PL * 2;
+    const half_t *pa = MODE == kGram ? L.x[from] + b * mn * PL : MODE == kPoly ? L.g + b * mm * PL : L.p + b * mm * PL;
+    const char *ga = reinterpret_cast<const char *>(pa) + (size_t)ti * TILE * row_bytes + (size_t)s0 * 128;
+    const char *gb = TR ? reinterpret_cast<const char *>(L.x[from] + b * mn * PL) + (size_t)tj * TILE * 2 * PL
+                        : reinterpret_cast<const char *>(pa) + (size_t)tj * TILE * row_bytes + (size_t)s0 * 128;
+    const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_char *)lds + wave * 1024);
 
-    auto stage_copy = [&](int st) __attribute__((always_inline)) {
-        const unsigned dst = lds0 + (st & 1) * 32768;
+    // where this thread's copies come from
+    const char *src_a[COPIES], *src_b[COPIES];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) {            // 8 rows of one operand each: waves 0, 1 copy A, waves 2, 3 B
-            const int r = (wave & 1) * 64 + q * 8 + (lane >> 3), seg = (lane & 7) ^ (r & 7);
-            copy16(dst + (wave >> 1) * 16384 + ((wave & 1) * 64 + q * 8) * 128, (wave >> 1 ? gb : ga) + r * row_bytes + (size_t)st * 128 + seg * 16);
+    for (int q = 0; q < COPIES; ++q) {
+        const int at = (q * 512 + (int)threadIdx.x) * 16, r = at >> 7, seg = ((at >> 4) & 7) ^ (r & 7);
+        src_a[q] = ga + (size_t)r * row_bytes + seg * 16;
+        if constexpr (TR) {
+            constexpr int RB = TILE * 2 * PL;      // bytes of a row of B's tile
+            const int k = at / RB, c = (at % RB >> 6) ^ (k & 3);
+            src_b[q] = gb + (size_t)k * x_bytes + c * 64 + (at & 63);
+        } else
+            src_b[q] = gb + (size_t)r * row_bytes + seg * 16;
+    }
+    const size_t step_b = TR ? (size_t)KS * x_bytes : 128;
+    int slot = 0;
+    auto stage_copy = [&] __attribute__((always_inline)) {
+        const unsigned dst = lds0 + slot * (2 * HALF);
+#pragma unroll
+        for (int q = 0; q < COPIES; ++q) {
+            copy16(dst + q * 8192, src_a[q]);
+            copy16(dst + HALF + q * 8192, src_b[q]);
+            src_a[q] += 128;
+            src_b[q] += step_b;
         }
+        slot = slot + 1 == STAGES ? 0 : slot + 1;
     };
 
-    f32x16 acc[2][2] = {};
-    const int wi = (wave >> 1) * 64, wj = (wave & 1) * 64;
-    stage_copy(0);
+    f32x16 acc[BX][BY] = {};
+    const int wi = (wave >> 2) * (TILE / 2), wj = (wave & 3) * (TILE / 4);
+    // this lane's part of a fragment's address: rows (of A, of B by rows), or the transposed read's
+    const int arow = wi + (lane & 31), brow = wj + (lane & 31), rx = lane & 7;
+    const int s16 = lane & 15, tr_k = 8 * (lane >> 5) + (s16 >> 2), tr_x = s16 >> 2, tr_at = (lane >> 4 & 1) * 32 + (s16 & 3) * 8;
+#pragma unroll
+    for (int k = 0; k < STAGES - 1; ++k)
+        if (k < stages) stage_copy();
+    int use = 0;
     for (int st = 0; st < stages; ++st) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-        if (st + 1 < stages) stage_copy(st + 1);
-        const char *A = lds + (st & 1) * 32768, *B = A + 16384;
-        auto frag = [&](const char *p, int row, int seg) __attribute__((always_inline)) {
-            return *reinterpret_cast<const f16x8 *>(p + row * 128 + ((seg ^ (row & 7)) << 4));
-        };
+        // this stage's copies have landed (those of the later ones may be on their way), and all waves are done with the last one
+        if (STAGES > 2 && st + STAGES - 2 < stages) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((STAGES - 2) * 2 * COPIES) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
+        if (st + STAGES - 1 < stages) stage_copy();
+        const char *A = lds + use * (2 * HALF), *B = A + HALF;
+        use = use + 1 == STAGES ? 0 : use + 1;
 #pragma unroll
         for (int k = 0; k < 4 / PL; ++k) {
-            f16x8 fa[PL][2], fb[PL][2];
+            f16x8 fa[PL][BX], fb[PL][BY];
 #pragma unroll
-            for (int p = 0; p < PL; ++p)
+            for (int p = 0; p < PL; ++p) {
+                const int seg = p * 4 + k * 2 + (lane >> 5);
 #pragma unroll
-                for (int q = 0; q < 2; ++q) {
-                    const int seg = p * 4 + k * 2 + (lane >> 5);
-                    fa[p][q] = frag(A, wi + q * 32 + (lane & 31), seg);
-                    fb[p][q] = frag(B, wj + q * 32 + (lane & 31), seg);
+                for (int q = 0; q < BX; ++q) fa[p][q] = *reinterpret_cast<const f16x8 *>(A + (arow + q * 32) * 128 + ((seg ^ rx) << 4));
+#pragma unroll
+                for (int q = 0; q < BY; ++q) {
+                    if constexpr (TR) {
+                        typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+                        typedef __fp16 fp16x4 __attribute__((__vector_size__(8)));
+                        const int c = ((wj >> 5) + q) * PL + p;
+                        const char *at = B + (k * 16 + tr_k) * (TILE * 2 * PL) + ((c ^ tr_x) << 6) + tr_at;
+                        typedef __attribute__((address_space(3))) fp16x4 lds_f16x4;
+                        const auto lo = __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_f16x4 *)at);
+                        const auto hi = __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_f16x4 *)(at + 4 * (TILE * 2 * PL)));
+                        fb[p][q] = __builtin_shufflevector(__builtin_bit_cast(f16x4, lo), __builtin_bit_cast(f16x4, hi), 0, 1, 2, 3, 4, 5, 6, 7);
+                    } else
+                        fb[p][q] = *reinterpret_cast<const f16x8 *>(B + (brow + q * 32) * 128 + ((seg ^ rx) << 4));
                 }
+            }
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
+            for (int x = 0; x < BX; ++x)
 #pragma unroll
-                for (int y = 0; y < 2; ++y) {
+                for (int y = 0; y < BY; ++y) {
                     if constexpr (PL == 2) {
                         acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[1][x], fb[0][y], acc[x][y], 0, 0, 0);
                         acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[0][x], fb[1][y], acc[x][y], 0, 0, 0);
@@ -209,62 +292,197 @@ __global__ __launch_bounds__(256, 2) void muon_product_kernel(Layout L, int from
     }
 
     // Value v of a block: row 8 (v / 4) + 4 (lane / 32) + v % 4, column lane % 32.
+    const int row0 = wi + 4 * (lane >> 5), col0 = wj + (lane & 31);
+    if constexpr (!TR) {
+        float *c = L.sums + (((size_t)b * (mt * (mt + 1) / 2) + ti * (ti + 1) / 2 + tj) * splits + split) * (TILE * TILE);
 #pragma unroll
-    for (int x = 0; x < 2; ++x)
+        for (int x = 0; x < BX; ++x)
 #pragma unroll
-        for (int y = 0; y < 2; ++y)
+            for (int y = 0; y < BY; ++y)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int i = ti * 128 + wi + x * 32 + 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3), j = tj * 128 + wj + y * 32 + (lane & 31);
-                const float c = acc[x][y][v];
-                if constexpr (MODE == kGram) {
-                    half_t *gm = L.g + b * mm * PL;
-                    if (i == j) L.gd[(size_t)b * L.mp + i] = c * (kDown * kDown);
-                    put<PL>(gm + (size_t)i * L.mp * PL, j, i == j ? 0.f : c * kDown);
-                    if (ti != tj) put<PL>(gm + (size_t)j * L.mp * PL, i, c * kDown);
-                } else if constexpr (MODE == kPoly) {
-                    const float *gd = L.gd + (size_t)b * L.mp;
-                    const float di = gd[i], dj = gd[j];
-                    const float w = __builtin_fmaf(kC, c * kDown, __builtin_fmaf(kC, di + dj, kB) * get<PL>(L.g + b * mm * PL + (size_t)i * L.mp * PL, j));
-                    half_t *pm = L.p + b * mm * PL;
-                    if (i == j) L.pd[(size_t)b * L.mp + i] = __builtin_fmaf(kC, __builtin_fmaf(di, di, c * (kDown * kDown)), kB * di);
-                    put<PL>(pm + (size_t)i * L.mp * PL, j, i == j ? 0.f : w);
-                    if (ti != tj) put<PL>(pm + (size_t)j * L.mp * PL, i, w);
+                for (int v = 0; v < 16; ++v) c[(row0 + x * 32 + 8 * (v >> 2) + (v & 3)) * TILE + col0 + y * 32] = acc[x][y][v];
+    } else {
+        const int i0 = ti * TILE + row0, j0 = tj * TILE + col0;
+#pragma unroll
+        for (int x = 0; x < BX; ++x) {
+            float pd[16];
+#pragma unroll
+            for (int v = 0; v < 16; ++v) pd[v] = kA + L.pd[(size_t)b * L.mp + i0 + x * 32 + 8 * (v >> 2) + (v & 3)];
+#pragma unroll
+            for (int y = 0; y < BY; ++y) {
+                const int j = j0 + y * 32;
+                float *x32 = L.x32 + b * mn + (size_t)(i0 + x * 32) * L.np + j;
+                float w[16];
+#pragma unroll
+                for (int v = 0; v < 16; ++v) w[v] = __builtin_fmaf(pd[v], x32[(size_t)(8 * (v >> 2) + (v & 3)) * L.np], acc[x][y][v] * (kDown * kDown));
+                if constexpr (MODE == kApply) {
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) x32[(size_t)(8 * (v >> 2) + (v & 3)) * L.np] = w[v];
+                    // a pair of rows and columns is shared out: even lanes take the first row's two columns, odd ones the second's
+                    const bool odd = lane & 1;
+#pragma unroll
+                    for (int v = 0; v < 16; v += 2) {
+                        const float mine = odd ? w[v + 1] : w[v], theirs = odd ? w[v] : w[v + 1];
+                        const float got = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(theirs), 0xB1, 0xf, 0xf, true));   // quad_perm 1 0 3 2
+                        const float c0 = (odd ? got : mine) * kUp, c1 = (odd ? mine : got) * kUp;
+                        half_t *to = L.x[1 - from] + (b * mn + (size_t)(i0 + x * 32 + 8 * (v >> 2) + (v & 3) + odd) * L.np) * PL + at_plane<PL>(j & ~1, 0);
+                        typedef half_t f16x2 __attribute__((ext_vector_type(2)));
+                        const f16x2 h = {(half_t)c0, (half_t)c1};
+                        *reinterpret_cast<f16x2 *>(to) = h;
+                        if constexpr (PL == 2) *reinterpret_cast<f16x2 *>(to + 32) = f16x2{(half_t)(c0 - (float)h[0]), (half_t)(c1 - (float)h[1])};
+                    }
                 } else {
-                    float *x32 = L.x32 + b * mn + (size_t)i * L.np + j;
-                    const float w = __builtin_fmaf(kA + L.pd[(size_t)b * L.mp + i], *x32, c * (kDown * kDown));
-                    if constexpr (MODE == kApply) {
-                        *x32 = w;
-                        put<PL>(L.x + b * mn * PL + (size_t)i * L.np * PL, j, w * kUp);
-                        put<PL>(L.xt[1 - from] + b * mn * PL + (size_t)j * L.mp * PL, i, w * kUp);
-                    } else if (i < L.m && j < L.n) {
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const int i = i0 + x * 32 + 8 * (v >> 2) + (v & 3);
+                        if (i >= L.m || j >= L.n) continue;
                         const size_t o = (size_t)b * L.rows * L.cols + (L.tall ? (size_t)j * L.cols + i : (size_t)i * L.cols + j);
-                        if (out.theta) out.theta[o] = __builtin_fmaf(-out.rate, w, out.keep * out.theta[o]);
-                        else Elem<T>::store(static_cast<T *>(out.out) + o, w);
+                        if (out.theta) out.theta[o] = __builtin_fmaf(-out.rate, w[v], out.keep * out.theta[o]);
+                        else Elem<T>::store(static_cast<T *>(out.out) + o, w[v]);
                     }
                 }
             }
+        }
+    }
+}
+
+// The ranges' sums to G, or to P = b G + c G G: 32 x 32 of a tile to a workgroup, and its mirror image.
+template <int PL, int MODE, int TILE>
+__global__ __launch_bounds__(256) void muon_symmetric_kernel(Layout L)
+{
+    __shared__ float turned[32][33];
+    constexpr int Q = TILE / 32;
+    const int b = blockIdx.y, t = blockIdx.x / (Q * Q), in = blockIdx.x - t * (Q * Q);
+    int ti = (int)((sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
+    while ((ti + 1) * (ti + 2) / 2 <= t) ++ti;
+    while (ti * (ti + 1) / 2 > t) --ti;
+    const int tj = t - ti * (ti + 1) / 2, mt = L.mp / TILE, splits = L.splits[MODE];
+    const int i0 = ti * TILE + in / Q * 32, j0 = tj * TILE + in % Q * 32;
+    const size_t mm = (size_t)L.mp * L.mp;
+    const int tx = threadIdx.x & 7, ty = threadIdx.x >> 3, i = i0 + ty, j = j0 + tx * 4;
+    const float *c = L.sums + ((size_t)b * (mt * (mt + 1) / 2) + t) * splits * (TILE * TILE) + (size_t)(in / Q * 32 + ty) * TILE + in % Q * 32 + tx * 4;
+    half_t *to = (MODE == kGram ? L.g : L.p) + b * mm * PL;
+    const half_t *g = L.g + b * mm * PL + (size_t)i * L.mp * PL;
+    float *gd = L.gd + (size_t)b * L.mp, *pd = L.pd + (size_t)b * L.mp;
+    typedef half_t f16x4 __attribute__((ext_vector_type(4)));
+    auto store = [&](int i, int j, const f32x4 &v) __attribute__((always_inline)) {
+        half_t *row = to + (size_t)i * L.mp * PL + at_plane<PL>(j, 0);
+        f16x4 h, l;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float w = i == j + k ? 0.f : v[k];
+            h[k] = (half_t)w;
+            l[k] = (half_t)(w - (float)h[k]);
+        }
+        *reinterpret_cast<f16x4 *>(row) = h;
+        if constexpr (PL == 2) *reinterpret_cast<f16x4 *>(row + 32) = l;
+    };
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    constexpr int U = 8;                           // sums on their way
+    for (int s = 0; s < splits; s += U) {
+        f32x4 u[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) u[k] = s + k < splits ? *reinterpret_cast<const f32x4 *>(c + (size_t)(s + k) * (TILE * TILE)) : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < U; ++k) v += u[k];
+    }
+    v *= kDown;
+    if constexpr (MODE == kGram) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (i == j + k) gd[i] = v[k] * kDown;
+    } else {
+        const float di = gd[i];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (i == j + k) pd[i] = __builtin_fmaf(kC, __builtin_fmaf(di, di, v[k] * kDown), kB * di);
+            v[k] = __builtin_fmaf(kC, v[k], __builtin_fmaf(kC, di + gd[j + k], kB) * get<PL>(g, j + k));
+        }
+    }
+    store(i, j, v);
+    if (ti == tj) return;                          // (all of a diagonal tile is formed)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) turned[tx * 4 + k][ty] = v[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = turned[ty][tx * 4 + k];
+    store(j0 + ty, i0 + tx * 4, v);
+}
+
+inline int round_to(int v, int to) { return (v + to - 1) / to * to; }
+
+// How many ranges a contraction of `all` stages is cut into for `tiles` workgroups each: rounds of the chip's 256 compute units
+// times what one takes, in cycles (a stage at the matrix unit's rate, some thousand to begin and end), and the sums' way through
+// memory.
+int split_count(int planes, int tile, long tiles, int all)
+{
+    const double stage = (tile == 256 ? 4 : 1) * (planes == 2 ? 768.0 : 512.0) * 1.3;
+    int best = 1;
+    double least = 0;
+    for (int s = 1; s <= 64 && s <= all; ++s) {
+        const double t = (double)((tiles * s + 255) / 256) * ((all + s - 1) / s * stage + 4000) + (double)tiles * s * tile * tile * 8 / 1600 + s * 150;
+        if (s == 1 || t < least) { least = t; best = s; }
+    }
+    return best;
 }
 
 Layout layout_of(int planes, int batch, int rows, int cols, char *ws, size_t &total)
 {
     Layout L;
-    L.rows = rows; L.cols = cols; L.tall = rows > cols;
+    L.rows = rows; L.cols = cols; L.tall = rows > cols; L.batch = batch;
     L.m = L.tall ? cols : rows; L.n = L.tall ? rows : cols;
-    L.mp = padded(L.m); L.np = padded(L.n);
+    // 256 x 256 tiles where the product with X takes no more of the chip's rounds with them (a tile is four times the work of a
+    // 128 x 128 one, in about 3.4 times its time)
+    auto rounds = [&](int t) { return ((long)batch * (round_to(L.m, t) / t) * (round_to(L.n, t) / t) + 255) / 256; };
+    L.tile = 3.4 * rounds(256) <= rounds(128) ? 256 : 128;
+    L.mp = round_to(L.m, L.tile); L.np = round_to(L.n, L.tile);
+    const int mt = L.mp / L.tile;
+    const long tiles = (long)batch * (mt * (mt + 1) / 2);
+    L.splits[kGram] = split_count(planes, L.tile, tiles, L.np * planes / 64);
+    L.splits[kPoly] = split_count(planes, L.tile, tiles, L.mp * planes / 64);
+    const size_t each = ((size_t)L.rows * L.cols + 2047) / 2048;
+    L.parts = each < kParts ? (int)each : kParts;
     size_t off = 0;
     auto take = [&](size_t bytes) { char *p = ws + off; off += round_up(bytes, 256); return p; };
     const size_t mn = (size_t)batch * L.mp * L.np, mm = (size_t)batch * L.mp * L.mp;
     L.part = reinterpret_cast<double *>(take((size_t)batch * kParts * 8));
     L.x32 = reinterpret_cast<float *>(take(mn * 4));
-    L.x = reinterpret_cast<half_t *>(take(mn * 2 * planes));
-    for (int k = 0; k < 2; ++k) L.xt[k] = reinterpret_cast<half_t *>(take(mn * 2 * planes));
+    for (int k = 0; k < 2; ++k) L.x[k] = reinterpret_cast<half_t *>(take(mn * 2 * planes));
     L.g = reinterpret_cast<half_t *>(take(mm * 2 * planes));
     L.p = reinterpret_cast<half_t *>(take(mm * 2 * planes));
     L.gd = reinterpret_cast<float *>(take((size_t)batch * L.mp * 4));
     L.pd = reinterpret_cast<float *>(take((size_t)batch * L.mp * 4));
+    const int most = L.splits[kGram] > L.splits[kPoly] ? L.splits[kGram] : L.splits[kPoly];
+    L.sums = reinterpret_cast<float *>(take((size_t)tiles * most * L.tile * L.tile * 4));
     total = off;
     return L;
+}
+
+template <typename T, int PL, int MODE, int TILE>
+int product(const Layout &L, int from, const Target &out, hipStream_t s)
+{
+    auto kern = muon_product_kernel<T, PL, MODE, TILE>;
+    if (!raise_lds_limit(reinterpret_cast<const void *>(kern))) return VGG_ERR_LAUNCH;
+    const int mt = L.mp / TILE, nt = L.np / TILE;
+    if constexpr (MODE == kApply || MODE == kLast) {
+        hipLaunchKernelGGL(kern, dim3(mt * nt, L.batch), dim3(512), 131072, s, L, from, out);
+    } else {
+        const int tiles = mt * (mt + 1) / 2;
+        hipLaunchKernelGGL(kern, dim3(tiles * L.splits[MODE], L.batch), dim3(512), 131072, s, L, from, out);
+        hipLaunchKernelGGL((muon_symmetric_kernel<PL, MODE, TILE>), dim3(tiles * (TILE / 32) * (TILE / 32), L.batch), dim3(256), 0, s, L);
+    }
+    return VGG_OK;
+}
+
+template <typename T, int PL, int TILE>
+int steps_of(const Layout &L, int steps, const Target &out, hipStream_t s)
+{
+    for (int k = 0; k < steps; ++k) {
+        if (const int rc = product<float, PL, kGram, TILE>(L, k & 1, out, s)) return rc;
+        if (const int rc = product<float, PL, kPoly, TILE>(L, k & 1, out, s)) return rc;
+        if (const int rc = k + 1 < steps ? product<float, PL, kApply, TILE>(L, k & 1, out, s) : product<T, PL, kLast, TILE>(L, k & 1, out, s)) return rc;
+    }
+    return VGG_OK;
 }
 
 template <typename T, int PL>
@@ -272,15 +490,9 @@ int run(int batch, int rows, int cols, int steps, const Source &src, const Targe
 {
     size_t total;
     const Layout L = layout_of(PL, batch, rows, cols, static_cast<char *>(ws), total);
-    const unsigned mt = L.mp / kTile, nt = L.np / kTile, b = batch;
-    hipLaunchKernelGGL((muon_norm_kernel<T>), dim3(kParts, b), dim3(256), 0, s, src, L.part, (size_t)rows * cols);
-    hipLaunchKernelGGL((muon_start_kernel<T, PL>), dim3(L.np / 64, L.mp / 64, b), dim3(256), 0, s, src, L);
-    for (int k = 0; k < steps; ++k) {
-        hipLaunchKernelGGL((muon_product_kernel<T, PL, kGram>), dim3(mt * (mt + 1) / 2, 1, b), dim3(256), 65536, s, L, 0, out);
-        hipLaunchKernelGGL((muon_product_kernel<T, PL, kPoly>), dim3(mt * (mt + 1) / 2, 1, b), dim3(256), 65536, s, L, 0, out);
-        if (k + 1 < steps) hipLaunchKernelGGL((muon_product_kernel<T, PL, kApply>), dim3(nt, mt, b), dim3(256), 65536, s, L, k & 1, out);
-        else hipLaunchKernelGGL((muon_product_kernel<T, PL, kLast>), dim3(nt, mt, b), dim3(256), 65536, s, L, k & 1, out);
-    }
+    hipLaunchKernelGGL((muon_norm_kernel<T>), dim3(L.parts, batch), dim3(256), 0, s, src, L.part, (size_t)rows * cols);
+    hipLaunchKernelGGL((muon_start_kernel<T, PL>), dim3(L.np / 64, L.mp / 64, batch), dim3(256), 0, s, src, L);
+    if (const int rc = L.tile == 256 ? steps_of<T, PL, 256>(L, steps, out, s) : steps_of<T, PL, 128>(L, steps, out, s)) return rc;
     return launch_status();
 }
 
