@@ -409,6 +409,278 @@ __global__ __launch_bounds__(256) void muon_symmetric_kernel(Layout L)
     store(j0 + ty, i0 + tx * 4, v);
 }
 
+// ------------------------------------------------------------------------------------------- small matrices
+// Everything of a matrix of up to 64 rows (of X) in one workgroup of eight waves, which nothing but its input and output passes
+// memory for: X itself in registers, in the layout of the products' results (32 columns w + 8 c to wave w), X^T's planes, G's and
+// P's in LDS.  By columns, a lane's four consecutive rows of a result are one LDS store; P X then reads columns of X as they lie,
+// and G reads its rows transposed.  G and G G are 16 blocks of 16 x 16, two to a wave; the sum (i, j) is stored as (j, i), the
+// same by symmetry and four in a row again.  Three barriers a step.  The launches that this saves are all that such a matrix
+// costs otherwise (64 x 576, bf16: 108 us in 27 launches, 37 us here).
+constexpr int kSmallRows = 64, kSmallLds = 160 * 1024;
+constexpr int small_stride(int planes) { return 128 * planes + 16; }   // bytes of 64 elements; 16 more: rows start in different banks
+inline size_t small_lds(int planes, int n) { return (size_t)((n + 31) / 32 * 32 + 2 * kSmallRows) * small_stride(planes) + 3 * 256; }
+
+template <typename T, int PL, int CB>
+__global__ __launch_bounds__(512) void muon_small_kernel(Source src, Target out, int rows, int cols, int steps)
+{
+    extern __shared__ __align__(16) char lds[];
+    typedef half_t f16x4 __attribute__((ext_vector_type(4)));
+    constexpr int S = small_stride(PL);
+    const bool tall = rows > cols;
+    const int m = tall ? cols : rows, n = tall ? rows : cols, blocks = (n + 31) / 32;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
+    char *X = lds, *G = X + blocks * 32 * S, *P = G + kSmallRows * S;
+    float *gd = reinterpret_cast<float *>(P + kSmallRows * S), *pd = gd + 64;
+    double *red = reinterpret_cast<double *>(pd + 64);
+    const size_t base = (size_t)blockIdx.x * rows * cols;
+    // element (r, v) of column block c: row 32 r + 8 (v / 4) + 4 half + v % 4, column 32 (wave + 8 c) + col
+    const int i_step = tall ? 1 : cols, j_step = tall ? cols : 1;
+    const T *in = static_cast<const T *>(src.x) + base;
+    auto place = [&](int c, int r, int v, bool &there) __attribute__((always_inline)) {   // (of an element that is there, where this one is not)
+        const int i = r * 32 + 8 * (v >> 2) + 4 * half + (v & 3), j = (wave + 8 * c) * 32 + col;
+        there = i < m && j < n;
+        return there ? i * i_step + j * j_step : 0;
+    };
+
+    float x[CB][2][16];
+    double sum = 0;
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            bool there;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) x[c][r][v] = Elem<T>::load(in + place(c, r, v, there));
+        }
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            bool there[16];
+            int at[16];
+#pragma unroll
+            for (int v = 0; v < 16; ++v) at[v] = place(c, r, v, there[v]);
+            if (src.momentum) {
+                float mom[16];
+#pragma unroll
+                for (int v = 0; v < 16; ++v) mom[v] = src.momentum[base + at[v]];
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    mom[v] = __builtin_fmaf(src.mu, mom[v], x[c][r][v]);
+                    if (there[v]) src.momentum[base + at[v]] = mom[v];
+                    x[c][r][v] = src.nesterov ? __builtin_fmaf(src.mu, mom[v], x[c][r][v]) : mom[v];
+                }
+            }
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                x[c][r][v] = there[v] ? x[c][r][v] : 0.f;
+                sum = __builtin_fma((double)x[c][r][v], (double)x[c][r][v], sum);
+            }
+        }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, kWave);
+    if (lane == 0) red[wave] = sum;
+    __syncthreads();
+    sum = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum += red[k];
+    const double by = sum < (double)INFINITY ? 1. / (sqrt(sum) + (double)kEps) : (double)NAN;
+
+    // four consecutive elements k.. of a row, scaled, into its planes; and back
+    auto put4 = [&](char *row, int k, const f32x4 &v) __attribute__((always_inline)) {
+        f16x4 h, l;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            h[q] = (half_t)v[q];
+            l[q] = (half_t)(v[q] - (float)h[q]);
+        }
+        char *to = row + at_plane<PL>(k, 0) * 2;
+        *reinterpret_cast<f16x4 *>(to) = h;
+        if constexpr (PL == 2) *reinterpret_cast<f16x4 *>(to + 64) = l;
+    };
+    auto get4 = [&](const char *row, int k) __attribute__((always_inline)) {
+        const char *from = row + at_plane<PL>(k, 0) * 2;
+        f32x4 v = __builtin_convertvector(*reinterpret_cast<const f16x4 *>(from), f32x4);
+        if constexpr (PL == 2) v += __builtin_convertvector(*reinterpret_cast<const f16x4 *>(from + 64), f32x4);
+        return v;
+    };
+    auto put_x = [&] __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+            if (wave + 8 * c < blocks)
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const f32x4 v = {x[c][r][4 * q], x[c][r][4 * q + 1], x[c][r][4 * q + 2], x[c][r][4 * q + 3]};
+                        put4(X + ((wave + 8 * c) * 32 + col) * S, r * 32 + 8 * q + 4 * half, v * kUp);
+                    }
+    };
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) x[c][r][v] = (float)(x[c][r][v] * by);
+    put_x();
+    __syncthreads();
+
+    const int bi = wave >> 1, bj = (wave & 1) * 2, r16 = lane & 15, quarter = lane >> 4;
+    auto mfma16 = [&](const f16x8 (&fa)[PL], const f16x8 (&fb)[PL], f32x4 acc) __attribute__((always_inline)) {
+        if constexpr (PL == 2) {
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[1], fb[0], acc, 0, 0, 0);
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[0], fb[1], acc, 0, 0, 0);
+        }
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[0], fb[0], acc, 0, 0, 0);
+    };
+    for (int step = 0; step < steps; ++step) {
+        // G: this wave's blocks (bi, bj) and (bi, bj + 1)
+        f32x4 acc[2] = {};
+        struct Rows { f16x8 a[PL], b[2][PL]; };
+        auto columns = [&](int jb, Rows &f) __attribute__((always_inline)) {        // 32 columns of X's rows
+            auto rows_of = [&](int b, f16x8 (&f)[PL]) __attribute__((always_inline)) {
+#pragma unroll
+                for (int p = 0; p < PL; ++p) {
+                    typedef __fp16 fp16x4 __attribute__((__vector_size__(8)));
+                    typedef __attribute__((address_space(3))) fp16x4 lds_f16x4;
+                    const char *at = X + (jb * 32 + 8 * quarter + (r16 >> 2)) * S + at_plane<PL>(b * 16, p) * 2 + (r16 & 3) * 8;
+                    const auto lo = __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_f16x4 *)at);
+                    const auto hi = __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_f16x4 *)(at + 4 * S));
+                    f[p] = __builtin_shufflevector(__builtin_bit_cast(f16x4, lo), __builtin_bit_cast(f16x4, hi), 0, 1, 2, 3, 4, 5, 6, 7);
+                }
+            };
+            rows_of(bi, f.a);
+            rows_of(bj, f.b[0]);
+            rows_of(bj + 1, f.b[1]);
+        };
+        Rows f0, f1;                               // one being multiplied, one on its way
+        columns(0, f0);
+        for (int jb = 0; jb < blocks; jb += 2) {
+            if (jb + 1 < blocks) columns(jb + 1, f1);
+#pragma unroll
+            for (int q = 0; q < 2; ++q) acc[q] = mfma16(f0.a, f0.b[q], acc[q]);
+            if (jb + 1 == blocks) break;
+            if (jb + 2 < blocks) columns(jb + 2, f0);
+#pragma unroll
+            for (int q = 0; q < 2; ++q) acc[q] = mfma16(f1.a, f1.b[q], acc[q]);
+        }
+        // value v of a lane: (16 bi + 4 quarter + v, 16 b + r16)
+        const int i = bi * 16 + 4 * quarter;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int j = (bj + q) * 16 + r16;
+            f32x4 v = acc[q] * kDown;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (i + k == j) {
+                    gd[j] = v[k] * kDown;
+                    v[k] = 0.f;
+                }
+            put4(G + j * S, i, v);
+        }
+        __syncthreads();
+        // P = b G + c G G
+        acc[0] = acc[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int jb = 0; jb < 2; ++jb) {
+            auto rows_of = [&](int b, f16x8 (&f)[PL]) __attribute__((always_inline)) {
+#pragma unroll
+                for (int p = 0; p < PL; ++p) f[p] = *reinterpret_cast<const f16x8 *>(G + (b * 16 + r16) * S + jb * 64 * PL + p * 64 + quarter * 16);
+            };
+            f16x8 fa[PL], fb[2][PL];
+            rows_of(bi, fa);
+            rows_of(bj, fb[0]);
+            rows_of(bj + 1, fb[1]);
+#pragma unroll
+            for (int q = 0; q < 2; ++q) acc[q] = mfma16(fa, fb[q], acc[q]);
+        }
+        const f32x4 di = *reinterpret_cast<const f32x4 *>(gd + i);
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int j = (bj + q) * 16 + r16;
+            const float dj = gd[j];
+            const f32x4 e = get4(G + j * S, i);
+            f32x4 v;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                v[k] = __builtin_fmaf(kC, acc[q][k] * kDown, __builtin_fmaf(kC, di[k] + dj, kB) * e[k]);
+                if (i + k == j) {
+                    pd[j] = __builtin_fmaf(kC, __builtin_fmaf(dj, dj, acc[q][k] * (kDown * kDown)), kB * dj);
+                    v[k] = 0.f;
+                }
+            }
+            put4(P + j * S, i, v);
+        }
+        __syncthreads();
+        // X <- a X + P X
+        f32x4 pdv[2][4];
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) pdv[r][q] = *reinterpret_cast<const f32x4 *>(pd + r * 32 + 8 * q + 4 * half);
+#pragma unroll
+        for (int c = 0; c < CB; ++c) {
+            const int jb = wave + 8 * c;
+            if (jb >= blocks) continue;
+            f32x16 sumx[2] = {};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int at = (k >> 1) * 64 * PL + (k & 1) * 32 + half * 16;
+                f16x8 fb[PL], fa[2][PL];
+#pragma unroll
+                for (int p = 0; p < PL; ++p) {
+                    fb[p] = *reinterpret_cast<const f16x8 *>(X + (jb * 32 + col) * S + at + p * 64);
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) fa[r][p] = *reinterpret_cast<const f16x8 *>(P + (r * 32 + col) * S + at + p * 64);
+                }
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    if constexpr (PL == 2) {
+                        sumx[r] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[r][1], fb[0], sumx[r], 0, 0, 0);
+                        sumx[r] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[r][0], fb[1], sumx[r], 0, 0, 0);
+                    }
+                    sumx[r] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[r][0], fb[0], sumx[r], 0, 0, 0);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) x[c][r][v] = __builtin_fmaf(kA + pdv[r][v >> 2][v & 3], x[c][r][v], sumx[r][v] * (kDown * kDown));
+        }
+        if (step + 1 < steps) {
+            put_x();                               // (a wave's own columns, which no other reads before the barrier)
+            __syncthreads();
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            bool there[16];
+            int at[16];
+#pragma unroll
+            for (int v = 0; v < 16; ++v) at[v] = place(c, r, v, there[v]);
+            if (out.theta) {
+                float t[16];
+#pragma unroll
+                for (int v = 0; v < 16; ++v) t[v] = out.theta[base + at[v]];
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    if (there[v]) out.theta[base + at[v]] = __builtin_fmaf(-out.rate, x[c][r][v], out.keep * t[v]);
+            } else
+#pragma unroll
+                for (int v = 0; v < 16; ++v)
+                    if (there[v]) Elem<T>::store(static_cast<T *>(out.out) + base + at[v], x[c][r][v]);
+        }
+}
+
+// Column blocks of a wave, 0 where a matrix is too large: its planes' room in LDS, and three blocks of X and as many sums in registers.
+int small_blocks(int planes, int rows, int cols)
+{
+    const int m = rows < cols ? rows : cols, n = rows < cols ? cols : rows, cb = ((n + 31) / 32 + 7) / 8;
+    return m <= kSmallRows && cb <= (planes == 2 ? 2 : 3) && small_lds(planes, n) <= kSmallLds ? cb : 0;
+}
+
 inline int round_to(int v, int to) { return (v + to - 1) / to * to; }
 
 // How many ranges a contraction of `all` stages is cut into for `tiles` workgroups each: rounds of the chip's 256 compute units
@@ -488,6 +760,12 @@ int steps_of(const Layout &L, int steps, const Target &out, hipStream_t s)
 template <typename T, int PL>
 int run(int batch, int rows, int cols, int steps, const Source &src, const Target &out, void *ws, hipStream_t s)
 {
+    if (const int cb = small_blocks(PL, rows, cols)) {
+        auto kern = cb == 1 ? muon_small_kernel<T, PL, 1> : cb == 2 || PL == 2 ? muon_small_kernel<T, PL, 2> : muon_small_kernel<T, PL, PL == 2 ? 2 : 3>;
+        if (!raise_lds_limit(reinterpret_cast<const void *>(kern))) return VGG_ERR_LAUNCH;
+        hipLaunchKernelGGL(kern, dim3(batch), dim3(512), small_lds(PL, rows < cols ? cols : rows), s, src, out, rows, cols, steps);
+        return launch_status();
+    }
     size_t total;
     const Layout L = layout_of(PL, batch, rows, cols, static_cast<char *>(ws), total);
     hipLaunchKernelGGL((muon_norm_kernel<T>), dim3(L.parts, batch), dim3(256), 0, s, src, L.part, (size_t)rows * cols);

@@ -55,7 +55,7 @@ def off(got, want):
 
 
 SHAPES = [(1, 1, 1), (1, 1, 37), (2, 37, 1), (1, 2, 3), (3, 16, 16), (1, 27, 64), (2, 64, 27), (1, 64, 576), (1, 127, 129), (1, 129, 127), (1, 130, 514),
-          (2, 200, 1000), (1, 1000, 200), (1, 255, 257), (1, 300, 300), (3, 96, 33)]
+          (2, 200, 1000), (1, 1000, 200), (1, 255, 257), (1, 300, 300), (3, 96, 33), (2, 33, 480), (1, 481, 64), (1, 64, 768), (1, 769, 40), (1, 65, 100), (5, 32, 32)]
 
 
 @pytest.mark.parametrize("dtype", [B.F32, B.BF16])
