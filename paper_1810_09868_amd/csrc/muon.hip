@@ -13,10 +13,13 @@
 //     (G G)_ij = (E E)_ij + (d_i + d_j) e_ij,   (G G)_ii = (E E)_ii + d_i^2,   (P X)_i = p_i X_i + (the rest of P) X.
 // One plane is then 3e-4 to 1e-3 off in all, against 1.3e-3 to 2.4e-3 with the diagonals rounded (bf16's own rounding: 1.7e-3).
 //
-// X, G and P lie by rows, a row's every 32 elements 64 bytes of the first plane and then of the second.  G and G G contract along
-// rows of both operands; P X takes X's columns, which LDS hands out transposed (ds_read_b64_tr_b16), so that X is kept once.  X is
-// padded with zeros to whole tiles.  G and P are symmetric: the tiles on and below the diagonal are formed, over a few ranges of
-// the contraction where they are too few to fill the chip, and a second kernel adds the ranges in order and mirrors them.
+// X, G and P lie in columns of 128 bytes to a row: [column][row][64 elements], or [32 elements of the first plane, 32 of the
+// second], so that what a workgroup copies for a stage of its contraction is contiguous.  (By whole rows, a stage's pieces are a
+// power of two apart, and all workgroups ask one channel of the L2 at a time: ROWTIMES.)  X's fp32 copy lies in columns of 32.
+// G and G G contract along rows of both operands; P X takes X's columns, which LDS hands out transposed (ds_read_b64_tr_b16), so
+// that X is kept once.  X is padded with zeros to whole tiles.  G and P are symmetric: the tiles on and below the diagonal are
+// formed, over a few ranges of the contraction where they are too few to fill the chip, and a second kernel adds the ranges in
+// order and mirrors them.
 #include "common.h"
 
 namespace vgg {
@@ -32,18 +35,13 @@ constexpr int kParts = 1024;                            // partial sums of squar
 
 // Element k of a row of K-blocks of 32 with PL planes.
 template <int PL> __device__ __forceinline__ size_t at_plane(int k, int plane) { return (size_t)(k >> 5) * (32 * PL) + plane * 32 + (k & 31); }
-template <int PL> __device__ __forceinline__ void put(half_t *row, int k, float scaled)
+// The same in a matrix of `rows` (padded) rows, columns of 128 bytes.
+template <int PL> __device__ __forceinline__ size_t at_column(int rows, int i, int k)
 {
-    const half_t hi = (half_t)scaled;
-    row[at_plane<PL>(k, 0)] = hi;
-    if constexpr (PL == 2) row[at_plane<PL>(k, 1)] = (half_t)(scaled - (float)hi);
+    constexpr int C = 64 / PL;
+    return ((size_t)(k / C) * rows + i) * 64 + k % C;
 }
-template <int PL> __device__ __forceinline__ float get(const half_t *row, int k)
-{
-    float v = (float)row[at_plane<PL>(k, 0)];
-    if constexpr (PL == 2) v += (float)row[at_plane<PL>(k, 1)];
-    return v;
-}
+__device__ __forceinline__ size_t at_x32(int rows, int i, int j) { return ((size_t)(j >> 5) * rows + i) * 32 + (j & 31); }
 
 // ----------------------------------------------------------------------------------- momentum and the norm
 // Squares are summed in 64 bits: they neither overflow nor vanish.
@@ -106,9 +104,9 @@ __global__ __launch_bounds__(256) void muon_norm_kernel(Source s, double *__rest
 struct Layout {
     int rows, cols, m, n, mp, np, tall, tile, parts, batch;   // tile: of the products, 128 or 256, which mp and np are multiples of
     int splits[2];         // of the Gram matrix and its square
-    float *x32;            // [batch][mp][np]
-    half_t *x[2];          // [batch][mp][np], PLANES each
-    half_t *g, *p;         // [batch][mp][mp], PLANES each, zero diagonals
+    float *x32;            // [batch][np / 32][mp][32]
+    half_t *x[2];          // [batch][columns][mp][64], of mp x np
+    half_t *g, *p;         // [batch][columns][mp][64], of mp x mp, zero diagonals
     float *gd, *pd;        // [batch][mp], the diagonals
     float *sums;           // [batch][tiles][splits][tile][tile]
     double *part;          // [batch][kParts]
@@ -145,8 +143,11 @@ __global__ __launch_bounds__(256) void muon_start_kernel(Source s, Layout L)
     for (int k = 0; k < 16; ++k) {
         const int y = ty + 4 * k;
         const float w = (float)(v[k] * by);
-        x32[(size_t)(i0 + y) * L.np + j0 + tx] = w;
-        put<PL>(x + (size_t)(i0 + y) * L.np * PL, j0 + tx, w * kUp);
+        x32[at_x32(L.mp, i0 + y, j0 + tx)] = w;
+        half_t *to = x + at_column<PL>(L.mp, i0 + y, j0 + tx);
+        const half_t hi = (half_t)(w * kUp);
+        to[0] = hi;
+        if constexpr (PL == 2) to[32] = (half_t)(w * kUp - (float)hi);
     }
 }
 
@@ -175,9 +176,9 @@ __device__ __forceinline__ int spread(int id, int count)
 
 // A workgroup of eight waves (2 x 4): TILE x TILE of C = A B^T (kGram, kPoly) or A B (kApply, kLast).  A stage is 128 bytes of
 // every row of A (64 contraction indices, or 32 in two planes), and as many rows or bytes of B; STAGES of them in LDS, all but one
-// on their way (128 KB, one workgroup to a compute unit).  A 16-byte segment s of a row r of A lies at s ^ (r & 7), so that eight
-// rows of one segment are in different banks; a 64-byte block c of a row r of B that is read transposed at c ^ (r & 3), for the
-// four rows that sixteen lanes read.  256 x 256 tiles take 2/3 of the LDS traffic of 128 x 128 ones, and four times the work.
+// on their way (128 KB, one workgroup to a compute unit).  A 16-byte segment s of a row r of A lies at s ^ (r / 2 % 8), so that
+// sixteen rows of one segment are in different banks; the two 64-byte blocks of a row r of
+// B that is read transposed change places where r / 2 is odd, for the four rows that sixteen lanes read.  256 x 256 tiles take 2/3 of the LDS traffic of 128 x 128 ones, and four times the work.
 template <typename T, int PL, int MODE, int TILE>
 __global__ __launch_bounds__(512) void muon_product_kernel(Layout L, int from, Target out)
 {
@@ -205,27 +206,26 @@ __global__ __launch_bounds__(512) void muon_product_kernel(Layout L, int from, T
     const int K = MODE == kGram ? L.np : L.mp, all = K / KS;
     const int splits = TR ? 1 : L.splits[MODE];
     const int s0 = (int)((long)all * split / splits), stages = (int)((long)all * (split + 1) / splits) - s0;
-    const size_t row_bytes = (size_t)K * PL * 2, x_bytes = (size_t)L.np * PL * 2;
     const half_t *pa = MODE == kGram ? L.x[from] + b * mn * PL : MODE == kPoly ? L.g + b * mm * PL : L.p + b * mm * PL;
-    const char *ga = reinterpret_cast<const char *>(pa) + (size_t)ti * TILE * row_bytes + (size_t)s0 * 128;
-    const char *gb = TR ? reinterpret_cast<const char *>(L.x[from] + b * mn * PL) + (size_t)tj * TILE * 2 * PL
-                        : reinterpret_cast<const char *>(pa) + (size_t)tj * TILE * row_bytes + (size_t)s0 * 128;
+    const size_t column = (size_t)L.mp * 128;     // bytes
+    const char *ga = reinterpret_cast<const char *>(pa) + s0 * column + (size_t)ti * TILE * 128;
+    const char *gb = TR ? reinterpret_cast<const char *>(L.x[from] + b * mn * PL) + (size_t)(tj * TILE / KS) * column
+                        : reinterpret_cast<const char *>(pa) + s0 * column + (size_t)tj * TILE * 128;
     const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_char *)lds + wave * 1024);
 
     // where this thread's copies come from
     const char *src_a[COPIES], *src_b[COPIES];
 #pragma unroll
     for (int q = 0; q < COPIES; ++q) {
-        const int at = (q * 512 + (int)threadIdx.x) * 16, r = at >> 7, seg = ((at >> 4) & 7) ^ (r & 7);
-        src_a[q] = ga + (size_t)r * row_bytes + seg * 16;
-        if constexpr (TR) {
-            constexpr int RB = TILE * 2 * PL;      // bytes of a row of B's tile
-            const int k = at / RB, c = (at % RB >> 6) ^ (k & 3);
-            src_b[q] = gb + (size_t)k * x_bytes + c * 64 + (at & 63);
+        const int at = (q * 512 + (int)threadIdx.x) * 16, r = at >> 7, seg = ((at >> 4) & 7) ^ (r >> 1 & 7);
+        src_a[q] = ga + r * 128 + seg * 16;
+        if constexpr (TR) {                        // [TILE / KS columns][KS rows][128 bytes]
+            const int k = r % KS;
+            src_b[q] = gb + r / KS * column + k * 128 + ((at & 127) ^ (k >> 1 & 1) << 6);
         } else
-            src_b[q] = gb + (size_t)r * row_bytes + seg * 16;
+            src_b[q] = gb + r * 128 + seg * 16;
     }
-    const size_t step_b = TR ? (size_t)KS * x_bytes : 128;
+    const size_t step_b = TR ? (size_t)KS * 128 : column;
     int slot = 0;
     auto stage_copy = [&] __attribute__((always_inline)) {
         const unsigned dst = lds0 + slot * (2 * HALF);
@@ -233,7 +233,7 @@ __global__ __launch_bounds__(512) void muon_product_kernel(Layout L, int from, T
         for (int q = 0; q < COPIES; ++q) {
             copy16(dst + q * 8192, src_a[q]);
             copy16(dst + HALF + q * 8192, src_b[q]);
-            src_a[q] += 128;
+            src_a[q] += column;
             src_b[q] += step_b;
         }
         slot = slot + 1 == STAGES ? 0 : slot + 1;
@@ -242,52 +242,70 @@ __global__ __launch_bounds__(512) void muon_product_kernel(Layout L, int from, T
     f32x16 acc[BX][BY] = {};
     const int wi = (wave >> 2) * (TILE / 2), wj = (wave & 3) * (TILE / 4);
     // this lane's part of a fragment's address: rows (of A, of B by rows), or the transposed read's
-    const int arow = wi + (lane & 31), brow = wj + (lane & 31), rx = lane & 7;
-    const int s16 = lane & 15, tr_k = 8 * (lane >> 5) + (s16 >> 2), tr_x = s16 >> 2, tr_at = (lane >> 4 & 1) * 32 + (s16 & 3) * 8;
+    const int arow = wi + (lane & 31), brow = wj + (lane & 31), rx = lane >> 1 & 7;
+    const int s16 = lane & 15, tr_k = 8 * (lane >> 5) + (s16 >> 2), tr_x = s16 >> 3, tr_at = (lane >> 4 & 1) * 32 + (s16 & 3) * 8;
+    // Fragments of one of a stage's KK steps are read while those of the step before are multiplied, the first ones of a stage during
+    // the last step of the one before: otherwise the waves, which the barrier lines up, would all read and then all multiply.
+    constexpr int KK = 4 / PL;
+    struct Fragments { f16x8 a[PL][BX], b[PL][BY]; };
+    auto read = [&](int use, int k, Fragments &f) __attribute__((always_inline)) {
+        const char *A = lds + use * (2 * HALF), *B = A + HALF;
 #pragma unroll
-    for (int k = 0; k < STAGES - 1; ++k)
+        for (int p = 0; p < PL; ++p) {
+            const int seg = p * 4 + k * 2 + (lane >> 5);
+#pragma unroll
+            for (int q = 0; q < BX; ++q) f.a[p][q] = *reinterpret_cast<const f16x8 *>(A + (arow + q * 32) * 128 + ((seg ^ rx) << 4));
+#pragma unroll
+            for (int q = 0; q < BY; ++q) {
+                if constexpr (TR) {
+                    typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+                    typedef __fp16 fp16x4 __attribute__((__vector_size__(8)));
+                    typedef __attribute__((address_space(3))) fp16x4 lds_f16x4;
+                    const int c = ((wj >> 5) + q) * PL + p;      // 64-byte block of a row
+                    const char *at = B + (c >> 1) * (KS * 128) + (k * 16 + tr_k) * 128 + (((c & 1) ^ tr_x) << 6) + tr_at;
+                    const auto lo = __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_f16x4 *)at);
+                    const auto hi = __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_f16x4 *)(at + 4 * 128));
+                    f.b[p][q] = __builtin_shufflevector(__builtin_bit_cast(f16x4, lo), __builtin_bit_cast(f16x4, hi), 0, 1, 2, 3, 4, 5, 6, 7);
+                } else
+                    f.b[p][q] = *reinterpret_cast<const f16x8 *>(B + (brow + q * 32) * 128 + ((seg ^ rx) << 4));
+            }
+        }
+    };
+#pragma unroll
+    for (int k = 0; k < STAGES; ++k)
         if (k < stages) stage_copy();
-    int use = 0;
-    for (int st = 0; st < stages; ++st) {
-        // this stage's copies have landed (those of the later ones may be on their way), and all waves are done with the last one
+    // The copies of stage `st` have landed (those of later ones may be on their way), and all waves have read what they need of the
+    // stage before, whose place the next copies take.
+    auto ready = [&](int st) __attribute__((always_inline)) {
         if (STAGES > 2 && st + STAGES - 2 < stages) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((STAGES - 2) * 2 * COPIES) : "memory");
         else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
-        if (st + STAGES - 1 < stages) stage_copy();
-        const char *A = lds + use * (2 * HALF), *B = A + HALF;
-        use = use + 1 == STAGES ? 0 : use + 1;
+    };
+    // (before stage 0 one stage more is on its way than before the others)
+    if (stages >= STAGES) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"((STAGES - 1) * 2 * COPIES) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" : : : "memory");
+    Fragments f[2];
+    read(0, 0, f[0]);
+    int use = 0;
+    for (int st = 0; st < stages; ++st) {
 #pragma unroll
-        for (int k = 0; k < 4 / PL; ++k) {
-            f16x8 fa[PL][BX], fb[PL][BY];
-#pragma unroll
-            for (int p = 0; p < PL; ++p) {
-                const int seg = p * 4 + k * 2 + (lane >> 5);
-#pragma unroll
-                for (int q = 0; q < BX; ++q) fa[p][q] = *reinterpret_cast<const f16x8 *>(A + (arow + q * 32) * 128 + ((seg ^ rx) << 4));
-#pragma unroll
-                for (int q = 0; q < BY; ++q) {
-                    if constexpr (TR) {
-                        typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-                        typedef __fp16 fp16x4 __attribute__((__vector_size__(8)));
-                        const int c = ((wj >> 5) + q) * PL + p;
-                        const char *at = B + (k * 16 + tr_k) * (TILE * 2 * PL) + ((c ^ tr_x) << 6) + tr_at;
-                        typedef __attribute__((address_space(3))) fp16x4 lds_f16x4;
-                        const auto lo = __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_f16x4 *)at);
-                        const auto hi = __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_f16x4 *)(at + 4 * (TILE * 2 * PL)));
-                        fb[p][q] = __builtin_shufflevector(__builtin_bit_cast(f16x4, lo), __builtin_bit_cast(f16x4, hi), 0, 1, 2, 3, 4, 5, 6, 7);
-                    } else
-                        fb[p][q] = *reinterpret_cast<const f16x8 *>(B + (brow + q * 32) * 128 + ((seg ^ rx) << 4));
-                }
+        for (int k = 0; k < KK; ++k) {
+            if (k + 1 < KK) read(use, k + 1, f[(k + 1) & 1]);
+            else if (st + 1 < stages) {
+                ready(st + 1);
+                if (st + STAGES < stages) stage_copy();
+                use = use + 1 == STAGES ? 0 : use + 1;
+                read(use, 0, f[0]);
             }
+            __builtin_amdgcn_sched_barrier(0);
+            const Fragments &g = f[k & 1];
+            // (all blocks' sums take one product each in turn: a sum's next product waits for its last)
 #pragma unroll
-            for (int x = 0; x < BX; ++x)
+            for (int p = PL == 2 ? 0 : 2; p < 3; ++p)
 #pragma unroll
-                for (int y = 0; y < BY; ++y) {
-                    if constexpr (PL == 2) {
-                        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[1][x], fb[0][y], acc[x][y], 0, 0, 0);
-                        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[0][x], fb[1][y], acc[x][y], 0, 0, 0);
-                    }
-                    acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[0][x], fb[0][y], acc[x][y], 0, 0, 0);
-                }
+                for (int x = 0; x < BX; ++x)
+#pragma unroll
+                    for (int y = 0; y < BY; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(g.a[p == 0][x], g.b[p == 1][y], acc[x][y], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
 
@@ -311,13 +329,13 @@ __global__ __launch_bounds__(512) void muon_product_kernel(Layout L, int from, T
 #pragma unroll
             for (int y = 0; y < BY; ++y) {
                 const int j = j0 + y * 32;
-                float *x32 = L.x32 + b * mn + (size_t)(i0 + x * 32) * L.np + j;
+                float *x32 = L.x32 + b * mn + at_x32(L.mp, i0 + x * 32, j);
                 float w[16];
 #pragma unroll
-                for (int v = 0; v < 16; ++v) w[v] = __builtin_fmaf(pd[v], x32[(size_t)(8 * (v >> 2) + (v & 3)) * L.np], acc[x][y][v] * (kDown * kDown));
+                for (int v = 0; v < 16; ++v) w[v] = __builtin_fmaf(pd[v], x32[(8 * (v >> 2) + (v & 3)) * 32], acc[x][y][v] * (kDown * kDown));
                 if constexpr (MODE == kApply) {
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) x32[(size_t)(8 * (v >> 2) + (v & 3)) * L.np] = w[v];
+                    for (int v = 0; v < 16; ++v) x32[(8 * (v >> 2) + (v & 3)) * 32] = w[v];
                     // a pair of rows and columns is shared out: even lanes take the first row's two columns, odd ones the second's
                     const bool odd = lane & 1;
 #pragma unroll
@@ -325,7 +343,7 @@ __global__ __launch_bounds__(512) void muon_product_kernel(Layout L, int from, T
                         const float mine = odd ? w[v + 1] : w[v], theirs = odd ? w[v] : w[v + 1];
                         const float got = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(theirs), 0xB1, 0xf, 0xf, true));   // quad_perm 1 0 3 2
                         const float c0 = (odd ? got : mine) * kUp, c1 = (odd ? mine : got) * kUp;
-                        half_t *to = L.x[1 - from] + (b * mn + (size_t)(i0 + x * 32 + 8 * (v >> 2) + (v & 3) + odd) * L.np) * PL + at_plane<PL>(j & ~1, 0);
+                        half_t *to = L.x[1 - from] + b * mn * PL + at_column<PL>(L.mp, i0 + x * 32 + 8 * (v >> 2) + (v & 3) + odd, j & ~1);
                         typedef half_t f16x2 __attribute__((ext_vector_type(2)));
                         const f16x2 h = {(half_t)c0, (half_t)c1};
                         *reinterpret_cast<f16x2 *>(to) = h;
@@ -362,11 +380,11 @@ __global__ __launch_bounds__(256) void muon_symmetric_kernel(Layout L)
     const int tx = threadIdx.x & 7, ty = threadIdx.x >> 3, i = i0 + ty, j = j0 + tx * 4;
     const float *c = L.sums + ((size_t)b * (mt * (mt + 1) / 2) + t) * splits * (TILE * TILE) + (size_t)(in / Q * 32 + ty) * TILE + in % Q * 32 + tx * 4;
     half_t *to = (MODE == kGram ? L.g : L.p) + b * mm * PL;
-    const half_t *g = L.g + b * mm * PL + (size_t)i * L.mp * PL;
+    const half_t *g = L.g + b * mm * PL + at_column<PL>(L.mp, i, j);
     float *gd = L.gd + (size_t)b * L.mp, *pd = L.pd + (size_t)b * L.mp;
     typedef half_t f16x4 __attribute__((ext_vector_type(4)));
     auto store = [&](int i, int j, const f32x4 &v) __attribute__((always_inline)) {
-        half_t *row = to + (size_t)i * L.mp * PL + at_plane<PL>(j, 0);
+        half_t *row = to + at_column<PL>(L.mp, i, j);
         f16x4 h, l;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -393,10 +411,12 @@ __global__ __launch_bounds__(256) void muon_symmetric_kernel(Layout L)
             if (i == j + k) gd[i] = v[k] * kDown;
     } else {
         const float di = gd[i];
+        f32x4 e = __builtin_convertvector(*reinterpret_cast<const f16x4 *>(g), f32x4);
+        if constexpr (PL == 2) e += __builtin_convertvector(*reinterpret_cast<const f16x4 *>(g + 32), f32x4);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             if (i == j + k) pd[i] = __builtin_fmaf(kC, __builtin_fmaf(di, di, v[k] * kDown), kB * di);
-            v[k] = __builtin_fmaf(kC, v[k], __builtin_fmaf(kC, di + gd[j + k], kB) * get<PL>(g, j + k));
+            v[k] = __builtin_fmaf(kC, v[k], __builtin_fmaf(kC, di + gd[j + k], kB) * e[k]);
         }
     }
     store(i, j, v);
