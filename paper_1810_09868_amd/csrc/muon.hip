@@ -22,6 +22,8 @@
 // order and mirrors them.
 #include "common.h"
 
+#include <type_traits>
+
 namespace vgg {
 
 namespace {
@@ -227,16 +229,16 @@ __global__ __launch_bounds__(512) void muon_product_kernel(Layout L, int from, T
     }
     const size_t step_b = TR ? (size_t)KS * 128 : column;
     int slot = 0;
-    auto stage_copy = [&] __attribute__((always_inline)) {
-        const unsigned dst = lds0 + slot * (2 * HALF);
-#pragma unroll
-        for (int q = 0; q < COPIES; ++q) {
-            copy16(dst + q * 8192, src_a[q]);
-            copy16(dst + HALF + q * 8192, src_b[q]);
-            src_a[q] += column;
+    auto copy_one = [&](int n) __attribute__((always_inline)) {      // of a stage's 2 COPIES
+        const int q = n >> 1;
+        if (n & 1) {
+            copy16(lds0 + slot * (2 * HALF) + HALF + q * 8192, src_b[q]);
             src_b[q] += step_b;
+        } else {
+            copy16(lds0 + slot * (2 * HALF) + q * 8192, src_a[q]);
+            src_a[q] += column;
         }
-        slot = slot + 1 == STAGES ? 0 : slot + 1;
+        if (n == 2 * COPIES - 1) slot = slot + 1 == STAGES ? 0 : slot + 1;
     };
 
     f32x16 acc[BX][BY] = {};
@@ -244,70 +246,73 @@ __global__ __launch_bounds__(512) void muon_product_kernel(Layout L, int from, T
     // this lane's part of a fragment's address: rows (of A, of B by rows), or the transposed read's
     const int arow = wi + (lane & 31), brow = wj + (lane & 31), rx = lane >> 1 & 7;
     const int s16 = lane & 15, tr_k = 8 * (lane >> 5) + (s16 >> 2), tr_x = s16 >> 3, tr_at = (lane >> 4 & 1) * 32 + (s16 & 3) * 8;
-    // Fragments of one of a stage's KK steps are read while those of the step before are multiplied, the first ones of a stage during
-    // the last step of the one before: otherwise the waves, which the barrier lines up, would all read and then all multiply.
-    constexpr int KK = 4 / PL;
+    // A stage is KK steps of 16 contraction indices.  Between a step's products the next step's fragments are read, and in a stage's
+    // last step, after the barrier, the next stage's first fragments and the copies of a stage to come: none of it would hide
+    // behind products in a block of its own, since the barrier lines the waves up.
+    constexpr int KK = 4 / PL, M = (PL == 2 ? 3 : 1) * BX * BY, R = PL * (BX + BY);
     struct Fragments { f16x8 a[PL][BX], b[PL][BY]; };
-    auto read = [&](int use, int k, Fragments &f) __attribute__((always_inline)) {
+    auto read_one = [&](int use, int k, int n, Fragments &f) __attribute__((always_inline)) {
         const char *A = lds + use * (2 * HALF), *B = A + HALF;
+        const int p = n / (BX + BY), q = n % (BX + BY), r = q - BX, seg = p * 4 + k * 2 + (lane >> 5);
+        if (q < BX) f.a[p][q] = *reinterpret_cast<const f16x8 *>(A + (arow + q * 32) * 128 + ((seg ^ rx) << 4));
+        else if constexpr (TR) {
+            typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+            typedef __fp16 fp16x4 __attribute__((__vector_size__(8)));
+            typedef __attribute__((address_space(3))) fp16x4 lds_f16x4;
+            const int c = ((wj >> 5) + r) * PL + p;      // 64-byte block of a row
+            const char *at = B + (c >> 1) * (KS * 128) + (k * 16 + tr_k) * 128 + (((c & 1) ^ tr_x) << 6) + tr_at;
+            const auto lo = __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_f16x4 *)at);
+            const auto hi = __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_f16x4 *)(at + 4 * 128));
+            f.b[p][r] = __builtin_shufflevector(__builtin_bit_cast(f16x4, lo), __builtin_bit_cast(f16x4, hi), 0, 1, 2, 3, 4, 5, 6, 7);
+        } else
+            f.b[p][r] = *reinterpret_cast<const f16x8 *>(B + (brow + r * 32) * 128 + ((seg ^ rx) << 4));
+    };
+    Fragments f[2];
+    int use = 0;
+    // One stage; READ: there is a next one, COPY: there is one to be copied.
+    auto stage = [&](auto READ, auto COPY) __attribute__((always_inline)) {
+        constexpr bool reads = decltype(READ)::value, copies = decltype(COPY)::value;
 #pragma unroll
-        for (int p = 0; p < PL; ++p) {
-            const int seg = p * 4 + k * 2 + (lane >> 5);
+        for (int k = 0; k < KK; ++k) {
+            const bool last = k + 1 == KK;
+            const int lead = last ? M / 3 : 0, tasks = last ? (reads ? R : 0) + (copies ? 2 * COPIES : 0) : R;
+            const Fragments &g = f[k & 1];
+            Fragments &next = f[(k + 1) & 1];
 #pragma unroll
-            for (int q = 0; q < BX; ++q) f.a[p][q] = *reinterpret_cast<const f16x8 *>(A + (arow + q * 32) * 128 + ((seg ^ rx) << 4));
+            for (int i = 0; i < M; ++i) {
+                // (the blocks' sums take one product each in turn: a sum's next product waits for its last)
+                const int p = PL == 2 ? i / (BX * BY) : 2, x = i % (BX * BY) / BY, y = i % BY;
+                if (last && reads && i == lead) {
+                    // The next stage's copies have landed (those of later ones may be on their way), and all waves have read what they
+                    // need of this one, whose place the next copies take.
+                    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(copies ? (STAGES - 2) * 2 * COPIES : 0) : "memory");
+                    use = use + 1 == STAGES ? 0 : use + 1;
+                }
+                acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(g.a[p == 0][x], g.b[p == 1][y], acc[x][y], 0, 0, 0);
+                if (i >= lead)
 #pragma unroll
-            for (int q = 0; q < BY; ++q) {
-                if constexpr (TR) {
-                    typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
-                    typedef __fp16 fp16x4 __attribute__((__vector_size__(8)));
-                    typedef __attribute__((address_space(3))) fp16x4 lds_f16x4;
-                    const int c = ((wj >> 5) + q) * PL + p;      // 64-byte block of a row
-                    const char *at = B + (c >> 1) * (KS * 128) + (k * 16 + tr_k) * 128 + (((c & 1) ^ tr_x) << 6) + tr_at;
-                    const auto lo = __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_f16x4 *)at);
-                    const auto hi = __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_f16x4 *)(at + 4 * 128));
-                    f.b[p][q] = __builtin_shufflevector(__builtin_bit_cast(f16x4, lo), __builtin_bit_cast(f16x4, hi), 0, 1, 2, 3, 4, 5, 6, 7);
-                } else
-                    f.b[p][q] = *reinterpret_cast<const f16x8 *>(B + (brow + q * 32) * 128 + ((seg ^ rx) << 4));
+                    for (int n = (i - lead) * tasks / (M - lead); n < (i - lead + 1) * tasks / (M - lead); ++n) {
+                        if (!last) read_one(use, k + 1, n, next);
+                        else if (n < R) read_one(use, 0, n, next);
+                        else copy_one(n - R);
+                    }
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
     };
 #pragma unroll
     for (int k = 0; k < STAGES; ++k)
-        if (k < stages) stage_copy();
-    // The copies of stage `st` have landed (those of later ones may be on their way), and all waves have read what they need of the
-    // stage before, whose place the next copies take.
-    auto ready = [&](int st) __attribute__((always_inline)) {
-        if (STAGES > 2 && st + STAGES - 2 < stages) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"((STAGES - 2) * 2 * COPIES) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" : : : "memory");
-    };
-    // (before stage 0 one stage more is on its way than before the others)
+        if (k < stages)
+#pragma unroll
+            for (int n = 0; n < 2 * COPIES; ++n) copy_one(n);
     if (stages >= STAGES) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"((STAGES - 1) * 2 * COPIES) : "memory");
     else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" : : : "memory");
-    Fragments f[2];
-    read(0, 0, f[0]);
-    int use = 0;
-    for (int st = 0; st < stages; ++st) {
 #pragma unroll
-        for (int k = 0; k < KK; ++k) {
-            if (k + 1 < KK) read(use, k + 1, f[(k + 1) & 1]);
-            else if (st + 1 < stages) {
-                ready(st + 1);
-                if (st + STAGES < stages) stage_copy();
-                use = use + 1 == STAGES ? 0 : use + 1;
-                read(use, 0, f[0]);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            const Fragments &g = f[k & 1];
-            // (all blocks' sums take one product each in turn: a sum's next product waits for its last)
-#pragma unroll
-            for (int p = PL == 2 ? 0 : 2; p < 3; ++p)
-#pragma unroll
-                for (int x = 0; x < BX; ++x)
-#pragma unroll
-                    for (int y = 0; y < BY; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(g.a[p == 0][x], g.b[p == 1][y], acc[x][y], 0, 0, 0);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    }
+    for (int n = 0; n < R; ++n) read_one(0, 0, n, f[0]);
+    int st = 0;
+    for (; st + STAGES < stages; ++st) stage(std::true_type{}, std::true_type{});
+    for (; st + 1 < stages; ++st) stage(std::true_type{}, std::false_type{});
+    stage(std::false_type{}, std::false_type{});
 
     // Value v of a block: row 8 (v / 4) + 4 (lane / 32) + v % 4, column lane % 32.
     const int row0 = wi + 4 * (lane >> 5), col0 = wj + (lane & 31);
