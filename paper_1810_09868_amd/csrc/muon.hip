@@ -14,8 +14,7 @@
 // One plane is then 3e-4 to 1e-3 off in all, against 1.3e-3 to 2.4e-3 with the diagonals rounded (bf16's own rounding: 1.7e-3).
 //
 // X, G and P lie in columns of 128 bytes to a row: [column][row][64 elements], or [32 elements of the first plane, 32 of the
-// second], so that what a workgroup copies for a stage of its contraction is contiguous.  (By whole rows, a stage's pieces are a
-// power of two apart, and all workgroups ask one channel of the L2 at a time: ROWTIMES.)  X's fp32 copy lies in columns of 32.
+// second], so that what a workgroup copies for a stage of its contraction is contiguous.  X's fp32 copy lies in columns of 32.
 // G and G G contract along rows of both operands; P X takes X's columns, which LDS hands out transposed (ds_read_b64_tr_b16), so
 // that X is kept once.  X is padded with zeros to whole tiles.  G and P are symmetric: the tiles on and below the diagonal are
 // formed, over a few ranges of the contraction where they are too few to fill the chip, and a second kernel adds the ranges in
@@ -56,6 +55,9 @@ __device__ __forceinline__ double block_sum(double v)
     __syncthreads();
     return red[0] + red[1] + red[2] + red[3];
 }
+
+// What a matrix is divided by, as a factor: in 64 bits, in which it is none of fp32's zeros for any norm; NaN for what is not finite.
+__device__ __forceinline__ double scale_of(double norm2) { return norm2 < (double)INFINITY ? 1. / (sqrt(norm2) + (double)kEps) : (double)NAN; }
 
 // momentum <- mu momentum + grad; U = grad + mu momentum (nesterov) or momentum.
 struct Source {
@@ -131,7 +133,7 @@ __global__ __launch_bounds__(256) void muon_start_kernel(Source s, Layout L)
     double norm2 = 0;
     for (int k = threadIdx.x; k < L.parts; k += 256) norm2 += L.part[b * kParts + k];
     norm2 = block_sum(norm2);
-    const double by = norm2 < (double)INFINITY ? 1. / (sqrt(norm2) + (double)kEps) : (double)NAN;   // (its product with fp32's largest is none of fp32's zeros)
+    const double by = scale_of(norm2);
     float *x32 = L.x32 + (size_t)b * L.mp * L.np;
     half_t *x = L.x[0] + (size_t)b * L.mp * L.np * PL;
     if (L.tall) {
@@ -434,85 +436,57 @@ __global__ __launch_bounds__(256) void muon_symmetric_kernel(Layout L)
     store(j0 + ty, i0 + tx * 4, v);
 }
 
-// ------------------------------------------------------------------------------------------- small matrices
-// Everything of a matrix of up to 64 rows (of X) in one workgroup of eight waves, which nothing but its input and output passes
-// memory for: X itself in registers, in the layout of the products' results (32 columns w + 8 c to wave w), X^T's planes, G's and
-// P's in LDS.  By columns, a lane's four consecutive rows of a result are one LDS store; P X then reads columns of X as they lie,
-// and G reads its rows transposed.  G and G G are 16 blocks of 16 x 16, two to a wave; the sum (i, j) is stored as (j, i), the
-// same by symmetry and four in a row again.  Three barriers a step.  The launches that this saves are all that such a matrix
-// costs otherwise (64 x 576, bf16: 108 us in 27 launches, 37 us here).
-constexpr int kSmallRows = 64, kSmallLds = 160 * 1024;
-constexpr int small_stride(int planes) { return 128 * planes + 16; }   // bytes of 64 elements; 16 more: rows start in different banks
-inline size_t small_lds(int planes, int n) { return (size_t)((n + 31) / 32 * 32 + 2 * kSmallRows) * small_stride(planes) + 3 * 256; }
+// ------------------------------------------------------------------------------------------- matrices of few rows
+// Up to 64 rows (of X), and the columns that a workgroup of eight waves has: X in registers, in the layout of the products' results
+// (32 columns w + 8 c to wave w), X^T's planes, G's and P's in LDS.  By columns, a lane's four consecutive rows of a result are one
+// LDS store; P X then reads columns of X as they lie, and G reads its rows transposed.  G and G G are 16 blocks of 16 x 16, two to
+// a wave; the sum (i, j) is stored as (j, i), the same by symmetry and four in a row again.
+constexpr int kFewRows = 64, kLds = 160 * 1024;
+constexpr int row_stride(int planes) { return 128 * planes + 16; }   // bytes of 64 elements; 16 more: rows start in different banks
+inline size_t few_lds(int planes, int blocks) { return (size_t)(blocks * 32 + 2 * kFewRows) * row_stride(planes) + 3 * 256; }
 
 template <typename T, int PL, int CB>
-__global__ __launch_bounds__(512) void muon_small_kernel(Source src, Target out, int rows, int cols, int steps)
-{
-    extern __shared__ __align__(16) char lds[];
+struct FewRows {
     typedef half_t f16x4 __attribute__((ext_vector_type(4)));
-    constexpr int S = small_stride(PL);
-    const bool tall = rows > cols;
-    const int m = tall ? cols : rows, n = tall ? rows : cols, blocks = (n + 31) / 32;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, col = lane & 31;
-    char *X = lds, *G = X + blocks * 32 * S, *P = G + kSmallRows * S;
-    float *gd = reinterpret_cast<float *>(P + kSmallRows * S), *pd = gd + 64;
-    double *red = reinterpret_cast<double *>(pd + 64);
-    const size_t base = (size_t)blockIdx.x * rows * cols;
-    // element (r, v) of column block c: row 32 r + 8 (v / 4) + 4 half + v % 4, column 32 (wave + 8 c) + col
-    const int i_step = tall ? 1 : cols, j_step = tall ? cols : 1;
-    const T *in = static_cast<const T *>(src.x) + base;
-    auto place = [&](int c, int r, int v, bool &there) __attribute__((always_inline)) {   // (of an element that is there, where this one is not)
-        const int i = r * 32 + 8 * (v >> 2) + 4 * half + (v & 3), j = (wave + 8 * c) * 32 + col;
-        there = i < m && j < n;
-        return there ? i * i_step + j * j_step : 0;
-    };
+    static constexpr int S = row_stride(PL);
+    int m, n, blocks, first, lane, wave, half, col, i_step, j_step;   // blocks of 32 columns: this workgroup's, from `first` on
+    char *X, *G, *P;
+    float *gd, *pd;
+    double *red;
+    float x[CB][2][16];    // (r, v) of column block c: row 32 r + 8 (v / 4) + 4 half + v % 4, column 32 (wave + 8 c) + col
+    f32x4 acc[2];          // G or G G: value v is (16 bi + 4 quarter + v, 16 (bj + q) + r16)
 
-    float x[CB][2][16];
-    double sum = 0;
-#pragma unroll
-    for (int c = 0; c < CB; ++c)
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            bool there;
-#pragma unroll
-            for (int v = 0; v < 16; ++v) x[c][r][v] = Elem<T>::load(in + place(c, r, v, there));
-        }
-#pragma unroll
-    for (int c = 0; c < CB; ++c)
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            bool there[16];
-            int at[16];
-#pragma unroll
-            for (int v = 0; v < 16; ++v) at[v] = place(c, r, v, there[v]);
-            if (src.momentum) {
-                float mom[16];
-#pragma unroll
-                for (int v = 0; v < 16; ++v) mom[v] = src.momentum[base + at[v]];
-#pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    mom[v] = __builtin_fmaf(src.mu, mom[v], x[c][r][v]);
-                    if (there[v]) src.momentum[base + at[v]] = mom[v];
-                    x[c][r][v] = src.nesterov ? __builtin_fmaf(src.mu, mom[v], x[c][r][v]) : mom[v];
-                }
-            }
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                x[c][r][v] = there[v] ? x[c][r][v] : 0.f;
-                sum = __builtin_fma((double)x[c][r][v], (double)x[c][r][v], sum);
-            }
-        }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, kWave);
-    if (lane == 0) red[wave] = sum;
-    __syncthreads();
-    sum = 0;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) sum += red[k];
-    const double by = sum < (double)INFINITY ? 1. / (sqrt(sum) + (double)kEps) : (double)NAN;
-
-    // four consecutive elements k.. of a row, scaled, into its planes; and back
-    auto put4 = [&](char *row, int k, const f32x4 &v) __attribute__((always_inline)) {
+    __device__ __forceinline__ FewRows(char *lds, int rows, int cols, int first_block, int most_blocks)
+    {
+        const bool tall = rows > cols;
+        m = tall ? cols : rows;
+        n = tall ? rows : cols;
+        first = first_block;
+        blocks = (n + 31) / 32 - first;
+        if (blocks > most_blocks) blocks = most_blocks;
+        lane = threadIdx.x & 63;
+        wave = threadIdx.x >> 6;
+        half = lane >> 5;
+        col = lane & 31;
+        i_step = tall ? 1 : cols;
+        j_step = tall ? cols : 1;
+        X = lds;
+        G = X + blocks * 32 * S;
+        P = G + kFewRows * S;
+        gd = reinterpret_cast<float *>(P + kFewRows * S);
+        pd = gd + 64;
+        red = reinterpret_cast<double *>(pd + 64);
+    }
+    // The place of element (c, r, v) in a matrix as the caller keeps it; that of an element that is there, where this one is not.
+    __device__ __forceinline__ size_t place(int c, int r, int v, bool &there) const
+    {
+        const int i = r * 32 + 8 * (v >> 2) + 4 * half + (v & 3), j = (first + wave + 8 * c) * 32 + col;
+        there = i < m && j < n && wave + 8 * c < blocks;
+        return there ? (size_t)i * i_step + (size_t)j * j_step : 0;
+    }
+    // Four consecutive elements k.. of a row, scaled, into its planes; and back.
+    static __device__ __forceinline__ void put4(char *row, int k, const f32x4 &v)
+    {
         f16x4 h, l;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
@@ -522,14 +496,16 @@ __global__ __launch_bounds__(512) void muon_small_kernel(Source src, Target out,
         char *to = row + at_plane<PL>(k, 0) * 2;
         *reinterpret_cast<f16x4 *>(to) = h;
         if constexpr (PL == 2) *reinterpret_cast<f16x4 *>(to + 64) = l;
-    };
-    auto get4 = [&](const char *row, int k) __attribute__((always_inline)) {
+    }
+    static __device__ __forceinline__ f32x4 get4(const char *row, int k)
+    {
         const char *from = row + at_plane<PL>(k, 0) * 2;
         f32x4 v = __builtin_convertvector(*reinterpret_cast<const f16x4 *>(from), f32x4);
         if constexpr (PL == 2) v += __builtin_convertvector(*reinterpret_cast<const f16x4 *>(from + 64), f32x4);
         return v;
-    };
-    auto put_x = [&] __attribute__((always_inline)) {
+    }
+    __device__ __forceinline__ void put_x() const
+    {
 #pragma unroll
         for (int c = 0; c < CB; ++c)
             if (wave + 8 * c < blocks)
@@ -540,28 +516,20 @@ __global__ __launch_bounds__(512) void muon_small_kernel(Source src, Target out,
                         const f32x4 v = {x[c][r][4 * q], x[c][r][4 * q + 1], x[c][r][4 * q + 2], x[c][r][4 * q + 3]};
                         put4(X + ((wave + 8 * c) * 32 + col) * S, r * 32 + 8 * q + 4 * half, v * kUp);
                     }
-    };
-#pragma unroll
-    for (int c = 0; c < CB; ++c)
-#pragma unroll
-        for (int r = 0; r < 2; ++r)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) x[c][r][v] = (float)(x[c][r][v] * by);
-    put_x();
-    __syncthreads();
-
-    const int bi = wave >> 1, bj = (wave & 1) * 2, r16 = lane & 15, quarter = lane >> 4;
-    auto mfma16 = [&](const f16x8 (&fa)[PL], const f16x8 (&fb)[PL], f32x4 acc) __attribute__((always_inline)) {
+    }
+    static __device__ __forceinline__ f32x4 mfma16(const f16x8 (&fa)[PL], const f16x8 (&fb)[PL], f32x4 acc)
+    {
         if constexpr (PL == 2) {
             acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[1], fb[0], acc, 0, 0, 0);
             acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[0], fb[1], acc, 0, 0, 0);
         }
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[0], fb[0], acc, 0, 0, 0);
-    };
-    for (int step = 0; step < steps; ++step) {
-        // G: this wave's blocks (bi, bj) and (bi, bj + 1)
-        f32x4 acc[2] = {};
-        struct Rows { f16x8 a[PL], b[2][PL]; };
+    }
+    struct Rows { f16x8 a[PL], b[2][PL]; };
+    // acc <- X X^T of the workgroup's columns, this wave's two blocks
+    __device__ __forceinline__ void gram()
+    {
+        const int bi = wave >> 1, bj = (wave & 1) * 2, r16 = lane & 15, quarter = lane >> 4;
         auto columns = [&](int jb, Rows &f) __attribute__((always_inline)) {        // 32 columns of X's rows
             auto rows_of = [&](int b, f16x8 (&f)[PL]) __attribute__((always_inline)) {
 #pragma unroll
@@ -578,6 +546,7 @@ __global__ __launch_bounds__(512) void muon_small_kernel(Source src, Target out,
             rows_of(bj, f.b[0]);
             rows_of(bj + 1, f.b[1]);
         };
+        acc[0] = acc[1] = f32x4{0.f, 0.f, 0.f, 0.f};
         Rows f0, f1;                               // one being multiplied, one on its way
         columns(0, f0);
         for (int jb = 0; jb < blocks; jb += 2) {
@@ -589,8 +558,11 @@ __global__ __launch_bounds__(512) void muon_small_kernel(Source src, Target out,
 #pragma unroll
             for (int q = 0; q < 2; ++q) acc[q] = mfma16(f1.a, f1.b[q], acc[q]);
         }
-        // value v of a lane: (16 bi + 4 quarter + v, 16 b + r16)
-        const int i = bi * 16 + 4 * quarter;
+    }
+    // G = acc, then P = b G + c G G, both to LDS (barriers between and after)
+    __device__ __forceinline__ void polynomial()
+    {
+        const int bi = wave >> 1, bj = (wave & 1) * 2, r16 = lane & 15, quarter = lane >> 4, i = bi * 16 + 4 * quarter;
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
             const int j = (bj + q) * 16 + r16;
@@ -604,7 +576,6 @@ __global__ __launch_bounds__(512) void muon_small_kernel(Source src, Target out,
             put4(G + j * S, i, v);
         }
         __syncthreads();
-        // P = b G + c G G
         acc[0] = acc[1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int jb = 0; jb < 2; ++jb) {
@@ -612,12 +583,12 @@ __global__ __launch_bounds__(512) void muon_small_kernel(Source src, Target out,
 #pragma unroll
                 for (int p = 0; p < PL; ++p) f[p] = *reinterpret_cast<const f16x8 *>(G + (b * 16 + r16) * S + jb * 64 * PL + p * 64 + quarter * 16);
             };
-            f16x8 fa[PL], fb[2][PL];
-            rows_of(bi, fa);
-            rows_of(bj, fb[0]);
-            rows_of(bj + 1, fb[1]);
+            Rows f;
+            rows_of(bi, f.a);
+            rows_of(bj, f.b[0]);
+            rows_of(bj + 1, f.b[1]);
 #pragma unroll
-            for (int q = 0; q < 2; ++q) acc[q] = mfma16(fa, fb[q], acc[q]);
+            for (int q = 0; q < 2; ++q) acc[q] = mfma16(f.a, f.b[q], acc[q]);
         }
         const f32x4 di = *reinterpret_cast<const f32x4 *>(gd + i);
 #pragma unroll
@@ -637,7 +608,10 @@ __global__ __launch_bounds__(512) void muon_small_kernel(Source src, Target out,
             put4(P + j * S, i, v);
         }
         __syncthreads();
-        // X <- a X + P X
+    }
+    // X <- a X + P X
+    __device__ __forceinline__ void apply()
+    {
         f32x4 pdv[2][4];
 #pragma unroll
         for (int r = 0; r < 2; ++r)
@@ -647,7 +621,7 @@ __global__ __launch_bounds__(512) void muon_small_kernel(Source src, Target out,
         for (int c = 0; c < CB; ++c) {
             const int jb = wave + 8 * c;
             if (jb >= blocks) continue;
-            f32x16 sumx[2] = {};
+            f32x16 sum[2] = {};
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int at = (k >> 1) * 64 * PL + (k & 1) * 32 + half * 16;
@@ -661,49 +635,215 @@ __global__ __launch_bounds__(512) void muon_small_kernel(Source src, Target out,
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
                     if constexpr (PL == 2) {
-                        sumx[r] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[r][1], fb[0], sumx[r], 0, 0, 0);
-                        sumx[r] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[r][0], fb[1], sumx[r], 0, 0, 0);
+                        sum[r] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[r][1], fb[0], sum[r], 0, 0, 0);
+                        sum[r] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[r][0], fb[1], sum[r], 0, 0, 0);
                     }
-                    sumx[r] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[r][0], fb[0], sumx[r], 0, 0, 0);
+                    sum[r] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[r][0], fb[0], sum[r], 0, 0, 0);
                 }
             }
 #pragma unroll
             for (int r = 0; r < 2; ++r)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) x[c][r][v] = __builtin_fmaf(kA + pdv[r][v >> 2][v & 3], x[c][r][v], sumx[r][v] * (kDown * kDown));
-        }
-        if (step + 1 < steps) {
-            put_x();                               // (a wave's own columns, which no other reads before the barrier)
-            __syncthreads();
+                for (int v = 0; v < 16; ++v) x[c][r][v] = __builtin_fmaf(kA + pdv[r][v >> 2][v & 3], x[c][r][v], sum[r][v] * (kDown * kDown));
         }
     }
+    __device__ __forceinline__ void scale(double by)
+    {
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) x[c][r][v] = (float)(x[c][r][v] * by);
+    }
+    __device__ __forceinline__ void write(const Target &out, size_t base) const
+    {
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                bool there[16];
+                size_t at[16];
+#pragma unroll
+                for (int v = 0; v < 16; ++v) at[v] = base + place(c, r, v, there[v]);
+                if (out.theta) {
+                    float t[16];
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) t[v] = out.theta[at[v]];
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        if (there[v]) out.theta[at[v]] = __builtin_fmaf(-out.rate, x[c][r][v], out.keep * t[v]);
+                } else
+#pragma unroll
+                    for (int v = 0; v < 16; ++v)
+                        if (there[v]) Elem<T>::store(static_cast<T *>(out.out) + at[v], x[c][r][v]);
+            }
+    }
+};
+
+// All columns in one workgroup: everything of a matrix in one launch, and nothing but its input and output passes memory.  Three
+// barriers a step.
+template <typename T, int PL, int CB>
+__global__ __launch_bounds__(512) void muon_small_kernel(Source src, Target out, int rows, int cols, int steps)
+{
+    extern __shared__ __align__(16) char lds[];
+    FewRows<T, PL, CB> w(lds, rows, cols, 0, CB * 8);
+    const size_t base = (size_t)blockIdx.x * rows * cols;
+    const T *in = static_cast<const T *>(src.x) + base;
+    double sum = 0;
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            bool there;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) w.x[c][r][v] = Elem<T>::load(in + w.place(c, r, v, there));
+        }
 #pragma unroll
     for (int c = 0; c < CB; ++c)
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             bool there[16];
-            int at[16];
+            size_t at[16];
 #pragma unroll
-            for (int v = 0; v < 16; ++v) at[v] = place(c, r, v, there[v]);
-            if (out.theta) {
-                float t[16];
+            for (int v = 0; v < 16; ++v) at[v] = base + w.place(c, r, v, there[v]);
+            if (src.momentum) {
+                float mom[16];
 #pragma unroll
-                for (int v = 0; v < 16; ++v) t[v] = out.theta[base + at[v]];
+                for (int v = 0; v < 16; ++v) mom[v] = src.momentum[at[v]];
 #pragma unroll
-                for (int v = 0; v < 16; ++v)
-                    if (there[v]) out.theta[base + at[v]] = __builtin_fmaf(-out.rate, x[c][r][v], out.keep * t[v]);
-            } else
+                for (int v = 0; v < 16; ++v) {
+                    mom[v] = __builtin_fmaf(src.mu, mom[v], w.x[c][r][v]);
+                    if (there[v]) src.momentum[at[v]] = mom[v];
+                    w.x[c][r][v] = src.nesterov ? __builtin_fmaf(src.mu, mom[v], w.x[c][r][v]) : mom[v];
+                }
+            }
 #pragma unroll
-                for (int v = 0; v < 16; ++v)
-                    if (there[v]) Elem<T>::store(static_cast<T *>(out.out) + base + at[v], x[c][r][v]);
+            for (int v = 0; v < 16; ++v) {
+                w.x[c][r][v] = there[v] ? w.x[c][r][v] : 0.f;
+                sum = __builtin_fma((double)w.x[c][r][v], (double)w.x[c][r][v], sum);
+            }
         }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, kWave);
+    if (w.lane == 0) w.red[w.wave] = sum;
+    __syncthreads();
+    sum = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum += w.red[k];
+    w.scale(scale_of(sum));
+    for (int step = 0; step < steps; ++step) {
+        w.put_x();                                 // (a wave's own columns, which no other reads before the barrier)
+        __syncthreads();
+        w.gram();
+        w.polynomial();
+        w.apply();
+    }
+    w.write(out, base);
 }
 
-// Column blocks of a wave, 0 where a matrix is too large: its planes' room in LDS, and three blocks of X and as many sums in registers.
+// More columns: `each` blocks of 32 to a workgroup (up to 8 CB), and a launch a step.  Every workgroup adds up all workgroups' shares of G itself, in
+// order, and forms P; what it writes for the next launch is its columns of X, as its registers hold them, and its share of their G.
+// step 0: X_0 from the input; step `steps`: the output.
+template <typename T, int PL, int CB>
+__global__ __launch_bounds__(512) void muon_wide_kernel(Source src, Target out, int rows, int cols, int each, int step, int steps, const double *part,
+                                                        int parts, float *x32, const f32x4 *shares, f32x4 *share)
+{
+    extern __shared__ __align__(16) char lds[];
+    const int wgs = gridDim.x, b = blockIdx.y;
+    FewRows<T, PL, CB> w(lds, rows, cols, blockIdx.x * each, each);
+    const size_t base = (size_t)b * rows * cols;
+    float *mine = x32 + ((size_t)b * wgs + blockIdx.x) * (CB * 8 * 2048) + w.wave * 2048 + w.lane;   // [c][wave][r][v][lane]
+    const size_t at = ((size_t)b * wgs * 8 + w.wave) * 128 + w.lane;                                 // [workgroup][wave][q][lane]
+    if (step == 0) {
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    bool there;
+                    const size_t k = base + w.place(c, r, v, there);
+                    const float u = source_at<T>(src, k);
+                    w.x[c][r][v] = there ? u : 0.f;
+                }
+        double norm2 = 0;
+        for (int k = threadIdx.x; k < parts; k += 512) norm2 += part[b * kParts + k];
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) norm2 += __shfl_xor(norm2, o, kWave);
+        if (w.lane == 0) w.red[w.wave] = norm2;
+        __syncthreads();
+        norm2 = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) norm2 += w.red[k];
+        w.scale(scale_of(norm2));
+    } else {
+#pragma unroll
+        for (int c = 0; c < CB; ++c)
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) w.x[c][r][v] = mine[c * (8 * 2048) + (r * 16 + v) * 64];
+        w.put_x();
+        w.acc[0] = w.acc[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        constexpr int U = 8;                       // shares on their way
+        for (int g = 0; g < wgs; g += U) {
+            f32x4 u[U][2];
+#pragma unroll
+            for (int k = 0; k < U; ++k)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) u[k][q] = g + k < wgs ? shares[at + (size_t)(g + k) * 1024 + q * 64] : f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int k = 0; k < U; ++k)
+#pragma unroll
+                for (int q = 0; q < 2; ++q) w.acc[q] += u[k][q];
+        }
+        w.polynomial();
+        w.apply();
+    }
+    if (step == steps) {
+        w.write(out, base);
+        return;
+    }
+    w.put_x();
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) mine[c * (8 * 2048) + (r * 16 + v) * 64] = w.x[c][r][v];
+    __syncthreads();
+    w.gram();
+#pragma unroll
+    for (int q = 0; q < 2; ++q) share[at + (size_t)blockIdx.x * 1024 + q * 64] = w.acc[q];
+}
+
+// Column blocks of a wave in one workgroup, 0 where a matrix is too large: its planes' room in LDS, and at most two blocks of X
+// (three spill registers and gain nothing: 64 x 576 takes 42 us with them, 43 us in three workgroups and seven launches).
 int small_blocks(int planes, int rows, int cols)
 {
-    const int m = rows < cols ? rows : cols, n = rows < cols ? cols : rows, cb = ((n + 31) / 32 + 7) / 8;
-    return m <= kSmallRows && cb <= (planes == 2 ? 2 : 3) && small_lds(planes, n) <= kSmallLds ? cb : 0;
+    const int m = rows < cols ? rows : cols, n = rows < cols ? cols : rows, blocks = (n + 31) / 32, cb = (blocks + 7) / 8;
+    return m <= kFewRows && cb <= 2 && few_lds(planes, blocks) <= kLds ? cb : 0;
+}
+// Matrices of few rows with more columns: 256 columns to a workgroup while that makes at most 16, whose shares each of them adds up,
+// else as many as LDS has room for, up to 512.
+struct Wide { int cb, each, wgs, parts; size_t part, x32, share, total; };
+bool is_wide(int rows, int cols) { return rows <= kFewRows || cols <= kFewRows; }
+Wide wide_plan(int planes, int batch, int rows, int cols)
+{
+    Wide w;
+    const int blocks = ((rows < cols ? cols : rows) + 31) / 32;
+    w.cb = blocks <= 16 * 8 ? 1 : 2;
+    w.each = w.cb * 8;
+    while (few_lds(planes, w.each) > kLds) --w.each;
+    w.wgs = (blocks + w.each - 1) / w.each;
+    const size_t each = ((size_t)rows * cols + 2047) / 2048;
+    w.parts = each < kParts ? (int)each : kParts;
+    w.part = round_up((size_t)batch * kParts * 8, 256);
+    w.x32 = round_up((size_t)batch * w.wgs * w.cb * 8 * 2048 * 4, 256);
+    w.share = round_up((size_t)batch * w.wgs * 16384, 256);
+    w.total = w.part + w.x32 + 2 * w.share;
+    return w;
 }
 
 inline int round_to(int v, int to) { return (v + to - 1) / to * to; }
@@ -729,9 +869,10 @@ Layout layout_of(int planes, int batch, int rows, int cols, char *ws, size_t &to
     L.rows = rows; L.cols = cols; L.tall = rows > cols; L.batch = batch;
     L.m = L.tall ? cols : rows; L.n = L.tall ? rows : cols;
     // 256 x 256 tiles where the product with X takes no more of the chip's rounds with them (a tile is four times the work of a
-    // 128 x 128 one, in about 3.4 times its time)
+    // 128 x 128 one, in about 3.4 times its time), and the contraction over m is long beside what a tile begins and ends with
+    // (7 x 512 x 4608, bf16: 468 us with them, 427 us without; 4096 x 4096: 1.63 ms, 2.02 ms)
     auto rounds = [&](int t) { return ((long)batch * (round_to(L.m, t) / t) * (round_to(L.n, t) / t) + 255) / 256; };
-    L.tile = 3.4 * rounds(256) <= rounds(128) ? 256 : 128;
+    L.tile = L.m >= 1024 && 3.4 * rounds(256) <= rounds(128) ? 256 : 128;
     L.mp = round_to(L.m, L.tile); L.np = round_to(L.n, L.tile);
     const int mt = L.mp / L.tile;
     const long tiles = (long)batch * (mt * (mt + 1) / 2);
@@ -786,9 +927,22 @@ template <typename T, int PL>
 int run(int batch, int rows, int cols, int steps, const Source &src, const Target &out, void *ws, hipStream_t s)
 {
     if (const int cb = small_blocks(PL, rows, cols)) {
-        auto kern = cb == 1 ? muon_small_kernel<T, PL, 1> : cb == 2 || PL == 2 ? muon_small_kernel<T, PL, 2> : muon_small_kernel<T, PL, PL == 2 ? 2 : 3>;
+        auto kern = cb == 1 ? muon_small_kernel<T, PL, 1> : muon_small_kernel<T, PL, 2>;
         if (!raise_lds_limit(reinterpret_cast<const void *>(kern))) return VGG_ERR_LAUNCH;
-        hipLaunchKernelGGL(kern, dim3(batch), dim3(512), small_lds(PL, rows < cols ? cols : rows), s, src, out, rows, cols, steps);
+        hipLaunchKernelGGL(kern, dim3(batch), dim3(512), few_lds(PL, ((rows < cols ? cols : rows) + 31) / 32), s, src, out, rows, cols, steps);
+        return launch_status();
+    }
+    if (is_wide(rows, cols)) {
+        const Wide p = wide_plan(PL, batch, rows, cols);
+        auto kern = p.cb == 1 ? muon_wide_kernel<T, PL, 1> : muon_wide_kernel<T, PL, 2>;
+        if (!raise_lds_limit(reinterpret_cast<const void *>(kern))) return VGG_ERR_LAUNCH;
+        double *part = static_cast<double *>(ws);
+        float *x32 = reinterpret_cast<float *>(static_cast<char *>(ws) + p.part);
+        f32x4 *share[2];
+        for (int k = 0; k < 2; ++k) share[k] = reinterpret_cast<f32x4 *>(static_cast<char *>(ws) + p.part + p.x32 + k * p.share);
+        hipLaunchKernelGGL((muon_norm_kernel<T>), dim3(p.parts, batch), dim3(256), 0, s, src, part, (size_t)rows * cols);
+        for (int k = 0; k <= steps; ++k)
+            hipLaunchKernelGGL(kern, dim3(p.wgs, batch), dim3(512), few_lds(PL, p.each), s, src, out, rows, cols, p.each, k, steps, part, p.parts, x32, share[1 - (k & 1)], share[k & 1]);
         return launch_status();
     }
     size_t total;
@@ -803,8 +957,10 @@ int run(int batch, int rows, int cols, int steps, const Source &src, const Targe
 
 size_t muon_workspace(int dtype, int batch, int rows, int cols)
 {
+    const int planes = dtype == VGG_BF16 ? 1 : 2;
+    if (is_wide(rows, cols)) return wide_plan(planes, batch, rows, cols).total;   // (one workgroup alone needs none)
     size_t total;
-    layout_of(dtype == VGG_BF16 ? 1 : 2, batch, rows, cols, nullptr, total);
+    layout_of(planes, batch, rows, cols, nullptr, total);
     return total;
 }
 

@@ -70,7 +70,7 @@ def test_orthogonalize_against_64_bits(dtype, shape):
 
 
 @pytest.mark.parametrize("dtype", [B.F32, B.BF16])
-@pytest.mark.parametrize("shape", [(1, 512, 4608), (1, 1000, 4096), (7, 256, 2304), (1, 2100, 700), (1, 1300, 5000), (2, 2048, 2048)])
+@pytest.mark.parametrize("shape", [(1, 512, 4608), (1, 1000, 4096), (7, 256, 2304), (1, 2100, 700), (3, 989, 16), (2, 28, 7933), (1, 64, 4097), (1, 30000, 10), (5, 3209, 64), (1, 1300, 5000), (2, 2048, 2048)])
 def test_orthogonalize_of_the_networks_shapes(dtype, shape):
     x = matrices(dtype, *shape, seed=1)
     got = orthogonalize(dtype, x, 5)
