@@ -1,0 +1,121 @@
+"""The dense head: training step, rounding and answers run together, against the same steps in 64 bits."""
+import os
+import subprocess
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+from paper_1810_09868_amd import binding as B
+from paper_1810_09868_amd.head import DenseHead
+
+pytestmark = pytest.mark.gpu
+
+DIMS = [96, 64, 40, 10]
+
+
+def parameters(seed):
+    rng = np.random.default_rng(seed)
+    w = [(rng.standard_normal((o, i)) * np.sqrt(2.0 / i)).astype(np.float32) for i, o in zip(DIMS[:-1], DIMS[1:])]
+    return w, [(0.1 * rng.standard_normal(o)).astype(np.float32) for o in DIMS[1:]]
+
+
+def ns64(u):
+    x = u.T if u.shape[0] > u.shape[1] else u
+    x = x / (np.sqrt((x * x).sum()) + 1e-7)
+    for _ in range(5):
+        g = x @ x.T
+        x = 3.4445 * x + (-4.775 * g + 2.0315 * (g @ g)) @ x
+    return x.T if u.shape[0] > u.shape[1] else x
+
+
+def step64(w, b, mom, x, y, lr, mu, bias_lr, weight):
+    acts = [x]
+    for l in range(len(w)):
+        z = acts[-1] @ w[l].T + b[l]
+        acts.append(np.maximum(z, 0) if l + 1 < len(w) else z)
+    z = acts[-1] - acts[-1].max(1, keepdims=True)
+    lp = z - np.log(np.exp(z).sum(1, keepdims=True))
+    p, n = np.exp(lp), len(y)
+    H = -(p * lp).sum(1, keepdims=True)
+    dz = (p - np.eye(p.shape[1])[y]) / n + weight / n * p * (lp + H)
+    grads = []
+    for l in reversed(range(len(w))):
+        grads.insert(0, (dz.T @ acts[l], dz.sum(0)))
+        if l:
+            dz = (dz @ w[l]) * (acts[l] > 0)
+    for l, (gw, gb) in enumerate(grads):
+        mom[l] = mu * mom[l] + gw
+        w[l] = w[l] - lr * np.sqrt(max(1, w[l].shape[0] / w[l].shape[1])) * ns64(gw + mu * mom[l])
+        b[l] = b[l] - bias_lr * gb
+    return lp[np.arange(n), y]
+
+
+@pytest.mark.parametrize("weight", [0.0, 0.1])
+def test_training_steps_in_fp32_follow_64_bits(weight):
+    w, b = parameters(0)
+    head = DenseHead(B.F32, 50, DIMS, lr=0.05, mu=0.9, bias_lr=0.1)
+    head.load([torch.from_numpy(a) for a in w], [torch.from_numpy(a) for a in b])
+    w, b = [a.astype(np.float64) for a in w], [a.astype(np.float64) for a in b]
+    mom = [np.zeros_like(a) for a in w]
+    rng = np.random.default_rng(1)
+    for n in (50, 17, 1):
+        x, y = np.maximum(rng.standard_normal((n, DIMS[0])), 0).astype(np.float32), rng.integers(0, DIMS[-1], n).astype(np.int32)
+        logp = head.train_step(torch.from_numpy(x).cuda(), torch.from_numpy(y).cuda(), weight)
+        want = step64(w, b, mom, x.astype(np.float64), y, 0.05, 0.9, 0.1, weight)
+        # fp32 layers are 1e-6 off and a step (of 0.05 to a weight) 3e-5 of itself; three of them
+        assert np.abs(logp.double().cpu().numpy() - want).max() < 1e-4
+    for mine, ref in zip(head.w + head.b, w + b):
+        assert np.linalg.norm(mine.double().cpu().numpy() - ref) <= 2e-4 * np.linalg.norm(ref)
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+def test_it_learns_and_its_four_bits_answer_alike(dtype):
+    td = torch.bfloat16 if dtype == B.BF16 else torch.float32
+    g = torch.Generator(device="cuda").manual_seed(2)
+    w, b = parameters(3)
+    head = DenseHead(dtype, 64, DIMS, lr=0.03, group=32, top=3)
+    head.load([torch.from_numpy(a) for a in w], [torch.from_numpy(a) for a in b])
+    centres = torch.randn((10, DIMS[0]), generator=g, device="cuda")
+
+    def batch(n):
+        y = torch.randint(0, 10, (n,), generator=g, device="cuda", dtype=torch.int32)
+        return (centres[y.long()] + 0.5 * torch.randn((n, DIMS[0]), generator=g, device="cuda")).clamp_min(0).to(td), y
+
+    first = float(head.train_step(*batch(64)).mean())
+    for _ in range(40):
+        last = float(head.train_step(*batch(64)).mean())
+    assert last > -0.1 > first
+    x, y = batch(64)
+    full = head.answer(x, y)
+    z = head.logits.double().clone()
+    assert (full.top_idx[:, 0] == y).float().mean() > 0.95
+    lp = torch.log_softmax(z, 1)
+    assert float((full.logp.double() - lp.gather(1, y.long()[:, None])[:, 0]).abs().max()) < 1e-5
+    assert float((full.entropy.double() + (lp.exp() * lp).sum(1)).abs().max()) < 1e-5
+    assert head.quantize() < sum(p.numel() for p in head.w)            # bytes of 4-bit weights and their scales
+    few = head.answer(x, y)
+    assert (few.top_idx[:, 0] == y).float().mean() > 0.95
+    one = head.answer(x[5:6].contiguous())
+    assert one.logp is None and int(one.top_idx[0, 0]) == int(few.top_idx[5, 0]) and one.top_logp.shape == (1, 3)
+
+
+def test_refusals():
+    head = DenseHead(B.F32, 4, [8, 3])
+    with pytest.raises(ValueError):
+        head.answer(torch.zeros((5, 8), device="cuda"))
+    with pytest.raises(ValueError):
+        head.answer(torch.zeros((2, 9), device="cuda"))
+    with pytest.raises(ValueError):
+        DenseHead(B.BF16, 4, [9, 3])
+    with pytest.raises(ValueError):
+        DenseHead(B.F32, 4, [9])
+
+
+def test_example_runs():
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, os.path.join(root, "examples", "train_and_serve_head.py"), "--steps", "21"], capture_output=True,
+                       text=True, timeout=100)
+    assert r.returncode == 0, r.stderr[-2000:]
+    assert "4-bit weights" in r.stdout and "one row" in r.stdout
