@@ -76,22 +76,22 @@ template <int V> __device__ __forceinline__ void add_scores(Sums &a, const float
     bool fresh = most > a.m;
     if (fresh) rebase(a, most);
     const float base = a.m == -INFINITY ? 0.f : a.m;
-    float e[V];
+    if (__any(fresh)) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const float d = z[j] - base;
-        e[j] = __expf(d);
-        a.t = __builtin_fmaf(fmaxf(d, kLowest), e[j], a.t);
-    }
-    if (__any(fresh))
-#pragma unroll
-        for (int j = 0; j < V; ++j) {       // one of the new largest does not count
-            const bool it = fresh && z[j] == a.m;
-            e[j] = it ? 0.f : e[j];
+        for (int j = 0; j < V; ++j) {
+            const float d = z[j] - base, e = __expf(d);
+            const bool it = fresh && z[j] == a.m;      // one of the new largest does not count
+            a.e += it ? 0.f : e;
+            a.t = __builtin_fmaf(fmaxf(d, kLowest), e, a.t);
             fresh = fresh && !it;
         }
+    } else
 #pragma unroll
-    for (int j = 0; j < V; ++j) a.e += e[j];
+        for (int j = 0; j < V; ++j) {
+            const float d = z[j] - base, e = __expf(d);
+            a.e += e;
+            a.t = __builtin_fmaf(fmaxf(d, kLowest), e, a.t);
+        }
 }
 
 // A score and its class as one number: the better, the larger; equal scores: the lower class.  0: none.
@@ -136,20 +136,27 @@ template <int I> __device__ __forceinline__ void cut_list(Key *list, int count, 
         mine[i] = lane + 64 * i < count ? list[lane + 64 * i] : 0;
         rank[i] = 0;
     }
-    int q = 0;
-    for (; q + 4 <= count; q += 4) {
-        Key k[4];
+    if constexpr (I == 1) {                          // one key to a lane: registers are nearer than LDS
+        for (int q = 0; q < count; ++q) {
+            const Key k = (Key)(unsigned)__builtin_amdgcn_readlane((int)(mine[0] >> 32), q) << 32 | (unsigned)__builtin_amdgcn_readlane((int)mine[0], q);
+            rank[0] += k > mine[0];
+        }
+    } else {
+        int q = 0;
+        for (; q + 4 <= count; q += 4) {
+            Key k[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) k[j] = list[q + j];
+            for (int j = 0; j < 4; ++j) k[j] = list[q + j];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int i = 0; i < I; ++i) rank[i] += k[j] > mine[i];
-    }
-    for (; q < count; ++q) {
-        const Key k = list[q];
+                for (int i = 0; i < I; ++i) rank[i] += k[j] > mine[i];
+        }
+        for (; q < count; ++q) {
+            const Key k = list[q];
 #pragma unroll
-        for (int i = 0; i < I; ++i) rank[i] += k > mine[i];
+            for (int i = 0; i < I; ++i) rank[i] += k > mine[i];
+        }
     }
     wave_sync();
 #pragma unroll
@@ -184,14 +191,29 @@ __device__ __forceinline__ void offer(Best &b, float v, int id, int lane)
     b.count += __builtin_popcountll(mask);
     if (b.count > kList - 64) cut(b, lane);
 }
-// From each lane's best of a first lot: at least `top` of all scores are as good as the top-th of these.
-__device__ __forceinline__ void expect(Best &b, float most)
+// A bar that at least `top` of a first lot's scores reach, so of all: halvings between the least of the lanes' best
+// and the largest bring it near the top-th.  For few alternatives only the lanes' best are counted.
+template <int V> __device__ __forceinline__ void expect(Best &b, const float (&z)[V], float most)
 {
-    int rank = 0;
+    const int lanes = __builtin_popcountll(__ballot(most > -INFINITY));
+    if (lanes < b.top) return;
+    float lo = all_min(most > -INFINITY ? most : INFINITY), hi = all_max(most);   // (`lanes` scores at least reach lo)
+    if (!(hi < INFINITY)) return;                    // (the row's results are NaN)
+#pragma unroll 1
+    for (int k = 0; k < 8; ++k) {
+        const float t = 0.5f * lo + 0.5f * hi;
+        int count = 0;
+        if (b.top > 8) {
 #pragma unroll
-    for (int l = 0; l < 64; ++l) rank += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(most), l)) > most;
-    const float t = all_min(rank < b.top ? most : INFINITY);
-    if (t > -INFINITY) { b.worst_v = t; b.worst_id = 0x7fffffff; }
+            for (int j = 0; j < V; ++j) count += __builtin_popcountll(__ballot(z[j] >= t));
+        } else
+            count = __builtin_popcountll(__ballot(most >= t));
+        const bool enough = count >= b.top;
+        lo = enough ? t : lo;
+        hi = enough ? hi : t;
+    }
+    b.worst_v = lo;
+    b.worst_id = 0x7fffffff;
 }
 
 template <typename T> constexpr int kVec = 16 / (int)sizeof(T);   // scores of a 16-byte load
@@ -271,7 +293,7 @@ template <int W, typename F> __device__ __forceinline__ void merge_lists(const K
 template <typename T, int W, bool TOP>
 __global__ __launch_bounds__(256) void log_probs_kernel(const T *__restrict__ z, ScoreArgs a)
 {
-    constexpr int V = kVec<T>, U = 4;    // U loads at a time
+    constexpr int V = kVec<T>, U = 16 / V;   // sixteen scores a lane at a time
     __shared__ Sums sums[4];
     __shared__ Key lists[TOP ? 4 : 1][kList];
     __shared__ int counts[4];
@@ -297,37 +319,30 @@ __global__ __launch_bounds__(256) void log_probs_kernel(const T *__restrict__ z,
     const int end_k = lane < head ? k0 + lane : tail0 + lane - head;
     if ((W == 1 || wave == 0) && (lane < head || end_k < k1)) ends = Elem<T>::load(zr + end_k);
     for (int i0 = ti; i0 - ti < nvec; i0 += U * tn) {
-        float x[U][V];
+        float x[U * V];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int i = i0 + u * tn;
-            if (i < nvec) load_scores(zr + v0 + (size_t)i * V, x[u]);
+            float v[V];
+            if (i < nvec) load_scores(zr + v0 + (size_t)i * V, v);
             else
 #pragma unroll
-                for (int j = 0; j < V; ++j) x[u][j] = -INFINITY;
-        }
-        float most[U];
+                for (int j = 0; j < V; ++j) v[j] = -INFINITY;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            most[u] = x[u][0];
-#pragma unroll
-            for (int j = 1; j < V; ++j) most[u] = fmaxf(most[u], x[u][j]);
+            for (int j = 0; j < V; ++j) x[u * V + j] = v[j];
         }
+        float lot = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < U * V; ++j) lot = fmaxf(lot, x[j]);
         if constexpr (TOP)
-            if (i0 == ti) expect(b, fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])));
+            if (i0 == ti) expect(b, x, lot);
+        add_scores<U * V>(mine, x, lot);
+        if constexpr (TOP)
+            if (__any(lot >= b.worst_v && lot > -INFINITY)) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) add_scores<V>(mine, x[u], most[u]);
-        if constexpr (TOP) {
-            const float lot = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
-            if (__ballot(lot >= b.worst_v && lot > -INFINITY)) {
-#pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (__ballot(most[u] >= b.worst_v))
-#pragma unroll
-                        for (int j = 0; j < V; ++j) offer(b, x[u][j], v0 + (i0 + u * tn) * V + j, lane);
+                for (int j = 0; j < U * V; ++j) offer(b, x[j], v0 + (i0 + j / V * tn) * V + j % V, lane);
                 if (b.count > b.top + 24 && i0 - ti + U * tn < nvec) cut(b, lane);   // (what follows meets a higher bar)
             }
-        }
     }
     {
         const float x[1] = {ends};
@@ -359,43 +374,42 @@ __global__ __launch_bounds__(256) void log_probs_kernel(const T *__restrict__ z,
     }
 }
 
-// The parts of a row: a workgroup of four waves to each row.
+// The parts of a row: a wave to each row, a part to a lane.  The parts' lists are in order: where no part's r-th best may enter, no
+// later one may.
 template <typename T, bool TOP>
-__global__ __launch_bounds__(256) void log_probs_join_kernel(const T *__restrict__ z, ScoreArgs a)
+__global__ __launch_bounds__(64) void log_probs_join_kernel(const T *__restrict__ z, ScoreArgs a)
 {
-    __shared__ Sums sums[4];
-    __shared__ Key lists[TOP ? 4 : 1][kList];
-    __shared__ int counts[4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = blockIdx.x;
+    __shared__ Key list[TOP ? kList : 1];
+    const int lane = threadIdx.x, row = blockIdx.x;
     const int y = a.logp ? a.labels[row] : -1;
     const float z_label = y >= 0 && y < a.K ? Elem<T>::load(z + (size_t)row * a.ldz + y) : 0.f;
+    const Key *keys = a.part_best + (size_t)row * a.parts * a.top;
     Sums mine = {-INFINITY, 0.f, 0.f};
-    for (int p = threadIdx.x; p < a.parts; p += 256) {
+    for (int p = lane; p < a.parts; p += 64) {
         const float *s = a.part_sums + ((size_t)row * a.parts + p) * 3;
         mine = joined(mine, {s[0], s[1], s[2]});
     }
-    mine = wave_joined(mine, lane);
-    Best b = {lists[TOP ? wave : 0], 0, a.top, -INFINITY, -1};
+    Best b = {list, 0, a.top, -INFINITY, -1};
     if constexpr (TOP) {
-        const int n = a.parts * a.top;
-        const Key *keys = a.part_best + (size_t)row * n;
-        for (int i0 = wave * 64; i0 < n; i0 += 256) {
-            const Key k = i0 + lane < n ? keys[i0 + lane] : 0;
-            const float v = k ? score_of(k) : -INFINITY;
-            if (i0 == wave * 64) expect(b, v);
-            offer(b, v, class_of(k), lane);
+        const int all = a.parts * a.top;             // (entry e: of part e % parts, its (e / parts)-th)
+        auto entry = [&](int e) __attribute__((always_inline)) {
+            return e < all ? keys[(size_t)(e % a.parts) * a.top + e / a.parts] : 0;
+        };
+        Key next = entry(lane);
+        for (int e0 = 0, without = 0; e0 < all && without < a.parts; e0 += 64) {
+            const Key k = next;
+            next = entry(e0 + 64 + lane);
+            const float v[1] = {k ? score_of(k) : -INFINITY};
+            if (e0 == 0) expect(b, v, v[0]);
+            without = __any(may_enter(b, v[0], class_of(k))) ? 0 : without + 64;
+            offer(b, v[0], class_of(k), lane);
+            if (b.count >= a.top + 32) cut(b, lane);
         }
         cut(b, lane);
     }
-    if (lane == 0) {
-        sums[wave] = mine;
-        counts[wave] = b.count;
-    }
-    __syncthreads();
-    mine = sums[0];
-    for (int w = 1; w < 4; ++w) mine = joined(mine, sums[w]);
-    if (threadIdx.x == 0) write_row(a, mine, z_label, y, row);
-    if constexpr (TOP) merge_lists<4>(lists, counts, a.top, [&](int i, Key k) { write_best(a, mine, row, i, k); });
+    mine = wave_joined(mine, lane);
+    if (lane == 0) write_row(a, mine, z_label, y, row);
+    if (TOP && lane < a.top) write_best(a, mine, row, lane, lane < b.count ? list[lane] : 0);
 }
 
 // dz_j = g (1[j = y] - p_j) - h p_j (log p_j + entropy).
@@ -477,7 +491,7 @@ static int log_probs_of(const T *z, const ScoreArgs &a, hipStream_t s)
     const unsigned units = (unsigned)a.N * a.parts;
     if (a.K <= kOneWave) hipLaunchKernelGGL((log_probs_kernel<T, 1, TOP>), dim3((units + 3) / 4), dim3(256), 0, s, z, a);
     else hipLaunchKernelGGL((log_probs_kernel<T, 4, TOP>), dim3(units), dim3(256), 0, s, z, a);
-    if (a.parts > 1) hipLaunchKernelGGL((log_probs_join_kernel<T, TOP>), dim3(a.N), dim3(256), 0, s, z, a);
+    if (a.parts > 1) hipLaunchKernelGGL((log_probs_join_kernel<T, TOP>), dim3(a.N), dim3(64), 0, s, z, a);
     return launch_status();
 }
 
