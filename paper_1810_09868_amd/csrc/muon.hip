@@ -7,14 +7,15 @@
 // Products are on the f16 matrix unit with fp32 sums.  X, G and P = b G + c G G are bounded (|X|, |G|, |P| <= 1.21, 1.47, 2.9), so
 // that they are held times 2^14, below f16's largest, and need no other scale; f16 then keeps 11 bits of everything down to
 // 2^-28.  PLANES = 2 (VGG_F32): a value is two f16 numbers, the nearest and what that leaves, 22 bits; hi hi + hi lo + lo hi
-// leaves out 2^-22 of a product at most.  PLANES = 1 (VGG_BF16): operands are rounded to 11 bits.  In both the term a X adds an
-// fp32 copy of X, since a rounding of X there would grow 3.4-fold in every later step where X has no (or small) singular values;
-// and the diagonals of G and P, which hold most of them, are kept apart in fp32 (zeros in the planes): with G = D + E,
+// leaves out 2^-22 of a product at most.  PLANES = 1 (VGG_BF16): operands are rounded to 11 bits.  The term a X takes all of X, an
+// fp32 copy or (PLANES = 1) the operand and what it leaves, another f16 number, 22 bits in all: a rounding of X to 11 bits there would
+// grow 3.4-fold in every later step where X has no (or small) singular values.  In both the diagonals of G and P, which hold most of them, are kept apart in fp32 (zeros in the planes): with G = D + E,
 //     (G G)_ij = (E E)_ij + (d_i + d_j) e_ij,   (G G)_ii = (E E)_ii + d_i^2,   (P X)_i = p_i X_i + (the rest of P) X.
 // One plane is then 3e-4 to 1e-3 off in all, against 1.3e-3 to 2.4e-3 with the diagonals rounded (bf16's own rounding: 1.7e-3).
 //
 // X, G and P lie in columns of 128 bytes to a row: [column][row][64 elements], or [32 elements of the first plane, 32 of the
-// second], so that what a workgroup copies for a stage of its contraction is contiguous.  X's fp32 copy lies in columns of 32.
+// second], so that what a workgroup copies for a stage of its contraction is contiguous.  X's fp32 copy lies in columns of 32,
+// the rest of its f16 copy as that does.
 // G and G G contract along rows of both operands; P X takes X's columns, which LDS hands out transposed (ds_read_b64_tr_b16), so
 // that X is kept once.  X is padded with zeros to whole tiles.  G and P are symmetric: the tiles on and below the diagonal are
 // formed, over a few ranges of the contraction where they are too few to fill the chip, and a second kernel adds the ranges in
@@ -74,31 +75,77 @@ template <typename T> __device__ __forceinline__ float source_at(const Source &s
     return s.nesterov ? __builtin_fmaf(s.mu, m, g) : m;
 }
 
+// 16 bytes from or to an address that is a multiple of an element's size only; a thread's V elements at a time, the first n of them.
+template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Loose { T v[16 / sizeof(T)]; };
+template <typename T, int V> __device__ __forceinline__ void load_some(const T *p, int n, float (&v)[V])
+{
+    constexpr int L = 16 / (int)sizeof(T);
+    if (n >= V) {
+#pragma unroll
+        for (int h = 0; h < V / L; ++h) {
+            const Loose<T> l = *reinterpret_cast<const Loose<T> *>(p + h * L);
+#pragma unroll
+            for (int k = 0; k < L; ++k) v[h * L + k] = Elem<T>::load(&l.v[k]);
+        }
+    } else
+#pragma unroll
+        for (int k = 0; k < V; ++k) v[k] = k < n ? Elem<T>::load(p + k) : 0.f;
+}
+template <typename T, int V> __device__ __forceinline__ void store_some(T *p, int n, const float (&v)[V])
+{
+    constexpr int L = 16 / (int)sizeof(T);
+    if (n >= V) {
+#pragma unroll
+        for (int h = 0; h < V / L; ++h) {
+            Loose<T> l;
+#pragma unroll
+            for (int k = 0; k < L; ++k) Elem<T>::store(&l.v[k], v[h * L + k]);
+            *reinterpret_cast<Loose<T> *>(p + h * L) = l;
+        }
+    } else
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            if (k < n) Elem<T>::store(p + k, v[k]);
+}
+
+constexpr int kNormLoads = 4;                           // of 16 bytes, in flight
+template <typename T> constexpr int kNormLot = 256 * kNormLoads * 16 / (int)sizeof(T);   // elements of a workgroup at a time
+inline int norm_parts(size_t count, size_t lot) { return (int)((count + lot - 1) / lot < (size_t)kParts ? (count + lot - 1) / lot : (size_t)kParts); }
 template <typename T>
 __global__ __launch_bounds__(256) void muon_norm_kernel(Source s, double *__restrict__ part, size_t count)
 {
-    constexpr int U = 8;                                // loads in flight
-    const size_t base = (size_t)blockIdx.y * count, step = (size_t)gridDim.x * 256;
+    constexpr int U = kNormLoads, V = 16 / (int)sizeof(T);
+    const size_t base = (size_t)blockIdx.y * count, step = (size_t)gridDim.x * 256 * V;
     const T *x = static_cast<const T *>(s.x) + base;
     float *mom = s.momentum ? s.momentum + base : nullptr;
     double sum = 0;
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < count; i += U * step) {
-        float u[U];
+    for (size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * V; i < count; i += U * step) {
+        float u[U][V];
+        auto left = [&](int k) __attribute__((always_inline)) {
+            const size_t at = i + k * step;
+            return at >= count ? 0 : count - at < (size_t)V ? (int)(count - at) : V;
+        };
 #pragma unroll
-        for (int k = 0; k < U; ++k) u[k] = i + k * step < count ? Elem<T>::load(x + i + k * step) : 0.f;
+        for (int k = 0; k < U; ++k) load_some<T, V>(x + i + k * step, left(k), u[k]);
         if (mom) {
-            float m[U];
+            float m[U][V];
 #pragma unroll
-            for (int k = 0; k < U; ++k) m[k] = i + k * step < count ? mom[i + k * step] : 0.f;
+            for (int k = 0; k < U; ++k) load_some<float, V>(mom + i + k * step, left(k), m[k]);
 #pragma unroll
             for (int k = 0; k < U; ++k) {
-                m[k] = __builtin_fmaf(s.mu, m[k], u[k]);
-                if (i + k * step < count) mom[i + k * step] = m[k];
-                u[k] = s.nesterov ? __builtin_fmaf(s.mu, m[k], u[k]) : m[k];
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    m[k][j] = __builtin_fmaf(s.mu, m[k][j], u[k][j]);
+                    u[k][j] = s.nesterov ? __builtin_fmaf(s.mu, m[k][j], u[k][j]) : m[k][j];
+                }
+                float *to = mom + i + k * step;
+                store_some<float, V>(to, left(k), m[k]);
             }
         }
 #pragma unroll
-        for (int k = 0; k < U; ++k) sum = __builtin_fma((double)u[k], (double)u[k], sum);
+        for (int k = 0; k < U; ++k)
+#pragma unroll
+            for (int j = 0; j < V; ++j) sum = __builtin_fma((double)u[k][j], (double)u[k][j], sum);
     }
     sum = block_sum(sum);
     if (threadIdx.x == 0) part[blockIdx.y * kParts + blockIdx.x] = sum;
@@ -108,7 +155,8 @@ __global__ __launch_bounds__(256) void muon_norm_kernel(Source s, double *__rest
 struct Layout {
     int rows, cols, m, n, mp, np, tall, tile, parts, batch;   // tile: of the products, 128 or 256, which mp and np are multiples of
     int splits[2];         // of the Gram matrix and its square
-    float *x32;            // [batch][np / 32][mp][32]
+    float *x32;            // [batch][np / 32][mp][32]: PLANES = 2
+    half_t *rest;          // as x, what that leaves: PLANES = 1
     half_t *x[2];          // [batch][columns][mp][64], of mp x np
     half_t *g, *p;         // [batch][columns][mp][64], of mp x mp, zero diagonals
     float *gd, *pd;        // [batch][mp], the diagonals
@@ -116,42 +164,63 @@ struct Layout {
     double *part;          // [batch][kParts]
 };
 
-// X_0 in all its forms, zeros where they are padded.  A workgroup: 64 x 64 of the padded X.
+// X_0 in all its forms, zeros where they are padded.  A workgroup: 64 x 64 of the padded X, eight consecutive elements to a thread.
 template <typename T, int PL>
 __global__ __launch_bounds__(256) void muon_start_kernel(Source s, Layout L)
 {
     __shared__ float tile[64][65];
-    const int b = blockIdx.z, i0 = blockIdx.y * 64, j0 = blockIdx.x * 64, tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
+    const int b = blockIdx.z, i0 = blockIdx.y * 64, j0 = blockIdx.x * 64, t8 = (threadIdx.x & 7) * 8, ty = threadIdx.x >> 3;
     const size_t base = (size_t)b * L.rows * L.cols;
     // the source is read along its own rows
-    float v[16];
+    float v[2][8];
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-        const int y = ty + 4 * k, i = L.tall ? i0 + tx : i0 + y, j = L.tall ? j0 + y : j0 + tx;      // of X
-        v[k] = i < L.m && j < L.n ? source_at<T>(s, base + (L.tall ? (size_t)j * L.cols + i : (size_t)i * L.cols + j)) : 0.f;
+    for (int k = 0; k < 2; ++k) {
+        const int r = (L.tall ? j0 : i0) + ty + 32 * k, c = (L.tall ? i0 : j0) + t8, n = r < L.rows ? L.cols - c : 0;
+        const size_t at = base + (size_t)r * L.cols + c;
+        load_some<T, 8>(static_cast<const T *>(s.x) + at, n, v[k]);
+        if (s.momentum) {                              // (stepped already)
+            float m[8];
+            load_some<float, 8>(s.momentum + at, n, m);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[k][j] = s.nesterov ? __builtin_fmaf(s.mu, m[j], v[k][j]) : m[j];
+        }
     }
     double norm2 = 0;
     for (int k = threadIdx.x; k < L.parts; k += 256) norm2 += L.part[b * kParts + k];
     norm2 = block_sum(norm2);
     const double by = scale_of(norm2);
-    float *x32 = L.x32 + (size_t)b * L.mp * L.np;
-    half_t *x = L.x[0] + (size_t)b * L.mp * L.np * PL;
     if (L.tall) {
 #pragma unroll
-        for (int k = 0; k < 16; ++k) tile[tx][ty + 4 * k] = v[k];
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) tile[t8 + j][ty + 32 * k] = v[k][j];
         __syncthreads();
 #pragma unroll
-        for (int k = 0; k < 16; ++k) v[k] = tile[ty + 4 * k][tx];
-    }
+        for (int k = 0; k < 2; ++k)
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-        const int y = ty + 4 * k;
-        const float w = (float)(v[k] * by);
-        x32[at_x32(L.mp, i0 + y, j0 + tx)] = w;
-        half_t *to = x + at_column<PL>(L.mp, i0 + y, j0 + tx);
-        const half_t hi = (half_t)(w * kUp);
-        to[0] = hi;
-        if constexpr (PL == 2) to[32] = (half_t)(w * kUp - (float)hi);
+            for (int j = 0; j < 8; ++j) v[k][j] = tile[ty + 32 * k][t8 + j];
+    }
+    const size_t mn = (size_t)L.mp * L.np;
+    half_t *x = L.x[0] + b * mn * PL;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int i = i0 + ty + 32 * k, j = j0 + t8;
+        float w[8];
+        f16x8 hi, lo;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            w[q] = (float)(v[k][q] * by);
+            hi[q] = (half_t)(w[q] * kUp);
+            lo[q] = (half_t)(w[q] * kUp - (float)hi[q]);
+        }
+        const size_t at = at_column<PL>(L.mp, i, j);
+        *reinterpret_cast<f16x8 *>(x + at) = hi;
+        *reinterpret_cast<f16x8 *>(PL == 2 ? x + at + 32 : L.rest + b * mn + at) = lo;
+        if constexpr (PL == 2) {
+            float *x32 = L.x32 + b * mn + at_x32(L.mp, i, j);
+            *reinterpret_cast<f32x4 *>(x32) = f32x4{w[0], w[1], w[2], w[3]};
+            *reinterpret_cast<f32x4 *>(x32 + 4) = f32x4{w[4], w[5], w[6], w[7]};
+        }
     }
 }
 
@@ -176,6 +245,24 @@ __device__ __forceinline__ int spread(int id, int count)
 {
     const int per = count >> 3, more = count & 7, xcd = id & 7, at = id >> 3;
     return xcd * per + (xcd < more ? xcd : more) + at;
+}
+
+// Eight consecutive elements of what the last product writes, the first n of them.
+template <typename T> __device__ __forceinline__ void write_some(const Target &out, size_t at, int n, const f32x4 (&w)[2])
+{
+    if (out.theta) {
+        float *to = out.theta + at;
+        float t[8];
+        load_some<float, 8>(to, n, t);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) t[q] = __builtin_fmaf(-out.rate, w[q / 4][q % 4], out.keep * t[q]);
+        store_some<float, 8>(to, n, t);
+    } else {
+        float t[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) t[q] = w[q / 4][q % 4];
+        store_some<T, 8>(static_cast<T *>(out.out) + at, n, t);
+    }
 }
 
 // A workgroup of eight waves (2 x 4): TILE x TILE of C = A B^T (kGram, kPoly) or A B (kApply, kLast).  A stage is 128 bytes of
@@ -290,7 +377,9 @@ __global__ __launch_bounds__(512) void muon_product_kernel(Layout L, int from, T
                     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(copies ? (STAGES - 2) * 2 * COPIES : 0) : "memory");
                     use = use + 1 == STAGES ? 0 : use + 1;
                 }
-                acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(g.a[p == 0][x], g.b[p == 1][y], acc[x][y], 0, 0, 0);
+                // (TR: the block's transpose, for four consecutive columns of X in a lane)
+                if constexpr (TR) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(g.b[p == 1][y], g.a[p == 0][x], acc[x][y], 0, 0, 0);
+                else acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(g.a[p == 0][x], g.b[p == 1][y], acc[x][y], 0, 0, 0);
                 if (i >= lead)
 #pragma unroll
                     for (int n = (i - lead) * tasks / (M - lead); n < (i - lead + 1) * tasks / (M - lead); ++n) {
@@ -317,8 +406,8 @@ __global__ __launch_bounds__(512) void muon_product_kernel(Layout L, int from, T
     stage(std::false_type{}, std::false_type{});
 
     // Value v of a block: row 8 (v / 4) + 4 (lane / 32) + v % 4, column lane % 32.
-    const int row0 = wi + 4 * (lane >> 5), col0 = wj + (lane & 31);
     if constexpr (!TR) {
+        const int row0 = wi + 4 * (lane >> 5), col0 = wj + (lane & 31);
         float *c = L.sums + (((size_t)b * (mt * (mt + 1) / 2) + ti * (ti + 1) / 2 + tj) * splits + split) * (TILE * TILE);
 #pragma unroll
         for (int x = 0; x < BX; ++x)
@@ -327,46 +416,101 @@ __global__ __launch_bounds__(512) void muon_product_kernel(Layout L, int from, T
 #pragma unroll
                 for (int v = 0; v < 16; ++v) c[(row0 + x * 32 + 8 * (v >> 2) + (v & 3)) * TILE + col0 + y * 32] = acc[x][y][v];
     } else {
-        const int i0 = ti * TILE + row0, j0 = tj * TILE + col0;
+        // A wave's 32 rows and all its columns go through LDS, in which it has a place of its own once no wave reads operands any more:
+        // then a lane has eight consecutive columns of X, 16 bytes of f16, and what it reads and writes are runs of 64 or 128 bytes.
+        constexpr int COLS = BY * 32, STRIDE = COLS * 4 + 16, LANES = COLS / 8, CHUNKS = COLS / 16;   // lanes of a row; a lane's chunks
+        char *turned = lds + wave * (32 * STRIDE);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");
+        auto wave_sync = [&]() __attribute__((always_inline)) {
+            __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+        };
+        const int row = lane / LANES, c8 = lane % LANES * 8, j = tj * TILE + wj + c8;
 #pragma unroll
         for (int x = 0; x < BX; ++x) {
-            float pd[16];
+            const int i = ti * TILE + wi + x * 32 + row;                 // and every (64 / LANES)-th further one
+            auto at = [&](int k) __attribute__((always_inline)) { return b * mn * PL + at_column<PL>(L.mp, i + k * (64 / LANES), j); };
+            float old[CHUNKS][8], pd[CHUNKS];
 #pragma unroll
-            for (int v = 0; v < 16; ++v) pd[v] = kA + L.pd[(size_t)b * L.mp + i0 + x * 32 + 8 * (v >> 2) + (v & 3)];
+            for (int k = 0; k < CHUNKS; ++k) {
+                pd[k] = kA + L.pd[(size_t)b * L.mp + i + k * (64 / LANES)];
+                if constexpr (PL == 2) {
+                    const float *from32 = L.x32 + b * mn + at_x32(L.mp, i + k * (64 / LANES), j);
+                    const f32x4 lo = *reinterpret_cast<const f32x4 *>(from32), hi = *reinterpret_cast<const f32x4 *>(from32 + 4);
 #pragma unroll
-            for (int y = 0; y < BY; ++y) {
-                const int j = j0 + y * 32;
-                float *x32 = L.x32 + b * mn + at_x32(L.mp, i0 + x * 32, j);
-                float w[16];
-#pragma unroll
-                for (int v = 0; v < 16; ++v) w[v] = __builtin_fmaf(pd[v], x32[(8 * (v >> 2) + (v & 3)) * 32], acc[x][y][v] * (kDown * kDown));
-                if constexpr (MODE == kApply) {
-#pragma unroll
-                    for (int v = 0; v < 16; ++v) x32[(8 * (v >> 2) + (v & 3)) * 32] = w[v];
-                    // a pair of rows and columns is shared out: even lanes take the first row's two columns, odd ones the second's
-                    const bool odd = lane & 1;
-#pragma unroll
-                    for (int v = 0; v < 16; v += 2) {
-                        const float mine = odd ? w[v + 1] : w[v], theirs = odd ? w[v] : w[v + 1];
-                        const float got = __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(theirs), 0xB1, 0xf, 0xf, true));   // quad_perm 1 0 3 2
-                        const float c0 = (odd ? got : mine) * kUp, c1 = (odd ? mine : got) * kUp;
-                        half_t *to = L.x[1 - from] + b * mn * PL + at_column<PL>(L.mp, i0 + x * 32 + 8 * (v >> 2) + (v & 3) + odd, j & ~1);
-                        typedef half_t f16x2 __attribute__((ext_vector_type(2)));
-                        const f16x2 h = {(half_t)c0, (half_t)c1};
-                        *reinterpret_cast<f16x2 *>(to) = h;
-                        if constexpr (PL == 2) *reinterpret_cast<f16x2 *>(to + 32) = f16x2{(half_t)(c0 - (float)h[0]), (half_t)(c1 - (float)h[1])};
-                    }
+                    for (int q = 0; q < 4; ++q) { old[k][q] = lo[q]; old[k][4 + q] = hi[q]; }
                 } else {
+                    const f16x8 h = *reinterpret_cast<const f16x8 *>(L.x[from] + at(k)), r = *reinterpret_cast<const f16x8 *>(L.rest + at(k));
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) {
-                        const int i = i0 + x * 32 + 8 * (v >> 2) + (v & 3);
-                        if (i >= L.m || j >= L.n) continue;
-                        const size_t o = (size_t)b * L.rows * L.cols + (L.tall ? (size_t)j * L.cols + i : (size_t)i * L.cols + j);
-                        if (out.theta) out.theta[o] = __builtin_fmaf(-out.rate, w[v], out.keep * out.theta[o]);
-                        else Elem<T>::store(static_cast<T *>(out.out) + o, w[v]);
-                    }
+                    for (int q = 0; q < 8; ++q) old[k][q] = ((float)h[q] + (float)r[q]) * kDown;
                 }
             }
+#pragma unroll
+            for (int y = 0; y < BY; ++y)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    *reinterpret_cast<f32x4 *>(turned + (lane & 31) * STRIDE + (y * 32 + 8 * q + 4 * (lane >> 5)) * 4) =
+                        f32x4{acc[x][y][4 * q], acc[x][y][4 * q + 1], acc[x][y][4 * q + 2], acc[x][y][4 * q + 3]};
+            wave_sync();
+#pragma unroll
+            for (int k = 0; k < CHUNKS; ++k) {
+                f32x4 *here = reinterpret_cast<f32x4 *>(turned + (row + k * (64 / LANES)) * STRIDE + c8 * 4);
+                f32x4 w[2] = {here[0], here[1]};
+#pragma unroll
+                for (int q = 0; q < 8; ++q) w[q / 4][q % 4] = __builtin_fmaf(pd[k], old[k][q], w[q / 4][q % 4] * (kDown * kDown));
+                if constexpr (MODE == kApply) {
+                    half_t *to = L.x[1 - from] + at(k);
+                    f16x8 h, r;
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        const float c = w[q / 4][q % 4] * kUp;
+                        h[q] = (half_t)c;
+                        r[q] = (half_t)(c - (float)h[q]);
+                    }
+                    *reinterpret_cast<f16x8 *>(to) = h;
+                    *reinterpret_cast<f16x8 *>(PL == 2 ? to + 32 : L.rest + at(k)) = r;
+                    if constexpr (PL == 2) {
+                        f32x4 *to32 = reinterpret_cast<f32x4 *>(L.x32 + b * mn + at_x32(L.mp, i + k * (64 / LANES), j));
+                        to32[0] = w[0];
+                        to32[1] = w[1];
+                    }
+                } else if (L.tall) {
+                    here[0] = w[0];
+                    here[1] = w[1];
+                } else if (i + k * (64 / LANES) < L.m) {
+                    write_some<T>(out, (size_t)b * L.rows * L.cols + (size_t)(i + k * (64 / LANES)) * L.cols + j, L.n - j, w);
+                }
+            }
+            wave_sync();
+            if constexpr (MODE == kLast)
+                if (L.tall) {                                            // along the rows of what is written: columns of X
+                    const int ic = ti * TILE + wi + x * 32 + (lane & 31), jc = tj * TILE + wj + (lane >> 5);
+#pragma unroll
+                    for (int h = 0; h < COLS / 2; h += 8) {
+                        float w[8];
+                        size_t o[8];
+                        bool there[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            w[k] = *reinterpret_cast<const float *>(turned + (lane & 31) * STRIDE + ((lane >> 5) + 2 * (h + k)) * 4);
+                            there[k] = ic < L.m && jc + 2 * (h + k) < L.n;
+                            o[k] = there[k] ? (size_t)b * L.rows * L.cols + (size_t)(jc + 2 * (h + k)) * L.cols + ic : 0;
+                        }
+                        if (out.theta) {
+                            float t[8];
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) t[k] = there[k] ? out.theta[o[k]] : 0.f;
+#pragma unroll
+                            for (int k = 0; k < 8; ++k)
+                                if (there[k]) out.theta[o[k]] = __builtin_fmaf(-out.rate, w[k], out.keep * t[k]);
+                        } else
+#pragma unroll
+                            for (int k = 0; k < 8; ++k)
+                                if (there[k]) Elem<T>::store(static_cast<T *>(out.out) + o[k], w[k]);
+                    }
+                    wave_sync();
+                }
         }
     }
 }
@@ -837,8 +981,7 @@ Wide wide_plan(int planes, int batch, int rows, int cols)
     w.each = w.cb * 8;
     while (few_lds(planes, w.each) > kLds) --w.each;
     w.wgs = (blocks + w.each - 1) / w.each;
-    const size_t each = ((size_t)rows * cols + 2047) / 2048;
-    w.parts = each < kParts ? (int)each : kParts;
+    w.parts = norm_parts((size_t)rows * cols, kNormLot<float>);
     w.part = round_up((size_t)batch * kParts * 8, 256);
     w.x32 = round_up((size_t)batch * w.wgs * w.cb * 8 * 2048 * 4, 256);
     w.share = round_up((size_t)batch * w.wgs * 16384, 256);
@@ -878,13 +1021,13 @@ Layout layout_of(int planes, int batch, int rows, int cols, char *ws, size_t &to
     const long tiles = (long)batch * (mt * (mt + 1) / 2);
     L.splits[kGram] = split_count(planes, L.tile, tiles, L.np * planes / 64);
     L.splits[kPoly] = split_count(planes, L.tile, tiles, L.mp * planes / 64);
-    const size_t each = ((size_t)L.rows * L.cols + 2047) / 2048;
-    L.parts = each < kParts ? (int)each : kParts;
+    L.parts = norm_parts((size_t)rows * cols, kNormLot<float>);
     size_t off = 0;
     auto take = [&](size_t bytes) { char *p = ws + off; off += round_up(bytes, 256); return p; };
     const size_t mn = (size_t)batch * L.mp * L.np, mm = (size_t)batch * L.mp * L.mp;
     L.part = reinterpret_cast<double *>(take((size_t)batch * kParts * 8));
-    L.x32 = reinterpret_cast<float *>(take(mn * 4));
+    L.x32 = planes == 2 ? reinterpret_cast<float *>(take(mn * 4)) : nullptr;
+    L.rest = planes == 1 ? reinterpret_cast<half_t *>(take(mn * 2)) : nullptr;
     for (int k = 0; k < 2; ++k) L.x[k] = reinterpret_cast<half_t *>(take(mn * 2 * planes));
     L.g = reinterpret_cast<half_t *>(take(mm * 2 * planes));
     L.p = reinterpret_cast<half_t *>(take(mm * 2 * planes));

@@ -339,8 +339,16 @@ __global__ __launch_bounds__(256) void log_probs_kernel(const T *__restrict__ z,
         add_scores<U * V>(mine, x, lot);
         if constexpr (TOP)
             if (__any(lot >= b.worst_v && lot > -INFINITY)) {
+                // (a loop over the most that a lane has, its scores read again: 16 offers in a row are more instructions than a
+                // short row waits for)
+                unsigned some = 0;
 #pragma unroll
-                for (int j = 0; j < U * V; ++j) offer(b, x[j], v0 + (i0 + j / V * tn) * V + j % V, lane);
+                for (int j = 0; j < U * V; ++j) some |= (x[j] >= b.worst_v && x[j] > -INFINITY ? 1u : 0u) << j;
+                while (__any(some)) {
+                    const int j = some ? __builtin_ctz(some) : 0, k = v0 + (i0 + j / V * tn) * V + j % V;
+                    offer(b, some ? Elem<T>::load(zr + k) : -INFINITY, k, lane);
+                    some &= some - 1;
+                }
                 if (b.count > b.top + 24 && i0 - ti + U * tn < nvec) cut(b, lane);   // (what follows meets a higher bar)
             }
     }
