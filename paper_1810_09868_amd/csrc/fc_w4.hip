@@ -33,7 +33,7 @@ __device__ __forceinline__ u32x4 loose16(const void *p)
 }
 
 // A lane takes eight inputs: two loads of 16 bytes, one store of its eight codes.  2^shift / 8 lanes share a group, all in one wave.
-// `units`: lanes of a row, whole groups.
+// `units`: lanes of a row, whole groups.  Bound by its 411 MB of reads at 25088 x 4096: 100 us, and 95 us the way back.
 __global__ __launch_bounds__(256) void w4_quantize_kernel(const float *__restrict__ w, uint8_t *__restrict__ codes, bf16_t *__restrict__ scales,
                                                           int In, int blocks, int groups, int shift, unsigned units, unsigned all)
 {
@@ -159,7 +159,8 @@ __device__ __forceinline__ float sum_lanes4(const float (&v)[4])
 
 // One row of a.  A lane keeps 32 consecutive inputs in registers and meets them with the codes of four outputs at a time (one or
 // 64 / 2^logl of them a load, 16 bytes a lane), while the next four's are on their way; the waves of a workgroup take the row's
-// further slices, and LDS adds up what they find.  Every code is read once, in runs of up to 1 KB.
+// further slices, and LDS adds up what they find.  Every code is read once, in runs of up to 1 KB.  Bound by that read: 25088 x 4096 in bf16
+// takes 12.8 us, a mere read of the same 53 MB 9.1 us.  (On the matrix unit with 15 of 16 rows empty: 23.3 us.)
 constexpr int kBatch = 4, kRowWaves = 16;
 template <typename T>
 __global__ __launch_bounds__(kRowWaves * 64) void fc_w4_row_kernel(const T *__restrict__ a_rows, W4Args p, int logl, int batches)
@@ -346,7 +347,8 @@ __device__ __forceinline__ f32x4 mfma(const u32x4 &x, const u32x4 &w, f32x4 acc)
 }
 
 // Up to 16 rows: 16 outputs to a workgroup, whose W waves take every W-th 128 inputs, the next ones' codes, scales and activations
-// on their way, and add up in LDS.
+// on their way, and add up in LDS.  Each workgroup reads (and in fp32 splits) all activations, so that it is bound by their way out of
+// L2 and, in fp32, by some 200 vector instructions for every 128 inputs (16 x 4096 x 4096, bf16: 7.5 us; 10 x 4096 x 1000, fp32: 9.8 us).
 template <typename T, int W, int G>
 __global__ __launch_bounds__(W * 64) void fc_w4_tile_kernel(const T *__restrict__ a, W4Args p)
 {
@@ -465,7 +467,9 @@ __global__ __launch_bounds__(256) void fc_w4_lay_kernel(const T *__restrict__ a,
 }
 
 // 16 RT outputs and 16 NT rows to a workgroup, whose eight waves take every eighth 128 inputs of its share and add up in LDS.
-// The next 128 inputs' codes and scales and the next few blocks of activations are on their way.
+// The next 128 inputs' codes and scales and the next few blocks of activations are on their way.  A code is spread once for NT
+// products, an activation read once for RT; the products fill a tenth of the time, the rest is the activations' way out of L2 and
+// the beginning and end of three launches (100 x 25088 x 4096, bf16: 43.7 us, 470 TFLOP/s; 100 x 4096 x 4096: 14.6 us).
 template <int P, int RT, int NT, int G>
 __global__ __launch_bounds__(512) void fc_w4_tiles_kernel(const u32x4 *__restrict__ x, W4Args p)
 {
@@ -612,22 +616,30 @@ constexpr size_t kTileBytes = 300000;
 
 bool one_tile(int dtype, int N, int In) { return N <= kTileRows && (size_t)N * In * dtype_size(dtype) <= kTileBytes; }
 
-struct W4Plan { int nt, tiles, splits, row_tiles; size_t lay_bytes; };
+// Tiles of 64 outputs read the laid out activations least often, those of 16 begin and end soonest and need the fewest splits.  16
+// where all workgroups run at once, 32 else, as long as the activations' way out of L2 is no more than this many bytes in all (32
+// x 4096 x 4096, bf16: 8.3, 10.8, 12.1 us with 16, 32, 64; 100 x 4096 x 4096: 18.4, 14.6, 18.3; 64 x 25088 x 4096: 41.7, 32.7, 29.5).
+constexpr size_t kReadAgain = 160u << 20;
+
+struct W4Plan { int nt, rt, tiles, splits, row_tiles; size_t lay_bytes; };
 W4Plan tiles_plan(int dtype, int N, int In, int Out)
 {
     W4Plan t;
     t.nt = N <= 16 ? 1 : N <= 32 ? 2 : 4;
     t.tiles = (N + 16 * t.nt - 1) / (16 * t.nt) * t.nt;
-    t.row_tiles = (Out + 63) / 64;
     const int kb = (In + 127) / 128, most = (kb + 7) / 8;
+    t.lay_bytes = round_up((size_t)kb * t.tiles * 4 * (dtype == VGG_BF16 ? 1 : 3) * 1024, 256);
+    auto row_tiles = [&](int rt) { return (Out + 16 * rt - 1) / (16 * rt); };
+    auto few = [&](int rt) { return t.lay_bytes * row_tiles(rt) <= kReadAgain; };
+    t.rt = few(1) && (long)row_tiles(1) * (t.tiles / t.nt) <= 256 ? 1 : few(2) ? 2 : 4;
+    t.row_tiles = row_tiles(t.rt);
     const long units = (long)t.row_tiles * (t.tiles / t.nt);
     t.splits = (int)(units >= 256 ? 1 : (256 + units - 1) / units);
     if (t.splits > most) t.splits = most;
-    t.lay_bytes = round_up((size_t)kb * t.tiles * 4 * (dtype == VGG_BF16 ? 1 : 3) * 1024, 256);
     return t;
 }
 
-template <typename T, int NT, int G>
+template <typename T, int RT, int NT, int G>
 int launch_tiles_of(const T *a, W4Args p, const W4Plan &t, void *ws, hipStream_t s)
 {
     constexpr int P = sizeof(T) == 2 ? 1 : 3;
@@ -637,16 +649,23 @@ int launch_tiles_of(const T *a, W4Args p, const W4Plan &t, void *ws, hipStream_t
     p.row_tiles = t.row_tiles;
     const unsigned units = (unsigned)((p.In + 127) / 128) * t.tiles * 4;
     hipLaunchKernelGGL(fc_w4_lay_kernel<T>, dim3((units + 3) / 4), dim3(256), 0, s, a, x, p.N, p.In, t.tiles, units);
-    hipLaunchKernelGGL((fc_w4_tiles_kernel<P, 4, NT, G>), dim3((unsigned)(t.row_tiles * t.splits), (unsigned)(t.tiles / NT)), dim3(512), (size_t)8 * NT * 1024, s, x, p);
+    hipLaunchKernelGGL((fc_w4_tiles_kernel<P, RT, NT, G>), dim3((unsigned)(t.row_tiles * t.splits), (unsigned)(t.tiles / NT)), dim3(512), (size_t)8 * NT * 1024, s, x, p);
     if (t.splits > 1) hipLaunchKernelGGL(fc_w4_join_kernel, dim3((unsigned)(((size_t)p.N * p.Out + 255) / 256)), dim3(256), 0, s, p);
     return launch_status();
+}
+template <typename T, int RT, int NT>
+int launch_tiles_by(const T *a, const W4Args &p, const W4Plan &t, void *ws, hipStream_t s)
+{
+    if (p.shift == 5) return launch_tiles_of<T, RT, NT, 1>(a, p, t, ws, s);
+    if (p.shift == 6) return launch_tiles_of<T, RT, NT, 2>(a, p, t, ws, s);
+    return launch_tiles_of<T, RT, NT, 4>(a, p, t, ws, s);
 }
 template <typename T, int NT>
 int launch_tiles(const T *a, const W4Args &p, const W4Plan &t, void *ws, hipStream_t s)
 {
-    if (p.shift == 5) return launch_tiles_of<T, NT, 1>(a, p, t, ws, s);
-    if (p.shift == 6) return launch_tiles_of<T, NT, 2>(a, p, t, ws, s);
-    return launch_tiles_of<T, NT, 4>(a, p, t, ws, s);
+    if (t.rt == 1) return launch_tiles_by<T, 1, NT>(a, p, t, ws, s);
+    if (t.rt == 2) return launch_tiles_by<T, 2, NT>(a, p, t, ws, s);
+    return launch_tiles_by<T, 4, NT>(a, p, t, ws, s);
 }
 template <typename T, int G>
 int launch_tile(const T *a, const W4Args &p, hipStream_t s)
