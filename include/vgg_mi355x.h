@@ -371,9 +371,9 @@ int vgg_fc_w4(int dtype, int N, int In, int Out, int group, const void *a, const
  * (with X^T in X's place where rows > cols: the same values), which takes the
  * singular values towards 1.  VGG_F32: products as exact as fp32 ones (two
  * f16 parts per value, fp32 sums).  VGG_BF16: x and y are bf16, operands of a
- * product hold 11 bits, sums and the iterate are fp32.  y may be x.  A matrix
- * with a NaN or an infinity comes out NaN.  min(rows, cols) <= 32768, both
- * <= 2^22, batch <= 65535. */
+ * product hold 11 bits, the iterate 22 or more, sums are fp32.  y may be x.  A
+ * matrix with a NaN or an infinity comes out NaN.  min(rows, cols) <= 32768,
+ * both <= 2^22, batch <= 65535. */
 size_t vgg_orthogonalize_workspace_bytes(int dtype, int batch, int rows, int cols);
 int vgg_orthogonalize(int dtype, int batch, int rows, int cols, int steps, const void *x, void *y, void *ws,
                       size_t ws_bytes, void *stream);

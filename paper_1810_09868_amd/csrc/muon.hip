@@ -8,8 +8,9 @@
 // that they are held times 2^14, below f16's largest, and need no other scale; f16 then keeps 11 bits of everything down to
 // 2^-28.  PLANES = 2 (VGG_F32): a value is two f16 numbers, the nearest and what that leaves, 22 bits; hi hi + hi lo + lo hi
 // leaves out 2^-22 of a product at most.  PLANES = 1 (VGG_BF16): operands are rounded to 11 bits.  The term a X takes all of X, an
-// fp32 copy or (PLANES = 1) the operand and what it leaves, another f16 number, 22 bits in all: a rounding of X to 11 bits there would
-// grow 3.4-fold in every later step where X has no (or small) singular values.  In both the diagonals of G and P, which hold most of them, are kept apart in fp32 (zeros in the planes): with G = D + E,
+// fp32 copy or (PLANES = 1, whose results have 8 bits) the operand and what it leaves as another f16 number, 22 bits in two thirds of the
+// bytes: a rounding of X to 11 bits there would grow 3.4-fold in every later step where X has no (or small) singular values.  In
+// both the diagonals of G and P, which hold most of them, are kept apart in fp32 (zeros in the planes): with G = D + E,
 //     (G G)_ij = (E E)_ij + (d_i + d_j) e_ij,   (G G)_ii = (E E)_ii + d_i^2,   (P X)_i = p_i X_i + (the rest of P) X.
 // One plane is then 3e-4 to 1e-3 off in all, against 1.3e-3 to 2.4e-3 with the diagonals rounded (bf16's own rounding: 1.7e-3).
 //
@@ -19,7 +20,7 @@
 // G and G G contract along rows of both operands; P X takes X's columns, which LDS hands out transposed (ds_read_b64_tr_b16), so
 // that X is kept once.  X is padded with zeros to whole tiles.  G and P are symmetric: the tiles on and below the diagonal are
 // formed, over a few ranges of the contraction where they are too few to fill the chip, and a second kernel adds the ranges in
-// order and mirrors them.
+// order and mirrors them (in the product kernel's own end, where there is one range: no faster).
 #include "common.h"
 
 #include <type_traits>
@@ -46,7 +47,8 @@ template <int PL> __device__ __forceinline__ size_t at_column(int rows, int i, i
 __device__ __forceinline__ size_t at_x32(int rows, int i, int j) { return ((size_t)(j >> 5) * rows + i) * 32 + (j & 31); }
 
 // ----------------------------------------------------------------------------------- momentum and the norm
-// Squares are summed in 64 bits: they neither overflow nor vanish.
+// Squares are summed in 64 bits: they neither overflow nor vanish.  Bound by the read (7 x 512 x 4608, bf16: 10 us for 33 MB; with a
+// step of the momentum, 4096 x 25088: 208 us for 1.2 GB, 5.9 TB/s).
 __device__ __forceinline__ double block_sum(double v)
 {
     __shared__ double red[4];
@@ -165,6 +167,7 @@ struct Layout {
 };
 
 // X_0 in all its forms, zeros where they are padded.  A workgroup: 64 x 64 of the padded X, eight consecutive elements to a thread.
+// Bound by what it writes (7 x 512 x 4608, bf16: 19 us for 99 MB, read and written).
 template <typename T, int PL>
 __global__ __launch_bounds__(256) void muon_start_kernel(Source s, Layout L)
 {
@@ -269,7 +272,11 @@ template <typename T> __device__ __forceinline__ void write_some(const Target &o
 // every row of A (64 contraction indices, or 32 in two planes), and as many rows or bytes of B; STAGES of them in LDS, all but one
 // on their way (128 KB, one workgroup to a compute unit).  A 16-byte segment s of a row r of A lies at s ^ (r / 2 % 8), so that
 // sixteen rows of one segment are in different banks; the two 64-byte blocks of a row r of
-// B that is read transposed change places where r / 2 is odd, for the four rows that sixteen lanes read.  256 x 256 tiles take 2/3 of the LDS traffic of 128 x 128 ones, and four times the work.
+// B that is read transposed change places where r / 2 is odd, for the four rows that sixteen lanes read.  256 x 256 tiles take 2/3 of the
+// LDS traffic of 128 x 128 ones, and four times the work.  Large products are bound by the matrix unit and its power (4096 x 25088, two
+// planes: G in 1.02 ms, 1.33 PFLOP/s of f16 products, pipes busy 0.73; P X in 2.1 ms, 1.2 PFLOP/s); 128 x 128 tiles of short
+// contractions by X's way through memory (7 x 512 x 4608, one plane: P X in 37 us for 165 MB) and, one to a compute unit, by their
+// beginnings and ends (two to one, with half the stages: 4 % faster there, 3 % slower where one round of the chip is enough).
 template <typename T, int PL, int MODE, int TILE>
 __global__ __launch_bounds__(512) void muon_product_kernel(Layout L, int from, Target out)
 {
@@ -515,7 +522,8 @@ __global__ __launch_bounds__(512) void muon_product_kernel(Layout L, int from, T
     }
 }
 
-// The ranges' sums to G, or to P = b G + c G G: 32 x 32 of a tile to a workgroup, and its mirror image.
+// The ranges' sums to G, or to P = b G + c G G: 32 x 32 of a tile to a workgroup, and its mirror image.  5 us for m up to 1000, most of it
+// the launch; 32 to 43 us at m = 4096.
 template <int PL, int MODE, int TILE>
 __global__ __launch_bounds__(256) void muon_symmetric_kernel(Layout L)
 {
@@ -826,7 +834,8 @@ struct FewRows {
 };
 
 // All columns in one workgroup: everything of a matrix in one launch, and nothing but its input and output passes memory.  Three
-// barriers a step.
+// barriers a step, which with the chains of LDS reads and products between them are all of its time (64 x 27, bf16: 16 us; 64 x 512:
+// 34 us; 64 matrices of 64 x 27 at once: 16.6 us).
 template <typename T, int PL, int CB>
 __global__ __launch_bounds__(512) void muon_small_kernel(Source src, Target out, int rows, int cols, int steps)
 {
@@ -886,9 +895,10 @@ __global__ __launch_bounds__(512) void muon_small_kernel(Source src, Target out,
     w.write(out, base);
 }
 
-// More columns: `each` blocks of 32 to a workgroup (up to 8 CB), and a launch a step.  Every workgroup adds up all workgroups' shares of G itself, in
-// order, and forms P; what it writes for the next launch is its columns of X, as its registers hold them, and its share of their G.
-// step 0: X_0 from the input; step `steps`: the output.
+// More columns: `each` blocks of 32 to a workgroup (up to 8 CB), and a launch a step.  Every workgroup adds up all workgroups' shares
+// of G itself, in order, and forms P; what it writes for the next launch is its columns of X, as its registers hold them, and its share of their G.
+// Bound by six launches of some 5 us each until the columns are many (64 x 576, bf16: 42 us; 2 x 28 x 7933: 74 us, 138 us by
+// tiles of products; 64 x 25088: 110 us).  step 0: X_0 from the input; step `steps`: the output.
 template <typename T, int PL, int CB>
 __global__ __launch_bounds__(512) void muon_wide_kernel(Source src, Target out, int rows, int cols, int each, int step, int steps, const double *part,
                                                         int parts, float *x32, const f32x4 *shares, f32x4 *share)
@@ -963,7 +973,7 @@ __global__ __launch_bounds__(512) void muon_wide_kernel(Source src, Target out, 
 }
 
 // Column blocks of a wave in one workgroup, 0 where a matrix is too large: its planes' room in LDS, and at most two blocks of X
-// (three spill registers and gain nothing: 64 x 576 takes 42 us with them, 43 us in three workgroups and seven launches).
+// (three spill registers and gain nothing: 64 x 576 takes 42 us either way).
 int small_blocks(int planes, int rows, int cols)
 {
     const int m = rows < cols ? rows : cols, n = rows < cols ? cols : rows, blocks = (n + 31) / 32, cb = (blocks + 7) / 8;
