@@ -230,6 +230,7 @@ __global__ __launch_bounds__(256) void muon_start_kernel(Source s, Layout L)
 // -------------------------------------------------------------------------------------------------- products
 enum { kGram, kPoly, kApply, kLast };
 
+
 // What the last product writes: X itself, or the step that it makes.
 struct Target {
     void *out;             // [batch][rows][cols], or null:
@@ -600,13 +601,13 @@ inline size_t few_lds(int planes, int blocks) { return (size_t)(blocks * 32 + 2 
 template <typename T, int PL, int CB>
 struct FewRows {
     typedef half_t f16x4 __attribute__((ext_vector_type(4)));
-    static constexpr int S = row_stride(PL);
+    static constexpr int S = row_stride(PL), W = 8, Q = 16 / W;   // waves; blocks of G of a wave
     int m, n, blocks, first, lane, wave, half, col, i_step, j_step;   // blocks of 32 columns: this workgroup's, from `first` on
     char *X, *G, *P;
     float *gd, *pd;
     double *red;
-    float x[CB][2][16];    // (r, v) of column block c: row 32 r + 8 (v / 4) + 4 half + v % 4, column 32 (wave + 8 c) + col
-    f32x4 acc[2];          // G or G G: value v is (16 bi + 4 quarter + v, 16 (bj + q) + r16)
+    float x[CB][2][16];    // (r, v) of column block c: row 32 r + 8 (v / 4) + 4 half + v % 4, column 32 (wave + W c) + col
+    f32x4 acc[Q];          // G or G G: value v is (16 bi + 4 quarter + v, 16 (bj + q) + r16)
 
     __device__ __forceinline__ FewRows(char *lds, int rows, int cols, int first_block, int most_blocks)
     {
@@ -630,11 +631,18 @@ struct FewRows {
         red = reinterpret_cast<double *>(pd + 64);
     }
     // The place of element (c, r, v) in a matrix as the caller keeps it; that of an element that is there, where this one is not.
-    __device__ __forceinline__ size_t place(int c, int r, int v, bool &there) const
+    __device__ __forceinline__ unsigned place(int c, int r, int v, bool &there) const
     {
-        const int i = r * 32 + 8 * (v >> 2) + 4 * half + (v & 3), j = (first + wave + 8 * c) * 32 + col;
-        there = i < m && j < n && wave + 8 * c < blocks;
-        return there ? (size_t)i * i_step + (size_t)j * j_step : 0;
+        const int i = r * 32 + 8 * (v >> 2) + 4 * half + (v & 3), j = (first + wave + W * c) * 32 + col;
+        there = i < m && j < n && wave + W * c < blocks;
+        return there ? (unsigned)i * i_step + (unsigned)j * j_step : 0u;   // (at most 2^28)
+    }
+    // Places are found again where they are used next: they would fill the registers in between.
+    __device__ __forceinline__ void forget_places() { asm volatile("" : "+v"(col), "+v"(half)); }
+    // (32-bit offsets from addresses that the workgroup shares)
+    template <typename U> static __device__ __forceinline__ U &element(U *p, unsigned at)
+    {
+        return *reinterpret_cast<U *>(reinterpret_cast<uintptr_t>(p) + at * (unsigned)sizeof(U));
     }
     // Four consecutive elements k.. of a row, scaled, into its planes; and back.
     static __device__ __forceinline__ void put4(char *row, int k, const f32x4 &v)
@@ -660,13 +668,13 @@ struct FewRows {
     {
 #pragma unroll
         for (int c = 0; c < CB; ++c)
-            if (wave + 8 * c < blocks)
+            if (wave + W * c < blocks)
 #pragma unroll
                 for (int r = 0; r < 2; ++r)
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
                         const f32x4 v = {x[c][r][4 * q], x[c][r][4 * q + 1], x[c][r][4 * q + 2], x[c][r][4 * q + 3]};
-                        put4(X + ((wave + 8 * c) * 32 + col) * S, r * 32 + 8 * q + 4 * half, v * kUp);
+                        put4(X + ((wave + W * c) * 32 + col) * S, r * 32 + 8 * q + 4 * half, v * kUp);
                     }
     }
     static __device__ __forceinline__ f32x4 mfma16(const f16x8 (&fa)[PL], const f16x8 (&fb)[PL], f32x4 acc)
@@ -677,11 +685,16 @@ struct FewRows {
         }
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(fa[0], fb[0], acc, 0, 0, 0);
     }
-    struct Rows { f16x8 a[PL], b[2][PL]; };
-    // acc <- X X^T of the workgroup's columns, this wave's two blocks
+    struct Rows { f16x8 a[PL], b[Q][PL]; };
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int q = 0; q < Q; ++q) acc[q] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // acc <- X X^T of the workgroup's columns, this wave's blocks
     __device__ __forceinline__ void gram()
     {
-        const int bi = wave >> 1, bj = (wave & 1) * 2, r16 = lane & 15, quarter = lane >> 4;
+        const int bi = wave / (W / 4), bj = wave % (W / 4) * Q, r16 = lane & 15, quarter = lane >> 4;
         auto columns = [&](int jb, Rows &f) __attribute__((always_inline)) {        // 32 columns of X's rows
             auto rows_of = [&](int b, f16x8 (&f)[PL]) __attribute__((always_inline)) {
 #pragma unroll
@@ -695,28 +708,28 @@ struct FewRows {
                 }
             };
             rows_of(bi, f.a);
-            rows_of(bj, f.b[0]);
-            rows_of(bj + 1, f.b[1]);
+#pragma unroll
+            for (int q = 0; q < Q; ++q) rows_of(bj + q, f.b[q]);
         };
-        acc[0] = acc[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        clear();
         Rows f0, f1;                               // one being multiplied, one on its way
         columns(0, f0);
         for (int jb = 0; jb < blocks; jb += 2) {
             if (jb + 1 < blocks) columns(jb + 1, f1);
 #pragma unroll
-            for (int q = 0; q < 2; ++q) acc[q] = mfma16(f0.a, f0.b[q], acc[q]);
+            for (int q = 0; q < Q; ++q) acc[q] = mfma16(f0.a, f0.b[q], acc[q]);
             if (jb + 1 == blocks) break;
             if (jb + 2 < blocks) columns(jb + 2, f0);
 #pragma unroll
-            for (int q = 0; q < 2; ++q) acc[q] = mfma16(f1.a, f1.b[q], acc[q]);
+            for (int q = 0; q < Q; ++q) acc[q] = mfma16(f1.a, f1.b[q], acc[q]);
         }
     }
     // G = acc, then P = b G + c G G, both to LDS (barriers between and after)
     __device__ __forceinline__ void polynomial()
     {
-        const int bi = wave >> 1, bj = (wave & 1) * 2, r16 = lane & 15, quarter = lane >> 4, i = bi * 16 + 4 * quarter;
+        const int bi = wave / (W / 4), bj = wave % (W / 4) * Q, r16 = lane & 15, quarter = lane >> 4, i = bi * 16 + 4 * quarter;
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
+        for (int q = 0; q < Q; ++q) {
             const int j = (bj + q) * 16 + r16;
             f32x4 v = acc[q] * kDown;
 #pragma unroll
@@ -728,7 +741,7 @@ struct FewRows {
             put4(G + j * S, i, v);
         }
         __syncthreads();
-        acc[0] = acc[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        clear();
 #pragma unroll
         for (int jb = 0; jb < 2; ++jb) {
             auto rows_of = [&](int b, f16x8 (&f)[PL]) __attribute__((always_inline)) {
@@ -737,14 +750,14 @@ struct FewRows {
             };
             Rows f;
             rows_of(bi, f.a);
-            rows_of(bj, f.b[0]);
-            rows_of(bj + 1, f.b[1]);
 #pragma unroll
-            for (int q = 0; q < 2; ++q) acc[q] = mfma16(f.a, f.b[q], acc[q]);
+            for (int q = 0; q < Q; ++q) rows_of(bj + q, f.b[q]);
+#pragma unroll
+            for (int q = 0; q < Q; ++q) acc[q] = mfma16(f.a, f.b[q], acc[q]);
         }
         const f32x4 di = *reinterpret_cast<const f32x4 *>(gd + i);
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
+        for (int q = 0; q < Q; ++q) {
             const int j = (bj + q) * 16 + r16;
             const float dj = gd[j];
             const f32x4 e = get4(G + j * S, i);
@@ -764,39 +777,35 @@ struct FewRows {
     // X <- a X + P X
     __device__ __forceinline__ void apply()
     {
-        f32x4 pdv[2][4];
-#pragma unroll
-        for (int r = 0; r < 2; ++r)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) pdv[r][q] = *reinterpret_cast<const f32x4 *>(pd + r * 32 + 8 * q + 4 * half);
 #pragma unroll
         for (int c = 0; c < CB; ++c) {
-            const int jb = wave + 8 * c;
+            const int jb = wave + W * c;
             if (jb >= blocks) continue;
-            f32x16 sum[2] = {};
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int at = (k >> 1) * 64 * PL + (k & 1) * 32 + half * 16;
-                f16x8 fb[PL], fa[2][PL];
+            for (int r = 0; r < 2; ++r) {
+                f32x16 sum = {};
 #pragma unroll
-                for (int p = 0; p < PL; ++p) {
-                    fb[p] = *reinterpret_cast<const f16x8 *>(X + (jb * 32 + col) * S + at + p * 64);
+                for (int k = 0; k < 4; ++k) {
+                    const int at = (k >> 1) * 64 * PL + (k & 1) * 32 + half * 16;
+                    f16x8 fb[PL], fa[PL];
 #pragma unroll
-                    for (int r = 0; r < 2; ++r) fa[r][p] = *reinterpret_cast<const f16x8 *>(P + (r * 32 + col) * S + at + p * 64);
+                    for (int p = 0; p < PL; ++p) {
+                        fb[p] = *reinterpret_cast<const f16x8 *>(X + (jb * 32 + col) * S + at + p * 64);
+                        fa[p] = *reinterpret_cast<const f16x8 *>(P + (r * 32 + col) * S + at + p * 64);
+                    }
+                    if constexpr (PL == 2) {
+                        sum = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[1], fb[0], sum, 0, 0, 0);
+                        sum = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[0], fb[1], sum, 0, 0, 0);
+                    }
+                    sum = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[0], fb[0], sum, 0, 0, 0);
                 }
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    if constexpr (PL == 2) {
-                        sum[r] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[r][1], fb[0], sum[r], 0, 0, 0);
-                        sum[r] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[r][0], fb[1], sum[r], 0, 0, 0);
-                    }
-                    sum[r] = __builtin_amdgcn_mfma_f32_32x32x16_f16(fa[r][0], fb[0], sum[r], 0, 0, 0);
+                for (int q = 0; q < 4; ++q) {
+                    const f32x4 pdv = *reinterpret_cast<const f32x4 *>(pd + r * 32 + 8 * q + 4 * half);
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) x[c][r][4 * q + v] = __builtin_fmaf(kA + pdv[v], x[c][r][4 * q + v], sum[4 * q + v] * (kDown * kDown));
                 }
             }
-#pragma unroll
-            for (int r = 0; r < 2; ++r)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) x[c][r][v] = __builtin_fmaf(kA + pdv[r][v >> 2][v & 3], x[c][r][v], sum[r][v] * (kDown * kDown));
         }
     }
     __device__ __forceinline__ void scale(double by)
@@ -806,36 +815,41 @@ struct FewRows {
 #pragma unroll
             for (int r = 0; r < 2; ++r)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) x[c][r][v] = (float)(x[c][r][v] * by);
+                for (int v = 0; v < 16; ++v) {
+                    x[c][r][v] = (float)(x[c][r][v] * by);
+                }
     }
-    __device__ __forceinline__ void write(const Target &out, size_t base) const
+    __device__ __forceinline__ void write(const Target &out, size_t base)
     {
+        float *theta = out.theta + base;
+        T *y = static_cast<T *>(out.out) + base;
 #pragma unroll
         for (int c = 0; c < CB; ++c)
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
                 bool there[16];
-                size_t at[16];
+                unsigned at[16];
 #pragma unroll
-                for (int v = 0; v < 16; ++v) at[v] = base + place(c, r, v, there[v]);
+                for (int v = 0; v < 16; ++v) at[v] = place(c, r, v, there[v]);
                 if (out.theta) {
                     float t[16];
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) t[v] = out.theta[at[v]];
+                    for (int v = 0; v < 16; ++v) t[v] = element(theta, at[v]);
 #pragma unroll
                     for (int v = 0; v < 16; ++v)
-                        if (there[v]) out.theta[at[v]] = __builtin_fmaf(-out.rate, x[c][r][v], out.keep * t[v]);
+                        if (there[v]) element(theta, at[v]) = __builtin_fmaf(-out.rate, x[c][r][v], out.keep * t[v]);
                 } else
 #pragma unroll
                     for (int v = 0; v < 16; ++v)
-                        if (there[v]) Elem<T>::store(static_cast<T *>(out.out) + at[v], x[c][r][v]);
+                        if (there[v]) Elem<T>::store(&element(y, at[v]), x[c][r][v]);
             }
     }
 };
 
 // All columns in one workgroup: everything of a matrix in one launch, and nothing but its input and output passes memory.  Three
-// barriers a step, which with the chains of LDS reads and products between them are all of its time (64 x 27, bf16: 16 us; 64 x 512:
-// 34 us; 64 matrices of 64 x 27 at once: 16.6 us).
+// barriers a step, which with the chains of LDS reads and products between them are all of its time (64 x 27, bf16: 15 us; 64 x 512:
+// 32 us; 64 matrices of 64 x 27 at once: 16 us).  Sixteen waves: 4 % faster for 64 x 512, 8 % slower for 64 x 256, and registers for one
+// block a wave only.
 template <typename T, int PL, int CB>
 __global__ __launch_bounds__(512) void muon_small_kernel(Source src, Target out, int rows, int cols, int steps)
 {
@@ -843,31 +857,27 @@ __global__ __launch_bounds__(512) void muon_small_kernel(Source src, Target out,
     FewRows<T, PL, CB> w(lds, rows, cols, 0, CB * 8);
     const size_t base = (size_t)blockIdx.x * rows * cols;
     const T *in = static_cast<const T *>(src.x) + base;
+    float *momentum = src.momentum + base;
     double sum = 0;
 #pragma unroll
     for (int c = 0; c < CB; ++c)
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            bool there;
-#pragma unroll
-            for (int v = 0; v < 16; ++v) w.x[c][r][v] = Elem<T>::load(in + w.place(c, r, v, there));
-        }
-#pragma unroll
-    for (int c = 0; c < CB; ++c)
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
             bool there[16];
-            size_t at[16];
+            unsigned at[16];
 #pragma unroll
-            for (int v = 0; v < 16; ++v) at[v] = base + w.place(c, r, v, there[v]);
+            for (int v = 0; v < 16; ++v) {
+                at[v] = w.place(c, r, v, there[v]);
+                w.x[c][r][v] = Elem<T>::load(&w.element(in, at[v]));
+            }
             if (src.momentum) {
                 float mom[16];
 #pragma unroll
-                for (int v = 0; v < 16; ++v) mom[v] = src.momentum[at[v]];
+                for (int v = 0; v < 16; ++v) mom[v] = w.element(momentum, at[v]);
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
                     mom[v] = __builtin_fmaf(src.mu, mom[v], w.x[c][r][v]);
-                    if (there[v]) src.momentum[at[v]] = mom[v];
+                    if (there[v]) w.element(momentum, at[v]) = mom[v];
                     w.x[c][r][v] = src.nesterov ? __builtin_fmaf(src.mu, mom[v], w.x[c][r][v]) : mom[v];
                 }
             }
@@ -885,6 +895,7 @@ __global__ __launch_bounds__(512) void muon_small_kernel(Source src, Target out,
 #pragma unroll
     for (int k = 0; k < 8; ++k) sum += w.red[k];
     w.scale(scale_of(sum));
+    w.forget_places();
     for (int step = 0; step < steps; ++step) {
         w.put_x();                                 // (a wave's own columns, which no other reads before the barrier)
         __syncthreads();
@@ -892,12 +903,13 @@ __global__ __launch_bounds__(512) void muon_small_kernel(Source src, Target out,
         w.polynomial();
         w.apply();
     }
+    w.forget_places();
     w.write(out, base);
 }
 
 // More columns: `each` blocks of 32 to a workgroup (up to 8 CB), and a launch a step.  Every workgroup adds up all workgroups' shares
 // of G itself, in order, and forms P; what it writes for the next launch is its columns of X, as its registers hold them, and its share of their G.
-// Bound by six launches of some 5 us each until the columns are many (64 x 576, bf16: 42 us; 2 x 28 x 7933: 74 us, 138 us by
+// Bound by six launches of some 5 us each until the columns are many (64 x 768, bf16: 42 us; 2 x 28 x 7933: 74 us, 138 us by
 // tiles of products; 64 x 25088: 110 us).  step 0: X_0 from the input; step `steps`: the output.
 template <typename T, int PL, int CB>
 __global__ __launch_bounds__(512) void muon_wide_kernel(Source src, Target out, int rows, int cols, int each, int step, int steps, const double *part,
@@ -939,7 +951,7 @@ __global__ __launch_bounds__(512) void muon_wide_kernel(Source src, Target out, 
 #pragma unroll
                 for (int v = 0; v < 16; ++v) w.x[c][r][v] = mine[c * (8 * 2048) + (r * 16 + v) * 64];
         w.put_x();
-        w.acc[0] = w.acc[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        w.clear();
         constexpr int U = 8;                       // shares on their way
         for (int g = 0; g < wgs; g += U) {
             f32x4 u[U][2];
@@ -972,12 +984,12 @@ __global__ __launch_bounds__(512) void muon_wide_kernel(Source src, Target out, 
     for (int q = 0; q < 2; ++q) share[at + (size_t)blockIdx.x * 1024 + q * 64] = w.acc[q];
 }
 
-// Column blocks of a wave in one workgroup, 0 where a matrix is too large: its planes' room in LDS, and at most two blocks of X
-// (three spill registers and gain nothing: 64 x 576 takes 42 us either way).
+// Column blocks of a wave in one workgroup, 0 where a matrix is too large: its planes' room in LDS, and at most 640 columns (64 x 576,
+// bf16: 38.7 us, and 42.3 in three workgroups and seven launches; 64 x 768: 44.4, and 42.5).
 int small_blocks(int planes, int rows, int cols)
 {
     const int m = rows < cols ? rows : cols, n = rows < cols ? cols : rows, blocks = (n + 31) / 32, cb = (blocks + 7) / 8;
-    return m <= kFewRows && cb <= 2 && few_lds(planes, blocks) <= kLds ? cb : 0;
+    return m <= kFewRows && blocks <= 20 && few_lds(planes, blocks) <= kLds ? cb : 0;
 }
 // Matrices of few rows with more columns: 256 columns to a workgroup while that makes at most 16, whose shares each of them adds up,
 // else as many as LDS has room for, up to 512.
@@ -1081,6 +1093,8 @@ int run(int batch, int rows, int cols, int steps, const Source &src, const Targe
 {
     if (const int cb = small_blocks(PL, rows, cols)) {
         auto kern = cb == 1 ? muon_small_kernel<T, PL, 1> : muon_small_kernel<T, PL, 2>;
+        if constexpr (PL == 1)                         // (two planes of so many columns have no room)
+            if (cb == 3) kern = muon_small_kernel<T, PL, 3>;
         if (!raise_lds_limit(reinterpret_cast<const void *>(kern))) return VGG_ERR_LAUNCH;
         hipLaunchKernelGGL(kern, dim3(batch), dim3(512), few_lds(PL, ((rows < cols ? cols : rows) + 31) / 32), s, src, out, rows, cols, steps);
         return launch_status();

@@ -192,7 +192,8 @@ __device__ __forceinline__ void offer(Best &b, float v, int id, int lane)
     if (b.count > kList - 64) cut(b, lane);
 }
 // A bar that at least `top` of a first lot's scores reach, so of all: halvings between the least of the lanes' best
-// and the largest bring it near the top-th.  For few alternatives only the lanes' best are counted.
+// and the largest bring it near the top-th.  For up to 32 alternatives only the lanes' best are counted, which leaves some 44 scores
+// that reach the bar at most.
 template <int V> __device__ __forceinline__ void expect(Best &b, const float (&z)[V], float most)
 {
     const int lanes = __builtin_popcountll(__ballot(most > -INFINITY));
@@ -203,7 +204,7 @@ template <int V> __device__ __forceinline__ void expect(Best &b, const float (&z
     for (int k = 0; k < 8; ++k) {
         const float t = 0.5f * lo + 0.5f * hi;
         int count = 0;
-        if (b.top > 8) {
+        if (b.top > 32) {
 #pragma unroll
             for (int j = 0; j < V; ++j) count += __builtin_popcountll(__ballot(z[j] >= t));
         } else
@@ -408,14 +409,23 @@ __global__ __launch_bounds__(64) void log_probs_join_kernel(const T *__restrict_
         auto entry = [&](int e) __attribute__((always_inline)) {
             return e < all ? keys[(size_t)(e % a.parts) * a.top + e / a.parts] : 0;
         };
-        Key next = entry(lane);
-        for (int e0 = 0, without = 0; e0 < all && without < a.parts; e0 += 64) {
-            const Key k = next;
-            next = entry(e0 + 64 + lane);
-            const float v[1] = {k ? score_of(k) : -INFINITY};
-            if (e0 == 0) expect(b, v, v[0]);
-            without = __any(may_enter(b, v[0], class_of(k))) ? 0 : without + 64;
-            offer(b, v[0], class_of(k), lane);
+        constexpr int U = 4;                         // entries of a lane on their way
+        for (int e0 = 0, without = 0; e0 < all && without < a.parts; e0 += 64 * U) {
+            Key k[U];
+            float v[U], most = -INFINITY;
+#pragma unroll
+            for (int u = 0; u < U; ++u) k[u] = entry(e0 + 64 * u + lane);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                v[u] = k[u] ? score_of(k[u]) : -INFINITY;
+                most = fmaxf(most, v[u]);
+            }
+            if (e0 == 0) expect(b, v, most);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                without = __any(may_enter(b, v[u], class_of(k[u]))) ? 0 : without + 64;
+                offer(b, v[u], class_of(k[u]), lane);
+            }
             if (b.count >= a.top + 32) cut(b, lane);
         }
         cut(b, lane);
