@@ -317,7 +317,7 @@ int vgg_sgd_update(size_t n, float *theta, const float *grad, float lr, void *st
  * when top is 0).  A score of -inf masks its class: probability 0, never an
  * alternative.  Missing alternatives are -inf at class -1; a row without a
  * class left has logp -inf and entropy 0.  A NaN or +inf among a row's scores
- * makes the row's results NaN (alternatives: at class -1).  N <= 2^23.
+ * makes the row's results NaN (alternatives: at class -1).  N <= 2^23, K <= 2^30.
  * The scores are read once; sums are fp32.  Rows too few to fill the chip are
  * cut into parts that a second kernel joins in a fixed order (workspace). */
 #define VGG_MAX_TOP 64
@@ -356,9 +356,11 @@ int vgg_fc_w4_quantize(int In, int Out, int group, const float *w, uint8_t *code
 int vgg_fc_w4_dequantize(int In, int Out, int group, const uint8_t *codes, const uint16_t *scales, float *w, void *stream);
 /* vgg_fc with such weights: z[n,o] = f(bias[o] + sum_i w[o,i] a[n,i]), a
  * [N][In] in `dtype` (rows densely packed), z [N][Out] in z_dtype, bias fp32
- * or NULL.  Any N, Out > 0, 0 < In <= 2^22.  Weights are never rounded further: products
- * of code values and activations (fp32 ones to 2^-24) are summed in fp32
- * group by group, and a group's sum is multiplied by its scale. */
+ * or NULL.  0 < N <= 2^23, 0 < In <= 2^22, 0 < Out <= 2^25, and In (in whole
+ * 128s) Out, N In
+ * and N Out at most 2^33.  Weights are never rounded further: products of code
+ * values and activations (fp32 ones to 2^-24) are summed in fp32 group by
+ * group, and a group's sum is multiplied by its scale. */
 size_t vgg_fc_w4_workspace_bytes(int dtype, int N, int In, int Out, int group);
 int vgg_fc_w4(int dtype, int N, int In, int Out, int group, const void *a, const uint8_t *codes, const uint16_t *scales,
               const float *bias, void *z, int z_dtype, int relu, void *ws, size_t ws_bytes, void *stream);

@@ -501,10 +501,11 @@ bool params_aligned(const vgg19_params *p)
     return true;
 }
 
-bool scores_shape_ok(int N, int K, size_t ld) { return N > 0 && N <= (1 << 23) && K > 0 && ld >= (size_t)K; }
+// (launches stay below 2^32 threads, offsets within a row below 2^31)
+bool scores_shape_ok(int N, int K, size_t ld) { return N > 0 && N <= (1 << 23) && K > 0 && K <= (1 << 30) && ld >= (size_t)K; }
 bool w4_shape_ok(int In, int Out, int group)
 {
-    return In > 0 && Out > 0 && In <= (1 << 22) && (long)((In + 127) / 128 * 128) * Out <= (1L << 33) && (group == 32 || group == 64 || group == 128);
+    return In > 0 && Out > 0 && In <= (1 << 22) && Out <= (1 << 25) && (long)((In + 127) / 128 * 128) * Out <= (1L << 33) && (group == 32 || group == 64 || group == 128);
 }
 bool muon_shape_ok(int batch, int rows, int cols)
 {
@@ -913,7 +914,7 @@ int vgg_fc_w4_dequantize(int In, int Out, int group, const uint8_t *codes, const
 
 size_t vgg_fc_w4_workspace_bytes(int dtype, int N, int In, int Out, int group)
 {
-    if (!dtype_ok(dtype) || N <= 0 || !w4_shape_ok(In, Out, group)) return 0;
+    if (!dtype_ok(dtype) || N <= 0 || N > (1 << 23) || !w4_shape_ok(In, Out, group)) return 0;
     return fc_w4_workspace(dtype, N, In, Out, group);
 }
 
@@ -922,7 +923,7 @@ int vgg_fc_w4(int dtype, int N, int In, int Out, int group, const void *a, const
 {
     if (!a || !codes || !scales || !z) return VGG_ERR_NULL;
     if (!dtype_ok(dtype) || !dtype_ok(z_dtype)) return VGG_ERR_DTYPE;
-    if (N <= 0 || !w4_shape_ok(In, Out, group) || (long)N * In > (1L << 33) || (long)N * Out > (1L << 33)) return VGG_ERR_SHAPE;
+    if (N <= 0 || N > (1 << 23) || !w4_shape_ok(In, Out, group) || (long)N * In > (1L << 33) || (long)N * Out > (1L << 33)) return VGG_ERR_SHAPE;
     if (!aligned16(a) || !aligned16(codes) || !aligned16(scales) || !aligned16(bias) || !aligned16(z) || !aligned16(ws)) return VGG_ERR_ALIGN;
     const size_t need = fc_w4_workspace(dtype, N, In, Out, group);
     if (need && (!ws || ws_bytes < need)) return VGG_ERR_WORKSPACE;

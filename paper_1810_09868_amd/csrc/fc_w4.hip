@@ -477,7 +477,8 @@ __global__ __launch_bounds__(512) void fc_w4_tiles_kernel(const u32x4 *__restric
     constexpr int W = 8, S = 4 / G, F = NT * 4;        // F: blocks of 16 rows x 32 inputs of a step
     constexpr int AHEAD = P == 1 ? 4 : 2;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, g = lane >> 4;
-    const int split = blockIdx.x / p.row_tiles, o0 = (blockIdx.x - split * p.row_tiles) * (16 * RT), n0 = blockIdx.y * (16 * NT);
+    const int across = p.row_tiles * p.splits, by = blockIdx.x / across, bx = blockIdx.x - by * across;
+    const int split = bx / p.row_tiles, o0 = (bx - split * p.row_tiles) * (16 * RT), n0 = by * (16 * NT);
     const int KB = (p.In + 127) / 128, whole = p.In / 128;
     const int kb0 = (int)((long)KB * split / p.splits), kb1 = (int)((long)KB * (split + 1) / p.splits);
     const int tiles = (p.N + 16 * NT - 1) / (16 * NT) * NT;
@@ -506,7 +507,7 @@ __global__ __launch_bounds__(512) void fc_w4_tiles_kernel(const u32x4 *__restric
     u32x4 ring[AHEAD][P];
     auto fetch_x = [&](int kb, int i, u32x4 (&f)[P]) __attribute__((always_inline)) {
         if (i >= F) { i -= F; kb = kb + W < kb1 ? kb + W : kb; }
-        const u32x4 *src = x + ((((size_t)kb * tiles + blockIdx.y * NT) * 4 + i) * P) * 64;
+        const u32x4 *src = x + ((((size_t)kb * tiles + by * NT) * 4 + i) * P) * 64;
 #pragma unroll
         for (int k = 0; k < P; ++k) f[k] = src[k * 64 + lane];
     };
@@ -649,7 +650,7 @@ int launch_tiles_of(const T *a, W4Args p, const W4Plan &t, void *ws, hipStream_t
     p.row_tiles = t.row_tiles;
     const unsigned units = (unsigned)((p.In + 127) / 128) * t.tiles * 4;
     hipLaunchKernelGGL(fc_w4_lay_kernel<T>, dim3((units + 3) / 4), dim3(256), 0, s, a, x, p.N, p.In, t.tiles, units);
-    hipLaunchKernelGGL((fc_w4_tiles_kernel<P, RT, NT, G>), dim3((unsigned)(t.row_tiles * t.splits), (unsigned)(t.tiles / NT)), dim3(512), (size_t)8 * NT * 1024, s, x, p);
+    hipLaunchKernelGGL((fc_w4_tiles_kernel<P, RT, NT, G>), dim3((unsigned)(t.row_tiles * t.splits * (t.tiles / NT))), dim3(512), (size_t)8 * NT * 1024, s, x, p);
     if (t.splits > 1) hipLaunchKernelGGL(fc_w4_join_kernel, dim3((unsigned)(((size_t)p.N * p.Out + 255) / 256)), dim3(256), 0, s, p);
     return launch_status();
 }

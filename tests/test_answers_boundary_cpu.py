@@ -49,3 +49,15 @@ def test_orthogonalised_updates_are_refused_on_the_host():
             assert B.vgg_muon_workspace_bytes(dt, *shape) == B.vgg_orthogonalize_workspace_bytes(dt, *shape) > 0
     # transposed matrices are worked on alike
     assert B.vgg_muon_workspace_bytes(B.F32, 1, 1000, 4096) == B.vgg_muon_workspace_bytes(B.F32, 1, 4096, 1000)
+
+
+def test_sizes_past_what_a_launch_holds_are_refused_on_the_host():
+    L = B.lib()
+    K = (1 << 30) + 1
+    assert L.vgg_log_probs(0, 1, K, K, A, A, 0, A, A, None, None, A, A, 1 << 40, None) == -2
+    assert L.vgg_log_probs_bwd(0, 1, K, K, A, A, A, A, A, None, 2 * A, K, None) == -2
+    assert B.vgg_log_probs_workspace_bytes(B.F32, 1, K, 0) == 0 < B.vgg_log_probs_workspace_bytes(B.F32, 1, K - 1, 0)
+    w4 = lambda N, i, o: L.vgg_fc_w4(0, N, i, o, 32, A, A, A, None, A, 0, 1, A, 1 << 50, None)  # noqa: E731
+    assert w4((1 << 23) + 1, 1, 1) == w4(1, 1, (1 << 25) + 1) == w4(1 << 22, 1, 1 << 12) == w4(1 << 22, 1 << 12, 1) == -2
+    assert L.vgg_fc_w4_quantize(1, (1 << 25) + 1, 32, A, A, A, None) == L.vgg_fc_w4_dequantize(1 << 22, 1 << 12, 32, A, A, A, None) == -2
+    assert B.vgg_fc_w4_workspace_bytes(B.F32, (1 << 23) + 1, 64, 64, 32) == 0 < B.vgg_fc_w4_workspace_bytes(B.F32, 1 << 23, 64, 64, 32)
