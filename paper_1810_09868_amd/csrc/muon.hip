@@ -275,9 +275,10 @@ template <typename T> __device__ __forceinline__ void write_some(const Target &o
 // sixteen rows of one segment are in different banks; the two 64-byte blocks of a row r of
 // B that is read transposed change places where r / 2 is odd, for the four rows that sixteen lanes read.  256 x 256 tiles take 2/3 of the
 // LDS traffic of 128 x 128 ones, and four times the work.  Large products are bound by the matrix unit and its power (4096 x 25088, two
-// planes: G in 1.02 ms, 1.33 PFLOP/s of f16 products, pipes busy 0.73; P X in 2.1 ms, 1.2 PFLOP/s); 128 x 128 tiles of short
-// contractions by X's way through memory (7 x 512 x 4608, one plane: P X in 37 us for 165 MB) and, one to a compute unit, by their
-// beginnings and ends (two to one, with half the stages: 4 % faster there, 3 % slower where one round of the chip is enough).
+// planes: G in 1.02 ms, 1.33 PFLOP/s of f16 products, pipes busy 0.73; P X in 2.1 ms, 1.2 PFLOP/s), smaller ones by what P X moves
+// between the eight L2s and memory (7 x 512 x 4608, one plane: 37 us for 165 MB; 1000 x 4096, two: 31 us for 98 MB) and by their
+// beginnings and ends, not by LDS or barriers: four waves to a tile are 2 to 5 % slower, stages twice as long or what the end
+// reads asked for at the start make no difference, two workgroups to a compute unit 4 % for many rounds and -3 % for one.
 template <typename T, int PL, int MODE, int TILE>
 __global__ __launch_bounds__(512) void muon_product_kernel(Layout L, int from, Target out)
 {
