@@ -94,6 +94,22 @@ template <int V> __device__ __forceinline__ void add_scores(Sums &a, const float
         }
 }
 
+// The same where there is none yet.
+template <int V> __device__ __forceinline__ void first_scores(Sums &a, const float (&z)[V], float most)
+{
+    bool fresh = most > -INFINITY;
+    const float base = fresh ? most : 0.f;
+    a.m = most;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        const float d = z[j] - base, e = __expf(d);
+        const bool it = fresh && z[j] == most;
+        a.e += it ? 0.f : e;
+        a.t = __builtin_fmaf(fmaxf(d, kLowest), e, a.t);
+        fresh = fresh && !it;
+    }
+}
+
 // A score and its class as one number: the better, the larger; equal scores: the lower class.  0: none.
 typedef unsigned long long Key;
 __device__ __forceinline__ Key key_of(float v, int id)
@@ -247,18 +263,16 @@ struct ScoreArgs {
 
 // Log of a row's sum: -inf where it has no class, NaN with a NaN or +inf.
 __device__ __forceinline__ float log_sum(const Sums &r) { return r.m == -INFINITY && r.e == 0.f ? -INFINITY : r.m < INFINITY ? log1pf(r.e) : NAN; }
-__device__ __forceinline__ void write_row(const ScoreArgs &a, const Sums &r, float z_label, int y, int row)
+__device__ __forceinline__ void write_row(const ScoreArgs &a, const Sums &r, float log_s, float z_label, int y, int row)
 {
-    const float log_s = log_sum(r);
     const bool empty = log_s == -INFINITY;
     if (a.logp) a.logp[row] = y < 0 || y >= a.K ? 0.f : empty ? -INFINITY : (z_label - r.m) - log_s;
     if (a.entropy) a.entropy[row] = empty ? 0.f : log_s - r.t / (1.f + r.e);
     if (a.stats) { a.stats[2 * (size_t)row] = r.m; a.stats[2 * (size_t)row + 1] = log_s; }
 }
 // Alternative i of a row: `k`, or none.
-__device__ __forceinline__ void write_best(const ScoreArgs &a, const Sums &r, int row, int i, Key k)
+__device__ __forceinline__ void write_best(const ScoreArgs &a, const Sums &r, float log_s, int row, int i, Key k)
 {
-    const float log_s = log_sum(r);
     const bool there = k && log_s > -INFINITY;       // (not with a NaN either)
     const size_t at = (size_t)row * a.top + i;
     a.top_logp[at] = there ? (score_of(k) - r.m) - log_s : log_s == log_s ? -INFINITY : log_s;
@@ -323,8 +337,11 @@ __global__ __launch_bounds__(256) void log_probs_kernel(const T *__restrict__ z,
     float ends = -INFINITY;
     const int end_k = lane < head ? k0 + lane : tail0 + lane - head;
     if ((W == 1 || wave == 0) && (lane < head || end_k < k1)) ends = Elem<T>::load(zr + end_k);
-    for (int i0 = ti; i0 - ti < nvec; i0 += U * tn) {
-        float x[U * V];
+    // (a row that one wave takes is one lot, its ends among it: what runs is short, and so are the instructions' own way from memory
+    // and what waits for it: 100 x 1000, top 5: OLD us with a loop around it)
+    constexpr int E = U * V + (W == 1);
+    auto lot = [&](int i0) __attribute__((always_inline)) {
+        float x[E];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int i = i0 + u * tn;
@@ -336,38 +353,43 @@ __global__ __launch_bounds__(256) void log_probs_kernel(const T *__restrict__ z,
 #pragma unroll
             for (int j = 0; j < V; ++j) x[u * V + j] = v[j];
         }
-        float lot = -INFINITY;
+        if constexpr (W == 1) x[E - 1] = ends;
+        float most = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < U * V; ++j) lot = fmaxf(lot, x[j]);
+        for (int j = 0; j < E; ++j) most = fmaxf(most, x[j]);
         if constexpr (TOP)
-            if (i0 == ti) expect(b, x, lot);
-        add_scores<U * V>(mine, x, lot);
+            if (i0 == ti) expect(b, x, most);
+        if constexpr (W == 1) first_scores(mine, x, most);
+        else add_scores(mine, x, most);
         if constexpr (TOP)
-            if (__any(lot >= b.worst_v && lot > -INFINITY)) {
+            if (__any(most >= b.worst_v && most > -INFINITY)) {
                 // (a loop over the most that a lane has, its scores read again: 16 offers in a row are more instructions than a
                 // short row waits for)
                 unsigned some = 0;
 #pragma unroll
-                for (int j = 0; j < U * V; ++j) some |= (x[j] >= b.worst_v && x[j] > -INFINITY ? 1u : 0u) << j;
+                for (int j = 0; j < E; ++j) some |= (x[j] >= b.worst_v && x[j] > -INFINITY ? 1u : 0u) << j;
                 while (__any(some)) {
-                    const int j = some ? __builtin_ctz(some) : 0, k = v0 + (i0 + j / V * tn) * V + j % V;
+                    const int j = some ? __builtin_ctz(some) : 0, k = j < U * V ? v0 + (i0 + j / V * tn) * V + j % V : end_k;
                     offer(b, some ? Elem<T>::load(zr + k) : -INFINITY, k, lane);
                     some &= some - 1;
                 }
                 if (b.count > b.top + 24 && i0 - ti + U * tn < nvec) cut(b, lane);   // (what follows meets a higher bar)
             }
-    }
-    {
+    };
+    if constexpr (W == 1) lot(ti);
+    else {
+        for (int i0 = ti; i0 - ti < nvec; i0 += U * tn) lot(i0);
         const float x[1] = {ends};
-        add_scores<1>(mine, x, ends);
+        add_scores(mine, x, ends);
         if constexpr (TOP) offer(b, ends, end_k, lane);
     }
     mine = wave_joined(mine, lane);
     if constexpr (TOP) cut(b, lane);
 
     if constexpr (W == 1) {
-        if (lane == 0) write_row(a, mine, z_label, y, row);
-        if (TOP && lane < a.top) write_best(a, mine, row, lane, lane < b.count ? b.list[lane] : 0);
+        const float log_s = log_sum(mine);
+        if (lane == 0) write_row(a, mine, log_s, z_label, y, row);
+        if (TOP && lane < a.top) write_best(a, mine, log_s, row, lane, lane < b.count ? b.list[lane] : 0);
     } else {
         if (lane == 0) {
             sums[wave] = mine;
@@ -376,14 +398,17 @@ __global__ __launch_bounds__(256) void log_probs_kernel(const T *__restrict__ z,
         __syncthreads();
         mine = sums[0];
         for (int w = 1; w < W; ++w) mine = joined(mine, sums[w]);
-        if (a.parts == 1) {
-            if (threadIdx.x == 0) write_row(a, mine, z_label, y, row);
-            if constexpr (TOP) merge_lists<W>(lists, counts, a.top, [&](int i, Key k) { write_best(a, mine, row, i, k); });
-            return;
-        }
+        const float log_s = log_sum(mine);
         const size_t at = (size_t)row * a.parts + part;
-        if (threadIdx.x == 0) { a.part_sums[at * 3] = mine.m; a.part_sums[at * 3 + 1] = mine.e; a.part_sums[at * 3 + 2] = mine.t; }
-        if constexpr (TOP) merge_lists<W>(lists, counts, a.top, [&](int i, Key k) { a.part_best[at * a.top + i] = k; });
+        if (threadIdx.x == 0) {
+            if (a.parts == 1) write_row(a, mine, log_s, z_label, y, row);
+            else { a.part_sums[at * 3] = mine.m; a.part_sums[at * 3 + 1] = mine.e; a.part_sums[at * 3 + 2] = mine.t; }
+        }
+        if constexpr (TOP)
+            merge_lists<W>(lists, counts, a.top, [&](int i, Key k) __attribute__((always_inline)) {
+                if (a.parts == 1) write_best(a, mine, log_s, row, i, k);
+                else a.part_best[at * a.top + i] = k;
+            });
     }
 }
 
@@ -431,8 +456,9 @@ __global__ __launch_bounds__(64) void log_probs_join_kernel(const T *__restrict_
         cut(b, lane);
     }
     mine = wave_joined(mine, lane);
-    if (lane == 0) write_row(a, mine, z_label, y, row);
-    if (TOP && lane < a.top) write_best(a, mine, row, lane, lane < b.count ? list[lane] : 0);
+    const float log_s = log_sum(mine);
+    if (lane == 0) write_row(a, mine, log_s, z_label, y, row);
+    if (TOP && lane < a.top) write_best(a, mine, log_s, row, lane, lane < b.count ? list[lane] : 0);
 }
 
 // dz_j = g (1[j = y] - p_j) - h p_j (log p_j + entropy).
