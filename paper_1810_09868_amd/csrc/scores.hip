@@ -10,6 +10,8 @@
 // A NaN makes E, and it or a +inf everything of its row NaN.
 #include "common.h"
 
+#include <type_traits>
+
 namespace vgg {
 
 namespace {
@@ -307,8 +309,8 @@ template <int W, typename F> __device__ __forceinline__ void merge_lists(const K
 // W waves to a row or to a part of one; W == 1: four rows to a workgroup.  A score is read once, in 16-byte loads,
 // and lives in registers from there on; long rows are bound by the read and the exponential beside it (4096 x
 // 32768, bf16: 60 us, 4.5 TB/s), short ones by the launch, one trip to memory, and the alternatives: listing and ranking them is a
-// chain of LDS and ballots that nothing hides (100 x 1000, fp32: 3.9 us without, 7.2 us with the best five; 4 x 200003, bf16: 6.5 us,
-// 17.2 us with the best twenty).
+// chain of LDS and ballots that nothing hides (100 x 1000, fp32: 3.2 us without, 5.4 us with the best five; 4 x 200003, bf16: 6.6 us,
+// 15.5 us with the best twenty).
 template <typename T, int W, bool TOP>
 __global__ __launch_bounds__(256) void log_probs_kernel(const T *__restrict__ z, ScoreArgs a)
 {
@@ -337,10 +339,11 @@ __global__ __launch_bounds__(256) void log_probs_kernel(const T *__restrict__ z,
     float ends = -INFINITY;
     const int end_k = lane < head ? k0 + lane : tail0 + lane - head;
     if ((W == 1 || wave == 0) && (lane < head || end_k < k1)) ends = Elem<T>::load(zr + end_k);
-    // (a row that one wave takes is one lot, its ends among it: what runs is short, and so are the instructions' own way from memory
-    // and what waits for it: 100 x 1000, top 5: OLD us with a loop around it)
-    constexpr int E = U * V + (W == 1);
-    auto lot = [&](int i0) __attribute__((always_inline)) {
+    // The first lot has the ends among it and no sums before it.  (A short row's time is largely its instructions' own way from memory:
+    // with the first lot in the loop, the ends after it and the log of the sum taken twice, 100 x 1000, top 5, took 7.2 us, not 5.4.)
+    auto lot = [&](auto is_first, int i0) __attribute__((always_inline)) {
+        constexpr bool FIRST = decltype(is_first)::value;
+        constexpr int E = U * V + FIRST;
         float x[E];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -353,13 +356,12 @@ __global__ __launch_bounds__(256) void log_probs_kernel(const T *__restrict__ z,
 #pragma unroll
             for (int j = 0; j < V; ++j) x[u * V + j] = v[j];
         }
-        if constexpr (W == 1) x[E - 1] = ends;
+        if constexpr (FIRST) x[E - 1] = ends;
         float most = -INFINITY;
 #pragma unroll
         for (int j = 0; j < E; ++j) most = fmaxf(most, x[j]);
-        if constexpr (TOP)
-            if (i0 == ti) expect(b, x, most);
-        if constexpr (W == 1) first_scores(mine, x, most);
+        if constexpr (TOP && FIRST) expect(b, x, most);
+        if constexpr (FIRST) first_scores(mine, x, most);
         else add_scores(mine, x, most);
         if constexpr (TOP)
             if (__any(most >= b.worst_v && most > -INFINITY)) {
@@ -376,13 +378,9 @@ __global__ __launch_bounds__(256) void log_probs_kernel(const T *__restrict__ z,
                 if (b.count > b.top + 24 && i0 - ti + U * tn < nvec) cut(b, lane);   // (what follows meets a higher bar)
             }
     };
-    if constexpr (W == 1) lot(ti);
-    else {
-        for (int i0 = ti; i0 - ti < nvec; i0 += U * tn) lot(i0);
-        const float x[1] = {ends};
-        add_scores(mine, x, ends);
-        if constexpr (TOP) offer(b, ends, end_k, lane);
-    }
+    lot(std::true_type{}, ti);
+    if constexpr (W > 1)                 // (one wave's row is one lot)
+        for (int i0 = ti + U * tn; i0 - ti < nvec; i0 += U * tn) lot(std::false_type{}, i0);
     mine = wave_joined(mine, lane);
     if constexpr (TOP) cut(b, lane);
 
@@ -413,8 +411,8 @@ __global__ __launch_bounds__(256) void log_probs_kernel(const T *__restrict__ z,
 }
 
 // The parts of a row: a wave to each row, a part to a lane.  The parts' lists are in order: where no part's r-th best may enter, no
-// later one may.  Bound by the launch and by the lists' way from memory, one step ahead (2.5 us; 7 us for 4 rows of 49 parts with the
-// best twenty; a wave that took the parts' scores one rank after another, without a step ahead, 10 us more).
+// later one may.  Bound by the launch and by the lists' way from memory, 256 entries at a time (2.5 us; 5.5 us for 4 rows of 49 parts with
+// the best twenty; 512 x 50001, top 20, in two parts: 46 us, 58 us with one rank of the parts at a time).
 template <typename T, bool TOP>
 __global__ __launch_bounds__(64) void log_probs_join_kernel(const T *__restrict__ z, ScoreArgs a)
 {
@@ -513,9 +511,10 @@ __global__ __launch_bounds__(256) void log_probs_bwd_kernel(const T *z, T *dz, G
     }
 }
 
-constexpr int kOneWave = 1024;   // scores that one wave takes by itself (16 x 2048, top 5: 9.9 us so, 7.2 us with four waves)
+constexpr int kOneWave = 1024;   // scores that one wave takes by itself (16 x 2048, top 5: 9.9 us so, 6.7 us with four waves; 4096 x 1000:
+                                 // 9.2 us so, 24 us with four)
 struct Split { int parts, span; };
-// Rows that are too few to fill the chip are cut into parts of at least 4096 scores (1 x 50000, top 1: 9.8 us, 17.4 us in one part of
+// Rows that are too few to fill the chip are cut into parts of at least 4096 scores (1 x 50000, top 1: 9.7 us, 17.4 us in one part of
 // sixteen waves).
 Split split_rows(int N, int K)
 {
