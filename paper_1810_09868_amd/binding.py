@@ -134,7 +134,7 @@ def _ptr(t) -> Optional[int]:
 
 
 def _nbytes(t) -> int:
-    return 0 if t is None else t.numel() * t.element_size()
+    return 0 if t is None else t.nbytes
 
 
 _RAW_STREAM = None
