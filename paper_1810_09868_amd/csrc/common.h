@@ -44,6 +44,15 @@ struct ConvStep {
     int Cout, CinP;
 };
 
+// A copy from each lane's own address straight to LDS, 16 bytes a lane, lane l's at lds + 16 l.  Issued as inline assembly on purpose: the
+// compiler would wait for it before every read of LDS that it cannot tell apart from what is written.  LDS copies take the address from
+// m0 one wait state after a scalar instruction has written it at the earliest, and the compiler, which sees to that elsewhere,
+// does not look into assembly: hence s_nop, here and at the copies of other forms (or another instruction between the two).
+__device__ __forceinline__ void copy16_to_lds(unsigned lds, const void *src)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds), "v"(src) : "m0", "memory");
+}
+
 __device__ __forceinline__ float bf16_to_f32(bf16_t h) { return __uint_as_float(((unsigned int)h) << 16); }
 
 template <typename T> struct Elem;

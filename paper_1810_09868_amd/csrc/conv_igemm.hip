@@ -254,7 +254,7 @@ __global__ __launch_bounds__(WM *WN * 64, WM *WN == 8 ? 4 : 3) void conv3x3_igem
             // Issued as inline assembly on purpose: the compiler cannot tell that this write and the
             // fragment reads of the other buffer never overlap and would wait for it before every read.
             const unsigned dst = bs_lds + buf * b_bytes + q * 1024;
-            asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(dst), "v"(woff[q]), "s"(base) : "m0", "memory");
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(dst), "v"(woff[q]), "s"(base) : "m0", "memory");
         }
     };
     dma_b(c_first, 0, 0);  // first: its latency covers the index arithmetic below
@@ -491,7 +491,7 @@ __global__ __launch_bounds__(WM *WN * 64, OCC) void conv3x3_igemm_wreg_kernel(Co
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)smem;
     auto copy_slot = [&](int buf, int k) __attribute__((always_inline)) {
         const unsigned dst = __builtin_amdgcn_readfirstlane(lds0 + buf * ABUF + (k * NW + wv) * 1024);
-        // (every lane of the wave is active where this is called)
+        // (every lane of the wave is active where this is called; the write of exec is the wait that m0 needs)
         asm volatile("s_mov_b32 m0, %0\n\ts_mov_b64 exec, %3\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1"
                      : : "s"(dst), "v"(aoff[k]), "s"(abase), "s"(alanes[k]) : "m0", "memory");
     };
@@ -915,7 +915,7 @@ __global__ __launch_bounds__(G * 64, 2) void conv3x3_small_bf16_kernel(ConvArgs 
         for (int k = 0; k < COPIES; ++k) {
             if (k * 16 < p.rowsA) {
                 const unsigned dst = __builtin_amdgcn_readfirstlane(lds0 + k * 1024);
-                asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
                              : : "s"(dst), "v"(from[k]), "s"(xbuf), "s"(c * kDataBytes) : "m0", "memory");
             }
         }

@@ -94,7 +94,7 @@ __device__ __forceinline__ void wgrad_body(const WgradArgs &p, char *smem)
     const float *zero = reinterpret_cast<const float *>(kZeroSeg);
     auto dma = [&](const float *src, char *dst) __attribute__((always_inline)) {
         const unsigned d = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)dst);
-        asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(d), "v"(src) : "m0", "memory");
+        copy16_to_lds(d, src);
     };
     constexpr int kXBatch = 3;                 // x blocks of a wave whose copies are spread over the steps
     constexpr int kOps = kGOps + kXBatch;      // copies that are spread over the MFMA steps
@@ -290,7 +290,7 @@ __global__ __launch_bounds__(kWaves * 64, 4) void conv3x3_wgrad_thin_kernel(Wgra
     const float *zero = reinterpret_cast<const float *>(kZeroSeg);
     auto dma = [&](const float *src, char *dst) __attribute__((always_inline)) {
         const unsigned d = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)dst);
-        asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(d), "v"(src) : "m0", "memory");
+        copy16_to_lds(d, src);
     };
     // all copies of a tile, in one go (there is little arithmetic to hide them behind)
     auto issue_tile = [&](const TileOrigin &org, char *base, int m_l) __attribute__((always_inline)) {

@@ -137,7 +137,7 @@ __device__ __forceinline__ void wgrad_bf16_body(const WgradBf16Args &p, char *sm
             if (!ok) src = reinterpret_cast<const bf16_t *>(kZero16);
             const unsigned d = __builtin_amdgcn_readfirstlane(
                 (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)(base + (k * kNW + wv) * 1024));
-            asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(d), "v"(src) : "m0", "memory");
+            copy16_to_lds(d, src);
         }
     };
 

@@ -972,7 +972,7 @@ struct DzSteps {
             const int b = wv + 8 * k;
             if (b < 3 * NB) {
                 const unsigned dst = __builtin_amdgcn_readfirstlane(lds + (buffer & (BUFFERS - 1)) * BYTES + b * 1024);
-                asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(dst), "v"(s + b * 1024) : "m0", "memory");
+                copy16_to_lds(dst, s + b * 1024);
             }
         }
     }

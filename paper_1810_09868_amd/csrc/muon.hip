@@ -238,10 +238,6 @@ struct Target {
     float keep, rate;
 };
 
-__device__ __forceinline__ void copy16(unsigned lds, const void *src)   // 16 bytes a lane to lds + 16 lane
-{
-    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds), "v"(src) : "m0", "memory");
-}
 typedef __attribute__((address_space(3))) char lds_char;
 
 // Workgroups go round the eight XCDs; each takes a run of the work, so that neighbours share their operands in its L2.
@@ -330,10 +326,10 @@ __global__ __launch_bounds__(512) void muon_product_kernel(Layout L, int from, T
     auto copy_one = [&](int n) __attribute__((always_inline)) {      // of a stage's 2 COPIES
         const int q = n >> 1;
         if (n & 1) {
-            copy16(lds0 + slot * (2 * HALF) + HALF + q * 8192, src_b[q]);
+            copy16_to_lds(lds0 + slot * (2 * HALF) + HALF + q * 8192, src_b[q]);
             src_b[q] += step_b;
         } else {
-            copy16(lds0 + slot * (2 * HALF) + q * 8192, src_a[q]);
+            copy16_to_lds(lds0 + slot * (2 * HALF) + q * 8192, src_a[q]);
             src_a[q] += column;
         }
         if (n == 2 * COPIES - 1) slot = slot + 1 == STAGES ? 0 : slot + 1;
