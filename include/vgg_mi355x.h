@@ -371,9 +371,9 @@ int vgg_fc_w4(int dtype, int N, int In, int Out, int group, const void *a, const
  * the other in memory: x / (|x|_F + 1e-7), then `steps` (1..20) times
  *   G = X X^T,  X <- 3.4445 X + (-4.7750 G + 2.0315 G G) X
  * (with X^T in X's place where rows > cols: the same values), which takes the
- * singular values towards 1.  VGG_F32: products as exact as fp32 ones (two
- * f16 parts per value, fp32 sums).  VGG_BF16: x and y are bf16, operands of a
- * product hold 11 bits, the iterate 22 or more, sums are fp32.  y may be x.  A
+ * singular values towards 1.  Products are as exact as fp32 ones (operands in
+ * two f16 parts, 22 bits down to 2^-17 and 2^-39 below; fp32 sums) and the
+ * iterate is fp32 in both types; a bf16 y is rounded once.  y may be x.  A
  * matrix with a NaN or an infinity comes out NaN.  min(rows, cols) <= 32768,
  * both <= 2^22, batch <= 65535. */
 size_t vgg_orthogonalize_workspace_bytes(int dtype, int batch, int rows, int cols);
@@ -384,7 +384,9 @@ int vgg_orthogonalize(int dtype, int batch, int rows, int cols, int steps, const
  *   momentum <- mu momentum + grad,  u = grad + mu momentum (nesterov != 0)
  *                                    or momentum,
  *   theta <- (1 - lr weight_decay) theta - lr sqrt(max(1, rows/cols)) NS(u).
- * dtype says how exact the products of NS are, as above (all buffers fp32). */
+ * All buffers are fp32; dtype says how exact the products of NS are: VGG_F32 as
+ * above, VGG_BF16 with operands of 11 bits (a third of the work; the step is
+ * some 1e-3 off). */
 size_t vgg_muon_workspace_bytes(int dtype, int batch, int rows, int cols);
 int vgg_muon_update(int dtype, int batch, int rows, int cols, int steps, float *theta, const float *grad, float *momentum,
                     float lr, float mu, int nesterov, float weight_decay, void *ws, size_t ws_bytes, void *stream);

@@ -84,7 +84,7 @@ int w4_dequantize(int In, int Out, int group, const uint8_t *codes, const bf16_t
 size_t fc_w4_workspace(int dtype, int N, int In, int Out, int group);
 int fc_w4(int dtype, int N, int In, int Out, int group, const void *a, const uint8_t *codes, const bf16_t *scales, const float *bias, void *z,
           int z_dtype, int relu, void *ws, hipStream_t s);
-size_t muon_workspace(int dtype, int batch, int rows, int cols);
+size_t muon_workspace(int batch, int rows, int cols);
 int orthogonalize(int dtype, int batch, int rows, int cols, int steps, const void *x, void *y, void *ws, hipStream_t s);
 int muon_update(int dtype, int batch, int rows, int cols, int steps, float *theta, const float *grad, float *momentum, float lr, float mu,
                 int nesterov, float weight_decay, void *ws, hipStream_t s);
@@ -516,7 +516,7 @@ int muon_refusal(int dtype, int batch, int rows, int cols, int steps, const void
 {
     if (!dtype_ok(dtype)) return VGG_ERR_DTYPE;
     if (!muon_shape_ok(batch, rows, cols) || steps < 1 || steps > 20) return VGG_ERR_SHAPE;
-    if (!ws || ws_bytes < muon_workspace(dtype, batch, rows, cols)) return VGG_ERR_WORKSPACE;
+    if (!ws || ws_bytes < muon_workspace(batch, rows, cols)) return VGG_ERR_WORKSPACE;
     return aligned16(ws) ? VGG_OK : VGG_ERR_ALIGN;
 }
 
@@ -932,7 +932,7 @@ int vgg_fc_w4(int dtype, int N, int In, int Out, int group, const void *a, const
 
 size_t vgg_orthogonalize_workspace_bytes(int dtype, int batch, int rows, int cols)
 {
-    return dtype_ok(dtype) && muon_shape_ok(batch, rows, cols) ? muon_workspace(dtype, batch, rows, cols) : 0;
+    return dtype_ok(dtype) && muon_shape_ok(batch, rows, cols) ? muon_workspace(batch, rows, cols) : 0;
 }
 
 int vgg_orthogonalize(int dtype, int batch, int rows, int cols, int steps, const void *x, void *y, void *ws, size_t ws_bytes, void *stream)

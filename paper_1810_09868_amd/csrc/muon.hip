@@ -6,8 +6,8 @@
 //
 // Products are on the f16 matrix unit with fp32 sums.  X, G and P = b G + c G G are bounded (|X|, |G|, |P| <= 1.21, 1.47, 2.9), so
 // that they are held times 2^14, below f16's largest, and need no other scale; f16 then keeps 11 bits of everything down to
-// 2^-28.  PLANES = 2 (VGG_F32): a value is two f16 numbers, the nearest and what that leaves, 22 bits; hi hi + hi lo + lo hi
-// leaves out 2^-22 of a product at most.  PLANES = 1 (VGG_BF16): operands are rounded to 11 bits.  The term a X takes all of X, an
+// 2^-28.  PLANES = 2: a value is two f16 numbers, the nearest and what that leaves, 22 bits down to 2^-17 and 2^-39 below; hi hi + hi lo
+// + lo hi leaves out 2^-22 of a product at most.  PLANES = 1 (updates that ask for VGG_BF16): operands are rounded to 11 bits.  The term a X takes all of X, an
 // fp32 copy or (PLANES = 1, whose results have 8 bits) the operand and what it leaves as another f16 number, 22 bits in two thirds of the
 // bytes: a rounding of X to 11 bits there would grow 3.4-fold in every later step where X has no (or small) singular values.  In
 // both the diagonals of G and P, which hold most of them, are kept apart in fp32 (zeros in the planes): with G = D + E,
@@ -1119,20 +1119,24 @@ int run(int batch, int rows, int cols, int steps, const Source &src, const Targe
 
 }  // namespace
 
-size_t muon_workspace(int dtype, int batch, int rows, int cols)
+// What either number of planes takes: both of a type's calls ask for the same.
+size_t muon_workspace(int batch, int rows, int cols)
 {
-    const int planes = dtype == VGG_BF16 ? 1 : 2;
-    if (is_wide(rows, cols)) return wide_plan(planes, batch, rows, cols).total;   // (one workgroup alone needs none)
-    size_t total;
-    layout_of(planes, batch, rows, cols, nullptr, total);
-    return total;
+    size_t most = 0;
+    for (int planes = 1; planes <= 2; ++planes) {
+        size_t total;
+        if (is_wide(rows, cols)) total = wide_plan(planes, batch, rows, cols).total;   // (one workgroup alone needs none)
+        else layout_of(planes, batch, rows, cols, nullptr, total);
+        if (total > most) most = total;
+    }
+    return most;
 }
 
 int orthogonalize(int dtype, int batch, int rows, int cols, int steps, const void *x, void *y, void *ws, hipStream_t s)
 {
     const Source src = {x, nullptr, 0.f, 0};
     const Target out = {y, nullptr, 0.f, 0.f};
-    return dtype == VGG_BF16 ? run<bf16_t, 1>(batch, rows, cols, steps, src, out, ws, s) : run<float, 2>(batch, rows, cols, steps, src, out, ws, s);
+    return dtype == VGG_BF16 ? run<bf16_t, 2>(batch, rows, cols, steps, src, out, ws, s) : run<float, 2>(batch, rows, cols, steps, src, out, ws, s);
 }
 
 int muon_update(int dtype, int batch, int rows, int cols, int steps, float *theta, const float *grad, float *momentum, float lr, float mu,

@@ -200,3 +200,25 @@ def test_on_another_stream_and_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, z), k
+
+
+def ns64_gpu(u, steps):
+    x = u.t().contiguous() if u.shape[0] > u.shape[1] else u
+    x = x / (torch.linalg.vector_norm(x) + 1e-7)
+    for _ in range(steps):
+        g = x @ x.t().contiguous()
+        x = COEFF[0] * x + COEFF[1] * (g @ x) + COEFF[2] * (g @ (g @ x))
+    return x.t() if u.shape[0] > u.shape[1] else x
+
+
+# A bf16 result that is off by a relative e before it is rounded is another bf16 number than the rounded exact value with
+# probability |error| / spacing, and then a spacing (at most 2^-7 of the value) off: a mean square of at most e 2^-7 of the values'.
+# e is fp32's bound; operands of 11 bits (e some 5e-4 to 1.6e-3) are 1.3e-3 off and more by this measure.
+@pytest.mark.parametrize("kind", ["gradient", "noise"])
+@pytest.mark.parametrize("shape", [(1, 64, 576), (1, 40, 300), (2, 50, 2000), (1, 130, 514), (1, 2100, 130), (2, 512, 4608)])
+def test_bf16_results_are_exact_ones_rounded(shape, kind):
+    x = matrices(B.BF16, *shape, seed=11, kind=kind)
+    got = orthogonalize(B.BF16, x, 5)
+    for b in range(shape[0]):
+        want = ns64_gpu(x[b].double().cuda(), 5).to(torch.bfloat16).double().cpu().numpy()
+        assert off(got[b], want) <= np.sqrt(2.0 ** -7 * bound(B.F32)) + bound(B.F32)
