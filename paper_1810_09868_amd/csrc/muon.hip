@@ -7,16 +7,15 @@
 // Products are on the f16 matrix unit with fp32 sums.  X, G and P = b G + c G G are bounded (|X|, |G|, |P| <= 1.21, 1.47, 2.9), so
 // that they are held times 2^14, below f16's largest, and need no other scale; f16 then keeps 11 bits of everything down to
 // 2^-28.  PLANES = 2: a value is two f16 numbers, the nearest and what that leaves, 22 bits down to 2^-17 and 2^-39 below; hi hi + hi lo
-// + lo hi leaves out 2^-22 of a product at most.  PLANES = 1 (updates that ask for VGG_BF16): operands are rounded to 11 bits.  The term a X takes all of X, an
-// fp32 copy or (PLANES = 1, whose results have 8 bits) the operand and what it leaves as another f16 number, 22 bits in two thirds of the
-// bytes: a rounding of X to 11 bits there would grow 3.4-fold in every later step where X has no (or small) singular values.  In
-// both the diagonals of G and P, which hold most of them, are kept apart in fp32 (zeros in the planes): with G = D + E,
+// + lo hi leaves out 2^-22 of a product at most.  PLANES = 1 (updates that ask for VGG_BF16): operands are rounded to 11 bits.  The term a X takes an
+// fp32 copy of X: a rounding to 11 bits there would grow 3.4-fold in every later step where X has no (or small) singular values, and where the
+// matrix's norm is small beside eps all of X is small and a X nearly all of the result: f16 parts at a fixed scale lose it (130 x 514 of
+// norm 1e-16: 28 % off).  In both the diagonals of G and P, which hold most of them, are kept apart in fp32 (zeros in the planes): with G = D + E,
 //     (G G)_ij = (E E)_ij + (d_i + d_j) e_ij,   (G G)_ii = (E E)_ii + d_i^2,   (P X)_i = p_i X_i + (the rest of P) X.
 // One plane is then 3e-4 to 1e-3 off in all, against 1.3e-3 to 2.4e-3 with the diagonals rounded (bf16's own rounding: 1.7e-3).
 //
 // X, G and P lie in columns of 128 bytes to a row: [column][row][64 elements], or [32 elements of the first plane, 32 of the
-// second], so that what a workgroup copies for a stage of its contraction is contiguous.  X's fp32 copy lies in columns of 32,
-// the rest of its f16 copy as that does.
+// second], so that what a workgroup copies for a stage of its contraction is contiguous.  X's fp32 copy lies in columns of 32.
 // G and G G contract along rows of both operands; P X takes X's columns, which LDS hands out transposed (ds_read_b64_tr_b16), so
 // that X is kept once.  X is padded with zeros to whole tiles.  G and P are symmetric: the tiles on and below the diagonal are
 // formed, over a few ranges of the contraction where they are too few to fill the chip, and a second kernel adds the ranges in
@@ -157,8 +156,7 @@ __global__ __launch_bounds__(256) void muon_norm_kernel(Source s, double *__rest
 struct Layout {
     int rows, cols, m, n, mp, np, tall, tile, parts, batch;   // tile: of the products, 128 or 256, which mp and np are multiples of
     int splits[2];         // of the Gram matrix and its square
-    float *x32;            // [batch][np / 32][mp][32]: PLANES = 2
-    half_t *rest;          // as x, what that leaves: PLANES = 1
+    float *x32;            // [batch][np / 32][mp][32]
     half_t *x[2];          // [batch][columns][mp][64], of mp x np
     half_t *g, *p;         // [batch][columns][mp][64], of mp x mp, zero diagonals
     float *gd, *pd;        // [batch][mp], the diagonals
@@ -218,12 +216,10 @@ __global__ __launch_bounds__(256) void muon_start_kernel(Source s, Layout L)
         }
         const size_t at = at_column<PL>(L.mp, i, j);
         *reinterpret_cast<f16x8 *>(x + at) = hi;
-        *reinterpret_cast<f16x8 *>(PL == 2 ? x + at + 32 : L.rest + b * mn + at) = lo;
-        if constexpr (PL == 2) {
-            float *x32 = L.x32 + b * mn + at_x32(L.mp, i, j);
-            *reinterpret_cast<f32x4 *>(x32) = f32x4{w[0], w[1], w[2], w[3]};
-            *reinterpret_cast<f32x4 *>(x32 + 4) = f32x4{w[4], w[5], w[6], w[7]};
-        }
+        if constexpr (PL == 2) *reinterpret_cast<f16x8 *>(x + at + 32) = lo;
+        float *x32 = L.x32 + b * mn + at_x32(L.mp, i, j);
+        *reinterpret_cast<f32x4 *>(x32) = f32x4{w[0], w[1], w[2], w[3]};
+        *reinterpret_cast<f32x4 *>(x32 + 4) = f32x4{w[4], w[5], w[6], w[7]};
     }
 }
 
@@ -435,21 +431,14 @@ __global__ __launch_bounds__(512) void muon_product_kernel(Layout L, int from, T
 #pragma unroll
         for (int x = 0; x < BX; ++x) {
             const int i = ti * TILE + wi + x * 32 + row;                 // and every (64 / LANES)-th further one
-            auto at = [&](int k) __attribute__((always_inline)) { return b * mn * PL + at_column<PL>(L.mp, i + k * (64 / LANES), j); };
             float old[CHUNKS][8], pd[CHUNKS];
 #pragma unroll
             for (int k = 0; k < CHUNKS; ++k) {
                 pd[k] = kA + L.pd[(size_t)b * L.mp + i + k * (64 / LANES)];
-                if constexpr (PL == 2) {
-                    const float *from32 = L.x32 + b * mn + at_x32(L.mp, i + k * (64 / LANES), j);
-                    const f32x4 lo = *reinterpret_cast<const f32x4 *>(from32), hi = *reinterpret_cast<const f32x4 *>(from32 + 4);
+                const float *from32 = L.x32 + b * mn + at_x32(L.mp, i + k * (64 / LANES), j);
+                const f32x4 lo = *reinterpret_cast<const f32x4 *>(from32), hi = *reinterpret_cast<const f32x4 *>(from32 + 4);
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) { old[k][q] = lo[q]; old[k][4 + q] = hi[q]; }
-                } else {
-                    const f16x8 h = *reinterpret_cast<const f16x8 *>(L.x[from] + at(k)), r = *reinterpret_cast<const f16x8 *>(L.rest + at(k));
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) old[k][q] = ((float)h[q] + (float)r[q]) * kDown;
-                }
+                for (int q = 0; q < 4; ++q) { old[k][q] = lo[q]; old[k][4 + q] = hi[q]; }
             }
 #pragma unroll
             for (int y = 0; y < BY; ++y)
@@ -465,7 +454,7 @@ __global__ __launch_bounds__(512) void muon_product_kernel(Layout L, int from, T
 #pragma unroll
                 for (int q = 0; q < 8; ++q) w[q / 4][q % 4] = __builtin_fmaf(pd[k], old[k][q], w[q / 4][q % 4] * (kDown * kDown));
                 if constexpr (MODE == kApply) {
-                    half_t *to = L.x[1 - from] + at(k);
+                    half_t *to = L.x[1 - from] + b * mn * PL + at_column<PL>(L.mp, i + k * (64 / LANES), j);
                     f16x8 h, r;
 #pragma unroll
                     for (int q = 0; q < 8; ++q) {
@@ -474,12 +463,10 @@ __global__ __launch_bounds__(512) void muon_product_kernel(Layout L, int from, T
                         r[q] = (half_t)(c - (float)h[q]);
                     }
                     *reinterpret_cast<f16x8 *>(to) = h;
-                    *reinterpret_cast<f16x8 *>(PL == 2 ? to + 32 : L.rest + at(k)) = r;
-                    if constexpr (PL == 2) {
-                        f32x4 *to32 = reinterpret_cast<f32x4 *>(L.x32 + b * mn + at_x32(L.mp, i + k * (64 / LANES), j));
-                        to32[0] = w[0];
-                        to32[1] = w[1];
-                    }
+                    if constexpr (PL == 2) *reinterpret_cast<f16x8 *>(to + 32) = r;
+                    f32x4 *to32 = reinterpret_cast<f32x4 *>(L.x32 + b * mn + at_x32(L.mp, i + k * (64 / LANES), j));
+                    to32[0] = w[0];
+                    to32[1] = w[1];
                 } else if (L.tall) {
                     here[0] = w[0];
                     here[1] = w[1];
@@ -1045,8 +1032,7 @@ Layout layout_of(int planes, int batch, int rows, int cols, char *ws, size_t &to
     auto take = [&](size_t bytes) { char *p = ws + off; off += round_up(bytes, 256); return p; };
     const size_t mn = (size_t)batch * L.mp * L.np, mm = (size_t)batch * L.mp * L.mp;
     L.part = reinterpret_cast<double *>(take((size_t)batch * kParts * 8));
-    L.x32 = planes == 2 ? reinterpret_cast<float *>(take(mn * 4)) : nullptr;
-    L.rest = planes == 1 ? reinterpret_cast<half_t *>(take(mn * 2)) : nullptr;
+    L.x32 = reinterpret_cast<float *>(take(mn * 4));
     for (int k = 0; k < 2; ++k) L.x[k] = reinterpret_cast<half_t *>(take(mn * 2 * planes));
     L.g = reinterpret_cast<half_t *>(take(mm * 2 * planes));
     L.p = reinterpret_cast<half_t *>(take(mm * 2 * planes));

@@ -222,3 +222,17 @@ def test_bf16_results_are_exact_ones_rounded(shape, kind):
     for b in range(shape[0]):
         want = ns64_gpu(x[b].double().cuda(), 5).to(torch.bfloat16).double().cpu().numpy()
         assert off(got[b], want) <= np.sqrt(2.0 ** -7 * bound(B.F32)) + bound(B.F32)
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("scale", [2.0 ** -110, 2.0 ** -64, 2.0 ** -50, 2.0 ** -40, 2.0 ** -30])
+@pytest.mark.parametrize("shape", [(40, 60), (50, 1500), (130, 514), (300, 130)])
+def test_matrices_whose_norm_is_small_beside_the_added_constant(dtype, scale, shape):
+    # X_0 is then small itself and grows 3.4445-fold a step: no fixed scale holds its digits
+    x = matrices(dtype, 1, *shape, seed=9) * scale
+    assert off(orthogonalize(dtype, x, 5)[0], ns64(x[0].double().numpy(), 5)) <= bound(dtype)
+    g = x.float().cuda()
+    theta, mom = torch.zeros_like(g), torch.zeros_like(g)
+    B.vgg_muon_update(dtype, 1, *shape, 5, theta, g, mom, 1.0, 0.9, False, 0.0, ws_bytes(B.vgg_muon_workspace_bytes(dtype, 1, *shape)))
+    want = -np.sqrt(max(1, shape[0] / shape[1])) * ns64(x[0].double().numpy(), 5)
+    assert off(theta[0].double().cpu().numpy(), want) <= bound(dtype)
