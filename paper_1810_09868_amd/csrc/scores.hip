@@ -459,7 +459,8 @@ __global__ __launch_bounds__(64) void log_probs_join_kernel(const T *__restrict_
     if (TOP && lane < a.top) write_best(a, mine, log_s, row, lane, lane < b.count ? list[lane] : 0);
 }
 
-// dz_j = g (1[j = y] - p_j) - h p_j (log p_j + entropy).
+// dz_j = g (1[j = y] - p_j) - h p_j (log p_j + entropy); g (1 - p) of the label itself from expm1(log p), which keeps its digits where p is
+// all but 1.
 struct GradArgs {
     int N, K, span, parts;
     size_t ldz, lddz;
@@ -484,11 +485,13 @@ __global__ __launch_bounds__(256) void log_probs_bwd_kernel(const T *z, T *dz, G
     const float m = a.stats[2 * (size_t)row], log_s = a.stats[2 * (size_t)row + 1];
     const bool none = m == -INFINITY && log_s == -INFINITY;
     const bool zero = none || (g == 0.f && h == 0.f);
-    auto grad = [&](float zj, int j) __attribute__((always_inline)) {
+    auto grad = [&](float zj) __attribute__((always_inline)) {
         const float lp = (zj - m) - log_s, p = expf(lp);
-        float x = -p * __builtin_fmaf(h, fmaxf(lp, kNothing) + ent, g);
-        if (j == y && zj > -INFINITY) x += g;
-        return x;
+        return -p * __builtin_fmaf(h, fmaxf(lp, kNothing) + ent, g);
+    };
+    auto grad_of_label = [&](float zj) __attribute__((always_inline)) {      // (masked: zero)
+        const float lp = (zj - m) - log_s;
+        return zj == -INFINITY ? grad(zj) : -__builtin_fmaf(g, expm1f(lp), expf(lp) * h * (fmaxf(lp, kNothing) + ent));
     };
     const int off = (int)((reinterpret_cast<uintptr_t>(zr + k0) & 15) / sizeof(T));
     const bool together = ((reinterpret_cast<uintptr_t>(zr) ^ reinterpret_cast<uintptr_t>(dr)) & 15) == 0;
@@ -500,14 +503,21 @@ __global__ __launch_bounds__(256) void log_probs_bwd_kernel(const T *z, T *dz, G
         if (!zero) {
             load_scores(zr + v0 + (size_t)i * V, x);
 #pragma unroll
-            for (int j = 0; j < V; ++j) x[j] = grad(x[j], v0 + i * V + j);
+            for (int j = 0; j < V; ++j) x[j] = grad(x[j]);
+            const int at = y - (v0 + i * V);
+            if (at >= 0 && at < V) {                     // (its score once more: this thread has not written it yet)
+                const float of_label = grad_of_label(Elem<T>::load(zr + y));
+#pragma unroll
+                for (int j = 0; j < V; ++j) x[j] = j == at ? of_label : x[j];
+            }
         }
 #pragma unroll
         for (int j = 0; j < V; j += 4) store4(dr + v0 + (size_t)i * V + j, x[j], x[j + 1], x[j + 2], x[j + 3]);
     }
     for (int i = tid; i < head + (k1 - tail0); i += TN) {
         const int k = i < head ? k0 + i : tail0 + i - head;
-        Elem<T>::store(dr + k, zero ? 0.f : grad(Elem<T>::load(zr + k), k));
+        const float zk = zero ? 0.f : Elem<T>::load(zr + k);
+        Elem<T>::store(dr + k, zero ? 0.f : k == y ? grad_of_label(zk) : grad(zk));
     }
 }
 

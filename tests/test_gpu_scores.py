@@ -323,3 +323,21 @@ def test_on_another_stream_and_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert same(), k
+
+
+@pytest.mark.parametrize("K", [2, 1000, 5000, 70001])
+def test_the_gradient_of_a_class_that_is_all_but_certain_keeps_its_digits(K):
+    # g (1 - p) = g E / (1 + E), E from 1e-5 to 1e-15: relative to itself, as the forward pass keeps log p = -log1p(E) (E to 4e-6);
+    # the other classes' gradients add up to its opposite (log p down to -40, rounded to 2^-24 of that: 2.4e-6 of p)
+    z = torch.zeros((4, K))
+    for n in range(4):
+        z[n, K // 2 + n - 1 if K > 4 else 0] = float(np.log(K)) + 12 + 7 * n
+    labels = z.argmax(1).int().numpy()
+    c = Call(B.F32, z, labels, 0).run()
+    g = np.array([1.0, -0.25, 3.0, 0.5], np.float32)
+    E = (K - 1) * np.exp(-z.double().max(1).values.numpy())
+    for in_place in (False, True):
+        dz = c.grad(g, None, in_place=in_place).double().cpu().numpy()
+        at = dz[np.arange(4), labels]
+        assert np.abs(at / (g * E / (1 + E)) - 1).max() < 6e-6
+        assert np.abs((dz.sum(1) - at) / at + 1).max() < 1e-5
