@@ -6,7 +6,7 @@
 //     log p_j = (z_j - m) - log S,   log S = log1p(E),   entropy = log S - T / S,
 // E without the largest's own 1, so that the log probability of a class that is all but certain, -E, keeps its digits.  m and
 // log S are kept apart (stats): their sum would round what the gradient takes the exponential of.
-// All sums are fp32.  A score of -inf has d = -inf and exp(d) = 0; only its product d exp(d) has to be kept from NaN.
+// All sums are fp32.  A score of -inf has d = -inf, which is raised to kNothing: exp(d) = 0, and its product with d no NaN.
 // A NaN makes E, and it or a +inf everything of its row NaN.
 #include "common.h"
 
@@ -16,7 +16,6 @@ namespace vgg {
 
 namespace {
 
-constexpr float kLowest = -3.402823466e38f;
 constexpr float kNothing = -1e4f;   // exp of it is 0, and no product with it overflows
 constexpr int kMaxTop = 64;   // one alternative to a lane
 
@@ -72,6 +71,17 @@ __device__ __forceinline__ Sums wave_joined(Sums a, int lane)
     return {M, all_sum(a.e), all_sum(a.t)};
 }
 
+// A difference as exp_of takes it: -inf, and what is too low for any exponential, to kNothing; a NaN as it is.
+__device__ __forceinline__ float below(float d) { return __builtin_elementwise_maximum(d, kNothing); }
+// exp(d), d <= 0 and not below kNothing (or NaN): 2^t, t = d / ln 2 rounded to fp32, times 1 + r, r = d - t ln 2 what that rounding leaves
+// (ln 2 in two parts).  Without r a term is off by up to |d| 2^-24, all terms of a flat tail in the same direction.
+__device__ __forceinline__ float exp_of(float d)
+{
+    constexpr float kLog2E = 1.44269504f, kLn2 = 0.693147182f, kLn2Rest = -1.90465421e-9f;
+    const float t = d * kLog2E, r = __builtin_fmaf(-t, kLn2Rest, __builtin_fmaf(-t, kLn2, d)), e = __builtin_amdgcn_exp2f(t);
+    return __builtin_fmaf(e, r, e);
+}
+
 // V scores, `most` the largest, into a thread's sums.
 template <int V> __device__ __forceinline__ void add_scores(Sums &a, const float (&z)[V], float most)
 {
@@ -81,18 +91,18 @@ template <int V> __device__ __forceinline__ void add_scores(Sums &a, const float
     if (__any(fresh)) {
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const float d = z[j] - base, e = __expf(d);
+            const float d = below(z[j] - base), e = exp_of(d);
             const bool it = fresh && z[j] == a.m;      // one of the new largest does not count
             a.e += it ? 0.f : e;
-            a.t = __builtin_fmaf(fmaxf(d, kLowest), e, a.t);
+            a.t = __builtin_fmaf(d, e, a.t);
             fresh = fresh && !it;
         }
     } else
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-            const float d = z[j] - base, e = __expf(d);
+            const float d = below(z[j] - base), e = exp_of(d);
             a.e += e;
-            a.t = __builtin_fmaf(fmaxf(d, kLowest), e, a.t);
+            a.t = __builtin_fmaf(d, e, a.t);
         }
 }
 
@@ -104,10 +114,10 @@ template <int V> __device__ __forceinline__ void first_scores(Sums &a, const flo
     a.m = most;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-        const float d = z[j] - base, e = __expf(d);
+        const float d = below(z[j] - base), e = exp_of(d);
         const bool it = fresh && z[j] == most;
         a.e += it ? 0.f : e;
-        a.t = __builtin_fmaf(fmaxf(d, kLowest), e, a.t);
+        a.t = __builtin_fmaf(d, e, a.t);
         fresh = fresh && !it;
     }
 }
@@ -307,8 +317,8 @@ template <int W, typename F> __device__ __forceinline__ void merge_lists(const K
 }
 
 // W waves to a row or to a part of one; W == 1: four rows to a workgroup.  A score is read once, in 16-byte loads,
-// and lives in registers from there on; long rows are bound by the read and the exponential beside it (4096 x
-// 32768, bf16: 60 us, 4.5 TB/s), short ones by the launch, one trip to memory, and the alternatives: listing and ranking them is a
+// and lives in registers from there on; long rows are bound by the read and the exponentials beside it (4096 x
+// 32768, bf16, four such tensors in turn: 67 us, 4.0 TB/s; 61 us with exponents rounded to fp32), short ones by the launch, one trip to memory, and the alternatives: listing and ranking them is a
 // chain of LDS and ballots that nothing hides (100 x 1000, fp32: 3.2 us without, 5.4 us with the best five; 4 x 200003, bf16: 6.6 us,
 // 15.5 us with the best twenty).
 template <typename T, int W, bool TOP>
@@ -467,7 +477,7 @@ struct GradArgs {
     const int32_t *labels;
     const float *stats, *entropy, *g_logp, *g_entropy;
 };
-// W waves to a row or to a part of one.  Bound by one read and one write of the scores (4096 x 32768, bf16: 108 us, 5.0 TB/s).
+// W waves to a row or to a part of one.  Bound by one read and one write of the scores (4096 x 32768, bf16, four such tensors in turn: 107 us, 5.0 TB/s).
 template <typename T, int W>
 __global__ __launch_bounds__(256) void log_probs_bwd_kernel(const T *z, T *dz, GradArgs a)
 {

@@ -341,3 +341,16 @@ def test_the_gradient_of_a_class_that_is_all_but_certain_keeps_its_digits(K):
         at = dz[np.arange(4), labels]
         assert np.abs(at / (g * E / (1 + E)) - 1).max() < 6e-6
         assert np.abs((dz.sum(1) - at) / at + 1).max() < 1e-5
+
+
+def test_exponentials_far_below_the_largest_score_are_exact_to_their_last_bits():
+    # E is three times one exponential (of an exact difference, to 2 units of 2^-23; one more for the sum, two for log1p): log p of the
+    # largest is -log1p(E), the entropy log1p(E) - d E / (1 + E).  An exponent rounded to fp32 before it is raised is 20 units off at -80.
+    d = -np.random.default_rng(5).uniform(0.5, 80, 4096).astype(np.float32)
+    z = torch.zeros((4096, 4))                    # (four scores of one lane)
+    z[:, 1:] = torch.from_numpy(d)[:, None]
+    c = Call(B.F32, z, np.zeros(4096, np.int32), 0).run()
+    torch.cuda.synchronize()
+    E = 3 * np.exp(d.astype(np.float64))
+    for got, want, units in ((c.logp, -np.log1p(E), 5), (c.entropy, np.log1p(E) - d * E / (1 + E), 7)):
+        assert np.abs(got.double().cpu().numpy() / want - 1).max() <= units * 2.0 ** -23
