@@ -25,6 +25,18 @@ def _bytes(n: int) -> torch.Tensor:
     return torch.empty((max(int(n), 16),), dtype=torch.uint8, device="cuda")
 
 
+def workspace_bytes(dtype: int, N: int, dims: Sequence[int], group: int, top: int) -> int:
+    """What the calls of a head of these layers need at most, over every number of rows up to N: fewer rows may need more, since
+    they are cut into more parts."""
+    need = [B.vgg_muon_workspace_bytes(dtype, 1, o, i) for i, o in zip(dims[:-1], dims[1:])]
+    for n in range(1, N + 1):
+        need += [B.vgg_log_probs_workspace_bytes(B.F32, n, dims[-1], t) for t in (0, top)]
+        for i, o in zip(dims[:-1], dims[1:]):
+            need += [B.vgg_fc_workspace_bytes(dtype, n, i, o), B.vgg_fc_bwd_workspace_bytes(dtype, n, i, o),
+                     B.vgg_fc_w4_workspace_bytes(dtype, n, i, o, group)]
+    return max(need)
+
+
 class DenseHead:
     """`dims` are the layers' widths, features first and classes last; at most N rows a call."""
 
@@ -52,12 +64,7 @@ class DenseHead:
         self.top_logp, self.top_idx = f32(N, self.top), torch.zeros((N, self.top), dtype=torch.int32, device="cuda")
         self.codes: List[torch.Tensor] = []
         self.scales: List[torch.Tensor] = []
-        need = [B.vgg_log_probs_workspace_bytes(B.F32, N, dims[-1], t) for t in (0, self.top)]
-        for i, o in pairs:
-            need += [B.vgg_fc_workspace_bytes(dtype, N, i, o), B.vgg_fc_bwd_workspace_bytes(dtype, N, i, o),
-                     B.vgg_muon_workspace_bytes(dtype, 1, o, i)]
-            need += [B.vgg_fc_w4_workspace_bytes(dtype, n, i, o, group) for n in range(1, N + 1)]   # (not larger with more rows)
-        self.ws = _bytes(max(need))
+        self.ws = _bytes(workspace_bytes(dtype, N, dims, group, self.top))
 
     def load(self, weights: Sequence[torch.Tensor], biases: Sequence[torch.Tensor]) -> None:
         """Takes fp32 parameters; momentum starts from zero, and 4-bit weights of earlier ones are dropped."""

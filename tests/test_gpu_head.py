@@ -119,3 +119,63 @@ def test_example_runs():
                        text=True, timeout=100)
     assert r.returncode == 0, r.stderr[-2000:]
     assert "4-bit weights" in r.stdout and "one row" in r.stdout
+
+
+def ns_gpu(u):
+    x = u.t().contiguous() if u.shape[0] > u.shape[1] else u
+    x = x / (torch.linalg.vector_norm(x) + 1e-7)
+    for _ in range(5):
+        g = x @ x.t().contiguous()
+        x = 3.4445 * x + (-4.775 * g + 2.0315 * (g @ g)) @ x
+    return x.t() if u.shape[0] > u.shape[1] else x
+
+
+@pytest.mark.parametrize("dims,rows", [([200, 300, 5000], (640, 100, 3)), ([8, 64, 4096, 1000], (1000, 640, 128, 41))])
+def test_wide_heads_follow_64_bits_at_any_number_of_rows(dims, rows):
+    # rows in parts, updates by product tiles, every plan of the dense backward, batches that need more workspace than the largest.
+    # The change of the weights: Newton-Schulz is 3e-5 off, and enlarges a gradient's rounding (1e-6) up to 485-fold: 1e-3 in all.
+    # A step changes a score by less than 1, of which 5e-4 are as far as the log probabilities are off.
+    g = torch.Generator(device="cuda").manual_seed(7)
+    normal = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    w = [normal(o, i) * (2.0 / i) ** 0.5 for i, o in zip(dims[:-1], dims[1:])]
+    b = [0.1 * normal(o) for o in dims[1:]]
+    lr, mu, bias_lr, weight = 0.01, 0.9, 0.1, 0.05
+    head = DenseHead(B.F32, rows[0], dims, lr=lr, mu=mu, bias_lr=bias_lr)
+    head.load(w, b)
+    first = [a.double() for a in w]
+    w, b = [a.double() for a in w], [a.double() for a in b]
+    mom = [torch.zeros_like(a) for a in w]
+    for n in rows:
+        x, y = normal(n, dims[0]).clamp_min(0), torch.randint(0, dims[-1], (n,), generator=g, device="cuda", dtype=torch.int32)
+        logp = head.train_step(x, y, weight)
+        acts = [x.double()]
+        for l in range(len(w)):
+            z = acts[-1] @ w[l].t().contiguous() + b[l]
+            acts.append(z.clamp_min(0) if l + 1 < len(w) else z)
+        lp = torch.log_softmax(acts[-1], 1)
+        p = lp.exp()
+        dz = p / n + weight / n * p * (lp - (p * lp).sum(1, keepdim=True))
+        dz[torch.arange(n, device="cuda"), y.long()] -= 1.0 / n
+        assert float((logp.double() - lp.gather(1, y.long()[:, None])[:, 0]).abs().max()) < 5e-4
+        for l in reversed(range(len(w))):
+            gw, gb = dz.t().contiguous() @ acts[l], dz.sum(0)
+            if l:
+                dz = (dz @ w[l]) * (acts[l] > 0)
+            mom[l] = mu * mom[l] + gw
+            w[l] = w[l] - lr * max(1.0, w[l].shape[0] / w[l].shape[1]) ** 0.5 * ns_gpu(gw + mu * mom[l])
+            b[l] = b[l] - bias_lr * gb
+    for mine, ref, was in zip(head.w, w, first):
+        assert float((mine.double() - ref).norm() / (ref - was).norm()) < 1e-3
+
+
+@pytest.mark.parametrize("N,n,dims", [(513, 512, [128, 10000]), (257, 256, [168, 10755])])
+def test_a_batch_that_needs_more_workspace_than_the_largest(N, n, dims):
+    head = DenseHead(B.BF16, N, dims)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    w = (torch.randn((dims[1], dims[0]), generator=g, device="cuda") * 0.1).to(torch.bfloat16)
+    head.load([w.float()], [torch.zeros(dims[1], device="cuda")])
+    x = torch.randn((n, dims[0]), generator=g, device="cuda").to(torch.bfloat16)
+    y = torch.randint(0, dims[1], (n,), generator=g, device="cuda", dtype=torch.int32)
+    logp = head.train_step(x, y)
+    want = torch.log_softmax(x.double() @ w.double().t().contiguous(), 1)
+    assert float((logp.double() - want.gather(1, y.long()[:, None])[:, 0]).abs().max()) < 1e-4
