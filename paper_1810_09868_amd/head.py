@@ -46,6 +46,8 @@ class DenseHead:
             raise RuntimeError("DenseHead needs a GPU: the HIP library is the only implementation")
         if len(dims) < 2 or N < 1:
             raise ValueError("a head has at least one layer and one row")
+        if dtype not in (B.F32, B.BF16) or group not in (32, 64, 128) or not 0 <= top <= B.MAX_TOP:
+            raise ValueError("dtype is F32 or BF16, group 32, 64 or 128, top 0 to %d" % B.MAX_TOP)
         if dtype == B.BF16 and any(d % 8 for d in dims[:-1]):
             raise ValueError("bf16: layer inputs are multiples of 8 (vgg_fc_bwd)")
         self.dtype, self.N, self.dims, self.group, self.top = dtype, N, list(dims), group, min(top, dims[-1])
@@ -68,6 +70,8 @@ class DenseHead:
 
     def load(self, weights: Sequence[torch.Tensor], biases: Sequence[torch.Tensor]) -> None:
         """Takes fp32 parameters; momentum starts from zero, and 4-bit weights of earlier ones are dropped."""
+        if [tuple(t.shape) for t in weights] != [tuple(w.shape) for w in self.w] or [tuple(t.shape) for t in biases] != [tuple(b.shape) for b in self.b]:
+            raise ValueError("a weight [out][in] and a bias [out] for each layer of %s" % self.dims)
         for mine, given in zip(self.w + self.b, list(weights) + list(biases)):
             mine.copy_(given)
         for m in self.momentum:
@@ -80,10 +84,14 @@ class DenseHead:
             for w, c in zip(self.w, self.operand):
                 B.vgg_convert(B.F32, B.BF16, w.numel(), w, c)
 
-    def _rows(self, x: torch.Tensor) -> int:
+    def _rows(self, x: torch.Tensor, labels: Optional[torch.Tensor]) -> int:
+        """The number of rows of a call, whose tensors are what the kernels take them for."""
+        td = torch.bfloat16 if self.dtype == B.BF16 else torch.float32
+        if x.dim() != 2 or not 1 <= x.shape[0] <= self.N or x.shape[1] != self.dims[0] or x.dtype != td or x.device != self.ws.device or not x.is_contiguous():
+            raise ValueError("features are contiguous [1..%d][%d], %s on %s" % (self.N, self.dims[0], td, self.ws.device))
         n = x.shape[0]
-        if not 1 <= n <= self.N or x.shape[1] != self.dims[0] or not x.is_contiguous():
-            raise ValueError("features are contiguous [1..%d][%d]" % (self.N, self.dims[0]))
+        if labels is not None and (labels.shape != (n,) or labels.dtype != torch.int32 or labels.device != x.device or not labels.is_contiguous()):
+            raise ValueError("labels are contiguous [%d], int32 on %s" % (n, x.device))
         return n
 
     def _forward(self, x: torch.Tensor, n: int) -> None:
@@ -98,7 +106,9 @@ class DenseHead:
         """One step on features x [n][dims[0]] and int32 labels: the mean of -log p[label] - entropy_weight * entropy is
         decreased; every weight matrix takes an orthogonalised step, biases a plain one.  Returns the rows' log probabilities
         before the step (a view)."""
-        n, K = self._rows(x), self.dims[-1]
+        if labels is None:
+            raise ValueError("a training step needs labels")
+        n, K = self._rows(x, labels), self.dims[-1]
         self._forward(x, n)
         B.vgg_log_probs(B.F32, n, K, self.logits, labels, 0, self.logp, self.entropy, None, None, self.stats, self.ws)
         up = torch.full((2, n + -n % 4), -1.0 / n, device="cuda")
@@ -131,7 +141,7 @@ class DenseHead:
 
     def answer(self, x: torch.Tensor, labels: Optional[torch.Tensor] = None) -> Answer:
         """Log probabilities of the given labels, entropy and the most likely classes of features x [n][dims[0]]."""
-        n, last, a = self._rows(x), len(self.w) - 1, x
+        n, last, a = self._rows(x, labels), len(self.w) - 1, x
         if not self.codes:
             self._forward(x, n)
         else:

@@ -179,3 +179,27 @@ def test_a_batch_that_needs_more_workspace_than_the_largest(N, n, dims):
     logp = head.train_step(x, y)
     want = torch.log_softmax(x.double() @ w.double().t().contiguous(), 1)
     assert float((logp.double() - want.gather(1, y.long()[:, None])[:, 0]).abs().max()) < 1e-4
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+def test_tensors_that_the_kernels_would_misread_are_refused(dtype):
+    head = DenseHead(dtype, 8, [16, 8, 3])
+    td, other = (torch.float32, torch.bfloat16) if dtype == B.F32 else (torch.bfloat16, torch.float32)
+    x, y = torch.zeros((4, 16), dtype=td, device="cuda"), torch.zeros((4,), dtype=torch.int32, device="cuda")
+    wrong_x = [x.to(other), x.cpu(), x[0], x[:, :15], x.t().contiguous().t(), torch.zeros((9, 16), dtype=td, device="cuda"), x[:0], x.double()]
+    wrong_y = [y.long(), y.cpu(), y[:3], y[:, None], torch.zeros((8,), dtype=torch.int32, device="cuda")[::2], y.float()]
+    for a, b in [(a, y) for a in wrong_x] + [(x, b) for b in wrong_y]:
+        for call in (head.train_step, head.answer):
+            with pytest.raises(ValueError):
+                call(a, b)
+    with pytest.raises(ValueError):
+        head.train_step(x, None)
+    w, b = [torch.zeros((8, 16)), torch.zeros((3, 8))], [torch.zeros(8), torch.zeros(3)]
+    for ws, bs in ((w[:1], b), (w, b[:1]), ([w[0], torch.zeros((1, 8))], b), (w, [b[0], torch.zeros(1)])):
+        with pytest.raises(ValueError):
+            head.load(ws, bs)
+    head.load(w, b)
+    for bad in (dict(dtype=5), dict(group=16), dict(top=65), dict(top=-1)):
+        with pytest.raises(ValueError):
+            DenseHead(**{**dict(dtype=dtype, N=4, dims=[8, 3]), **bad})
+    assert head.answer(x, y).logp.shape == (4,) and head.train_step(x, y).shape == (4,)
