@@ -25,7 +25,10 @@
  *    operation.  It is serialised inside the library, so entry points may be
  *    called from several host threads; but run every call once before
  *    recording it into a HIP graph.
- *  - Tensor pointers must be 16-byte aligned (VGG_ERR_ALIGN otherwise).
+ *  - Tensor pointers must be 16-byte aligned (VGG_ERR_ALIGN otherwise), but
+ *    for what is given one number to a row, of which a part of a longer
+ *    sequence may be passed: labels, and the gradients that
+ *    vgg_log_probs_bwd takes (4 bytes).
  *  - dtype: VGG_F32 = activations and weights fp32, fp32 MFMA.
  *           VGG_BF16 = activations and weights bf16 (round-to-nearest-even
  *           from fp32), fp32 MFMA accumulation, bias and logits fp32.

@@ -878,7 +878,7 @@ int vgg_log_probs(int dtype, int N, int K, size_t ldz, const void *z, const int3
     if (!z || !labels != !logp || (top > 0) != !!top_logp || (top > 0) != !!top_idx || (!logp && !entropy && !top_logp && !stats)) return VGG_ERR_NULL;
     if (!dtype_ok(dtype)) return VGG_ERR_DTYPE;
     if (!scores_shape_ok(N, K, ldz) || top < 0 || top > VGG_MAX_TOP || top > K) return VGG_ERR_SHAPE;
-    if (!aligned16(z) || !aligned16(labels) || !aligned16(logp) || !aligned16(entropy) || !aligned16(top_logp) || !aligned16(top_idx) || !aligned16(stats) || !aligned16(ws))
+    if (!aligned16(z) || !aligned4(labels) || !aligned16(logp) || !aligned16(entropy) || !aligned16(top_logp) || !aligned16(top_idx) || !aligned16(stats) || !aligned16(ws))
         return VGG_ERR_ALIGN;
     const size_t need = log_probs_workspace(N, K, top);
     if (need && (!ws || ws_bytes < need)) return VGG_ERR_WORKSPACE;
@@ -891,7 +891,7 @@ int vgg_log_probs_bwd(int dtype, int N, int K, size_t ldz, const void *z, const 
     if (!z || !stats || !dz || (!g_logp && !g_entropy) || (g_logp && !labels) || (g_entropy && !entropy)) return VGG_ERR_NULL;
     if (!dtype_ok(dtype)) return VGG_ERR_DTYPE;
     if (!scores_shape_ok(N, K, ldz) || lddz < (size_t)K || (z == dz && ldz != lddz)) return VGG_ERR_SHAPE;
-    if (!aligned16(z) || !aligned16(labels) || !aligned16(stats) || !aligned16(entropy) || !aligned16(g_logp) || !aligned16(g_entropy) || !aligned16(dz))
+    if (!aligned16(z) || !aligned4(labels) || !aligned16(stats) || !aligned16(entropy) || !aligned4(g_logp) || !aligned4(g_entropy) || !aligned16(dz))
         return VGG_ERR_ALIGN;
     return log_probs_bwd(dtype, N, K, ldz, z, labels, stats, entropy, g_logp, g_entropy, dz, lddz, (hipStream_t)stream);
 }

@@ -17,6 +17,7 @@ constexpr int kWave = 64;  // CDNA wavefront width
 
 __host__ __device__ constexpr inline int round_up16(int v) { return (v + 15) & ~15; }
 inline bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+inline bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 inline int dtype_size(int dtype) { return dtype == VGG_BF16 ? 2 : 4; }
 inline bool dtype_ok(int dtype) { return dtype == VGG_F32 || dtype == VGG_BF16; }

@@ -63,6 +63,7 @@ class DenseHead:
         self.logits, self.dz = f32(N, dims[-1]), [f32(N, o) for _, o in pairs]
         self.dw, self.db = [f32(o, i) for i, o in pairs], [f32(o) for _, o in pairs]
         self.logp, self.entropy, self.stats = f32(N), f32(N), f32(N, 2)
+        self.g_logp, self.g_entropy = f32(N), f32(N)
         self.top_logp, self.top_idx = f32(N, self.top), torch.zeros((N, self.top), dtype=torch.int32, device="cuda")
         self.codes: List[torch.Tensor] = []
         self.scales: List[torch.Tensor] = []
@@ -111,9 +112,9 @@ class DenseHead:
         n, K = self._rows(x, labels), self.dims[-1]
         self._forward(x, n)
         B.vgg_log_probs(B.F32, n, K, self.logits, labels, 0, self.logp, self.entropy, None, None, self.stats, self.ws)
-        up = torch.full((2, n + -n % 4), -1.0 / n, device="cuda")
-        up[1] *= entropy_weight
-        B.vgg_log_probs_bwd(B.F32, n, K, self.logits, labels, self.stats, self.entropy, up[0], up[1] if entropy_weight else None,
+        self.g_logp[:n].fill_(-1.0 / n)
+        self.g_entropy[:n].fill_(-entropy_weight / n)
+        B.vgg_log_probs_bwd(B.F32, n, K, self.logits, labels, self.stats, self.entropy, self.g_logp, self.g_entropy if entropy_weight else None,
                             self.dz[-1])
         for l in reversed(range(len(self.w))):
             o, i = self.w[l].shape

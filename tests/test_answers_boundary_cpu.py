@@ -61,3 +61,10 @@ def test_sizes_past_what_a_launch_holds_are_refused_on_the_host():
     assert w4((1 << 23) + 1, 1, 1) == w4(1, 1, (1 << 25) + 1) == w4(1 << 22, 1, 1 << 12) == w4(1 << 22, 1 << 12, 1) == -2
     assert L.vgg_fc_w4_quantize(1, (1 << 25) + 1, 32, A, A, A, None) == L.vgg_fc_w4_dequantize(1 << 22, 1 << 12, 32, A, A, A, None) == -2
     assert B.vgg_fc_w4_workspace_bytes(B.F32, (1 << 23) + 1, 64, 64, 32) == 0 < B.vgg_fc_w4_workspace_bytes(B.F32, 1 << 23, 64, 64, 32)
+
+
+def test_a_part_of_a_longer_sequence_of_labels_is_taken():
+    # (the workspace is looked at after the alignment: nothing is launched)
+    L = B.lib()
+    call = lambda y: L.vgg_log_probs(0, 1, 200003, 200003, A, y, 0, A, A, None, None, A, None, 0, None)  # noqa: E731
+    assert call(A + 4) == call(A + 200) == -5 and call(A + 2) == -4

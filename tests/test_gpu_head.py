@@ -203,3 +203,18 @@ def test_tensors_that_the_kernels_would_misread_are_refused(dtype):
         with pytest.raises(ValueError):
             DenseHead(**{**dict(dtype=dtype, N=4, dims=[8, 3]), **bad})
     assert head.answer(x, y).logp.shape == (4,) and head.train_step(x, y).shape == (4,)
+
+
+def test_minibatches_are_parts_of_longer_tensors():
+    x = torch.randn((100, 16), device="cuda")
+    y = torch.randint(0, 3, (100,), dtype=torch.int32, device="cuda")
+    w, b = [torch.randn((8, 16)), torch.randn((3, 8))], [torch.randn(8), torch.randn(3)]
+    got = []
+    for copy in (False, True):
+        head = DenseHead(B.F32, 50, [16, 8, 3])
+        head.load(w, b)
+        for first, last in ((0, 50), (50, 99), (1, 4), (99, 100)):
+            part = y[first:last].clone() if copy else y[first:last]
+            head.train_step(x[first:last], part, 0.1)
+        got.append([t.clone() for t in head.w] + [head.answer(x[50:100], y[50:100].clone() if copy else y[50:100]).logp.clone()])
+    assert all(torch.equal(a, b) for a, b in zip(*got))

@@ -354,3 +354,16 @@ def test_exponentials_far_below_the_largest_score_are_exact_to_their_last_bits()
     E = 3 * np.exp(d.astype(np.float64))
     for got, want, units in ((c.logp, -np.log1p(E), 5), (c.entropy, np.log1p(E) - d * E / (1 + E), 7)):
         assert np.abs(got.double().cpu().numpy() / want - 1).max() <= units * 2.0 ** -23
+
+
+def test_labels_and_upstream_gradients_may_begin_anywhere():
+    z, _ = scores(B.F32, 37, 300, 6)
+    many, up = torch.randint(0, 300, (64,), dtype=torch.int32, device="cuda"), torch.randn(64, device="cuda")
+    for first in (1, 2, 3, 5):
+        labels = many[first : first + 37]
+        c = Call(B.F32, z, labels.cpu().numpy(), 0).run()
+        want = c.grad(up[first : first + 37].cpu().numpy(), up[first + 1 : first + 38].cpu().numpy()).clone()
+        logp, dz = torch.zeros(37, device="cuda"), torch.zeros((37, 300), device="cuda")
+        B.vgg_log_probs(B.F32, 37, 300, c.z, labels, 0, logp, c.entropy, None, None, c.stats)
+        B.vgg_log_probs_bwd(B.F32, 37, 300, c.z, labels, c.stats, c.entropy, up[first : first + 37], up[first + 1 : first + 38], dz)
+        assert torch.equal(logp, c.logp) and torch.equal(dz, want)
