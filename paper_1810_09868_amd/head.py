@@ -28,7 +28,7 @@ def _bytes(n: int) -> torch.Tensor:
 def workspace_bytes(dtype: int, N: int, dims: Sequence[int], group: int, top: int) -> int:
     """What the calls of a head of these layers need at most, over every number of rows up to N: fewer rows may need more, since
     they are cut into more parts."""
-    need = [B.vgg_muon_workspace_bytes(dtype, 1, o, i) for i, o in zip(dims[:-1], dims[1:])]
+    need = [B.vgg_muon_workspace_bytes(d, 1, o, i) for d in (B.F32, B.BF16) for i, o in zip(dims[:-1], dims[1:])]
     for n in range(1, N + 1):
         need += [B.vgg_log_probs_workspace_bytes(B.F32, n, dims[-1], t) for t in (0, top)]
         for i, o in zip(dims[:-1], dims[1:]):
@@ -38,19 +38,21 @@ def workspace_bytes(dtype: int, N: int, dims: Sequence[int], group: int, top: in
 
 
 class DenseHead:
-    """`dims` are the layers' widths, features first and classes last; at most N rows a call."""
+    """`dims` are the layers' widths, features first and classes last; at most N rows a call.  `update_dtype`: how exact the
+    products of the updates are (vgg_muon_update; BF16: operands of 11 bits), whatever `dtype` the layers have."""
 
     def __init__(self, dtype: int, N: int, dims: Sequence[int], lr: float = 0.02, mu: float = 0.95, weight_decay: float = 0.0,
-                 bias_lr: float = 0.01, ns_steps: int = 5, group: int = 64, top: int = 5):
+                 bias_lr: float = 0.01, ns_steps: int = 5, group: int = 64, top: int = 5, update_dtype: int = B.F32):
         if not torch.cuda.is_available():
             raise RuntimeError("DenseHead needs a GPU: the HIP library is the only implementation")
         if len(dims) < 2 or N < 1:
             raise ValueError("a head has at least one layer and one row")
-        if dtype not in (B.F32, B.BF16) or group not in (32, 64, 128) or not 0 <= top <= B.MAX_TOP:
-            raise ValueError("dtype is F32 or BF16, group 32, 64 or 128, top 0 to %d" % B.MAX_TOP)
+        if dtype not in (B.F32, B.BF16) or update_dtype not in (B.F32, B.BF16) or group not in (32, 64, 128) or not 0 <= top <= B.MAX_TOP:
+            raise ValueError("dtypes are F32 or BF16, group 32, 64 or 128, top 0 to %d" % B.MAX_TOP)
         if dtype == B.BF16 and any(d % 8 for d in dims[:-1]):
             raise ValueError("bf16: layer inputs are multiples of 8 (vgg_fc_bwd)")
         self.dtype, self.N, self.dims, self.group, self.top = dtype, N, list(dims), group, min(top, dims[-1])
+        self.update_dtype = update_dtype
         self.lr, self.mu, self.weight_decay, self.bias_lr, self.ns_steps = lr, mu, weight_decay, bias_lr, ns_steps
         td = torch.bfloat16 if dtype == B.BF16 else torch.float32
         f32 = lambda *s: torch.zeros(s, device="cuda")  # noqa: E731
@@ -121,7 +123,7 @@ class DenseHead:
             B.vgg_fc_bwd(self.dtype, n, i, o, self.act[l - 1] if l else x, self.operand[l], self.dz[l], self.dw[l], self.db[l],
                          self.dz[l - 1] if l else None, l > 0, self.ws)
         for l, w in enumerate(self.w):
-            B.vgg_muon_update(self.dtype, 1, *w.shape, self.ns_steps, w, self.dw[l], self.momentum[l], self.lr, self.mu, True,
+            B.vgg_muon_update(self.update_dtype, 1, *w.shape, self.ns_steps, w, self.dw[l], self.momentum[l], self.lr, self.mu, True,
                               self.weight_decay, self.ws)
             B.vgg_sgd_update(self.b[l].numel(), self.b[l], self.db[l], self.bias_lr)
         self.codes, self.scales = [], []

@@ -218,3 +218,21 @@ def test_minibatches_are_parts_of_longer_tensors():
             head.train_step(x[first:last], part, 0.1)
         got.append([t.clone() for t in head.w] + [head.answer(x[50:100], y[50:100].clone() if copy else y[50:100]).logp.clone()])
     assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("update_dtype", [None, B.BF16])
+def test_weights_meet_exact_updates_unless_short_operands_are_asked_for(update_dtype):
+    g = torch.Generator(device="cuda").manual_seed(3)
+    kw = {} if update_dtype is None else dict(update_dtype=update_dtype)
+    head = DenseHead(B.BF16, 96, [256, 200, 120], lr=0.02, mu=0.9, weight_decay=0.01, **kw)
+    head.load([torch.randn((o, i), generator=g, device="cuda") * (2.0 / i) ** 0.5 for i, o in ((256, 200), (200, 120))],
+              [torch.zeros(200, device="cuda"), torch.zeros(120, device="cuda")])
+    for _ in range(2):
+        w, mom = [t.clone() for t in head.w], [t.clone() for t in head.momentum]
+        x, y = torch.randn((96, 256), generator=g, device="cuda").to(torch.bfloat16), torch.randint(0, 120, (96,), device="cuda", dtype=torch.int32)
+        head.train_step(x, y)
+        for l, (theta, m) in enumerate(zip(w, mom)):
+            shape, dt = (1, *theta.shape), B.F32 if update_dtype is None else update_dtype
+            ws = torch.empty(B.vgg_muon_workspace_bytes(dt, *shape), dtype=torch.uint8, device="cuda")
+            B.vgg_muon_update(dt, *shape, 5, theta, head.dw[l], m, 0.02, 0.9, True, 0.01, ws)
+            assert torch.equal(theta, head.w[l]) and torch.equal(m, head.momentum[l])
