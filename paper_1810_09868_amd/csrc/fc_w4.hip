@@ -3,6 +3,7 @@
 // A code is a sign and one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (E2M1); a weight is its value times the bf16 scale of its group of
 // consecutive inputs.  Codes lie two to a byte, the even input low, rows padded to 32 codes (16 bytes).
 #include "common.h"
+#include "plans.h"
 
 #include <type_traits>
 
@@ -607,39 +608,6 @@ int w4_dequantize(int In, int Out, int group, const uint8_t *codes, const bf16_t
 
 namespace {
 
-constexpr int kFewRows = 1;    // rows of a up to which the first kernel runs
-
-// ... and the second: its workgroups of 16 outputs read all of a each, in pieces scattered over its rows, so that long rows are
-// worth laying out first (25088 inputs, bf16: 5 rows 18.2 against 20.7 us, 10 rows 23.5 against 20.8; 4096 inputs, fp32, 16 rows:
-// 11.5 against 11.7).
-constexpr int kTileRows = 16;
-constexpr size_t kTileBytes = 300000;
-
-bool one_tile(int dtype, int N, int In) { return N <= kTileRows && (size_t)N * In * dtype_size(dtype) <= kTileBytes; }
-
-// Tiles of 64 outputs read the laid out activations least often, those of 16 begin and end soonest and need the fewest splits.  16
-// where all workgroups run at once, 32 else, as long as the activations' way out of L2 is no more than this many bytes in all (32
-// x 4096 x 4096, bf16: 8.3, 10.8, 12.1 us with 16, 32, 64; 100 x 4096 x 4096: 18.4, 14.6, 18.3; 64 x 25088 x 4096: 41.7, 32.7, 29.5).
-constexpr size_t kReadAgain = 160u << 20;
-
-struct W4Plan { int nt, rt, tiles, splits, row_tiles; size_t lay_bytes; };
-W4Plan tiles_plan(int dtype, int N, int In, int Out)
-{
-    W4Plan t;
-    t.nt = N <= 16 ? 1 : N <= 32 ? 2 : 4;
-    t.tiles = (N + 16 * t.nt - 1) / (16 * t.nt) * t.nt;
-    const int kb = (In + 127) / 128, most = (kb + 7) / 8;
-    t.lay_bytes = round_up((size_t)kb * t.tiles * 4 * (dtype == VGG_BF16 ? 1 : 3) * 1024, 256);
-    auto row_tiles = [&](int rt) { return (Out + 16 * rt - 1) / (16 * rt); };
-    auto few = [&](int rt) { return t.lay_bytes * row_tiles(rt) <= kReadAgain; };
-    t.rt = few(1) && (long)row_tiles(1) * (t.tiles / t.nt) <= 256 ? 1 : few(2) ? 2 : 4;
-    t.row_tiles = row_tiles(t.rt);
-    const long units = (long)t.row_tiles * (t.tiles / t.nt);
-    t.splits = (int)(units >= 256 ? 1 : (256 + units - 1) / units);
-    if (t.splits > most) t.splits = most;
-    return t;
-}
-
 template <typename T, int RT, int NT, int G>
 int launch_tiles_of(const T *a, W4Args p, const W4Plan &t, void *ws, hipStream_t s)
 {
@@ -694,9 +662,9 @@ int launch_rows(const T *a, const W4Args &p, hipStream_t s)
 template <typename T>
 int fc_w4_of(const T *a, const W4Args &p, void *ws, hipStream_t s)
 {
-    if (p.N <= kFewRows) return launch_rows(a, p, s);
-    if (one_tile(sizeof(T) == 2 ? VGG_BF16 : VGG_F32, p.N, p.In)) return p.shift == 5 ? launch_tile<T, 1>(a, p, s) : p.shift == 6 ? launch_tile<T, 2>(a, p, s) : launch_tile<T, 4>(a, p, s);
-    const W4Plan t = tiles_plan(sizeof(T) == 2 ? VGG_BF16 : VGG_F32, p.N, p.In, p.Out);
+    if (p.N <= kW4FewRows) return launch_rows(a, p, s);
+    if (w4_one_tile(sizeof(T) == 2 ? VGG_BF16 : VGG_F32, p.N, p.In)) return p.shift == 5 ? launch_tile<T, 1>(a, p, s) : p.shift == 6 ? launch_tile<T, 2>(a, p, s) : launch_tile<T, 4>(a, p, s);
+    const W4Plan t = w4_tiles_plan(sizeof(T) == 2 ? VGG_BF16 : VGG_F32, p.N, p.In, p.Out);
     return t.nt == 1 ? launch_tiles<T, 1>(a, p, t, ws, s) : t.nt == 2 ? launch_tiles<T, 2>(a, p, t, ws, s) : launch_tiles<T, 4>(a, p, t, ws, s);
 }
 
@@ -705,8 +673,8 @@ int fc_w4_of(const T *a, const W4Args &p, void *ws, hipStream_t s)
 size_t fc_w4_workspace(int dtype, int N, int In, int Out, int group)
 {
     (void)group;
-    if (N <= kFewRows || one_tile(dtype, N, In)) return 0;
-    const W4Plan t = tiles_plan(dtype, N, In, Out);
+    if (N <= kW4FewRows || w4_one_tile(dtype, N, In)) return 0;
+    const W4Plan t = w4_tiles_plan(dtype, N, In, Out);
     return t.lay_bytes + (t.splits > 1 ? round_up((size_t)t.splits * N * Out * 4, 256) : 0);
 }
 

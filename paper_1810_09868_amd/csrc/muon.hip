@@ -21,6 +21,7 @@
 // formed, over a few ranges of the contraction where they are too few to fill the chip, and a second kernel adds the ranges in
 // order and mirrors them (in the product kernel's own end, where there is one range: no faster).
 #include "common.h"
+#include "plans.h"
 
 #include <type_traits>
 
@@ -995,8 +996,6 @@ Wide wide_plan(int planes, int batch, int rows, int cols)
     return w;
 }
 
-inline int round_to(int v, int to) { return (v + to - 1) / to * to; }
-
 // How many ranges a contraction of `all` stages is cut into for `tiles` workgroups each: rounds of the chip's 256 compute units
 // times what one takes, in cycles (a stage at the matrix unit's rate, some thousand to begin and end), and the sums' way through
 // memory.
@@ -1017,11 +1016,7 @@ Layout layout_of(int planes, int batch, int rows, int cols, char *ws, size_t &to
     Layout L;
     L.rows = rows; L.cols = cols; L.tall = rows > cols; L.batch = batch;
     L.m = L.tall ? cols : rows; L.n = L.tall ? rows : cols;
-    // 256 x 256 tiles where the product with X takes no more of the chip's rounds with them (a tile is four times the work of a
-    // 128 x 128 one, in about 3.4 times its time), and the contraction over m is long beside what a tile begins and ends with
-    // (7 x 512 x 4608, bf16: 468 us with them, 427 us without; 4096 x 4096: 1.63 ms, 2.02 ms)
-    auto rounds = [&](int t) { return ((long)batch * (round_to(L.m, t) / t) * (round_to(L.n, t) / t) + 255) / 256; };
-    L.tile = L.m >= 1024 && 3.4 * rounds(256) <= rounds(128) ? 256 : 128;
+    L.tile = muon_tile(batch, L.m, L.n);
     L.mp = round_to(L.m, L.tile); L.np = round_to(L.n, L.tile);
     const int mt = L.mp / L.tile;
     const long tiles = (long)batch * (mt * (mt + 1) / 2);
