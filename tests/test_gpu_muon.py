@@ -7,6 +7,7 @@ import torch
 from paper_1810_09868_amd import binding as B
 
 from gpu_util import TDT, ws_bytes
+from plan_shapes import MUON_256
 
 pytestmark = pytest.mark.gpu
 
@@ -236,3 +237,60 @@ def test_matrices_whose_norm_is_small_beside_the_added_constant(dtype, scale, sh
     B.vgg_muon_update(dtype, 1, *shape, 5, theta, g, mom, 1.0, 0.9, False, 0.0, ws_bytes(B.vgg_muon_workspace_bytes(dtype, 1, *shape)))
     want = -np.sqrt(max(1, shape[0] / shape[1])) * ns64(x[0].double().numpy(), 5)
     assert off(theta[0].double().cpu().numpy(), want) <= bound(dtype)
+
+
+def on_gpu(dtype, shape, seed):
+    """matrices(), drawn on the GPU."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    normal = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    x = torch.stack([0.05 * normal(*shape[1:]) + normal(shape[1], 4) @ normal(4, shape[2]).abs() for _ in range(shape[0])])
+    return x.to(TDT[dtype])
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("shape", MUON_256)
+def test_orthogonalize_by_the_largest_tiles(dtype, shape):
+    x = on_gpu(dtype, shape, 5)
+    y = torch.full_like(x, float("nan"))
+    ws = ws_bytes(B.vgg_orthogonalize_workspace_bytes(dtype, *shape))
+    ws.fill_(0xFF)
+    B.vgg_orthogonalize(dtype, *shape, 5, x, y, ws)
+    for b in range(shape[0]):
+        want = ns64_gpu(x[b].double(), 5)
+        assert float((y[b].double() - want).norm() / want.norm()) <= bound(dtype)
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("shape", MUON_256[1:])
+def test_update_by_the_largest_tiles(dtype, shape):
+    lr, mu, decay = 0.05, 0.9, 0.1
+    theta, m = (torch.randn(shape, generator=torch.Generator(device="cuda").manual_seed(k), device="cuda") for k in (1, 2))
+    ws = ws_bytes(B.vgg_muon_workspace_bytes(dtype, *shape))
+    want_t, want_m = theta.double(), m.double()
+    for k in range(2):
+        g = on_gpu(B.F32, shape, 10 + k)
+        ws.fill_(0xFF)
+        B.vgg_muon_update(dtype, *shape, 5, theta, g, m, lr, mu, True, decay, ws)
+        want_m = mu * want_m + g.double()
+        o = torch.stack([ns64_gpu(u, 5) for u in g.double() + mu * want_m])
+        want_t = (1 - lr * decay) * want_t - lr * max(1.0, shape[1] / shape[2]) ** 0.5 * o
+    assert float((m.double() - want_m).norm() / want_m.norm()) < 3e-7
+    allow = 2 * lr * max(1.0, shape[1] / shape[2]) ** 0.5 * bound(dtype) * float(o.norm()) + 1e-6 * float(want_t.norm())
+    assert float((theta.double() - want_t).norm()) <= allow
+
+
+def test_matrices_of_the_largest_tiles_do_not_meet():
+    shape = (4, 1270, 2500)
+    x = on_gpu(B.BF16, shape, 3)
+    x[1] = 0
+    x[2, 700, 2400] = float("nan")
+    alone = torch.empty_like(x)
+    ws = ws_bytes(B.vgg_orthogonalize_workspace_bytes(B.BF16, *shape))
+    B.vgg_orthogonalize(B.BF16, *shape, 5, x, alone, ws)
+    again = x.clone()
+    B.vgg_orthogonalize(B.BF16, *shape, 5, again, again, ws)
+    assert not alone[1].any() and alone[2].isnan().all()
+    for b in (0, 3):
+        assert torch.equal(alone[b], again[b])
+        want = ns64_gpu(x[b].double(), 5)
+        assert float((alone[b].double() - want).norm() / want.norm()) <= bound(B.BF16)
