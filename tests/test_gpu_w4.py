@@ -7,6 +7,7 @@ import torch
 from paper_1810_09868_amd import binding as B
 
 from gpu_util import TDT, ws_bytes
+from plan_shapes import W4_TILES
 
 pytestmark = pytest.mark.gpu
 
@@ -218,3 +219,27 @@ def test_product_in_a_graph_and_on_another_stream():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(z, y), k
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("shape", list(W4_TILES))
+def test_product_by_every_tile_of_rows_and_outputs(shape, group):
+    dtype, N, In, Out = shape
+    g = torch.Generator(device="cuda").manual_seed(N + In)
+    codes = torch.randint(0, 256, (Out, -(-In // 32) * 16), generator=g, device="cuda", dtype=torch.uint8)
+    scales = (torch.rand((Out, -(-In // group)), generator=g, device="cuda") * 0.02 + 1e-3).to(torch.bfloat16)
+    a = torch.randn((N, In), generator=g, device="cuda").to(TDT[dtype])
+    b = torch.randn((Out,), generator=g, device="cuda")
+    relu, zdt = group == 64, dtype if group == 32 else B.F32
+    z = torch.full((N, Out), float("nan"), dtype=TDT[zdt], device="cuda")
+    ws = ws_bytes(B.vgg_fc_w4_workspace_bytes(dtype, N, In, Out, group))
+    ws.fill_(0xFF)
+    B.vgg_fc_w4(dtype, N, In, Out, group, a, codes, scales, b, z, zdt, relu, ws)
+    table, a64 = torch.from_numpy(np.concatenate((GRID, -GRID))).cuda(), a.double()
+    for o in range(0, Out, 512):                                       # (the weights in 64 bits, some outputs at a time)
+        c = codes[o : o + 512]
+        w = table[torch.stack((c & 15, c >> 4), 2).flatten(1)[:, :In].int()]
+        w *= scales[o : o + 512].double().repeat_interleave(group, 1)[:, :In]
+        wt = w.t().contiguous()
+        want, size = a64 @ wt + b[o : o + 512].double(), a64.abs() @ wt.abs() + b[o : o + 512].double().abs()
+        check(z[:, o : o + 512].double(), want.clamp_min(0) if relu else want, size, zdt)
