@@ -332,14 +332,19 @@ __global__ __launch_bounds__(256, 2) void conv_pair_kernel(PairArgs p)
 #pragma unroll
                     for (int a = 0; a < 4; ++a) {
                         float m[4];
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            // max(row 0, row 1, 0), then the maximum with the neighbouring lane's: two instructions
-                            // (fmaxf would first quieten signalling NaNs, one more instruction per operand)
-                            float v;
-                            asm("v_max3_f32 %0, %1, %2, 0" : "=v"(v) : "v"(acc[pair * 2][j][a * 4 + k]), "v"(acc[pair * 2 + 1][j][a * 4 + k]));
-                            asm("v_max_f32_dpp %0, %1, %1 quad_perm:[1,0,3,2] row_mask:0xf bank_mask:0xf" : "=&v"(m[k]) : "v"(v));
-                        }
+                        // max(row 0, row 1, 0), then the maximum with the neighbouring lane's: two instructions a value (fmaxf would first
+                        // quieten signalling NaNs, one more instruction per operand).  All four values in one piece of assembly: three
+                        // instructions between a value's two, where a DPP read has to come two wait states after the write and the compiler
+                        // does not see to it between pieces.
+                        const f32x16 &q0 = acc[pair * 2][j], &q1 = acc[pair * 2 + 1][j];
+                        asm("v_max3_f32 %0, %4, %8, 0\n\tv_max3_f32 %1, %5, %9, 0\n\tv_max3_f32 %2, %6, %10, 0\n\tv_max3_f32 %3, %7, %11, 0\n\t"
+                            "v_max_f32_dpp %0, %0, %0 quad_perm:[1,0,3,2] row_mask:0xf bank_mask:0xf\n\t"
+                            "v_max_f32_dpp %1, %1, %1 quad_perm:[1,0,3,2] row_mask:0xf bank_mask:0xf\n\t"
+                            "v_max_f32_dpp %2, %2, %2 quad_perm:[1,0,3,2] row_mask:0xf bank_mask:0xf\n\t"
+                            "v_max_f32_dpp %3, %3, %3 quad_perm:[1,0,3,2] row_mask:0xf bank_mask:0xf"
+                            : "=&v"(m[0]), "=&v"(m[1]), "=&v"(m[2]), "=&v"(m[3])
+                            : "v"(q0[a * 4]), "v"(q0[a * 4 + 1]), "v"(q0[a * 4 + 2]), "v"(q0[a * 4 + 3]), "v"(q1[a * 4]), "v"(q1[a * 4 + 1]),
+                              "v"(q1[a * 4 + 2]), "v"(q1[a * 4 + 3]));
                         // (both lanes of a pair hold the result; the even one stores it: pooled pixel r / 2)
                         if ((r & 1) == 0)
                             store4(reinterpret_cast<T *>(stage + (r >> 1) * kStageRow) + j * 32 + a * 8 + khalf * 4, m[0], m[1], m[2], m[3]);
