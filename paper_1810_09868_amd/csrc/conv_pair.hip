@@ -237,7 +237,7 @@ __global__ __launch_bounds__(256, 2) void conv_pair_kernel(PairArgs p)
                     typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
                     float rl[4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) asm("v_max_f32 %0, %1, 0" : "=v"(rl[k]) : "v"(a1[j][a * 4 + k]));   // (fmaxf: one more instruction)
+                    for (int k = 0; k < 4; ++k) rl[k] = __builtin_amdgcn_fmed3f(a1[j][a * 4 + k], 0.f, INFINITY);   // (fmaxf: one more instruction)
                     const f32x2_t v0 = {rl[0], rl[1]};
                     const f32x2_t v1 = {rl[2], rl[3]};
                     u32x2 w2v = {__builtin_bit_cast(unsigned int, __builtin_convertvector(v0, bf16x2_t)),

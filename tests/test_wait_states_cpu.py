@@ -2,7 +2,8 @@
 them for its own instructions, not within and around inline assembly.
 
 A copy from memory to LDS takes its LDS address from m0, which a scalar instruction must have written one wait state earlier at
-least; a DPP instruction reads another lane's register that a vector instruction must have written two earlier."""
+least; a DPP instruction reads another lane's register that a vector instruction must have written two earlier; a result of the
+matrix unit may be read by other vector instructions as many wait states later as its instruction has passes, and four more."""
 import glob
 import os
 import re
@@ -76,6 +77,39 @@ def test_the_check_of_dpp_itself():
     assert dpp_too_early(at % "\ts_nop 1\n") == dpp_too_early(at % "\tv_mov_b32 v9, 0\n\ts_nop 0\n") == (1, [])
 
 
+PASSES = {"v_mfma_f32_32x32x16_bf16": 8, "v_mfma_f32_32x32x16_f16": 8, "v_mfma_f32_16x16x32_bf16": 4, "v_mfma_f32_16x16x32_f16": 4}
+
+
+def results_too_early(listing):
+    """(vector instructions that read a result of the matrix unit within 16 wait states, those that do too early); what follows a
+    branch in the listing is not looked at together with what precedes it."""
+    count, bad, before = 0, [], []
+    for line in listing.splitlines():
+        inst = line.split("//")[0].strip()
+        op, _, args = inst.partition(" ")
+        if not inst or re.match(r"[0-9a-f]+ <", line) or op.startswith(("s_branch", "s_cbranch", "s_endpgm", "s_setpc")):
+            before = [] if inst else before
+            continue
+        to, _, sources = args.partition(",")
+        if op.startswith("v_") and not op.startswith("v_mfma"):
+            states, source = 0, registers(sources)
+            for earlier, written, passes in reversed(before):
+                if source & written:
+                    count += passes > 0
+                    if 0 < passes and states < passes + 4:
+                        bad.append(inst)
+                    break
+                states += int(earlier.split()[1], 0) + 1 if earlier.startswith("s_nop") else 1
+        before = before[-15:] + [(inst, registers(to) if op.startswith("v_") else set(), PASSES.get(op, 0))]
+    return count, bad
+
+
+def test_the_check_of_results_itself():
+    at = "\tv_mfma_f32_32x32x16_bf16 v[0:15], v[20:23], v[24:27], v[0:15]\n%s\tv_max_f32_e64 v30, v3, 0\n"
+    assert len(results_too_early(at % "\ts_nop 10\n")[1]) == 1 and results_too_early(at % "\ts_nop 11\n") == (1, [])
+    assert results_too_early(at % "\tv_mov_b32 v3, 0\n") == (0, []) == results_too_early(at % "\ts_cbranch_scc1 5\n")
+
+
 @pytest.fixture(scope="module")
 def listings(tmp_path_factory):
     lib = shutil.copy(B.LIB_PATH, tmp_path_factory.mktemp("code"))
@@ -94,3 +128,9 @@ def test_no_copy_to_lds_follows_the_write_of_its_address(listings):
 def test_no_lane_reads_another_lanes_register_too_early(listings):
     found = [dpp_too_early(listing) for listing in listings]
     assert sum(n for n, _ in found) > 100 and not sum((bad for _, bad in found), [])
+
+
+@pytest.mark.skipif(not os.path.exists(OBJDUMP), reason="llvm-objdump not available")
+def test_no_result_of_the_matrix_unit_is_read_too_early(listings):
+    found = [results_too_early(listing) for listing in listings]
+    assert sum(n for n, _ in found) > 1000 and not sum((bad for _, bad in found), [])
