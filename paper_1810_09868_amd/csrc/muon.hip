@@ -579,10 +579,6 @@ __global__ __launch_bounds__(256) void muon_symmetric_kernel(Layout L)
 // (32 columns w + 8 c to wave w), X^T's planes, G's and P's in LDS.  By columns, a lane's four consecutive rows of a result are one
 // LDS store; P X then reads columns of X as they lie, and G reads its rows transposed.  G and G G are 16 blocks of 16 x 16, two to
 // a wave; the sum (i, j) is stored as (j, i), the same by symmetry and four in a row again.
-constexpr int kFewRows = 64, kLds = 160 * 1024;
-constexpr int row_stride(int planes) { return 128 * planes + 16; }   // bytes of 64 elements; 16 more: rows start in different banks
-inline size_t few_lds(int planes, int blocks) { return (size_t)(blocks * 32 + 2 * kFewRows) * row_stride(planes) + 3 * 256; }
-
 template <typename T, int PL, int CB>
 struct FewRows {
     typedef half_t f16x4 __attribute__((ext_vector_type(4)));
@@ -969,25 +965,10 @@ __global__ __launch_bounds__(512) void muon_wide_kernel(Source src, Target out, 
     for (int q = 0; q < 2; ++q) share[at + (size_t)blockIdx.x * 1024 + q * 64] = w.acc[q];
 }
 
-// Column blocks of a wave in one workgroup, 0 where a matrix is too large: its planes' room in LDS, and at most 640 columns (64 x 576,
-// bf16: 38.7 us, and 42.3 in three workgroups and seven launches; 64 x 768: 44.4, and 42.5).
-int small_blocks(int planes, int rows, int cols)
-{
-    const int m = rows < cols ? rows : cols, n = rows < cols ? cols : rows, blocks = (n + 31) / 32, cb = (blocks + 7) / 8;
-    return m <= kFewRows && blocks <= 20 && few_lds(planes, blocks) <= kLds ? cb : 0;
-}
-// Matrices of few rows with more columns: 256 columns to a workgroup while that makes at most 16, whose shares each of them adds up,
-// else as many as LDS has room for, up to 512.
-struct Wide { int cb, each, wgs, parts; size_t part, x32, share, total; };
-bool is_wide(int rows, int cols) { return rows <= kFewRows || cols <= kFewRows; }
+struct Wide : FewPlan { int parts; size_t part, x32, share, total; };
 Wide wide_plan(int planes, int batch, int rows, int cols)
 {
-    Wide w;
-    const int blocks = ((rows < cols ? cols : rows) + 31) / 32;
-    w.cb = blocks <= 16 * 8 ? 1 : 2;
-    w.each = w.cb * 8;
-    while (few_lds(planes, w.each) > kLds) --w.each;
-    w.wgs = (blocks + w.each - 1) / w.each;
+    Wide w = {few_plan(planes, rows, cols)};
     w.parts = norm_parts((size_t)rows * cols, kNormLot<float>);
     w.part = round_up((size_t)batch * kParts * 8, 256);
     w.x32 = round_up((size_t)batch * w.wgs * w.cb * 8 * 2048 * 4, 256);
@@ -1077,7 +1058,7 @@ int run(int batch, int rows, int cols, int steps, const Source &src, const Targe
         hipLaunchKernelGGL(kern, dim3(batch), dim3(512), few_lds(PL, ((rows < cols ? cols : rows) + 31) / 32), s, src, out, rows, cols, steps);
         return launch_status();
     }
-    if (is_wide(rows, cols)) {
+    if (is_wide(PL, rows, cols)) {
         const Wide p = wide_plan(PL, batch, rows, cols);
         auto kern = p.cb == 1 ? muon_wide_kernel<T, PL, 1> : muon_wide_kernel<T, PL, 2>;
         if (!raise_lds_limit(reinterpret_cast<const void *>(kern))) return VGG_ERR_LAUNCH;
@@ -1106,7 +1087,7 @@ size_t muon_workspace(int batch, int rows, int cols)
     size_t most = 0;
     for (int planes = 1; planes <= 2; ++planes) {
         size_t total;
-        if (is_wide(rows, cols)) total = wide_plan(planes, batch, rows, cols).total;   // (one workgroup alone needs none)
+        if (is_wide(planes, rows, cols)) total = wide_plan(planes, batch, rows, cols).total;   // (one workgroup alone needs none)
         else layout_of(planes, batch, rows, cols, nullptr, total);
         if (total > most) most = total;
     }

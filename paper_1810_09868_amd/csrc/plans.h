@@ -44,6 +44,39 @@ inline W4Plan w4_tiles_plan(int dtype, int N, int In, int Out)
 // ------------------------------------------------------------------------------------------------ orthogonalised updates
 inline int round_to(int v, int to) { return (v + to - 1) / to * to; }
 
+// Matrices of few rows (of X): the bytes of 64 elements in LDS (16 more: rows start in different banks), and what a workgroup with
+// `blocks` of 32 columns has there.
+constexpr int kFewRows = 64, kLds = 160 * 1024;
+constexpr int row_stride(int planes) { return 128 * planes + 16; }
+inline size_t few_lds(int planes, int blocks) { return (size_t)(blocks * 32 + 2 * kFewRows) * row_stride(planes) + 3 * 256; }
+// Column blocks of a wave in one workgroup, 0 where a matrix is too large: its planes' room in LDS, and at most 640 columns (64 x 576,
+// bf16: 38.7 us, and 42.3 in three workgroups and seven launches; 64 x 768: 44.4, and 42.5).
+inline int small_blocks(int planes, int rows, int cols)
+{
+    const int m = rows < cols ? rows : cols, n = rows < cols ? cols : rows, blocks = (n + 31) / 32, cb = (blocks + 7) / 8;
+    return m <= kFewRows && blocks <= 20 && few_lds(planes, blocks) <= kLds ? cb : 0;
+}
+// With more columns: 256 columns to a workgroup while that makes at most 16, whose shares each of them adds up, else as many as LDS has
+// room for, up to 512.
+struct FewPlan { int cb, each, wgs; };
+inline FewPlan few_plan(int planes, int rows, int cols)
+{
+    const int blocks = ((rows < cols ? cols : rows) + 31) / 32;
+    FewPlan w;
+    w.cb = blocks <= 16 * 8 ? 1 : 2;
+    w.each = w.cb * 8;
+    while (few_lds(planes, w.each) > kLds) --w.each;
+    w.wgs = (blocks + w.each - 1) / w.each;
+    return w;
+}
+// ... as long as a matrix's workgroups run at once: they all add up all shares, so that what is read grows with their square, and products
+// by tiles are faster then (fp32 update of 64 x 98304: 280 us, 384 by tiles; 64 x 131072, 293 workgroups: 622, 498; 64 x 1000000: 14.6 ms,
+// 3.4 ms).
+inline bool is_wide(int planes, int rows, int cols)
+{
+    return (rows <= kFewRows || cols <= kFewRows) && few_plan(planes, rows, cols).wgs <= 256;
+}
+
 // Tiles of an update's products, X of m x n, m <= n: 256 x 256 where the product with X takes no more of the chip's rounds with them (a tile is four times the work of a
 // 128 x 128 one, in about 3.4 times its time), and the contraction over m is long beside what a tile begins and ends with
 // (7 x 512 x 4608, bf16: 468 us with them, 427 us without; 4096 x 4096: 1.63 ms, 2.02 ms).

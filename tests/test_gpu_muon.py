@@ -294,3 +294,21 @@ def test_matrices_of_the_largest_tiles_do_not_meet():
         assert torch.equal(alone[b], again[b])
         want = ns64_gpu(x[b].double(), 5)
         assert float((alone[b].double() - want).norm() / want.norm()) <= bound(B.BF16)
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("shape", [(1, 40, 200001), (2, 140001, 17), (1, 1, 250000), (1, 64, 114700)])
+def test_few_rows_and_very_many_columns(dtype, shape):
+    # about where one launch a step ends and tiles begin, and beyond
+    x = on_gpu(dtype, shape, 21)
+    y = torch.full_like(x, float("nan"))
+    ws = ws_bytes(B.vgg_orthogonalize_workspace_bytes(dtype, *shape))
+    ws.fill_(0xFF)
+    B.vgg_orthogonalize(dtype, *shape, 5, x, y, ws)
+    theta, mom, g = torch.zeros_like(y, dtype=torch.float32), torch.zeros_like(y, dtype=torch.float32), x.float()
+    B.vgg_muon_update(dtype, *shape, 5, theta, g, mom, 1.0, 0.9, False, 0.0, ws)
+    scale = max(1.0, shape[1] / shape[2]) ** 0.5
+    for b in range(shape[0]):
+        want = ns64_gpu(x[b].double(), 5)
+        assert float((y[b].double() - want).norm() / want.norm()) <= bound(dtype)
+        assert float((theta[b].double() / -scale - want).norm() / want.norm()) <= bound(dtype)

@@ -12,14 +12,16 @@ from plan_shapes import MUON_256, W4_TILES
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
-@pytest.mark.skipif(shutil.which("g++") is None, reason="g++ not available")
-def test_shapes_reach_their_variants(tmp_path):
-    exe = str(tmp_path / "plans_check")
+@pytest.fixture(scope="module")
+def ask(tmp_path_factory):
+    if shutil.which("g++") is None:
+        pytest.skip("g++ not available")
+    exe = str(tmp_path_factory.mktemp("plans") / "plans_check")
     subprocess.check_call(["g++", "-O1", "-std=c++17", "-o", exe, os.path.join(ROOT, "tests", "host", "plans_check.cpp")])
+    return lambda lines: subprocess.run([exe], input="\n".join(lines), capture_output=True, text=True, check=True, timeout=60).stdout.splitlines()
 
-    def ask(lines):
-        return subprocess.run([exe], input="\n".join(lines), capture_output=True, text=True, check=True, timeout=60).stdout.splitlines()
 
+def test_shapes_reach_their_variants(ask):
     def muon(shapes):
         return ask(["muon %d %d %d" % (b, min(m, n), max(m, n)) for b, m, n in shapes])
 
@@ -31,3 +33,9 @@ def test_shapes_reach_their_variants(tmp_path):
     # the network's dense layers, batch 1, 10 and 100
     assert ask(["w4 1 1 25088 4096", "w4 1 10 4096 4096", "w4 1 100 25088 4096", "w4 1 100 4096 4096", "w4 0 100 4096 1000"]) == [
         "row", "tile", "4 4", "4 2", "4 2"]
+
+
+def test_matrices_of_few_rows_that_are_too_long_go_by_tiles(ask):
+    # (a launch a step reads the square of its workgroups: no more of them than run at once)
+    shapes = [(2, 1, 1), (2, 64, 448), (1, 640, 64), (2, 64, 98304), (1, 131072, 64), (2, 64, 131072), (1, 64, 196608), (2, 1000000, 16), (1, 1, 1 << 22), (2, 65, 65)]
+    assert ask(["few %d %d %d" % s for s in shapes]) == ["1"] * 5 + ["0"] * 5
