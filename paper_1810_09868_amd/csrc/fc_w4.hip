@@ -161,7 +161,7 @@ __device__ __forceinline__ float sum_lanes4(const float (&v)[4])
 // One row of a.  A lane keeps 32 consecutive inputs in registers and meets them with the codes of four outputs at a time (one or
 // 64 / 2^logl of them a load, 16 bytes a lane), while the next four's are on their way; the waves of a workgroup take the row's
 // further slices, and LDS adds up what they find.  Every code is read once, in runs of up to 1 KB.  Bound by that read: 25088 x 4096 in bf16
-// takes 12.8 us, a mere read of the same 53 MB 9.1 us.  (On the matrix unit with 15 of 16 rows empty: 23.3 us.)
+// takes 12.8 us, with fp32 activations 16.3 us, a mere read of the same 53 MB 9.1 us.  (On the matrix unit with 15 of 16 rows empty: 23.3 us.)
 constexpr int kBatch = 4, kRowWaves = 16;
 template <typename T>
 __global__ __launch_bounds__(kRowWaves * 64) void fc_w4_row_kernel(const T *__restrict__ a_rows, W4Args p, int logl, int batches)
@@ -349,7 +349,8 @@ __device__ __forceinline__ f32x4 mfma(const u32x4 &x, const u32x4 &w, f32x4 acc)
 
 // Up to 16 rows: 16 outputs to a workgroup, whose W waves take every W-th 128 inputs, the next ones' codes, scales and activations
 // on their way, and add up in LDS.  Each workgroup reads (and in fp32 splits) all activations, so that it is bound by their way out of
-// L2 and, in fp32, by some 200 vector instructions for every 128 inputs (16 x 4096 x 4096, bf16: 7.5 us; 10 x 4096 x 1000, fp32: 9.8 us).
+// L2 and, in fp32, by some 200 vector instructions for every 128 inputs, which with few outputs few compute units share (16 x 4096 x 4096,
+// bf16: 7.4 us, fp32: 11.9 us; 10 x 4096 x 1000, fp32, 63 workgroups: 9.8 us).
 template <typename T, int W, int G>
 __global__ __launch_bounds__(W * 64) void fc_w4_tile_kernel(const T *__restrict__ a, W4Args p)
 {
@@ -470,7 +471,8 @@ __global__ __launch_bounds__(256) void fc_w4_lay_kernel(const T *__restrict__ a,
 // 16 RT outputs and 16 NT rows to a workgroup, whose eight waves take every eighth 128 inputs of its share and add up in LDS.
 // The next 128 inputs' codes and scales and the next few blocks of activations are on their way.  A code is spread once for NT
 // products, an activation read once for RT; the products fill a tenth of the time, the rest is the activations' way out of L2 and
-// the beginning and end of three launches (100 x 25088 x 4096, bf16: 43.7 us, 470 TFLOP/s; 100 x 4096 x 4096: 14.6 us).
+// the beginning and end of three launches (100 x 25088 x 4096, bf16: 43.7 us, 470 TFLOP/s, fp32: 80 us; 100 x 4096 x
+// 4096: 14.7 us, 24.5 us).
 template <int P, int RT, int NT, int G>
 __global__ __launch_bounds__(512) void fc_w4_tiles_kernel(const u32x4 *__restrict__ x, W4Args p)
 {

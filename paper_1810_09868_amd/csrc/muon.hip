@@ -9,10 +9,11 @@
 // 2^-28.  PLANES = 2: a value is two f16 numbers, the nearest and what that leaves, 22 bits down to 2^-17 and 2^-39 below; hi hi + hi lo
 // + lo hi leaves out 2^-22 of a product at most.  PLANES = 1 (updates that ask for VGG_BF16): operands are rounded to 11 bits.  The term a X takes an
 // fp32 copy of X: a rounding to 11 bits there would grow 3.4-fold in every later step where X has no (or small) singular values, and where the
-// matrix's norm is small beside eps all of X is small and a X nearly all of the result: f16 parts at a fixed scale lose it (130 x 514 of
-// norm 1e-16: 28 % off).  In both the diagonals of G and P, which hold most of them, are kept apart in fp32 (zeros in the planes): with G = D + E,
+// matrix's norm is small beside eps all of X is small and a X nearly all of the result: f16 parts at a fixed scale lose it (130 x 514, a gradient
+// times 2^-64: 73 % off).  In both the diagonals of G and P, which hold most of them, are kept apart in fp32 (zeros in the planes): with G = D + E,
 //     (G G)_ij = (E E)_ij + (d_i + d_j) e_ij,   (G G)_ii = (E E)_ii + d_i^2,   (P X)_i = p_i X_i + (the rest of P) X.
-// One plane is then 3e-4 to 1e-3 off in all, against 1.3e-3 to 2.4e-3 with the diagonals rounded (bf16's own rounding: 1.7e-3).
+// One plane is then, by an emulation of its roundings in 64 bits, 3.6e-4 to 6.5e-4 off for noise, 6e-5 to 5.6e-4 for few strong directions
+// and 6e-4 to 1.6e-3 for singular values over six decades (64 x 576 to 1000 x 1003), against up to 2.4e-3 with the diagonals rounded.
 //
 // X, G and P lie in columns of 128 bytes to a row: [column][row][64 elements], or [32 elements of the first plane, 32 of the
 // second], so that what a workgroup copies for a stage of its contraction is contiguous.  X's fp32 copy lies in columns of 32.
@@ -47,7 +48,7 @@ template <int PL> __device__ __forceinline__ size_t at_column(int rows, int i, i
 __device__ __forceinline__ size_t at_x32(int rows, int i, int j) { return ((size_t)(j >> 5) * rows + i) * 32 + (j & 31); }
 
 // ----------------------------------------------------------------------------------- momentum and the norm
-// Squares are summed in 64 bits: they neither overflow nor vanish.  Bound by the read (7 x 512 x 4608, bf16: 10 us for 33 MB; with a
+// Squares are summed in 64 bits: they neither overflow nor vanish.  Bound by the read (7 x 512 x 4608, bf16: 13 to 16 us for 33 MB, from the launch on; with a
 // step of the momentum, 4096 x 25088: 208 us for 1.2 GB, 5.9 TB/s).
 __device__ __forceinline__ double block_sum(double v)
 {
@@ -166,7 +167,7 @@ struct Layout {
 };
 
 // X_0 in all its forms, zeros where they are padded.  A workgroup: 64 x 64 of the padded X, eight consecutive elements to a thread.
-// Bound by what it writes (7 x 512 x 4608, bf16: 19 us for 99 MB, read and written).
+// Bound by what it writes (7 x 512 x 4608, bf16: 34 us for 165 MB, read and written).
 template <typename T, int PL>
 __global__ __launch_bounds__(256) void muon_start_kernel(Source s, Layout L)
 {
@@ -269,7 +270,7 @@ template <typename T> __device__ __forceinline__ void write_some(const Target &o
 // B that is read transposed change places where r / 2 is odd, for the four rows that sixteen lanes read.  256 x 256 tiles take 2/3 of the
 // LDS traffic of 128 x 128 ones, and four times the work.  Large products are bound by the matrix unit and its power (4096 x 25088, two
 // planes: G in 1.02 ms, 1.33 PFLOP/s of f16 products, pipes busy 0.73; P X in 2.1 ms, 1.2 PFLOP/s), smaller ones by what P X moves
-// between the eight L2s and memory (7 x 512 x 4608, one plane: 37 us for 165 MB; 1000 x 4096, two: 31 us for 98 MB) and by their
+// between the eight L2s and memory (two planes: 7 x 512 x 4608: 72 to 87 us for 270 MB; 1000 x 4096: 32 us for 98 MB) and by their
 // beginnings and ends, not by LDS or barriers: four waves to a tile are 2 to 5 % slower, stages twice as long or what the end
 // reads asked for at the start make no difference, two workgroups to a compute unit 4 % for many rounds and -3 % for one.
 template <typename T, int PL, int MODE, int TILE>
@@ -828,9 +829,9 @@ struct FewRows {
 };
 
 // All columns in one workgroup: everything of a matrix in one launch, and nothing but its input and output passes memory.  Three
-// barriers a step, which with the chains of LDS reads and products between them are all of its time (64 x 27, bf16: 15 us; 64 x 512:
-// 32 us; 64 matrices of 64 x 27 at once: 16 us).  Sixteen waves: 4 % faster for 64 x 512, 8 % slower for 64 x 256, and registers for one
-// block a wave only.
+// barriers a step, which with the chains of LDS reads and products between them are all of its time (two planes, fp32: 64 x 27: 20 us; 64 x 448:
+// 46 us; 64 matrices of 64 x 27 at once: 21 us).  Sixteen waves, one plane: 4 % faster for 64 x 512, 8 % slower for 64 x 256, and registers
+// for one block a wave only.
 template <typename T, int PL, int CB>
 __global__ __launch_bounds__(512) void muon_small_kernel(Source src, Target out, int rows, int cols, int steps)
 {
@@ -890,8 +891,8 @@ __global__ __launch_bounds__(512) void muon_small_kernel(Source src, Target out,
 
 // More columns: `each` blocks of 32 to a workgroup (up to 8 CB), and a launch a step.  Every workgroup adds up all workgroups' shares
 // of G itself, in order, and forms P; what it writes for the next launch is its columns of X, as its registers hold them, and its share of their G.
-// Bound by six launches of some 5 us each until the columns are many (64 x 768, bf16: 42 us; 2 x 28 x 7933: 74 us, 138 us by
-// tiles of products; 64 x 25088: 110 us).  step 0: X_0 from the input; step `steps`: the output.
+// Bound by six launches of some 8 us each until the columns are many (two planes, fp32: 64 x 768: 51 us; 2 x 28 x 7933: 93 us; 64 x 25088:
+// 120 us; with an update's step 148 us, 178 us by tiles of products).  step 0: X_0 from the input; step `steps`: the output.
 template <typename T, int PL, int CB>
 __global__ __launch_bounds__(512) void muon_wide_kernel(Source src, Target out, int rows, int cols, int each, int step, int steps, const double *part,
                                                         int parts, float *x32, const f32x4 *shares, f32x4 *share)

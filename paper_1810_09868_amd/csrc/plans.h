@@ -49,8 +49,9 @@ inline int round_to(int v, int to) { return (v + to - 1) / to * to; }
 constexpr int kFewRows = 64, kLds = 160 * 1024;
 constexpr int row_stride(int planes) { return 128 * planes + 16; }
 inline size_t few_lds(int planes, int blocks) { return (size_t)(blocks * 32 + 2 * kFewRows) * row_stride(planes) + 3 * 256; }
-// Column blocks of a wave in one workgroup, 0 where a matrix is too large: its planes' room in LDS, and at most 640 columns (64 x 576,
-// bf16: 38.7 us, and 42.3 in three workgroups and seven launches; 64 x 768: 44.4, and 42.5).
+// Column blocks of a wave in one workgroup, 0 where a matrix is too large: its planes' room in LDS (448 columns of two), and at most 640
+// columns of one plane (updates of 64 x 576: 48.4 us, and 51.1 in three workgroups and seven launches; 64 x 640: 50.0, 51.2; 64 x 768: 53.9,
+// 51.5).
 inline int small_blocks(int planes, int rows, int cols)
 {
     const int m = rows < cols ? rows : cols, n = rows < cols ? cols : rows, blocks = (n + 31) / 32, cb = (blocks + 7) / 8;
@@ -77,9 +78,10 @@ inline bool is_wide(int planes, int rows, int cols)
     return (rows <= kFewRows || cols <= kFewRows) && few_plan(planes, rows, cols).wgs <= 256;
 }
 
-// Tiles of an update's products, X of m x n, m <= n: 256 x 256 where the product with X takes no more of the chip's rounds with them (a tile is four times the work of a
-// 128 x 128 one, in about 3.4 times its time), and the contraction over m is long beside what a tile begins and ends with
-// (7 x 512 x 4608, bf16: 468 us with them, 427 us without; 4096 x 4096: 1.63 ms, 2.02 ms).
+// Tiles of an update's products, X of m x n, m <= n: 256 x 256 where the product with X takes no more of the chip's rounds with them (a
+// tile is four times the work of a 128 x 128 one, in about 3.4 times its time), and the contraction over m is long beside what a tile begins and ends with
+// (fp32 updates: 7 x 512 x 4608: 831 us with them, 775 us without; 1024 x 4096: 605, 375; 4096 x 4096: 3.94 ms, 4.40 ms; 1088 x 10944, where
+// they are taken: 1.03 ms, 0.99 ms).
 inline int muon_tile(long batch, int m, int n)
 {
     auto rounds = [&](int t) { return (batch * (round_to(m, t) / t) * (round_to(n, t) / t) + 255) / 256; };

@@ -318,9 +318,11 @@ template <int W, typename F> __device__ __forceinline__ void merge_lists(const K
 
 // W waves to a row or to a part of one; W == 1: four rows to a workgroup.  A score is read once, in 16-byte loads,
 // and lives in registers from there on; long rows are bound by the read and the exponentials beside it (4096 x
-// 32768, bf16, four such tensors in turn: 67 us, 4.0 TB/s; 61 us with exponents rounded to fp32), short ones by the launch, one trip to memory, and the alternatives: listing and ranking them is a
-// chain of LDS and ballots that nothing hides (100 x 1000, fp32: 3.2 us without, 5.4 us with the best five; 4 x 200003, bf16: 6.6 us,
-// 15.5 us with the best twenty).
+// 32768, bf16, four such tensors in turn: 67 us, 4.0 TB/s; 61 us with exponents rounded to fp32), short ones by the launch, one trip to
+// memory, and the alternatives: listing and ranking them is a chain of LDS and ballots that nothing hides (100 x 1000, fp32: 3.2 us
+// without, 5.5 us with the best five; 4 x 200003, bf16: 7.1 us, 15.3 us with the best twenty).  Rows in order are the slowest, since nearly
+// every lot then offers all it has, or the first one all of the best (4 x 200003, bf16, rising or falling: 32 us; 512 x 50001, fp32: 399 us
+// rising, 32 us falling, 44 us in any order).
 template <typename T, int W, bool TOP>
 __global__ __launch_bounds__(256) void log_probs_kernel(const T *__restrict__ z, ScoreArgs a)
 {
