@@ -28,7 +28,7 @@
  *  - Tensor pointers must be 16-byte aligned (VGG_ERR_ALIGN otherwise), but
  *    for what is given one number to a row, of which a part of a longer
  *    sequence may be passed: labels, and the gradients that
- *    vgg_log_probs_bwd takes (4 bytes).
+ *    vgg_log_probs_bwd and vgg_fc_xent_bwd take (4 bytes).
  *  - dtype: VGG_F32 = activations and weights fp32, fp32 MFMA.
  *           VGG_BF16 = activations and weights bf16 (round-to-nearest-even
  *           from fp32), fp32 MFMA accumulation, bias and logits fp32.
@@ -393,6 +393,84 @@ int vgg_orthogonalize(int dtype, int batch, int rows, int cols, int steps, const
 size_t vgg_muon_workspace_bytes(int dtype, int batch, int rows, int cols);
 int vgg_muon_update(int dtype, int batch, int rows, int cols, int steps, float *theta, const float *grad, float *momentum,
                     float lr, float mu, int nesterov, float weight_decay, void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------- between dense layers: layer norm, dropout */
+
+/* Dropout.  An element (row n, column c) is dropped where a 16-bit number of
+ * its own is less than round(65536 p), else multiplied by 65536 / (65536 -
+ * round(65536 p)): p in whole 65536ths, 0 <= p <= 1 (what is less than half of
+ * one drops nothing).  The numbers are Philox 4x32-10's (Salmon, Moraes, Dror,
+ * Shaw, SC 2011): key = the seed; counter = (c / 8, n, low word of the step,
+ * layer << 16 | bits 32..47 of the step); the block's four words, low halves
+ * first, are the numbers of columns 8 (c / 8) .. + 7.  Nothing is stored: the
+ * same seed, step and layer give the same mask, in whatever type, with
+ * whatever strides, and by whichever of these entry points, so that the
+ * gradient is dropped by the same call.  rng: seed and step, two 64-bit numbers in DEVICE memory, read when the kernel
+ * runs (a graph's replay takes the step it finds); NULL where p is 0.
+ * layer < 65536 tells the dropouts of one step apart.  What is dropped is 0
+ * whatever was there, NaN included.
+ *
+ * y = dropout(x): N rows of C values in `dtype`, every ldx (ldy) elements, any
+ * alignment of a row; y may be x (with ldy = ldx).  N <= 2^23, C <= 2^30. */
+int vgg_dropout(int dtype, int N, int C, size_t ldx, const void *x, float p, const void *rng, unsigned layer, void *y,
+                size_t ldy, void *stream);
+
+/* Layer norm of N rows of C values, with dropout as above of what it writes:
+ *   y[n,c] = dropout(gamma[c] (x[n,c] - mean[n]) rstd[n] + beta[c]),
+ *   rstd = 1 / sqrt(sum_c (x - mean)^2 / C + eps),  eps >= 0.
+ * x and y in `dtype`, rows as in vgg_dropout; y may be x.  gamma, beta fp32 [C]
+ * or NULL (1 and 0).  stats fp32 [N][2], mean and rstd, which the gradient
+ * takes, or NULL.  Statistics are fp32 sums, the variance of the differences
+ * from the mean; y is rounded once. */
+int vgg_layer_norm(int dtype, int N, int C, size_t ldx, const void *x, const float *gamma, const float *beta, float eps,
+                   float p, const void *rng, unsigned layer, void *y, size_t ldy, float *stats, void *stream);
+/* Its gradient, g = dropout(dy), xh = (x - mean) rstd:
+ *   dbeta = sum_n g, dgamma = sum_n g xh (fp32 [C], either may be NULL),
+ *   dx = rstd (g gamma - mean_c(g gamma) - xh mean_c(g gamma xh)).
+ * relu_mask != 0: x is what a ReLU left, and dx is 0 where x > 0 does not hold.
+ * dy and dx in g_dtype (`dtype`, or VGG_F32); dx may be dy, or x where it has
+ * its type (with the same stride).  p, rng (and what it holds), layer: the
+ * forward call's.  Sums go over a workgroup's rows, then over workgroups in a
+ * fixed order (workspace). */
+size_t vgg_layer_norm_bwd_workspace_bytes(int dtype, int g_dtype, int N, int C);
+int vgg_layer_norm_bwd(int dtype, int g_dtype, int N, int C, size_t ldx, const void *x, const float *gamma,
+                       const float *stats, float p, const void *rng, unsigned layer, size_t lddy, const void *dy, void *dx,
+                       size_t lddx, float *dgamma, float *dbeta, int relu_mask, void *ws, size_t ws_bytes, void *stream);
+
+/* ------------------------------------------------ losses over many classes */
+
+/* A dense layer over K classes and its softmax cross entropy, with no score
+ * kept: z[n,k] = sum_i w[k,i] a[n,i] + bias[k],
+ *   loss[n] = log sum_k exp(z[n,k]) - z[n,y], y = labels[n]; 0 where y is not
+ *             in [0,K);
+ *   stats[n][2], or NULL: the row's largest score and the log of the sum of
+ *             the exponentials of what the scores are above it, which
+ *             vgg_fc_xent_bwd takes.
+ * a [N][In] and w [K][In] in `dtype`, densely packed, bias fp32 [K] or NULL.  A
+ * bias of -inf masks its class; the loss of a masked label is inf, and a row
+ * without a class left has the loss inf (stats -inf).  A NaN or +inf among a
+ * row's scores makes its loss NaN; in fp32 an infinity among activations or
+ * weights makes the scores it has part in infinite or NaN.  Products are
+ * summed in fp32, those of fp32 operands exact to 2^-24; loss and stats are fp32.
+ * N <= 2^22, In <= 2^20, K <= 2^24. */
+size_t vgg_fc_xent_workspace_bytes(int dtype, int N, int In, int K);
+int vgg_fc_xent(int dtype, int N, int In, int K, const void *a, const void *w, const float *bias, const int32_t *labels,
+                float *loss, float *stats, void *ws, size_t ws_bytes, void *stream);
+/* The gradients for an upstream gradient g_loss[n] of every row's loss, with
+ *   dz[n,k] = g_loss[n] (exp(z[n,k] - log sum exp) - 1[k = labels[n]]):
+ *   da = dz w [N][In], dw = dz^T a [K][In], db[k] = sum_n dz[n,k] (fp32).
+ * Each of the three may be NULL, not all.  da and dw are in g_dtype (`dtype`, or VGG_F32)
+ * and overlap nothing that is read.  stats are vgg_fc_xent's of the same
+ * activations, weights and bias.  The scores are formed again, in pieces of
+ * the classes whose dz fits 256 MB of workspace (or 256 classes).  bf16: dz is
+ * rounded to bf16 where it enters the two products, as in vgg_fc_bwd, not in
+ * db; sums are fp32.  Masked classes have no gradient.  Rows without a label
+ * or with g_loss 0 have the gradient 0 and no part in dw and db, whatever
+ * their activations hold. */
+size_t vgg_fc_xent_bwd_workspace_bytes(int dtype, int N, int In, int K);
+int vgg_fc_xent_bwd(int dtype, int g_dtype, int N, int In, int K, const void *a, const void *w, const float *bias,
+                    const int32_t *labels, const float *stats, const float *g_loss, void *da, void *dw, float *db, void *ws,
+                    size_t ws_bytes, void *stream);
 
 /* ------------------------------------------------------------- whole model */
 

@@ -33,6 +33,8 @@ EXPORTS = [
     "vgg_log_probs_workspace_bytes", "vgg_log_probs", "vgg_log_probs_bwd",
     "vgg_fc_w4_quantize", "vgg_fc_w4_dequantize", "vgg_fc_w4_workspace_bytes", "vgg_fc_w4",
     "vgg_orthogonalize_workspace_bytes", "vgg_orthogonalize", "vgg_muon_workspace_bytes", "vgg_muon_update",
+    "vgg_dropout", "vgg_layer_norm", "vgg_layer_norm_bwd_workspace_bytes", "vgg_layer_norm_bwd",
+    "vgg_fc_xent_workspace_bytes", "vgg_fc_xent", "vgg_fc_xent_bwd_workspace_bytes", "vgg_fc_xent_bwd",
 ]
 
 
@@ -109,6 +111,16 @@ def lib() -> C.CDLL:
             getattr(L, n).argtypes = [_i] * 4
         L.vgg_orthogonalize.argtypes = [_i] * 5 + [_vp, _vp, _vp, _sz, _vp]
         L.vgg_muon_update.argtypes = [_i] * 5 + [_vp] * 3 + [C.c_float, C.c_float, _i, C.c_float, _vp, _sz, _vp]
+        L.vgg_dropout.argtypes = [_i, _i, _i, _sz, _vp, C.c_float, _vp, C.c_uint, _vp, _sz, _vp]
+        L.vgg_layer_norm.argtypes = [_i, _i, _i, _sz, _vp, _vp, _vp, C.c_float, C.c_float, _vp, C.c_uint, _vp, _sz, _vp, _vp]
+        L.vgg_layer_norm_bwd_workspace_bytes.restype = _sz
+        L.vgg_layer_norm_bwd_workspace_bytes.argtypes = [_i] * 4
+        L.vgg_layer_norm_bwd.argtypes = ([_i] * 4 + [_sz, _vp, _vp, _vp, C.c_float, _vp, C.c_uint, _sz, _vp, _vp, _sz, _vp, _vp, _i, _vp, _sz, _vp])
+        for n in ("vgg_fc_xent_workspace_bytes", "vgg_fc_xent_bwd_workspace_bytes"):
+            getattr(L, n).restype = _sz
+            getattr(L, n).argtypes = [_i] * 4
+        L.vgg_fc_xent.argtypes = [_i] * 4 + [_vp] * 7 + [_sz, _vp]
+        L.vgg_fc_xent_bwd.argtypes = [_i] * 5 + [_vp] * 10 + [_sz, _vp]
         cfgp = C.POINTER(VggConfig)
         prmp = C.POINTER(Vgg19Params)
         for n in ("vgg19_packed_bytes", "vgg19_forward_workspace_bytes", "vgg19_train_workspace_bytes"):
@@ -353,6 +365,46 @@ def vgg_muon_workspace_bytes(dtype, batch, rows, cols) -> int:
 def vgg_muon_update(dtype, batch, rows, cols, steps, theta, grad, momentum, lr, mu, nesterov, weight_decay, ws):
     _chk(lib().vgg_muon_update(dtype, batch, rows, cols, steps, _ptr(theta), _ptr(grad), _ptr(momentum), float(lr), float(mu),
                                int(nesterov), float(weight_decay), _ptr(ws), _nbytes(ws), _stream()), "vgg_muon_update")
+
+
+# -------------------------------------------- between dense layers, and losses over many classes
+def vgg_dropout(dtype, N, Cc, x, p, rng, layer, y, ldx=None, ldy=None):
+    _chk(lib().vgg_dropout(dtype, N, Cc, Cc if ldx is None else ldx, _ptr(x), float(p), _ptr(rng), layer, _ptr(y), Cc if ldy is None else ldy,
+                           _stream()), "vgg_dropout")
+
+
+def vgg_layer_norm(dtype, N, Cc, x, gamma, beta, eps, p, rng, layer, y, stats, ldx=None, ldy=None):
+    _chk(lib().vgg_layer_norm(dtype, N, Cc, Cc if ldx is None else ldx, _ptr(x), _ptr(gamma), _ptr(beta), float(eps), float(p), _ptr(rng),
+                              layer, _ptr(y), Cc if ldy is None else ldy, _ptr(stats), _stream()), "vgg_layer_norm")
+
+
+def vgg_layer_norm_bwd_workspace_bytes(dtype, g_dtype, N, Cc) -> int:
+    return lib().vgg_layer_norm_bwd_workspace_bytes(dtype, g_dtype, N, Cc)
+
+
+def vgg_layer_norm_bwd(dtype, g_dtype, N, Cc, x, gamma, stats, p, rng, layer, dy, dx, dgamma, dbeta, relu_mask, ws=None, ldx=None,
+                       lddy=None, lddx=None):
+    _chk(lib().vgg_layer_norm_bwd(dtype, g_dtype, N, Cc, Cc if ldx is None else ldx, _ptr(x), _ptr(gamma), _ptr(stats), float(p), _ptr(rng),
+                                  layer, Cc if lddy is None else lddy, _ptr(dy), _ptr(dx), Cc if lddx is None else lddx, _ptr(dgamma),
+                                  _ptr(dbeta), int(relu_mask), _ptr(ws), _nbytes(ws), _stream()), "vgg_layer_norm_bwd")
+
+
+def vgg_fc_xent_workspace_bytes(dtype, N, In, K) -> int:
+    return lib().vgg_fc_xent_workspace_bytes(dtype, N, In, K)
+
+
+def vgg_fc_xent(dtype, N, In, K, a, w, bias, labels, loss, stats, ws=None):
+    _chk(lib().vgg_fc_xent(dtype, N, In, K, _ptr(a), _ptr(w), _ptr(bias), _ptr(labels), _ptr(loss), _ptr(stats), _ptr(ws), _nbytes(ws),
+                           _stream()), "vgg_fc_xent")
+
+
+def vgg_fc_xent_bwd_workspace_bytes(dtype, N, In, K) -> int:
+    return lib().vgg_fc_xent_bwd_workspace_bytes(dtype, N, In, K)
+
+
+def vgg_fc_xent_bwd(dtype, g_dtype, N, In, K, a, w, bias, labels, stats, g_loss, da, dw, db, ws=None):
+    _chk(lib().vgg_fc_xent_bwd(dtype, g_dtype, N, In, K, _ptr(a), _ptr(w), _ptr(bias), _ptr(labels), _ptr(stats), _ptr(g_loss), _ptr(da),
+                               _ptr(dw), _ptr(db), _ptr(ws), _nbytes(ws), _stream()), "vgg_fc_xent_bwd")
 
 
 # ------------------------------------------------------------- whole model

@@ -79,6 +79,18 @@ int log_probs(int dtype, int N, int K, size_t ldz, const void *z, const int32_t 
 size_t log_probs_workspace(int N, int K, int top);
 int log_probs_bwd(int dtype, int N, int K, size_t ldz, const void *z, const int32_t *labels, const float *stats, const float *entropy,
                   const float *g_logp, const float *g_entropy, void *dz, size_t lddz, hipStream_t s);
+int layer_norm(int dtype, int N, int C, size_t ldx, const void *x, const float *gamma, const float *beta, float eps, float p, const void *rng, unsigned layer,
+               void *y, size_t ldy, float *stats, hipStream_t s);
+size_t layer_norm_bwd_workspace(int dtype, int g_dtype, int N, int C);
+int layer_norm_bwd(int dtype, int g_dtype, int N, int C, size_t ldx, const void *x, const float *gamma, const float *stats, float p, const void *rng,
+                   unsigned layer, size_t lddy, const void *dy, void *dx, size_t lddx, float *dgamma, float *dbeta, int relu_mask, void *ws, hipStream_t s);
+int dropout(int dtype, int N, int C, size_t ldx, const void *x, float p, const void *rng, unsigned layer, void *y, size_t ldy, hipStream_t s);
+size_t fc_xent_workspace(int dtype, int N, int In, int K);
+size_t fc_xent_bwd_workspace(int dtype, int N, int In, int K);
+int fc_xent(int dtype, int N, int In, int K, const void *a, const void *w, const float *bias, const int32_t *labels, float *loss, float *stats, void *ws,
+            hipStream_t s);
+int fc_xent_bwd(int dtype, int g_dtype, int N, int In, int K, const void *a, const void *w, const float *bias, const int32_t *labels, const float *stats,
+                const float *g_loss, void *da, void *dw, float *db, void *ws, hipStream_t s);
 int w4_quantize(int In, int Out, int group, const float *w, uint8_t *codes, bf16_t *scales, hipStream_t s);
 int w4_dequantize(int In, int Out, int group, const uint8_t *codes, const bf16_t *scales, float *w, hipStream_t s);
 size_t fc_w4_workspace(int dtype, int N, int In, int Out, int group);
@@ -503,6 +515,8 @@ bool params_aligned(const vgg19_params *p)
 
 // (launches stay below 2^32 threads, offsets within a row below 2^31)
 bool scores_shape_ok(int N, int K, size_t ld) { return N > 0 && N <= (1 << 23) && K > 0 && K <= (1 << 30) && ld >= (size_t)K; }
+bool drop_ok(float p, unsigned layer) { return p >= 0 && p <= 1 && layer < 65536; }
+bool xent_shape_ok(int N, int In, int K) { return N > 0 && N <= (1 << 22) && In > 0 && In <= (1 << 20) && K > 0 && K <= (1 << 24); }
 bool w4_shape_ok(int In, int Out, int group)
 {
     return In > 0 && Out > 0 && In <= (1 << 22) && Out <= (1 << 25) && (long)((In + 127) / 128 * 128) * Out <= (1L << 33) && (group == 32 || group == 64 || group == 128);
@@ -952,6 +966,77 @@ int vgg_muon_update(int dtype, int batch, int rows, int cols, int steps, float *
     if (const int rc = muon_refusal(dtype, batch, rows, cols, steps, ws, ws_bytes)) return rc;
     if (!aligned16(theta) || !aligned16(grad) || !aligned16(momentum)) return VGG_ERR_ALIGN;
     return muon_update(dtype, batch, rows, cols, steps, theta, grad, momentum, lr, mu, nesterov ? 1 : 0, weight_decay, ws, (hipStream_t)stream);
+}
+
+int vgg_dropout(int dtype, int N, int C, size_t ldx, const void *x, float p, const void *rng, unsigned layer, void *y, size_t ldy, void *stream)
+{
+    if (!x || !y || (!rng && p > 0)) return VGG_ERR_NULL;
+    if (!dtype_ok(dtype)) return VGG_ERR_DTYPE;
+    if (!scores_shape_ok(N, C, ldx) || ldy < (size_t)C || (x == y && ldx != ldy) || !drop_ok(p, layer)) return VGG_ERR_SHAPE;
+    if (!aligned16(x) || !aligned16(y) || !aligned16(rng)) return VGG_ERR_ALIGN;
+    return dropout(dtype, N, C, ldx, x, p, rng, layer, y, ldy, (hipStream_t)stream);
+}
+
+int vgg_layer_norm(int dtype, int N, int C, size_t ldx, const void *x, const float *gamma, const float *beta, float eps, float p, const void *rng,
+                   unsigned layer, void *y, size_t ldy, float *stats, void *stream)
+{
+    if (!x || !y || (!rng && p > 0)) return VGG_ERR_NULL;
+    if (!dtype_ok(dtype)) return VGG_ERR_DTYPE;
+    if (!scores_shape_ok(N, C, ldx) || ldy < (size_t)C || (x == y && ldx != ldy) || !drop_ok(p, layer) || !(eps >= 0)) return VGG_ERR_SHAPE;
+    if (!aligned16(x) || !aligned16(y) || !aligned16(gamma) || !aligned16(beta) || !aligned16(stats) || !aligned16(rng)) return VGG_ERR_ALIGN;
+    return layer_norm(dtype, N, C, ldx, x, gamma, beta, eps, p, rng, layer, y, ldy, stats, (hipStream_t)stream);
+}
+
+size_t vgg_layer_norm_bwd_workspace_bytes(int dtype, int g_dtype, int N, int C)
+{
+    return dtype_ok(dtype) && (g_dtype == dtype || g_dtype == VGG_F32) && scores_shape_ok(N, C, C) ? layer_norm_bwd_workspace(dtype, g_dtype, N, C) : 0;
+}
+
+int vgg_layer_norm_bwd(int dtype, int g_dtype, int N, int C, size_t ldx, const void *x, const float *gamma, const float *stats, float p, const void *rng,
+                       unsigned layer, size_t lddy, const void *dy, void *dx, size_t lddx, float *dgamma, float *dbeta, int relu_mask, void *ws,
+                       size_t ws_bytes, void *stream)
+{
+    if (!x || !stats || !dy || !dx || (!rng && p > 0)) return VGG_ERR_NULL;
+    if (!dtype_ok(dtype) || (g_dtype != dtype && g_dtype != VGG_F32)) return VGG_ERR_DTYPE;
+    if (!scores_shape_ok(N, C, ldx) || lddy < (size_t)C || lddx < (size_t)C || (dx == dy && lddx != lddy) || !drop_ok(p, layer)) return VGG_ERR_SHAPE;
+    if (dx == x && (lddx != ldx || g_dtype != dtype)) return VGG_ERR_SHAPE;
+    if (!aligned16(x) || !aligned16(gamma) || !aligned16(stats) || !aligned16(rng) || !aligned16(dy) || !aligned16(dx) || !aligned16(dgamma) || !aligned16(dbeta) ||
+        !aligned16(ws))
+        return VGG_ERR_ALIGN;
+    const size_t need = layer_norm_bwd_workspace(dtype, g_dtype, N, C);
+    if (need && (!ws || ws_bytes < need)) return VGG_ERR_WORKSPACE;
+    return layer_norm_bwd(dtype, g_dtype, N, C, ldx, x, gamma, stats, p, rng, layer, lddy, dy, dx, lddx, dgamma, dbeta, relu_mask ? 1 : 0, ws, (hipStream_t)stream);
+}
+
+size_t vgg_fc_xent_workspace_bytes(int dtype, int N, int In, int K) { return dtype_ok(dtype) && xent_shape_ok(N, In, K) ? fc_xent_workspace(dtype, N, In, K) : 0; }
+
+int vgg_fc_xent(int dtype, int N, int In, int K, const void *a, const void *w, const float *bias, const int32_t *labels, float *loss, float *stats, void *ws,
+                size_t ws_bytes, void *stream)
+{
+    if (!a || !w || !labels || !loss) return VGG_ERR_NULL;
+    if (!dtype_ok(dtype)) return VGG_ERR_DTYPE;
+    if (!xent_shape_ok(N, In, K)) return VGG_ERR_SHAPE;
+    if (!aligned16(a) || !aligned16(w) || !aligned16(bias) || !aligned4(labels) || !aligned16(loss) || !aligned16(stats) || !aligned16(ws)) return VGG_ERR_ALIGN;
+    if (!ws || ws_bytes < fc_xent_workspace(dtype, N, In, K)) return VGG_ERR_WORKSPACE;
+    return fc_xent(dtype, N, In, K, a, w, bias, labels, loss, stats, ws, (hipStream_t)stream);
+}
+
+size_t vgg_fc_xent_bwd_workspace_bytes(int dtype, int N, int In, int K)
+{
+    return dtype_ok(dtype) && xent_shape_ok(N, In, K) ? fc_xent_bwd_workspace(dtype, N, In, K) : 0;
+}
+
+int vgg_fc_xent_bwd(int dtype, int g_dtype, int N, int In, int K, const void *a, const void *w, const float *bias, const int32_t *labels, const float *stats,
+                    const float *g_loss, void *da, void *dw, float *db, void *ws, size_t ws_bytes, void *stream)
+{
+    if (!a || !w || !labels || !stats || !g_loss || (!da && !dw && !db)) return VGG_ERR_NULL;
+    if (!dtype_ok(dtype) || (g_dtype != dtype && g_dtype != VGG_F32)) return VGG_ERR_DTYPE;
+    if (!xent_shape_ok(N, In, K)) return VGG_ERR_SHAPE;
+    if (!aligned16(a) || !aligned16(w) || !aligned16(bias) || !aligned4(labels) || !aligned16(stats) || !aligned4(g_loss) || !aligned16(da) || !aligned16(dw) ||
+        !aligned16(db) || !aligned16(ws))
+        return VGG_ERR_ALIGN;
+    if (!ws || ws_bytes < fc_xent_bwd_workspace(dtype, N, In, K)) return VGG_ERR_WORKSPACE;
+    return fc_xent_bwd(dtype, g_dtype, N, In, K, a, w, bias, labels, stats, g_loss, da, dw, db, ws, (hipStream_t)stream);
 }
 
 size_t vgg19_packed_bytes(const vgg_config *cfg) { return cfg_ok(cfg) ? packed_total(cfg) : 0; }

@@ -1,0 +1,803 @@
+// A dense layer over many classes and its softmax cross entropy, without the scores [N][K] in memory.
+//
+// z = a w^T + b.  Forward: every tile of scores leaves its rows' largest score m and E, the sum of the exponentials of the others above it;
+// joined over a row's tiles, loss = log(1 + E) - (z_label - m).  Backward, for a piece of the classes at a time: the scores again, from them
+// dz = g (softmax - 1[label]), and with it da += dz w, dw = dz^T a, db = sum_n dz.  E is kept without the largest's own 1, and the label's
+// dz is g expm1(log p), so that a label that is all but certain keeps its digits.
+//
+// The three products are one kernel: C[col][row] = sum_k A[row][k] B[col][k], where an operand lies by its rows or by the contraction
+// index (which is then read transposed out of LDS).  bf16 operands are multiplied as they are, fp32 ones in three bf16 parts (f32x3.h).
+#include "common.h"
+#include "exp_of.h"
+#include "f32x3.h"
+#include "wave.h"
+
+#include <type_traits>
+
+namespace vgg {
+
+namespace {
+
+constexpr int kTA = 256;      // rows of C in a tile
+constexpr int kStep = 64;     // contraction indices of a stage: 128 bytes of a row
+constexpr size_t kPieceBytes = 256u << 20;   // what a piece of the classes may take of the workspace
+constexpr int kTileStride = 528;             // bytes from row to row of 256 bf16 numbers in LDS
+
+enum { kStore, kStats, kGrad };
+
+struct Operand {
+    const char *p;
+    size_t ld;            // bytes from row to row
+    size_t plane;         // bytes from part to part of fp32 numbers
+    int rows;             // by rows: of these; by the contraction index: bytes of a row that are there (a multiple of 16)
+    const char *tail;     // by the contraction index: where the last stage's 64 rows lie, if not with the others
+};
+
+struct Sums { float m, e; };   // largest score, and the exponentials of the others above it; of none: -inf, 0
+__device__ __forceinline__ Sums joined(Sums a, Sums b)
+{
+    if (b.m > a.m) { const Sums c = a; a = b; b = c; }
+    const float d = a.m == b.m ? 0.f : below(b.m - a.m), one = b.m > -INFINITY ? 1.f : 0.f;
+    return {a.m, a.e + exp_of(d) * (b.e + one)};
+}
+
+struct Product {
+    Operand a, b;
+    int rows, cols, steps, splits;   // of C; stages of the contraction (of one part); ranges of them
+    // kStore: C[col][row], a row of C^T every ld elements, fp32 or bf16; a range's every `part` elements, added to what is there if asked
+    void *out;
+    size_t ld, part;
+    int bf16, add;
+    // kStats, kGrad: classes are rows of C, examples its columns
+    const float *bias;
+    const int32_t *labels;
+    int class0, classes, all_classes;   // of this piece: the first, how many; of all
+    Sums *sums;                          // kStats: [tiles of classes, of all pieces][N]
+    float *z_label;                      // [N]
+    const float *stats, *g;              // kGrad: [N][2], [N]
+    bf16_t *dz;                          // [parts][N ...][ld_dz]
+    size_t ld_dz, dz_plane;
+    float *db;                           // [tiles of examples][ld_db]
+    size_t ld_db;
+};
+
+typedef __attribute__((address_space(3))) char lds_char;
+
+// Workgroups go round the eight XCDs; each takes a run of the work, so that neighbours share their operands in its L2.
+__device__ __forceinline__ int spread(int id, int count)
+{
+    const int per = count >> 3, more = count & 7, xcd = id & 7, at = id >> 3;
+    return xcd * per + (xcd < more ? xcd : more) + at;
+}
+
+__device__ __forceinline__ bf16x8 read_transposed(const char *at)
+{
+    typedef short s16x4 __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) s16x4 *lp;
+    const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)at);
+    const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)(at + 4 * 128));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+__device__ __forceinline__ void wave_sync()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+__host__ __device__ constexpr int stages_of(int tn) { return tn == 256 ? 2 : 3; }
+// LDS of a tile: its stages, or what its end turns round in it
+__host__ __device__ constexpr int lds_of(int tn, int mode)
+{
+    const int run = stages_of(tn) * (kTA + tn) * 128, stored = 8 * 32 * (tn == 64 ? 144 : tn == 128 ? 272 : 528), graded = tn * kTileStride;
+    const int end = mode == kStore ? stored : mode == kGrad ? graded : 0;
+    return run > end ? run : end;
+}
+
+template <bool A_TR, bool B_TR, int TN, int PL, int MODE>
+__global__ __launch_bounds__(512) void xent_product_kernel(Product p)
+{
+    extern __shared__ __align__(16) char lds[];   // [STAGES][A: 256 x 128 bytes, B: TN x 128 bytes]
+    // eight waves, WA x WB of them, BX x BY blocks of 32 x 32 each
+    constexpr int STAGES = stages_of(TN), WB = TN == 256 ? 4 : TN == 128 ? 2 : 1, WA = 8 / WB, BX = kTA / 32 / WA, BY = TN / 32 / WB;
+    constexpr int HALF = kTA * 128, STAGE = (kTA + TN) * 128, CA = kTA / 64, CB = TN / 64, COPIES = CA + CB;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int mt = (p.rows + kTA - 1) / kTA, nt = (p.cols + TN - 1) / TN;
+    const int unit = spread(blockIdx.x, gridDim.x), split = unit / (mt * nt), in_all = unit - split * (mt * nt);
+    // eight tiles down, then one to the right
+    const int wide = 8 * nt, group = in_all / wide, in = in_all - group * wide, down = mt - group * 8 < 8 ? mt - group * 8 : 8;
+    const int ti = group * 8 + in % down, tj = in / down;
+    const int s0 = (int)((long)p.steps * split / p.splits), ks = (int)((long)p.steps * (split + 1) / p.splits) - s0, total = PL == 3 ? 6 * ks : ks;
+
+    // Where this thread's copies come from, within a stage; rows and columns that are not there are others that are (what they give is
+    // not used).
+    unsigned from_a[CA], from_b[CB];
+    auto source = [&](const Operand &o, bool tr, int tile0, int q) __attribute__((always_inline)) {
+        const int at = (q * 512 + (int)threadIdx.x) * 16;
+        if (!tr) {
+            const int r = at >> 7, seg = ((at >> 4) & 7) ^ (r >> 1 & 7);
+            return (unsigned)((tile0 + r < o.rows ? r : o.rows - 1 - tile0) * (long)o.ld) + seg * 16;
+        }
+        const int k = (at >> 7) & 63, col = tile0 * 2 + (at >> 13) * 128 + ((at & 127) ^ (k >> 1 & 1) << 6);   // [TILE / 64][64][128 bytes]
+        return (unsigned)(k * (long)o.ld) + (col < o.rows ? col : o.rows - 16);
+    };
+#pragma unroll
+    for (int q = 0; q < CA; ++q) from_a[q] = source(p.a, A_TR, ti * kTA, q);
+#pragma unroll
+    for (int q = 0; q < CB; ++q) from_b[q] = source(p.b, B_TR, tj * TN, q);
+    const char *tile_a = p.a.p + (A_TR ? 0 : (size_t)ti * kTA * p.a.ld), *tile_b = p.b.p + (B_TR ? 0 : (size_t)tj * TN * p.b.ld);
+    const size_t step_a = A_TR ? kStep * p.a.ld : kStep * 2, step_b = B_TR ? kStep * p.b.ld : kStep * 2;
+    const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_char *)lds + wave * 1024);
+    // the stage that is copied next: of parts 1 1, then 1 2, 2 1, 2 2, 1 3, 3 1
+    int slot = 0, pair = 0, k_at = s0;
+    const char *at_a, *at_b;
+    auto aim = [&]() __attribute__((always_inline)) {
+        const unsigned pa = PL == 3 ? 0x201100u >> (4 * pair) & 3 : 0, pb = PL == 3 ? 0x021010u >> (4 * pair) & 3 : 0;
+        at_a = tile_a + k_at * step_a + pa * p.a.plane;
+        at_b = tile_b + k_at * step_b + pb * p.b.plane;
+        if (A_TR && p.a.tail && k_at == p.steps - 1) at_a = p.a.tail;
+    };
+    aim();
+    auto copy_one = [&](int n) __attribute__((always_inline)) {      // of a stage's COPIES
+        const unsigned to = lds0 + slot * STAGE + (n < CA ? n * 8192 : HALF + (n - CA) * 8192), off = n < CA ? from_a[n < CA ? n : 0] : from_b[n < CA ? 0 : n - CA];
+        const char *base = n < CA ? at_a : at_b;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(off), "s"(base) : "m0", "memory");
+        if (n == COPIES - 1) {
+            slot = slot + 1 == STAGES ? 0 : slot + 1;
+            if (++k_at == s0 + ks) { k_at = s0; ++pair; }
+            aim();
+        }
+    };
+
+    f32x16 acc[BX][BY] = {}, first[PL == 3 ? BX : 1][PL == 3 ? BY : 1];
+    const int wi = wave / WB * (BX * 32), wj = wave % WB * (BY * 32);
+    const int rx = lane >> 1 & 7;
+    const int s16 = lane & 15, tr_k = 8 * (lane >> 5) + (s16 >> 2), tr_x = s16 >> 3, tr_at = (lane >> 4 & 1) * 32 + (s16 & 3) * 8;
+    // A stage is four steps of 16 contraction indices.  Between a step's products the next step's fragments are read, and in a stage's last
+    // step, after the barrier, the next stage's first fragments and the copies of a stage to come.
+    constexpr int KK = 4, M = BX * BY, R = BX + BY;
+    struct Fragments { bf16x8 a[BX], b[BY]; };
+    auto read_one = [&](int use, int k, int n, Fragments &f) __attribute__((always_inline)) {
+        const bool is_a = n < BX;
+        const int q = is_a ? n : n - BX, w0 = is_a ? wi : wj;
+        const char *from = lds + use * STAGE + (is_a ? 0 : HALF);
+        bf16x8 v;
+        if (is_a ? A_TR : B_TR) {
+            const int c = (w0 >> 5) + q;                 // 64-byte block of a row
+            v = read_transposed(from + (c >> 1) * (64 * 128) + (k * 16 + tr_k) * 128 + (((c & 1) ^ tr_x) << 6) + tr_at);
+        } else
+            v = *reinterpret_cast<const bf16x8 *>(from + (w0 + (lane & 31) + q * 32) * 128 + (((k * 2 + (lane >> 5)) ^ rx) << 4));
+        if (is_a) f.a[is_a ? q : 0] = v;
+        else f.b[is_a ? 0 : q] = v;
+    };
+    Fragments f[2];
+    int use = 0;
+    // One stage; READ: there is a next one, COPY: there is one to be copied.
+    auto stage = [&](auto READ, auto COPY) __attribute__((always_inline)) {
+        constexpr bool reads = decltype(READ)::value, copies = decltype(COPY)::value;
+#pragma unroll
+        for (int k = 0; k < KK; ++k) {
+            const bool last = k + 1 == KK;
+            const int lead = last ? M / 3 : 0, tasks = last ? (reads ? R : 0) + (copies ? COPIES : 0) : R;
+            const Fragments &g = f[k & 1];
+            Fragments &next = f[(k + 1) & 1];
+#pragma unroll
+            for (int i = 0; i < M; ++i) {
+                const int x = i / BY, y = i % BY;
+                if (last && reads && i == lead) {
+                    // The next stage's copies have landed (those of later ones may be on their way), and all waves have read what they need
+                    // of this one, whose place the next copies take.
+                    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(copies ? (STAGES - 2) * COPIES : 0) : "memory");
+                    use = use + 1 == STAGES ? 0 : use + 1;
+                }
+                acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(g.a[x], g.b[y], acc[x][y], 0, 0, 0);
+                if (i >= lead)
+#pragma unroll
+                    for (int n = (i - lead) * tasks / (M - lead); n < (i - lead + 1) * tasks / (M - lead); ++n) {
+                        if (!last) read_one(use, k + 1, n, next);
+                        else if (reads && n < R) read_one(use, 0, n, next);
+                        else copy_one(reads ? n - R : n);
+                    }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    };
+#pragma unroll
+    for (int k = 0; k < STAGES; ++k)
+        if (k < total)
+#pragma unroll
+            for (int n = 0; n < COPIES; ++n) copy_one(n);
+    if (total >= STAGES) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" : : "n"((STAGES - 1) * COPIES) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" : : : "memory");
+#pragma unroll
+    for (int n = 0; n < R; ++n) read_one(0, 0, n, f[0]);
+    int st = 0;
+    if constexpr (PL == 3) {
+        for (; st < ks; ++st) stage(std::true_type{}, std::true_type{});      // (6 ks > ks + STAGES)
+#pragma unroll
+        for (int x = 0; x < BX; ++x)
+#pragma unroll
+            for (int y = 0; y < BY; ++y) {
+                first[x][y] = acc[x][y];
+                acc[x][y] = f32x16{};
+            }
+    }
+    for (; st + STAGES < total; ++st) stage(std::true_type{}, std::true_type{});
+    for (; st + 1 < total; ++st) stage(std::true_type{}, std::false_type{});
+    stage(std::false_type{}, std::false_type{});
+    if constexpr (PL == 3)
+#pragma unroll
+        for (int x = 0; x < BX; ++x)
+#pragma unroll
+            for (int y = 0; y < BY; ++y)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[x][y][v] = join_parts(first[x][y][v], acc[x][y][v]);
+
+    // Value v of a block: row 8 (v / 4) + 4 (lane / 32) + v % 4, column lane % 32.
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");   // no wave reads operands any more
+    if constexpr (MODE == kStore) {
+        // A wave's 32 columns and all its rows go through a place of its own in LDS: then a lane has eight consecutive rows.
+        constexpr int ROWS = BX * 32, STRIDE = ROWS * 4 + 16, LANES = ROWS / 8;
+        char *turned = lds + wave * (32 * STRIDE);
+        const int r8 = lane % LANES * 8, row = ti * kTA + wi + r8;
+#pragma unroll
+        for (int y = 0; y < BY; ++y) {
+#pragma unroll
+            for (int x = 0; x < BX; ++x)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    *reinterpret_cast<f32x4 *>(turned + (lane & 31) * STRIDE + (x * 32 + 8 * q + 4 * (lane >> 5)) * 4) =
+                        f32x4{acc[x][y][4 * q], acc[x][y][4 * q + 1], acc[x][y][4 * q + 2], acc[x][y][4 * q + 3]};
+            wave_sync();
+#pragma unroll
+            for (int c = lane / LANES; c < 32; c += 64 / LANES) {
+                const int col = tj * TN + wj + y * 32 + c, n = p.rows - row;
+                const f32x4 *here = reinterpret_cast<const f32x4 *>(turned + c * STRIDE + r8 * 4);
+                f32x4 lo = here[0], hi = here[1];
+                if (col < p.cols && n > 0) {
+                    const size_t at = (size_t)split * p.part + (size_t)col * p.ld + row;
+                    if (p.bf16) {
+                        bf16_t *to = static_cast<bf16_t *>(p.out) + at;
+                        if (n >= 8 && p.ld % 8 == 0) {
+                            store4(to, lo[0], lo[1], lo[2], lo[3]);
+                            store4(to + 4, hi[0], hi[1], hi[2], hi[3]);
+                        } else
+#pragma unroll
+                            for (int k = 0; k < 8; ++k)
+                                if (k < n) to[k] = f32_to_bf16(k < 4 ? lo[k] : hi[k - 4]);
+                    } else {
+                        float *to = static_cast<float *>(p.out) + at;
+                        if (n >= 8 && p.ld % 4 == 0) {
+                            f32x4 *to4 = reinterpret_cast<f32x4 *>(to);
+                            if (p.add) { lo += to4[0]; hi += to4[1]; }
+                            to4[0] = lo;
+                            to4[1] = hi;
+                        } else
+#pragma unroll
+                            for (int k = 0; k < 8; ++k)
+                                if (k < n) to[k] = (k < 4 ? lo[k] : hi[k - 4]) + (p.add ? to[k] : 0.f);
+                    }
+                }
+            }
+            wave_sync();
+        }
+    } else {
+        // scores of this lane: example tj TN + wj + 32 y + lane % 32, class row0 + 32 x + 8 (v / 4) + v % 4 of the piece
+        const int row0 = ti * kTA + wi + 4 * (lane >> 5);
+#pragma unroll
+        for (int x = 0; x < BX; ++x)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int row = row0 + 32 * x + 8 * (v >> 2) + (v & 3);
+                const float b = row >= p.classes ? -INFINITY : p.bias ? p.bias[p.class0 + row] : 0.f;
+#pragma unroll
+                for (int y = 0; y < BY; ++y) acc[x][y][v] = row >= p.classes ? -INFINITY : acc[x][y][v] + b;
+            }
+        if constexpr (MODE == kStats) {
+            Sums *all = reinterpret_cast<Sums *>(lds);    // [WA][TN]
+#pragma unroll
+            for (int y = 0; y < BY; ++y) {
+                const int col = tj * TN + wj + 32 * y + (lane & 31);
+                const int label = col < p.cols ? (int)((unsigned)p.labels[col] - p.class0) : -1;
+                Sums s = {-INFINITY, 0.f};
+#pragma unroll
+                for (int x = 0; x < BX; ++x)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        s.m = fmaxf(s.m, acc[x][y][v]);
+                        if (label == row0 + 32 * x + 8 * (v >> 2) + (v & 3) && label < p.classes) p.z_label[col] = acc[x][y][v];
+                    }
+                bool own = s.m > -INFINITY;               // one of the largest does not count
+                const float base = own ? s.m : 0.f;
+#pragma unroll
+                for (int x = 0; x < BX; ++x)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const float z = acc[x][y][v], e = exp_of(below(z - base));
+                        const bool it = own && z == s.m;
+                        s.e += it ? 0.f : e;
+                        own = own && !it;
+                    }
+                s = joined(s, Sums{__shfl_xor(s.m, 32), __shfl_xor(s.e, 32)});
+                if (lane < 32) all[wave / WB * TN + wj + 32 * y + lane] = s;
+            }
+            __syncthreads();
+            if (threadIdx.x < TN) {
+                Sums s = all[threadIdx.x];
+#pragma unroll
+                for (int w = 1; w < WA; ++w) s = joined(s, all[w * TN + threadIdx.x]);
+                const int col = tj * TN + threadIdx.x;
+                if (col < p.cols) p.sums[(size_t)(p.class0 / kTA + ti) * p.cols + col] = s;
+            }
+        } else {
+            float sum[BX][16] = {};
+#pragma unroll
+            for (int y = 0; y < BY; ++y) {
+                const int col = tj * TN + wj + 32 * y + (lane & 31);
+                const int y_label = col < p.cols ? p.labels[col] : -1, label = (int)((unsigned)y_label - p.class0);
+                const float g = y_label >= 0 && y_label < p.all_classes ? p.g[col] : 0.f;
+                const float m = g != 0.f ? p.stats[2 * (size_t)col] : 0.f, log_s = g != 0.f ? p.stats[2 * (size_t)col + 1] : 0.f;
+#pragma unroll
+                for (int x = 0; x < BX; ++x)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const int row = row0 + 32 * x + 8 * (v >> 2) + (v & 3);
+                        const float z = acc[x][y][v], d = (z - m) - log_s;
+                        float share = exp_of(below(d));
+                        if (row == label) share = z > -INFINITY || z != z ? expm1f(d) : 0.f;
+                        // (a row without a class: -inf - -inf)
+                        const float out = g == 0.f || row >= p.classes || log_s == -INFINITY ? 0.f : g * share;
+                        acc[x][y][v] = out;
+                        sum[x][v] += out;
+                    }
+            }
+            // dz, a part at a time: [example][class] in LDS, then runs of 512 bytes
+#pragma unroll
+            for (int part = 0; part < PL; ++part) {
+#pragma unroll
+                for (int y = 0; y < BY; ++y)
+#pragma unroll
+                    for (int x = 0; x < BX; ++x)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const float w0 = acc[x][y][4 * q], w1 = acc[x][y][4 * q + 1], w2 = acc[x][y][4 * q + 2], w3 = acc[x][y][4 * q + 3];
+                            char *to = lds + (wj + 32 * y + (lane & 31)) * kTileStride + (wi + 32 * x + 8 * q + 4 * (lane >> 5)) * 2;
+                            if constexpr (PL == 1) store4(reinterpret_cast<bf16_t *>(to), w0, w1, w2, w3);
+                            else {
+                                const Parts4 s = split_parts(f32x3_u32x4{__float_as_uint(w0), __float_as_uint(w1), __float_as_uint(w2), __float_as_uint(w3)});
+                                *reinterpret_cast<f32x3_u32x2 *>(to) = s.p[part];
+                            }
+                        }
+                __syncthreads();
+                for (int at = threadIdx.x; at < TN * 32; at += 512) {
+                    const int col = tj * TN + (at >> 5), row = ti * kTA + (at & 31) * 8;
+                    if (col < p.cols && row < (int)p.ld_dz)
+                        *reinterpret_cast<f32x4 *>(p.dz + part * p.dz_plane + (size_t)col * p.ld_dz + row) =
+                            *reinterpret_cast<const f32x4 *>(lds + (at >> 5) * kTileStride + (at & 31) * 16);
+                }
+                __syncthreads();
+            }
+            // db: over the 32 lanes that have an example each, then over the waves that share classes
+            float *all = reinterpret_cast<float *>(lds);    // [WB][256]
+#pragma unroll
+            for (int x = 0; x < BX; ++x)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    float s = sum[x][v];
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor(s, o);
+                    if ((lane & 31) == 0) all[wave % WB * kTA + wi + 4 * (lane >> 5) + 32 * x + 8 * (v >> 2) + (v & 3)] = s;
+                }
+            __syncthreads();
+            if (p.db && threadIdx.x < kTA) {
+                float s = 0.f;
+#pragma unroll
+                for (int w = 0; w < WB; ++w) s += all[w * kTA + threadIdx.x];
+                const int row = ti * kTA + threadIdx.x;
+                if (row < p.classes) p.db[(size_t)tj * p.ld_db + row] = s;
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------ before and after the products
+// A matrix [rows][cols] as the products take it: bf16 parts [PL][rows_p][cols_p], zeros past its end, and, where there are labels, in rows
+// that have none or whose weight is zero.
+template <typename T>
+__global__ __launch_bounds__(256) void xent_lay_kernel(const T *__restrict__ from, int rows, int cols, bf16_t *to, int rows_p, int cols_p,
+                                                       const int32_t *labels, const float *g, int classes)
+{
+    const int groups = cols_p / 8;
+    for (size_t at = (size_t)blockIdx.x * 256 + threadIdx.x; at < (size_t)rows_p * groups; at += (size_t)gridDim.x * 256) {
+        const int row = (int)(at / groups), c = (int)(at - (size_t)row * groups) * 8;
+        bool there = row < rows;
+        if (there && labels) {
+            const int y = labels[row];
+            there = y >= 0 && y < classes && (!g || g[row] != 0.f);
+        }
+        bf16_t *dst = to + (size_t)row * cols_p + c;
+        const T *src = from + (size_t)row * cols + c;
+        if constexpr (sizeof(T) == 2) {
+            bf16_t v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = there && c + k < cols ? src[k] : 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) dst[k] = v[k];
+        } else {
+            unsigned v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = there && c + k < cols ? __float_as_uint(src[k]) : 0u;
+            const Parts4 lo = split_parts(f32x3_u32x4{v[0], v[1], v[2], v[3]}), hi = split_parts(f32x3_u32x4{v[4], v[5], v[6], v[7]});
+#pragma unroll
+            for (int k = 0; k < 3; ++k) {
+                f32x3_u32x2 *d = reinterpret_cast<f32x3_u32x2 *>(dst + k * (size_t)rows_p * cols_p);
+                d[0] = lo.p[k];
+                d[1] = hi.p[k];
+            }
+        }
+    }
+}
+
+// What the contraction over examples finds past the last of them: zeros in rows [N, NP) of every part of dz.
+__global__ __launch_bounds__(256) void xent_clear_kernel(bf16_t *dz, size_t plane, size_t from, size_t count)
+{
+    for (size_t at = (size_t)blockIdx.x * 256 + threadIdx.x; at < count; at += (size_t)gridDim.x * 256)
+        *reinterpret_cast<f32x4 *>(dz + blockIdx.y * plane + from + at * 8) = f32x4{};
+}
+
+__device__ __forceinline__ void write_loss(Sums s, float z_label, int label, int classes, float *loss, float *stats, int row)
+{
+    const float log_s = s.m == -INFINITY && s.e == 0.f ? -INFINITY : s.m < INFINITY ? log1pf(s.e) : NAN;
+    if (loss) loss[row] = label < 0 || label >= classes ? 0.f : log_s != log_s ? log_s : z_label == -INFINITY ? INFINITY : log_s - (z_label - s.m);
+    if (stats) { stats[2 * (size_t)row] = s.m; stats[2 * (size_t)row + 1] = log_s; }
+}
+
+// The tiles' sums [tiles][N] of a row: 32 rows to a workgroup, eight runs of tiles each.
+__global__ __launch_bounds__(256) void xent_join_kernel(const Sums *__restrict__ sums, int tiles, int N, int classes, const int32_t *__restrict__ labels,
+                                                        const float *__restrict__ z_label, float *loss, float *stats)
+{
+    __shared__ Sums all[8][32];
+    const int at = threadIdx.x & 31, run = threadIdx.x >> 5, row = blockIdx.x * 32 + at;
+    Sums s = {-INFINITY, 0.f};
+    if (row < N)
+        for (int t = run; t < tiles; t += 8) s = joined(s, sums[(size_t)t * N + row]);
+    all[run][at] = s;
+    __syncthreads();
+    if (run || row >= N) return;
+#pragma unroll
+    for (int k = 1; k < 8; ++k) s = joined(s, all[k][at]);
+    const int y = labels[row];
+    write_loss(s, y >= 0 && y < classes ? z_label[row] : 0.f, y, classes, loss, stats, row);
+}
+
+// Scores in `parts` sums [parts][N][ld] of contraction ranges.
+struct Scores {
+    const float *part;
+    int parts, N, classes;
+    size_t ld;
+    const float *bias;
+    __device__ __forceinline__ float at(int row, int k) const
+    {
+        float z = 0.f;
+        for (int q = 0; q < parts; ++q) z += part[((size_t)q * N + row) * ld + k];
+        return bias ? z + bias[k] : z;
+    }
+};
+__global__ __launch_bounds__(256) void xent_rows_kernel(Scores z, const int32_t *__restrict__ labels, float *loss, float *stats)
+{
+    __shared__ Sums all[4];
+    const int row = blockIdx.x;
+    Sums s = {-INFINITY, 0.f};
+    for (int k = threadIdx.x; k < z.classes; k += 256) {
+        const float v = z.at(row, k);
+        s = v == v ? joined(s, Sums{v, 0.f}) : Sums{s.m, v};
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) s = joined(s, Sums{__shfl_xor(s.m, o), __shfl_xor(s.e, o)});
+    if ((threadIdx.x & 63) == 0) all[threadIdx.x >> 6] = s;
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int w = 1; w < 4; ++w) s = joined(s, all[w]);
+    const int y = labels[row];
+    write_loss(s, y >= 0 && y < z.classes ? z.at(row, y) : 0.f, y, z.classes, loss, stats, row);
+}
+// dz [PL][N][ld_dz] of all classes, and db of a range of rows: 256 classes to a workgroup.
+template <int PL>
+__global__ __launch_bounds__(256) void xent_grad_kernel(Scores z, const int32_t *__restrict__ labels, const float *__restrict__ stats, const float *__restrict__ g,
+                                                        bf16_t *dz, size_t ld_dz, size_t dz_plane, float *db, size_t ld_db)
+{
+    const int k = blockIdx.x * 256 + threadIdx.x;
+    if (k >= (int)ld_dz) return;
+    const int r0 = (int)((long)z.N * blockIdx.y / gridDim.y), r1 = (int)((long)z.N * (blockIdx.y + 1) / gridDim.y);
+    float sum = 0.f;
+    for (int row = r0; row < r1; ++row) {
+        const int y = labels[row];
+        const float w = y >= 0 && y < z.classes ? g[row] : 0.f, m = stats[2 * (size_t)row], log_s = stats[2 * (size_t)row + 1];
+        float out = 0.f;
+        if (k < z.classes && w != 0.f && log_s != -INFINITY) {
+            const float v = z.at(row, k), d = (v - m) - log_s;
+            out = w * (k == y ? v > -INFINITY || v != v ? expm1f(d) : 0.f : exp_of(below(d)));
+        }
+        sum += out;
+        if constexpr (PL == 1) dz[(size_t)row * ld_dz + k] = f32_to_bf16(out);
+        else {
+            const Parts4 s = split_parts(f32x3_u32x4{__float_as_uint(out), 0u, 0u, 0u});
+#pragma unroll
+            for (int q = 0; q < 3; ++q) dz[q * dz_plane + (size_t)row * ld_dz + k] = (bf16_t)(s.p[q][0] & 0xffffu);
+        }
+    }
+    if (db && k < z.classes) db[(size_t)blockIdx.y * ld_db + k] = sum;
+}
+
+// out [rows][cols] = the sum of `parts` matrices [rows][ld], `part` elements apart, in order.
+template <typename T>
+__global__ __launch_bounds__(256) void xent_add_kernel(const float *__restrict__ from, int parts, size_t part, size_t ld, int rows, int cols, T *out)
+{
+    const int groups = (cols + 3) / 4;
+    for (size_t at = (size_t)blockIdx.x * 256 + threadIdx.x; at < (size_t)rows * groups; at += (size_t)gridDim.x * 256) {
+        const size_t row = at / groups;
+        const int c = (int)(at - row * groups) * 4;
+        f32x4 s = {};
+        for (int q = 0; q < parts; ++q) s += *reinterpret_cast<const f32x4 *>(from + q * part + row * ld + c);     // (ld is a multiple of 4)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (c + k < cols) Elem<T>::store(out + row * cols + c + k, s[k]);
+    }
+}
+
+// --------------------------------------------------------------------------------------------------------- plans
+inline int up(long v, int to) { return (int)((v + to - 1) / to * to); }
+inline long div_up(long a, long b) { return (a + b - 1) / b; }
+
+// Columns of a tile: examples for the scores and da, classes for dw.
+inline int tile_of(int dtype, int cols) { return cols > 128 && dtype == VGG_BF16 ? 256 : cols > 64 ? 128 : 64; }
+// Ranges of a contraction of `steps` stages, where `tiles` do not fill the chip: at least four stages each.
+inline int splits_of(long tiles, int steps)
+{
+    const long most = div_up(steps, 4), want = tiles >= 256 ? 1 : div_up(256, tiles);
+    return (int)(want < most ? want : most);
+}
+
+struct XentPlan {
+    int PL, In, InP, NP, tn;
+    bool direct_w, direct_a;      // read where they are (bf16, whole stages)
+    int classes, pieces;          // of a piece (the last has what is left)
+    int z_splits;                 // 0: scores' tiles end in their sums or gradients; else their parts are added up (then one piece)
+    size_t ld_dz, ld_z;
+    // forward
+    size_t a_at, w_at, z_at, sums_at, label_at, forward_bytes;
+    // backward
+    int da_splits, dw_splits, dw_tn, db_parts;
+    bool da_direct;
+    size_t tail_at, dz_at, da_at, dw_at, db_at, backward_bytes;
+};
+
+XentPlan xent_plan(int dtype, int N, int In, int K)
+{
+    XentPlan p;
+    p.PL = dtype == VGG_BF16 ? 1 : 3;
+    p.In = In; p.InP = up(In, kStep); p.NP = up(N, kStep);
+    p.tn = tile_of(dtype, N);
+    p.direct_w = p.direct_a = dtype == VGG_BF16 && In % kStep == 0;
+    const long n_tiles = div_up(N, p.tn), d_tiles = div_up(In, kTA);
+    const int steps = p.InP / kStep;
+    // scores of few tiles: their contraction is split, so that all of them have to be kept for a moment
+    const long z_tiles = div_up(K, kTA) * n_tiles;
+    p.z_splits = z_tiles < 128 && steps >= 8 ? splits_of(z_tiles, steps) : 0;
+    if (p.z_splits == 1) p.z_splits = 0;
+    const size_t per_class = (size_t)p.PL * 2 * (p.NP + (p.direct_w ? 0 : p.InP));
+    long classes = (long)(kPieceBytes / per_class) / kTA * kTA;
+    if (classes < kTA) classes = kTA;
+    if (p.z_splits || classes > K) classes = up(K, kTA);
+    p.pieces = (int)div_up(K, classes);
+    p.classes = up(div_up(K, p.pieces), kTA);
+    p.pieces = (int)div_up(K, p.classes);
+    const int most = p.classes < K ? p.classes : K;
+    p.ld_dz = up(most, kStep);
+    p.ld_z = up(K, 4);
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t here = at; at += round_up(bytes, 256); return here; };
+    // (the gradients take the activations laid out in any case: rows without a label have to be zeros)
+    p.a_at = take((size_t)p.PL * 2 * p.NP * p.InP);
+    p.w_at = take(p.direct_w ? 0 : (size_t)p.PL * 2 * up(most, kStep) * p.InP);
+    p.z_at = take(p.z_splits ? (size_t)p.z_splits * N * p.ld_z * 4 : 0);
+    const size_t both = at;
+    p.sums_at = take(p.z_splits ? 0 : (size_t)div_up(K, kTA) * N * sizeof(Sums));
+    p.label_at = take(p.z_splits ? 0 : (size_t)N * 4);
+    p.forward_bytes = at;
+    at = both;
+    p.tail_at = take(p.direct_w ? (size_t)kStep * In * 2 : 0);
+    p.dz_at = take((size_t)p.PL * 2 * p.NP * p.ld_dz);
+    p.da_splits = splits_of(n_tiles * d_tiles, (int)div_up(most, kStep));
+    p.da_direct = p.pieces == 1 && p.da_splits == 1;
+    p.da_at = take(p.da_direct ? 0 : (size_t)p.da_splits * N * p.InP * 4);
+    p.dw_tn = tile_of(dtype, most);
+    p.dw_splits = splits_of(d_tiles * div_up(most, p.dw_tn), p.NP / kStep);
+    p.dw_at = take(p.dw_splits == 1 ? 0 : (size_t)p.dw_splits * most * p.InP * 4);
+    // rows' ranges that db is summed in
+    p.db_parts = (int)(p.z_splits ? (N < 64 ? 1 : N < 64 * 64 ? div_up(N, 64) : 64) : n_tiles);
+    p.db_at = take(p.db_parts == 1 ? 0 : (size_t)p.db_parts * p.ld_dz * 4);
+    p.backward_bytes = at;
+    return p;
+}
+
+// ------------------------------------------------------------------------------------------------------ launches
+template <bool A_TR, bool B_TR, int TN, int PL, int MODE> int launch_product(const Product &p, hipStream_t s)
+{
+    auto *kernel = &xent_product_kernel<A_TR, B_TR, TN, PL, MODE>;
+    constexpr int lds = lds_of(TN, MODE);
+    if (lds > 65536 && !raise_lds_limit(reinterpret_cast<const void *>(kernel))) return VGG_ERR_LAUNCH;
+    const long grid = div_up(p.rows, kTA) * div_up(p.cols, TN) * p.splits;
+    kernel<<<(int)grid, 512, lds, s>>>(p);
+    return launch_status();
+}
+template <bool A_TR, bool B_TR, int MODE> int product(int PL, int tn, const Product &p, hipStream_t s)
+{
+    if (PL == 3) return tn == 128 ? launch_product<A_TR, B_TR, 128, 3, MODE>(p, s) : launch_product<A_TR, B_TR, 64, 3, MODE>(p, s);
+    return tn == 256   ? launch_product<A_TR, B_TR, 256, 1, MODE>(p, s)
+           : tn == 128 ? launch_product<A_TR, B_TR, 128, 1, MODE>(p, s)
+                       : launch_product<A_TR, B_TR, 64, 1, MODE>(p, s);
+}
+
+int lay(int dtype, const void *from, int rows, int cols, void *to, int rows_p, int cols_p, const int32_t *labels, const float *g, int classes, hipStream_t s)
+{
+    const long groups = (long)rows_p * (cols_p / 8), blocks = div_up(groups, 256);
+    const int grid = (int)(blocks < 8192 ? blocks : 8192);
+    if (dtype == VGG_BF16)
+        xent_lay_kernel<bf16_t><<<grid, 256, 0, s>>>(static_cast<const bf16_t *>(from), rows, cols, static_cast<bf16_t *>(to), rows_p, cols_p, labels, g, classes);
+    else
+        xent_lay_kernel<float><<<grid, 256, 0, s>>>(static_cast<const float *>(from), rows, cols, static_cast<bf16_t *>(to), rows_p, cols_p, labels, g, classes);
+    return launch_status();
+}
+int add_parts(int dtype, const float *from, int parts, size_t part, size_t ld, int rows, int cols, void *out, hipStream_t s)
+{
+    const long blocks = div_up((long)rows * div_up(cols, 4), 256);
+    const int grid = (int)(blocks < 8192 ? blocks : 8192);
+    if (dtype == VGG_BF16) xent_add_kernel<bf16_t><<<grid, 256, 0, s>>>(from, parts, part, ld, rows, cols, static_cast<bf16_t *>(out));
+    else xent_add_kernel<float><<<grid, 256, 0, s>>>(from, parts, part, ld, rows, cols, static_cast<float *>(out));
+    return launch_status();
+}
+
+struct Call {
+    int dtype, N, In, K;
+    const void *a, *w;
+    const float *bias;
+    const int32_t *labels;
+    char *ws;
+    hipStream_t s;
+};
+// The product that gives the scores of a piece: classes are the rows of C, examples its columns.
+int scores_product(const Call &c, const XentPlan &pl, int piece, bool laid_a, Product &p)
+{
+    const int es = c.dtype == VGG_BF16 ? 2 : 4, class0 = piece * pl.classes, here = c.K - class0 < pl.classes ? c.K - class0 : pl.classes;
+    const char *w = static_cast<const char *>(c.w) + (size_t)class0 * c.In * es;
+    p = Product{};
+    p.rows = here; p.cols = c.N; p.steps = pl.InP / kStep; p.splits = 1;
+    if (pl.direct_w) p.a = {w, (size_t)c.In * 2, 0, here, nullptr};
+    else {
+        const int rows_p = up(here, kStep);
+        if (const int rc = lay(c.dtype, w, here, c.In, c.ws + pl.w_at, rows_p, pl.InP, nullptr, nullptr, 0, c.s)) return rc;
+        p.a = {c.ws + pl.w_at, (size_t)pl.InP * 2, (size_t)rows_p * pl.InP * 2, here, nullptr};
+    }
+    if (!laid_a) p.b = {static_cast<const char *>(c.a), (size_t)c.In * 2, 0, c.N, nullptr};
+    else p.b = {c.ws + pl.a_at, (size_t)pl.InP * 2, (size_t)pl.NP * pl.InP * 2, c.N, nullptr};
+    p.bias = c.bias; p.labels = c.labels;
+    p.class0 = class0; p.classes = here; p.all_classes = c.K;
+    return VGG_OK;
+}
+int scores_in_parts(const XentPlan &pl, const Call &c, Product &p, Scores &z)
+{
+    p.splits = pl.z_splits;
+    p.out = c.ws + pl.z_at; p.ld = pl.ld_z; p.part = (size_t)c.N * pl.ld_z;
+    z = {static_cast<const float *>(p.out), pl.z_splits, c.N, c.K, pl.ld_z, c.bias};
+    return product<false, false, kStore>(pl.PL, pl.tn, p, c.s);
+}
+
+int forward(const Call &c, float *loss, float *stats)
+{
+    const XentPlan pl = xent_plan(c.dtype, c.N, c.In, c.K);
+    int rc;
+    if (!pl.direct_a && (rc = lay(c.dtype, c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, nullptr, nullptr, 0, c.s))) return rc;
+    Sums *sums = reinterpret_cast<Sums *>(c.ws + pl.sums_at);
+    float *z_label = reinterpret_cast<float *>(c.ws + pl.label_at);
+    for (int piece = 0; piece < pl.pieces; ++piece) {
+        Product p;
+        if ((rc = scores_product(c, pl, piece, !pl.direct_a, p))) return rc;
+        if (pl.z_splits) {
+            Scores z;
+            if ((rc = scores_in_parts(pl, c, p, z))) return rc;
+            xent_rows_kernel<<<c.N, 256, 0, c.s>>>(z, c.labels, loss, stats);
+            return launch_status();
+        }
+        p.sums = sums; p.z_label = z_label;
+        if ((rc = product<false, false, kStats>(pl.PL, pl.tn, p, c.s))) return rc;
+    }
+    xent_join_kernel<<<(int)div_up(c.N, 32), 256, 0, c.s>>>(sums, (int)div_up(c.K, kTA), c.N, c.K, c.labels, z_label, loss, stats);
+    return launch_status();
+}
+
+int backward(const Call &c, int g_dtype, const float *stats, const float *g, void *da, void *dw, float *db)
+{
+    const XentPlan pl = xent_plan(c.dtype, c.N, c.In, c.K);
+    const int gs = g_dtype == VGG_BF16 ? 2 : 4;
+    int rc;
+    if ((rc = lay(c.dtype, c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, c.labels, g, c.K, c.s))) return rc;
+    bf16_t *dz = reinterpret_cast<bf16_t *>(c.ws + pl.dz_at);
+    const size_t dz_plane = (size_t)pl.NP * pl.ld_dz, a_plane = (size_t)pl.NP * pl.InP * 2;
+    if (const size_t past = (size_t)(pl.NP - c.N) * pl.ld_dz / 8) {
+        xent_clear_kernel<<<dim3((unsigned)(past < 256 * 1024 ? (past + 255) / 256 : 1024), (unsigned)pl.PL), 256, 0, c.s>>>(dz, dz_plane, (size_t)c.N * pl.ld_dz, past);
+        if ((rc = launch_status())) return rc;
+    }
+    float *da_part = reinterpret_cast<float *>(c.ws + pl.da_at), *dw_part = reinterpret_cast<float *>(c.ws + pl.dw_at);
+    for (int piece = 0; piece < pl.pieces; ++piece) {
+        Product p;
+        if ((rc = scores_product(c, pl, piece, true, p))) return rc;
+        const Operand w = p.a;
+        const int class0 = p.class0, here = p.classes;
+        float *db_to = db ? pl.db_parts == 1 ? db + class0 : reinterpret_cast<float *>(c.ws + pl.db_at) : nullptr;
+        if (pl.z_splits) {
+            Scores z;
+            if ((rc = scores_in_parts(pl, c, p, z))) return rc;
+            const dim3 grid((unsigned)div_up(pl.ld_dz, 256), (unsigned)pl.db_parts);
+            if (pl.PL == 1) xent_grad_kernel<1><<<grid, 256, 0, c.s>>>(z, c.labels, stats, g, dz, pl.ld_dz, dz_plane, db_to, pl.ld_dz);
+            else xent_grad_kernel<3><<<grid, 256, 0, c.s>>>(z, c.labels, stats, g, dz, pl.ld_dz, dz_plane, db_to, pl.ld_dz);
+            if ((rc = launch_status())) return rc;
+        } else {
+            p.stats = stats; p.g = g;
+            p.dz = dz; p.ld_dz = pl.ld_dz; p.dz_plane = dz_plane;
+            p.db = db_to; p.ld_db = pl.ld_dz;
+            if ((rc = product<false, false, kGrad>(pl.PL, pl.tn, p, c.s))) return rc;
+        }
+        if (db && pl.db_parts > 1 && (rc = add_parts(VGG_F32, db_to, pl.db_parts, pl.ld_dz, pl.ld_dz, 1, here, db + class0, c.s))) return rc;
+        // (a last piece's gradients beyond its classes: zeros up to the contraction's next stage)
+        if (da) {
+            Product q = {};
+            const int steps = (int)div_up(here, kStep);
+            q.a = w;
+            q.a.rows = (int)w.ld;
+            if (pl.direct_w && here % kStep) {
+                const int from = here / kStep * kStep;
+                if ((rc = lay(c.dtype, w.p + (size_t)from * w.ld, here - from, c.In, c.ws + pl.tail_at, kStep, c.In, nullptr, nullptr, 0, c.s))) return rc;
+                q.a.tail = c.ws + pl.tail_at;
+            }
+            q.b = {reinterpret_cast<const char *>(dz), pl.ld_dz * 2, dz_plane * 2, c.N, nullptr};
+            q.rows = c.In; q.cols = c.N; q.steps = steps; q.splits = pl.da_splits < steps ? pl.da_splits : steps;
+            if (pl.da_direct) { q.out = da; q.ld = c.In; q.bf16 = g_dtype == VGG_BF16; }
+            else { q.out = da_part; q.ld = pl.InP; q.part = (size_t)c.N * pl.InP; q.add = piece > 0; }
+            if ((rc = product<true, false, kStore>(pl.PL, pl.tn, q, c.s))) return rc;
+        }
+        if (dw) {
+            Product q = {};
+            q.a = {c.ws + pl.a_at, (size_t)pl.InP * 2, a_plane, pl.InP * 2, nullptr};
+            q.b = {reinterpret_cast<const char *>(dz), pl.ld_dz * 2, dz_plane * 2, (int)pl.ld_dz * 2, nullptr};
+            q.rows = c.In; q.cols = here; q.steps = pl.NP / kStep; q.splits = pl.dw_splits;
+            void *out = static_cast<char *>(dw) + (size_t)class0 * c.In * gs;
+            if (q.splits == 1) { q.out = out; q.ld = c.In; q.bf16 = g_dtype == VGG_BF16; }
+            else { q.out = dw_part; q.ld = pl.InP; q.part = (size_t)here * pl.InP; }
+            if ((rc = product<true, true, kStore>(pl.PL, pl.dw_tn, q, c.s))) return rc;
+            if (q.splits > 1 && (rc = add_parts(g_dtype, dw_part, q.splits, q.part, pl.InP, here, c.In, out, c.s))) return rc;
+        }
+    }
+    if (da && !pl.da_direct) return add_parts(g_dtype, da_part, pl.da_splits, (size_t)c.N * pl.InP, pl.InP, c.N, c.In, da, c.s);
+    return VGG_OK;
+}
+
+}  // namespace
+
+size_t fc_xent_workspace(int dtype, int N, int In, int K) { return xent_plan(dtype, N, In, K).forward_bytes; }
+size_t fc_xent_bwd_workspace(int dtype, int N, int In, int K) { return xent_plan(dtype, N, In, K).backward_bytes; }
+
+int fc_xent(int dtype, int N, int In, int K, const void *a, const void *w, const float *bias, const int32_t *labels, float *loss, float *stats, void *ws,
+            hipStream_t s)
+{
+    return forward(Call{dtype, N, In, K, a, w, bias, labels, static_cast<char *>(ws), s}, loss, stats);
+}
+
+int fc_xent_bwd(int dtype, int g_dtype, int N, int In, int K, const void *a, const void *w, const float *bias, const int32_t *labels, const float *stats,
+                const float *g_loss, void *da, void *dw, float *db, void *ws, hipStream_t s)
+{
+    return backward(Call{dtype, N, In, K, a, w, bias, labels, static_cast<char *>(ws), s}, g_dtype, stats, g_loss, da, dw, db);
+}
+
+}  // namespace vgg

@@ -9,6 +9,8 @@
 // All sums are fp32.  A score of -inf has d = -inf, which is raised to kNothing: exp(d) = 0, and its product with d no NaN.
 // A NaN makes E, and it or a +inf everything of its row NaN.
 #include "common.h"
+#include "exp_of.h"
+#include "wave.h"
 
 #include <type_traits>
 
@@ -16,7 +18,6 @@ namespace vgg {
 
 namespace {
 
-constexpr float kNothing = -1e4f;   // exp of it is 0, and no product with it overflows
 constexpr int kMaxTop = 64;   // one alternative to a lane
 
 struct Sums { float m, e, t; };   // of no scores: -inf, 0, 0
@@ -36,50 +37,11 @@ __device__ __forceinline__ Sums joined(Sums a, Sums b)
     return {a.m, a.e + b.e, a.t + b.t};
 }
 
-// Sums and maxima over a wave without LDS: rotations within 16 lanes, then quarters and halves that change places.
-template <int N> __device__ __forceinline__ float row_ror(float x)
-{
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x120 + N, 0xf, 0xf, true));
-}
-template <typename F> __device__ __forceinline__ float quarters(float v, F f)
-{
-    const auto q = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    const unsigned q0 = q[0], q1 = q[1];
-    return f(__uint_as_float(q0), __uint_as_float(q1));
-}
-template <typename F> __device__ __forceinline__ float halves(float v, F f)
-{
-    const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    const unsigned h0 = h[0], h1 = h[1];
-    return f(__uint_as_float(h0), __uint_as_float(h1));
-}
-template <typename F> __device__ __forceinline__ float wave_all(float v, F f)
-{
-    v = f(v, row_ror<8>(v));
-    v = f(v, row_ror<4>(v));
-    v = f(v, row_ror<2>(v));
-    v = f(v, row_ror<1>(v));
-    return halves(quarters(v, f), f);
-}
-__device__ __forceinline__ float all_max(float v) { return wave_all(v, [](float a, float b) { return fmaxf(a, b); }); }
-__device__ __forceinline__ float all_min(float v) { return wave_all(v, [](float a, float b) { return fminf(a, b); }); }
-__device__ __forceinline__ float all_sum(float v) { return wave_all(v, [](float a, float b) { return a + b; }); }
 __device__ __forceinline__ Sums wave_joined(Sums a, int lane)
 {
     const float M = all_max(a.m);
     if (lane != __builtin_ctzll(__ballot(a.m == M) | 1ull << 63)) rebase(a, M);   // (the first with the largest keeps its E)
     return {M, all_sum(a.e), all_sum(a.t)};
-}
-
-// A difference as exp_of takes it: -inf, and what is too low for any exponential, to kNothing; a NaN as it is.
-__device__ __forceinline__ float below(float d) { return __builtin_elementwise_maximum(d, kNothing); }
-// exp(d), d <= 0 and not below kNothing (or NaN): 2^t, t = d / ln 2 rounded to fp32, times 1 + r, r = d - t ln 2 what that rounding leaves
-// (ln 2 in two parts).  Without r a term is off by up to |d| 2^-24, all terms of a flat tail in the same direction.
-__device__ __forceinline__ float exp_of(float d)
-{
-    constexpr float kLog2E = 1.44269504f, kLn2 = 0.693147182f, kLn2Rest = -1.90465421e-9f;
-    const float t = d * kLog2E, r = __builtin_fmaf(-t, kLn2Rest, __builtin_fmaf(-t, kLn2, d)), e = __builtin_amdgcn_exp2f(t);
-    return __builtin_fmaf(e, r, e);
 }
 
 // V scores, `most` the largest, into a thread's sums.

@@ -1,0 +1,281 @@
+"""Losses over many classes and their gradients against the definition in 64 bits: one class to many pieces, sizes around the tiles', masks that
+leave nothing, rows without a label, NaN and infinities, labels that are all but certain, another stream, a graph."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_1810_09868_amd import binding as B
+
+from gpu_util import TDT, ws_bytes
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+class Xent:
+    def __init__(self, dtype, N, In, K, seed, masked=0.0, bias=True, g_dtype=None, std=2.5):
+        self.dtype, self.g_dtype, self.N, self.In, self.K = dtype, dtype if g_dtype is None else g_dtype, N, In, K
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        normal = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+        self.a = normal(N, In).to(TDT[dtype])
+        self.w = (normal(K, In) * (std / math.sqrt(In))).to(TDT[dtype])
+        self.bias = normal(K) * 0.3 if bias else None
+        if masked:
+            self.bias[torch.rand((K,), generator=g, device="cuda") < masked] = -math.inf
+        self.labels = torch.randint(-1, K + 1, (N,), generator=g, device="cuda", dtype=torch.int32)
+        self.g = normal(N)
+        if N > 4:
+            self.g[3] = 0
+
+    def run(self, want=("da", "dw", "db")):
+        N, In, K = self.N, self.In, self.K
+        guard = lambda n, t: torch.full((n + 64,), 9.0, dtype=t, device="cuda")  # noqa: E731
+        f32, gt = torch.float32, TDT[self.g_dtype]
+        self.buf = {"loss": guard(N, f32), "stats": guard(2 * N, f32), "da": guard(N * In, gt), "dw": guard(K * In, gt), "db": guard(K, f32)}
+        count = {"loss": N, "stats": 2 * N, "da": N * In, "dw": K * In, "db": K}
+        ws = ws_bytes(B.vgg_fc_xent_workspace_bytes(self.dtype, N, In, K))
+        ws.fill_(0xFF)
+        B.vgg_fc_xent(self.dtype, N, In, K, self.a, self.w, self.bias, self.labels, self.buf["loss"], self.buf["stats"], ws)
+        if want:
+            ws = ws_bytes(B.vgg_fc_xent_bwd_workspace_bytes(self.dtype, N, In, K))
+            ws.fill_(0xFF)
+            B.vgg_fc_xent_bwd(self.dtype, self.g_dtype, N, In, K, self.a, self.w, self.bias, self.labels, self.buf["stats"], self.g,
+                              *[self.buf[k] if k in want else None for k in ("da", "dw", "db")], ws)
+        torch.cuda.synchronize()
+        for k, b in self.buf.items():
+            assert (b[count[k]:] == 9.0).all(), k
+            if k in ("da", "dw", "db") and k not in want:
+                assert (b == 9.0).all()
+        self.loss, self.stats, self.db = self.buf["loss"][:N], self.buf["stats"][:2 * N].view(N, 2), self.buf["db"][:K]
+        self.da, self.dw = self.buf["da"][:N * In].view(N, In), self.buf["dw"][:K * In].view(K, In)
+        return self
+
+    def reference(self):
+        """Values and how far off they may be, for rows whose scores are finite or -inf.
+
+        Scores: products of bf16 numbers are exact in fp32 and those of three-part numbers left out by 2^-24; sums of 16 are cut off at 2^-23 of the larger one as
+        they meet the running sum, at most In / 16 + 1 times and as often again where parts of a contraction are joined: e_z.  Exponentials 4 u, and a sum of K positive
+        terms over at most 64 in turn and then in pairs: 100 u relative.  A gradient's term dz is then off by 2 e_z + 110 u of its share, and in bf16 by
+        2^-8 of itself where it enters a product; the sums over n or k as the scores'."""
+        a, w = self.a.double(), self.w.double()
+        b = torch.zeros(self.K, dtype=torch.float64, device="cuda") if self.bias is None else self.bias.double()
+        z = a @ w.t() + b
+        size = a.abs() @ w.abs().t()
+        e_z = (2 * (self.In / 16 + 1) * 2 * U + 4 * U) * size + 2 * U * torch.where(b > -math.inf, b, 0.0).abs()
+        e_row = e_z.amax(1, keepdim=True)
+        here = (self.labels >= 0) & (self.labels < self.K)
+        at = self.labels.long().clamp(0, self.K - 1)[:, None]
+        m = z.amax(1, keepdim=True)
+        m0 = torch.where(m > -math.inf, m, 0.0)
+        lse = (z - m0).exp().sum(1, keepdim=True).log() + m0
+        zl = z.gather(1, at)
+        loss = torch.where(here[:, None], torch.where(zl > -math.inf, lse - zl, math.inf), 0.0)[:, 0]
+        p = torch.where(lse > -math.inf, (z - lse).exp(), 0.0)
+        mark = torch.zeros_like(p).scatter_(1, at, (zl > -math.inf).double())
+        g = torch.where(here, self.g.double(), 0.0)[:, None]
+        dz = g * (p - mark)
+        share = torch.where(mark > 0, 1 - p, p)
+        e_dz = g.abs() * (p + share * (mark > 0)) * (2 * e_row + 110 * U)
+        half = 2.0 ** -8 if self.dtype == B.BF16 else 4 * U
+        out = {"loss": loss, "da": dz @ w, "dw": dz.t() @ a, "db": dz.sum(0)}
+        wide, finite = (dz.abs() * half + e_dz), torch.where(torch.isfinite(loss), loss, 0.0)
+        tol = {"loss": 2 * e_row[:, 0] + 110 * U * (1 + finite.abs()), "db": (e_dz + (self.N / 32 + 80) * U * dz.abs()).sum(0)}
+        sums = lambda n: 4 * (n / 16 + 70) * U  # noqa: E731
+        rounding = 2.0 ** -8 if self.g_dtype == B.BF16 else U
+        tol["da"] = (wide + sums(self.K) * dz.abs()) @ w.abs() + rounding * out["da"].abs()
+        tol["dw"] = (wide + sums(self.N) * dz.abs()).t() @ torch.where(torch.isfinite(a), a, 0.0).abs() + rounding * out["dw"].abs()
+        return out, tol
+
+    def check(self, want=("da", "dw", "db")):
+        out, tol = self.reference()
+        for k in ("loss",) + tuple(want):
+            got = getattr(self, k).double()
+            assert torch.equal(torch.isinf(got), torch.isinf(out[k])) and not torch.isnan(got).any(), k
+            f = torch.isfinite(out[k])
+            over = ((got - out[k]).abs() - tol[k])[f]
+            assert over.numel() == 0 or over.max() <= 1e-30, (k, float(over.max()))
+            # and the whole of it: roundings have either sign
+            norm = out[k][f].norm()
+            if norm > 0 and got.numel() > 200:
+                limit = (6e-3 if k != "loss" and k != "db" and self.dtype == B.BF16 else 2e-5)
+                assert (got - out[k])[f].norm() <= limit * norm, (k, float((got - out[k])[f].norm() / norm))
+        return self
+
+
+TYPES = [(B.F32, B.F32), (B.BF16, B.BF16), (B.BF16, B.F32)]
+SIZES = [(1, 1, 1), (1, 64, 2), (2, 3, 1), (3, 7, 5), (64, 128, 256), (65, 64, 257), (63, 130, 255), (128, 192, 64), (129, 66, 300), (257, 256, 513), (300, 200, 700), (1, 4096, 1000),
+         (100, 4096, 1000), (5, 512, 40000), (700, 1000, 14), (1000, 33, 3000), (33, 2048, 129), (4, 1024, 10007)]
+
+
+@pytest.mark.parametrize("dtype,g_dtype", TYPES)
+@pytest.mark.parametrize("N,In,K", SIZES)
+def test_loss_and_gradients(dtype, g_dtype, N, In, K):
+    Xent(dtype, N, In, K, N + In + K, g_dtype=g_dtype, bias=K % 2 == 0).run().check()
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("N,In,K", [(8200, 64, 17000), (4100, 70, 20011), (8192, 130, 9000)])
+def test_classes_in_pieces(dtype, N, In, K):
+    Xent(dtype, N, In, K, 3, masked=0.1).run().check()
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("N,In,K", [(70, 128, 300), (40, 1024, 600), (3, 24, 9)])
+def test_masks(dtype, N, In, K):
+    c = Xent(dtype, N, In, K, 4, masked=0.5)
+    c.labels[0] = int(torch.nonzero(c.bias == -math.inf)[0])
+    c.run().check()
+    assert c.loss[0] == math.inf
+    c.bias[:] = -math.inf                      # nothing is left
+    c.run().check()
+    assert (c.stats == -math.inf).all() and (c.da == 0).all() and (c.dw == 0).all() and (c.db == 0).all()
+    c.bias[K - 1] = 0.5                        # one class is
+    c.labels[:] = K - 1
+    c.run().check()
+    assert (c.loss == 0).all() and (c.da == 0).all() and (c.dw == 0).all()
+    c.bias[:] = -3.4028234663852886e38         # the type's lowest number masks nothing by itself
+    c.run()
+    assert torch.allclose(c.loss, torch.full_like(c.loss, math.log(K)), rtol=1e-6)       # (all scores round to it)
+    c.bias[K // 2] = 0.0
+    c.labels[:] = K // 2
+    c.run()
+    assert (c.loss == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("N,In,K", [(70, 128, 300), (40, 1024, 600)])
+def test_rows_without_a_label_have_no_part(dtype, N, In, K):
+    c = Xent(dtype, N, In, K, 5)
+    c.labels[torch.arange(N) % 3 == 0] = -1
+    c.labels[1], c.labels[4], c.labels[7] = 2 ** 31 - 1, -2 ** 31, K
+    c.labels[5] = 2                       # with a weight of zero
+    c.g[5] = 0
+    out = ~((c.labels >= 0) & (c.labels < K))
+    c.run().check()
+    dw, db = c.dw.clone(), c.db.clone()
+    assert (c.loss[out] == 0).all() and (c.da[out] == 0).all() and (c.da[5] == 0).all()
+    for bad in (math.nan, math.inf):
+        c.a[out] = bad
+        c.a[5] = bad
+        c.run()
+        assert torch.equal(c.dw, dw) and torch.equal(c.db, db) and (c.da[out] == 0).all() and (c.da[5] == 0).all() and (c.loss[out] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("N,In,K", [(70, 128, 300), (40, 1024, 600)])
+def test_nan_and_infinite_scores(dtype, N, In, K):
+    c = Xent(dtype, N, In, K, 6)
+    c.labels[:] = 7
+    c.run()
+    loss, da = c.loss.clone(), c.da.clone()
+    c.a[2, 5] = math.nan
+    c.run()
+    rest = torch.arange(N, device="cuda") != 2
+    assert torch.isnan(c.loss[2]) and torch.isnan(c.da[2]).all() and torch.equal(c.loss[rest], loss[rest]) and torch.equal(c.da[rest], da[rest])
+    assert torch.isnan(c.db).all() and torch.isnan(c.dw).all()
+    c.a[2, 5] = 1.0
+    c.bias[9] = math.inf
+    c.run()
+    assert torch.isnan(c.loss).all()
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("N,In,K", [(8, 64, 40), (8, 1024, 40), (200, 256, 1000)])
+def test_labels_that_are_all_but_certain_keep_their_digits(dtype, N, In, K):
+    # scores by the bias alone: losses from 1e-20 on, exact but for exp, log1p and expm1
+    c = Xent(dtype, N, In, K, 7)
+    c.a.zero_()
+    c.labels[:] = 3
+    c.g[:] = 1.0
+    for gap in (1.0, 10.0, 20.0, 46.0):
+        c.bias.fill_(-gap)
+        c.bias[3] = 0.0
+        c.run()
+        want = math.log1p((K - 1) * math.exp(-gap))
+        # (K - 1 terms of 4 u and their sum)
+        assert ((c.loss.double() / want - 1).abs() <= 120 * U).all(), gap
+        assert abs(float(c.db[3]) / (N * math.expm1(-want)) - 1) <= (200 + N / 8) * U, gap
+
+
+def test_gradient_against_differences():
+    c = Xent(B.F32, 7, 33, 50, 8, masked=0.1)
+    c.run()
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    here = (c.labels >= 0) & (c.labels < c.K)
+    here &= ~torch.isinf(c.loss)
+    c.g = torch.where(here, c.g, 0.0)
+    c.run()
+
+    def loss(a, w, b):
+        z = a @ w.t() + b
+        lse = torch.logsumexp(z, 1)
+        zl = z.gather(1, c.labels.long().clamp(0, c.K - 1)[:, None])[:, 0]
+        return torch.where(here, c.g.double() * (lse - zl), 0.0).sum()
+
+    at = (c.a.double(), c.w.double(), c.bias.double())
+    for i, grad in enumerate((c.da, c.dw, c.db)):
+        way = torch.randn(at[i].shape, generator=gen, device="cuda", dtype=torch.float64)
+        h = 1e-5
+        up, down = (loss(*[t + s * h * way if k == i else t for k, t in enumerate(at)]) for s in (1, -1))
+        got = (grad.double() * way).sum()
+        # differences leave h^2 of a third derivative and 1e-16 / h; fp32 gradients 1e-6 of the sum of magnitudes
+        assert abs((up - down) / (2 * h) - got) <= 1e-5 * (grad.double() * way).abs().sum() + 1e-8
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("N,In,K", [(70, 128, 300), (100, 1024, 1000)])
+def test_parts_of_the_gradient_other_streams_and_twice_the_same(dtype, N, In, K):
+    c = Xent(dtype, N, In, K, 9).run()
+    whole = {k: getattr(c, k).clone() for k in ("loss", "da", "dw", "db")}
+    for want in (("da",), ("dw",), ("db",), ("da", "db")):
+        c.run(want)
+        assert all(torch.equal(getattr(c, k), whole[k]) for k in want)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        c.run()
+    assert all(torch.equal(getattr(c, k), v) for k, v in whole.items())
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("N,In,K", [(70, 128, 300), (100, 1024, 1000)])
+def test_recorded_in_a_graph(dtype, N, In, K):
+    c = Xent(dtype, N, In, K, 10).run()
+    ws = ws_bytes(max(B.vgg_fc_xent_workspace_bytes(dtype, N, In, K), B.vgg_fc_xent_bwd_workspace_bytes(dtype, N, In, K)))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        B.vgg_fc_xent(dtype, N, In, K, c.a, c.w, c.bias, c.labels, c.loss, c.stats, ws)
+        B.vgg_fc_xent_bwd(dtype, dtype, N, In, K, c.a, c.w, c.bias, c.labels, c.stats, c.g, c.da, c.dw, c.db, ws)
+    for seed in (11, 12, 13):
+        other = Xent(dtype, N, In, K, seed).run()
+        for k in ("a", "w", "bias", "labels", "g"):
+            getattr(c, k).copy_(getattr(other, k))
+        ws.fill_(0xFF)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(getattr(c, k), getattr(other, k)) for k in ("loss", "da", "dw", "db"))
+
+
+def test_weights_past_32_bit_offsets():
+    # 4.9 GB of weights; the reference in pieces
+    N, In, K = 3, 4096, 600011
+    c = Xent(B.BF16, N, In, K, 14)
+    c.labels = torch.tensor([K - 1, 5, 524288], dtype=torch.int32, device="cuda")
+    c.g = torch.tensor([1.0, 0.5, 2.0], device="cuda")
+    c.run()
+    z = torch.cat([c.a.double() @ c.w[k:k + 50000].double().t() for k in range(0, K, 50000)], 1) + c.bias.double()
+    lse = torch.logsumexp(z, 1, keepdim=True)
+    want = (lse - z.gather(1, c.labels.long()[:, None]))[:, 0]
+    assert ((c.loss.double() - want).abs() <= 2e-5 * want).all()
+    dz = (z - lse).exp()
+    dz[torch.arange(N), c.labels.long()] -= 1
+    dz *= c.g.double()[:, None]
+    da = sum(dz[:, k:k + 50000] @ c.w[k:k + 50000].double() for k in range(0, K, 50000))
+    assert (c.da.double() - da).norm() <= 6e-3 * da.norm()
+    assert (c.db.double() - dz.sum(0)).norm() <= 2e-5 * dz.sum(0).norm()
+    for k0 in (0, 262144, 524288, K - 300):
+        part = dz[:, k0:k0 + 300].t() @ c.a.double()
+        assert (c.dw[k0:k0 + 300].double() - part).norm() <= 6e-3 * part.norm()
