@@ -24,7 +24,7 @@ struct Rows {
     Drop drop;
 };
 
-// A team of LANES threads has a row, U groups of eight neighbouring values each: group u LANES + thread.  Teams of less than a workgroup
+// A team of LANES threads has a row, U groups of eight neighbouring values to a thread: group u LANES + thread.  Teams of less than a workgroup
 // take a row each of its 256 threads'; teams of several waves exchange their sums through LDS, one barrier a row.
 constexpr int kPlace = 64;    // floats of LDS for the sums of up to 16 waves, twice
 template <int LANES> constexpr int kBlock = LANES < 256 ? 256 : LANES;
@@ -46,35 +46,84 @@ template <int LANES> __device__ __forceinline__ void team_sums(float &a, float &
     }
 }
 
-// The row's mean and the sum of the squares around it: those of a wave's values, then of the waves.  A wave has `count` of the row's C
-// values, v[u][k] the n[u] first ones of this lane's groups.
-template <int LANES, int U> __device__ __forceinline__ void team_moments(const float (&v)[U][8], const int (&n)[U], int C, int turn, float &mean, float &m2)
-{
-    constexpr int W = LANES / 64, L = LANES < 64 ? LANES : 64;
-    int count = C;
-    if constexpr (W > 1) {
-        count = 0;
-        const int first = (threadIdx.x >> 6) * 512;
+// A lane's share of a row: U groups of eight columns, those that are there, and, of the C % 8 columns behind the last whole group, one in
+// each of the first lanes.  Groups that are not there are read as the first one and left out of sums: no load hangs on a branch, which
+// would cost registers that the rows need.
+template <int LANES, int U> struct Columns {
+    int C, groups, rest, lane;
+    __device__ __forceinline__ Columns(int C_, int lane_) : C(C_), groups(C_ / 8), rest(C_ - C_ / 8 * 8), lane(lane_) {}
+    __device__ __forceinline__ int group(int u) const { return u * LANES + lane; }
+    __device__ __forceinline__ bool has(int u) const { return group(u) < groups; }
+    __device__ __forceinline__ int at(int u) const { return has(u) ? group(u) * 8 : 0; }
+    __device__ __forceinline__ bool has_rest() const { return lane < rest; }
+    __device__ __forceinline__ int at_rest() const { return has_rest() ? groups * 8 + lane : 0; }
+    // how many columns this wave's lanes have
+    __device__ __forceinline__ int of_wave() const
+    {
+        if constexpr (LANES <= 64) return C;
+        const int first = lane & ~63;
+        int n = first ? 0 : rest;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int left = C - u * LANES * 8 - first;
-            count += left < 0 ? 0 : left < 512 ? left : 512;
+            const int left = groups - u * LANES - first;
+            n += 8 * (left < 0 ? 0 : left < 64 ? left : 64);
         }
+        return n;
     }
-    float s = 0.f;
+};
+// Of the bits that this lane's groups are kept by (a function of u), those of the group that the columns behind the last whole one begin:
+// teams within a wave have them from the lane whose place that group would be.
+template <int LANES, int U, typename F>
+__device__ __forceinline__ unsigned bits_of_rest(const Columns<LANES, U> &cols, const Drop &drop, int row, F bits)
+{
+    if (!drop.state) return 0xff;
+    if constexpr (LANES <= 64 && U > 0) {
+        unsigned mine = 0;
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) mine = cols.groups / LANES == u ? bits(u) : mine;
+        return __shfl(mine, cols.groups % LANES, LANES);
+    } else
+        return cols.lane < 8 ? Philox(drop).kept(cols.groups, row, drop) : 0;
+}
+constexpr int at_least_one(int u) { return u ? u : 1; }
+
+// The compiler computes these here, and not where they are used next: it would put a row's groups off until all of their numbers are in
+// registers at once.
+__device__ __forceinline__ void settle(float (&v)[8])
+{
+    asm volatile("" : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]), "+v"(v[4]), "+v"(v[5]), "+v"(v[6]), "+v"(v[7]));
+}
+__device__ __forceinline__ void settle(float &a, float &b) { asm volatile("" : "+v"(a), "+v"(b)); }
+
+// The row's mean and the sum of the squares around it: those of a wave's values, then of the waves.  in: this lane's groups, one: the column
+// behind them.
+template <typename T, int LANES, int U>
+__device__ __forceinline__ void team_moments(const Columns<LANES, U> &cols, Eight<T> (&in)[at_least_one(U)], float one, int count, float each_of_wave, float each, int turn, float &mean, float &m2)
+{
+    constexpr int W = LANES / 64, L = LANES < 64 ? LANES : 64;
+    float s = cols.has_rest() ? one : 0.f;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) s += v[u][k];          // (values past the row are zeros)
-    mean = count ? team_sum<L>(s) / (float)count : 0.f;
-    m2 = 0.f;
+    for (int u = 0; u < U; ++u) {
+        float t = 0.f;
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+        for (int k = 0; k < 8; ++k) t += in[u].get(k);
+        s += cols.has(u) ? t : 0.f;
+        if constexpr (U > 1) settle(s, t);
+    }
+    mean = team_sum<L>(s) * each_of_wave;
+    m2 = cols.has_rest() ? (one - mean) * (one - mean) : 0.f;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        float t = 0.f;
+        in[u].forget();
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-            const float d = v[u][k] - mean;
-            m2 = k < n[u] ? __builtin_fmaf(d, d, m2) : m2;
+            const float d = in[u].get(k) - mean;
+            t = __builtin_fmaf(d, d, t);
         }
+        m2 += cols.has(u) ? t : 0.f;
+        if constexpr (U > 1) settle(m2, t);
+    }
     m2 = team_sum<L>(m2);
     if constexpr (W > 1) {
         __shared__ float part[2][W][3];
@@ -86,22 +135,13 @@ template <int LANES, int U> __device__ __forceinline__ void team_moments(const f
         float all = 0.f;
 #pragma unroll
         for (int w = 0; w < W; ++w) all = __builtin_fmaf(part[turn][w][0], part[turn][w][1], all);
-        mean = all / (float)C;
+        mean = all * each;
         m2 = 0.f;
 #pragma unroll
         for (int w = 0; w < W; ++w) {
             const float d = part[turn][w][1] - mean;
             m2 += __builtin_fmaf(part[turn][w][0] * d, d, part[turn][w][2]);
         }
-    }
-}
-
-template <int LANES, int U> __device__ __forceinline__ void groups_of_row(int lane, int C, int (&n)[U])
-{
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int left = C - (u * LANES + lane) * 8;
-        n[u] = left < 0 ? 0 : left < 8 ? left : 8;
     }
 }
 
@@ -117,54 +157,60 @@ __device__ __forceinline__ void load_columns(const float *p, int c, int n, float
 template <typename T, int LANES, int U>
 __global__ __launch_bounds__(kBlock<LANES>) void layer_norm_kernel(Rows r, const T *__restrict__ x, T *y)
 {
-    constexpr int TEAMS = kBlock<LANES> / LANES;
-    constexpr bool KEEP = !(LANES == 1024 && U == 4 && sizeof(T) == 4);     // gamma and beta in registers (128 of them at 1024 threads)
-    const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES;
-    int n[U];
-    groups_of_row<LANES, U>(lane, r.C, n);
-    float gamma[U][8], beta[U][8];
-    if constexpr (KEEP)
+    constexpr int TEAMS = kBlock<LANES> / LANES, V = at_least_one(U);
+    const int lane = threadIdx.x % LANES, team = TEAMS == 1 ? 0 : threadIdx.x / LANES;
+    const Columns<LANES, U> cols(r.C, lane);
+    const int count = cols.of_wave();
+    const float each = 1.f / (float)r.C, each_of_wave = 1.f / (float)(count ? count : 1);
+    float gamma[V][8], beta[V][8], gamma1 = 1.f, beta1 = 0.f;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            load_columns(r.gamma, (u * LANES + lane) * 8, n[u], 1.f, gamma[u]);
-            load_columns(r.beta, (u * LANES + lane) * 8, n[u], 0.f, beta[u]);
-        }
+    for (int u = 0; u < U; ++u) {
+        load_columns(r.gamma, cols.at(u), 8, 1.f, gamma[u]);
+        load_columns(r.beta, cols.at(u), 8, 0.f, beta[u]);
+    }
+    if (r.gamma) gamma1 = r.gamma[cols.at_rest()];
+    if (r.beta) beta1 = r.beta[cols.at_rest()];
     int turn = 0;
+    Eight<T> in[V];
+    T one;
+    auto row_at = [&](int row) __attribute__((always_inline)) { return x + (size_t)(row < r.N ? row : r.N - 1) * r.ldx; };
+    const T *from = row_at(blockIdx.x * TEAMS + team);
+#pragma unroll
+    for (int u = 0; u < U; ++u) in[u].load(from + cols.at(u), 8);
+    one = from[cols.at_rest()];
     // (all lanes stay: sums go over neighbouring ones)
     for (int base = blockIdx.x * TEAMS; base < r.N; base += gridDim.x * TEAMS, turn ^= 1) {
         const int row = base + team;
         const bool there = row < r.N;
-        Eight<T> in[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) in[u].load(x + (there ? (size_t)row * r.ldx + (u * LANES + lane) * 8 : 0), there ? n[u] : 0);
-        float v[U][8], mean, m2;
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[u][k] = in[u].get(k);
-        team_moments<LANES, U>(v, n, r.C, turn, mean, m2);
-        const float rstd = 1.f / sqrtf(m2 / (float)r.C + r.eps);
-        if (!there) continue;
-        if (r.stats && lane == 0) { r.stats[2 * (size_t)row] = mean; r.stats[2 * (size_t)row + 1] = rstd; }
+        const float v1 = Elem<T>::load(&one);
+        float mean, m2;
+        team_moments<T, LANES, U>(cols, in, v1, count, each_of_wave, each, turn, mean, m2);
+        const float rstd = __builtin_amdgcn_rsqf(__builtin_fmaf(m2, each, r.eps)), scale = r.drop.state ? r.drop.scale : 1.f;
+        from = row_at(row + gridDim.x * TEAMS);
+        if (r.stats && lane == 0 && there) { r.stats[2 * (size_t)row] = mean; r.stats[2 * (size_t)row + 1] = rstd; }
+        T *to = y + (size_t)(there ? row : 0) * r.ldy;
+        unsigned kept[V];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if constexpr (!KEEP) {
-                load_columns(r.gamma, (u * LANES + lane) * 8, n[u], 1.f, gamma[u]);
-                load_columns(r.beta, (u * LANES + lane) * 8, n[u], 0.f, beta[u]);
-            }
-            unsigned keep = 0xff;
-            float scale = 1.f;
-            if (r.drop.state) {
-                keep = Philox(r.drop).kept(u * LANES + lane, row, r.drop.bar);
-                scale = r.drop.scale;
-            }
+            const unsigned keep = kept[u] = r.drop.state ? Philox(r.drop).kept(cols.group(u), row, r.drop) : 0xff;
             Eight<T> out;
+            float o[8];
+            in[u].forget();
+            if constexpr (U > 1) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const float w = __builtin_fmaf((v[u][k] - mean) * rstd, gamma[u][k], beta[u][k]) * scale;
-                out.set(k, keep >> k & 1 ? w : 0.f);
+                const float w = __builtin_fmaf((in[u].get(k) - mean) * rstd, gamma[u][k], beta[u][k]) * scale;
+                o[k] = keep >> k & 1 ? w : 0.f;
             }
-            out.store(y + (size_t)row * r.ldy + (u * LANES + lane) * 8, n[u]);
+            out.set(o);
+            in[u].load(from + cols.at(u), 8);          // the next row's values, while this one's leave
+            if (there && cols.has(u)) out.store(to + cols.at(u), 8);
+        }
+        if (cols.rest) {
+            const unsigned keep = bits_of_rest(cols, r.drop, row, [&](int u) { return kept[u]; });
+            const float w = __builtin_fmaf((v1 - mean) * rstd, gamma1, beta1) * scale;
+            one = from[cols.at_rest()];
+            if (there && cols.has_rest()) Elem<T>::store(to + cols.at_rest(), keep >> (lane & 7) & 1 ? w : 0.f);
         }
     }
 }
@@ -211,13 +257,15 @@ __global__ __launch_bounds__(1024) void layer_norm_long_kernel(Rows r, const T *
             float gamma[8], beta[8];
             load_columns(r.gamma, c, n, 1.f, gamma);
             load_columns(r.beta, c, n, 0.f, beta);
-            const unsigned keep = r.drop.state ? Philox(r.drop).kept(c / 8, row, r.drop.bar) : 0xff;
+            const unsigned keep = r.drop.state ? Philox(r.drop).kept(c / 8, row, r.drop) : 0xff;
             const float scale = r.drop.state ? r.drop.scale : 1.f;
+            float o[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const float w = __builtin_fmaf((in.get(k) - mean) * rstd, gamma[k], beta[k]) * scale;
-                out.set(k, keep >> k & 1 ? w : 0.f);
+                o[k] = keep >> k & 1 ? w : 0.f;
             }
+            out.set(o);
             out.store(y + (size_t)row * r.ldy + c, n);
         }
     }
@@ -234,113 +282,211 @@ __device__ __forceinline__ Share share_of(float x, float dy, float gamma, float 
     return s;
 }
 
+// dgamma and dbeta of 64 columns of all rows by one workgroup: 32 rows at a time, a thread's eight columns.
+template <typename T, typename G>
+__device__ __forceinline__ void gradients_of_columns(const Rows &r, const T *__restrict__ x, const G *__restrict__ dy, float *dgamma, float *dbeta, int tile, float *lds)
+{
+    const int at = threadIdx.x & 7, first = threadIdx.x >> 3, c = (tile * 8 + at) * 8, n = r.C - c < 0 ? 0 : r.C - c < 8 ? r.C - c : 8;
+    const float scale = r.drop.state ? r.drop.scale : 1.f;
+    float sum[2][8] = {};
+    for (int row = first; row < r.N; row += 32) {
+        Eight<T> xs;
+        Eight<G> gs;
+        xs.load(x + (size_t)row * r.ldx + c, n);
+        gs.load(dy + (size_t)row * r.ldy + c, n);
+        const float mean = r.stats[2 * (size_t)row], rstd = r.stats[2 * (size_t)row + 1];
+        const unsigned keep = r.drop.state ? Philox(r.drop).kept(c / 8, row, r.drop) : 0xff;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const Share s = share_of(xs.get(k), gs.get(k), 1.f, mean, rstd, keep >> k & 1, scale);
+            sum[1][k] += s.g;
+            sum[0][k] = __builtin_fmaf(s.g, s.xh, sum[0][k]);
+        }
+    }
+    // [32 rows][2][64 columns]
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) lds[first * 129 + h * 64 + at * 8 + k] = sum[h][k];
+    __syncthreads();
+    if (threadIdx.x >= 128) return;
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < 32; ++k) s += lds[k * 129 + threadIdx.x];
+    float *to = threadIdx.x < 64 ? dgamma : dbeta;
+    const int col = tile * 64 + (threadIdx.x & 63);
+    if (to && col < r.C) to[col] = s;
+}
+constexpr int kColumnsLds = 32 * 129 * 4;
+// Up to this many rows the gradients of gamma and beta are taken by columns, in workgroups of the same launch, which read the rows once more
+// (out of L2), instead of from the rows' workgroups by another launch.
+constexpr int kFewRows = 256;
+
 // The gradients' sums over a workgroup's rows go to part [workgroup][2][C] (dgamma, dbeta), or, where there is only one, to where they
 // belong.
 template <typename T, typename G, int LANES, int U>
 __global__ __launch_bounds__(kBlock<LANES>) void layer_norm_bwd_kernel(Rows r, const T *__restrict__ x, const G *dy, G *dx, float *dgamma, float *dbeta,
-                                                                       float *part, int relu_mask)
+                                                                       float *part, int relu_mask, int row_blocks)
 {
-    // teams of several waves: the waves' sums, then gamma, where U is 4 (128 registers do not hold it at 1024 threads); else what the teams have to add up
+    // teams of several waves: the waves' sums, then gamma, where U is 7 (the registers do not hold it); else what the teams have to add up
     extern __shared__ __align__(16) float lds[];
     float *lds_gamma = lds + kPlace;
-    constexpr int TEAMS = kBlock<LANES> / LANES;
-    constexpr bool IN_LDS = LANES == 1024 && U == 4;
-    const int lane = threadIdx.x % LANES, team = threadIdx.x / LANES;
-    int n[U];
-    groups_of_row<LANES, U>(lane, r.C, n);
-    float gamma[IN_LDS ? 1 : U][8], at_gamma[U][8], at_beta[U][8];
+    if constexpr (kBlock<LANES> == 256)
+        if ((int)blockIdx.x >= row_blocks) return gradients_of_columns<T, G>(r, x, dy, dgamma, dbeta, blockIdx.x - row_blocks, lds);
+    constexpr int TEAMS = kBlock<LANES> / LANES, V = at_least_one(U);
+    constexpr bool IN_LDS = U == 7;
+    const int lane = threadIdx.x % LANES, team = TEAMS == 1 ? 0 : threadIdx.x / LANES;
+    const Columns<LANES, U> cols(r.C, lane);
+    float gamma[IN_LDS ? 1 : V][8], at_gamma[V][8], at_beta[V][8], gamma1 = 1.f, at_gamma1 = 0.f, at_beta1 = 0.f;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         if constexpr (IN_LDS) {
             float g[8];
-            load_columns(r.gamma, (u * LANES + lane) * 8, n[u], 1.f, g);
+            load_columns(r.gamma, cols.at(u), 8, 1.f, g);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) lds_gamma[(u * LANES + lane) * 8 + k] = g[k];       // (read by this thread only)
+            for (int k = 0; k < 8; ++k) lds_gamma[cols.group(u) * 8 + k] = g[k];       // (read by this thread only)
         } else
-            load_columns(r.gamma, (u * LANES + lane) * 8, n[u], 1.f, gamma[u]);
+            load_columns(r.gamma, cols.at(u), 8, 1.f, gamma[u]);
 #pragma unroll
         for (int k = 0; k < 8; ++k) at_gamma[u][k] = at_beta[u][k] = 0.f;
     }
-    auto gamma_of = [&](int u, int k) __attribute__((always_inline)) { return IN_LDS ? lds_gamma[(u * LANES + lane) * 8 + k] : gamma[IN_LDS ? 0 : u][k]; };
+    if (r.gamma) gamma1 = r.gamma[cols.at_rest()];
+    auto gamma_of = [&](int u, int k) __attribute__((always_inline)) { return IN_LDS ? lds_gamma[cols.group(u) * 8 + k] : gamma[IN_LDS ? 0 : u][k]; };
     const float scale = r.drop.state ? r.drop.scale : 1.f, each = 1.f / (float)r.C;
     int turn = 0;
-    for (int base = blockIdx.x * TEAMS; base < r.N; base += gridDim.x * TEAMS, turn ^= 1) {
+    Eight<T> xs[V];
+    Eight<G> gs[V];
+    const T *from_x;
+    const G *from_g;
+    T one_x;
+    G one_g;
+    auto aim = [&](int row) __attribute__((always_inline)) {
+        const size_t at = row < r.N ? row : r.N - 1;
+        from_x = x + at * r.ldx;
+        from_g = dy + at * r.ldy;
+    };
+    aim(blockIdx.x * TEAMS + team);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        xs[u].load(from_x + cols.at(u), 8);
+        gs[u].load(from_g + cols.at(u), 8);
+    }
+    one_x = from_x[cols.at_rest()];
+    one_g = from_g[cols.at_rest()];
+    for (int base = blockIdx.x * TEAMS; base < r.N; base += row_blocks * TEAMS, turn ^= 1) {
         const int row = base + team;
         const bool there = row < r.N;
-        Eight<T> xs[U];
-        Eight<G> gs[U];
-        unsigned keep[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int c = (u * LANES + lane) * 8, m = there ? n[u] : 0;
-            xs[u].load(x + (there ? (size_t)row * r.ldx + c : 0), m);
-            gs[u].load(dy + (there ? (size_t)row * r.ldy + c : 0), m);
-        }
-        const float mean = there ? r.stats[2 * (size_t)row] : 0.f, rstd = there ? r.stats[2 * (size_t)row + 1] : 0.f;
+        unsigned kept[(U + 4) / 4] = {};         // eight bits a group
+        const size_t row_there = there ? row : r.N - 1;
+        const float mean = r.stats[2 * row_there], rstd = r.stats[2 * row_there + 1];
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            keep[u] = r.drop.state ? Philox(r.drop).kept(u * LANES + lane, row, r.drop.bar) : 0xff;
-            if (!there) keep[u] = 0;
+            const unsigned keep = !there ? 0 : r.drop.state ? Philox(r.drop).kept(cols.group(u), row, r.drop) : 0xff;
+            kept[u / 4] |= keep << 8 * (u % 4);
+            if constexpr (U > 1) {
+                xs[u].forget();
+                gs[u].forget();
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            float t1 = 0.f, t2 = 0.f;
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const Share s = share_of(xs[u].get(k), gs[u].get(k), gamma_of(u, k), mean, rstd, k < n[u] && keep[u] >> k & 1, scale);
+                const Share s = share_of(xs[u].get(k), gs[u].get(k), gamma_of(u, k), mean, rstd, keep >> k & 1, scale);
                 at_beta[u][k] += s.g;
                 at_gamma[u][k] = __builtin_fmaf(s.g, s.xh, at_gamma[u][k]);
-                s1 += s.gg;
-                s2 = __builtin_fmaf(s.gg, s.xh, s2);
+                t1 += s.gg;
+                t2 = __builtin_fmaf(s.gg, s.xh, t2);
             }
+            s1 += cols.has(u) ? t1 : 0.f;
+            s2 += cols.has(u) ? t2 : 0.f;
+            if constexpr (U > 1) {
+                settle(at_gamma[u]);
+                settle(at_beta[u]);
+                settle(s1, s2);
+            }
+        }
+        Share rest = {};
+        const float v1 = Elem<T>::load(&one_x);
+        if (cols.rest) {
+            const unsigned bits = bits_of_rest(cols, r.drop, row, [&](int u) { return kept[u / 4] >> 8 * (u % 4); }), keep = there ? bits : 0;
+            rest = share_of(v1, Elem<G>::load(&one_g), gamma1, mean, rstd, keep >> (lane & 7) & 1, scale);
+            at_beta1 += rest.g;
+            at_gamma1 = __builtin_fmaf(rest.g, rest.xh, at_gamma1);
+            s1 += cols.has_rest() ? rest.gg : 0.f;
+            s2 += cols.has_rest() ? rest.gg * rest.xh : 0.f;
         }
         team_sums<LANES>(s1, s2, turn, reinterpret_cast<float2 *>(lds));
         s1 *= each;
         s2 *= each;
-        if (!there) continue;
+        aim(row + row_blocks * TEAMS);
+        G *to = dx + row_there * r.lddx;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             Eight<G> out;
+            float o[8];
+            xs[u].forget();
+            gs[u].forget();
+            if constexpr (U > 1) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const float v = xs[u].get(k);
-                const Share s = share_of(v, gs[u].get(k), gamma_of(u, k), mean, rstd, keep[u] >> k & 1, scale);
+                const Share s = share_of(v, gs[u].get(k), gamma_of(u, k), mean, rstd, kept[u / 4] >> (8 * (u % 4) + k) & 1, scale);
                 const float d = rstd * (s.gg - s1 - s.xh * s2);
-                out.set(k, !relu_mask || v > 0.f ? d : 0.f);
+                o[k] = !relu_mask || v > 0.f ? d : 0.f;
             }
-            out.store(dx + (size_t)row * r.lddx + (u * LANES + lane) * 8, n[u]);
+            out.set(o);
+            xs[u].load(from_x + cols.at(u), 8);          // the next row's values, while this one's leave
+            gs[u].load(from_g + cols.at(u), 8);
+            if (there && cols.has(u)) out.store(to + cols.at(u), 8);
+        }
+        if (cols.rest) {
+            const float d = rstd * (rest.gg - s1 - rest.xh * s2);
+            one_x = from_x[cols.at_rest()];
+            one_g = from_g[cols.at_rest()];
+            if (there && cols.has_rest()) Elem<G>::store(to + cols.at_rest(), !relu_mask || v1 > 0.f ? d : 0.f);
         }
     }
-    if (!part && !dgamma && !dbeta) return;
+    if (row_blocks < (int)gridDim.x || (!part && !dgamma && !dbeta)) return;
     float *to_gamma = part ? part + (size_t)blockIdx.x * 2 * r.C : dgamma, *to_beta = part ? part + (size_t)blockIdx.x * 2 * r.C + r.C : dbeta;
     if constexpr (TEAMS == 1) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int c = (u * LANES + lane) * 8;
+            if (!cols.has(u)) continue;
             Eight<float> e;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) e.set(k, at_gamma[u][k]);
-            if (to_gamma) e.store(to_gamma + c, n[u]);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) e.set(k, at_beta[u][k]);
-            if (to_beta) e.store(to_beta + c, n[u]);
+            e.set(at_gamma[u]);
+            if (to_gamma) e.store(to_gamma + cols.at(u), 8);
+            e.set(at_beta[u]);
+            if (to_beta) e.store(to_beta + cols.at(u), 8);
+        }
+        if (cols.has_rest()) {
+            if (to_gamma) to_gamma[cols.at_rest()] = at_gamma1;
+            if (to_beta) to_beta[cols.at_rest()] = at_beta1;
         }
     } else {
-        constexpr int COLS = LANES * U * 8;     // [TEAMS][2][COLS]
+        constexpr int COLS = LANES * U * 8 + 8;     // [TEAMS][2][COLS], the columns behind the last group in the last eight
         float *mine = lds + team * 2 * COLS;
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int k = 0; k < 8; k += 4) {
-                const int c = (u * LANES + lane) * 8 + k;
+                const int c = cols.group(u) * 8 + k;
                 *reinterpret_cast<f32x4 *>(mine + c) = f32x4{at_gamma[u][k], at_gamma[u][k + 1], at_gamma[u][k + 2], at_gamma[u][k + 3]};
                 *reinterpret_cast<f32x4 *>(mine + COLS + c) = f32x4{at_beta[u][k], at_beta[u][k + 1], at_beta[u][k + 2], at_beta[u][k + 3]};
             }
+        if (lane < 8) {
+            mine[COLS - 8 + lane] = at_gamma1;
+            mine[2 * COLS - 8 + lane] = at_beta1;
+        }
         __syncthreads();
         for (int c = threadIdx.x; c < 2 * COLS; c += kBlock<LANES>) {
-            const int col = c < COLS ? c : c - COLS;
+            const int in = c < COLS ? c : c - COLS, behind = in - (COLS - 8);
+            const bool there = behind >= 0 ? behind < cols.rest : in < cols.groups * 8;
             float s = 0.f;
 #pragma unroll
             for (int t = 0; t < TEAMS; ++t) s += lds[t * 2 * COLS + c];
             float *to = c < COLS ? to_gamma : to_beta;
-            if (to && col < r.C) to[col] = s;
+            if (to && there) to[behind >= 0 ? cols.groups * 8 + behind : in] = s;
         }
     }
 }
@@ -362,7 +508,7 @@ __global__ __launch_bounds__(1024) void layer_norm_bwd_sums_kernel(Rows r, const
             gs.load(dy + (size_t)row * r.ldy + c, n);
             float gamma[8], t1 = 0.f, t2 = 0.f;
             load_columns(r.gamma, c, n, 1.f, gamma);
-            const unsigned keep = r.drop.state ? Philox(r.drop).kept(c / 8, row, r.drop.bar) : 0xff;
+            const unsigned keep = r.drop.state ? Philox(r.drop).kept(c / 8, row, r.drop) : 0xff;
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const Share s = share_of(xs.get(k), gs.get(k), gamma[k], mean, rstd, k < n && keep >> k & 1, scale);
@@ -393,7 +539,8 @@ __global__ __launch_bounds__(256) void layer_norm_bwd_long_kernel(Rows r, const 
         Eight<G> gs, out;
         xs.load(x + (size_t)row * r.ldx + c, n);
         gs.load(dy + (size_t)row * r.ldy + c, n);
-        const unsigned keep = r.drop.state ? Philox(r.drop).kept(c / 8, row, r.drop.bar) : 0xff;
+        const unsigned keep = r.drop.state ? Philox(r.drop).kept(c / 8, row, r.drop) : 0xff;
+        float o[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             const float v = xs.get(k);
@@ -401,37 +548,36 @@ __global__ __launch_bounds__(256) void layer_norm_bwd_long_kernel(Rows r, const 
             at_beta[k] += s.g;
             at_gamma[k] = __builtin_fmaf(s.g, s.xh, at_gamma[k]);
             const float d = rstd * (s.gg - s1 - s.xh * s2);
-            out.set(k, !relu_mask || v > 0.f ? d : 0.f);
+            o[k] = !relu_mask || v > 0.f ? d : 0.f;
         }
+        out.set(o);
         out.store(dx + (size_t)row * r.lddx + c, n);
     }
     if (!part || n == 0) return;
     Eight<float> e;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) e.set(k, at_gamma[k]);
+    e.set(at_gamma);
     e.store(part + (size_t)range * 2 * r.C + c, n);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) e.set(k, at_beta[k]);
+    e.set(at_beta);
     e.store(part + (size_t)range * 2 * r.C + r.C + c, n);
 }
 
-// part [parts][2][C] added up in order: 64 columns to a workgroup, sixteen ranges of parts, then these.
+// part [parts][2][C] added up in order: 16 columns to a workgroup, 64 ranges of parts, then these.
 __global__ __launch_bounds__(1024) void layer_norm_join_kernel(const float *__restrict__ part, int parts, int C, float *dgamma, float *dbeta)
 {
-    __shared__ float sums[16][64];
-    const int at = threadIdx.x & 63, slice = threadIdx.x >> 6;
-    const long col = (long)blockIdx.x * 64 + at, all = 2l * C;
+    __shared__ float sums[64][17];
+    const int at = threadIdx.x & 15, slice = threadIdx.x >> 4;
+    const long col = (long)blockIdx.x * 16 + at, all = 2l * C;
     float s = 0.f;
     if (col < all)
-        for (int p = slice; p < parts; p += 16) s += part[(size_t)p * all + col];
+        for (int p = slice; p < parts; p += 64) s += part[(size_t)p * all + col];
     sums[slice][at] = s;
     __syncthreads();
-    if (slice || col >= all) return;
-    s = 0.f;
-#pragma unroll
-    for (int k = 0; k < 16; ++k) s += sums[k][at];
-    float *to = col < C ? dgamma : dbeta;
-    if (to) to[col < C ? col : col - C] = s;
+    // a wave's 64 lanes have a column's 64 ranges
+    const long mine = (long)blockIdx.x * 16 + (threadIdx.x >> 6);
+    s = team_sum<64>(sums[threadIdx.x & 63][threadIdx.x >> 6]);
+    if ((threadIdx.x & 63) || mine >= all) return;
+    float *to = mine < C ? dgamma : dbeta;
+    if (to) to[mine < C ? mine : mine - C] = s;
 }
 
 // A thread has UNITS groups of eight columns, 256 apart.
@@ -453,18 +599,21 @@ __global__ __launch_bounds__(256) void dropout_kernel(int C, int groups, FastDiv
     }
 #pragma unroll
     for (int u = 0; u < kDropUnits; ++u) {
-        const unsigned keep = drop.state ? Philox(drop).kept(group[u], row[u], drop.bar) : 0xff;
+        const unsigned keep = drop.state ? Philox(drop).kept(group[u], row[u], drop) : 0xff;
+        float o[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[u].set(k, !(keep >> k & 1) ? 0.f : drop.state ? v[u].get(k) * drop.scale : v[u].get(k));
+        for (int k = 0; k < 8; ++k) o[k] = !(keep >> k & 1) ? 0.f : drop.state ? v[u].get(k) * drop.scale : v[u].get(k);
+        v[u].set(o);
         v[u].store(y + (size_t)row[u] * ldy + (size_t)group[u] * 8, n[u]);
     }
 }
 
 // Which team a row of C values takes: the smallest that holds it.
-constexpr int kLongest = 32768;
+constexpr int kLongest = 28672;
 
 template <typename F> int by_team(int C, F f)
 {
+    if (C < 8) return f(std::integral_constant<int, 8>{}, std::integral_constant<int, 0>{});
     if (C <= 64) return f(std::integral_constant<int, 8>{}, std::integral_constant<int, 1>{});
     if (C <= 128) return f(std::integral_constant<int, 16>{}, std::integral_constant<int, 1>{});
     if (C <= 256) return f(std::integral_constant<int, 32>{}, std::integral_constant<int, 1>{});
@@ -472,17 +621,19 @@ template <typename F> int by_team(int C, F f)
     if (C <= 1024) return f(std::integral_constant<int, 64>{}, std::integral_constant<int, 2>{});
     if (C <= 2048) return f(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
     if (C <= 4096) return f(std::integral_constant<int, 256>{}, std::integral_constant<int, 2>{});
-    if (C <= 8192) return f(std::integral_constant<int, 256>{}, std::integral_constant<int, 4>{});
-    if (C <= 16384) return f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{});
-    return f(std::integral_constant<int, 1024>{}, std::integral_constant<int, 4>{});
+    if (C <= 8192) return f(std::integral_constant<int, 512>{}, std::integral_constant<int, 2>{});
+    if (C <= 16384) return f(std::integral_constant<int, 512>{}, std::integral_constant<int, 4>{});
+    return f(std::integral_constant<int, 512>{}, std::integral_constant<int, 7>{});
 }
-// Workgroups that run at once: four of 256 threads to a compute unit, or one of 1024.
-inline int blocks_at_once(int block) { return 256 * (1024 / block); }
-inline int lanes_of(int C) { return C <= 64 ? 8 : C <= 128 ? 16 : C <= 256 ? 32 : C <= 1024 ? 64 : C <= 8192 ? 256 : 1024; }
+// Workgroups that run at once: four of 256 threads to a compute unit, or one of 512.
+inline int blocks_at_once(int block) { return block == 256 ? 1024 : 256; }
+inline int lanes_of(int C) { return C <= 64 ? 8 : C <= 128 ? 16 : C <= 256 ? 32 : C <= 1024 ? 64 : C <= 4096 ? 256 : 512; }
 inline int least(long a, long b) { return (int)(a < b ? a : b); }
 
 // Parts that a backward call's gradients of gamma and beta are summed in.
-bool bwd_is_long(int dtype, int g_dtype, int C) { return C > kLongest || (C > kLongest / 2 && (dtype == VGG_F32 || g_dtype == VGG_F32)); }
+bool bwd_is_long(int dtype, int g_dtype, int C) { return C > kLongest || (C > 16384 && (dtype == VGG_F32 || g_dtype == VGG_F32)); }
+// ... and whether they are taken by columns, in the rows' launch (not where dx takes the place of what they read).
+bool bwd_by_columns(int dtype, int g_dtype, int N, int C) { return N <= kFewRows && C <= 4096 && !bwd_is_long(dtype, g_dtype, C); }
 int bwd_parts(int dtype, int g_dtype, int N, int C)
 {
     if (bwd_is_long(dtype, g_dtype, C)) {
@@ -513,9 +664,9 @@ int backward_of(const Rows &r, int dtype, int g_dtype, const void *x, const void
     const T *from = static_cast<const T *>(x);
     const G *dyp = static_cast<const G *>(dy);
     G *dxp = static_cast<G *>(dx);
-    const bool sums = dgamma || dbeta, is_long = bwd_is_long(dtype, g_dtype, r.C);
+    const bool sums = dgamma || dbeta, columns = sums && dx != dy && dx != x && bwd_by_columns(dtype, g_dtype, r.N, r.C), is_long = bwd_is_long(dtype, g_dtype, r.C);
     const int parts = bwd_parts(dtype, g_dtype, r.N, r.C);
-    float *row_sums = static_cast<float *>(ws), *part = sums && (parts > 1 || is_long) ? row_sums + (is_long ? 2 * (size_t)((r.N + 1) & ~1) : 0) : nullptr;
+    float *row_sums = static_cast<float *>(ws), *part = sums && !columns && (parts > 1 || is_long) ? row_sums + (is_long ? 2 * (size_t)((r.N + 1) & ~1) : 0) : nullptr;
     int rc = VGG_OK;
     if (is_long) {
         const int tiles = (r.C + 2047) / 2048;
@@ -525,17 +676,19 @@ int backward_of(const Rows &r, int dtype, int g_dtype, const void *x, const void
     } else
         rc = by_team(r.C, [&](auto lanes, auto u) {
             constexpr int LANES = decltype(lanes)::value, U = decltype(u)::value, TEAMS = kBlock<LANES> / LANES;
-            if constexpr (LANES == 1024 && U == 4 && (sizeof(T) == 4 || sizeof(G) == 4)) return (int)VGG_ERR_UNSUPPORTED;     // (is_long)
+            if constexpr (U == 7 && (sizeof(T) == 4 || sizeof(G) == 4)) return (int)VGG_ERR_UNSUPPORTED;     // (is_long)
             else {
                 auto *kernel = &layer_norm_bwd_kernel<T, G, LANES, U>;
-                const size_t lds = (TEAMS > 1 ? (size_t)TEAMS * 2 * LANES * U * 8 : kPlace + (LANES == 1024 && U == 4 ? kLongest : 0)) * 4;
+                size_t lds = (TEAMS > 1 ? (size_t)TEAMS * 2 * (LANES * U * 8 + 8) : kPlace + (U == 7 ? kLongest : 0)) * 4;
                 if (lds > 65536 && !raise_lds_limit(reinterpret_cast<const void *>(kernel))) return (int)VGG_ERR_LAUNCH;
-                kernel<<<parts, kBlock<LANES>, lds, s>>>(r, from, dyp, dxp, part ? nullptr : dgamma, part ? nullptr : dbeta, part, relu_mask);
+                if (columns && lds < (size_t)kColumnsLds) lds = kColumnsLds;
+                const int grid = parts + (columns ? (r.C + 63) / 64 : 0);
+                kernel<<<grid, kBlock<LANES>, lds, s>>>(r, from, dyp, dxp, part ? nullptr : dgamma, part ? nullptr : dbeta, part, relu_mask, parts);
                 return (int)VGG_OK;
             }
         });
     if (rc != VGG_OK || (rc = launch_status()) != VGG_OK || !part) return rc;
-    layer_norm_join_kernel<<<(int)((2l * r.C + 63) / 64), 1024, 0, s>>>(part, parts, r.C, dgamma, dbeta);
+    layer_norm_join_kernel<<<(int)((2l * r.C + 15) / 16), 1024, 0, s>>>(part, parts, r.C, dgamma, dbeta);
     return launch_status();
 }
 
