@@ -462,7 +462,7 @@ int vgg_fc_xent(int dtype, int N, int In, int K, const void *a, const void *w, c
  * Each of the three may be NULL, not all.  da and dw are in g_dtype (`dtype`, or VGG_F32)
  * and overlap nothing that is read.  stats are vgg_fc_xent's of the same
  * activations, weights and bias.  The scores are formed again, in pieces of
- * the classes whose dz fits 256 MB of workspace (or 256 classes).  bf16: dz is
+ * the classes that take up to 512 MB of workspace (or 256 classes).  bf16: dz is
  * rounded to bf16 where it enters the two products, as in vgg_fc_bwd, not in
  * db; sums are fp32.  Masked classes have no gradient.  Rows without a label
  * or with g_loss 0 have the gradient 0 and no part in dw and db, whatever

@@ -8,6 +8,7 @@
 // The three products are one kernel: C[col][row] = sum_k A[row][k] B[col][k], where an operand lies by its rows or by the contraction
 // index (which is then read transposed out of LDS).  bf16 operands are multiplied as they are, fp32 ones in three bf16 parts (f32x3.h).
 #include "common.h"
+#include "dropout.h"
 #include "exp_of.h"
 #include "f32x3.h"
 #include "wave.h"
@@ -19,8 +20,9 @@ namespace vgg {
 namespace {
 
 constexpr int kTA = 256;      // rows of C in a tile
-constexpr int kStep = 64;     // contraction indices of a stage: 128 bytes of a row
-constexpr size_t kPieceBytes = 256u << 20;   // what a piece of the classes may take of the workspace
+constexpr int kStep = 64;     // contractions are whole multiples of this many indices
+constexpr size_t kPieceBytes = 512u << 20;   // what a piece of the classes may take of the workspace
+constexpr int kFewRows = 16;                 // rows up to which dw is written by its own kernel
 constexpr int kTileStride = 528;             // bytes from row to row of 256 bf16 numbers in LDS
 
 enum { kStore, kStats, kGrad };
@@ -86,90 +88,121 @@ __device__ __forceinline__ void wave_sync()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-__host__ __device__ constexpr int stages_of(int tn) { return tn == 256 ? 2 : 3; }
+// A stage is 64 contraction indices of bf16 operands (128 bytes of a row), or 32 of the three parts of fp32 ones (64 bytes of a row of each).
+__host__ __device__ constexpr int stage_indices(int pl) { return pl == 3 ? 32 : 64; }
+__host__ __device__ constexpr int operand_lds(int pl, int rows) { return pl == 3 ? (rows * 192 + 8191) / 8192 * 8192 : rows * 128; }
+__host__ __device__ constexpr int stage_lds(int pl, int tn) { return operand_lds(pl, kTA) + operand_lds(pl, tn); }
+__host__ __device__ constexpr int stages_of(int pl, int tn) { return pl == 3 || tn == 256 ? 2 : 3; }
 // LDS of a tile: its stages, or what its end turns round in it
-__host__ __device__ constexpr int lds_of(int tn, int mode)
+struct Example { float m, log_s, g; int label; };   // what the end of a tile knows of a column
+__host__ __device__ constexpr int main_lds_of(int pl, int tn, int mode, int stages)
 {
-    const int run = stages_of(tn) * (kTA + tn) * 128, stored = 8 * 32 * (tn == 64 ? 144 : tn == 128 ? 272 : 528), graded = tn * kTileStride;
-    const int end = mode == kStore ? stored : mode == kGrad ? graded : 0;
+    const int run = (stages < stages_of(pl, tn) ? stages : stages_of(pl, tn)) * stage_lds(pl, tn), stored = 8 * 32 * (tn == 64 ? 144 : tn == 128 ? 272 : 528);
+    const int end = mode == kStore ? stored : mode == kGrad ? tn * kTileStride : 8 * tn * (int)sizeof(Sums);
     return run > end ? run : end;
 }
+// ... and behind that the tile's biases and examples
+__host__ __device__ constexpr int lds_of(int pl, int tn, int mode, int stages) { return main_lds_of(pl, tn, mode, stages) + (mode == kStore ? 0 : kTA * 4 + tn * 16); }
 
 template <bool A_TR, bool B_TR, int TN, int PL, int MODE>
 __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
 {
-    extern __shared__ __align__(16) char lds[];   // [STAGES][A: 256 x 128 bytes, B: TN x 128 bytes]
+    extern __shared__ __align__(16) char lds[];   // [STAGES][A, B]
     // eight waves, WA x WB of them, BX x BY blocks of 32 x 32 each
-    constexpr int STAGES = stages_of(TN), WB = TN == 256 ? 4 : TN == 128 ? 2 : 1, WA = 8 / WB, BX = kTA / 32 / WA, BY = TN / 32 / WB;
-    constexpr int HALF = kTA * 128, STAGE = (kTA + TN) * 128, CA = kTA / 64, CB = TN / 64, COPIES = CA + CB;
+    constexpr int KS = stage_indices(PL), STAGES = stages_of(PL, TN), WB = TN == 256 ? 4 : TN == 128 ? 2 : 1, WA = 8 / WB, BX = kTA / 32 / WA, BY = TN / 32 / WB;
+    constexpr int HALF = operand_lds(PL, kTA), STAGE = stage_lds(PL, TN), CA = HALF / 8192, CB = (STAGE - HALF) / 8192, COPIES = CA + CB;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int mt = (p.rows + kTA - 1) / kTA, nt = (p.cols + TN - 1) / TN;
     const int unit = spread(blockIdx.x, gridDim.x), split = unit / (mt * nt), in_all = unit - split * (mt * nt);
     // eight tiles down, then one to the right
     const int wide = 8 * nt, group = in_all / wide, in = in_all - group * wide, down = mt - group * 8 < 8 ? mt - group * 8 : 8;
     const int ti = group * 8 + in % down, tj = in / down;
-    const int s0 = (int)((long)p.steps * split / p.splits), ks = (int)((long)p.steps * (split + 1) / p.splits) - s0, total = PL == 3 ? 6 * ks : ks;
+    const int s0 = (int)((long)p.steps * split / p.splits), total = ((int)((long)p.steps * (split + 1) / p.splits) - s0) * (kStep / KS);
 
-    // Where this thread's copies come from, within a stage; rows and columns that are not there are others that are (what they give is
-    // not used).
-    unsigned from_a[CA], from_b[CB];
-    auto source = [&](const Operand &o, bool tr, int tile0, int q) __attribute__((always_inline)) {
-        const int at = (q * 512 + (int)threadIdx.x) * 16;
+    // Where this thread's copies come from, within a stage of a part; rows and columns that are not there are others that are (what they give
+    // is not used).  By rows: [rows][KS * 2 bytes], the 16-byte segments of a row in an order that puts sixteen rows of one segment in different banks.
+    // By the contraction index: [columns / 64][KS][128 bytes], the halves of every other pair of rows exchanged.
+    constexpr int ROW = KS * 2, FA = PL == 3 ? CA / 3 : CA, FB = PL == 3 ? 1 : CB;
+    unsigned from_a[FA], from_b[FB];
+    auto source = [&](const Operand &o, bool tr, int tile0, int at) __attribute__((always_inline)) {
         if (!tr) {
-            const int r = at >> 7, seg = ((at >> 4) & 7) ^ (r >> 1 & 7);
+            const int r = at / ROW, seg = ((at >> 4) & (ROW / 16 - 1)) ^ (PL == 3 ? r >> 2 & 3 : r >> 1 & 7);
             return (unsigned)((tile0 + r < o.rows ? r : o.rows - 1 - tile0) * (long)o.ld) + seg * 16;
         }
-        const int k = (at >> 7) & 63, col = tile0 * 2 + (at >> 13) * 128 + ((at & 127) ^ (k >> 1 & 1) << 6);   // [TILE / 64][64][128 bytes]
+        const int k = (at >> 7) % KS, col = tile0 * 2 + at / (KS * 128) * 128 + ((at & 127) ^ (k >> 1 & 1) << 6);
         return (unsigned)(k * (long)o.ld) + (col < o.rows ? col : o.rows - 16);
     };
 #pragma unroll
-    for (int q = 0; q < CA; ++q) from_a[q] = source(p.a, A_TR, ti * kTA, q);
+    for (int q = 0; q < FA; ++q) from_a[q] = source(p.a, A_TR, ti * kTA, (q * 512 + (int)threadIdx.x) * 16);
 #pragma unroll
-    for (int q = 0; q < CB; ++q) from_b[q] = source(p.b, B_TR, tj * TN, q);
-    const char *tile_a = p.a.p + (A_TR ? 0 : (size_t)ti * kTA * p.a.ld), *tile_b = p.b.p + (B_TR ? 0 : (size_t)tj * TN * p.b.ld);
-    const size_t step_a = A_TR ? kStep * p.a.ld : kStep * 2, step_b = B_TR ? kStep * p.b.ld : kStep * 2;
+    for (int q = 0; q < FB; ++q) from_b[q] = source(p.b, B_TR, tj * TN, (q * 512 + (int)threadIdx.x) * 16 % (TN * ROW));
+    const size_t step_a = A_TR ? KS * p.a.ld : KS * 2, step_b = B_TR ? KS * p.b.ld : KS * 2;
+    const char *at_a = p.a.p + (A_TR ? 0 : (size_t)ti * kTA * p.a.ld) + (size_t)s0 * (kStep / KS) * step_a;
+    const char *at_b = p.b.p + (B_TR ? 0 : (size_t)tj * TN * p.b.ld) + (size_t)s0 * (kStep / KS) * step_b;
     const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_char *)lds + wave * 1024);
-    // the stage that is copied next: of parts 1 1, then 1 2, 2 1, 2 2, 1 3, 3 1
-    int slot = 0, pair = 0, k_at = s0;
-    const char *at_a, *at_b;
+    const int upper = PL == 3 && TN == 64 ? __builtin_amdgcn_readfirstlane(wave >> 2) : 0;     // (64 columns: two parts of B in a copy)
+    // the stage that is copied next
+    int slot = 0, to_come = p.steps - s0;
     auto aim = [&]() __attribute__((always_inline)) {
-        const unsigned pa = PL == 3 ? 0x201100u >> (4 * pair) & 3 : 0, pb = PL == 3 ? 0x021010u >> (4 * pair) & 3 : 0;
-        at_a = tile_a + k_at * step_a + pa * p.a.plane;
-        at_b = tile_b + k_at * step_b + pb * p.b.plane;
-        if (A_TR && p.a.tail && k_at == p.steps - 1) at_a = p.a.tail;
+        if (A_TR && PL == 1 && p.a.tail && to_come == 1) at_a = p.a.tail;
     };
     aim();
     auto copy_one = [&](int n) __attribute__((always_inline)) {      // of a stage's COPIES
-        const unsigned to = lds0 + slot * STAGE + (n < CA ? n * 8192 : HALF + (n - CA) * 8192), off = n < CA ? from_a[n < CA ? n : 0] : from_b[n < CA ? 0 : n - CA];
-        const char *base = n < CA ? at_a : at_b;
+        const bool is_a = n < CA;
+        const int q = is_a ? n : n - CA;
+        const unsigned to = lds0 + slot * STAGE + n * 8192, off = is_a ? from_a[is_a ? q % FA : 0] : from_b[is_a ? 0 : q % FB];
+        const char *base = is_a ? at_a : at_b;
+        if constexpr (PL == 3) {
+            const int part = is_a ? q / FA : TN == 128 ? q : q == 0 ? upper : 2;
+            base += part * (is_a ? p.a.plane : p.b.plane);
+        }
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(off), "s"(base) : "m0", "memory");
         if (n == COPIES - 1) {
             slot = slot + 1 == STAGES ? 0 : slot + 1;
-            if (++k_at == s0 + ks) { k_at = s0; ++pair; }
+            at_a += step_a;
+            at_b += step_b;
+            --to_come;
             aim();
         }
     };
 
-    f32x16 acc[BX][BY] = {}, first[PL == 3 ? BX : 1][PL == 3 ? BY : 1];
+    // What the tile's end needs of its classes and examples: asked for now, put into LDS then.
+    float own_bias = -INFINITY;
+    Example own = {0.f, 0.f, 0.f, -1};
+    if constexpr (MODE != kStore) {
+        const int row = ti * kTA + (int)threadIdx.x, col = tj * TN + (int)threadIdx.x;
+        if (threadIdx.x < kTA && row < p.classes) own_bias = p.bias ? p.bias[p.class0 + row] : 0.f;
+        if (threadIdx.x < TN && col < p.cols) {
+            const int label = p.labels[col];
+            own.label = (int)((unsigned)label - p.class0);
+            if constexpr (MODE == kGrad) {
+                own.m = p.stats[2 * (size_t)col];
+                own.log_s = p.stats[2 * (size_t)col + 1];
+                own.g = label >= 0 && label < p.all_classes ? p.g[col] : 0.f;
+            }
+        }
+    }
+    f32x16 acc[BX][BY] = {}, small[PL == 3 ? BX : 1][PL == 3 ? BY : 1] = {};     // fp32: the products of first parts, and the others
     const int wi = wave / WB * (BX * 32), wj = wave % WB * (BY * 32);
-    const int rx = lane >> 1 & 7;
+    const int rx = PL == 3 ? lane >> 2 & 3 : lane >> 1 & 7;
     const int s16 = lane & 15, tr_k = 8 * (lane >> 5) + (s16 >> 2), tr_x = s16 >> 3, tr_at = (lane >> 4 & 1) * 32 + (s16 & 3) * 8;
-    // A stage is four steps of 16 contraction indices.  Between a step's products the next step's fragments are read, and in a stage's last
+    // A stage is KK steps of 16 contraction indices.  Between a step's products the next step's fragments are read, and in a stage's last
     // step, after the barrier, the next stage's first fragments and the copies of a stage to come.
-    constexpr int KK = 4, M = BX * BY, R = BX + BY;
-    struct Fragments { bf16x8 a[BX], b[BY]; };
+    constexpr int KK = KS / 16, M = (PL == 3 ? 6 : 1) * BX * BY, R = PL * (BX + BY);
+    struct Fragments { bf16x8 a[PL][BX], b[PL][BY]; };
     auto read_one = [&](int use, int k, int n, Fragments &f) __attribute__((always_inline)) {
-        const bool is_a = n < BX;
-        const int q = is_a ? n : n - BX, w0 = is_a ? wi : wj;
-        const char *from = lds + use * STAGE + (is_a ? 0 : HALF);
+        const int part = n / (BX + BY), m = n % (BX + BY);
+        const bool is_a = m < BX;
+        const int q = is_a ? m : m - BX, w0 = is_a ? wi : wj;
+        const char *from = lds + use * STAGE + (is_a ? part * (kTA * ROW) : HALF + part * (TN * ROW));
         bf16x8 v;
         if (is_a ? A_TR : B_TR) {
             const int c = (w0 >> 5) + q;                 // 64-byte block of a row
-            v = read_transposed(from + (c >> 1) * (64 * 128) + (k * 16 + tr_k) * 128 + (((c & 1) ^ tr_x) << 6) + tr_at);
+            v = read_transposed(from + (c >> 1) * (KS * 128) + (k * 16 + tr_k) * 128 + (((c & 1) ^ tr_x) << 6) + tr_at);
         } else
-            v = *reinterpret_cast<const bf16x8 *>(from + (w0 + (lane & 31) + q * 32) * 128 + (((k * 2 + (lane >> 5)) ^ rx) << 4));
-        if (is_a) f.a[is_a ? q : 0] = v;
-        else f.b[is_a ? 0 : q] = v;
+            v = *reinterpret_cast<const bf16x8 *>(from + (w0 + (lane & 31) + q * 32) * ROW + (((k * 2 + (lane >> 5)) ^ rx) << 4));
+        if (is_a) f.a[part][is_a ? q : 0] = v;
+        else f.b[part][is_a ? 0 : q] = v;
     };
     Fragments f[2];
     int use = 0;
@@ -184,14 +217,17 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
             Fragments &next = f[(k + 1) & 1];
 #pragma unroll
             for (int i = 0; i < M; ++i) {
-                const int x = i / BY, y = i % BY;
+                // (fp32: a sum's next product waits for its last, so the blocks take turns; parts 1 1, 1 2, 2 1, 2 2, 1 3, 3 1)
+                const int pair = i / (BX * BY), x = i % (BX * BY) / BY, y = i % BY;
+                const int pa = PL == 3 ? 0x201100 >> (4 * pair) & 3 : 0, pb = PL == 3 ? 0x021010 >> (4 * pair) & 3 : 0;
                 if (last && reads && i == lead) {
                     // The next stage's copies have landed (those of later ones may be on their way), and all waves have read what they need
                     // of this one, whose place the next copies take.
                     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(copies ? (STAGES - 2) * COPIES : 0) : "memory");
                     use = use + 1 == STAGES ? 0 : use + 1;
                 }
-                acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(g.a[x], g.b[y], acc[x][y], 0, 0, 0);
+                f32x16 &sum = PL == 3 && pair ? small[PL == 3 ? x : 0][PL == 3 ? y : 0] : acc[x][y];
+                sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(g.a[pa][x], g.b[pb][y], sum, 0, 0, 0);
                 if (i >= lead)
 #pragma unroll
                     for (int n = (i - lead) * tasks / (M - lead); n < (i - lead + 1) * tasks / (M - lead); ++n) {
@@ -213,16 +249,6 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
 #pragma unroll
     for (int n = 0; n < R; ++n) read_one(0, 0, n, f[0]);
     int st = 0;
-    if constexpr (PL == 3) {
-        for (; st < ks; ++st) stage(std::true_type{}, std::true_type{});      // (6 ks > ks + STAGES)
-#pragma unroll
-        for (int x = 0; x < BX; ++x)
-#pragma unroll
-            for (int y = 0; y < BY; ++y) {
-                first[x][y] = acc[x][y];
-                acc[x][y] = f32x16{};
-            }
-    }
     for (; st + STAGES < total; ++st) stage(std::true_type{}, std::true_type{});
     for (; st + 1 < total; ++st) stage(std::true_type{}, std::false_type{});
     stage(std::false_type{}, std::false_type{});
@@ -232,7 +258,7 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
 #pragma unroll
             for (int y = 0; y < BY; ++y)
 #pragma unroll
-                for (int v = 0; v < 16; ++v) acc[x][y][v] = join_parts(first[x][y][v], acc[x][y][v]);
+                for (int v = 0; v < 16; ++v) acc[x][y][v] = join_parts(acc[x][y][v], small[x][y][v]);
 
     // Value v of a block: row 8 (v / 4) + 4 (lane / 32) + v % 4, column lane % 32.
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");   // no wave reads operands any more
@@ -284,40 +310,62 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
         }
     } else {
         // scores of this lane: example tj TN + wj + 32 y + lane % 32, class row0 + 32 x + 8 (v / 4) + v % 4 of the piece
-        const int row0 = ti * kTA + wi + 4 * (lane >> 5);
+        float *bias = reinterpret_cast<float *>(lds + main_lds_of(PL, TN, MODE, stages_of(PL, TN)));
+        Example *examples = reinterpret_cast<Example *>(bias + kTA);
+        if (threadIdx.x < kTA) bias[threadIdx.x] = own_bias;
+        if (threadIdx.x < TN) examples[threadIdx.x] = own;
+        __syncthreads();
+        const int row0 = wi + 4 * (lane >> 5);          // of the tile
 #pragma unroll
         for (int x = 0; x < BX; ++x)
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int row = row0 + 32 * x + 8 * (v >> 2) + (v & 3);
-                const float b = row >= p.classes ? -INFINITY : p.bias ? p.bias[p.class0 + row] : 0.f;
+            for (int q = 0; q < 4; ++q) {
+                const f32x4 b = *reinterpret_cast<const f32x4 *>(bias + row0 + 32 * x + 8 * q);     // (-inf past the last class)
 #pragma unroll
-                for (int y = 0; y < BY; ++y) acc[x][y][v] = row >= p.classes ? -INFINITY : acc[x][y][v] + b;
+                for (int y = 0; y < BY; ++y)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) acc[x][y][4 * q + k] += b[k];
             }
+        // the score of this lane's label, if it is among the lane's
+        auto score_at = [&](int y, int label) __attribute__((always_inline)) {
+            float z = -INFINITY;
+            const int rel = label - row0;
+#pragma unroll
+            for (int x = 0; x < BX; ++x)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) z = rel == 32 * x + 8 * (v >> 2) + (v & 3) ? acc[x][y][v] : z;
+            return z;
+        };
+        auto is_here = [&](int label) __attribute__((always_inline)) {
+            const int rel = label - row0;
+            return rel >= 0 && rel < 32 * BX && !(rel & 4);
+        };
         if constexpr (MODE == kStats) {
             Sums *all = reinterpret_cast<Sums *>(lds);    // [WA][TN]
 #pragma unroll
             for (int y = 0; y < BY; ++y) {
-                const int col = tj * TN + wj + 32 * y + (lane & 31);
-                const int label = col < p.cols ? (int)((unsigned)p.labels[col] - p.class0) : -1;
+                if constexpr (TN == 64) if (tj * TN + 32 * y >= p.cols) continue;     // (few rows)
+                const int at = wj + 32 * y + (lane & 31), label = (int)((unsigned)examples[at].label - ti * kTA);
+                const bool here = is_here(label);
+                if (__any(here)) {
+                    const float z = score_at(y, label);
+                    if (here) p.z_label[tj * TN + at] = z;       // (no label: past the last class or column)
+                }
                 Sums s = {-INFINITY, 0.f};
 #pragma unroll
                 for (int x = 0; x < BX; ++x)
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) {
-                        s.m = fmaxf(s.m, acc[x][y][v]);
-                        if (label == row0 + 32 * x + 8 * (v >> 2) + (v & 3) && label < p.classes) p.z_label[col] = acc[x][y][v];
-                    }
-                bool own = s.m > -INFINITY;               // one of the largest does not count
-                const float base = own ? s.m : 0.f;
+                    for (int v = 0; v < 16; ++v) s.m = fmaxf(s.m, acc[x][y][v]);
+                bool fresh = s.m > -INFINITY;               // one of the largest does not count
+                const float base = fresh ? s.m : 0.f;
 #pragma unroll
                 for (int x = 0; x < BX; ++x)
 #pragma unroll
                     for (int v = 0; v < 16; ++v) {
                         const float z = acc[x][y][v], e = exp_of(below(z - base));
-                        const bool it = own && z == s.m;
+                        const bool it = fresh && z == s.m;
                         s.e += it ? 0.f : e;
-                        own = own && !it;
+                        fresh = fresh && !it;
                     }
                 s = joined(s, Sums{__shfl_xor(s.m, 32), __shfl_xor(s.e, 32)});
                 if (lane < 32) all[wave / WB * TN + wj + 32 * y + lane] = s;
@@ -334,23 +382,35 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
             float sum[BX][16] = {};
 #pragma unroll
             for (int y = 0; y < BY; ++y) {
-                const int col = tj * TN + wj + 32 * y + (lane & 31);
-                const int y_label = col < p.cols ? p.labels[col] : -1, label = (int)((unsigned)y_label - p.class0);
-                const float g = y_label >= 0 && y_label < p.all_classes ? p.g[col] : 0.f;
-                const float m = g != 0.f ? p.stats[2 * (size_t)col] : 0.f, log_s = g != 0.f ? p.stats[2 * (size_t)col + 1] : 0.f;
+                if constexpr (TN == 64) if (tj * TN + 32 * y >= p.cols) continue;     // (few rows)
+                const Example e = examples[wj + 32 * y + (lane & 31)];
+                const int label = (int)((unsigned)e.label - ti * kTA);
+                const bool here = is_here(label), none = e.g == 0.f || e.log_s == -INFINITY;     // (-inf: a row without a class)
+                float fixed = 0.f;
+                const bool any = __any(here);
+                if (any) {
+                    const float z = score_at(y, label);
+                    fixed = none || z == -INFINITY ? 0.f : e.g * expm1f((z - e.m) - e.log_s);
+                }
 #pragma unroll
                 for (int x = 0; x < BX; ++x)
 #pragma unroll
                     for (int v = 0; v < 16; ++v) {
-                        const int row = row0 + 32 * x + 8 * (v >> 2) + (v & 3);
-                        const float z = acc[x][y][v], d = (z - m) - log_s;
-                        float share = exp_of(below(d));
-                        if (row == label) share = z > -INFINITY || z != z ? expm1f(d) : 0.f;
-                        // (a row without a class: -inf - -inf)
-                        const float out = g == 0.f || row >= p.classes || log_s == -INFINITY ? 0.f : g * share;
-                        acc[x][y][v] = out;
-                        sum[x][v] += out;
+                        // (bf16: off by |d| 2^-24 of a share that is rounded to 2^-9, either way)
+                        const float d = below((acc[x][y][v] - e.m) - e.log_s), share = PL == 1 ? __builtin_amdgcn_exp2f(d * 1.44269504f) : exp_of(d);
+                        acc[x][y][v] = none ? 0.f : e.g * share;
                     }
+                if (any) {
+                    const int rel = label - row0;
+#pragma unroll
+                    for (int x = 0; x < BX; ++x)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) acc[x][y][v] = rel == 32 * x + 8 * (v >> 2) + (v & 3) ? fixed : acc[x][y][v];
+                }
+#pragma unroll
+                for (int x = 0; x < BX; ++x)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) sum[x][v] += acc[x][y][v];
             }
             // dz, a part at a time: [example][class] in LDS, then runs of 512 bytes
 #pragma unroll
@@ -362,7 +422,7 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
                             const float w0 = acc[x][y][4 * q], w1 = acc[x][y][4 * q + 1], w2 = acc[x][y][4 * q + 2], w3 = acc[x][y][4 * q + 3];
-                            char *to = lds + (wj + 32 * y + (lane & 31)) * kTileStride + (wi + 32 * x + 8 * q + 4 * (lane >> 5)) * 2;
+                            char *to = lds + (wj + 32 * y + (lane & 31)) * kTileStride + (row0 + 32 * x + 8 * q) * 2;
                             if constexpr (PL == 1) store4(reinterpret_cast<bf16_t *>(to), w0, w1, w2, w3);
                             else {
                                 const Parts4 s = split_parts(f32x3_u32x4{__float_as_uint(w0), __float_as_uint(w1), __float_as_uint(w2), __float_as_uint(w3)});
@@ -370,25 +430,37 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
                             }
                         }
                 __syncthreads();
-                for (int at = threadIdx.x; at < TN * 32; at += 512) {
-                    const int col = tj * TN + (at >> 5), row = ti * kTA + (at & 31) * 8;
+#pragma unroll
+                for (int k = 0; k < TN / 16; ++k) {
+                    const int at = k * 512 + threadIdx.x, col = tj * TN + (at >> 5), row = ti * kTA + (at & 31) * 8;
                     if (col < p.cols && row < (int)p.ld_dz)
                         *reinterpret_cast<f32x4 *>(p.dz + part * p.dz_plane + (size_t)col * p.ld_dz + row) =
                             *reinterpret_cast<const f32x4 *>(lds + (at >> 5) * kTileStride + (at & 31) * 16);
                 }
                 __syncthreads();
             }
-            // db: over the 32 lanes that have an example each, then over the waves that share classes
+            // db: over the 32 lanes that have an example each, then over the waves that share classes.  Sixteen sums to a lane become one: at each step a
+            // lane hands half of them to its partner and adds up the other half.
             float *all = reinterpret_cast<float *>(lds);    // [WB][256]
+            const bool odd8 = lane & 8, odd2 = lane & 2, odd1 = lane & 1;
 #pragma unroll
-            for (int x = 0; x < BX; ++x)
+            for (int x = 0; x < BX; ++x) {
+                float h8[8], h4[4], h2[2];
 #pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    float s = sum[x][v];
-#pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor(s, o);
-                    if ((lane & 31) == 0) all[wave % WB * kTA + wi + 4 * (lane >> 5) + 32 * x + 8 * (v >> 2) + (v & 3)] = s;
+                for (int v = 0; v < 8; ++v) {
+                    const auto q = __builtin_amdgcn_permlane16_swap(__float_as_uint(sum[x][v]), __float_as_uint(sum[x][v + 8]), false, false);
+                    const unsigned q0 = q[0], q1 = q[1];
+                    h8[v] = __uint_as_float(q0) + __uint_as_float(q1);
                 }
+#pragma unroll
+                for (int v = 0; v < 4; ++v) h4[v] = (odd8 ? h8[v + 4] : h8[v]) + row_ror<8>(odd8 ? h8[v] : h8[v + 4]);
+#pragma unroll
+                for (int v = 0; v < 2; ++v) h2[v] = (odd2 ? h4[v + 2] : h4[v]) + dpp<0x4E>(odd2 ? h4[v] : h4[v + 2]);
+                float h = (odd1 ? h2[1] : h2[0]) + dpp<0xB1>(odd1 ? h2[0] : h2[1]);
+                h += __shfl_xor(h, 4);
+                const int v = (lane & 16 ? 8 : 0) + (odd8 ? 4 : 0) + (odd2 ? 2 : 0) + (odd1 ? 1 : 0);
+                if (!(lane & 4)) all[wave % WB * kTA + row0 + 32 * x + 8 * (v >> 2) + (v & 3)] = h;
+            }
             __syncthreads();
             if (p.db && threadIdx.x < kTA) {
                 float s = 0.f;
@@ -419,15 +491,15 @@ __global__ __launch_bounds__(256) void xent_lay_kernel(const T *__restrict__ fro
         bf16_t *dst = to + (size_t)row * cols_p + c;
         const T *src = from + (size_t)row * cols + c;
         if constexpr (sizeof(T) == 2) {
-            bf16_t v[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = there && c + k < cols ? src[k] : 0;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) dst[k] = v[k];
+            Eight<bf16_t> v;
+            v.load(there ? src : from, there ? cols - c : 0);
+            *reinterpret_cast<Eight<bf16_t>::u32x4 *>(dst) = v.w;
         } else {
+            Eight<float> e;
+            e.load(there ? src : from, there ? cols - c : 0);
             unsigned v[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = there && c + k < cols ? __float_as_uint(src[k]) : 0u;
+            for (int k = 0; k < 8; ++k) v[k] = __float_as_uint(e.get(k));
             const Parts4 lo = split_parts(f32x3_u32x4{v[0], v[1], v[2], v[3]}), hi = split_parts(f32x3_u32x4{v[4], v[5], v[6], v[7]});
 #pragma unroll
             for (int k = 0; k < 3; ++k) {
@@ -453,20 +525,25 @@ __device__ __forceinline__ void write_loss(Sums s, float z_label, int label, int
     if (stats) { stats[2 * (size_t)row] = s.m; stats[2 * (size_t)row + 1] = log_s; }
 }
 
-// The tiles' sums [tiles][N] of a row: 32 rows to a workgroup, eight runs of tiles each.
+// The tiles' sums [tiles][N] of a row: ROWS rows to a workgroup, 256 / ROWS runs of tiles each.
+template <int ROWS>
 __global__ __launch_bounds__(256) void xent_join_kernel(const Sums *__restrict__ sums, int tiles, int N, int classes, const int32_t *__restrict__ labels,
                                                         const float *__restrict__ z_label, float *loss, float *stats)
 {
-    __shared__ Sums all[8][32];
-    const int at = threadIdx.x & 31, run = threadIdx.x >> 5, row = blockIdx.x * 32 + at;
+    constexpr int RUNS = 256 / ROWS;
+    __shared__ Sums all[RUNS][ROWS];
+    const int at = threadIdx.x % ROWS, run = threadIdx.x / ROWS, row = blockIdx.x * ROWS + at;
     Sums s = {-INFINITY, 0.f};
     if (row < N)
-        for (int t = run; t < tiles; t += 8) s = joined(s, sums[(size_t)t * N + row]);
+#pragma unroll 4
+        for (int t = run; t < tiles; t += RUNS) s = joined(s, sums[(size_t)t * N + row]);
     all[run][at] = s;
-    __syncthreads();
-    if (run || row >= N) return;
 #pragma unroll
-    for (int k = 1; k < 8; ++k) s = joined(s, all[k][at]);
+    for (int half = RUNS / 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (run < half) all[run][at] = s = joined(s, all[run + half][at]);
+    }
+    if (run || row >= N) return;
     const int y = labels[row];
     write_loss(s, y >= 0 && y < classes ? z_label[row] : 0.f, y, classes, loss, stats, row);
 }
@@ -477,21 +554,30 @@ struct Scores {
     int parts, N, classes;
     size_t ld;
     const float *bias;
-    __device__ __forceinline__ float at(int row, int k) const
+    // of four neighbouring classes, -inf past the last
+    __device__ __forceinline__ f32x4 at(int row, int k) const
     {
-        float z = 0.f;
-        for (int q = 0; q < parts; ++q) z += part[((size_t)q * N + row) * ld + k];
-        return bias ? z + bias[k] : z;
+        f32x4 z = {};
+#pragma unroll 8
+        for (int q = 0; q < parts; ++q) z += *reinterpret_cast<const f32x4 *>(part + ((size_t)q * N + row) * ld + k);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) z[j] = k + j < classes ? z[j] + (bias ? bias[k + j] : 0.f) : -INFINITY;
+        return z;
     }
 };
 __global__ __launch_bounds__(256) void xent_rows_kernel(Scores z, const int32_t *__restrict__ labels, float *loss, float *stats)
 {
     __shared__ Sums all[4];
-    const int row = blockIdx.x;
+    __shared__ float z_label;
+    const int row = blockIdx.x, y = labels[row];
     Sums s = {-INFINITY, 0.f};
-    for (int k = threadIdx.x; k < z.classes; k += 256) {
-        const float v = z.at(row, k);
-        s = v == v ? joined(s, Sums{v, 0.f}) : Sums{s.m, v};
+    for (int k = threadIdx.x * 4; k < z.classes; k += 1024) {
+        const f32x4 v = z.at(row, k);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            s = v[j] == v[j] ? joined(s, Sums{v[j], 0.f}) : Sums{s.m, v[j]};
+            if (k + j == y) z_label = v[j];
+        }
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) s = joined(s, Sums{__shfl_xor(s.m, o), __shfl_xor(s.e, o)});
@@ -499,35 +585,98 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(Scores z, const int32_t 
     __syncthreads();
     if (threadIdx.x) return;
     for (int w = 1; w < 4; ++w) s = joined(s, all[w]);
-    const int y = labels[row];
-    write_loss(s, y >= 0 && y < z.classes ? z.at(row, y) : 0.f, y, z.classes, loss, stats, row);
+    write_loss(s, y >= 0 && y < z.classes ? z_label : 0.f, y, z.classes, loss, stats, row);
 }
-// dz [PL][N][ld_dz] of all classes, and db of a range of rows: 256 classes to a workgroup.
+// dz [PL][N][ld_dz] of all classes, and db of a range of rows: 256 classes to a workgroup, four rows at a time.
 template <int PL>
 __global__ __launch_bounds__(256) void xent_grad_kernel(Scores z, const int32_t *__restrict__ labels, const float *__restrict__ stats, const float *__restrict__ g,
                                                         bf16_t *dz, size_t ld_dz, size_t dz_plane, float *db, size_t ld_db)
 {
-    const int k = blockIdx.x * 256 + threadIdx.x;
-    if (k >= (int)ld_dz) return;
+    __shared__ f32x4 sums[4][64];
+    const int k = blockIdx.x * 256 + (threadIdx.x & 63) * 4, r = threadIdx.x >> 6;
     const int r0 = (int)((long)z.N * blockIdx.y / gridDim.y), r1 = (int)((long)z.N * (blockIdx.y + 1) / gridDim.y);
-    float sum = 0.f;
-    for (int row = r0; row < r1; ++row) {
-        const int y = labels[row];
-        const float w = y >= 0 && y < z.classes ? g[row] : 0.f, m = stats[2 * (size_t)row], log_s = stats[2 * (size_t)row + 1];
-        float out = 0.f;
-        if (k < z.classes && w != 0.f && log_s != -INFINITY) {
-            const float v = z.at(row, k), d = (v - m) - log_s;
-            out = w * (k == y ? v > -INFINITY || v != v ? expm1f(d) : 0.f : exp_of(below(d)));
-        }
-        sum += out;
-        if constexpr (PL == 1) dz[(size_t)row * ld_dz + k] = f32_to_bf16(out);
-        else {
-            const Parts4 s = split_parts(f32x3_u32x4{__float_as_uint(out), 0u, 0u, 0u});
+    f32x4 sum = {};
+    if (k < (int)ld_dz)
+        for (int row = r0 + r; row < r1; row += 4) {
+            const int y = labels[row];
+            const float w = y >= 0 && y < z.classes ? g[row] : 0.f, m = stats[2 * (size_t)row], log_s = stats[2 * (size_t)row + 1];
+            f32x4 out = {};
+            if (k < z.classes && w != 0.f && log_s != -INFINITY) {
+                const f32x4 v = z.at(row, k);
 #pragma unroll
-            for (int q = 0; q < 3; ++q) dz[q * dz_plane + (size_t)row * ld_dz + k] = (bf16_t)(s.p[q][0] & 0xffffu);
+                for (int j = 0; j < 4; ++j) {
+                    const float d = (v[j] - m) - log_s;
+                    out[j] = w * (k + j != y ? exp_of(below(d)) : v[j] == -INFINITY ? 0.f : expm1f(d));
+                }
+            }
+            sum += out;
+            bf16_t *to = dz + (size_t)row * ld_dz + k;
+            if constexpr (PL == 1) store4(to, out[0], out[1], out[2], out[3]);
+            else {
+                const Parts4 s = split_parts(f32x3_u32x4{__float_as_uint(out[0]), __float_as_uint(out[1]), __float_as_uint(out[2]), __float_as_uint(out[3])});
+#pragma unroll
+                for (int q = 0; q < 3; ++q) *reinterpret_cast<f32x3_u32x2 *>(to + q * dz_plane) = s.p[q];
+            }
+        }
+    sums[r][threadIdx.x & 63] = sum;
+    __syncthreads();
+    if (r || !db) return;
+#pragma unroll
+    for (int q = 1; q < 4; ++q) sum += sums[q][threadIdx.x];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (k + j < z.classes) db[(size_t)blockIdx.y * ld_db + k + j] = sum[j];
+}
+
+// dw of few rows, a sum of up to NMAX outer products: a thread's eight columns of the activations stay in registers, dz is the same for all
+// threads, and what is left is the write (4 rows, 200003 x 4096 bf16: `kFewRows`).
+template <int PL, int NMAX, typename G>
+__global__ __launch_bounds__(256) void xent_outer_kernel(const bf16_t *__restrict__ a, size_t ld_a, size_t a_plane, const bf16_t *__restrict__ dz, size_t ld_dz,
+                                                         size_t dz_plane, int N, int cols, int classes, G *dw)
+{
+    const int c = (blockIdx.x * 256 + threadIdx.x) * 8, n = cols - c < 0 ? 0 : cols - c < 8 ? cols - c : 8;
+    if (n == 0) return;
+    // (three parts stand for half of a number)
+    float v[NMAX][8];
+#pragma unroll
+    for (int r = 0; r < NMAX; ++r) {
+        const bf16_t *from = a + (r < N ? r : 0) * ld_a + c;          // (laid out in whole stages)
+        Eight<bf16_t> e;
+        e.load(from, 8);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[r][k] = r < N ? e.get(k) : 0.f;
+#pragma unroll
+        for (int part = 1; part < PL; ++part) {
+            e.load(from + part * a_plane, 8);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[r][k] += r < N ? e.get(k) : 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[r][k] *= PL == 3 ? 4.f : 1.f;
+    }
+    const int groups = (classes + 7) / 8, g0 = (int)((long)groups * blockIdx.y / gridDim.y), g1 = (int)((long)groups * (blockIdx.y + 1) / gridDim.y);
+    for (int group = g0; group < g1; ++group) {
+        Eight<bf16_t> w[NMAX][PL];
+#pragma unroll
+        for (int r = 0; r < NMAX; ++r)
+#pragma unroll
+            for (int part = 0; part < PL; ++part) w[r][part].load(dz + part * dz_plane + (r < N ? r : 0) * ld_dz + (size_t)group * 8, 8);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            if (group * 8 + k >= classes) break;
+            float out[8] = {};
+#pragma unroll
+            for (int r = 0; r < NMAX; ++r) {
+                float s = w[r][0].get(k);
+                if constexpr (PL == 3) s += w[r][1].get(k) + w[r][2].get(k);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) out[q] = __builtin_fmaf(s, v[r][q], out[q]);
+            }
+            Eight<G> e;
+            e.set(out);
+            e.store(dw + (size_t)(group * 8 + k) * cols + c, n);
         }
     }
-    if (db && k < z.classes) db[(size_t)blockIdx.y * ld_db + k] = sum;
 }
 
 // out [rows][cols] = the sum of `parts` matrices [rows][ld], `part` elements apart, in order.
@@ -552,10 +701,11 @@ inline long div_up(long a, long b) { return (a + b - 1) / b; }
 
 // Columns of a tile: examples for the scores and da, classes for dw.
 inline int tile_of(int dtype, int cols) { return cols > 128 && dtype == VGG_BF16 ? 256 : cols > 64 ? 128 : 64; }
-// Ranges of a contraction of `steps` stages, where `tiles` do not fill the chip: at least four stages each.
-inline int splits_of(long tiles, int steps)
+// Ranges of a contraction of `steps` stages, where `tiles` do not fill the chip: at least four stages of bf16 each, or two of fp32, which are
+// six times as long.
+inline int splits_of(int dtype, long tiles, int steps)
 {
-    const long most = div_up(steps, 4), want = tiles >= 256 ? 1 : div_up(256, tiles);
+    const long most = div_up(steps, dtype == VGG_BF16 ? 4 : 2), want = tiles >= 256 ? 1 : div_up(256, tiles);
     return (int)(want < most ? want : most);
 }
 
@@ -584,14 +734,21 @@ XentPlan xent_plan(int dtype, int N, int In, int K)
     const int steps = p.InP / kStep;
     // scores of few tiles: their contraction is split, so that all of them have to be kept for a moment
     const long z_tiles = div_up(K, kTA) * n_tiles;
-    p.z_splits = z_tiles < 128 && steps >= 8 ? splits_of(z_tiles, steps) : 0;
+    p.z_splits = z_tiles < 128 && steps >= 8 ? splits_of(dtype, z_tiles, steps) : 0;
     if (p.z_splits == 1) p.z_splits = 0;
     const size_t per_class = (size_t)p.PL * 2 * (p.NP + (p.direct_w ? 0 : p.InP));
     long classes = (long)(kPieceBytes / per_class) / kTA * kTA;
     if (classes < kTA) classes = kTA;
     if (p.z_splits || classes > K) classes = up(K, kTA);
-    p.pieces = (int)div_up(K, classes);
-    p.classes = up(div_up(K, p.pieces), kTA);
+    // as large as they may be, and of the 64 largest sizes the one whose tiles leave least of the chip idle in their last rounds
+    const long all = div_up(K, kTA), largest = classes / kTA < all ? classes / kTA : all;
+    auto rounds = [&](long tiles) { return div_up(tiles * n_tiles, 256); };
+    long best = 0, best_rounds = 0;
+    for (long t = largest; t > 0 && t > largest - 64; --t) {
+        const long r = all / t * rounds(t) + (all % t ? rounds(all % t) : 0);
+        if (!best || r < best_rounds) { best = t; best_rounds = r; }
+    }
+    p.classes = (int)(best * kTA);
     p.pieces = (int)div_up(K, p.classes);
     const int most = p.classes < K ? p.classes : K;
     p.ld_dz = up(most, kStep);
@@ -609,14 +766,14 @@ XentPlan xent_plan(int dtype, int N, int In, int K)
     at = both;
     p.tail_at = take(p.direct_w ? (size_t)kStep * In * 2 : 0);
     p.dz_at = take((size_t)p.PL * 2 * p.NP * p.ld_dz);
-    p.da_splits = splits_of(n_tiles * d_tiles, (int)div_up(most, kStep));
+    p.da_splits = splits_of(dtype, n_tiles * d_tiles, (int)div_up(most, kStep));
     p.da_direct = p.pieces == 1 && p.da_splits == 1;
     p.da_at = take(p.da_direct ? 0 : (size_t)p.da_splits * N * p.InP * 4);
     p.dw_tn = tile_of(dtype, most);
-    p.dw_splits = splits_of(d_tiles * div_up(most, p.dw_tn), p.NP / kStep);
-    p.dw_at = take(p.dw_splits == 1 ? 0 : (size_t)p.dw_splits * most * p.InP * 4);
+    p.dw_splits = splits_of(dtype, d_tiles * div_up(most, p.dw_tn), p.NP / kStep);
+    p.dw_at = take(p.dw_splits == 1 || N <= kFewRows ? 0 : (size_t)p.dw_splits * most * p.InP * 4);
     // rows' ranges that db is summed in
-    p.db_parts = (int)(p.z_splits ? (N < 64 ? 1 : N < 64 * 64 ? div_up(N, 64) : 64) : n_tiles);
+    p.db_parts = (int)(p.z_splits ? div_up(N, N < 512 ? 8 : div_up(N, 64)) : n_tiles);
     p.db_at = take(p.db_parts == 1 ? 0 : (size_t)p.db_parts * p.ld_dz * 4);
     p.backward_bytes = at;
     return p;
@@ -626,7 +783,8 @@ XentPlan xent_plan(int dtype, int N, int In, int K)
 template <bool A_TR, bool B_TR, int TN, int PL, int MODE> int launch_product(const Product &p, hipStream_t s)
 {
     auto *kernel = &xent_product_kernel<A_TR, B_TR, TN, PL, MODE>;
-    constexpr int lds = lds_of(TN, MODE);
+    // (a short contraction has no more stages: more workgroups to a compute unit)
+    const int lds = lds_of(PL, TN, MODE, MODE == kStore ? (kStep / stage_indices(PL)) * (p.steps / p.splits + 1) : stages_of(PL, TN));
     if (lds > 65536 && !raise_lds_limit(reinterpret_cast<const void *>(kernel))) return VGG_ERR_LAUNCH;
     const long grid = div_up(p.rows, kTA) * div_up(p.cols, TN) * p.splits;
     kernel<<<(int)grid, 512, lds, s>>>(p);
@@ -638,6 +796,18 @@ template <bool A_TR, bool B_TR, int MODE> int product(int PL, int tn, const Prod
     return tn == 256   ? launch_product<A_TR, B_TR, 256, 1, MODE>(p, s)
            : tn == 128 ? launch_product<A_TR, B_TR, 128, 1, MODE>(p, s)
                        : launch_product<A_TR, B_TR, 64, 1, MODE>(p, s);
+}
+
+template <int PL, typename G> int outer(int N, const bf16_t *a, size_t ld_a, size_t a_plane, const bf16_t *dz, size_t ld_dz, size_t dz_plane, int cols, int classes, void *dw,
+                                        hipStream_t s)
+{
+    const long across = div_up(cols, 2048), down = div_up(2048, across), most = div_up(classes, 8);
+    const dim3 grid((unsigned)across, (unsigned)(down < most ? down : most));
+    G *to = static_cast<G *>(dw);
+    if (N <= 4) xent_outer_kernel<PL, 4, G><<<grid, 256, 0, s>>>(a, ld_a, a_plane, dz, ld_dz, dz_plane, N, cols, classes, to);
+    else if (N <= 8) xent_outer_kernel<PL, 8, G><<<grid, 256, 0, s>>>(a, ld_a, a_plane, dz, ld_dz, dz_plane, N, cols, classes, to);
+    else xent_outer_kernel<PL, 16, G><<<grid, 256, 0, s>>>(a, ld_a, a_plane, dz, ld_dz, dz_plane, N, cols, classes, to);
+    return launch_status();
 }
 
 int lay(int dtype, const void *from, int rows, int cols, void *to, int rows_p, int cols_p, const int32_t *labels, const float *g, int classes, hipStream_t s)
@@ -713,7 +883,9 @@ int forward(const Call &c, float *loss, float *stats)
         p.sums = sums; p.z_label = z_label;
         if ((rc = product<false, false, kStats>(pl.PL, pl.tn, p, c.s))) return rc;
     }
-    xent_join_kernel<<<(int)div_up(c.N, 32), 256, 0, c.s>>>(sums, (int)div_up(c.K, kTA), c.N, c.K, c.labels, z_label, loss, stats);
+    const int tiles = (int)div_up(c.K, kTA);
+    if (c.N <= 512) xent_join_kernel<1><<<c.N, 256, 0, c.s>>>(sums, tiles, c.N, c.K, c.labels, z_label, loss, stats);
+    else xent_join_kernel<16><<<(int)div_up(c.N, 16), 256, 0, c.s>>>(sums, tiles, c.N, c.K, c.labels, z_label, loss, stats);
     return launch_status();
 }
 
@@ -767,7 +939,15 @@ int backward(const Call &c, int g_dtype, const float *stats, const float *g, voi
             else { q.out = da_part; q.ld = pl.InP; q.part = (size_t)c.N * pl.InP; q.add = piece > 0; }
             if ((rc = product<true, false, kStore>(pl.PL, pl.tn, q, c.s))) return rc;
         }
-        if (dw) {
+        if (dw && c.N <= kFewRows) {
+            void *out = static_cast<char *>(dw) + (size_t)class0 * c.In * gs;
+            const bf16_t *a = reinterpret_cast<const bf16_t *>(c.ws + pl.a_at);
+            const size_t plane = (size_t)pl.NP * pl.InP;
+            rc = pl.PL == 3           ? outer<3, float>(c.N, a, pl.InP, plane, dz, pl.ld_dz, dz_plane, c.In, here, out, c.s)
+                 : g_dtype == VGG_F32 ? outer<1, float>(c.N, a, pl.InP, plane, dz, pl.ld_dz, dz_plane, c.In, here, out, c.s)
+                                      : outer<1, bf16_t>(c.N, a, pl.InP, plane, dz, pl.ld_dz, dz_plane, c.In, here, out, c.s);
+            if (rc) return rc;
+        } else if (dw) {
             Product q = {};
             q.a = {c.ws + pl.a_at, (size_t)pl.InP * 2, a_plane, pl.InP * 2, nullptr};
             q.b = {reinterpret_cast<const char *>(dz), pl.ld_dz * 2, dz_plane * 2, (int)pl.ld_dz * 2, nullptr};
