@@ -6,12 +6,21 @@
 // dz is g expm1(log p), so that a label that is all but certain keeps its digits.
 //
 // The three products are one kernel: C[col][row] = sum_k A[row][k] B[col][k], where an operand lies by its rows or by the contraction
-// index (which is then read transposed out of LDS).  bf16 operands are multiplied as they are, fp32 ones in three bf16 parts (f32x3.h).
+// index (which is then read transposed out of LDS).  bf16 operands are multiplied as they are, fp32 ones in two f16 parts, 22 bits: their
+// products without those of two second parts are off by 2^-22, and are three where three bf16 parts need six.  f16 has few exponents, so
+// each row of activations and weights is laid out in units of a power of two of its own, in which its largest is between 2^14 and 2^15; what
+// is 2^18 times smaller has 22 bits still, and below that 2^-40 of the largest is left out:
+//     a = a' 2^(ea[n] - 14),  w = w' 2^(ew[k] - 14),  z = sum_i a' w' 2^(ea[n] + ew[k] - 28).
+// A contraction needs units that do not depend on its index.  With 2^eg[n] <= |g_loss[n]| < 2 2^eg[n], W = max ew and A = max (ea + eg),
+//     D = dz 2^(-eg[n]) 2^(ew[k] - W) 2^14,   da = sum_k D w' 2^(eg[n] + W - 28),
+//     a" = a 2^(eg[n] - A) 2^14,              dw = sum_n D a" 2^(A + W - ew[k] - 28):
+// a row's da has its digits however small its weight in the loss, and dw loses those of rows that add next to nothing to it.
 #include "common.h"
 #include "dropout.h"
 #include "exp_of.h"
-#include "f32x3.h"
 #include "wave.h"
+
+#include <limits.h>
 
 #include <type_traits>
 
@@ -30,7 +39,6 @@ enum { kStore, kStats, kGrad };
 struct Operand {
     const char *p;
     size_t ld;            // bytes from row to row
-    size_t plane;         // bytes from part to part of fp32 numbers
     int rows;             // by rows: of these; by the contraction index: bytes of a row that are there (a multiple of 16)
     const char *tail;     // by the contraction index: where the last stage's 64 rows lie, if not with the others
 };
@@ -45,7 +53,9 @@ __device__ __forceinline__ Sums joined(Sums a, Sums b)
 
 struct Product {
     Operand a, b;
-    int rows, cols, steps, splits;   // of C; stages of the contraction (of one part); ranges of them
+    int rows, cols, steps, splits;   // of C; the contraction's indices in whole 64s; ranges of them
+    // fp32: C's units, 2^(ea[col] + ew[row] + *more - less[col] - 28), each where it is given
+    const int *ea, *ew, *more[2], *less;
     // kStore: C[col][row], a row of C^T every ld elements, fp32 or bf16; a range's every `part` elements, added to what is there if asked
     void *out;
     size_t ld, part;
@@ -57,11 +67,32 @@ struct Product {
     Sums *sums;                          // kStats: [tiles of classes, of all pieces][N]
     float *z_label;                      // [N]
     const float *stats, *g;              // kGrad: [N][2], [N]
-    bf16_t *dz;                          // [parts][N ...][ld_dz]
-    size_t ld_dz, dz_plane;
+    const int *eg, *w_most;              // fp32: eg, W
+    bf16_t *dz;                          // [N ...][ld_dz], parts side by side
+    int ld_dz;                           // classes of a row
     float *db;                           // [tiles of examples][ld_db]
     size_t ld_db;
 };
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned short u16x4 __attribute__((ext_vector_type(4)));
+
+// Where column c of a row in PL parts lies, in 16-bit numbers: parts of 32 columns side by side.
+template <int PL> __host__ __device__ __forceinline__ size_t column_at(int c, int part) { return PL == 1 ? c : (size_t)(c >> 5) * 64 + part * 32 + (c & 31); }
+// Four numbers in the unit 2^-e, in two f16 parts; of what is not finite the first says it all.
+__device__ __forceinline__ void two_parts(const f32x4 &v, int e, f16x4 (&part)[2])
+{
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float x = ldexpf(v[k], e);
+        part[0][k] = (_Float16)x;
+        const float rest = x - (float)part[0][k];
+        part[1][k] = (_Float16)(__builtin_fabsf(rest) < INFINITY ? rest : 0.f);
+    }
+}
+// e with 2^e <= |v| < 2 2^e; 0 for zeros and what is not finite.
+__device__ __forceinline__ int exponent_of(float v) { return v != 0.f && __builtin_fabsf(v) < INFINITY ? ilogbf(v) : 0; }
 
 typedef __attribute__((address_space(3))) char lds_char;
 
@@ -88,59 +119,56 @@ __device__ __forceinline__ void wave_sync()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// A stage is 64 contraction indices of bf16 operands (128 bytes of a row), or 32 of the three parts of fp32 ones (64 bytes of a row of each).
-__host__ __device__ constexpr int stage_indices(int pl) { return pl == 3 ? 32 : 64; }
-__host__ __device__ constexpr int operand_lds(int pl, int rows) { return pl == 3 ? (rows * 192 + 8191) / 8192 * 8192 : rows * 128; }
-__host__ __device__ constexpr int stage_lds(int pl, int tn) { return operand_lds(pl, kTA) + operand_lds(pl, tn); }
-__host__ __device__ constexpr int stages_of(int pl, int tn) { return pl == 3 || tn == 256 ? 2 : 3; }
+// A stage is 128 bytes of a row: 64 contraction indices of bf16 operands, or both parts of 32 of fp32 ones, which lie side by side.
+__host__ __device__ constexpr int stage_lds(int tn) { return (kTA + tn) * 128; }
+__host__ __device__ constexpr int stages_of(int tn) { return tn == 256 ? 2 : 3; }
 // LDS of a tile: its stages, or what its end turns round in it
-struct Example { float m, log_s, g; int label; };   // what the end of a tile knows of a column
-__host__ __device__ constexpr int main_lds_of(int pl, int tn, int mode, int stages)
+struct Example { float m, log_s, g; int label, ea, eg; };   // what the end of a tile knows of a column
+__host__ __device__ constexpr int main_lds_of(int tn, int mode, int stages)
 {
-    const int run = (stages < stages_of(pl, tn) ? stages : stages_of(pl, tn)) * stage_lds(pl, tn), stored = 8 * 32 * (tn == 64 ? 144 : tn == 128 ? 272 : 528);
+    const int run = (stages < stages_of(tn) ? stages : stages_of(tn)) * stage_lds(tn), stored = 8 * 32 * (tn == 64 ? 144 : tn == 128 ? 272 : 528);
     const int end = mode == kStore ? stored : mode == kGrad ? tn * kTileStride : 8 * tn * (int)sizeof(Sums);
     return run > end ? run : end;
 }
 // ... and behind that the tile's biases and examples
-__host__ __device__ constexpr int lds_of(int pl, int tn, int mode, int stages) { return main_lds_of(pl, tn, mode, stages) + (mode == kStore ? 0 : kTA * 4 + tn * 16); }
+__host__ __device__ constexpr int lds_of(int tn, int mode, int stages) { return main_lds_of(tn, mode, stages) + (mode == kStore ? 0 : kTA * 8 + tn * (int)sizeof(Example)); }
 
 template <bool A_TR, bool B_TR, int TN, int PL, int MODE>
 __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
 {
     extern __shared__ __align__(16) char lds[];   // [STAGES][A, B]
     // eight waves, WA x WB of them, BX x BY blocks of 32 x 32 each
-    constexpr int KS = stage_indices(PL), STAGES = stages_of(PL, TN), WB = TN == 256 ? 4 : TN == 128 ? 2 : 1, WA = 8 / WB, BX = kTA / 32 / WA, BY = TN / 32 / WB;
-    constexpr int HALF = operand_lds(PL, kTA), STAGE = stage_lds(PL, TN), CA = HALF / 8192, CB = (STAGE - HALF) / 8192, COPIES = CA + CB;
+    constexpr int KS = kStep / PL, STAGES = stages_of(TN), WB = TN == 256 ? 4 : TN == 128 ? 2 : 1, WA = 8 / WB, BX = kTA / 32 / WA, BY = TN / 32 / WB;
+    constexpr int HALF = kTA * 128, STAGE = stage_lds(TN), CA = kTA / 64, CB = TN / 64, COPIES = CA + CB;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int mt = (p.rows + kTA - 1) / kTA, nt = (p.cols + TN - 1) / TN;
     const int unit = spread(blockIdx.x, gridDim.x), split = unit / (mt * nt), in_all = unit - split * (mt * nt);
     // eight tiles down, then one to the right
     const int wide = 8 * nt, group = in_all / wide, in = in_all - group * wide, down = mt - group * 8 < 8 ? mt - group * 8 : 8;
     const int ti = group * 8 + in % down, tj = in / down;
-    const int s0 = (int)((long)p.steps * split / p.splits), total = ((int)((long)p.steps * (split + 1) / p.splits) - s0) * (kStep / KS);
+    const int s0 = (int)((long)p.steps * split / p.splits), total = ((int)((long)p.steps * (split + 1) / p.splits) - s0) * PL;
 
-    // Where this thread's copies come from, within a stage of a part; rows and columns that are not there are others that are (what they give
-    // is not used).  By rows: [rows][KS * 2 bytes], the 16-byte segments of a row in an order that puts sixteen rows of one segment in different banks.
-    // By the contraction index: [columns / 64][KS][128 bytes], the halves of every other pair of rows exchanged.
-    constexpr int ROW = KS * 2, FA = PL == 3 ? CA / 3 : CA, FB = PL == 3 ? 1 : CB;
-    unsigned from_a[FA], from_b[FB];
-    auto source = [&](const Operand &o, bool tr, int tile0, int at) __attribute__((always_inline)) {
+    // Where this thread's copies come from, within a stage; rows and columns that are not there are others that are (what they give is not
+    // used).  By rows: [rows][128 bytes], the 16-byte segments of a row in an order that puts sixteen rows of one segment in different banks.  By the
+    // contraction index: [128 bytes of columns][KS][128 bytes], the halves of every other pair of rows exchanged.
+    unsigned from_a[CA], from_b[CB];
+    auto source = [&](const Operand &o, bool tr, int tile0, int q) __attribute__((always_inline)) {
+        const int at = (q * 512 + (int)threadIdx.x) * 16;
         if (!tr) {
-            const int r = at / ROW, seg = ((at >> 4) & (ROW / 16 - 1)) ^ (PL == 3 ? r >> 2 & 3 : r >> 1 & 7);
+            const int r = at >> 7, seg = ((at >> 4) & 7) ^ (r >> 1 & 7);
             return (unsigned)((tile0 + r < o.rows ? r : o.rows - 1 - tile0) * (long)o.ld) + seg * 16;
         }
-        const int k = (at >> 7) % KS, col = tile0 * 2 + at / (KS * 128) * 128 + ((at & 127) ^ (k >> 1 & 1) << 6);
+        const int k = (at >> 7) % KS, col = tile0 * 2 * PL + at / (KS * 128) * 128 + ((at & 127) ^ (k >> 1 & 1) << 6);
         return (unsigned)(k * (long)o.ld) + (col < o.rows ? col : o.rows - 16);
     };
 #pragma unroll
-    for (int q = 0; q < FA; ++q) from_a[q] = source(p.a, A_TR, ti * kTA, (q * 512 + (int)threadIdx.x) * 16);
+    for (int q = 0; q < CA; ++q) from_a[q] = source(p.a, A_TR, ti * kTA, q);
 #pragma unroll
-    for (int q = 0; q < FB; ++q) from_b[q] = source(p.b, B_TR, tj * TN, (q * 512 + (int)threadIdx.x) * 16 % (TN * ROW));
-    const size_t step_a = A_TR ? KS * p.a.ld : KS * 2, step_b = B_TR ? KS * p.b.ld : KS * 2;
-    const char *at_a = p.a.p + (A_TR ? 0 : (size_t)ti * kTA * p.a.ld) + (size_t)s0 * (kStep / KS) * step_a;
-    const char *at_b = p.b.p + (B_TR ? 0 : (size_t)tj * TN * p.b.ld) + (size_t)s0 * (kStep / KS) * step_b;
+    for (int q = 0; q < CB; ++q) from_b[q] = source(p.b, B_TR, tj * TN, q);
+    const size_t step_a = A_TR ? KS * p.a.ld : 128, step_b = B_TR ? KS * p.b.ld : 128;
+    const char *at_a = p.a.p + (A_TR ? 0 : (size_t)ti * kTA * p.a.ld) + (size_t)s0 * PL * step_a;
+    const char *at_b = p.b.p + (B_TR ? 0 : (size_t)tj * TN * p.b.ld) + (size_t)s0 * PL * step_b;
     const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_char *)lds + wave * 1024);
-    const int upper = PL == 3 && TN == 64 ? __builtin_amdgcn_readfirstlane(wave >> 2) : 0;     // (64 columns: two parts of B in a copy)
     // the stage that is copied next
     int slot = 0, to_come = p.steps - s0;
     auto aim = [&]() __attribute__((always_inline)) {
@@ -149,13 +177,8 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
     aim();
     auto copy_one = [&](int n) __attribute__((always_inline)) {      // of a stage's COPIES
         const bool is_a = n < CA;
-        const int q = is_a ? n : n - CA;
-        const unsigned to = lds0 + slot * STAGE + n * 8192, off = is_a ? from_a[is_a ? q % FA : 0] : from_b[is_a ? 0 : q % FB];
+        const unsigned to = lds0 + slot * STAGE + n * 8192, off = is_a ? from_a[is_a ? n : 0] : from_b[is_a ? 0 : n - CA];
         const char *base = is_a ? at_a : at_b;
-        if constexpr (PL == 3) {
-            const int part = is_a ? q / FA : TN == 128 ? q : q == 0 ? upper : 2;
-            base += part * (is_a ? p.a.plane : p.b.plane);
-        }
         asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(off), "s"(base) : "m0", "memory");
         if (n == COPIES - 1) {
             slot = slot + 1 == STAGES ? 0 : slot + 1;
@@ -168,39 +191,45 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
 
     // What the tile's end needs of its classes and examples: asked for now, put into LDS then.
     float own_bias = -INFINITY;
-    Example own = {0.f, 0.f, 0.f, -1};
+    float own_m = 0.f, own_log_s = 0.f, own_g = 0.f;
+    int own_label = -1, own_ea = 0, own_eg = 0, own_ew = 0;
     if constexpr (MODE != kStore) {
         const int row = ti * kTA + (int)threadIdx.x, col = tj * TN + (int)threadIdx.x;
-        if (threadIdx.x < kTA && row < p.classes) own_bias = p.bias ? p.bias[p.class0 + row] : 0.f;
+        if (threadIdx.x < kTA && row < p.classes) {
+            own_bias = p.bias ? p.bias[p.class0 + row] : 0.f;
+            if constexpr (PL == 2) own_ew = p.ew[row];
+        }
         if (threadIdx.x < TN && col < p.cols) {
             const int label = p.labels[col];
-            own.label = (int)((unsigned)label - p.class0);
+            own_label = (int)((unsigned)label - p.class0);
+            if constexpr (PL == 2) own_ea = p.ea[col];
             if constexpr (MODE == kGrad) {
-                own.m = p.stats[2 * (size_t)col];
-                own.log_s = p.stats[2 * (size_t)col + 1];
-                own.g = label >= 0 && label < p.all_classes ? p.g[col] : 0.f;
+                own_m = p.stats[2 * (size_t)col];
+                own_log_s = p.stats[2 * (size_t)col + 1];
+                own_g = label >= 0 && label < p.all_classes ? p.g[col] : 0.f;
+                if constexpr (PL == 2) own_eg = p.eg[col];
             }
         }
     }
-    f32x16 acc[BX][BY] = {}, small[PL == 3 ? BX : 1][PL == 3 ? BY : 1] = {};     // fp32: the products of first parts, and the others
+    f32x16 acc[BX][BY] = {};
     const int wi = wave / WB * (BX * 32), wj = wave % WB * (BY * 32);
-    const int rx = PL == 3 ? lane >> 2 & 3 : lane >> 1 & 7;
+    const int rx = lane >> 1 & 7;
     const int s16 = lane & 15, tr_k = 8 * (lane >> 5) + (s16 >> 2), tr_x = s16 >> 3, tr_at = (lane >> 4 & 1) * 32 + (s16 & 3) * 8;
     // A stage is KK steps of 16 contraction indices.  Between a step's products the next step's fragments are read, and in a stage's last
     // step, after the barrier, the next stage's first fragments and the copies of a stage to come.
-    constexpr int KK = KS / 16, M = (PL == 3 ? 6 : 1) * BX * BY, R = PL * (BX + BY);
+    constexpr int KK = 4 / PL, M = (PL == 2 ? 3 : 1) * BX * BY, R = PL * (BX + BY);
     struct Fragments { bf16x8 a[PL][BX], b[PL][BY]; };
     auto read_one = [&](int use, int k, int n, Fragments &f) __attribute__((always_inline)) {
         const int part = n / (BX + BY), m = n % (BX + BY);
         const bool is_a = m < BX;
         const int q = is_a ? m : m - BX, w0 = is_a ? wi : wj;
-        const char *from = lds + use * STAGE + (is_a ? part * (kTA * ROW) : HALF + part * (TN * ROW));
+        const char *from = lds + use * STAGE + (is_a ? 0 : HALF);
         bf16x8 v;
         if (is_a ? A_TR : B_TR) {
-            const int c = (w0 >> 5) + q;                 // 64-byte block of a row
+            const int c = ((w0 >> 5) + q) * PL + part;                 // 64-byte block of a row
             v = read_transposed(from + (c >> 1) * (KS * 128) + (k * 16 + tr_k) * 128 + (((c & 1) ^ tr_x) << 6) + tr_at);
         } else
-            v = *reinterpret_cast<const bf16x8 *>(from + (w0 + (lane & 31) + q * 32) * ROW + (((k * 2 + (lane >> 5)) ^ rx) << 4));
+            v = *reinterpret_cast<const bf16x8 *>(from + (w0 + (lane & 31) + q * 32) * 128 + (((part * 4 + k * 2 + (lane >> 5)) ^ rx) << 4));
         if (is_a) f.a[part][is_a ? q : 0] = v;
         else f.b[part][is_a ? 0 : q] = v;
     };
@@ -217,17 +246,17 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
             Fragments &next = f[(k + 1) & 1];
 #pragma unroll
             for (int i = 0; i < M; ++i) {
-                // (fp32: a sum's next product waits for its last, so the blocks take turns; parts 1 1, 1 2, 2 1, 2 2, 1 3, 3 1)
-                const int pair = i / (BX * BY), x = i % (BX * BY) / BY, y = i % BY;
-                const int pa = PL == 3 ? 0x201100 >> (4 * pair) & 3 : 0, pb = PL == 3 ? 0x021010 >> (4 * pair) & 3 : 0;
+                // (fp32: the small terms first; a sum's next product waits for its last, so the blocks take turns)
+                const int term = PL == 2 ? i / (BX * BY) : 2, x = i % (BX * BY) / BY, y = i % BY;
                 if (last && reads && i == lead) {
                     // The next stage's copies have landed (those of later ones may be on their way), and all waves have read what they need
                     // of this one, whose place the next copies take.
                     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(copies ? (STAGES - 2) * COPIES : 0) : "memory");
                     use = use + 1 == STAGES ? 0 : use + 1;
                 }
-                f32x16 &sum = PL == 3 && pair ? small[PL == 3 ? x : 0][PL == 3 ? y : 0] : acc[x][y];
-                sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(g.a[pa][x], g.b[pb][y], sum, 0, 0, 0);
+                const bf16x8 ga = g.a[term == 0 ? PL - 1 : 0][x], gb = g.b[term == 1 ? PL - 1 : 0][y];
+                if constexpr (PL == 2) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, ga), __builtin_bit_cast(f16x8, gb), acc[x][y], 0, 0, 0);
+                else acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ga, gb, acc[x][y], 0, 0, 0);
                 if (i >= lead)
 #pragma unroll
                     for (int n = (i - lead) * tasks / (M - lead); n < (i - lead + 1) * tasks / (M - lead); ++n) {
@@ -252,14 +281,6 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
     for (; st + STAGES < total; ++st) stage(std::true_type{}, std::true_type{});
     for (; st + 1 < total; ++st) stage(std::true_type{}, std::false_type{});
     stage(std::false_type{}, std::false_type{});
-    if constexpr (PL == 3)
-#pragma unroll
-        for (int x = 0; x < BX; ++x)
-#pragma unroll
-            for (int y = 0; y < BY; ++y)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) acc[x][y][v] = join_parts(acc[x][y][v], small[x][y][v]);
-
     // Value v of a block: row 8 (v / 4) + 4 (lane / 32) + v % 4, column lane % 32.
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" : : : "memory");   // no wave reads operands any more
     if constexpr (MODE == kStore) {
@@ -267,6 +288,17 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
         constexpr int ROWS = BX * 32, STRIDE = ROWS * 4 + 16, LANES = ROWS / 8;
         char *turned = lds + wave * (32 * STRIDE);
         const int r8 = lane % LANES * 8, row = ti * kTA + wi + r8;
+        int units[8] = {}, of_col[BY] = {};     // exponents of this lane's rows, and of column lane % 32 of a block
+        if constexpr (PL == 2) {
+            const int all = (p.more[0] ? *p.more[0] : 0) + (p.more[1] ? *p.more[1] : 0) - 28;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) units[k] = p.ew && row + k < p.rows ? p.ew[row + k] : 0;
+#pragma unroll
+            for (int y = 0; y < BY; ++y) {
+                const int col = tj * TN + wj + y * 32 + (lane & 31);
+                of_col[y] = all + (col < p.cols ? (p.ea ? p.ea[col] : 0) - (p.less ? p.less[col] : 0) : 0);
+            }
+        }
 #pragma unroll
         for (int y = 0; y < BY; ++y) {
 #pragma unroll
@@ -276,33 +308,38 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
                     *reinterpret_cast<f32x4 *>(turned + (lane & 31) * STRIDE + (x * 32 + 8 * q + 4 * (lane >> 5)) * 4) =
                         f32x4{acc[x][y][4 * q], acc[x][y][4 * q + 1], acc[x][y][4 * q + 2], acc[x][y][4 * q + 3]};
             wave_sync();
-#pragma unroll
-            for (int c = lane / LANES; c < 32; c += 64 / LANES) {
-                const int col = tj * TN + wj + y * 32 + c, n = p.rows - row;
+#pragma unroll 2      // (a tile of a short contraction waits for code)
+            for (int i = 0; i < LANES / 2; ++i) {
+                const int c = i * (64 / LANES) + lane / LANES, col = tj * TN + wj + y * 32 + c, n = p.rows - row;
                 const f32x4 *here = reinterpret_cast<const f32x4 *>(turned + c * STRIDE + r8 * 4);
                 f32x4 lo = here[0], hi = here[1];
+                if constexpr (PL == 2) {
+                    const int e = __shfl(of_col[y], c);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        lo[k] = ldexpf(lo[k], e + units[k]);
+                        hi[k] = ldexpf(hi[k], e + units[k + 4]);
+                    }
+                }
                 if (col < p.cols && n > 0) {
                     const size_t at = (size_t)split * p.part + (size_t)col * p.ld + row;
-                    if (p.bf16) {
-                        bf16_t *to = static_cast<bf16_t *>(p.out) + at;
-                        if (n >= 8 && p.ld % 8 == 0) {
-                            store4(to, lo[0], lo[1], lo[2], lo[3]);
-                            store4(to + 4, hi[0], hi[1], hi[2], hi[3]);
-                        } else
+                    float v[8];
 #pragma unroll
-                            for (int k = 0; k < 8; ++k)
-                                if (k < n) to[k] = f32_to_bf16(k < 4 ? lo[k] : hi[k - 4]);
+                    for (int k = 0; k < 4; ++k) { v[k] = lo[k]; v[k + 4] = hi[k]; }
+                    if (p.bf16) {
+                        Eight<bf16_t> e;
+                        e.set(v);
+                        e.store(static_cast<bf16_t *>(p.out) + at, n);
                     } else {
                         float *to = static_cast<float *>(p.out) + at;
-                        if (n >= 8 && p.ld % 4 == 0) {
-                            f32x4 *to4 = reinterpret_cast<f32x4 *>(to);
-                            if (p.add) { lo += to4[0]; hi += to4[1]; }
-                            to4[0] = lo;
-                            to4[1] = hi;
-                        } else
+                        Eight<float> e, old;
+                        if (p.add) {
+                            old.load(to, n);
 #pragma unroll
-                            for (int k = 0; k < 8; ++k)
-                                if (k < n) to[k] = (k < 4 ? lo[k] : hi[k - 4]) + (p.add ? to[k] : 0.f);
+                            for (int k = 0; k < 8; ++k) v[k] += old.get(k);
+                        }
+                        e.set(v);
+                        e.store(to, n);
                     }
                 }
             }
@@ -310,10 +347,17 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
         }
     } else {
         // scores of this lane: example tj TN + wj + 32 y + lane % 32, class row0 + 32 x + 8 (v / 4) + v % 4 of the piece
-        float *bias = reinterpret_cast<float *>(lds + main_lds_of(PL, TN, MODE, stages_of(PL, TN)));
-        Example *examples = reinterpret_cast<Example *>(bias + kTA);
-        if (threadIdx.x < kTA) bias[threadIdx.x] = own_bias;
-        if (threadIdx.x < TN) examples[threadIdx.x] = own;
+        float *bias = reinterpret_cast<float *>(lds + main_lds_of(TN, MODE, stages_of(TN)));
+        int *ew = reinterpret_cast<int *>(bias + kTA);
+        Example *examples = reinterpret_cast<Example *>(ew + kTA);
+        if (threadIdx.x < kTA) { bias[threadIdx.x] = own_bias; ew[threadIdx.x] = own_ew; }
+        if (threadIdx.x < TN) {
+            Example &e = examples[threadIdx.x];
+            e.label = own_label;
+            if constexpr (PL == 2) e.ea = own_ea;
+            if constexpr (MODE == kGrad) { e.m = own_m; e.log_s = own_log_s; e.g = own_g; }
+            if constexpr (MODE == kGrad && PL == 2) e.eg = own_eg;
+        }
         __syncthreads();
         const int row0 = wi + 4 * (lane >> 5);          // of the tile
 #pragma unroll
@@ -321,10 +365,14 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const f32x4 b = *reinterpret_cast<const f32x4 *>(bias + row0 + 32 * x + 8 * q);     // (-inf past the last class)
+                typedef int i32x4 __attribute__((ext_vector_type(4)));
+                const i32x4 e = *reinterpret_cast<const i32x4 *>(ew + row0 + 32 * x + 8 * q);
 #pragma unroll
-                for (int y = 0; y < BY; ++y)
+                for (int y = 0; y < BY; ++y) {
+                    const int ea = PL == 2 ? examples[wj + 32 * y + (lane & 31)].ea - 28 : 0;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) acc[x][y][4 * q + k] += b[k];
+                    for (int k = 0; k < 4; ++k) acc[x][y][4 * q + k] = b[k] + (PL == 2 ? ldexpf(acc[x][y][4 * q + k], ea + e[k]) : acc[x][y][4 * q + k]);
+                }
             }
         // the score of this lane's label, if it is among the lane's
         auto score_at = [&](int y, int label) __attribute__((always_inline)) {
@@ -383,7 +431,7 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
 #pragma unroll
             for (int y = 0; y < BY; ++y) {
                 if constexpr (TN == 64) if (tj * TN + 32 * y >= p.cols) continue;     // (few rows)
-                const Example e = examples[wj + 32 * y + (lane & 31)];
+                const Example &e = examples[wj + 32 * y + (lane & 31)];
                 const int label = (int)((unsigned)e.label - ti * kTA);
                 const bool here = is_here(label), none = e.g == 0.f || e.log_s == -INFINITY;     // (-inf: a row without a class)
                 float fixed = 0.f;
@@ -412,29 +460,41 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
 #pragma unroll
                     for (int v = 0; v < 16; ++v) sum[x][v] += acc[x][y][v];
             }
-            // dz, a part at a time: [example][class] in LDS, then runs of 512 bytes
+            // dz, a part at a time: [example][class] in LDS, then runs of 512 (fp32: 64) bytes
+            const int units = PL == 2 ? 14 - *p.w_most : 0;
 #pragma unroll
             for (int part = 0; part < PL; ++part) {
 #pragma unroll
-                for (int y = 0; y < BY; ++y)
+                for (int y = 0; y < BY; ++y) {
+                    const int eg = PL == 2 ? examples[wj + 32 * y + (lane & 31)].eg : 0;
 #pragma unroll
-                    for (int x = 0; x < BX; ++x)
+                    for (int x = 0; x < BX; ++x) {
+                        // (the second parts anew, not all of them kept from the first ones' turn on)
+                        int r0 = row0;
+                        if constexpr (PL == 2) asm volatile("" : "+v"(acc[x][y]), "+v"(r0));
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
-                            const float w0 = acc[x][y][4 * q], w1 = acc[x][y][4 * q + 1], w2 = acc[x][y][4 * q + 2], w3 = acc[x][y][4 * q + 3];
+                            f32x4 w = {acc[x][y][4 * q], acc[x][y][4 * q + 1], acc[x][y][4 * q + 2], acc[x][y][4 * q + 3]};
                             char *to = lds + (wj + 32 * y + (lane & 31)) * kTileStride + (row0 + 32 * x + 8 * q) * 2;
-                            if constexpr (PL == 1) store4(reinterpret_cast<bf16_t *>(to), w0, w1, w2, w3);
+                            if constexpr (PL == 1) store4(reinterpret_cast<bf16_t *>(to), w[0], w[1], w[2], w[3]);
                             else {
-                                const Parts4 s = split_parts(f32x3_u32x4{__float_as_uint(w0), __float_as_uint(w1), __float_as_uint(w2), __float_as_uint(w3)});
-                                *reinterpret_cast<f32x3_u32x2 *>(to) = s.p[part];
+                                if (part == 0) {
+#pragma unroll
+                                    for (int k = 0; k < 4; ++k) acc[x][y][4 * q + k] = w[k] = ldexpf(w[k], units - eg + ew[r0 + 32 * x + 8 * q + k]);
+                                }
+                                f16x4 h[2];
+                                two_parts(w, 0, h);
+                                *reinterpret_cast<f16x4 *>(to) = h[part];
                             }
                         }
+                    }
+                }
                 __syncthreads();
 #pragma unroll
                 for (int k = 0; k < TN / 16; ++k) {
                     const int at = k * 512 + threadIdx.x, col = tj * TN + (at >> 5), row = ti * kTA + (at & 31) * 8;
-                    if (col < p.cols && row < (int)p.ld_dz)
-                        *reinterpret_cast<f32x4 *>(p.dz + part * p.dz_plane + (size_t)col * p.ld_dz + row) =
+                    if (col < p.cols && row < p.ld_dz)
+                        *reinterpret_cast<f32x4 *>(p.dz + (size_t)col * p.ld_dz * PL + column_at<PL>(row, part)) =
                             *reinterpret_cast<const f32x4 *>(lds + (at >> 5) * kTileStride + (at & 31) * 16);
                 }
                 __syncthreads();
@@ -474,48 +534,110 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
 }
 
 // ------------------------------------------------------------------------------------------ before and after the products
-// A matrix [rows][cols] as the products take it: bf16 parts [PL][rows_p][cols_p], zeros past its end, and, where there are labels, in rows
-// that have none or whose weight is zero.
-template <typename T>
-__global__ __launch_bounds__(256) void xent_lay_kernel(const T *__restrict__ from, int rows, int cols, bf16_t *to, int rows_p, int cols_p,
-                                                       const int32_t *labels, const float *g, int classes)
+// A bf16 matrix [rows][cols] as the products take it: [rows_p][cols_p], zeros past its end, and, where there are labels, in rows that have
+// none or whose weight is zero.
+__device__ __forceinline__ bool row_counts(int row, const int32_t *labels, const float *g, int classes)
+{
+    if (!labels) return true;
+    const int y = labels[row];
+    return y >= 0 && y < classes && (!g || g[row] != 0.f);
+}
+__global__ __launch_bounds__(256) void xent_lay_kernel(const bf16_t *__restrict__ from, int rows, int cols, bf16_t *to, int rows_p, int cols_p, const int32_t *labels,
+                                                       const float *g, int classes)
 {
     const int groups = cols_p / 8;
     for (size_t at = (size_t)blockIdx.x * 256 + threadIdx.x; at < (size_t)rows_p * groups; at += (size_t)gridDim.x * 256) {
         const int row = (int)(at / groups), c = (int)(at - (size_t)row * groups) * 8;
-        bool there = row < rows;
-        if (there && labels) {
-            const int y = labels[row];
-            there = y >= 0 && y < classes && (!g || g[row] != 0.f);
-        }
-        bf16_t *dst = to + (size_t)row * cols_p + c;
-        const T *src = from + (size_t)row * cols + c;
-        if constexpr (sizeof(T) == 2) {
-            Eight<bf16_t> v;
-            v.load(there ? src : from, there ? cols - c : 0);
-            *reinterpret_cast<Eight<bf16_t>::u32x4 *>(dst) = v.w;
-        } else {
-            Eight<float> e;
-            e.load(there ? src : from, there ? cols - c : 0);
-            unsigned v[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = __float_as_uint(e.get(k));
-            const Parts4 lo = split_parts(f32x3_u32x4{v[0], v[1], v[2], v[3]}), hi = split_parts(f32x3_u32x4{v[4], v[5], v[6], v[7]});
-#pragma unroll
-            for (int k = 0; k < 3; ++k) {
-                f32x3_u32x2 *d = reinterpret_cast<f32x3_u32x2 *>(dst + k * (size_t)rows_p * cols_p);
-                d[0] = lo.p[k];
-                d[1] = hi.p[k];
-            }
-        }
+        const bool there = row < rows && row_counts(row, labels, g, classes);
+        Eight<bf16_t> v;
+        v.load(there ? from + (size_t)row * cols + c : from, there ? cols - c : 0);
+        *reinterpret_cast<Eight<bf16_t>::u32x4 *>(to + (size_t)row * cols_p + c) = v.w;
     }
 }
-
-// What the contraction over examples finds past the last of them: zeros in rows [N, NP) of every part of dz.
-__global__ __launch_bounds__(256) void xent_clear_kernel(bf16_t *dz, size_t plane, size_t from, size_t count)
+// An fp32 matrix in two f16 parts: in units of its own, e[row] - 14, whose largest (with eg[row], of g[row], where there are
+// weights) goes into *most, which began as INT_MIN; or, again, in units of eg[row] - *most + 14.
+template <bool AGAIN, int U, int W>      // W waves to a row, U groups of eight columns a lane in registers; U = 0: rows of any length, met twice
+__global__ __launch_bounds__(256) void xent_lay32_kernel(const float *__restrict__ from, int rows, int cols, bf16_t *to, int rows_p, int cols_p, const int32_t *labels,
+                                                         const float *g, int classes, int *e, int *eg, int *most)
 {
-    for (size_t at = (size_t)blockIdx.x * 256 + threadIdx.x; at < count; at += (size_t)gridDim.x * 256)
-        *reinterpret_cast<f32x4 *>(dz + blockIdx.y * plane + from + at * 8) = f32x4{};
+    constexpr int LANES = 64 * W, ROWS = 4 / W;
+    __shared__ float waves[2][4];
+    const int lane = threadIdx.x % LANES, groups = cols_p / 8;
+    int largest = INT_MIN, turn = 0;
+    auto magnitude = [](const Eight<float> &v) __attribute__((always_inline)) {
+        float m = 0.f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float x = __builtin_fabsf(v.get(k));
+            m = x < INFINITY ? fmaxf(m, x) : m;
+        }
+        return m;
+    };
+    for (int row = blockIdx.x * ROWS + threadIdx.x / LANES; row < rows_p; row += gridDim.x * ROWS) {
+        const bool there = row < rows && row_counts(row, labels, g, classes);
+        const float *src = from + (size_t)(there ? row : 0) * cols;
+        Eight<float> kept[U ? U : 1];
+        auto group_of = [&](int u) __attribute__((always_inline)) { return u * LANES + lane; };
+#pragma unroll
+        for (int u = 0; u < U; ++u) kept[u].load(there && group_of(u) * 8 < cols ? src + group_of(u) * 8 : from, there ? cols - group_of(u) * 8 : 0);
+        int unit;
+        if constexpr (AGAIN) unit = there ? eg[row] - *most + 14 : 0;
+        else {
+            float m = 0.f;
+            if constexpr (U > 0)
+#pragma unroll
+                for (int u = 0; u < U; ++u) m = fmaxf(m, magnitude(kept[u]));
+            else if (there)
+                for (int c = lane * 8; c < cols; c += LANES * 8) {
+                    Eight<float> v;
+                    v.load(src + c, cols - c);
+                    m = fmaxf(m, magnitude(v));
+                }
+            m = all_max(m);
+            if constexpr (W == 4) {
+                if ((threadIdx.x & 63) == 0) waves[turn][threadIdx.x >> 6] = m;
+                __syncthreads();
+                m = fmaxf(fmaxf(waves[turn][0], waves[turn][1]), fmaxf(waves[turn][2], waves[turn][3]));
+                turn ^= 1;
+            }
+            const int mine = exponent_of(m), of_g = there && g ? exponent_of(g[row]) : 0;
+            unit = 14 - mine;
+            if (lane == 0 && row < rows) {
+                e[row] = mine;
+                if (eg) eg[row] = of_g;
+            }
+            if (m > 0.f && mine + of_g > largest) largest = mine + of_g;
+        }
+        auto write = [&](int c, const Eight<float> &v) __attribute__((always_inline)) {
+            f16x4 lo[2], hi[2];
+            two_parts(v.lo, unit, lo);
+            two_parts(v.hi, unit, hi);
+#pragma unroll
+            for (int part = 0; part < 2; ++part)
+                *reinterpret_cast<f16x8 *>(to + (size_t)row * cols_p * 2 + column_at<2>(c, part)) = __builtin_shufflevector(lo[part], hi[part], 0, 1, 2, 3, 4, 5, 6, 7);
+        };
+        if constexpr (U > 0) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (group_of(u) < groups) write(group_of(u) * 8, kept[u]);
+        } else
+            for (int group = lane; group < groups; group += LANES) {
+                Eight<float> v;
+                v.load(there && group * 8 < cols ? src + group * 8 : from, there ? cols - group * 8 : 0);
+                write(group * 8, v);
+            }
+    }
+    if constexpr (!AGAIN)
+        // (the same in any order; most waves find that it is as large already)
+        if (lane == 0 && most && largest > __hip_atomic_load(most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(most, largest);
+}
+
+// Zeros where the contraction over examples reads past the last of them, `count` 16 bytes of dz, and the largest exponents' beginnings.
+__global__ __launch_bounds__(256) void xent_clear_kernel(bf16_t *dz, size_t count, int *most, int pieces)
+{
+    for (size_t at = (size_t)blockIdx.x * 256 + threadIdx.x; at < count; at += (size_t)gridDim.x * 256) *reinterpret_cast<f32x4 *>(dz + at * 8) = f32x4{};
+    if (blockIdx.x == 0)
+        for (int k = threadIdx.x; k < pieces; k += 256) most[k] = INT_MIN;
 }
 
 __device__ __forceinline__ void write_loss(Sums s, float z_label, int label, int classes, float *loss, float *stats, int row)
@@ -590,13 +712,14 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(Scores z, const int32_t 
 // dz [PL][N][ld_dz] of all classes, and db of a range of rows: 256 classes to a workgroup, four rows at a time.
 template <int PL>
 __global__ __launch_bounds__(256) void xent_grad_kernel(Scores z, const int32_t *__restrict__ labels, const float *__restrict__ stats, const float *__restrict__ g,
-                                                        bf16_t *dz, size_t ld_dz, size_t dz_plane, float *db, size_t ld_db)
+                                                        bf16_t *dz, int ld_dz, float *db, size_t ld_db, const int *__restrict__ ew, const int *__restrict__ eg,
+                                                        const int *__restrict__ w_most)
 {
     __shared__ f32x4 sums[4][64];
     const int k = blockIdx.x * 256 + (threadIdx.x & 63) * 4, r = threadIdx.x >> 6;
     const int r0 = (int)((long)z.N * blockIdx.y / gridDim.y), r1 = (int)((long)z.N * (blockIdx.y + 1) / gridDim.y);
     f32x4 sum = {};
-    if (k < (int)ld_dz)
+    if (k < ld_dz)
         for (int row = r0 + r; row < r1; row += 4) {
             const int y = labels[row];
             const float w = y >= 0 && y < z.classes ? g[row] : 0.f, m = stats[2 * (size_t)row], log_s = stats[2 * (size_t)row + 1];
@@ -610,12 +733,15 @@ __global__ __launch_bounds__(256) void xent_grad_kernel(Scores z, const int32_t 
                 }
             }
             sum += out;
-            bf16_t *to = dz + (size_t)row * ld_dz + k;
-            if constexpr (PL == 1) store4(to, out[0], out[1], out[2], out[3]);
+            bf16_t *to = dz + (size_t)row * ld_dz * PL;
+            if constexpr (PL == 1) store4(to + k, out[0], out[1], out[2], out[3]);
             else {
-                const Parts4 s = split_parts(f32x3_u32x4{__float_as_uint(out[0]), __float_as_uint(out[1]), __float_as_uint(out[2]), __float_as_uint(out[3])});
 #pragma unroll
-                for (int q = 0; q < 3; ++q) *reinterpret_cast<f32x3_u32x2 *>(to + q * dz_plane) = s.p[q];
+                for (int j = 0; j < 4; ++j) out[j] = k + j < z.classes ? ldexpf(out[j], 14 - *w_most - eg[row] + ew[k + j]) : 0.f;
+                f16x4 h[2];
+                two_parts(out, 0, h);
+#pragma unroll
+                for (int part = 0; part < 2; ++part) *reinterpret_cast<f16x4 *>(to + column_at<2>(k, part)) = h[part];
             }
         }
     sums[r][threadIdx.x & 63] = sum;
@@ -631,46 +757,49 @@ __global__ __launch_bounds__(256) void xent_grad_kernel(Scores z, const int32_t 
 // dw of few rows, a sum of up to NMAX outer products: a thread's eight columns of the activations stay in registers, dz is the same for all
 // threads, and what is left is the write (4 rows, 200003 x 4096 bf16: `kFewRows`).
 template <int PL, int NMAX, typename G>
-__global__ __launch_bounds__(256) void xent_outer_kernel(const bf16_t *__restrict__ a, size_t ld_a, size_t a_plane, const bf16_t *__restrict__ dz, size_t ld_dz,
-                                                         size_t dz_plane, int N, int cols, int classes, G *dw)
+__global__ __launch_bounds__(256) void xent_outer_kernel(const bf16_t *__restrict__ a, int cols_a, const bf16_t *__restrict__ dz, int ld_dz, int N, int cols, int classes,
+                                                         const int *__restrict__ more0, const int *__restrict__ more1, const int *__restrict__ less, G *dw)
 {
     const int c = (blockIdx.x * 256 + threadIdx.x) * 8, n = cols - c < 0 ? 0 : cols - c < 8 ? cols - c : 8;
     if (n == 0) return;
-    // (three parts stand for half of a number)
+    // eight numbers of a row in PL parts
+    auto numbers = [](const bf16_t *row, int at, float (&v)[8]) __attribute__((always_inline)) {
+        if constexpr (PL == 1) {
+            Eight<bf16_t> e;
+            e.load(row + at, 8);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = e.get(k);
+        } else {
+            const f16x8 h = *reinterpret_cast<const f16x8 *>(row + column_at<2>(at, 0)), l = *reinterpret_cast<const f16x8 *>(row + column_at<2>(at, 1));
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = (float)h[k] + (float)l[k];
+        }
+    };
     float v[NMAX][8];
 #pragma unroll
     for (int r = 0; r < NMAX; ++r) {
-        const bf16_t *from = a + (r < N ? r : 0) * ld_a + c;          // (laid out in whole stages)
-        Eight<bf16_t> e;
-        e.load(from, 8);
+        numbers(a + (size_t)(r < N ? r : 0) * cols_a * PL, c, v[r]);        // (laid out in whole stages)
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[r][k] = r < N ? e.get(k) : 0.f;
-#pragma unroll
-        for (int part = 1; part < PL; ++part) {
-            e.load(from + part * a_plane, 8);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) v[r][k] += r < N ? e.get(k) : 0.f;
-        }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[r][k] *= PL == 3 ? 4.f : 1.f;
+        for (int k = 0; k < 8; ++k) v[r][k] = r < N ? v[r][k] : 0.f;
     }
     const int groups = (classes + 7) / 8, g0 = (int)((long)groups * blockIdx.y / gridDim.y), g1 = (int)((long)groups * (blockIdx.y + 1) / gridDim.y);
+    const int units = PL == 2 ? *more0 + *more1 - 28 : 0;
     for (int group = g0; group < g1; ++group) {
-        Eight<bf16_t> w[NMAX][PL];
+        float w[NMAX][8];
 #pragma unroll
-        for (int r = 0; r < NMAX; ++r)
-#pragma unroll
-            for (int part = 0; part < PL; ++part) w[r][part].load(dz + part * dz_plane + (r < N ? r : 0) * ld_dz + (size_t)group * 8, 8);
+        for (int r = 0; r < NMAX; ++r) numbers(dz + (size_t)(r < N ? r : 0) * ld_dz * PL, group * 8, w[r]);
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             if (group * 8 + k >= classes) break;
             float out[8] = {};
 #pragma unroll
-            for (int r = 0; r < NMAX; ++r) {
-                float s = w[r][0].get(k);
-                if constexpr (PL == 3) s += w[r][1].get(k) + w[r][2].get(k);
+            for (int r = 0; r < NMAX; ++r)
 #pragma unroll
-                for (int q = 0; q < 8; ++q) out[q] = __builtin_fmaf(s, v[r][q], out[q]);
+                for (int q = 0; q < 8; ++q) out[q] = __builtin_fmaf(w[r][k], v[r][q], out[q]);
+            if constexpr (PL == 2) {
+                const int e = units - less[group * 8 + k];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) out[q] = ldexpf(out[q], e);
             }
             Eight<G> e;
             e.set(out);
@@ -699,10 +828,16 @@ __global__ __launch_bounds__(256) void xent_add_kernel(const float *__restrict__
 inline int up(long v, int to) { return (int)((v + to - 1) / to * to); }
 inline long div_up(long a, long b) { return (a + b - 1) / b; }
 
-// Columns of a tile: examples for the scores and da, classes for dw.
-inline int tile_of(int dtype, int cols) { return cols > 128 && dtype == VGG_BF16 ? 256 : cols > 64 ? 128 : 64; }
-// Ranges of a contraction of `steps` stages, where `tiles` do not fill the chip: at least four stages of bf16 each, or two of fp32, which are
-// six times as long.
+// Columns of a tile, of examples for the scores and da, of classes for dw: as many as leave no half of it empty, and give every compute unit a tile
+// of its own where that can be.
+inline int tile_of(int cols, long row_tiles)
+{
+    int tn = cols > 128 ? 256 : cols > 64 ? 128 : 64;
+    while (tn > 64 && row_tiles * div_up(cols, tn) < 256) tn /= 2;
+    return tn;
+}
+// Ranges of a contraction of `steps` stages, where `tiles` do not fill the chip: at least 256 indices of bf16 operands each, or 128 of
+// fp32 ones, which take three times as long.
 inline int splits_of(int dtype, long tiles, int steps)
 {
     const long most = div_up(steps, dtype == VGG_BF16 ? 4 : 2), want = tiles >= 256 ? 1 : div_up(256, tiles);
@@ -710,25 +845,27 @@ inline int splits_of(int dtype, long tiles, int steps)
 }
 
 struct XentPlan {
-    int PL, In, InP, NP, tn;
+    int PL, In, InP, NP, tn, grad_tn;
     bool direct_w, direct_a;      // read where they are (bf16, whole stages)
     int classes, pieces;          // of a piece (the last has what is left)
     int z_splits;                 // 0: scores' tiles end in their sums or gradients; else their parts are added up (then one piece)
-    size_t ld_dz, ld_z;
+    int ld_dz;
+    size_t ld_z;
     // forward
-    size_t a_at, w_at, z_at, sums_at, label_at, forward_bytes;
+    size_t a_at, w_at, ea_at, ew_at, z_at, sums_at, label_at, forward_bytes;
     // backward
     int da_splits, dw_splits, dw_tn, db_parts;
     bool da_direct;
-    size_t tail_at, dz_at, da_at, dw_at, db_at, backward_bytes;
+    size_t a2_at, eg_at, most_at, tail_at, dz_at, da_at, dw_at, db_at, backward_bytes;
 };
 
 XentPlan xent_plan(int dtype, int N, int In, int K)
 {
     XentPlan p;
-    p.PL = dtype == VGG_BF16 ? 1 : 3;
+    p.PL = dtype == VGG_BF16 ? 1 : 2;
     p.In = In; p.InP = up(In, kStep); p.NP = up(N, kStep);
-    p.tn = tile_of(dtype, N);
+    p.tn = N > 128 ? 256 : N > 64 ? 128 : 64;
+    p.grad_tn = p.PL == 2 && p.tn == 256 ? 128 : p.tn;     // (256: more registers than there are)
     p.direct_w = p.direct_a = dtype == VGG_BF16 && In % kStep == 0;
     const long n_tiles = div_up(N, p.tn), d_tiles = div_up(In, kTA);
     const int steps = p.InP / kStep;
@@ -758,22 +895,28 @@ XentPlan xent_plan(int dtype, int N, int In, int K)
     // (the gradients take the activations laid out in any case: rows without a label have to be zeros)
     p.a_at = take((size_t)p.PL * 2 * p.NP * p.InP);
     p.w_at = take(p.direct_w ? 0 : (size_t)p.PL * 2 * up(most, kStep) * p.InP);
+    p.ea_at = take(p.PL == 2 ? (size_t)N * 4 : 0);
+    p.ew_at = take(p.PL == 2 ? (size_t)most * 4 : 0);
     p.z_at = take(p.z_splits ? (size_t)p.z_splits * N * p.ld_z * 4 : 0);
     const size_t both = at;
     p.sums_at = take(p.z_splits ? 0 : (size_t)div_up(K, kTA) * N * sizeof(Sums));
     p.label_at = take(p.z_splits ? 0 : (size_t)N * 4);
     p.forward_bytes = at;
     at = both;
+    p.a2_at = take(p.PL == 2 ? (size_t)4 * p.NP * p.InP : 0);
+    p.eg_at = take(p.PL == 2 ? (size_t)N * 4 : 0);
+    p.most_at = take(p.PL == 2 ? (size_t)(p.pieces + 1) * 4 : 0);
     p.tail_at = take(p.direct_w ? (size_t)kStep * In * 2 : 0);
     p.dz_at = take((size_t)p.PL * 2 * p.NP * p.ld_dz);
     p.da_splits = splits_of(dtype, n_tiles * d_tiles, (int)div_up(most, kStep));
     p.da_direct = p.pieces == 1 && p.da_splits == 1;
     p.da_at = take(p.da_direct ? 0 : (size_t)p.da_splits * N * p.InP * 4);
-    p.dw_tn = tile_of(dtype, most);
+    p.dw_tn = tile_of(most, d_tiles);
     p.dw_splits = splits_of(dtype, d_tiles * div_up(most, p.dw_tn), p.NP / kStep);
     p.dw_at = take(p.dw_splits == 1 || N <= kFewRows ? 0 : (size_t)p.dw_splits * most * p.InP * 4);
     // rows' ranges that db is summed in
-    p.db_parts = (int)(p.z_splits ? div_up(N, N < 512 ? 8 : div_up(N, 64)) : n_tiles);
+    p.db_parts = (int)(p.z_splits ? div_up(N, N < 512 ? 8 : div_up(N, 64)) 
+                       : div_up(N, p.grad_tn));
     p.db_at = take(p.db_parts == 1 ? 0 : (size_t)p.db_parts * p.ld_dz * 4);
     p.backward_bytes = at;
     return p;
@@ -784,7 +927,7 @@ template <bool A_TR, bool B_TR, int TN, int PL, int MODE> int launch_product(con
 {
     auto *kernel = &xent_product_kernel<A_TR, B_TR, TN, PL, MODE>;
     // (a short contraction has no more stages: more workgroups to a compute unit)
-    const int lds = lds_of(PL, TN, MODE, MODE == kStore ? (kStep / stage_indices(PL)) * (p.steps / p.splits + 1) : stages_of(PL, TN));
+    const int lds = lds_of(TN, MODE, MODE == kStore ? PL * (p.steps / p.splits + 1) : stages_of(TN));
     if (lds > 65536 && !raise_lds_limit(reinterpret_cast<const void *>(kernel))) return VGG_ERR_LAUNCH;
     const long grid = div_up(p.rows, kTA) * div_up(p.cols, TN) * p.splits;
     kernel<<<(int)grid, 512, lds, s>>>(p);
@@ -792,32 +935,52 @@ template <bool A_TR, bool B_TR, int TN, int PL, int MODE> int launch_product(con
 }
 template <bool A_TR, bool B_TR, int MODE> int product(int PL, int tn, const Product &p, hipStream_t s)
 {
-    if (PL == 3) return tn == 128 ? launch_product<A_TR, B_TR, 128, 3, MODE>(p, s) : launch_product<A_TR, B_TR, 64, 3, MODE>(p, s);
+    if (PL == 2)
+        return tn == 256   ? launch_product<A_TR, B_TR, MODE == kGrad ? 128 : 256, 2, MODE>(p, s)
+               : tn == 128 ? launch_product<A_TR, B_TR, 128, 2, MODE>(p, s)
+                           : launch_product<A_TR, B_TR, 64, 2, MODE>(p, s);
     return tn == 256   ? launch_product<A_TR, B_TR, 256, 1, MODE>(p, s)
            : tn == 128 ? launch_product<A_TR, B_TR, 128, 1, MODE>(p, s)
                        : launch_product<A_TR, B_TR, 64, 1, MODE>(p, s);
 }
 
-template <int PL, typename G> int outer(int N, const bf16_t *a, size_t ld_a, size_t a_plane, const bf16_t *dz, size_t ld_dz, size_t dz_plane, int cols, int classes, void *dw,
-                                        hipStream_t s)
+template <int PL, typename G> int outer(const Product &q, const bf16_t *a, int cols_a, const bf16_t *dz, int ld_dz, int N, hipStream_t s)
 {
-    const long across = div_up(cols, 2048), down = div_up(2048, across), most = div_up(classes, 8);
+    const long across = div_up(q.rows, 2048), down = div_up(2048, across), most = div_up(q.cols, 8);
     const dim3 grid((unsigned)across, (unsigned)(down < most ? down : most));
-    G *to = static_cast<G *>(dw);
-    if (N <= 4) xent_outer_kernel<PL, 4, G><<<grid, 256, 0, s>>>(a, ld_a, a_plane, dz, ld_dz, dz_plane, N, cols, classes, to);
-    else if (N <= 8) xent_outer_kernel<PL, 8, G><<<grid, 256, 0, s>>>(a, ld_a, a_plane, dz, ld_dz, dz_plane, N, cols, classes, to);
-    else xent_outer_kernel<PL, 16, G><<<grid, 256, 0, s>>>(a, ld_a, a_plane, dz, ld_dz, dz_plane, N, cols, classes, to);
+    G *to = static_cast<G *>(q.out);
+    if (N <= 4) xent_outer_kernel<PL, 4, G><<<grid, 256, 0, s>>>(a, cols_a, dz, ld_dz, N, q.rows, q.cols, q.more[0], q.more[1], q.less, to);
+    else if (N <= 8) xent_outer_kernel<PL, 8, G><<<grid, 256, 0, s>>>(a, cols_a, dz, ld_dz, N, q.rows, q.cols, q.more[0], q.more[1], q.less, to);
+    else xent_outer_kernel<PL, 16, G><<<grid, 256, 0, s>>>(a, cols_a, dz, ld_dz, N, q.rows, q.cols, q.more[0], q.more[1], q.less, to);
     return launch_status();
 }
 
-int lay(int dtype, const void *from, int rows, int cols, void *to, int rows_p, int cols_p, const int32_t *labels, const float *g, int classes, hipStream_t s)
+int lay(const void *from, int rows, int cols, void *to, int rows_p, int cols_p, const int32_t *labels, const float *g, int classes, hipStream_t s)
 {
-    const long groups = (long)rows_p * (cols_p / 8), blocks = div_up(groups, 256);
-    const int grid = (int)(blocks < 8192 ? blocks : 8192);
-    if (dtype == VGG_BF16)
-        xent_lay_kernel<bf16_t><<<grid, 256, 0, s>>>(static_cast<const bf16_t *>(from), rows, cols, static_cast<bf16_t *>(to), rows_p, cols_p, labels, g, classes);
-    else
-        xent_lay_kernel<float><<<grid, 256, 0, s>>>(static_cast<const float *>(from), rows, cols, static_cast<bf16_t *>(to), rows_p, cols_p, labels, g, classes);
+    const long blocks = div_up((long)rows_p * (cols_p / 8), 256);
+    xent_lay_kernel<<<(int)(blocks < 8192 ? blocks : 8192), 256, 0, s>>>(static_cast<const bf16_t *>(from), rows, cols, static_cast<bf16_t *>(to), rows_p, cols_p, labels, g,
+                                                                         classes);
+    return launch_status();
+}
+template <bool AGAIN>
+int lay32(const void *from, int rows, int cols, void *to, int rows_p, int cols_p, const int32_t *labels, const float *g, int classes, int *e, int *eg, int *most, hipStream_t s)
+{
+    auto launch = [&](auto u, auto w) {
+        constexpr int W = decltype(w)::value;
+        const long blocks = div_up(rows_p, 4 / W);
+        xent_lay32_kernel<AGAIN, decltype(u)::value, W><<<(int)(blocks < 2048 ? blocks : 2048), 256, 0, s>>>(static_cast<const float *>(from), rows, cols, static_cast<bf16_t *>(to),
+                                                                                                             rows_p, cols_p, labels, g, classes, e, eg, most);
+    };
+    const std::integral_constant<int, 0> any{};
+    const std::integral_constant<int, 1> one{};
+    const std::integral_constant<int, 2> two{};
+    const std::integral_constant<int, 4> four{};
+    if (cols <= 512) launch(one, one);
+    else if (cols <= 1024) launch(two, one);
+    else if (cols <= 2048) launch(one, four);
+    else if (cols <= 4096) launch(two, four);
+    else if (cols <= 8192) launch(four, four);
+    else launch(any, four);
     return launch_status();
 }
 int add_parts(int dtype, const float *from, int parts, size_t part, size_t ld, int rows, int cols, void *out, hipStream_t s)
@@ -837,21 +1000,26 @@ struct Call {
     char *ws;
     hipStream_t s;
 };
-// The product that gives the scores of a piece: classes are the rows of C, examples its columns.
-int scores_product(const Call &c, const XentPlan &pl, int piece, bool laid_a, Product &p)
+template <typename T> T *at(const Call &c, size_t offset) { return reinterpret_cast<T *>(c.ws + offset); }
+
+// The product that gives the scores of a piece: classes are the rows of C, examples its columns.  w_most: where the largest of its exponents goes.
+int scores_product(const Call &c, const XentPlan &pl, int piece, bool laid_a, int *w_most, Product &p)
 {
     const int es = c.dtype == VGG_BF16 ? 2 : 4, class0 = piece * pl.classes, here = c.K - class0 < pl.classes ? c.K - class0 : pl.classes;
     const char *w = static_cast<const char *>(c.w) + (size_t)class0 * c.In * es;
+    const size_t ld = (size_t)pl.InP * 2 * pl.PL;
     p = Product{};
     p.rows = here; p.cols = c.N; p.steps = pl.InP / kStep; p.splits = 1;
-    if (pl.direct_w) p.a = {w, (size_t)c.In * 2, 0, here, nullptr};
+    if (pl.direct_w) p.a = {w, ld, here, nullptr};
     else {
         const int rows_p = up(here, kStep);
-        if (const int rc = lay(c.dtype, w, here, c.In, c.ws + pl.w_at, rows_p, pl.InP, nullptr, nullptr, 0, c.s)) return rc;
-        p.a = {c.ws + pl.w_at, (size_t)pl.InP * 2, (size_t)rows_p * pl.InP * 2, here, nullptr};
+        const int rc = pl.PL == 2 ? lay32<false>(w, here, c.In, c.ws + pl.w_at, rows_p, pl.InP, nullptr, nullptr, 0, at<int>(c, pl.ew_at), nullptr, w_most, c.s)
+                                  : lay(w, here, c.In, c.ws + pl.w_at, rows_p, pl.InP, nullptr, nullptr, 0, c.s);
+        if (rc) return rc;
+        p.a = {c.ws + pl.w_at, ld, here, nullptr};
     }
-    if (!laid_a) p.b = {static_cast<const char *>(c.a), (size_t)c.In * 2, 0, c.N, nullptr};
-    else p.b = {c.ws + pl.a_at, (size_t)pl.InP * 2, (size_t)pl.NP * pl.InP * 2, c.N, nullptr};
+    p.b = {laid_a ? c.ws + pl.a_at : static_cast<const char *>(c.a), ld, c.N, nullptr};
+    if (pl.PL == 2) { p.ea = at<int>(c, pl.ea_at); p.ew = at<int>(c, pl.ew_at); }
     p.bias = c.bias; p.labels = c.labels;
     p.class0 = class0; p.classes = here; p.all_classes = c.K;
     return VGG_OK;
@@ -867,13 +1035,15 @@ int scores_in_parts(const XentPlan &pl, const Call &c, Product &p, Scores &z)
 int forward(const Call &c, float *loss, float *stats)
 {
     const XentPlan pl = xent_plan(c.dtype, c.N, c.In, c.K);
-    int rc;
-    if (!pl.direct_a && (rc = lay(c.dtype, c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, nullptr, nullptr, 0, c.s))) return rc;
-    Sums *sums = reinterpret_cast<Sums *>(c.ws + pl.sums_at);
-    float *z_label = reinterpret_cast<float *>(c.ws + pl.label_at);
+    int rc = VGG_OK;
+    if (pl.PL == 2) rc = lay32<false>(c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, nullptr, nullptr, 0, at<int>(c, pl.ea_at), nullptr, nullptr, c.s);
+    else if (!pl.direct_a) rc = lay(c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, nullptr, nullptr, 0, c.s);
+    if (rc) return rc;
+    Sums *sums = at<Sums>(c, pl.sums_at);
+    float *z_label = at<float>(c, pl.label_at);
     for (int piece = 0; piece < pl.pieces; ++piece) {
         Product p;
-        if ((rc = scores_product(c, pl, piece, !pl.direct_a, p))) return rc;
+        if ((rc = scores_product(c, pl, piece, !pl.direct_a, nullptr, p))) return rc;
         if (pl.z_splits) {
             Scores z;
             if ((rc = scores_in_parts(pl, c, p, z))) return rc;
@@ -893,35 +1063,45 @@ int backward(const Call &c, int g_dtype, const float *stats, const float *g, voi
 {
     const XentPlan pl = xent_plan(c.dtype, c.N, c.In, c.K);
     const int gs = g_dtype == VGG_BF16 ? 2 : 4;
+    const bool two = pl.PL == 2;
+    bf16_t *dz = at<bf16_t>(c, pl.dz_at);
+    int *ea = two ? at<int>(c, pl.ea_at) : nullptr, *ew = two ? at<int>(c, pl.ew_at) : nullptr, *eg = two ? at<int>(c, pl.eg_at) : nullptr;
+    int *a_most = two ? at<int>(c, pl.most_at) : nullptr;        // and, behind it, the pieces'
+    const size_t past = (size_t)(pl.NP - c.N) * pl.ld_dz * pl.PL / 8;
     int rc;
-    if ((rc = lay(c.dtype, c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, c.labels, g, c.K, c.s))) return rc;
-    bf16_t *dz = reinterpret_cast<bf16_t *>(c.ws + pl.dz_at);
-    const size_t dz_plane = (size_t)pl.NP * pl.ld_dz, a_plane = (size_t)pl.NP * pl.InP * 2;
-    if (const size_t past = (size_t)(pl.NP - c.N) * pl.ld_dz / 8) {
-        xent_clear_kernel<<<dim3((unsigned)(past < 256 * 1024 ? (past + 255) / 256 : 1024), (unsigned)pl.PL), 256, 0, c.s>>>(dz, dz_plane, (size_t)c.N * pl.ld_dz, past);
+    if (past || two) {
+        xent_clear_kernel<<<(unsigned)(past < 256 * 1024 ? div_up(past + 1, 256) : 1024), 256, 0, c.s>>>(dz + (size_t)c.N * pl.ld_dz * pl.PL, past, a_most, two ? pl.pieces + 1 : 0);
         if ((rc = launch_status())) return rc;
     }
-    float *da_part = reinterpret_cast<float *>(c.ws + pl.da_at), *dw_part = reinterpret_cast<float *>(c.ws + pl.dw_at);
+    bf16_t *a_of_dw = at<bf16_t>(c, two ? pl.a2_at : pl.a_at);
+    if (two) {
+        if ((rc = lay32<false>(c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, c.labels, g, c.K, ea, eg, a_most, c.s))) return rc;
+        if (dw && (rc = lay32<true>(c.a, c.N, c.In, a_of_dw, pl.NP, pl.InP, c.labels, g, c.K, ea, eg, a_most, c.s))) return rc;
+    } else if ((rc = lay(c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, c.labels, g, c.K, c.s)))
+        return rc;
+    float *da_part = at<float>(c, pl.da_at), *dw_part = at<float>(c, pl.dw_at);
     for (int piece = 0; piece < pl.pieces; ++piece) {
         Product p;
-        if ((rc = scores_product(c, pl, piece, true, p))) return rc;
+        int *w_most = two ? a_most + 1 + piece : nullptr;
+        if ((rc = scores_product(c, pl, piece, true, w_most, p))) return rc;
         const Operand w = p.a;
         const int class0 = p.class0, here = p.classes;
-        float *db_to = db ? pl.db_parts == 1 ? db + class0 : reinterpret_cast<float *>(c.ws + pl.db_at) : nullptr;
+        float *db_to = db ? pl.db_parts == 1 ? db + class0 : at<float>(c, pl.db_at) : nullptr;
         if (pl.z_splits) {
             Scores z;
             if ((rc = scores_in_parts(pl, c, p, z))) return rc;
             const dim3 grid((unsigned)div_up(pl.ld_dz, 256), (unsigned)pl.db_parts);
-            if (pl.PL == 1) xent_grad_kernel<1><<<grid, 256, 0, c.s>>>(z, c.labels, stats, g, dz, pl.ld_dz, dz_plane, db_to, pl.ld_dz);
-            else xent_grad_kernel<3><<<grid, 256, 0, c.s>>>(z, c.labels, stats, g, dz, pl.ld_dz, dz_plane, db_to, pl.ld_dz);
+            if (two) xent_grad_kernel<2><<<grid, 256, 0, c.s>>>(z, c.labels, stats, g, dz, pl.ld_dz, db_to, pl.ld_dz, ew, eg, w_most);
+            else xent_grad_kernel<1><<<grid, 256, 0, c.s>>>(z, c.labels, stats, g, dz, pl.ld_dz, db_to, pl.ld_dz, ew, eg, w_most);
             if ((rc = launch_status())) return rc;
         } else {
-            p.stats = stats; p.g = g;
-            p.dz = dz; p.ld_dz = pl.ld_dz; p.dz_plane = dz_plane;
+            p.stats = stats; p.g = g; p.eg = eg; p.w_most = w_most;
+            p.dz = dz; p.ld_dz = pl.ld_dz;
             p.db = db_to; p.ld_db = pl.ld_dz;
-            if ((rc = product<false, false, kGrad>(pl.PL, pl.tn, p, c.s))) return rc;
+            if ((rc = product<false, false, kGrad>(pl.PL, pl.grad_tn, p, c.s))) return rc;
         }
         if (db && pl.db_parts > 1 && (rc = add_parts(VGG_F32, db_to, pl.db_parts, pl.ld_dz, pl.ld_dz, 1, here, db + class0, c.s))) return rc;
+        const size_t ld_dz = (size_t)pl.ld_dz * 2 * pl.PL;
         // (a last piece's gradients beyond its classes: zeros up to the contraction's next stage)
         if (da) {
             Product q = {};
@@ -930,30 +1110,32 @@ int backward(const Call &c, int g_dtype, const float *stats, const float *g, voi
             q.a.rows = (int)w.ld;
             if (pl.direct_w && here % kStep) {
                 const int from = here / kStep * kStep;
-                if ((rc = lay(c.dtype, w.p + (size_t)from * w.ld, here - from, c.In, c.ws + pl.tail_at, kStep, c.In, nullptr, nullptr, 0, c.s))) return rc;
+                if ((rc = lay(w.p + (size_t)from * w.ld, here - from, c.In, c.ws + pl.tail_at, kStep, c.In, nullptr, nullptr, 0, c.s))) return rc;
                 q.a.tail = c.ws + pl.tail_at;
             }
-            q.b = {reinterpret_cast<const char *>(dz), pl.ld_dz * 2, dz_plane * 2, c.N, nullptr};
+            q.b = {reinterpret_cast<const char *>(dz), ld_dz, c.N, nullptr};
             q.rows = c.In; q.cols = c.N; q.steps = steps; q.splits = pl.da_splits < steps ? pl.da_splits : steps;
+            q.ea = eg; q.more[0] = w_most;
             if (pl.da_direct) { q.out = da; q.ld = c.In; q.bf16 = g_dtype == VGG_BF16; }
             else { q.out = da_part; q.ld = pl.InP; q.part = (size_t)c.N * pl.InP; q.add = piece > 0; }
             if ((rc = product<true, false, kStore>(pl.PL, pl.tn, q, c.s))) return rc;
         }
-        if (dw && c.N <= kFewRows) {
-            void *out = static_cast<char *>(dw) + (size_t)class0 * c.In * gs;
-            const bf16_t *a = reinterpret_cast<const bf16_t *>(c.ws + pl.a_at);
-            const size_t plane = (size_t)pl.NP * pl.InP;
-            rc = pl.PL == 3           ? outer<3, float>(c.N, a, pl.InP, plane, dz, pl.ld_dz, dz_plane, c.In, here, out, c.s)
-                 : g_dtype == VGG_F32 ? outer<1, float>(c.N, a, pl.InP, plane, dz, pl.ld_dz, dz_plane, c.In, here, out, c.s)
-                                      : outer<1, bf16_t>(c.N, a, pl.InP, plane, dz, pl.ld_dz, dz_plane, c.In, here, out, c.s);
-            if (rc) return rc;
-        } else if (dw) {
+        if (dw) {
             Product q = {};
-            q.a = {c.ws + pl.a_at, (size_t)pl.InP * 2, a_plane, pl.InP * 2, nullptr};
-            q.b = {reinterpret_cast<const char *>(dz), pl.ld_dz * 2, dz_plane * 2, (int)pl.ld_dz * 2, nullptr};
+            q.a = {reinterpret_cast<const char *>(a_of_dw), (size_t)pl.InP * 2 * pl.PL, pl.InP * 2 * pl.PL, nullptr};
+            q.b = {reinterpret_cast<const char *>(dz), ld_dz, (int)ld_dz, nullptr};
             q.rows = c.In; q.cols = here; q.steps = pl.NP / kStep; q.splits = pl.dw_splits;
+            q.more[0] = a_most; q.more[1] = w_most; q.less = ew;
             void *out = static_cast<char *>(dw) + (size_t)class0 * c.In * gs;
-            if (q.splits == 1) { q.out = out; q.ld = c.In; q.bf16 = g_dtype == VGG_BF16; }
+            q.out = out;
+            if (c.N <= kFewRows) {
+                rc = two                  ? outer<2, float>(q, a_of_dw, pl.InP, dz, pl.ld_dz, c.N, c.s)
+                     : g_dtype == VGG_F32 ? outer<1, float>(q, a_of_dw, pl.InP, dz, pl.ld_dz, c.N, c.s)
+                                          : outer<1, bf16_t>(q, a_of_dw, pl.InP, dz, pl.ld_dz, c.N, c.s);
+                if (rc) return rc;
+                continue;
+            }
+            if (q.splits == 1) { q.ld = c.In; q.bf16 = g_dtype == VGG_BF16; }
             else { q.out = dw_part; q.ld = pl.InP; q.part = (size_t)here * pl.InP; }
             if ((rc = product<true, true, kStore>(pl.PL, pl.dw_tn, q, c.s))) return rc;
             if (q.splits > 1 && (rc = add_parts(g_dtype, dw_part, q.splits, q.part, pl.InP, here, c.In, out, c.s))) return rc;
