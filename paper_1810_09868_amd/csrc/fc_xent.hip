@@ -31,6 +31,9 @@ namespace {
 constexpr int kTA = 256;      // rows of C in a tile
 constexpr int kStep = 64;     // contractions are whole multiples of this many indices
 constexpr size_t kPieceBytes = 512u << 20;   // what a piece of the classes may take of the workspace
+// bf16 rows up to which what rounding leaves of dz enters dw, as a contraction twice as long.  Off by 2^-9 of each term, dw is as exact as its own
+// rounding to bf16 on the average of many rows; the fewer there are, the more hangs on single ones.
+constexpr int kRestRows = 512;
 constexpr int kFewRows = 16;                 // rows up to which dw is written by its own kernel
 constexpr int kTileStride = 528;             // bytes from row to row of 256 bf16 numbers in LDS
 
@@ -70,6 +73,9 @@ struct Product {
     const int *eg, *w_most;              // fp32: eg, W
     bf16_t *dz;                          // [N ...][ld_dz], parts side by side
     int ld_dz;                           // classes of a row
+    int rest_rows;                       // bf16: what rounding leaves of dz lies so many rows on; 0: it is not kept
+    float *rest_of_label;                // bf16: [N], ... of dz at the labels
+    int wrap;                            // contraction indices, in whole 64s, after which A begins again; 0: never
     float *db;                           // [tiles of examples][ld_db]
     size_t ld_db;
 };
@@ -90,6 +96,12 @@ __device__ __forceinline__ void two_parts(const f32x4 &v, int e, f16x4 (&part)[2
         const float rest = x - (float)part[0][k];
         part[1][k] = (_Float16)(__builtin_fabsf(rest) < INFINITY ? rest : 0.f);
     }
+}
+// What rounding to bf16 leaves (of infinities and NaN: nothing).
+__device__ __forceinline__ float rest_of(float v)
+{
+    const float r = v - bf16_to_f32(f32_to_bf16(v));
+    return __builtin_fabsf(r) < INFINITY ? r : 0.f;
 }
 // e with 2^e <= |v| < 2 2^e; 0 for zeros and what is not finite.
 __device__ __forceinline__ int exponent_of(float v) { return v != 0.f && __builtin_fabsf(v) < INFINITY ? ilogbf(v) : 0; }
@@ -166,13 +178,14 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
 #pragma unroll
     for (int q = 0; q < CB; ++q) from_b[q] = source(p.b, B_TR, tj * TN, q);
     const size_t step_a = A_TR ? KS * p.a.ld : 128, step_b = B_TR ? KS * p.b.ld : 128;
-    const char *at_a = p.a.p + (A_TR ? 0 : (size_t)ti * kTA * p.a.ld) + (size_t)s0 * PL * step_a;
+    const char *at_a = p.a.p + (A_TR ? 0 : (size_t)ti * kTA * p.a.ld) + (size_t)(A_TR && PL == 1 && p.wrap ? s0 % p.wrap : s0) * PL * step_a;
     const char *at_b = p.b.p + (B_TR ? 0 : (size_t)tj * TN * p.b.ld) + (size_t)s0 * PL * step_b;
     const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(lds_char *)lds + wave * 1024);
     // the stage that is copied next
     int slot = 0, to_come = p.steps - s0;
     auto aim = [&]() __attribute__((always_inline)) {
         if (A_TR && PL == 1 && p.a.tail && to_come == 1) at_a = p.a.tail;
+        if (A_TR && PL == 1 && p.wrap && to_come == p.steps - p.wrap) at_a = p.a.p;
     };
     aim();
     auto copy_one = [&](int n) __attribute__((always_inline)) {      // of a stage's COPIES
@@ -439,6 +452,8 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
                 if (any) {
                     const float z = score_at(y, label);
                     fixed = none || z == -INFINITY ? 0.f : e.g * expm1f((z - e.m) - e.log_s);
+                    if constexpr (PL == 1)
+                        if (here && tj * TN + wj + 32 * y + (lane & 31) < p.cols) p.rest_of_label[tj * TN + wj + 32 * y + (lane & 31)] = rest_of(fixed);
                 }
 #pragma unroll
                 for (int x = 0; x < BX; ++x)
@@ -460,10 +475,12 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
 #pragma unroll
                     for (int v = 0; v < 16; ++v) sum[x][v] += acc[x][y][v];
             }
-            // dz, a part at a time: [example][class] in LDS, then runs of 512 (fp32: 64) bytes
+            // dz, a part (bf16: it, and what rounding leaves of it) at a time: [example][class] in LDS, then runs of 512 (fp32: 64) bytes
+            const int parts = PL == 1 && p.rest_rows ? 2 : PL;
             const int units = PL == 2 ? 14 - *p.w_most : 0;
 #pragma unroll
-            for (int part = 0; part < PL; ++part) {
+            for (int part = 0; part < 2; ++part) {
+                if (part >= parts) continue;
 #pragma unroll
                 for (int y = 0; y < BY; ++y) {
                     const int eg = PL == 2 ? examples[wj + 32 * y + (lane & 31)].eg : 0;
@@ -471,13 +488,15 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
                     for (int x = 0; x < BX; ++x) {
                         // (the second parts anew, not all of them kept from the first ones' turn on)
                         int r0 = row0;
-                        if constexpr (PL == 2) asm volatile("" : "+v"(acc[x][y]), "+v"(r0));
+                        if (PL == 2 || part == 1) asm volatile("" : "+v"(acc[x][y]), "+v"(r0));
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
                             f32x4 w = {acc[x][y][4 * q], acc[x][y][4 * q + 1], acc[x][y][4 * q + 2], acc[x][y][4 * q + 3]};
                             char *to = lds + (wj + 32 * y + (lane & 31)) * kTileStride + (row0 + 32 * x + 8 * q) * 2;
-                            if constexpr (PL == 1) store4(reinterpret_cast<bf16_t *>(to), w[0], w[1], w[2], w[3]);
-                            else {
+                            if constexpr (PL == 1) {
+                                if (part == 1) w = f32x4{rest_of(w[0]), rest_of(w[1]), rest_of(w[2]), rest_of(w[3])};
+                                store4(reinterpret_cast<bf16_t *>(to), w[0], w[1], w[2], w[3]);
+                            } else {
                                 if (part == 0) {
 #pragma unroll
                                     for (int k = 0; k < 4; ++k) acc[x][y][4 * q + k] = w[k] = ldexpf(w[k], units - eg + ew[r0 + 32 * x + 8 * q + k]);
@@ -494,7 +513,7 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
                 for (int k = 0; k < TN / 16; ++k) {
                     const int at = k * 512 + threadIdx.x, col = tj * TN + (at >> 5), row = ti * kTA + (at & 31) * 8;
                     if (col < p.cols && row < p.ld_dz)
-                        *reinterpret_cast<f32x4 *>(p.dz + (size_t)col * p.ld_dz * PL + column_at<PL>(row, part)) =
+                        *reinterpret_cast<f32x4 *>(p.dz + (size_t)(col + (PL == 1 ? part * p.rest_rows : 0)) * p.ld_dz * PL + column_at<PL>(row, part)) =
                             *reinterpret_cast<const f32x4 *>(lds + (at >> 5) * kTileStride + (at & 31) * 16);
                 }
                 __syncthreads();
@@ -632,10 +651,16 @@ __global__ __launch_bounds__(256) void xent_lay32_kernel(const float *__restrict
         if (lane == 0 && most && largest > __hip_atomic_load(most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(most, largest);
 }
 
-// Zeros where the contraction over examples reads past the last of them, `count` 16 bytes of dz, and the largest exponents' beginnings.
-__global__ __launch_bounds__(256) void xent_clear_kernel(bf16_t *dz, size_t count, int *most, int pieces)
+// Zeros where the contraction over examples reads past the last of them, `count` 16 bytes of dz (and of what rounding leaves of it), in rows
+// whose label no piece holds, and the largest exponents' beginnings.
+__global__ __launch_bounds__(256) void xent_clear_kernel(bf16_t *dz, bf16_t *dz_rest, size_t count, float *rest_of_label, int N, int *most, int pieces)
 {
-    for (size_t at = (size_t)blockIdx.x * 256 + threadIdx.x; at < count; at += (size_t)gridDim.x * 256) *reinterpret_cast<f32x4 *>(dz + at * 8) = f32x4{};
+    for (size_t at = (size_t)blockIdx.x * 256 + threadIdx.x; at < count; at += (size_t)gridDim.x * 256) {
+        *reinterpret_cast<f32x4 *>(dz + at * 8) = f32x4{};
+        if (dz_rest) *reinterpret_cast<f32x4 *>(dz_rest + at * 8) = f32x4{};
+    }
+    if (rest_of_label)
+        for (int at = blockIdx.x * 256 + threadIdx.x; at < N; at += gridDim.x * 256) rest_of_label[at] = 0.f;
     if (blockIdx.x == 0)
         for (int k = threadIdx.x; k < pieces; k += 256) most[k] = INT_MIN;
 }
@@ -713,7 +738,7 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(Scores z, const int32_t 
 template <int PL>
 __global__ __launch_bounds__(256) void xent_grad_kernel(Scores z, const int32_t *__restrict__ labels, const float *__restrict__ stats, const float *__restrict__ g,
                                                         bf16_t *dz, int ld_dz, float *db, size_t ld_db, const int *__restrict__ ew, const int *__restrict__ eg,
-                                                        const int *__restrict__ w_most)
+                                                        const int *__restrict__ w_most, int rest_rows, float *rest_of_label)
 {
     __shared__ f32x4 sums[4][64];
     const int k = blockIdx.x * 256 + (threadIdx.x & 63) * 4, r = threadIdx.x >> 6;
@@ -734,8 +759,13 @@ __global__ __launch_bounds__(256) void xent_grad_kernel(Scores z, const int32_t 
             }
             sum += out;
             bf16_t *to = dz + (size_t)row * ld_dz * PL;
-            if constexpr (PL == 1) store4(to + k, out[0], out[1], out[2], out[3]);
-            else {
+            if constexpr (PL == 1) {
+                store4(to + k, out[0], out[1], out[2], out[3]);
+                if (rest_rows) store4(to + (size_t)rest_rows * ld_dz + k, rest_of(out[0]), rest_of(out[1]), rest_of(out[2]), rest_of(out[3]));
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (k + j == y && k + j < z.classes) rest_of_label[row] = rest_of(out[j]);
+            } else {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) out[j] = k + j < z.classes ? ldexpf(out[j], 14 - *w_most - eg[row] + ew[k + j]) : 0.f;
                 f16x4 h[2];
@@ -757,7 +787,7 @@ __global__ __launch_bounds__(256) void xent_grad_kernel(Scores z, const int32_t 
 // dw of few rows, a sum of up to NMAX outer products: a thread's eight columns of the activations stay in registers, dz is the same for all
 // threads, and what is left is the write (4 rows, 200003 x 4096 bf16: `kFewRows`).
 template <int PL, int NMAX, typename G>
-__global__ __launch_bounds__(256) void xent_outer_kernel(const bf16_t *__restrict__ a, int cols_a, const bf16_t *__restrict__ dz, int ld_dz, int N, int cols, int classes,
+__global__ __launch_bounds__(256) void xent_outer_kernel(const bf16_t *__restrict__ a, int cols_a, const bf16_t *__restrict__ dz, int ld_dz, int rest_rows, int N, int cols, int classes,
                                                          const int *__restrict__ more0, const int *__restrict__ more1, const int *__restrict__ less, G *dw)
 {
     const int c = (blockIdx.x * 256 + threadIdx.x) * 8, n = cols - c < 0 ? 0 : cols - c < 8 ? cols - c : 8;
@@ -787,7 +817,15 @@ __global__ __launch_bounds__(256) void xent_outer_kernel(const bf16_t *__restric
     for (int group = g0; group < g1; ++group) {
         float w[NMAX][8];
 #pragma unroll
-        for (int r = 0; r < NMAX; ++r) numbers(dz + (size_t)(r < N ? r : 0) * ld_dz * PL, group * 8, w[r]);
+        for (int r = 0; r < NMAX; ++r) {
+            numbers(dz + (size_t)(r < N ? r : 0) * ld_dz * PL, group * 8, w[r]);
+            if constexpr (PL == 1) {
+                float rest[8];
+                numbers(dz + (size_t)(rest_rows + (r < N ? r : 0)) * ld_dz, group * 8, rest);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) w[r][k] += rest[k];
+            }
+        }
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             if (group * 8 + k >= classes) break;
@@ -808,9 +846,12 @@ __global__ __launch_bounds__(256) void xent_outer_kernel(const bf16_t *__restric
     }
 }
 
-// out [rows][cols] = the sum of `parts` matrices [rows][ld], `part` elements apart, in order.
+// out [rows][cols] = the sum of `parts` matrices [rows][ld], `part` elements apart, in order; da of bf16 operands: and of what rounding left of dz
+// at a row's label, times the label's weights.  That one number is most of a row's dz: without it da would be off by as much again as by
+// its own rounding to bf16, with one sign for the whole row.
 template <typename T>
-__global__ __launch_bounds__(256) void xent_add_kernel(const float *__restrict__ from, int parts, size_t part, size_t ld, int rows, int cols, T *out)
+__global__ __launch_bounds__(256) void xent_add_kernel(const float *__restrict__ from, int parts, size_t part, size_t ld, int rows, int cols, T *out,
+                                                       const float *__restrict__ rest_of_label, const int32_t *__restrict__ labels, const bf16_t *__restrict__ w)
 {
     const int groups = (cols + 3) / 4;
     for (size_t at = (size_t)blockIdx.x * 256 + threadIdx.x; at < (size_t)rows * groups; at += (size_t)gridDim.x * 256) {
@@ -818,6 +859,13 @@ __global__ __launch_bounds__(256) void xent_add_kernel(const float *__restrict__
         const int c = (int)(at - row * groups) * 4;
         f32x4 s = {};
         for (int q = 0; q < parts; ++q) s += *reinterpret_cast<const f32x4 *>(from + q * part + row * ld + c);     // (ld is a multiple of 4)
+        if (rest_of_label)
+            if (const float r = rest_of_label[row]; r != 0.f) {
+                const bf16_t *of = w + (size_t)labels[row] * cols + c;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (c + k < cols) s[k] = __builtin_fmaf(r, bf16_to_f32(of[k]), s[k]);
+            }
 #pragma unroll
         for (int k = 0; k < 4; ++k)
             if (c + k < cols) Elem<T>::store(out + row * cols + c + k, s[k]);
@@ -849,14 +897,14 @@ struct XentPlan {
     bool direct_w, direct_a;      // read where they are (bf16, whole stages)
     int classes, pieces;          // of a piece (the last has what is left)
     int z_splits;                 // 0: scores' tiles end in their sums or gradients; else their parts are added up (then one piece)
-    int ld_dz;
+    int ld_dz, rest_rows;
     size_t ld_z;
     // forward
     size_t a_at, w_at, ea_at, ew_at, z_at, sums_at, label_at, forward_bytes;
     // backward
     int da_splits, dw_splits, dw_tn, db_parts;
     bool da_direct;
-    size_t a2_at, eg_at, most_at, tail_at, dz_at, da_at, dw_at, db_at, backward_bytes;
+    size_t a2_at, eg_at, most_at, rest_at, tail_at, dz_at, da_at, dw_at, db_at, backward_bytes;
 };
 
 XentPlan xent_plan(int dtype, int N, int In, int K)
@@ -907,12 +955,14 @@ XentPlan xent_plan(int dtype, int N, int In, int K)
     p.eg_at = take(p.PL == 2 ? (size_t)N * 4 : 0);
     p.most_at = take(p.PL == 2 ? (size_t)(p.pieces + 1) * 4 : 0);
     p.tail_at = take(p.direct_w ? (size_t)kStep * In * 2 : 0);
-    p.dz_at = take((size_t)p.PL * 2 * p.NP * p.ld_dz);
+    p.rest_rows = p.PL == 1 && N <= kRestRows ? p.NP : 0;
+    p.rest_at = take(p.PL == 1 ? (size_t)N * 4 : 0);
+    p.dz_at = take((size_t)p.PL * 2 * (p.NP + p.rest_rows) * p.ld_dz);
     p.da_splits = splits_of(dtype, n_tiles * d_tiles, (int)div_up(most, kStep));
-    p.da_direct = p.pieces == 1 && p.da_splits == 1;
+    p.da_direct = p.PL == 2 && p.pieces == 1 && p.da_splits == 1;
     p.da_at = take(p.da_direct ? 0 : (size_t)p.da_splits * N * p.InP * 4);
     p.dw_tn = tile_of(most, d_tiles);
-    p.dw_splits = splits_of(dtype, d_tiles * div_up(most, p.dw_tn), p.NP / kStep);
+    p.dw_splits = splits_of(dtype, d_tiles * div_up(most, p.dw_tn), (p.NP + p.rest_rows) / kStep);
     p.dw_at = take(p.dw_splits == 1 || N <= kFewRows ? 0 : (size_t)p.dw_splits * most * p.InP * 4);
     // rows' ranges that db is summed in
     p.db_parts = (int)(p.z_splits ? div_up(N, N < 512 ? 8 : div_up(N, 64)) 
@@ -944,14 +994,14 @@ template <bool A_TR, bool B_TR, int MODE> int product(int PL, int tn, const Prod
                        : launch_product<A_TR, B_TR, 64, 1, MODE>(p, s);
 }
 
-template <int PL, typename G> int outer(const Product &q, const bf16_t *a, int cols_a, const bf16_t *dz, int ld_dz, int N, hipStream_t s)
+template <int PL, typename G> int outer(const Product &q, const bf16_t *a, int cols_a, const bf16_t *dz, int ld_dz, int rest_rows, int N, hipStream_t s)
 {
     const long across = div_up(q.rows, 2048), down = div_up(2048, across), most = div_up(q.cols, 8);
     const dim3 grid((unsigned)across, (unsigned)(down < most ? down : most));
     G *to = static_cast<G *>(q.out);
-    if (N <= 4) xent_outer_kernel<PL, 4, G><<<grid, 256, 0, s>>>(a, cols_a, dz, ld_dz, N, q.rows, q.cols, q.more[0], q.more[1], q.less, to);
-    else if (N <= 8) xent_outer_kernel<PL, 8, G><<<grid, 256, 0, s>>>(a, cols_a, dz, ld_dz, N, q.rows, q.cols, q.more[0], q.more[1], q.less, to);
-    else xent_outer_kernel<PL, 16, G><<<grid, 256, 0, s>>>(a, cols_a, dz, ld_dz, N, q.rows, q.cols, q.more[0], q.more[1], q.less, to);
+    if (N <= 4) xent_outer_kernel<PL, 4, G><<<grid, 256, 0, s>>>(a, cols_a, dz, ld_dz, rest_rows, N, q.rows, q.cols, q.more[0], q.more[1], q.less, to);
+    else if (N <= 8) xent_outer_kernel<PL, 8, G><<<grid, 256, 0, s>>>(a, cols_a, dz, ld_dz, rest_rows, N, q.rows, q.cols, q.more[0], q.more[1], q.less, to);
+    else xent_outer_kernel<PL, 16, G><<<grid, 256, 0, s>>>(a, cols_a, dz, ld_dz, rest_rows, N, q.rows, q.cols, q.more[0], q.more[1], q.less, to);
     return launch_status();
 }
 
@@ -983,12 +1033,14 @@ int lay32(const void *from, int rows, int cols, void *to, int rows_p, int cols_p
     else launch(any, four);
     return launch_status();
 }
-int add_parts(int dtype, const float *from, int parts, size_t part, size_t ld, int rows, int cols, void *out, hipStream_t s)
+int add_parts(int dtype, const float *from, int parts, size_t part, size_t ld, int rows, int cols, void *out, hipStream_t s, const float *rest = nullptr,
+              const int32_t *labels = nullptr, const void *w = nullptr)
 {
+    const bf16_t *w16 = static_cast<const bf16_t *>(w);
     const long blocks = div_up((long)rows * div_up(cols, 4), 256);
     const int grid = (int)(blocks < 8192 ? blocks : 8192);
-    if (dtype == VGG_BF16) xent_add_kernel<bf16_t><<<grid, 256, 0, s>>>(from, parts, part, ld, rows, cols, static_cast<bf16_t *>(out));
-    else xent_add_kernel<float><<<grid, 256, 0, s>>>(from, parts, part, ld, rows, cols, static_cast<float *>(out));
+    if (dtype == VGG_BF16) xent_add_kernel<bf16_t><<<grid, 256, 0, s>>>(from, parts, part, ld, rows, cols, static_cast<bf16_t *>(out), rest, labels, w16);
+    else xent_add_kernel<float><<<grid, 256, 0, s>>>(from, parts, part, ld, rows, cols, static_cast<float *>(out), rest, labels, w16);
     return launch_status();
 }
 
@@ -1069,8 +1121,12 @@ int backward(const Call &c, int g_dtype, const float *stats, const float *g, voi
     int *a_most = two ? at<int>(c, pl.most_at) : nullptr;        // and, behind it, the pieces'
     const size_t past = (size_t)(pl.NP - c.N) * pl.ld_dz * pl.PL / 8;
     int rc;
-    if (past || two) {
-        xent_clear_kernel<<<(unsigned)(past < 256 * 1024 ? div_up(past + 1, 256) : 1024), 256, 0, c.s>>>(dz + (size_t)c.N * pl.ld_dz * pl.PL, past, a_most, two ? pl.pieces + 1 : 0);
+    float *rest = two ? nullptr : at<float>(c, pl.rest_at);
+    {
+        bf16_t *from = dz + (size_t)c.N * pl.ld_dz * pl.PL;
+        const size_t most = past > (size_t)c.N ? past : c.N;
+        xent_clear_kernel<<<(unsigned)(most < 256 * 1024 ? div_up(most, 256) : 1024), 256, 0, c.s>>>(from, pl.rest_rows ? from + (size_t)pl.rest_rows * pl.ld_dz : nullptr, past, rest, c.N,
+                                                                                                     a_most, two ? pl.pieces + 1 : 0);
         if ((rc = launch_status())) return rc;
     }
     bf16_t *a_of_dw = at<bf16_t>(c, two ? pl.a2_at : pl.a_at);
@@ -1091,12 +1147,12 @@ int backward(const Call &c, int g_dtype, const float *stats, const float *g, voi
             Scores z;
             if ((rc = scores_in_parts(pl, c, p, z))) return rc;
             const dim3 grid((unsigned)div_up(pl.ld_dz, 256), (unsigned)pl.db_parts);
-            if (two) xent_grad_kernel<2><<<grid, 256, 0, c.s>>>(z, c.labels, stats, g, dz, pl.ld_dz, db_to, pl.ld_dz, ew, eg, w_most);
-            else xent_grad_kernel<1><<<grid, 256, 0, c.s>>>(z, c.labels, stats, g, dz, pl.ld_dz, db_to, pl.ld_dz, ew, eg, w_most);
+            if (two) xent_grad_kernel<2><<<grid, 256, 0, c.s>>>(z, c.labels, stats, g, dz, pl.ld_dz, db_to, pl.ld_dz, ew, eg, w_most, 0, nullptr);
+            else xent_grad_kernel<1><<<grid, 256, 0, c.s>>>(z, c.labels, stats, g, dz, pl.ld_dz, db_to, pl.ld_dz, ew, eg, w_most, pl.rest_rows, rest);
             if ((rc = launch_status())) return rc;
         } else {
             p.stats = stats; p.g = g; p.eg = eg; p.w_most = w_most;
-            p.dz = dz; p.ld_dz = pl.ld_dz;
+            p.dz = dz; p.ld_dz = pl.ld_dz; p.rest_rows = pl.rest_rows; p.rest_of_label = rest;
             p.db = db_to; p.ld_db = pl.ld_dz;
             if ((rc = product<false, false, kGrad>(pl.PL, pl.grad_tn, p, c.s))) return rc;
         }
@@ -1124,14 +1180,15 @@ int backward(const Call &c, int g_dtype, const float *stats, const float *g, voi
             Product q = {};
             q.a = {reinterpret_cast<const char *>(a_of_dw), (size_t)pl.InP * 2 * pl.PL, pl.InP * 2 * pl.PL, nullptr};
             q.b = {reinterpret_cast<const char *>(dz), ld_dz, (int)ld_dz, nullptr};
-            q.rows = c.In; q.cols = here; q.steps = pl.NP / kStep; q.splits = pl.dw_splits;
+            q.rows = c.In; q.cols = here; q.steps = (pl.NP + pl.rest_rows) / kStep; q.splits = pl.dw_splits;
+            q.wrap = pl.rest_rows / kStep;
             q.more[0] = a_most; q.more[1] = w_most; q.less = ew;
             void *out = static_cast<char *>(dw) + (size_t)class0 * c.In * gs;
             q.out = out;
             if (c.N <= kFewRows) {
-                rc = two                  ? outer<2, float>(q, a_of_dw, pl.InP, dz, pl.ld_dz, c.N, c.s)
-                     : g_dtype == VGG_F32 ? outer<1, float>(q, a_of_dw, pl.InP, dz, pl.ld_dz, c.N, c.s)
-                                          : outer<1, bf16_t>(q, a_of_dw, pl.InP, dz, pl.ld_dz, c.N, c.s);
+                rc = two                  ? outer<2, float>(q, a_of_dw, pl.InP, dz, pl.ld_dz, pl.rest_rows, c.N, c.s)
+                     : g_dtype == VGG_F32 ? outer<1, float>(q, a_of_dw, pl.InP, dz, pl.ld_dz, pl.rest_rows, c.N, c.s)
+                                          : outer<1, bf16_t>(q, a_of_dw, pl.InP, dz, pl.ld_dz, pl.rest_rows, c.N, c.s);
                 if (rc) return rc;
                 continue;
             }
@@ -1141,7 +1198,7 @@ int backward(const Call &c, int g_dtype, const float *stats, const float *g, voi
             if (q.splits > 1 && (rc = add_parts(g_dtype, dw_part, q.splits, q.part, pl.InP, here, c.In, out, c.s))) return rc;
         }
     }
-    if (da && !pl.da_direct) return add_parts(g_dtype, da_part, pl.da_splits, (size_t)c.N * pl.InP, pl.InP, c.N, c.In, da, c.s);
+    if (da && !pl.da_direct) return add_parts(g_dtype, da_part, pl.da_splits, (size_t)c.N * pl.InP, pl.InP, c.N, c.In, da, c.s, rest, c.labels, c.w);
     return VGG_OK;
 }
 

@@ -100,7 +100,7 @@ class Xent:
             # and the whole of it: roundings have either sign
             norm = out[k][f].norm()
             if norm > 0 and got.numel() > 200:
-                limit = (6e-3 if k != "loss" and k != "db" and self.dtype == B.BF16 else 2e-5)
+                limit = (3e-3 if k != "loss" and k != "db" and self.dtype == B.BF16 else 2e-5)
                 assert (got - out[k])[f].norm() <= limit * norm, (k, float((got - out[k])[f].norm() / norm))
         return self
 
@@ -274,8 +274,8 @@ def test_weights_past_32_bit_offsets():
     dz[torch.arange(N), c.labels.long()] -= 1
     dz *= c.g.double()[:, None]
     da = sum(dz[:, k:k + 50000] @ c.w[k:k + 50000].double() for k in range(0, K, 50000))
-    assert (c.da.double() - da).norm() <= 6e-3 * da.norm()
+    assert (c.da.double() - da).norm() <= 3e-3 * da.norm()
     assert (c.db.double() - dz.sum(0)).norm() <= 2e-5 * dz.sum(0).norm()
     for k0 in (0, 262144, 524288, K - 300):
         part = dz[:, k0:k0 + 300].t() @ c.a.double()
-        assert (c.dw[k0:k0 + 300].double() - part).norm() <= 6e-3 * part.norm()
+        assert (c.dw[k0:k0 + 300].double() - part).norm() <= 3e-3 * part.norm()
