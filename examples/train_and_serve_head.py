@@ -1,11 +1,12 @@
 #!/usr/bin/env python3
 """Trains a classifier of dense layers on features, rounds it to 4 bits and lets it answer.
 
-  python examples/train_and_serve_head.py [--dtype bf16|f32] [--steps 60]
+  python examples/train_and_serve_head.py [--dtype bf16|f32] [--steps 60] [--norm] [--dropout 0.1] [--pieces]
 
 The features stand for a network's last pooled layer: 64 classes, each a direction of its own under noise and a ReLU.
 Every weight matrix takes orthogonalised steps; the trained head then answers with the most likely classes, their log
-probabilities and the entropy, from its fp32 or bf16 weights and from 4-bit ones.
+probabilities and the entropy, from its fp32 or bf16 weights and from 4-bit ones.  --norm puts a layer norm in front of
+every layer, --dropout drops a share of what goes between them, --pieces takes the loss without keeping the scores.
 """
 import argparse
 import os
@@ -30,11 +31,14 @@ def main():
     ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
     ap.add_argument("--dtype", choices=("bf16", "f32"), default="bf16")
     ap.add_argument("--steps", type=int, default=60)
+    ap.add_argument("--norm", action="store_true")
+    ap.add_argument("--dropout", type=float, default=0.0)
+    ap.add_argument("--pieces", action="store_true")
     a = ap.parse_args()
     dtype, td = (B.BF16, torch.bfloat16) if a.dtype == "bf16" else (B.F32, torch.float32)
     g = torch.Generator(device="cuda").manual_seed(0)
     dims = [FEATURES, HIDDEN, HIDDEN, CLASSES]
-    head = DenseHead(dtype, BATCH, dims, lr=0.02)
+    head = DenseHead(dtype, BATCH, dims, lr=0.02, norm=a.norm, dropout=a.dropout, pieces=a.pieces)
     head.load([torch.randn((o, i), generator=g, device="cuda") * (2.0 / i) ** 0.5 for i, o in zip(dims[:-1], dims[1:])],
               [torch.zeros(o, device="cuda") for o in dims[1:]])
     centres = torch.randn((CLASSES, FEATURES), generator=g, device="cuda")

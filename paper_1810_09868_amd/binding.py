@@ -120,7 +120,7 @@ def lib() -> C.CDLL:
             getattr(L, n).restype = _sz
             getattr(L, n).argtypes = [_i] * 4
         L.vgg_fc_xent.argtypes = [_i] * 4 + [_vp] * 7 + [_sz, _vp]
-        L.vgg_fc_xent_bwd.argtypes = [_i] * 5 + [_vp] * 10 + [_sz, _vp]
+        L.vgg_fc_xent_bwd.argtypes = [_i] * 5 + [_vp] * 9 + [_i, _vp, _sz, _vp]
         cfgp = C.POINTER(VggConfig)
         prmp = C.POINTER(Vgg19Params)
         for n in ("vgg19_packed_bytes", "vgg19_forward_workspace_bytes", "vgg19_train_workspace_bytes"):
@@ -402,9 +402,9 @@ def vgg_fc_xent_bwd_workspace_bytes(dtype, N, In, K) -> int:
     return lib().vgg_fc_xent_bwd_workspace_bytes(dtype, N, In, K)
 
 
-def vgg_fc_xent_bwd(dtype, g_dtype, N, In, K, a, w, bias, labels, stats, g_loss, da, dw, db, ws=None):
+def vgg_fc_xent_bwd(dtype, g_dtype, N, In, K, a, w, bias, labels, stats, g_loss, da, dw, db, ws=None, relu_mask=False):
     _chk(lib().vgg_fc_xent_bwd(dtype, g_dtype, N, In, K, _ptr(a), _ptr(w), _ptr(bias), _ptr(labels), _ptr(stats), _ptr(g_loss), _ptr(da),
-                               _ptr(dw), _ptr(db), _ptr(ws), _nbytes(ws), _stream()), "vgg_fc_xent_bwd")
+                               _ptr(dw), _ptr(db), int(relu_mask), _ptr(ws), _nbytes(ws), _stream()), "vgg_fc_xent_bwd")
 
 
 # ------------------------------------------------------------- whole model

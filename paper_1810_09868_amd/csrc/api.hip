@@ -90,7 +90,7 @@ size_t fc_xent_bwd_workspace(int dtype, int N, int In, int K);
 int fc_xent(int dtype, int N, int In, int K, const void *a, const void *w, const float *bias, const int32_t *labels, float *loss, float *stats, void *ws,
             hipStream_t s);
 int fc_xent_bwd(int dtype, int g_dtype, int N, int In, int K, const void *a, const void *w, const float *bias, const int32_t *labels, const float *stats,
-                const float *g_loss, void *da, void *dw, float *db, void *ws, hipStream_t s);
+                const float *g_loss, void *da, void *dw, float *db, int relu_mask, void *ws, hipStream_t s);
 int w4_quantize(int In, int Out, int group, const float *w, uint8_t *codes, bf16_t *scales, hipStream_t s);
 int w4_dequantize(int In, int Out, int group, const uint8_t *codes, const bf16_t *scales, float *w, hipStream_t s);
 size_t fc_w4_workspace(int dtype, int N, int In, int Out, int group);
@@ -1027,7 +1027,7 @@ size_t vgg_fc_xent_bwd_workspace_bytes(int dtype, int N, int In, int K)
 }
 
 int vgg_fc_xent_bwd(int dtype, int g_dtype, int N, int In, int K, const void *a, const void *w, const float *bias, const int32_t *labels, const float *stats,
-                    const float *g_loss, void *da, void *dw, float *db, void *ws, size_t ws_bytes, void *stream)
+                    const float *g_loss, void *da, void *dw, float *db, int relu_mask, void *ws, size_t ws_bytes, void *stream)
 {
     if (!a || !w || !labels || !stats || !g_loss || (!da && !dw && !db)) return VGG_ERR_NULL;
     if (!dtype_ok(dtype) || (g_dtype != dtype && g_dtype != VGG_F32)) return VGG_ERR_DTYPE;
@@ -1036,7 +1036,7 @@ int vgg_fc_xent_bwd(int dtype, int g_dtype, int N, int In, int K, const void *a,
         !aligned16(db) || !aligned16(ws))
         return VGG_ERR_ALIGN;
     if (!ws || ws_bytes < fc_xent_bwd_workspace(dtype, N, In, K)) return VGG_ERR_WORKSPACE;
-    return fc_xent_bwd(dtype, g_dtype, N, In, K, a, w, bias, labels, stats, g_loss, da, dw, db, ws, (hipStream_t)stream);
+    return fc_xent_bwd(dtype, g_dtype, N, In, K, a, w, bias, labels, stats, g_loss, da, dw, db, relu_mask ? 1 : 0, ws, (hipStream_t)stream);
 }
 
 size_t vgg19_packed_bytes(const vgg_config *cfg) { return cfg_ok(cfg) ? packed_total(cfg) : 0; }

@@ -577,7 +577,7 @@ __global__ __launch_bounds__(256) void xent_lay_kernel(const bf16_t *__restrict_
 // weights) goes into *most, which began as INT_MIN; or, again, in units of eg[row] - *most + 14.
 template <bool AGAIN, int U, int W>      // W waves to a row, U groups of eight columns a lane in registers; U = 0: rows of any length, met twice
 __global__ __launch_bounds__(256) void xent_lay32_kernel(const float *__restrict__ from, int rows, int cols, bf16_t *to, int rows_p, int cols_p, const int32_t *labels,
-                                                         const float *g, int classes, int *e, int *eg, int *most)
+                                                         const float *g, int classes, const float *bias, int *e, int *eg, int *most)
 {
     constexpr int LANES = 64 * W, ROWS = 4 / W;
     __shared__ float waves[2][4];
@@ -593,7 +593,7 @@ __global__ __launch_bounds__(256) void xent_lay32_kernel(const float *__restrict
         return m;
     };
     for (int row = blockIdx.x * ROWS + threadIdx.x / LANES; row < rows_p; row += gridDim.x * ROWS) {
-        const bool there = row < rows && row_counts(row, labels, g, classes);
+        const bool there = row < rows && row_counts(row, labels, g, classes) && (!bias || bias[row] > -INFINITY);
         const float *src = from + (size_t)(there ? row : 0) * cols;
         Eight<float> kept[U ? U : 1];
         auto group_of = [&](int u) __attribute__((always_inline)) { return u * LANES + lane; };
@@ -848,10 +848,11 @@ __global__ __launch_bounds__(256) void xent_outer_kernel(const bf16_t *__restric
 
 // out [rows][cols] = the sum of `parts` matrices [rows][ld], `part` elements apart, in order; da of bf16 operands: and of what rounding left of dz
 // at a row's label, times the label's weights.  That one number is most of a row's dz: without it da would be off by as much again as by
-// its own rounding to bf16, with one sign for the whole row.
+// its own rounding to bf16, with one sign for the whole row.  Where relu_of is given, 0 where that is not above 0.
 template <typename T>
 __global__ __launch_bounds__(256) void xent_add_kernel(const float *__restrict__ from, int parts, size_t part, size_t ld, int rows, int cols, T *out,
-                                                       const float *__restrict__ rest_of_label, const int32_t *__restrict__ labels, const bf16_t *__restrict__ w)
+                                                       const float *__restrict__ rest_of_label, const int32_t *__restrict__ labels, const bf16_t *__restrict__ w,
+                                                       const void *relu_of, int relu_dtype)
 {
     const int groups = (cols + 3) / 4;
     for (size_t at = (size_t)blockIdx.x * 256 + threadIdx.x; at < (size_t)rows * groups; at += (size_t)gridDim.x * 256) {
@@ -867,8 +868,12 @@ __global__ __launch_bounds__(256) void xent_add_kernel(const float *__restrict__
                     if (c + k < cols) s[k] = __builtin_fmaf(r, bf16_to_f32(of[k]), s[k]);
             }
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (c + k < cols) Elem<T>::store(out + row * cols + c + k, s[k]);
+        for (int k = 0; k < 4; ++k) {
+            if (c + k >= cols) continue;
+            const size_t to = row * cols + c + k;
+            const bool open = !relu_of || (relu_dtype == VGG_BF16 ? bf16_to_f32(static_cast<const bf16_t *>(relu_of)[to]) : static_cast<const float *>(relu_of)[to]) > 0.f;
+            Elem<T>::store(out + to, open ? s[k] : 0.f);
+        }
     }
 }
 
@@ -903,7 +908,6 @@ struct XentPlan {
     size_t a_at, w_at, ea_at, ew_at, z_at, sums_at, label_at, forward_bytes;
     // backward
     int da_splits, dw_splits, dw_tn, db_parts;
-    bool da_direct;
     size_t a2_at, eg_at, most_at, rest_at, tail_at, dz_at, da_at, dw_at, db_at, backward_bytes;
 };
 
@@ -959,8 +963,7 @@ XentPlan xent_plan(int dtype, int N, int In, int K)
     p.rest_at = take(p.PL == 1 ? (size_t)N * 4 : 0);
     p.dz_at = take((size_t)p.PL * 2 * (p.NP + p.rest_rows) * p.ld_dz);
     p.da_splits = splits_of(dtype, n_tiles * d_tiles, (int)div_up(most, kStep));
-    p.da_direct = p.PL == 2 && p.pieces == 1 && p.da_splits == 1;
-    p.da_at = take(p.da_direct ? 0 : (size_t)p.da_splits * N * p.InP * 4);
+    p.da_at = take((size_t)p.da_splits * N * p.InP * 4);
     p.dw_tn = tile_of(most, d_tiles);
     p.dw_splits = splits_of(dtype, d_tiles * div_up(most, p.dw_tn), (p.NP + p.rest_rows) / kStep);
     p.dw_at = take(p.dw_splits == 1 || N <= kFewRows ? 0 : (size_t)p.dw_splits * most * p.InP * 4);
@@ -1013,13 +1016,14 @@ int lay(const void *from, int rows, int cols, void *to, int rows_p, int cols_p, 
     return launch_status();
 }
 template <bool AGAIN>
-int lay32(const void *from, int rows, int cols, void *to, int rows_p, int cols_p, const int32_t *labels, const float *g, int classes, int *e, int *eg, int *most, hipStream_t s)
+int lay32(const void *from, int rows, int cols, void *to, int rows_p, int cols_p, const int32_t *labels, const float *g, int classes, const float *bias, int *e, int *eg, int *most,
+          hipStream_t s)
 {
     auto launch = [&](auto u, auto w) {
         constexpr int W = decltype(w)::value;
         const long blocks = div_up(rows_p, 4 / W);
         xent_lay32_kernel<AGAIN, decltype(u)::value, W><<<(int)(blocks < 2048 ? blocks : 2048), 256, 0, s>>>(static_cast<const float *>(from), rows, cols, static_cast<bf16_t *>(to),
-                                                                                                             rows_p, cols_p, labels, g, classes, e, eg, most);
+                                                                                                             rows_p, cols_p, labels, g, classes, bias, e, eg, most);
     };
     const std::integral_constant<int, 0> any{};
     const std::integral_constant<int, 1> one{};
@@ -1034,13 +1038,13 @@ int lay32(const void *from, int rows, int cols, void *to, int rows_p, int cols_p
     return launch_status();
 }
 int add_parts(int dtype, const float *from, int parts, size_t part, size_t ld, int rows, int cols, void *out, hipStream_t s, const float *rest = nullptr,
-              const int32_t *labels = nullptr, const void *w = nullptr)
+              const int32_t *labels = nullptr, const void *w = nullptr, const void *relu_of = nullptr, int relu_dtype = 0)
 {
     const bf16_t *w16 = static_cast<const bf16_t *>(w);
     const long blocks = div_up((long)rows * div_up(cols, 4), 256);
     const int grid = (int)(blocks < 8192 ? blocks : 8192);
-    if (dtype == VGG_BF16) xent_add_kernel<bf16_t><<<grid, 256, 0, s>>>(from, parts, part, ld, rows, cols, static_cast<bf16_t *>(out), rest, labels, w16);
-    else xent_add_kernel<float><<<grid, 256, 0, s>>>(from, parts, part, ld, rows, cols, static_cast<float *>(out), rest, labels, w16);
+    if (dtype == VGG_BF16) xent_add_kernel<bf16_t><<<grid, 256, 0, s>>>(from, parts, part, ld, rows, cols, static_cast<bf16_t *>(out), rest, labels, w16, relu_of, relu_dtype);
+    else xent_add_kernel<float><<<grid, 256, 0, s>>>(from, parts, part, ld, rows, cols, static_cast<float *>(out), rest, labels, w16, relu_of, relu_dtype);
     return launch_status();
 }
 
@@ -1065,7 +1069,8 @@ int scores_product(const Call &c, const XentPlan &pl, int piece, bool laid_a, in
     if (pl.direct_w) p.a = {w, ld, here, nullptr};
     else {
         const int rows_p = up(here, kStep);
-        const int rc = pl.PL == 2 ? lay32<false>(w, here, c.In, c.ws + pl.w_at, rows_p, pl.InP, nullptr, nullptr, 0, at<int>(c, pl.ew_at), nullptr, w_most, c.s)
+        const int rc = pl.PL == 2 ? lay32<false>(w, here, c.In, c.ws + pl.w_at, rows_p, pl.InP, nullptr, nullptr, 0, c.bias ? c.bias + class0 : nullptr, at<int>(c, pl.ew_at), nullptr,
+                                               w_most, c.s)
                                   : lay(w, here, c.In, c.ws + pl.w_at, rows_p, pl.InP, nullptr, nullptr, 0, c.s);
         if (rc) return rc;
         p.a = {c.ws + pl.w_at, ld, here, nullptr};
@@ -1088,7 +1093,7 @@ int forward(const Call &c, float *loss, float *stats)
 {
     const XentPlan pl = xent_plan(c.dtype, c.N, c.In, c.K);
     int rc = VGG_OK;
-    if (pl.PL == 2) rc = lay32<false>(c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, nullptr, nullptr, 0, at<int>(c, pl.ea_at), nullptr, nullptr, c.s);
+    if (pl.PL == 2) rc = lay32<false>(c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, nullptr, nullptr, 0, nullptr, at<int>(c, pl.ea_at), nullptr, nullptr, c.s);
     else if (!pl.direct_a) rc = lay(c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, nullptr, nullptr, 0, c.s);
     if (rc) return rc;
     Sums *sums = at<Sums>(c, pl.sums_at);
@@ -1111,7 +1116,7 @@ int forward(const Call &c, float *loss, float *stats)
     return launch_status();
 }
 
-int backward(const Call &c, int g_dtype, const float *stats, const float *g, void *da, void *dw, float *db)
+int backward(const Call &c, int g_dtype, const float *stats, const float *g, void *da, void *dw, float *db, int relu_mask)
 {
     const XentPlan pl = xent_plan(c.dtype, c.N, c.In, c.K);
     const int gs = g_dtype == VGG_BF16 ? 2 : 4;
@@ -1131,8 +1136,8 @@ int backward(const Call &c, int g_dtype, const float *stats, const float *g, voi
     }
     bf16_t *a_of_dw = at<bf16_t>(c, two ? pl.a2_at : pl.a_at);
     if (two) {
-        if ((rc = lay32<false>(c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, c.labels, g, c.K, ea, eg, a_most, c.s))) return rc;
-        if (dw && (rc = lay32<true>(c.a, c.N, c.In, a_of_dw, pl.NP, pl.InP, c.labels, g, c.K, ea, eg, a_most, c.s))) return rc;
+        if ((rc = lay32<false>(c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, c.labels, g, c.K, nullptr, ea, eg, a_most, c.s))) return rc;
+        if (dw && (rc = lay32<true>(c.a, c.N, c.In, a_of_dw, pl.NP, pl.InP, c.labels, g, c.K, nullptr, ea, eg, a_most, c.s))) return rc;
     } else if ((rc = lay(c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, c.labels, g, c.K, c.s)))
         return rc;
     float *da_part = at<float>(c, pl.da_at), *dw_part = at<float>(c, pl.dw_at);
@@ -1172,8 +1177,7 @@ int backward(const Call &c, int g_dtype, const float *stats, const float *g, voi
             q.b = {reinterpret_cast<const char *>(dz), ld_dz, c.N, nullptr};
             q.rows = c.In; q.cols = c.N; q.steps = steps; q.splits = pl.da_splits < steps ? pl.da_splits : steps;
             q.ea = eg; q.more[0] = w_most;
-            if (pl.da_direct) { q.out = da; q.ld = c.In; q.bf16 = g_dtype == VGG_BF16; }
-            else { q.out = da_part; q.ld = pl.InP; q.part = (size_t)c.N * pl.InP; q.add = piece > 0; }
+            q.out = da_part; q.ld = pl.InP; q.part = (size_t)c.N * pl.InP; q.add = piece > 0;
             if ((rc = product<true, false, kStore>(pl.PL, pl.tn, q, c.s))) return rc;
         }
         if (dw) {
@@ -1198,7 +1202,7 @@ int backward(const Call &c, int g_dtype, const float *stats, const float *g, voi
             if (q.splits > 1 && (rc = add_parts(g_dtype, dw_part, q.splits, q.part, pl.InP, here, c.In, out, c.s))) return rc;
         }
     }
-    if (da && !pl.da_direct) return add_parts(g_dtype, da_part, pl.da_splits, (size_t)c.N * pl.InP, pl.InP, c.N, c.In, da, c.s, rest, c.labels, c.w);
+    if (da) return add_parts(g_dtype, da_part, pl.da_splits, (size_t)c.N * pl.InP, pl.InP, c.N, c.In, da, c.s, rest, c.labels, c.w, relu_mask ? c.a : nullptr, c.dtype);
     return VGG_OK;
 }
 
@@ -1214,9 +1218,9 @@ int fc_xent(int dtype, int N, int In, int K, const void *a, const void *w, const
 }
 
 int fc_xent_bwd(int dtype, int g_dtype, int N, int In, int K, const void *a, const void *w, const float *bias, const int32_t *labels, const float *stats,
-                const float *g_loss, void *da, void *dw, float *db, void *ws, hipStream_t s)
+                const float *g_loss, void *da, void *dw, float *db, int relu_mask, void *ws, hipStream_t s)
 {
-    return backward(Call{dtype, N, In, K, a, w, bias, labels, static_cast<char *>(ws), s}, g_dtype, stats, g_loss, da, dw, db);
+    return backward(Call{dtype, N, In, K, a, w, bias, labels, static_cast<char *>(ws), s}, g_dtype, stats, g_loss, da, dw, db, relu_mask);
 }
 
 }  // namespace vgg

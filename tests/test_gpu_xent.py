@@ -240,6 +240,48 @@ def test_parts_of_the_gradient_other_streams_and_twice_the_same(dtype, N, In, K)
     assert all(torch.equal(getattr(c, k), v) for k, v in whole.items())
 
 
+@pytest.mark.parametrize("N,In,K", [(10, 40, 90), (70, 128, 300), (300, 200, 700), (40, 1024, 600)])
+def test_fp32_rows_of_any_size(N, In, K):
+    """Activations, weights of the loss and classes' weights whose rows are powers of two apart: every row of da has its digits."""
+    c = Xent(B.F32, N, In, K, 16)
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    power = lambda n, lo, hi: torch.exp2(torch.randint(lo, hi + 1, (n,), generator=gen, device="cuda").float())  # noqa: E731
+    c.labels.clamp_(0, K - 1)
+    c.g = (0.5 + torch.rand(N, generator=gen, device="cuda")) * power(N, -40, 40)
+    c.a *= power(N, -30, 2)[:, None]
+    c.w *= power(K, -3, 3)[:, None]
+    c.run().check()
+    a, w = c.a.double(), c.w.double()
+    p = torch.softmax(a @ w.t() + (0 if c.bias is None else c.bias.double()), 1)
+    p[torch.arange(N), c.labels.long()] -= 1
+    da = p @ w
+    # (22 bits of each operand and sums of up to 700 terms that partly cancel: 1e-6 of the row; scores up to 50 are off by 1e-6 of themselves)
+    off = (c.da.double() / c.g.double()[:, None] - da).norm(dim=1) / (p.abs() @ w.abs()).norm(dim=1)
+    assert float(off.max()) <= 1e-4 and float(off.median()) <= 1e-6, (float(off.max()), float(off.median()))
+
+
+def test_fp32_weights_of_masked_classes_do_not_count():
+    c = Xent(B.F32, 70, 128, 300, 17, masked=0.3)
+    c.labels.clamp_(0, 299)
+    c.run()
+    want = {k: getattr(c, k).clone() for k in ("loss", "da", "dw", "db")}
+    c.w[c.bias == -math.inf] = 1e30
+    c.run()
+    assert all(torch.equal(getattr(c, k), v) for k, v in want.items())
+
+
+@pytest.mark.parametrize("dtype,g_dtype", TYPES)
+@pytest.mark.parametrize("N,In,K", [(5, 7, 30), (70, 128, 300), (100, 1024, 1000)])
+def test_activations_that_a_relu_left(dtype, g_dtype, N, In, K):
+    c = Xent(dtype, N, In, K, 15, g_dtype=g_dtype)
+    c.a.clamp_min_(0)
+    c.run()
+    da = torch.full((N, In), 9.0, dtype=TDT[g_dtype], device="cuda")
+    ws = ws_bytes(B.vgg_fc_xent_bwd_workspace_bytes(dtype, N, In, K))
+    B.vgg_fc_xent_bwd(dtype, g_dtype, N, In, K, c.a, c.w, c.bias, c.labels, c.stats, c.g, da, None, None, ws, relu_mask=True)
+    assert torch.equal(da, torch.where(c.a > 0, c.da, 0.0))
+
+
 @pytest.mark.parametrize("dtype", [B.F32, B.BF16])
 @pytest.mark.parametrize("N,In,K", [(70, 128, 300), (100, 1024, 1000)])
 def test_recorded_in_a_graph(dtype, N, In, K):

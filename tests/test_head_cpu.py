@@ -36,3 +36,12 @@ def test_tensors_that_the_kernels_would_misread_are_refused(dtype):
     for a, b in [(a, y) for a in wrong_x] + [(x, b) for b in wrong_y]:
         with pytest.raises(ValueError):
             DenseHead._rows(head, a, b)
+
+
+@pytest.mark.parametrize("dtype,N,dims", [(B.BF16, 300, [128, 10000]), (B.BF16, 700, [64, 64, 256, 5000]), (B.F32, 300, [8, 64, 4096, 1000]), (B.F32, 130, [96, 64, 40, 10])])
+def test_the_workspace_covers_layer_norms_and_losses_in_pieces(dtype, N, dims):
+    have = workspace_bytes(dtype, N, dims, 64, 5, True, True)
+    for n in range(1, N + 1):
+        for i in dims[:-1]:
+            assert B.vgg_layer_norm_bwd_workspace_bytes(dtype, B.F32, n, i) <= have
+        assert max(B.vgg_fc_xent_workspace_bytes(dtype, n, *dims[-2:]), B.vgg_fc_xent_bwd_workspace_bytes(dtype, n, *dims[-2:])) <= have, n

@@ -44,7 +44,7 @@ def test_losses_over_classes_are_refused_on_the_host():
     assert call(ws=None) == call(nb=B.vgg_fc_xent_workspace_bytes(B.F32, 2, 8, 10) - 1) == -5
     assert call(y=A + 4, nb=0) == -5                # a part of a longer sequence of labels is taken
     back = lambda dt=1, gt=1, N=2, i=8, k=10, a=A, w=A, b=A, y=A, st=A, g=A, da=A, dw=A, db=A, ws=A, nb=1 << 50: (  # noqa: E731
-        L.vgg_fc_xent_bwd(dt, gt, N, i, k, a, w, b, y, st, g, da, dw, db, ws, nb, None))
+        L.vgg_fc_xent_bwd(dt, gt, N, i, k, a, w, b, y, st, g, da, dw, db, 1, ws, nb, None))
     assert back(a=None) == back(w=None) == back(y=None) == back(st=None) == back(g=None) == back(da=None, dw=None, db=None) == -1
     assert back(dt=3) == back(dt=0, gt=1) == back(gt=5) == -3 and back(N=-1) == back(i=0) == back(k=0) == -2
     assert back(da=A + 2) == back(dw=A + 2) == back(db=A + 4) == back(g=A + 2) == -4 and back(ws=None) == back(nb=100) == back(g=A + 4, nb=0) == -5
