@@ -18,7 +18,9 @@
 #include "common.h"
 #include "dropout.h"
 #include "exp_of.h"
+#include "plans.h"
 #include "wave.h"
+#include "xent.h"
 
 #include <limits.h>
 
@@ -695,44 +697,40 @@ __global__ __launch_bounds__(256) void xent_join_kernel(const Sums *__restrict__
     write_loss(s, y >= 0 && y < classes ? z_label[row] : 0.f, y, classes, loss, stats, row);
 }
 
-// Scores in `parts` sums [parts][N][ld] of contraction ranges.
-struct Scores {
-    const float *part;
-    int parts, N, classes;
-    size_t ld;
-    const float *bias;
-    // of four neighbouring classes, -inf past the last
-    __device__ __forceinline__ f32x4 at(int row, int k) const
-    {
-        f32x4 z = {};
-#pragma unroll 8
-        for (int q = 0; q < parts; ++q) z += *reinterpret_cast<const f32x4 *>(part + ((size_t)q * N + row) * ld + k);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) z[j] = k + j < classes ? z[j] + (bias ? bias[k + j] : 0.f) : -INFINITY;
-        return z;
-    }
-};
+// WAVES waves to a row, 1 or 4.
+template <int WAVES>
 __global__ __launch_bounds__(256) void xent_rows_kernel(Scores z, const int32_t *__restrict__ labels, float *loss, float *stats)
 {
     __shared__ Sums all[4];
-    __shared__ float z_label;
-    const int row = blockIdx.x, y = labels[row];
+    __shared__ float z_labels[4];
+    const int wave = threadIdx.x >> 6, row = WAVES == 4 ? blockIdx.x : blockIdx.x * 4 + wave, at = threadIdx.x % (64 * WAVES);
+    if (row >= z.N) return;                 // (one wave to a row: no barrier)
+    const int y = labels[row];
+    float z_label = -INFINITY;
     Sums s = {-INFINITY, 0.f};
-    for (int k = threadIdx.x * 4; k < z.classes; k += 1024) {
+    for (int k = at * 4; k < z.classes; k += 256 * WAVES) {
         const f32x4 v = z.at(row, k);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             s = v[j] == v[j] ? joined(s, Sums{v[j], 0.f}) : Sums{s.m, v[j]};
-            if (k + j == y) z_label = v[j];
+            z_label = k + j == y ? v[j] : z_label;
         }
     }
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) s = joined(s, Sums{__shfl_xor(s.m, o), __shfl_xor(s.e, o)});
-    if ((threadIdx.x & 63) == 0) all[threadIdx.x >> 6] = s;
-    __syncthreads();
-    if (threadIdx.x) return;
-    for (int w = 1; w < 4; ++w) s = joined(s, all[w]);
-    write_loss(s, y >= 0 && y < z.classes ? z_label : 0.f, y, z.classes, loss, stats, row);
+    for (int o = 32; o > 0; o >>= 1) {
+        s = joined(s, Sums{__shfl_xor(s.m, o), __shfl_xor(s.e, o)});
+        const float other = __shfl_xor(z_label, o);
+        z_label = z_label == -INFINITY ? other : z_label;       // (a masked label's is -inf in any case)
+    }
+    if constexpr (WAVES == 4) {
+        if ((threadIdx.x & 63) == 0) { all[wave] = s; z_labels[wave] = z_label; }
+        __syncthreads();
+        for (int w = 1; w < 4; ++w) {
+            s = joined(s, all[w]);
+            z_label = z_label == -INFINITY ? z_labels[w] : z_label;
+        }
+    }
+    if (at == 0) write_loss(s, z_label, y, z.classes, loss, stats, row);
 }
 // dz [PL][N][ld_dz] of all classes, and db of a range of rows: 256 classes to a workgroup, four rows at a time.
 template <int PL>
@@ -1104,8 +1102,7 @@ int forward(const Call &c, float *loss, float *stats)
         if (pl.z_splits) {
             Scores z;
             if ((rc = scores_in_parts(pl, c, p, z))) return rc;
-            xent_rows_kernel<<<c.N, 256, 0, c.s>>>(z, c.labels, loss, stats);
-            return launch_status();
+            return xent_rows(z, c.labels, loss, stats, c.s);
         }
         p.sums = sums; p.z_label = z_label;
         if ((rc = product<false, false, kStats>(pl.PL, pl.tn, p, c.s))) return rc;
@@ -1208,18 +1205,36 @@ int backward(const Call &c, int g_dtype, const float *stats, const float *g, voi
 
 }  // namespace
 
-size_t fc_xent_workspace(int dtype, int N, int In, int K) { return xent_plan(dtype, N, In, K).forward_bytes; }
-size_t fc_xent_bwd_workspace(int dtype, int N, int In, int K) { return xent_plan(dtype, N, In, K).backward_bytes; }
+int xent_rows(const Scores &z, const int32_t *labels, float *loss, float *stats, hipStream_t s)
+{
+    if (z.classes <= 1024 && z.parts == 1) xent_rows_kernel<1><<<(z.N + 3) / 4, 256, 0, s>>>(z, labels, loss, stats);
+    else xent_rows_kernel<4><<<z.N, 256, 0, s>>>(z, labels, loss, stats);
+    return launch_status();
+}
+
+size_t fc_xent_workspace(int dtype, int N, int In, int K)
+{
+    return xent_is_small(dtype, N, In, K) ? fc_xent_small_workspace(N, K) : xent_plan(dtype, N, In, K).forward_bytes;
+}
+size_t fc_xent_bwd_workspace(int dtype, int N, int In, int K)
+{
+    return xent_is_small(dtype, N, In, K) ? fc_xent_small_workspace(N, K) : xent_plan(dtype, N, In, K).backward_bytes;
+}
 
 int fc_xent(int dtype, int N, int In, int K, const void *a, const void *w, const float *bias, const int32_t *labels, float *loss, float *stats, void *ws,
             hipStream_t s)
 {
+    if (xent_is_small(dtype, N, In, K)) 
+        return fc_xent_small(N, In, K, static_cast<const float *>(a), static_cast<const float *>(w), bias, labels, loss, stats, ws, s);
     return forward(Call{dtype, N, In, K, a, w, bias, labels, static_cast<char *>(ws), s}, loss, stats);
 }
 
 int fc_xent_bwd(int dtype, int g_dtype, int N, int In, int K, const void *a, const void *w, const float *bias, const int32_t *labels, const float *stats,
                 const float *g_loss, void *da, void *dw, float *db, int relu_mask, void *ws, hipStream_t s)
 {
+    if (xent_is_small(dtype, N, In, K)) 
+        return fc_xent_small_bwd(N, In, K, static_cast<const float *>(a), static_cast<const float *>(w), bias, labels, stats, g_loss, static_cast<float *>(da),
+                                 static_cast<float *>(dw), db, relu_mask, ws, s);
     return backward(Call{dtype, N, In, K, a, w, bias, labels, static_cast<char *>(ws), s}, g_dtype, stats, g_loss, da, dw, db, relu_mask);
 }
 

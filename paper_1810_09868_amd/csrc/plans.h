@@ -41,6 +41,17 @@ inline W4Plan w4_tiles_plan(int dtype, int N, int In, int Out)
     return t;
 }
 
+// ------------------------------------------------------------------------------------------------ losses over many classes
+// Whether fp32 products are short enough for 32 x 32 tiles of the fp32 matrix unit, in half the launches: their number, and each contraction, which a
+// tile's waves go along while others wait (loss and gradients in us, so and by large tiles: 64 x 64 x 64 33, 50; 100 x 1024 x 1000 61, 95; 500 x 500 x 500 73,
+// 133; 1000 x 300 x 1000 124, 138; 2000 x 256 x 2000 232, 160; 100 x 100 x 4000 99, 92; 1 x 4096 x 1000 107, 83).
+constexpr long kXentSmall = 5l << 26;
+inline bool xent_is_small(int dtype, int N, int In, int K)
+{
+    const long n = (N + 31) / 32 * 32, k = (K + 31) / 32 * 32;
+    return dtype == VGG_F32 && N <= 4096 && In <= 1024 && K <= 2048 && n * k * In <= kXentSmall;
+}
+
 // ------------------------------------------------------------------------------------------------ orthogonalised updates
 inline int round_to(int v, int to) { return (v + to - 1) / to * to; }
 

@@ -107,7 +107,8 @@ class Xent:
 
 TYPES = [(B.F32, B.F32), (B.BF16, B.BF16), (B.BF16, B.F32)]
 SIZES = [(1, 1, 1), (1, 64, 2), (2, 3, 1), (3, 7, 5), (64, 128, 256), (65, 64, 257), (63, 130, 255), (128, 192, 64), (129, 66, 300), (257, 256, 513), (300, 200, 700), (1, 4096, 1000),
-         (100, 4096, 1000), (5, 512, 40000), (700, 1000, 14), (1000, 33, 3000), (33, 2048, 129), (4, 1024, 10007)]
+         (100, 4096, 1000), (5, 512, 40000), (700, 1000, 14), (1000, 33, 3000), (33, 2048, 129), (4, 1024, 10007),
+         (500, 500, 500), (4096, 70, 33), (31, 1024, 2048), (33, 1025, 65), (4097, 40, 20), (5, 8, 2049), (17, 300, 3000), (16, 100, 5000), (513, 320, 2500)]
 
 
 @pytest.mark.parametrize("dtype,g_dtype", TYPES)
