@@ -905,7 +905,7 @@ struct XentPlan {
     // forward
     size_t a_at, w_at, ea_at, ew_at, z_at, sums_at, label_at, forward_bytes;
     // backward
-    int da_splits, dw_splits, dw_tn, db_parts;
+    int da_splits, da_tn, dw_splits, dw_tn, db_parts;
     size_t a2_at, eg_at, most_at, rest_at, tail_at, dz_at, da_at, dw_at, db_at, backward_bytes;
 };
 
@@ -914,7 +914,8 @@ XentPlan xent_plan(int dtype, int N, int In, int K)
     XentPlan p;
     p.PL = dtype == VGG_BF16 ? 1 : 2;
     p.In = In; p.InP = up(In, kStep); p.NP = up(N, kStep);
-    p.tn = N > 128 ? 256 : N > 64 ? 128 : 64;
+    // (the contraction of scores of few tiles is split: their columns by what that leaves idle)
+    p.tn = tile_of(N, div_up(K, kTA) * splits_of(dtype, div_up(K, kTA), p.InP / kStep));
     p.grad_tn = p.PL == 2 && p.tn == 256 ? 128 : p.tn;     // (256: more registers than there are)
     p.direct_w = p.direct_a = dtype == VGG_BF16 && In % kStep == 0;
     const long n_tiles = div_up(N, p.tn), d_tiles = div_up(In, kTA);
@@ -960,13 +961,14 @@ XentPlan xent_plan(int dtype, int N, int In, int K)
     p.rest_rows = p.PL == 1 && N <= kRestRows ? p.NP : 0;
     p.rest_at = take(p.PL == 1 ? (size_t)N * 4 : 0);
     p.dz_at = take((size_t)p.PL * 2 * (p.NP + p.rest_rows) * p.ld_dz);
-    p.da_splits = splits_of(dtype, n_tiles * d_tiles, (int)div_up(most, kStep));
+    p.da_tn = tile_of(N, d_tiles * splits_of(dtype, d_tiles, (int)div_up(most, kStep)));
+    p.da_splits = splits_of(dtype, div_up(N, p.da_tn) * d_tiles, (int)div_up(most, kStep));
     p.da_at = take((size_t)p.da_splits * N * p.InP * 4);
     p.dw_tn = tile_of(most, d_tiles);
     p.dw_splits = splits_of(dtype, d_tiles * div_up(most, p.dw_tn), (p.NP + p.rest_rows) / kStep);
     p.dw_at = take(p.dw_splits == 1 || N <= kFewRows ? 0 : (size_t)p.dw_splits * most * p.InP * 4);
     // rows' ranges that db is summed in
-    p.db_parts = (int)(p.z_splits ? div_up(N, N < 512 ? 8 : div_up(N, 64)) 
+    p.db_parts = (int)(p.z_splits ? div_up(N, N < 256 ? 4 : div_up(N, 64)) 
                        : div_up(N, p.grad_tn));
     p.db_at = take(p.db_parts == 1 ? 0 : (size_t)p.db_parts * p.ld_dz * 4);
     p.backward_bytes = at;
@@ -1175,7 +1177,7 @@ int backward(const Call &c, int g_dtype, const float *stats, const float *g, voi
             q.rows = c.In; q.cols = c.N; q.steps = steps; q.splits = pl.da_splits < steps ? pl.da_splits : steps;
             q.ea = eg; q.more[0] = w_most;
             q.out = da_part; q.ld = pl.InP; q.part = (size_t)c.N * pl.InP; q.add = piece > 0;
-            if ((rc = product<true, false, kStore>(pl.PL, pl.tn, q, c.s))) return rc;
+            if ((rc = product<true, false, kStore>(pl.PL, pl.da_tn, q, c.s))) return rc;
         }
         if (dw) {
             Product q = {};
