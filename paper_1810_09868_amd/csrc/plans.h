@@ -52,6 +52,115 @@ inline bool xent_is_small(int dtype, int N, int In, int K)
     return dtype == VGG_F32 && N <= 4096 && In <= 1024 && K <= 2048 && n * k * In <= kXentSmall;
 }
 
+// Other products: tiles of 256 rows (classes for the scores, inputs for da and dw) and 64, 128 or 256 columns.
+constexpr int kTA = 256;      // rows of C in a tile
+constexpr int kStep = 64;     // contractions are whole multiples of this many indices
+constexpr size_t kPieceBytes = 512u << 20;   // what a piece of the classes may take of the workspace,
+constexpr long kPieceClasses = 1 << 20;      // and how many there are (a tile's 256 rows of dz by offsets of 31 bits)
+// bf16 rows up to which what rounding leaves of dz enters dw, as a contraction twice as long.  Off by 2^-9 of each term, dw is as exact as its own
+// rounding to bf16 on the average of many rows; the fewer there are, the more hangs on single ones.
+constexpr int kRestRows = 512;
+constexpr int kOuterRows = 16;               // rows up to which dw is written by its own kernel
+
+inline int up(long v, int to) { return (int)((v + to - 1) / to * to); }
+inline long div_up(long a, long b) { return (a + b - 1) / b; }
+
+// Columns of a tile, of examples for the scores and da, of classes for dw: as many as leave no half of it empty, and give every compute unit a tile
+// of its own where that can be.
+inline int tile_of(int cols, long row_tiles)
+{
+    int tn = cols > 128 ? 256 : cols > 64 ? 128 : 64;
+    while (tn > 64 && row_tiles * div_up(cols, tn) < 256) tn /= 2;
+    return tn;
+}
+// Ranges of a contraction of `steps` stages, where `tiles` do not fill the chip: at least 256 indices of bf16 operands each, or 128 of
+// fp32 ones, which take three times as long.
+inline int splits_of(int dtype, long tiles, int steps)
+{
+    const long most = div_up(steps, dtype == VGG_BF16 ? 4 : 2), want = tiles >= 256 ? 1 : div_up(256, tiles);
+    return (int)(want < most ? want : most);
+}
+
+struct XentPlan {
+    int PL, In, InP, NP, tn, grad_tn;
+    bool direct_w, direct_a;      // read where they are (bf16, whole stages)
+    int classes, pieces;          // of a piece (the last has what is left)
+    int z_splits;                 // 0: scores' tiles end in their sums or gradients; else their parts are added up (then one piece)
+    int ld_dz, rest_rows;
+    size_t ld_z;
+    // forward
+    size_t a_at, w_at, ea_at, ew_at, z_at, sums_at, label_at, forward_bytes;
+    // backward
+    int da_splits, da_tn, dw_splits, dw_tn, db_parts;
+    size_t a2_at, eg_at, most_at, rest_at, tail_at, dz_at, da_at, dw_at, db_at, backward_bytes;
+};
+
+inline XentPlan xent_plan(int dtype, int N, int In, int K)
+{
+    XentPlan p;
+    p.PL = dtype == VGG_BF16 ? 1 : 2;
+    p.In = In; p.InP = up(In, kStep); p.NP = up(N, kStep);
+    // (the contraction of scores of few tiles is split: their columns by what that leaves idle)
+    p.tn = tile_of(N, div_up(K, kTA) * splits_of(dtype, div_up(K, kTA), p.InP / kStep));
+    p.grad_tn = p.PL == 2 && p.tn == 256 ? 128 : p.tn;     // (256: more registers than there are)
+    p.direct_w = p.direct_a = dtype == VGG_BF16 && In % kStep == 0;
+    const long n_tiles = div_up(N, p.tn), d_tiles = div_up(In, kTA);
+    const int steps = p.InP / kStep;
+    // scores of few tiles: their contraction is split, so that all of them have to be kept for a moment
+    const long z_tiles = div_up(K, kTA) * n_tiles;
+    p.z_splits = z_tiles < 128 && steps >= 8 ? splits_of(dtype, z_tiles, steps) : 0;
+    if (p.z_splits == 1) p.z_splits = 0;
+    const size_t per_class = (size_t)p.PL * 2 * (p.NP + (p.direct_w ? 0 : p.InP));
+    long classes = (long)(kPieceBytes / per_class) / kTA * kTA;
+    if (classes < kTA) classes = kTA;
+    if (classes > kPieceClasses) classes = kPieceClasses;
+    if (p.z_splits || classes > K) classes = up(K, kTA);      // (z_splits: one piece)
+    // as large as they may be, and of the 64 largest sizes the one whose tiles leave least of the chip idle in their last rounds
+    const long all = div_up(K, kTA), largest = classes / kTA < all ? classes / kTA : all;
+    auto rounds = [&](long tiles) { return div_up(tiles * n_tiles, 256); };
+    long best = 0, best_rounds = 0;
+    for (long t = largest; t > 0 && t > largest - (p.z_splits ? 1 : 64); --t) {
+        const long r = all / t * rounds(t) + (all % t ? rounds(all % t) : 0);
+        if (!best || r < best_rounds) { best = t; best_rounds = r; }
+    }
+    p.classes = (int)(best * kTA);
+    p.pieces = (int)div_up(K, p.classes);
+    const int most = p.classes < K ? p.classes : K;
+    p.ld_dz = up(most, kStep);
+    p.ld_z = up(K, 4);
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t here = at; at += (bytes + 255) / 256 * 256; return here; };
+    // (the gradients take the activations laid out in any case: rows without a label have to be zeros)
+    p.a_at = take((size_t)p.PL * 2 * p.NP * p.InP);
+    p.w_at = take(p.direct_w ? 0 : (size_t)p.PL * 2 * up(most, kStep) * p.InP);
+    p.ea_at = take(p.PL == 2 ? (size_t)N * 4 : 0);
+    p.ew_at = take(p.PL == 2 ? (size_t)most * 4 : 0);
+    p.z_at = take(p.z_splits ? (size_t)p.z_splits * N * p.ld_z * 4 : 0);
+    const size_t both = at;
+    p.sums_at = take(p.z_splits ? 0 : (size_t)div_up(K, kTA) * N * 8);
+    p.label_at = take(p.z_splits ? 0 : (size_t)N * 4);
+    p.forward_bytes = at;
+    at = both;
+    p.a2_at = take(p.PL == 2 ? (size_t)4 * p.NP * p.InP : 0);
+    p.eg_at = take(p.PL == 2 ? (size_t)N * 4 : 0);
+    p.most_at = take(p.PL == 2 ? (size_t)(p.pieces + 1) * 4 : 0);
+    p.tail_at = take(p.direct_w ? (size_t)kStep * In * 2 : 0);
+    p.rest_rows = p.PL == 1 && N <= kRestRows ? p.NP : 0;
+    p.rest_at = take(p.PL == 1 ? (size_t)N * 4 : 0);
+    p.dz_at = take((size_t)p.PL * 2 * (p.NP + p.rest_rows) * p.ld_dz);
+    p.da_tn = tile_of(N, d_tiles * splits_of(dtype, d_tiles, (int)div_up(most, kStep)));
+    p.da_splits = splits_of(dtype, div_up(N, p.da_tn) * d_tiles, (int)div_up(most, kStep));
+    p.da_at = take((size_t)p.da_splits * N * p.InP * 4);
+    p.dw_tn = tile_of(most, d_tiles);
+    p.dw_splits = splits_of(dtype, d_tiles * div_up(most, p.dw_tn), (p.NP + p.rest_rows) / kStep);
+    p.dw_at = take(p.dw_splits == 1 || N <= kOuterRows ? 0 : (size_t)p.dw_splits * most * p.InP * 4);
+    // rows' ranges that db is summed in
+    p.db_parts = (int)(p.z_splits ? div_up(N, N < 256 ? 4 : div_up(N, 64)) : div_up(N, p.grad_tn));
+    p.db_at = take(p.db_parts == 1 ? 0 : (size_t)p.db_parts * p.ld_dz * 4);
+    p.backward_bytes = at;
+    return p;
+}
+
 // ------------------------------------------------------------------------------------------------ orthogonalised updates
 inline int round_to(int v, int to) { return (v + to - 1) / to * to; }
 

@@ -9,6 +9,7 @@ import torch
 from paper_1810_09868_amd import binding as B
 
 from gpu_util import TDT, ws_bytes
+from plan_shapes import XENT
 
 pytestmark = pytest.mark.gpu
 
@@ -117,8 +118,13 @@ def test_loss_and_gradients(dtype, g_dtype, N, In, K):
     Xent(dtype, N, In, K, N + In + K, g_dtype=g_dtype, bias=K % 2 == 0).run().check()
 
 
+@pytest.mark.parametrize("dtype,N,In,K", list(XENT))
+def test_every_width_of_tiles(dtype, N, In, K):
+    Xent(dtype, N, In, K, 18, masked=0.05).run().check()
+
+
 @pytest.mark.parametrize("dtype", [B.F32, B.BF16])
-@pytest.mark.parametrize("N,In,K", [(8200, 64, 17000), (4100, 70, 20011), (8192, 130, 9000)])
+@pytest.mark.parametrize("N,In,K", [(8200, 64, 40000), (16390, 70, 20011), (30000, 130, 9000)])
 def test_classes_in_pieces(dtype, N, In, K):
     Xent(dtype, N, In, K, 3, masked=0.1).run().check()
 
