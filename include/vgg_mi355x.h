@@ -452,8 +452,9 @@ int vgg_layer_norm_bwd(int dtype, int g_dtype, int N, int C, size_t ldx, const v
  * without a class left has the loss inf (stats -inf).  A NaN or +inf among a
  * row's scores makes its loss NaN; in fp32 an infinity among activations or
  * weights makes the scores it has part in infinite or NaN.  Products are
- * summed in fp32; fp32 operands enter them with 22 bits (the elements of a row down to 2^-18 of
- * its largest, others exact to 2^-40 of that); loss and stats are fp32.
+ * summed in fp32; fp32 operands enter them with 22 bits (activations down to 2^-17
+ * of their row's largest, weights of the largest of all, and exact to 2^-39 of
+ * that below); loss and stats are fp32.
  * N <= 2^22, In <= 2^20, K <= 2^24. */
 size_t vgg_fc_xent_workspace_bytes(int dtype, int N, int In, int K);
 int vgg_fc_xent(int dtype, int N, int In, int K, const void *a, const void *w, const float *bias, const int32_t *labels,
@@ -466,12 +467,12 @@ int vgg_fc_xent(int dtype, int N, int In, int K, const void *a, const void *w, c
  * activations, weights and bias.  The scores are formed again, in pieces of
  * the classes that take up to 512 MB of workspace (or 256 classes).  bf16: dz is
  * rounded to bf16 where it enters the two products, as in vgg_fc_bwd, not in
- * db, but what that leaves of it at a row's label enters da, and with up to 512 rows
- * all of it dw.  fp32: operands of the products have 22 bits, but dz times its class's largest weight
- * no more than down to 2^-40 of g_loss[n] times the largest weight of all.  Sums are
- * fp32.  relu_mask != 0: a is what a ReLU left, and da is 0 where a > 0 does not hold.  Masked classes have no gradient.  Rows without a label
- * or with g_loss 0 have the gradient 0 and no part in dw and db, whatever
- * their activations hold. */
+ * db, but what that leaves of it at a row's label enters da, and with up to 512
+ * rows all of it dw.  fp32: operands of the products have 22 bits as above, dz
+ * down to 2^-17 of the row's g_loss and exact to 2^-39 of it below.  Sums are
+ * fp32.  relu_mask != 0: a is what a ReLU left, and da is 0 where a > 0 does not
+ * hold.  Masked classes have no gradient.  Rows without a label or with g_loss 0
+ * have the gradient 0 and no part in dw and db, whatever their activations hold. */
 size_t vgg_fc_xent_bwd_workspace_bytes(int dtype, int N, int In, int K);
 int vgg_fc_xent_bwd(int dtype, int g_dtype, int N, int In, int K, const void *a, const void *w, const float *bias,
                     const int32_t *labels, const float *stats, const float *g_loss, void *da, void *dw, float *db,

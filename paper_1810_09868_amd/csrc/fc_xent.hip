@@ -8,13 +8,14 @@
 // The three products are one kernel: C[col][row] = sum_k A[row][k] B[col][k], where an operand lies by its rows or by the contraction
 // index (which is then read transposed out of LDS).  bf16 operands are multiplied as they are, fp32 ones in two f16 parts, 22 bits: their
 // products without those of two second parts are off by 2^-22, and are three where three bf16 parts need six.  f16 has few exponents, so
-// each row of activations and weights is laid out in units of a power of two of its own, in which its largest is between 2^14 and 2^15; what
-// is 2^18 times smaller has 22 bits still, and below that 2^-40 of the largest is left out:
-//     a = a' 2^(ea[n] - 14),  w = w' 2^(ew[k] - 14),  z = sum_i a' w' 2^(ea[n] + ew[k] - 28).
-// A contraction needs units that do not depend on its index.  With 2^eg[n] <= |g_loss[n]| < 2 2^eg[n], W = max ew and A = max (ea + eg),
-//     D = dz 2^(-eg[n]) 2^(ew[k] - W) 2^14,   da = sum_k D w' 2^(eg[n] + W - 28),
-//     a" = a 2^(eg[n] - A) 2^14,              dw = sum_n D a" 2^(A + W - ew[k] - 28):
-// a row's da has its digits however small its weight in the loss, and dw loses those of rows that add next to nothing to it.
+// operands are laid out in units of powers of two, in which the largest is between 2^14 and 2^15; what is 2^17 times smaller has 22 bits still, and
+// below that 2^-39 of the largest is left out.  Activations have units of their own in every row, weights one in all of a piece, W:
+//     a = a' 2^(ea[n] - 14),  w = w' 2^(W - 14),  z = sum_i a' w' 2^(ea[n] + W - 28).
+// A contraction needs units that do not depend on its index.  With 2^eg[n] <= |g_loss[n]| < 2 2^eg[n] and A = max (ea + eg),
+//     D = dz 2^(14 - eg[n]),      da = sum_k D w' 2^(eg[n] + W - 28),
+//     a" = a 2^(eg[n] - A + 14),  dw = sum_n D a" 2^(A - 28):
+// a row's da has its digits however small its weight in the loss, and dw loses those of rows that add next to nothing to it.  (With weights in
+// units of their rows, D would have to make up for them: a class of small weights would lose its dw.)
 #include "common.h"
 #include "dropout.h"
 #include "exp_of.h"
@@ -52,8 +53,8 @@ __device__ __forceinline__ Sums joined(Sums a, Sums b)
 struct Product {
     Operand a, b;
     int rows, cols, steps, splits;   // of C; the contraction's indices in whole 64s; ranges of them
-    // fp32: C's units, 2^(ea[col] + ew[row] + *more - less[col] - 28), each where it is given
-    const int *ea, *ew, *more[2], *less;
+    // fp32: C's units, 2^(ea[col] + *most - 28), each where it is given
+    const int *ea, *most;
     // kStore: C[col][row], a row of C^T every ld elements, fp32 or bf16; a range's every `part` elements, added to what is there if asked
     void *out;
     size_t ld, part;
@@ -65,7 +66,7 @@ struct Product {
     Sums *sums;                          // kStats: [tiles of classes, of all pieces][N]
     float *z_label;                      // [N]
     const float *stats, *g;              // kGrad: [N][2], [N]
-    const int *eg, *w_most;              // fp32: eg, W
+    const int *eg;                       // fp32
     bf16_t *dz;                          // [N ...][ld_dz], parts side by side
     int ld_dz;                           // classes of a row
     int rest_rows;                       // bf16: what rounding leaves of dz lies so many rows on; 0: it is not kept
@@ -100,6 +101,9 @@ __device__ __forceinline__ float rest_of(float v)
 }
 // e with 2^e <= |v| < 2 2^e; 0 for zeros and what is not finite.
 __device__ __forceinline__ int exponent_of(float v) { return v != 0.f && __builtin_fabsf(v) < INFINITY ? ilogbf(v) : 0; }
+
+// The largest exponent of all, 0 where there are zeros only.
+__device__ __forceinline__ int most_of(const int *most) { return *most == INT_MIN ? 0 : *most; }
 
 typedef __attribute__((address_space(3))) char lds_char;
 
@@ -138,7 +142,7 @@ __host__ __device__ constexpr int main_lds_of(int tn, int mode, int stages)
     return run > end ? run : end;
 }
 // ... and behind that the tile's biases and examples
-__host__ __device__ constexpr int lds_of(int tn, int mode, int stages) { return main_lds_of(tn, mode, stages) + (mode == kStore ? 0 : kTA * 8 + tn * (int)sizeof(Example)); }
+__host__ __device__ constexpr int lds_of(int tn, int mode, int stages) { return main_lds_of(tn, mode, stages) + (mode == kStore ? 0 : kTA * 4 + tn * (int)sizeof(Example)); }
 
 template <bool A_TR, bool B_TR, int TN, int PL, int MODE>
 __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
@@ -200,17 +204,14 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
     // What the tile's end needs of its classes and examples: asked for now, put into LDS then.
     float own_bias = -INFINITY;
     float own_m = 0.f, own_log_s = 0.f, own_g = 0.f;
-    int own_label = -1, own_ea = 0, own_eg = 0, own_ew = 0;
+    int own_label = -1, own_ea = 0, own_eg = 0;
     if constexpr (MODE != kStore) {
         const int row = ti * kTA + (int)threadIdx.x, col = tj * TN + (int)threadIdx.x;
-        if (threadIdx.x < kTA && row < p.classes) {
-            own_bias = p.bias ? p.bias[p.class0 + row] : 0.f;
-            if constexpr (PL == 2) own_ew = p.ew[row];
-        }
+        if (threadIdx.x < kTA && row < p.classes) own_bias = p.bias ? p.bias[p.class0 + row] : 0.f;
         if (threadIdx.x < TN && col < p.cols) {
             const int label = p.labels[col];
             own_label = (int)((unsigned)label - p.class0);
-            if constexpr (PL == 2) own_ea = p.ea[col];
+            if constexpr (PL == 2) own_ea = p.ea[col] + most_of(p.most) - 28;
             if constexpr (MODE == kGrad) {
                 own_m = p.stats[2 * (size_t)col];
                 own_log_s = p.stats[2 * (size_t)col + 1];
@@ -296,15 +297,13 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
         constexpr int ROWS = BX * 32, STRIDE = ROWS * 4 + 16, LANES = ROWS / 8;
         char *turned = lds + wave * (32 * STRIDE);
         const int r8 = lane % LANES * 8, row = ti * kTA + wi + r8;
-        int units[8] = {}, of_col[BY] = {};     // exponents of this lane's rows, and of column lane % 32 of a block
+        int of_col[BY] = {};     // the exponent of column lane % 32 of a block
         if constexpr (PL == 2) {
-            const int all = (p.more[0] ? *p.more[0] : 0) + (p.more[1] ? *p.more[1] : 0) - 28;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) units[k] = p.ew && row + k < p.rows ? p.ew[row + k] : 0;
+            const int all = (p.most ? most_of(p.most) : 0) - 28;
 #pragma unroll
             for (int y = 0; y < BY; ++y) {
                 const int col = tj * TN + wj + y * 32 + (lane & 31);
-                of_col[y] = all + (col < p.cols ? (p.ea ? p.ea[col] : 0) - (p.less ? p.less[col] : 0) : 0);
+                of_col[y] = all + (p.ea && col < p.cols ? p.ea[col] : 0);
             }
         }
 #pragma unroll
@@ -325,8 +324,8 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
                     const int e = __shfl(of_col[y], c);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        lo[k] = ldexpf(lo[k], e + units[k]);
-                        hi[k] = ldexpf(hi[k], e + units[k + 4]);
+                        lo[k] = ldexpf(lo[k], e);
+                        hi[k] = ldexpf(hi[k], e);
                     }
                 }
                 if (col < p.cols && n > 0) {
@@ -356,9 +355,8 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
     } else {
         // scores of this lane: example tj TN + wj + 32 y + lane % 32, class row0 + 32 x + 8 (v / 4) + v % 4 of the piece
         float *bias = reinterpret_cast<float *>(lds + main_lds_of(TN, MODE, stages_of(TN)));
-        int *ew = reinterpret_cast<int *>(bias + kTA);
-        Example *examples = reinterpret_cast<Example *>(ew + kTA);
-        if (threadIdx.x < kTA) { bias[threadIdx.x] = own_bias; ew[threadIdx.x] = own_ew; }
+        Example *examples = reinterpret_cast<Example *>(bias + kTA);
+        if (threadIdx.x < kTA) bias[threadIdx.x] = own_bias;
         if (threadIdx.x < TN) {
             Example &e = examples[threadIdx.x];
             e.label = own_label;
@@ -373,13 +371,11 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const f32x4 b = *reinterpret_cast<const f32x4 *>(bias + row0 + 32 * x + 8 * q);     // (-inf past the last class)
-                typedef int i32x4 __attribute__((ext_vector_type(4)));
-                const i32x4 e = *reinterpret_cast<const i32x4 *>(ew + row0 + 32 * x + 8 * q);
 #pragma unroll
                 for (int y = 0; y < BY; ++y) {
-                    const int ea = PL == 2 ? examples[wj + 32 * y + (lane & 31)].ea - 28 : 0;
+                    const int ea = PL == 2 ? examples[wj + 32 * y + (lane & 31)].ea : 0;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) acc[x][y][4 * q + k] = b[k] + (PL == 2 ? ldexpf(acc[x][y][4 * q + k], ea + e[k]) : acc[x][y][4 * q + k]);
+                    for (int k = 0; k < 4; ++k) acc[x][y][4 * q + k] = b[k] + (PL == 2 ? ldexpf(acc[x][y][4 * q + k], ea) : acc[x][y][4 * q + k]);
                 }
             }
         // the score of this lane's label, if it is among the lane's
@@ -472,7 +468,6 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
             }
             // dz, a part (bf16: it, and what rounding leaves of it) at a time: [example][class] in LDS, then runs of 512 (fp32: 64) bytes
             const int parts = PL == 1 && p.rest_rows ? 2 : PL;
-            const int units = PL == 2 ? 14 - *p.w_most : 0;
 #pragma unroll
             for (int part = 0; part < 2; ++part) {
                 if (part >= parts) continue;
@@ -482,8 +477,7 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
 #pragma unroll
                     for (int x = 0; x < BX; ++x) {
                         // (the second parts anew, not all of them kept from the first ones' turn on)
-                        int r0 = row0;
-                        if (PL == 2 || part == 1) asm volatile("" : "+v"(acc[x][y]), "+v"(r0));
+                        if (PL == 2 || part == 1) asm volatile("" : "+v"(acc[x][y]));
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {
                             f32x4 w = {acc[x][y][4 * q], acc[x][y][4 * q + 1], acc[x][y][4 * q + 2], acc[x][y][4 * q + 3]};
@@ -494,7 +488,7 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
                             } else {
                                 if (part == 0) {
 #pragma unroll
-                                    for (int k = 0; k < 4; ++k) acc[x][y][4 * q + k] = w[k] = ldexpf(w[k], units - eg + ew[r0 + 32 * x + 8 * q + k]);
+                                    for (int k = 0; k < 4; ++k) acc[x][y][4 * q + k] = w[k] = ldexpf(w[k], 14 - eg);
                                 }
                                 f16x4 h[2];
                                 two_parts(w, 0, h);
@@ -568,16 +562,46 @@ __global__ __launch_bounds__(256) void xent_lay_kernel(const bf16_t *__restrict_
         *reinterpret_cast<Eight<bf16_t>::u32x4 *>(to + (size_t)row * cols_p + c) = v.w;
     }
 }
-// An fp32 matrix in two f16 parts: in units of its own, e[row] - 14, whose largest (with eg[row], of g[row], where there are
-// weights) goes into *most, which began as INT_MIN; or, again, in units of eg[row] - *most + 14.
-template <bool AGAIN, int U, int W>      // W waves to a row, U groups of eight columns a lane in registers; U = 0: rows of any length, met twice
+// The largest exponent of a matrix [rows][cols], but for masked rows, into *most, which began as INT_MIN.
+__global__ __launch_bounds__(256) void xent_most_kernel(const float *__restrict__ from, int rows, int cols, const float *__restrict__ bias, int *most)
+{
+    __shared__ float waves[4];
+    float m = 0.f;
+    for (int row = blockIdx.x * 4 + (threadIdx.x >> 6); row < rows; row += gridDim.x * 4) {
+        if (bias && !(bias[row] > -INFINITY)) continue;
+        const float *src = from + (size_t)row * cols;
+        for (int c = (threadIdx.x & 63) * 8; c < cols; c += 512) {
+            Eight<float> v;
+            v.load(src + c, cols - c);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float x = __builtin_fabsf(v.get(k));
+                m = x < INFINITY ? fmaxf(m, x) : m;
+            }
+        }
+    }
+    m = all_max(m);
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = m;
+    __syncthreads();
+    if (threadIdx.x) return;
+    m = fmaxf(fmaxf(waves[0], waves[1]), fmaxf(waves[2], waves[3]));
+    // (the same in any order; most workgroups find that it is as large already)
+    if (m > 0.f && exponent_of(m) > __hip_atomic_load(most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(most, exponent_of(m));
+}
+// An fp32 matrix in two f16 parts.  kOwn: in units of its rows, whose exponents go into e and the largest of them (with eg[row], of g[row], where there
+// are weights) into *most, which began as INT_MIN.  kShared: of what eg[row] leaves of *most.  kAll: of *most, masked rows as zeros.  `clean`:
+// exponents yet to be sought begin as INT_MIN.
+enum { kOwn, kShared, kAll };
+template <int KIND, int U, int W>      // W waves to a row, U groups of eight columns a lane in registers; U = 0: rows of any length, met twice
 __global__ __launch_bounds__(256) void xent_lay32_kernel(const float *__restrict__ from, int rows, int cols, bf16_t *to, int rows_p, int cols_p, const int32_t *labels,
-                                                         const float *g, int classes, const float *bias, int *e, int *eg, int *most)
+                                                         const float *g, int classes, const float *bias, int *e, int *eg, int *most, int *clean, int cleaned)
 {
     constexpr int LANES = 64 * W, ROWS = 4 / W;
     __shared__ float waves[2][4];
     const int lane = threadIdx.x % LANES, groups = cols_p / 8;
     int largest = INT_MIN, turn = 0;
+    if (clean && blockIdx.x == 0)
+        for (int k = threadIdx.x; k < cleaned; k += 256) clean[k] = INT_MIN;
     auto magnitude = [](const Eight<float> &v) __attribute__((always_inline)) {
         float m = 0.f;
 #pragma unroll
@@ -595,7 +619,8 @@ __global__ __launch_bounds__(256) void xent_lay32_kernel(const float *__restrict
 #pragma unroll
         for (int u = 0; u < U; ++u) kept[u].load(there && group_of(u) * 8 < cols ? src + group_of(u) * 8 : from, there ? cols - group_of(u) * 8 : 0);
         int unit;
-        if constexpr (AGAIN) unit = there ? eg[row] - *most + 14 : 0;
+        if constexpr (KIND == kShared) unit = there ? eg[row] - most_of(most) + 14 : 0;
+        else if constexpr (KIND == kAll) unit = 14 - most_of(most);
         else {
             float m = 0.f;
             if constexpr (U > 0)
@@ -641,7 +666,7 @@ __global__ __launch_bounds__(256) void xent_lay32_kernel(const float *__restrict
                 write(group * 8, v);
             }
     }
-    if constexpr (!AGAIN)
+    if constexpr (KIND == kOwn)
         // (the same in any order; most waves find that it is as large already)
         if (lane == 0 && most && largest > __hip_atomic_load(most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(most, largest);
 }
@@ -728,8 +753,7 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(Scores z, const int32_t 
 // dz [PL][N][ld_dz] of all classes, and db of a range of rows: 256 classes to a workgroup, four rows at a time.
 template <int PL>
 __global__ __launch_bounds__(256) void xent_grad_kernel(Scores z, const int32_t *__restrict__ labels, const float *__restrict__ stats, const float *__restrict__ g,
-                                                        bf16_t *dz, int ld_dz, float *db, size_t ld_db, const int *__restrict__ ew, const int *__restrict__ eg,
-                                                        const int *__restrict__ w_most, int rest_rows, float *rest_of_label)
+                                                        bf16_t *dz, int ld_dz, float *db, size_t ld_db, const int *__restrict__ eg, int rest_rows, float *rest_of_label)
 {
     __shared__ f32x4 sums[4][64];
     const int k = blockIdx.x * 256 + (threadIdx.x & 63) * 4, r = threadIdx.x >> 6;
@@ -758,7 +782,7 @@ __global__ __launch_bounds__(256) void xent_grad_kernel(Scores z, const int32_t 
                     if (k + j == y && k + j < z.classes) rest_of_label[row] = rest_of(out[j]);
             } else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) out[j] = k + j < z.classes ? ldexpf(out[j], 14 - *w_most - eg[row] + ew[k + j]) : 0.f;
+                for (int j = 0; j < 4; ++j) out[j] = ldexpf(out[j], 14 - eg[row]);
                 f16x4 h[2];
                 two_parts(out, 0, h);
 #pragma unroll
@@ -779,7 +803,7 @@ __global__ __launch_bounds__(256) void xent_grad_kernel(Scores z, const int32_t 
 // threads, and what is left is the write (4 rows, 200003 x 4096 bf16: 284 us, 5.8 TB/s of writes; in 256 x 256 tiles 432, in narrower ones 558).
 template <int PL, int NMAX, typename G>
 __global__ __launch_bounds__(256) void xent_outer_kernel(const bf16_t *__restrict__ a, int cols_a, const bf16_t *__restrict__ dz, int ld_dz, int rest_rows, int N, int cols, int classes,
-                                                         const int *__restrict__ more0, const int *__restrict__ more1, const int *__restrict__ less, G *dw)
+                                                         const int *__restrict__ most, G *dw)
 {
     const int c = (blockIdx.x * 256 + threadIdx.x) * 8, n = cols - c < 0 ? 0 : cols - c < 8 ? cols - c : 8;
     if (n == 0) return;
@@ -804,7 +828,7 @@ __global__ __launch_bounds__(256) void xent_outer_kernel(const bf16_t *__restric
         for (int k = 0; k < 8; ++k) v[r][k] = r < N ? v[r][k] : 0.f;
     }
     const int groups = (classes + 7) / 8, g0 = (int)((long)groups * blockIdx.y / gridDim.y), g1 = (int)((long)groups * (blockIdx.y + 1) / gridDim.y);
-    const int units = PL == 2 ? *more0 + *more1 - 28 : 0;
+    const int units = PL == 2 ? most_of(most) - 28 : 0;
     for (int group = g0; group < g1; ++group) {
         float w[NMAX][8];
 #pragma unroll
@@ -826,9 +850,8 @@ __global__ __launch_bounds__(256) void xent_outer_kernel(const bf16_t *__restric
 #pragma unroll
                 for (int q = 0; q < 8; ++q) out[q] = __builtin_fmaf(w[r][k], v[r][q], out[q]);
             if constexpr (PL == 2) {
-                const int e = units - less[group * 8 + k];
 #pragma unroll
-                for (int q = 0; q < 8; ++q) out[q] = ldexpf(out[q], e);
+                for (int q = 0; q < 8; ++q) out[q] = ldexpf(out[q], units);
             }
             Eight<G> e;
             e.set(out);
@@ -896,9 +919,9 @@ template <int PL, typename G> int outer(const Product &q, const bf16_t *a, int c
     const long across = div_up(q.rows, 2048), down = div_up(2048, across), most = div_up(q.cols, 8);
     const dim3 grid((unsigned)across, (unsigned)(down < most ? down : most));
     G *to = static_cast<G *>(q.out);
-    if (N <= 4) xent_outer_kernel<PL, 4, G><<<grid, 256, 0, s>>>(a, cols_a, dz, ld_dz, rest_rows, N, q.rows, q.cols, q.more[0], q.more[1], q.less, to);
-    else if (N <= 8) xent_outer_kernel<PL, 8, G><<<grid, 256, 0, s>>>(a, cols_a, dz, ld_dz, rest_rows, N, q.rows, q.cols, q.more[0], q.more[1], q.less, to);
-    else xent_outer_kernel<PL, 16, G><<<grid, 256, 0, s>>>(a, cols_a, dz, ld_dz, rest_rows, N, q.rows, q.cols, q.more[0], q.more[1], q.less, to);
+    if (N <= 4) xent_outer_kernel<PL, 4, G><<<grid, 256, 0, s>>>(a, cols_a, dz, ld_dz, rest_rows, N, q.rows, q.cols, q.most, to);
+    else if (N <= 8) xent_outer_kernel<PL, 8, G><<<grid, 256, 0, s>>>(a, cols_a, dz, ld_dz, rest_rows, N, q.rows, q.cols, q.most, to);
+    else xent_outer_kernel<PL, 16, G><<<grid, 256, 0, s>>>(a, cols_a, dz, ld_dz, rest_rows, N, q.rows, q.cols, q.most, to);
     return launch_status();
 }
 
@@ -909,15 +932,15 @@ int lay(const void *from, int rows, int cols, void *to, int rows_p, int cols_p, 
                                                                          classes);
     return launch_status();
 }
-template <bool AGAIN>
+template <int KIND>
 int lay32(const void *from, int rows, int cols, void *to, int rows_p, int cols_p, const int32_t *labels, const float *g, int classes, const float *bias, int *e, int *eg, int *most,
-          hipStream_t s)
+          int *clean, int cleaned, hipStream_t s)
 {
     auto launch = [&](auto u, auto w) {
         constexpr int W = decltype(w)::value;
         const long blocks = div_up(rows_p, 4 / W);
-        xent_lay32_kernel<AGAIN, decltype(u)::value, W><<<(int)(blocks < 2048 ? blocks : 2048), 256, 0, s>>>(static_cast<const float *>(from), rows, cols, static_cast<bf16_t *>(to),
-                                                                                                             rows_p, cols_p, labels, g, classes, bias, e, eg, most);
+        xent_lay32_kernel<KIND, decltype(u)::value, W><<<(int)(blocks < 2048 ? blocks : 2048), 256, 0, s>>>(static_cast<const float *>(from), rows, cols, static_cast<bf16_t *>(to),
+                                                                                                             rows_p, cols_p, labels, g, classes, bias, e, eg, most, clean, cleaned);
     };
     const std::integral_constant<int, 0> any{};
     const std::integral_constant<int, 1> one{};
@@ -963,14 +986,20 @@ int scores_product(const Call &c, const XentPlan &pl, int piece, bool laid_a, in
     if (pl.direct_w) p.a = {w, ld, here, nullptr};
     else {
         const int rows_p = up(here, kStep);
-        const int rc = pl.PL == 2 ? lay32<false>(w, here, c.In, c.ws + pl.w_at, rows_p, pl.InP, nullptr, nullptr, 0, c.bias ? c.bias + class0 : nullptr, at<int>(c, pl.ew_at), nullptr,
-                                               w_most, c.s)
-                                  : lay(w, here, c.In, c.ws + pl.w_at, rows_p, pl.InP, nullptr, nullptr, 0, c.s);
+        int rc;
+        if (pl.PL == 2) {
+            const float *bias = c.bias ? c.bias + class0 : nullptr;
+            const long blocks = div_up(here, 4);
+            xent_most_kernel<<<(int)(blocks < 2048 ? blocks : 2048), 256, 0, c.s>>>(reinterpret_cast<const float *>(w), here, c.In, bias, w_most);
+            if ((rc = launch_status())) return rc;
+            rc = lay32<kAll>(w, here, c.In, c.ws + pl.w_at, rows_p, pl.InP, nullptr, nullptr, 0, bias, nullptr, nullptr, w_most, nullptr, 0, c.s);
+        } else
+            rc = lay(w, here, c.In, c.ws + pl.w_at, rows_p, pl.InP, nullptr, nullptr, 0, c.s);
         if (rc) return rc;
         p.a = {c.ws + pl.w_at, ld, here, nullptr};
     }
     p.b = {laid_a ? c.ws + pl.a_at : static_cast<const char *>(c.a), ld, c.N, nullptr};
-    if (pl.PL == 2) { p.ea = at<int>(c, pl.ea_at); p.ew = at<int>(c, pl.ew_at); }
+    if (pl.PL == 2) { p.ea = at<int>(c, pl.ea_at); p.most = w_most; }
     p.bias = c.bias; p.labels = c.labels;
     p.class0 = class0; p.classes = here; p.all_classes = c.K;
     return VGG_OK;
@@ -986,15 +1015,15 @@ int scores_in_parts(const XentPlan &pl, const Call &c, Product &p, Scores &z)
 int forward(const Call &c, float *loss, float *stats)
 {
     const XentPlan pl = xent_plan(c.dtype, c.N, c.In, c.K);
-    int rc = VGG_OK;
-    if (pl.PL == 2) rc = lay32<false>(c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, nullptr, nullptr, 0, nullptr, at<int>(c, pl.ea_at), nullptr, nullptr, c.s);
+    int rc = VGG_OK, *most = pl.PL == 2 ? at<int>(c, pl.most_at) + 1 : nullptr;      // the pieces' (behind what the gradients need of the activations)
+    if (pl.PL == 2) rc = lay32<kOwn>(c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, nullptr, nullptr, 0, nullptr, at<int>(c, pl.ea_at), nullptr, nullptr, most, pl.pieces, c.s);
     else if (!pl.direct_a) rc = lay(c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, nullptr, nullptr, 0, c.s);
     if (rc) return rc;
     Sums *sums = at<Sums>(c, pl.sums_at);
     float *z_label = at<float>(c, pl.label_at);
     for (int piece = 0; piece < pl.pieces; ++piece) {
         Product p;
-        if ((rc = scores_product(c, pl, piece, !pl.direct_a, nullptr, p))) return rc;
+        if ((rc = scores_product(c, pl, piece, !pl.direct_a, most ? most + piece : nullptr, p))) return rc;
         if (pl.z_splits) {
             Scores z;
             if ((rc = scores_in_parts(pl, c, p, z))) return rc;
@@ -1015,7 +1044,7 @@ int backward(const Call &c, int g_dtype, const float *stats, const float *g, voi
     const int gs = g_dtype == VGG_BF16 ? 2 : 4;
     const bool two = pl.PL == 2;
     bf16_t *dz = at<bf16_t>(c, pl.dz_at);
-    int *ea = two ? at<int>(c, pl.ea_at) : nullptr, *ew = two ? at<int>(c, pl.ew_at) : nullptr, *eg = two ? at<int>(c, pl.eg_at) : nullptr;
+    int *ea = two ? at<int>(c, pl.ea_at) : nullptr, *eg = two ? at<int>(c, pl.eg_at) : nullptr;
     int *a_most = two ? at<int>(c, pl.most_at) : nullptr;        // and, behind it, the pieces'
     const size_t past = (size_t)(pl.NP - c.N) * pl.ld_dz * pl.PL / 8;
     int rc;
@@ -1029,8 +1058,8 @@ int backward(const Call &c, int g_dtype, const float *stats, const float *g, voi
     }
     bf16_t *a_of_dw = at<bf16_t>(c, two ? pl.a2_at : pl.a_at);
     if (two) {
-        if ((rc = lay32<false>(c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, c.labels, g, c.K, nullptr, ea, eg, a_most, c.s))) return rc;
-        if (dw && (rc = lay32<true>(c.a, c.N, c.In, a_of_dw, pl.NP, pl.InP, c.labels, g, c.K, nullptr, ea, eg, a_most, c.s))) return rc;
+        if ((rc = lay32<kOwn>(c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, c.labels, g, c.K, nullptr, ea, eg, a_most, nullptr, 0, c.s))) return rc;
+        if (dw && (rc = lay32<kShared>(c.a, c.N, c.In, a_of_dw, pl.NP, pl.InP, c.labels, g, c.K, nullptr, ea, eg, a_most, nullptr, 0, c.s))) return rc;
     } else if ((rc = lay(c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, c.labels, g, c.K, c.s)))
         return rc;
     float *da_part = at<float>(c, pl.da_at), *dw_part = at<float>(c, pl.dw_at);
@@ -1045,11 +1074,11 @@ int backward(const Call &c, int g_dtype, const float *stats, const float *g, voi
             Scores z;
             if ((rc = scores_in_parts(pl, c, p, z))) return rc;
             const dim3 grid((unsigned)div_up(pl.ld_dz, 256), (unsigned)pl.db_parts);
-            if (two) xent_grad_kernel<2><<<grid, 256, 0, c.s>>>(z, c.labels, stats, g, dz, pl.ld_dz, db_to, pl.ld_dz, ew, eg, w_most, 0, nullptr);
-            else xent_grad_kernel<1><<<grid, 256, 0, c.s>>>(z, c.labels, stats, g, dz, pl.ld_dz, db_to, pl.ld_dz, ew, eg, w_most, pl.rest_rows, rest);
+            if (two) xent_grad_kernel<2><<<grid, 256, 0, c.s>>>(z, c.labels, stats, g, dz, pl.ld_dz, db_to, pl.ld_dz, eg, 0, nullptr);
+            else xent_grad_kernel<1><<<grid, 256, 0, c.s>>>(z, c.labels, stats, g, dz, pl.ld_dz, db_to, pl.ld_dz, eg, pl.rest_rows, rest);
             if ((rc = launch_status())) return rc;
         } else {
-            p.stats = stats; p.g = g; p.eg = eg; p.w_most = w_most;
+            p.stats = stats; p.g = g; p.eg = eg;
             p.dz = dz; p.ld_dz = pl.ld_dz; p.rest_rows = pl.rest_rows; p.rest_of_label = rest;
             p.db = db_to; p.ld_db = pl.ld_dz;
             if ((rc = product<false, false, kGrad>(pl.PL, pl.grad_tn, p, c.s))) return rc;
@@ -1069,7 +1098,7 @@ int backward(const Call &c, int g_dtype, const float *stats, const float *g, voi
             }
             q.b = {reinterpret_cast<const char *>(dz), ld_dz, c.N, nullptr};
             q.rows = c.In; q.cols = c.N; q.steps = steps; q.splits = pl.da_splits < steps ? pl.da_splits : steps;
-            q.ea = eg; q.more[0] = w_most;
+            q.ea = eg; q.most = w_most;
             q.out = da_part; q.ld = pl.InP; q.part = (size_t)c.N * pl.InP; q.add = piece > 0;
             if ((rc = product<true, false, kStore>(pl.PL, pl.da_tn, q, c.s))) return rc;
         }
@@ -1079,7 +1108,7 @@ int backward(const Call &c, int g_dtype, const float *stats, const float *g, voi
             q.b = {reinterpret_cast<const char *>(dz), ld_dz, (int)ld_dz, nullptr};
             q.rows = c.In; q.cols = here; q.steps = (pl.NP + pl.rest_rows) / kStep; q.splits = pl.dw_splits;
             q.wrap = pl.rest_rows / kStep;
-            q.more[0] = a_most; q.more[1] = w_most; q.less = ew;
+            q.most = a_most;
             void *out = static_cast<char *>(dw) + (size_t)class0 * c.In * gs;
             q.out = out;
             if (c.N <= kOuterRows) {

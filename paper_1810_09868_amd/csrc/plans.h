@@ -89,10 +89,10 @@ struct XentPlan {
     int ld_dz, rest_rows;
     size_t ld_z;
     // forward
-    size_t a_at, w_at, ea_at, ew_at, z_at, sums_at, label_at, forward_bytes;
+    size_t a_at, w_at, ea_at, most_at, z_at, sums_at, label_at, forward_bytes;
     // backward
     int da_splits, da_tn, dw_splits, dw_tn, db_parts;
-    size_t a2_at, eg_at, most_at, rest_at, tail_at, dz_at, da_at, dw_at, db_at, backward_bytes;
+    size_t a2_at, eg_at, rest_at, tail_at, dz_at, da_at, dw_at, db_at, backward_bytes;
 };
 
 inline XentPlan xent_plan(int dtype, int N, int In, int K)
@@ -134,7 +134,7 @@ inline XentPlan xent_plan(int dtype, int N, int In, int K)
     p.a_at = take((size_t)p.PL * 2 * p.NP * p.InP);
     p.w_at = take(p.direct_w ? 0 : (size_t)p.PL * 2 * up(most, kStep) * p.InP);
     p.ea_at = take(p.PL == 2 ? (size_t)N * 4 : 0);
-    p.ew_at = take(p.PL == 2 ? (size_t)most * 4 : 0);
+    p.most_at = take(p.PL == 2 ? (size_t)(p.pieces + 1) * 4 : 0);
     p.z_at = take(p.z_splits ? (size_t)p.z_splits * N * p.ld_z * 4 : 0);
     const size_t both = at;
     p.sums_at = take(p.z_splits ? 0 : (size_t)div_up(K, kTA) * N * 8);
@@ -143,7 +143,6 @@ inline XentPlan xent_plan(int dtype, int N, int In, int K)
     at = both;
     p.a2_at = take(p.PL == 2 ? (size_t)4 * p.NP * p.InP : 0);
     p.eg_at = take(p.PL == 2 ? (size_t)N * 4 : 0);
-    p.most_at = take(p.PL == 2 ? (size_t)(p.pieces + 1) * 4 : 0);
     p.tail_at = take(p.direct_w ? (size_t)kStep * In * 2 : 0);
     p.rest_rows = p.PL == 1 && N <= kRestRows ? p.NP : 0;
     p.rest_at = take(p.PL == 1 ? (size_t)N * 4 : 0);

@@ -26,7 +26,7 @@ static const char *fault(const vgg::XentPlan &p, int dtype, int N, int In, int K
         if (g < 1 || g >= 1l << 31) return "workgroups";
     if (!p.z_splits && p.db_parts != div_up(N, p.grad_tn)) return "db";
     if (p.direct_w && (dtype != VGG_BF16 || In % kStep)) return "weights";
-    const size_t order[] = {p.a_at, p.w_at, p.ea_at, p.ew_at, p.z_at, p.a2_at, p.eg_at, p.most_at, p.tail_at, p.rest_at, p.dz_at, p.da_at, p.dw_at, p.db_at, p.backward_bytes};
+    const size_t order[] = {p.a_at, p.w_at, p.ea_at, p.most_at, p.z_at, p.a2_at, p.eg_at, p.tail_at, p.rest_at, p.dz_at, p.da_at, p.dw_at, p.db_at, p.backward_bytes};
     for (size_t k = 1; k < sizeof order / sizeof *order; ++k)
         if (order[k] < order[k - 1] || order[k] % 256) return "places";
     return nullptr;

@@ -60,7 +60,10 @@ class Xent:
         Scores: products of bf16 numbers are exact in fp32 and those of three-part numbers left out by 2^-24; sums of 16 are cut off at 2^-23 of the larger one as
         they meet the running sum, at most In / 16 + 1 times and as often again where parts of a contraction are joined: e_z.  Exponentials 4 u, and a sum of K positive
         terms over at most 64 in turn and then in pairs: 100 u relative.  A gradient's term dz is then off by 2 e_z + 110 u of its share, and in bf16 by
-        2^-8 of itself where it enters a product; the sums over n or k as the scores'."""
+        2^-8 of itself where it enters a product; the sums over n or k as the scores'.
+
+        fp32's dz enters as two f16 parts of D = dz 2^(14 - eg), 2^eg <= |g|.  The second part's steps are no finer than f16's last, 2^-24, so D is off by up to 2^-25
+        where 22 bits of it would be less, and dz by 2^-25 2^(eg - 14) <= 2^-39 |g|: 2^-39 of a row's g for each class, however small its share."""
         a, w = self.a.double(), self.w.double()
         b = torch.zeros(self.K, dtype=torch.float64, device="cuda") if self.bias is None else self.bias.double()
         z = a @ w.t() + b
@@ -82,7 +85,8 @@ class Xent:
         e_dz = g.abs() * (p + share * (mark > 0)) * (2 * e_row + 110 * U)
         half = 2.0 ** -8 if self.dtype == B.BF16 else 4 * U
         out = {"loss": loss, "da": dz @ w, "dw": dz.t() @ a, "db": dz.sum(0)}
-        wide, finite = (dz.abs() * half + e_dz), torch.where(torch.isfinite(loss), loss, 0.0)
+        floor = 2.0 ** -39 * g.abs() if self.dtype == B.F32 else 0.0
+        wide, finite = (dz.abs() * half + e_dz + floor), torch.where(torch.isfinite(loss), loss, 0.0)
         tol = {"loss": 2 * e_row[:, 0] + 110 * U * (1 + finite.abs()), "db": (e_dz + (self.N / 32 + 80) * U * dz.abs()).sum(0)}
         sums = lambda n: 4 * (n / 16 + 70) * U  # noqa: E731
         rounding = 2.0 ** -8 if self.g_dtype == B.BF16 else U
@@ -109,7 +113,7 @@ class Xent:
 TYPES = [(B.F32, B.F32), (B.BF16, B.BF16), (B.BF16, B.F32)]
 SIZES = [(1, 1, 1), (1, 64, 2), (2, 3, 1), (3, 7, 5), (64, 128, 256), (65, 64, 257), (63, 130, 255), (128, 192, 64), (129, 66, 300), (257, 256, 513), (300, 200, 700), (1, 4096, 1000),
          (100, 4096, 1000), (5, 512, 40000), (700, 1000, 14), (1000, 33, 3000), (33, 2048, 129), (4, 1024, 10007),
-         (500, 500, 500), (4096, 70, 33), (31, 1024, 2048), (33, 1025, 65), (4097, 40, 20), (5, 8, 2049), (17, 300, 3000), (16, 100, 5000), (513, 320, 2500)]
+         (500, 500, 500), (4096, 70, 33), (31, 1024, 2048), (33, 1025, 65), (4097, 40, 20), (5, 8, 2049), (17, 300, 3000), (16, 100, 5000), (513, 320, 2500), (4097, 1, 1), (5, 1, 2049), (1, 1025, 1)]
 
 
 @pytest.mark.parametrize("dtype,g_dtype", TYPES)
@@ -247,7 +251,7 @@ def test_parts_of_the_gradient_other_streams_and_twice_the_same(dtype, N, In, K)
     assert all(torch.equal(getattr(c, k), v) for k, v in whole.items())
 
 
-@pytest.mark.parametrize("N,In,K", [(10, 40, 90), (70, 128, 300), (300, 200, 700), (40, 1024, 600)])
+@pytest.mark.parametrize("N,In,K", [(10, 40, 90), (70, 128, 300), (300, 200, 700), (40, 1024, 600), (40, 1100, 600), (300, 200, 3000), (10, 1100, 300), (200, 300, 40000)])
 def test_fp32_rows_of_any_size(N, In, K):
     """Activations, weights of the loss and classes' weights whose rows are powers of two apart: every row of da has its digits."""
     c = Xent(B.F32, N, In, K, 16)
@@ -267,9 +271,27 @@ def test_fp32_rows_of_any_size(N, In, K):
     assert float(off.max()) <= 1e-4 and float(off.median()) <= 1e-6, (float(off.max()), float(off.median()))
 
 
-def test_fp32_weights_of_masked_classes_do_not_count():
-    c = Xent(B.F32, 70, 128, 300, 17, masked=0.3)
-    c.labels.clamp_(0, 299)
+@pytest.mark.parametrize("dtype", [B.F32, B.BF16])
+@pytest.mark.parametrize("N,In,K", [(10, 40, 90), (70, 1100, 300), (10, 1100, 300), (300, 200, 3000), (200, 300, 40000)])
+def test_weights_and_activations_that_are_zeros(dtype, N, In, K):
+    c = Xent(dtype, N, In, K, 19, bias=False)
+    c.w.zero_()                                    # as a classifier may begin
+    c.run().check()
+    assert (c.da == 0).all() and float(c.dw.float().abs().max()) > 0
+    c = Xent(dtype, N, In, K, 20)
+    c.w *= 1e-4
+    c.w[::3] = 0                                   # rows of zeros among small ones
+    c.a[::2] = 0
+    c.run().check()
+    c.a.zero_()
+    c.run().check()
+    assert (c.dw == 0).all() and float(c.da.float().abs().max()) > 0
+
+
+@pytest.mark.parametrize("N,In,K", [(70, 128, 300), (70, 1100, 300), (10, 1100, 300), (300, 200, 3000)])
+def test_fp32_weights_of_masked_classes_do_not_count(N, In, K):
+    c = Xent(B.F32, N, In, K, 17, masked=0.3)
+    c.labels.clamp_(0, K - 1)
     c.run()
     want = {k: getattr(c, k).clone() for k in ("loss", "da", "dw", "db")}
     c.w[c.bias == -math.inf] = 1e30
