@@ -102,9 +102,6 @@ __device__ __forceinline__ float rest_of(float v)
 // e with 2^e <= |v| < 2 2^e; 0 for zeros and what is not finite.
 __device__ __forceinline__ int exponent_of(float v) { return v != 0.f && __builtin_fabsf(v) < INFINITY ? ilogbf(v) : 0; }
 
-// The largest exponent of all, 0 where there are zeros only.
-__device__ __forceinline__ int most_of(const int *most) { return *most == INT_MIN ? 0 : *most; }
-
 typedef __attribute__((address_space(3))) char lds_char;
 
 // Workgroups go round the eight XCDs; each takes a run of the work, so that neighbours share their operands in its L2.
@@ -211,7 +208,7 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
         if (threadIdx.x < TN && col < p.cols) {
             const int label = p.labels[col];
             own_label = (int)((unsigned)label - p.class0);
-            if constexpr (PL == 2) own_ea = p.ea[col] + most_of(p.most) - 28;
+            if constexpr (PL == 2) own_ea = p.ea[col] + *p.most - 28;
             if constexpr (MODE == kGrad) {
                 own_m = p.stats[2 * (size_t)col];
                 own_log_s = p.stats[2 * (size_t)col + 1];
@@ -299,7 +296,7 @@ __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
         const int r8 = lane % LANES * 8, row = ti * kTA + wi + r8;
         int of_col[BY] = {};     // the exponent of column lane % 32 of a block
         if constexpr (PL == 2) {
-            const int all = (p.most ? most_of(p.most) : 0) - 28;
+            const int all = (p.most ? *p.most : 0) - 28;
 #pragma unroll
             for (int y = 0; y < BY; ++y) {
                 const int col = tj * TN + wj + y * 32 + (lane & 31);
@@ -562,46 +559,47 @@ __global__ __launch_bounds__(256) void xent_lay_kernel(const bf16_t *__restrict_
         *reinterpret_cast<Eight<bf16_t>::u32x4 *>(to + (size_t)row * cols_p + c) = v.w;
     }
 }
-// The largest exponent of a matrix [rows][cols], but for masked rows, into *most, which began as INT_MIN.
-__global__ __launch_bounds__(256) void xent_most_kernel(const float *__restrict__ from, int rows, int cols, const float *__restrict__ bias, int *most)
-{
-    __shared__ float waves[4];
-    float m = 0.f;
-    for (int row = blockIdx.x * 4 + (threadIdx.x >> 6); row < rows; row += gridDim.x * 4) {
-        if (bias && !(bias[row] > -INFINITY)) continue;
-        const float *src = from + (size_t)row * cols;
-        for (int c = (threadIdx.x & 63) * 8; c < cols; c += 512) {
-            Eight<float> v;
-            v.load(src + c, cols - c);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const float x = __builtin_fabsf(v.get(k));
-                m = x < INFINITY ? fmaxf(m, x) : m;
-            }
-        }
-    }
-    m = all_max(m);
-    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = m;
-    __syncthreads();
-    if (threadIdx.x) return;
-    m = fmaxf(fmaxf(waves[0], waves[1]), fmaxf(waves[2], waves[3]));
-    // (the same in any order; most workgroups find that it is as large already)
-    if (m > 0.f && exponent_of(m) > __hip_atomic_load(most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(most, exponent_of(m));
-}
-// An fp32 matrix in two f16 parts.  kOwn: in units of its rows, whose exponents go into e and the largest of them (with eg[row], of g[row], where there
-// are weights) into *most, which began as INT_MIN.  kShared: of what eg[row] leaves of *most.  kAll: of *most, masked rows as zeros.  `clean`:
-// exponents yet to be sought begin as INT_MIN.
-enum { kOwn, kShared, kAll };
+// An fp32 matrix in two f16 parts: [rows][cols] becomes [rows_p][cols_p], rows that do not count (as above, or masked by a bias) zeros.  kMost only seeks
+// the rows' largest exponent; kOwn lays rows in units of their own, which go into e (and the exponents of g into eg), and seeks the largest of both.
+// Every workgroup leaves the largest it met in part [blocks].  The next launch makes one of the n_part of them, which it leaves in *most: kShared takes
+// units of what eg[row] leaves of it, kAll takes it as it is.  (The largest is the same in any order.)
+enum { kMost, kOwn, kShared, kAll };
+struct Lay32 {
+    const float *from;
+    int rows, cols;
+    bf16_t *to;
+    int rows_p, cols_p;
+    const int32_t *labels;
+    const float *g;
+    int classes;
+    const float *bias;
+    int *e, *eg, *part, n_part, *most;
+    int blocks;
+};
 template <int KIND, int U, int W>      // W waves to a row, U groups of eight columns a lane in registers; U = 0: rows of any length, met twice
-__global__ __launch_bounds__(256) void xent_lay32_kernel(const float *__restrict__ from, int rows, int cols, bf16_t *to, int rows_p, int cols_p, const int32_t *labels,
-                                                         const float *g, int classes, const float *bias, int *e, int *eg, int *most, int *clean, int cleaned)
+__device__ __forceinline__ void lay32_rows(const Lay32 &l, int block)
 {
+    const float *from = l.from;
+    const int rows = l.rows, cols = l.cols, rows_p = l.rows_p, cols_p = l.cols_p;
     constexpr int LANES = 64 * W, ROWS = 4 / W;
     __shared__ float waves[2][4];
+    __shared__ int most_of_wave[4];
     const int lane = threadIdx.x % LANES, groups = cols_p / 8;
-    int largest = INT_MIN, turn = 0;
-    if (clean && blockIdx.x == 0)
-        for (int k = threadIdx.x; k < cleaned; k += 256) clean[k] = INT_MIN;
+    auto most_of_all = [&](int most) __attribute__((always_inline)) {
+#pragma unroll
+        for (int d = 32; d; d >>= 1) most = max(most, __shfl_xor(most, d));
+        if ((threadIdx.x & 63) == 0) most_of_wave[threadIdx.x >> 6] = most;
+        __syncthreads();
+        return max(max(most_of_wave[0], most_of_wave[1]), max(most_of_wave[2], most_of_wave[3]));
+    };
+    int largest = INT_MIN, turn = 0, most = 0;
+    if constexpr (KIND == kShared || KIND == kAll) {
+        most = INT_MIN;
+        for (int k = threadIdx.x; k < l.n_part; k += 256) most = max(most, l.part[k]);
+        most = most_of_all(most);
+        if (most == INT_MIN) most = 0;        // of zeros only
+        if (block == 0 && threadIdx.x == 0) *l.most = most;
+    }
     auto magnitude = [](const Eight<float> &v) __attribute__((always_inline)) {
         float m = 0.f;
 #pragma unroll
@@ -611,16 +609,16 @@ __global__ __launch_bounds__(256) void xent_lay32_kernel(const float *__restrict
         }
         return m;
     };
-    for (int row = blockIdx.x * ROWS + threadIdx.x / LANES; row < rows_p; row += gridDim.x * ROWS) {
-        const bool there = row < rows && row_counts(row, labels, g, classes) && (!bias || bias[row] > -INFINITY);
+    for (int row = block * ROWS + threadIdx.x / LANES; row < rows_p; row += l.blocks * ROWS) {
+        const bool there = row < rows && row_counts(row, l.labels, l.g, l.classes) && (!l.bias || l.bias[row] > -INFINITY);
         const float *src = from + (size_t)(there ? row : 0) * cols;
         Eight<float> kept[U ? U : 1];
         auto group_of = [&](int u) __attribute__((always_inline)) { return u * LANES + lane; };
 #pragma unroll
         for (int u = 0; u < U; ++u) kept[u].load(there && group_of(u) * 8 < cols ? src + group_of(u) * 8 : from, there ? cols - group_of(u) * 8 : 0);
         int unit;
-        if constexpr (KIND == kShared) unit = there ? eg[row] - most_of(most) + 14 : 0;
-        else if constexpr (KIND == kAll) unit = 14 - most_of(most);
+        if constexpr (KIND == kShared) unit = there ? l.eg[row] - most + 14 : 0;
+        else if constexpr (KIND == kAll) unit = 14 - most;
         else {
             float m = 0.f;
             if constexpr (U > 0)
@@ -639,21 +637,22 @@ __global__ __launch_bounds__(256) void xent_lay32_kernel(const float *__restrict
                 m = fmaxf(fmaxf(waves[turn][0], waves[turn][1]), fmaxf(waves[turn][2], waves[turn][3]));
                 turn ^= 1;
             }
-            const int mine = exponent_of(m), of_g = there && g ? exponent_of(g[row]) : 0;
+            const int mine = exponent_of(m), of_g = there && l.g ? exponent_of(l.g[row]) : 0;
             unit = 14 - mine;
-            if (lane == 0 && row < rows) {
-                e[row] = mine;
-                if (eg) eg[row] = of_g;
+            if (KIND == kOwn && lane == 0 && row < rows) {
+                l.e[row] = mine;
+                if (l.eg) l.eg[row] = of_g;
             }
             if (m > 0.f && mine + of_g > largest) largest = mine + of_g;
         }
+        if constexpr (KIND == kMost) continue;
         auto write = [&](int c, const Eight<float> &v) __attribute__((always_inline)) {
             f16x4 lo[2], hi[2];
             two_parts(v.lo, unit, lo);
             two_parts(v.hi, unit, hi);
 #pragma unroll
             for (int part = 0; part < 2; ++part)
-                *reinterpret_cast<f16x8 *>(to + (size_t)row * cols_p * 2 + column_at<2>(c, part)) = __builtin_shufflevector(lo[part], hi[part], 0, 1, 2, 3, 4, 5, 6, 7);
+                *reinterpret_cast<f16x8 *>(l.to + (size_t)row * cols_p * 2 + column_at<2>(c, part)) = __builtin_shufflevector(lo[part], hi[part], 0, 1, 2, 3, 4, 5, 6, 7);
         };
         if constexpr (U > 0) {
 #pragma unroll
@@ -666,23 +665,41 @@ __global__ __launch_bounds__(256) void xent_lay32_kernel(const float *__restrict
                 write(group * 8, v);
             }
     }
-    if constexpr (KIND == kOwn)
-        // (the same in any order; most waves find that it is as large already)
-        if (lane == 0 && most && largest > __hip_atomic_load(most, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMax(most, largest);
+    if constexpr (KIND == kMost || KIND == kOwn)
+        if (l.part) {
+            largest = most_of_all(largest);
+            if (threadIdx.x == 0) l.part[block] = largest;
+        }
 }
 
-// Zeros where the contraction over examples reads past the last of them, `count` 16 bytes of dz (and of what rounding leaves of it), in rows
-// whose label no piece holds, and the largest exponents' beginnings.
-__global__ __launch_bounds__(256) void xent_clear_kernel(bf16_t *dz, bf16_t *dz_rest, size_t count, float *rest_of_label, int N, int *most, int pieces)
+// Zeros where the contraction over examples reads past the last of them, `count` 16 bytes of dz (and of what rounding leaves of it), and in rows
+// whose label no piece holds.
+struct Clear { bf16_t *dz, *dz_rest; size_t count; float *rest_of_label; int N, blocks; };
+__device__ __forceinline__ void clear(const Clear &c, int block)
 {
-    for (size_t at = (size_t)blockIdx.x * 256 + threadIdx.x; at < count; at += (size_t)gridDim.x * 256) {
-        *reinterpret_cast<f32x4 *>(dz + at * 8) = f32x4{};
-        if (dz_rest) *reinterpret_cast<f32x4 *>(dz_rest + at * 8) = f32x4{};
+    for (size_t at = (size_t)block * 256 + threadIdx.x; at < c.count; at += (size_t)c.blocks * 256) {
+        *reinterpret_cast<f32x4 *>(c.dz + at * 8) = f32x4{};
+        if (c.dz_rest) *reinterpret_cast<f32x4 *>(c.dz_rest + at * 8) = f32x4{};
     }
-    if (rest_of_label)
-        for (int at = blockIdx.x * 256 + threadIdx.x; at < N; at += gridDim.x * 256) rest_of_label[at] = 0.f;
-    if (blockIdx.x == 0)
-        for (int k = threadIdx.x; k < pieces; k += 256) most[k] = INT_MIN;
+    if (c.rest_of_label)
+        for (int at = block * 256 + threadIdx.x; at < c.N; at += c.blocks * 256) c.rest_of_label[at] = 0.f;
+}
+__global__ __launch_bounds__(256) void xent_clear_kernel(Clear c) { clear(c, blockIdx.x); }
+
+// What comes before the first product of fp32 operands, in two launches (100 x 4096 x 1000, loss and gradients: 97 us; 111 with each
+// of the five parts in a launch of its own).
+template <int U, int W> __global__ __launch_bounds__(256) void xent_first_kernel(Lay32 a, Lay32 w, Clear c)
+{
+    const int block = blockIdx.x;
+    if (block < a.blocks) lay32_rows<kOwn, U, W>(a, block);
+    else if (block < a.blocks + w.blocks) lay32_rows<kMost, U, W>(w, block - a.blocks);
+    else clear(c, block - a.blocks - w.blocks);
+}
+template <int U, int W> __global__ __launch_bounds__(256) void xent_second_kernel(Lay32 a, Lay32 w)
+{
+    const int block = blockIdx.x;
+    if (block < a.blocks) lay32_rows<kShared, U, W>(a, block);
+    else lay32_rows<kAll, U, W>(w, block - a.blocks);
 }
 
 __device__ __forceinline__ void write_loss(Sums s, float z_label, int label, int classes, float *loss, float *stats, int row)
@@ -828,7 +845,7 @@ __global__ __launch_bounds__(256) void xent_outer_kernel(const bf16_t *__restric
         for (int k = 0; k < 8; ++k) v[r][k] = r < N ? v[r][k] : 0.f;
     }
     const int groups = (classes + 7) / 8, g0 = (int)((long)groups * blockIdx.y / gridDim.y), g1 = (int)((long)groups * (blockIdx.y + 1) / gridDim.y);
-    const int units = PL == 2 ? most_of(most) - 28 : 0;
+    const int units = PL == 2 ? *most - 28 : 0;
     for (int group = g0; group < g1; ++group) {
         float w[NMAX][8];
 #pragma unroll
@@ -932,27 +949,35 @@ int lay(const void *from, int rows, int cols, void *to, int rows_p, int cols_p, 
                                                                          classes);
     return launch_status();
 }
-template <int KIND>
-int lay32(const void *from, int rows, int cols, void *to, int rows_p, int cols_p, const int32_t *labels, const float *g, int classes, const float *bias, int *e, int *eg, int *most,
-          int *clean, int cleaned, hipStream_t s)
+// fp32: a row's waves and its groups in registers, for activations and weights alike, which are as long; f takes both as constants.
+template <typename F> int by_length(int cols, F f)
 {
-    auto launch = [&](auto u, auto w) {
-        constexpr int W = decltype(w)::value;
-        const long blocks = div_up(rows_p, 4 / W);
-        xent_lay32_kernel<KIND, decltype(u)::value, W><<<(int)(blocks < 2048 ? blocks : 2048), 256, 0, s>>>(static_cast<const float *>(from), rows, cols, static_cast<bf16_t *>(to),
-                                                                                                             rows_p, cols_p, labels, g, classes, bias, e, eg, most, clean, cleaned);
-    };
     const std::integral_constant<int, 0> any{};
     const std::integral_constant<int, 1> one{};
     const std::integral_constant<int, 2> two{};
     const std::integral_constant<int, 4> four{};
-    if (cols <= 512) launch(one, one);
-    else if (cols <= 1024) launch(two, one);
-    else if (cols <= 2048) launch(one, four);
-    else if (cols <= 4096) launch(two, four);
-    else if (cols <= 8192) launch(four, four);
-    else launch(any, four);
+    if (cols <= 512) f(one, one);
+    else if (cols <= 1024) f(two, one);
+    else if (cols <= 2048) f(one, four);
+    else if (cols <= 4096) f(two, four);
+    else if (cols <= 8192) f(four, four);
+    else f(any, four);
     return launch_status();
+}
+int lay32_blocks(int rows, int cols)
+{
+    const long blocks = cols <= 1024 ? div_up(rows, 4) : rows;
+    return (int)(blocks < kParts ? blocks : kParts);
+}
+int lay32_first(Lay32 a, Lay32 w, Clear clear, hipStream_t s)      // each where it has blocks
+{
+    return by_length(a.cols, [&](auto u, auto waves) {
+        xent_first_kernel<decltype(u)::value, decltype(waves)::value><<<a.blocks + w.blocks + clear.blocks, 256, 0, s>>>(a, w, clear);
+    });
+}
+int lay32_second(Lay32 a, Lay32 w, hipStream_t s)
+{
+    return by_length(w.cols, [&](auto u, auto waves) { xent_second_kernel<decltype(u)::value, decltype(waves)::value><<<a.blocks + w.blocks, 256, 0, s>>>(a, w); });
 }
 int add_parts(int dtype, const float *from, int parts, size_t part, size_t ld, int rows, int cols, void *out, hipStream_t s, const float *rest = nullptr,
               const int32_t *labels = nullptr, const void *w = nullptr, const void *relu_of = nullptr, int relu_dtype = 0)
@@ -975,8 +1000,31 @@ struct Call {
 };
 template <typename T> T *at(const Call &c, size_t offset) { return reinterpret_cast<T *>(c.ws + offset); }
 
-// The product that gives the scores of a piece: classes are the rows of C, examples its columns.  w_most: where the largest of its exponents goes.
-int scores_product(const Call &c, const XentPlan &pl, int piece, bool laid_a, int *w_most, Product &p)
+// fp32: activations, and a piece's weights (of `here` classes), as they are laid out; exponents behind another: those of all, the parts of them.
+Lay32 activations(const Call &c, const XentPlan &pl)
+{
+    Lay32 l = {};
+    l.from = static_cast<const float *>(c.a); l.rows = c.N; l.cols = c.In; l.rows_p = pl.NP; l.cols_p = pl.InP;
+    l.to = at<bf16_t>(c, pl.a_at);
+    l.e = at<int>(c, pl.ea_at);
+    l.most = at<int>(c, pl.most_at); l.part = l.most + 2;
+    l.blocks = l.n_part = lay32_blocks(l.rows_p, c.In);
+    return l;
+}
+Lay32 weights(const Call &c, const XentPlan &pl, int class0, int here)
+{
+    Lay32 l = {};
+    l.from = static_cast<const float *>(c.w) + (size_t)class0 * c.In; l.rows = l.rows_p = here; l.cols = c.In; l.cols_p = pl.InP;
+    l.to = at<bf16_t>(c, pl.w_at);
+    l.bias = c.bias ? c.bias + class0 : nullptr;
+    l.most = at<int>(c, pl.most_at) + 1; l.part = l.most + 1 + kParts;
+    l.blocks = l.n_part = lay32_blocks(here, c.In);
+    return l;
+}
+
+// The product that gives the scores of a piece: classes are the rows of C, examples its columns.  fp32: `first`, `clear`: what goes with the search for
+// its weights' largest exponent, `second`: with laying them out.
+int scores_product(const Call &c, const XentPlan &pl, int piece, bool laid_a, const Lay32 &first, const Clear &clear, const Lay32 &second, Product &p)
 {
     const int es = c.dtype == VGG_BF16 ? 2 : 4, class0 = piece * pl.classes, here = c.K - class0 < pl.classes ? c.K - class0 : pl.classes;
     const char *w = static_cast<const char *>(c.w) + (size_t)class0 * c.In * es;
@@ -988,18 +1036,18 @@ int scores_product(const Call &c, const XentPlan &pl, int piece, bool laid_a, in
         const int rows_p = up(here, kStep);
         int rc;
         if (pl.PL == 2) {
-            const float *bias = c.bias ? c.bias + class0 : nullptr;
-            const long blocks = div_up(here, 4);
-            xent_most_kernel<<<(int)(blocks < 2048 ? blocks : 2048), 256, 0, c.s>>>(reinterpret_cast<const float *>(w), here, c.In, bias, w_most);
-            if ((rc = launch_status())) return rc;
-            rc = lay32<kAll>(w, here, c.In, c.ws + pl.w_at, rows_p, pl.InP, nullptr, nullptr, 0, bias, nullptr, nullptr, w_most, nullptr, 0, c.s);
+            Lay32 of_w = weights(c, pl, class0, here);
+            if ((rc = lay32_first(first, of_w, clear, c.s))) return rc;
+            of_w.rows_p = rows_p;
+            of_w.blocks = lay32_blocks(rows_p, c.In);
+            rc = lay32_second(second, of_w, c.s);
         } else
             rc = lay(w, here, c.In, c.ws + pl.w_at, rows_p, pl.InP, nullptr, nullptr, 0, c.s);
         if (rc) return rc;
         p.a = {c.ws + pl.w_at, ld, here, nullptr};
     }
     p.b = {laid_a ? c.ws + pl.a_at : static_cast<const char *>(c.a), ld, c.N, nullptr};
-    if (pl.PL == 2) { p.ea = at<int>(c, pl.ea_at); p.most = w_most; }
+    if (pl.PL == 2) { p.ea = at<int>(c, pl.ea_at); p.most = at<int>(c, pl.most_at) + 1; }
     p.bias = c.bias; p.labels = c.labels;
     p.class0 = class0; p.classes = here; p.all_classes = c.K;
     return VGG_OK;
@@ -1015,20 +1063,26 @@ int scores_in_parts(const XentPlan &pl, const Call &c, Product &p, Scores &z)
 int forward(const Call &c, float *loss, float *stats)
 {
     const XentPlan pl = xent_plan(c.dtype, c.N, c.In, c.K);
-    int rc = VGG_OK, *most = pl.PL == 2 ? at<int>(c, pl.most_at) + 1 : nullptr;      // the pieces' (behind what the gradients need of the activations)
-    if (pl.PL == 2) rc = lay32<kOwn>(c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, nullptr, nullptr, 0, nullptr, at<int>(c, pl.ea_at), nullptr, nullptr, most, pl.pieces, c.s);
-    else if (!pl.direct_a) rc = lay(c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, nullptr, nullptr, 0, c.s);
-    if (rc) return rc;
+    int rc;
+    if (pl.PL == 1 && !pl.direct_a && (rc = lay(c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, nullptr, nullptr, 0, c.s))) return rc;
+    Lay32 of_a = {};
+    if (pl.PL == 2) {
+        of_a = activations(c, pl);
+        of_a.part = nullptr;
+    }
     Sums *sums = at<Sums>(c, pl.sums_at);
     float *z_label = at<float>(c, pl.label_at);
+    Lay32 none = {};
+    none.cols = c.In;
     for (int piece = 0; piece < pl.pieces; ++piece) {
         Product p;
-        if ((rc = scores_product(c, pl, piece, !pl.direct_a, most ? most + piece : nullptr, p))) return rc;
+        if ((rc = scores_product(c, pl, piece, !pl.direct_a, of_a, {}, none, p))) return rc;
         if (pl.z_splits) {
             Scores z;
             if ((rc = scores_in_parts(pl, c, p, z))) return rc;
             return xent_rows(z, c.labels, loss, stats, c.s);
         }
+        of_a = none;
         p.sums = sums; p.z_label = z_label;
         if ((rc = product<false, false, kStats>(pl.PL, pl.tn, p, c.s))) return rc;
     }
@@ -1044,29 +1098,38 @@ int backward(const Call &c, int g_dtype, const float *stats, const float *g, voi
     const int gs = g_dtype == VGG_BF16 ? 2 : 4;
     const bool two = pl.PL == 2;
     bf16_t *dz = at<bf16_t>(c, pl.dz_at);
-    int *ea = two ? at<int>(c, pl.ea_at) : nullptr, *eg = two ? at<int>(c, pl.eg_at) : nullptr;
-    int *a_most = two ? at<int>(c, pl.most_at) : nullptr;        // and, behind it, the pieces'
-    const size_t past = (size_t)(pl.NP - c.N) * pl.ld_dz * pl.PL / 8;
-    int rc;
+    int *eg = two ? at<int>(c, pl.eg_at) : nullptr;
     float *rest = two ? nullptr : at<float>(c, pl.rest_at);
-    {
-        bf16_t *from = dz + (size_t)c.N * pl.ld_dz * pl.PL;
-        const size_t most = past > (size_t)c.N ? past : c.N;
-        xent_clear_kernel<<<(unsigned)(most < 256 * 1024 ? div_up(most, 256) : 1024), 256, 0, c.s>>>(from, pl.rest_rows ? from + (size_t)pl.rest_rows * pl.ld_dz : nullptr, past, rest, c.N,
-                                                                                                     a_most, two ? pl.pieces + 1 : 0);
-        if ((rc = launch_status())) return rc;
-    }
+    int rc;
+    Clear clear = {};
+    clear.dz = dz + (size_t)c.N * pl.ld_dz * pl.PL;
+    clear.count = (size_t)(pl.NP - c.N) * pl.ld_dz * pl.PL / 8;
+    clear.dz_rest = pl.rest_rows ? clear.dz + (size_t)pl.rest_rows * pl.ld_dz : nullptr;
+    clear.rest_of_label = rest;
+    clear.N = c.N;
+    const size_t most = clear.count > (size_t)c.N || !rest ? clear.count : c.N;
+    clear.blocks = (int)(most < 256 * 1024 ? div_up(most, 256) : 1024);
     bf16_t *a_of_dw = at<bf16_t>(c, two ? pl.a2_at : pl.a_at);
+    Lay32 first = {}, second = {}, none = {};
+    none.cols = c.In;
     if (two) {
-        if ((rc = lay32<kOwn>(c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, c.labels, g, c.K, nullptr, ea, eg, a_most, nullptr, 0, c.s))) return rc;
-        if (dw && (rc = lay32<kShared>(c.a, c.N, c.In, a_of_dw, pl.NP, pl.InP, c.labels, g, c.K, nullptr, ea, eg, a_most, nullptr, 0, c.s))) return rc;
-    } else if ((rc = lay(c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, c.labels, g, c.K, c.s)))
-        return rc;
+        first = activations(c, pl);
+        first.labels = c.labels; first.g = g; first.classes = c.K; first.eg = eg;
+        second = dw ? first : none;
+        second.to = a_of_dw;
+    } else {
+        if (clear.blocks) {
+            xent_clear_kernel<<<clear.blocks, 256, 0, c.s>>>(clear);
+            if ((rc = launch_status())) return rc;
+        }
+        if ((rc = lay(c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, c.labels, g, c.K, c.s))) return rc;
+    }
     float *da_part = at<float>(c, pl.da_at), *dw_part = at<float>(c, pl.dw_at);
     for (int piece = 0; piece < pl.pieces; ++piece) {
         Product p;
-        int *w_most = two ? a_most + 1 + piece : nullptr;
-        if ((rc = scores_product(c, pl, piece, true, w_most, p))) return rc;
+        if ((rc = scores_product(c, pl, piece, true, first, clear, second, p))) return rc;
+        first = second = none;
+        clear.blocks = 0;
         const Operand w = p.a;
         const int class0 = p.class0, here = p.classes;
         float *db_to = db ? pl.db_parts == 1 ? db + class0 : at<float>(c, pl.db_at) : nullptr;
@@ -1098,7 +1161,7 @@ int backward(const Call &c, int g_dtype, const float *stats, const float *g, voi
             }
             q.b = {reinterpret_cast<const char *>(dz), ld_dz, c.N, nullptr};
             q.rows = c.In; q.cols = c.N; q.steps = steps; q.splits = pl.da_splits < steps ? pl.da_splits : steps;
-            q.ea = eg; q.most = w_most;
+            q.ea = eg; q.most = p.most;
             q.out = da_part; q.ld = pl.InP; q.part = (size_t)c.N * pl.InP; q.add = piece > 0;
             if ((rc = product<true, false, kStore>(pl.PL, pl.da_tn, q, c.s))) return rc;
         }
@@ -1108,7 +1171,7 @@ int backward(const Call &c, int g_dtype, const float *stats, const float *g, voi
             q.b = {reinterpret_cast<const char *>(dz), ld_dz, (int)ld_dz, nullptr};
             q.rows = c.In; q.cols = here; q.steps = (pl.NP + pl.rest_rows) / kStep; q.splits = pl.dw_splits;
             q.wrap = pl.rest_rows / kStep;
-            q.most = a_most;
+            q.most = two ? at<int>(c, pl.most_at) : nullptr;
             void *out = static_cast<char *>(dw) + (size_t)class0 * c.In * gs;
             q.out = out;
             if (c.N <= kOuterRows) {

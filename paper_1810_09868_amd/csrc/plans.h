@@ -43,9 +43,9 @@ inline W4Plan w4_tiles_plan(int dtype, int N, int In, int Out)
 
 // ------------------------------------------------------------------------------------------------ losses over many classes
 // Whether fp32 products are short enough for 32 x 32 tiles of the fp32 matrix unit, in half the launches: their number, and each contraction, which a
-// tile's waves go along while others wait (loss and gradients in us, so and by large tiles: 64 x 64 x 64 33, 50; 100 x 1024 x 1000 61, 95; 500 x 500 x 500 73,
-// 133; 1000 x 300 x 1000 124, 138; 2000 x 256 x 2000 232, 160; 100 x 100 x 4000 99, 92; 1 x 4096 x 1000 107, 83).
-constexpr long kXentSmall = 5l << 26;
+// tile's waves go along while others wait (loss and gradients in us, so and by large tiles: 64 x 64 x 64 32, 44; 100 x 1024 x 1000 59, 72; 500 x 500 x 500
+// 71, 88; 2000 x 256 x 300 92, 78; 1000 x 300 x 1000 122, 80; 4000 x 64 x 1000 145, 95; 1 x 1024 x 2000 52, 62; 1 x 4096 x 1000 104, 76).
+constexpr long kXentSmall = 9l << 24;
 inline bool xent_is_small(int dtype, int N, int In, int K)
 {
     const long n = (N + 31) / 32 * 32, k = (K + 31) / 32 * 32;
@@ -54,6 +54,7 @@ inline bool xent_is_small(int dtype, int N, int In, int K)
 
 // Other products: tiles of 256 rows (classes for the scores, inputs for da and dw) and 64, 128 or 256 columns.
 constexpr int kTA = 256;      // rows of C in a tile
+constexpr int kParts = 2048;  // workgroups that seek an fp32 operand's largest exponent, at the most
 constexpr int kStep = 64;     // contractions are whole multiples of this many indices
 constexpr size_t kPieceBytes = 512u << 20;   // what a piece of the classes may take of the workspace,
 constexpr long kPieceClasses = 1 << 20;      // and how many there are (a tile's 256 rows of dz by offsets of 31 bits)
@@ -134,7 +135,7 @@ inline XentPlan xent_plan(int dtype, int N, int In, int K)
     p.a_at = take((size_t)p.PL * 2 * p.NP * p.InP);
     p.w_at = take(p.direct_w ? 0 : (size_t)p.PL * 2 * up(most, kStep) * p.InP);
     p.ea_at = take(p.PL == 2 ? (size_t)N * 4 : 0);
-    p.most_at = take(p.PL == 2 ? (size_t)(p.pieces + 1) * 4 : 0);
+    p.most_at = take(p.PL == 2 ? (size_t)(2 + 2 * kParts) * 4 : 0);
     p.z_at = take(p.z_splits ? (size_t)p.z_splits * N * p.ld_z * 4 : 0);
     const size_t both = at;
     p.sums_at = take(p.z_splits ? 0 : (size_t)div_up(K, kTA) * N * 8);
