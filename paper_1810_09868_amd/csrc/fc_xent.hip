@@ -141,6 +141,11 @@ __host__ __device__ constexpr int main_lds_of(int tn, int mode, int stages)
 // ... and behind that the tile's biases and examples
 __host__ __device__ constexpr int lds_of(int tn, int mode, int stages) { return main_lds_of(tn, mode, stages) + (mode == kStore ? 0 : kTA * 4 + tn * (int)sizeof(Example)); }
 
+// A tile of 256 rows by TN columns of C: eight waves of 32 x 32 blocks, stages copied straight into LDS, two or three of them, the next under way while one is
+// multiplied.  Columns are 256 where they fill the chip, since each operand of a stage is then met 256 times; few examples take as few columns as hold
+// them.  The matrix unit bounds large ones, at the power it draws: of 8192 x 2048 x 131072 bf16 a fourth of the classes takes 936 us with the scores' sums, 1003
+// with dz, 852 for da and 863 for dw (1.10 to 1.29 PFLOP/s); 1000 x 1001 x 50001 fp32 333, 371 (in 128 columns: 256 have no registers for their end), 263 and 343
+// (0.81 to 1.14 PFLOP/s of f16).  The read of w bounds few rows: 4 x 4096 x 200003 bf16 380 us with the sums, 345 with dz, 260 for da (4.3, 4.8 and 6.3 TB/s).
 template <bool A_TR, bool B_TR, int TN, int PL, int MODE>
 __global__ __launch_bounds__(512) void xent_product_kernel(Product p)
 {
@@ -686,8 +691,8 @@ __device__ __forceinline__ void clear(const Clear &c, int block)
 }
 __global__ __launch_bounds__(256) void xent_clear_kernel(Clear c) { clear(c, blockIdx.x); }
 
-// What comes before the first product of fp32 operands, in two launches (100 x 4096 x 1000, loss and gradients: 97 us; 111 with each
-// of the five parts in a launch of its own).
+// What comes before the first product of fp32 operands, in two launches: bytes bound them (50001 x 1001: 49 and 80 us, 4.1 and 5.1 TB/s), or, where there
+// are few, a chain of loads each (100 x 4096 x 1000, loss and gradients: 97 us in all; 111 with each of the five parts in a launch of its own).
 template <int U, int W> __global__ __launch_bounds__(256) void xent_first_kernel(Lay32 a, Lay32 w, Clear c)
 {
     const int block = blockIdx.x;

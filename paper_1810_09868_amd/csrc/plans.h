@@ -67,12 +67,22 @@ inline int up(long v, int to) { return (int)((v + to - 1) / to * to); }
 inline long div_up(long a, long b) { return (a + b - 1) / b; }
 
 // Columns of a tile, of examples for the scores and da, of classes for dw: as many as leave no half of it empty, and give every compute unit a tile
-// of its own where that can be.
-inline int tile_of(int cols, long row_tiles)
+// of its own where that can be.  Scores in one go: half of the compute units, since tiles of half the width in two rounds read w twice (bf16 128 x 2048 x
+// 40000 34 us for 49; of less than half, narrower ones are faster: 1000 x 1024 x 5000 22 us in 128 columns, 31 in 256, 28 in 64).
+inline int tile_of(int cols, long row_tiles, int least = 256)
 {
     int tn = cols > 128 ? 256 : cols > 64 ? 128 : 64;
-    while (tn > 64 && row_tiles * div_up(cols, tn) < 256) tn /= 2;
+    while (tn > 64 && row_tiles * div_up(cols, tn) < least) tn /= 2;
     return tn;
+}
+// Whether the contraction of few tiles of scores is split.  All of them have to be kept for a moment then, and read again, which takes the longer the more
+// classes and rows there are, while a contraction in one goes on for 0.6 us (fp32 1.1) a stage.  (Loss and gradients in us, split and not: bf16 100 x 4096 x
+// 1000 63, 98; 1000 x 4096 x 4000 229, 262; 100 x 4096 x 8192 130, 155; 100 x 4096 x 12000 194, 175; 1000 x 1024 x 1000 98, 73; 100 x 1024 x 1000 53, 54; fp32 100 x
+// 4096 x 1000 95, 192; 100 x 4096 x 16000 734, 767; 100 x 4096 x 25000 1100, 1067; 100 x 1024 x 2500 90, 103; 1000 x 1024 x 2500 244, 207.)
+inline bool scores_are_split(int dtype, int N, int K, int steps)
+{
+    const long work = dtype == VGG_BF16 ? steps : 2l * steps;
+    return work >= 16 && work >= K / 144 + N / 64;
 }
 // Ranges of a contraction of `steps` stages, where `tiles` do not fill the chip: at least 256 indices of bf16 operands each, or 128 of
 // fp32 ones, which take three times as long.
@@ -101,16 +111,18 @@ inline XentPlan xent_plan(int dtype, int N, int In, int K)
     XentPlan p;
     p.PL = dtype == VGG_BF16 ? 1 : 2;
     p.In = In; p.InP = up(In, kStep); p.NP = up(N, kStep);
-    // (the contraction of scores of few tiles is split: their columns by what that leaves idle)
-    p.tn = tile_of(N, div_up(K, kTA) * splits_of(dtype, div_up(K, kTA), p.InP / kStep));
+    const int steps = p.InP / kStep;
+    const long k_tiles = div_up(K, kTA);
+    // (where the contraction of scores is split: their columns by what that leaves idle)
+    p.tn = tile_of(N, k_tiles * splits_of(dtype, k_tiles, steps));
+    p.z_splits = scores_are_split(dtype, N, K, steps) && k_tiles * div_up(N, p.tn) < 128 ? splits_of(dtype, k_tiles * div_up(N, p.tn), steps) : 0;
+    if (p.z_splits <= 1) {
+        p.z_splits = 0;
+        p.tn = tile_of(N, k_tiles, 128);
+    }
     p.grad_tn = p.PL == 2 && p.tn == 256 ? 128 : p.tn;     // (256: more registers than there are)
     p.direct_w = p.direct_a = dtype == VGG_BF16 && In % kStep == 0;
     const long n_tiles = div_up(N, p.tn), d_tiles = div_up(In, kTA);
-    const int steps = p.InP / kStep;
-    // scores of few tiles: their contraction is split, so that all of them have to be kept for a moment
-    const long z_tiles = div_up(K, kTA) * n_tiles;
-    p.z_splits = z_tiles < 128 && steps >= 8 ? splits_of(dtype, z_tiles, steps) : 0;
-    if (p.z_splits == 1) p.z_splits = 0;
     const size_t per_class = (size_t)p.PL * 2 * (p.NP + (p.direct_w ? 0 : p.InP));
     long classes = (long)(kPieceBytes / per_class) / kTA * kTA;
     if (classes < kTA) classes = kTA;

@@ -113,7 +113,7 @@ class Xent:
 TYPES = [(B.F32, B.F32), (B.BF16, B.BF16), (B.BF16, B.F32)]
 SIZES = [(1, 1, 1), (1, 64, 2), (2, 3, 1), (3, 7, 5), (64, 128, 256), (65, 64, 257), (63, 130, 255), (128, 192, 64), (129, 66, 300), (257, 256, 513), (300, 200, 700), (1, 4096, 1000),
          (100, 4096, 1000), (5, 512, 40000), (700, 1000, 14), (1000, 33, 3000), (33, 2048, 129), (4, 1024, 10007),
-         (500, 500, 500), (4096, 70, 33), (31, 1024, 2048), (33, 1025, 65), (4097, 40, 20), (5, 8, 2049), (17, 300, 3000), (16, 100, 5000), (513, 320, 2500), (4097, 1, 1), (5, 1, 2049), (1, 1025, 1)]
+         (500, 500, 500), (4096, 70, 33), (31, 1024, 2048), (33, 1025, 65), (4097, 40, 20), (5, 8, 2049), (17, 300, 3000), (16, 100, 5000), (513, 320, 2500), (4097, 1, 1), (5, 1, 2049), (1, 1025, 1), (3, 5000, 70), (20, 9001, 300)]
 
 
 @pytest.mark.parametrize("dtype,g_dtype", TYPES)
@@ -237,7 +237,7 @@ def test_gradient_against_differences():
 
 
 @pytest.mark.parametrize("dtype", [B.F32, B.BF16])
-@pytest.mark.parametrize("N,In,K", [(70, 128, 300), (100, 1024, 1000)])
+@pytest.mark.parametrize("N,In,K", [(70, 128, 300), (100, 1024, 1000), (100, 1100, 1000), (300, 200, 3000)])
 def test_parts_of_the_gradient_other_streams_and_twice_the_same(dtype, N, In, K):
     c = Xent(dtype, N, In, K, 9).run()
     whole = {k: getattr(c, k).clone() for k in ("loss", "da", "dw", "db")}
@@ -300,7 +300,7 @@ def test_fp32_weights_of_masked_classes_do_not_count(N, In, K):
 
 
 @pytest.mark.parametrize("dtype,g_dtype", TYPES)
-@pytest.mark.parametrize("N,In,K", [(5, 7, 30), (70, 128, 300), (100, 1024, 1000)])
+@pytest.mark.parametrize("N,In,K", [(5, 7, 30), (70, 128, 300), (100, 1024, 1000), (100, 1100, 1000), (300, 200, 3000)])
 def test_activations_that_a_relu_left(dtype, g_dtype, N, In, K):
     c = Xent(dtype, N, In, K, 15, g_dtype=g_dtype)
     c.a.clamp_min_(0)
@@ -312,7 +312,7 @@ def test_activations_that_a_relu_left(dtype, g_dtype, N, In, K):
 
 
 @pytest.mark.parametrize("dtype", [B.F32, B.BF16])
-@pytest.mark.parametrize("N,In,K", [(70, 128, 300), (100, 1024, 1000)])
+@pytest.mark.parametrize("N,In,K", [(70, 128, 300), (100, 1024, 1000), (100, 1100, 1000), (300, 200, 3000)])
 def test_recorded_in_a_graph(dtype, N, In, K):
     c = Xent(dtype, N, In, K, 10).run()
     ws = ws_bytes(max(B.vgg_fc_xent_workspace_bytes(dtype, N, In, K), B.vgg_fc_xent_bwd_workspace_bytes(dtype, N, In, K)))
