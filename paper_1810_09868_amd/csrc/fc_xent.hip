@@ -821,6 +821,103 @@ __global__ __launch_bounds__(256) void xent_grad_kernel(Scores z, const int32_t 
         if (k + j < z.classes) db[(size_t)blockIdx.y * ld_db + k + j] = sum[j];
 }
 
+// The sums of fp32 scores of few rows, from weights where they are: seeking their exponent, laying them out and reading that back would pass memory four
+// times instead of once.  A wave: 32 classes and R times 32 rows, by the fp32 matrix unit; a lane has a class (and a row) of its own and, of 8
+// contraction indices, four; U times 8 of them at once and the next on their way.  The read bounds one group of 32 rows (1 x 4096 x 131072: 498 us, 4.3 TB/s),
+// the way of the rows out of L2 two (64 rows 909).
+template <int R, int U>
+__global__ __launch_bounds__(512) void xent_few_kernel(const float *__restrict__ a, const float *__restrict__ w, int N, int In, int K, const float *__restrict__ bias,
+                                                       const int32_t *__restrict__ labels, Sums *sums, float *z_label)
+{
+    __shared__ Sums all[8][R * 32];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, k0 = blockIdx.x * kTA + wave * 32;
+    const float *of_w = w + (size_t)(k0 + (lane & 31) < K ? k0 + (lane & 31) : K - 1) * In, *of_a[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) of_a[r] = a + (size_t)(32 * r + (lane & 31) < N ? 32 * r + (lane & 31) : N - 1) * In;
+    f32x16 acc[R] = {};
+    f32x4 vw[2][U], va[2][R][U];
+    auto fetch = [&](int c0, f32x4 (&to_w)[U], f32x4 (&to_a)[R][U]) __attribute__((always_inline)) {
+        if (c0 + 8 * U <= In) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) __builtin_memcpy(&to_w[u], of_w + c0 + 8 * u + 4 * half, 16);
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int u = 0; u < U; ++u) __builtin_memcpy(&to_a[r][u], of_a[r] + c0 + 8 * u + 4 * half, 16);
+        } else
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int c = c0 + 8 * u + 4 * half + k, at = c < In ? c : In - 1;
+                    const float x = of_w[at];
+                    to_w[u][k] = c < In ? x : 0.f;
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        const float y = of_a[r][at];
+                        to_a[r][u][k] = c < In ? y : 0.f;
+                    }
+                }
+    };
+    auto multiply = [&](const f32x4 (&by_w)[U], const f32x4 (&by_a)[R][U]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int r = 0; r < R; ++r) acc[r] = __builtin_amdgcn_mfma_f32_32x32x2f32(by_w[u][k], by_a[r][u][k], acc[r], 0, 0, 0);
+    };
+    fetch(0, vw[0], va[0]);
+    for (int c = 0; c < In; c += 16 * U) {
+        if (c + 8 * U < In) fetch(c + 8 * U, vw[1], va[1]);
+        multiply(vw[0], va[0]);
+        if (c + 8 * U >= In) break;
+        if (c + 16 * U < In) fetch(c + 16 * U, vw[0], va[0]);
+        multiply(vw[1], va[1]);
+    }
+    // value v of a lane: class 8 (v / 4) + 4 (lane / 32) + v % 4, row lane % 32
+    float b[16];
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+        const int k = k0 + 8 * (v >> 2) + 4 * half + (v & 3);
+        b[v] = k >= K ? -INFINITY : bias ? bias[k] : 0.f;
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int row = 32 * r + (lane & 31), label = row < N ? labels[row] : -1;
+        Sums s = {-INFINITY, 0.f};
+        bool here = false;
+        float z_of = 0.f;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const int k = k0 + 8 * (v >> 2) + 4 * half + (v & 3);
+            const float z = b[v] == -INFINITY ? -INFINITY : acc[r][v] + b[v];
+            acc[r][v] = z;
+            s.m = fmaxf(s.m, z);
+            if (k == label && k < K) { here = true; z_of = z; }
+        }
+        if (here) z_label[row] = z_of;
+        bool fresh = s.m > -INFINITY;               // one of the largest does not count
+        const float base = fresh ? s.m : 0.f;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const float e = exp_of(below(acc[r][v] - base));
+            const bool it = fresh && acc[r][v] == s.m;
+            s.e += it ? 0.f : e;
+            fresh = fresh && !it;
+        }
+        s = joined(s, Sums{__shfl_xor(s.m, 32), __shfl_xor(s.e, 32)});
+        if (half == 0) all[wave][row] = s;
+    }
+    __syncthreads();
+    const int row = threadIdx.x;
+    if (row >= R * 32 || row >= N) return;
+    Sums s = all[0][row];
+#pragma unroll
+    for (int q = 1; q < 8; ++q) s = joined(s, all[q][row]);
+    sums[(size_t)blockIdx.x * N + row] = s;
+}
+
 // dw of few rows, a sum of up to NMAX outer products: a thread's eight columns of the activations stay in registers, dz is the same for all
 // threads, and what is left is the write (4 rows, 200003 x 4096 bf16: 284 us, 5.8 TB/s of writes; in 256 x 256 tiles 432, in narrower ones 558).
 template <int PL, int NMAX, typename G>
@@ -1069,14 +1166,30 @@ int forward(const Call &c, float *loss, float *stats)
 {
     const XentPlan pl = xent_plan(c.dtype, c.N, c.In, c.K);
     int rc;
+    Sums *sums = at<Sums>(c, pl.sums_at);
+    float *z_label = at<float>(c, pl.label_at);
+    const int tiles = (int)div_up(c.K, kTA);
+    auto join = [&] {
+        if (c.N <= 512) xent_join_kernel<1><<<c.N, 256, 0, c.s>>>(sums, tiles, c.N, c.K, c.labels, z_label, loss, stats);
+        else xent_join_kernel<16><<<(int)div_up(c.N, 16), 256, 0, c.s>>>(sums, tiles, c.N, c.K, c.labels, z_label, loss, stats);
+        return launch_status();
+    };
+    if (pl.PL == 2 && !pl.z_splits && c.N <= kDirectRows && c.K >= kDirectClasses) {
+        auto few = [&](auto r, auto u) {
+            xent_few_kernel<decltype(r)::value, decltype(u)::value><<<tiles, 512, 0, c.s>>>(static_cast<const float *>(c.a), static_cast<const float *>(c.w), c.N, c.In, c.K, c.bias,
+                                                                                            c.labels, sums, z_label);
+        };
+        if (c.N <= 32) few(std::integral_constant<int, 1>{}, std::integral_constant<int, 8>{});
+        else few(std::integral_constant<int, 2>{}, std::integral_constant<int, 4>{});
+        if ((rc = launch_status())) return rc;
+        return join();
+    }
     if (pl.PL == 1 && !pl.direct_a && (rc = lay(c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, nullptr, nullptr, 0, c.s))) return rc;
     Lay32 of_a = {};
     if (pl.PL == 2) {
         of_a = activations(c, pl);
         of_a.part = nullptr;
     }
-    Sums *sums = at<Sums>(c, pl.sums_at);
-    float *z_label = at<float>(c, pl.label_at);
     Lay32 none = {};
     none.cols = c.In;
     for (int piece = 0; piece < pl.pieces; ++piece) {
@@ -1091,10 +1204,7 @@ int forward(const Call &c, float *loss, float *stats)
         p.sums = sums; p.z_label = z_label;
         if ((rc = product<false, false, kStats>(pl.PL, pl.tn, p, c.s))) return rc;
     }
-    const int tiles = (int)div_up(c.K, kTA);
-    if (c.N <= 512) xent_join_kernel<1><<<c.N, 256, 0, c.s>>>(sums, tiles, c.N, c.K, c.labels, z_label, loss, stats);
-    else xent_join_kernel<16><<<(int)div_up(c.N, 16), 256, 0, c.s>>>(sums, tiles, c.N, c.K, c.labels, z_label, loss, stats);
-    return launch_status();
+    return join();
 }
 
 int backward(const Call &c, int g_dtype, const float *stats, const float *g, void *da, void *dw, float *db, int relu_mask)

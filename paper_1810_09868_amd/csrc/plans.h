@@ -61,6 +61,9 @@ constexpr long kPieceClasses = 1 << 20;      // and how many there are (a tile's
 // bf16 rows up to which what rounding leaves of dz enters dw, as a contraction twice as long.  Off by 2^-9 of each term, dw is as exact as its own
 // rounding to bf16 on the average of many rows; the fewer there are, the more hangs on single ones.
 constexpr int kRestRows = 512;
+// fp32 rows up to which, and classes from which on, the loss takes weights from where they are (loss in us, so and with weights laid out: 1 x 4096 x 131072 498,
+// 1842; 64 x 4096 x 131072 909, 1890; 4 x 1024 x 10007 65, 49; with four times 32 rows to a wave 100 x 4096 x 25000 949, 357).
+constexpr int kDirectRows = 64, kDirectClasses = 1 << 14;
 constexpr int kOuterRows = 16;               // rows up to which dw is written by its own kernel
 
 inline int up(long v, int to) { return (int)((v + to - 1) / to * to); }

@@ -127,6 +127,22 @@ def test_every_width_of_tiles(dtype, N, In, K):
     Xent(dtype, N, In, K, 18, masked=0.05).run().check()
 
 
+@pytest.mark.parametrize("N,In,K", [(1, 1, 16384), (1, 63, 16385), (3, 129, 40003), (32, 64, 20000), (33, 35, 20001), (64, 200, 16400), (65, 64, 20000), (5, 700, 16639)])
+def test_fp32_weights_from_where_they_are(N, In, K):
+    c = Xent(B.F32, N, In, K, 21, masked=0.2).run().check()
+    Xent(B.F32, N, In, K, 22, bias=False).run().check()
+    whole = c.loss.clone()
+    c.w[c.bias == -math.inf] = 1e30                # of classes that do not count
+    c.a, a = torch.full((N + 1, In), math.nan, device="cuda")[:N], c.a
+    c.a.copy_(a)                                   # NaN behind the last row
+    c.run(())
+    assert torch.equal(c.loss, whole)
+    c.a[N // 2] = math.nan
+    c.run(())
+    counts = (c.labels >= 0) & (c.labels < K)
+    assert torch.equal(torch.isnan(c.loss), counts & (torch.arange(N, device="cuda") == N // 2))
+
+
 @pytest.mark.parametrize("dtype", [B.F32, B.BF16])
 @pytest.mark.parametrize("N,In,K", [(8200, 64, 40000), (16390, 70, 20011), (30000, 130, 9000)])
 def test_classes_in_pieces(dtype, N, In, K):
