@@ -454,7 +454,8 @@ int vgg_layer_norm_bwd(int dtype, int g_dtype, int N, int C, size_t ldx, const v
  * weights makes the scores it has part in infinite or NaN.  Products are
  * summed in fp32; fp32 operands enter them with 22 bits (activations down to 2^-17
  * of their row's largest, weights of the largest of all, and exact to 2^-39 of
- * that below); loss and stats are fp32.
+ * that below), or whole where products are short, or rows few and classes many;
+ * loss and stats are fp32.
  * N <= 2^22, In <= 2^20, K <= 2^24. */
 size_t vgg_fc_xent_workspace_bytes(int dtype, int N, int In, int K);
 int vgg_fc_xent(int dtype, int N, int In, int K, const void *a, const void *w, const float *bias, const int32_t *labels,
@@ -464,7 +465,8 @@ int vgg_fc_xent(int dtype, int N, int In, int K, const void *a, const void *w, c
  *   da = dz w [N][In], dw = dz^T a [K][In], db[k] = sum_n dz[n,k] (fp32).
  * Each of the three may be NULL, not all.  da and dw are in g_dtype (`dtype`, or VGG_F32)
  * and overlap nothing that is read.  stats are vgg_fc_xent's of the same
- * activations, weights and bias.  The scores are formed again, in pieces of
+ * activations, all N rows of them, weights and bias: the scores are the same then
+ * to the last bit, on which the gradients of nearly certain labels hang.  They are formed again, in pieces of
  * the classes that take up to 512 MB of workspace (or 256 classes).  bf16: dz is
  * rounded to bf16 where it enters the two products, as in vgg_fc_bwd, not in
  * db, but what that leaves of it at a row's label enters da, and with up to 512

@@ -821,16 +821,31 @@ __global__ __launch_bounds__(256) void xent_grad_kernel(Scores z, const int32_t 
         if (k + j < z.classes) db[(size_t)blockIdx.y * ld_db + k + j] = sum[j];
 }
 
-// The sums of fp32 scores of few rows, from weights where they are: seeking their exponent, laying them out and reading that back would pass memory four
-// times instead of once.  A wave: 32 classes and R times 32 rows, by the fp32 matrix unit; a lane has a class (and a row) of its own and, of 8
-// contraction indices, four; U times 8 of them at once and the next on their way.  The read bounds one group of 32 rows (1 x 4096 x 131072: 498 us, 4.3 TB/s),
-// the way of the rows out of L2 two (64 rows 909).
-template <int R, int U>
-__global__ __launch_bounds__(512) void xent_few_kernel(const float *__restrict__ a, const float *__restrict__ w, int N, int In, int K, const float *__restrict__ bias,
-                                                       const int32_t *__restrict__ labels, Sums *sums, float *z_label)
+// Scores of few fp32 rows, from weights where they are, and what becomes of them: their sums, or dz and db.  Seeking the weights' exponent, laying them out and
+// reading that back would pass memory four times instead of once.  Both come from here, bit for bit the same scores: the gradient of a label that is all but
+// certain is what z - m and log s leave of each other, and scores of another product, off by their own rounding, would leave that instead.  A wave: 32 classes and R times 32 rows, by the fp32 matrix unit; a lane has a class (and a row) of its own and, of 8
+// contraction indices, four; U times 8 of them at once and the next on their way.  The read bounds one group of 32 rows (sums, 1 x 4096 x 131072: 496 us, 4.3 TB/s),
+// the way of the rows out of L2 two (64 rows 914).
+struct Few {
+    const float *a, *w, *bias;       // w and bias of class0 on
+    const int32_t *labels;
+    int N, In, class0, classes, all_classes;
+    Sums *sums;                      // kStats: [tiles of classes][N]
+    float *z_label;                  // [N]
+    const float *stats, *g;          // kGrad, and as in Product:
+    const int *eg;
+    bf16_t *dz;
+    int ld_dz;
+    float *db;
+};
+// (gradients: pieces of the classes, in workgroups that fill the chip sooner.  Loss and gradients of 64 x 4096 x 131072 5502 us with eight waves, 4473 with four, 4812 with two)
+constexpr int few_waves(int mode) { return mode == kStats ? kTA / 32 : 4; }
+template <int R, int U, int MODE>
+__global__ __launch_bounds__(64 * few_waves(MODE)) void xent_few_kernel(Few p)
 {
-    __shared__ Sums all[8][R * 32];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, k0 = blockIdx.x * kTA + wave * 32;
+    const float *a = p.a, *w = p.w, *bias = p.bias;
+    const int N = p.N, In = p.In, K = p.classes;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5, k0 = (blockIdx.x * few_waves(MODE) + wave) * 32;
     const float *of_w = w + (size_t)(k0 + (lane & 31) < K ? k0 + (lane & 31) : K - 1) * In, *of_a[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) of_a[r] = a + (size_t)(32 * r + (lane & 31) < N ? 32 * r + (lane & 31) : N - 1) * In;
@@ -882,40 +897,80 @@ __global__ __launch_bounds__(512) void xent_few_kernel(const float *__restrict__
         const int k = k0 + 8 * (v >> 2) + 4 * half + (v & 3);
         b[v] = k >= K ? -INFINITY : bias ? bias[k] : 0.f;
     }
+    if constexpr (MODE == kStats) {
+        __shared__ Sums all[8][R * 32];
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int row = 32 * r + (lane & 31), label = row < N ? labels[row] : -1;
-        Sums s = {-INFINITY, 0.f};
-        bool here = false;
-        float z_of = 0.f;
+        for (int r = 0; r < R; ++r) {
+            const int row = 32 * r + (lane & 31), label = row < N ? p.labels[row] : -1;
+            Sums s = {-INFINITY, 0.f};
+            bool here = false;
+            float z_of = 0.f;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int k = k0 + 8 * (v >> 2) + 4 * half + (v & 3);
+                const float z = b[v] == -INFINITY ? -INFINITY : acc[r][v] + b[v];
+                acc[r][v] = z;
+                s.m = fmaxf(s.m, z);
+                if (k == label && k < K) { here = true; z_of = z; }
+            }
+            if (here) p.z_label[row] = z_of;
+            bool fresh = s.m > -INFINITY;               // one of the largest does not count
+            const float base = fresh ? s.m : 0.f;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const float e = exp_of(below(acc[r][v] - base));
+                const bool it = fresh && acc[r][v] == s.m;
+                s.e += it ? 0.f : e;
+                fresh = fresh && !it;
+            }
+            s = joined(s, Sums{__shfl_xor(s.m, 32), __shfl_xor(s.e, 32)});
+            if (half == 0) all[wave][row] = s;
+        }
+        __syncthreads();
+        const int row = threadIdx.x;
+        if (row >= R * 32 || row >= N) return;
+        Sums s = all[0][row];
+#pragma unroll
+        for (int q = 1; q < 8; ++q) s = joined(s, all[q][row]);
+        p.sums[(size_t)blockIdx.x * N + row] = s;
+    } else {
+        float sum[16] = {};
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int row = 32 * r + (lane & 31), label = row < N ? p.labels[row] : -1;
+            const bool counts = label >= 0 && label < p.all_classes;
+            const float g = counts ? p.g[row] : 0.f, m = counts ? p.stats[2 * row] : 0.f, log_s = counts ? p.stats[2 * row + 1] : 0.f;
+            const bool none = g == 0.f || log_s == -INFINITY;      // (-inf: a row without a class)
+            const int own = counts ? label - p.class0 : -1, unit = row < N ? 14 - p.eg[row] : 0;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int k = k0 + 8 * q + 4 * half;
+                f32x4 out;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int v = 4 * q + j;
+                    const float z = b[v] == -INFINITY ? -INFINITY : acc[r][v] + b[v], d = (z - m) - log_s;
+                    float share = exp_of(below(d));
+                    if (k + j == own) share = z == -INFINITY ? 0.f : expm1f(d);
+                    out[j] = none || k + j >= K ? 0.f : g * share;
+                    sum[v] += out[j];
+                    out[j] = ldexpf(out[j], unit);
+                }
+                f16x4 h[2];
+                two_parts(out, 0, h);
+                if (row < N && k < p.ld_dz)
+#pragma unroll
+                    for (int part = 0; part < 2; ++part) *reinterpret_cast<f16x4 *>(p.dz + (size_t)row * p.ld_dz * 2 + column_at<2>(k, part)) = h[part];
+            }
+        }
+        if (!p.db) return;
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
+            const float s = team_sum<32>(sum[v]);
             const int k = k0 + 8 * (v >> 2) + 4 * half + (v & 3);
-            const float z = b[v] == -INFINITY ? -INFINITY : acc[r][v] + b[v];
-            acc[r][v] = z;
-            s.m = fmaxf(s.m, z);
-            if (k == label && k < K) { here = true; z_of = z; }
+            if ((lane & 31) == 0 && k < K) p.db[k] = s;
         }
-        if (here) z_label[row] = z_of;
-        bool fresh = s.m > -INFINITY;               // one of the largest does not count
-        const float base = fresh ? s.m : 0.f;
-#pragma unroll
-        for (int v = 0; v < 16; ++v) {
-            const float e = exp_of(below(acc[r][v] - base));
-            const bool it = fresh && acc[r][v] == s.m;
-            s.e += it ? 0.f : e;
-            fresh = fresh && !it;
-        }
-        s = joined(s, Sums{__shfl_xor(s.m, 32), __shfl_xor(s.e, 32)});
-        if (half == 0) all[wave][row] = s;
     }
-    __syncthreads();
-    const int row = threadIdx.x;
-    if (row >= R * 32 || row >= N) return;
-    Sums s = all[0][row];
-#pragma unroll
-    for (int q = 1; q < 8; ++q) s = joined(s, all[q][row]);
-    sums[(size_t)blockIdx.x * N + row] = s;
 }
 
 // dw of few rows, a sum of up to NMAX outer products: a thread's eight columns of the activations stay in registers, dz is the same for all
@@ -1162,6 +1217,23 @@ int scores_in_parts(const XentPlan &pl, const Call &c, Product &p, Scores &z)
     return product<false, false, kStore>(pl.PL, pl.tn, p, c.s);
 }
 
+Few few_rows(const Call &c, int class0, int here)
+{
+    Few p = {};
+    p.a = static_cast<const float *>(c.a); p.w = static_cast<const float *>(c.w) + (size_t)class0 * c.In; p.bias = c.bias ? c.bias + class0 : nullptr;
+    p.labels = c.labels;
+    p.N = c.N; p.In = c.In; p.class0 = class0; p.classes = here; p.all_classes = c.K;
+    return p;
+}
+template <int MODE> int few_scores(const Few &p, hipStream_t s)
+{
+    constexpr int W = few_waves(MODE);
+    const int tiles = (int)div_up(p.classes, 32 * W);
+    if (p.N <= 32) xent_few_kernel<1, 8, MODE><<<tiles, 64 * W, 0, s>>>(p);
+    else xent_few_kernel<2, 4, MODE><<<tiles, 64 * W, 0, s>>>(p);
+    return launch_status();
+}
+
 int forward(const Call &c, float *loss, float *stats)
 {
     const XentPlan pl = xent_plan(c.dtype, c.N, c.In, c.K);
@@ -1174,14 +1246,10 @@ int forward(const Call &c, float *loss, float *stats)
         else xent_join_kernel<16><<<(int)div_up(c.N, 16), 256, 0, c.s>>>(sums, tiles, c.N, c.K, c.labels, z_label, loss, stats);
         return launch_status();
     };
-    if (pl.PL == 2 && !pl.z_splits && c.N <= kDirectRows && c.K >= kDirectClasses) {
-        auto few = [&](auto r, auto u) {
-            xent_few_kernel<decltype(r)::value, decltype(u)::value><<<tiles, 512, 0, c.s>>>(static_cast<const float *>(c.a), static_cast<const float *>(c.w), c.N, c.In, c.K, c.bias,
-                                                                                            c.labels, sums, z_label);
-        };
-        if (c.N <= 32) few(std::integral_constant<int, 1>{}, std::integral_constant<int, 8>{});
-        else few(std::integral_constant<int, 2>{}, std::integral_constant<int, 4>{});
-        if ((rc = launch_status())) return rc;
+    if (pl.few_rows) {
+        Few p = few_rows(c, 0, c.K);
+        p.sums = sums; p.z_label = z_label;
+        if ((rc = few_scores<kStats>(p, c.s))) return rc;
         return join();
     }
     if (pl.PL == 1 && !pl.direct_a && (rc = lay(c.a, c.N, c.In, c.ws + pl.a_at, pl.NP, pl.InP, nullptr, nullptr, 0, c.s))) return rc;
@@ -1255,6 +1323,12 @@ int backward(const Call &c, int g_dtype, const float *stats, const float *g, voi
             if (two) xent_grad_kernel<2><<<grid, 256, 0, c.s>>>(z, c.labels, stats, g, dz, pl.ld_dz, db_to, pl.ld_dz, eg, 0, nullptr);
             else xent_grad_kernel<1><<<grid, 256, 0, c.s>>>(z, c.labels, stats, g, dz, pl.ld_dz, db_to, pl.ld_dz, eg, pl.rest_rows, rest);
             if ((rc = launch_status())) return rc;
+        } else if (pl.few_rows) {
+            Few q = few_rows(c, class0, here);
+            q.stats = stats; q.g = g; q.eg = eg;
+            q.dz = dz; q.ld_dz = pl.ld_dz;
+            q.db = db_to;      // (of 64 rows at the most: one part)
+            if ((rc = few_scores<kGrad>(q, c.s))) return rc;
         } else {
             p.stats = stats; p.g = g; p.eg = eg;
             p.dz = dz; p.ld_dz = pl.ld_dz; p.rest_rows = pl.rest_rows; p.rest_of_label = rest;

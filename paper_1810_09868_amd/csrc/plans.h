@@ -61,8 +61,8 @@ constexpr long kPieceClasses = 1 << 20;      // and how many there are (a tile's
 // bf16 rows up to which what rounding leaves of dz enters dw, as a contraction twice as long.  Off by 2^-9 of each term, dw is as exact as its own
 // rounding to bf16 on the average of many rows; the fewer there are, the more hangs on single ones.
 constexpr int kRestRows = 512;
-// fp32 rows up to which, and classes from which on, the loss takes weights from where they are (loss in us, so and with weights laid out: 1 x 4096 x 131072 498,
-// 1842; 64 x 4096 x 131072 909, 1890; 4 x 1024 x 10007 65, 49; with four times 32 rows to a wave 100 x 4096 x 25000 949, 357).
+// fp32 rows up to which, and classes from which on, scores are formed from weights where they are, by the loss and by its gradients alike: m and log_s of one product with
+// the scores of another would give a nearly certain label the difference of the two (loss in us, so and with weights laid out: 1 x 4096 x 131072 498, 1842; 64 x 4096 x 131072 909, 1890; 4 x 1024 x 10007 65, 49; with four times 32 rows to a wave 100 x 4096 x 25000 949, 357).
 constexpr int kDirectRows = 64, kDirectClasses = 1 << 14;
 constexpr int kOuterRows = 16;               // rows up to which dw is written by its own kernel
 
@@ -98,6 +98,7 @@ inline int splits_of(int dtype, long tiles, int steps)
 struct XentPlan {
     int PL, In, InP, NP, tn, grad_tn;
     bool direct_w, direct_a;      // read where they are (bf16, whole stages)
+    bool few_rows;                // scores by the fp32 matrix unit, from operands where they are
     int classes, pieces;          // of a piece (the last has what is left)
     int z_splits;                 // 0: scores' tiles end in their sums or gradients; else their parts are added up (then one piece)
     int ld_dz, rest_rows;
@@ -125,6 +126,7 @@ inline XentPlan xent_plan(int dtype, int N, int In, int K)
     }
     p.grad_tn = p.PL == 2 && p.tn == 256 ? 128 : p.tn;     // (256: more registers than there are)
     p.direct_w = p.direct_a = dtype == VGG_BF16 && In % kStep == 0;
+    p.few_rows = dtype == VGG_F32 && !p.z_splits && N <= kDirectRows && K >= kDirectClasses;
     const long n_tiles = div_up(N, p.tn), d_tiles = div_up(In, kTA);
     const size_t per_class = (size_t)p.PL * 2 * (p.NP + (p.direct_w ? 0 : p.InP));
     long classes = (long)(kPieceBytes / per_class) / kTA * kTA;
