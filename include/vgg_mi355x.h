@@ -467,7 +467,8 @@ int vgg_fc_xent(int dtype, int N, int In, int K, const void *a, const void *w, c
  * and overlap nothing that is read.  stats are vgg_fc_xent's of the same
  * activations, all N rows of them, weights and bias: the scores are the same then
  * to the last bit, on which the gradients of nearly certain labels hang.  They are formed again, in pieces of
- * the classes that take up to 512 MB of workspace (or 256 classes).  bf16: dz is
+ * the classes whose dz and laid out weights take up to 512 MB of workspace (or in
+ * pieces of 256 classes; in one where the contraction of few scores is split).  bf16: dz is
  * rounded to bf16 where it enters the two products, as in vgg_fc_bwd, not in
  * db, but what that leaves of it at a row's label enters da, and with up to 512
  * rows all of it dw.  fp32: operands of the products have 22 bits as above, dz

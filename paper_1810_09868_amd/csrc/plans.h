@@ -56,7 +56,7 @@ inline bool xent_is_small(int dtype, int N, int In, int K)
 constexpr int kTA = 256;      // rows of C in a tile
 constexpr int kParts = 2048;  // workgroups that seek an fp32 operand's largest exponent, at the most
 constexpr int kStep = 64;     // contractions are whole multiples of this many indices
-constexpr size_t kPieceBytes = 512u << 20;   // what a piece of the classes may take of the workspace,
+constexpr size_t kPieceBytes = 512u << 20;   // what dz and laid out weights of a piece of the classes may take of the workspace,
 constexpr long kPieceClasses = 1 << 20;      // and how many there are (a tile's 256 rows of dz by offsets of 31 bits)
 // bf16 rows up to which what rounding leaves of dz enters dw, as a contraction twice as long.  Off by 2^-9 of each term, dw is as exact as its own
 // rounding to bf16 on the average of many rows; the fewer there are, the more hangs on single ones.
@@ -128,7 +128,8 @@ inline XentPlan xent_plan(int dtype, int N, int In, int K)
     p.direct_w = p.direct_a = dtype == VGG_BF16 && In % kStep == 0;
     p.few_rows = dtype == VGG_F32 && !p.z_splits && N <= kDirectRows && K >= kDirectClasses;
     const long n_tiles = div_up(N, p.tn), d_tiles = div_up(In, kTA);
-    const size_t per_class = (size_t)p.PL * 2 * (p.NP + (p.direct_w ? 0 : p.InP));
+    p.rest_rows = p.PL == 1 && N <= kRestRows ? p.NP : 0;
+    const size_t per_class = (size_t)p.PL * 2 * (p.NP + p.rest_rows + (p.direct_w ? 0 : p.InP));
     long classes = (long)(kPieceBytes / per_class) / kTA * kTA;
     if (classes < kTA) classes = kTA;
     if (classes > kPieceClasses) classes = kPieceClasses;
@@ -162,7 +163,6 @@ inline XentPlan xent_plan(int dtype, int N, int In, int K)
     p.a2_at = take(p.PL == 2 ? (size_t)4 * p.NP * p.InP : 0);
     p.eg_at = take(p.PL == 2 ? (size_t)N * 4 : 0);
     p.tail_at = take(p.direct_w ? (size_t)kStep * In * 2 : 0);
-    p.rest_rows = p.PL == 1 && N <= kRestRows ? p.NP : 0;
     p.rest_at = take(p.PL == 1 ? (size_t)N * 4 : 0);
     p.dz_at = take((size_t)p.PL * 2 * (p.NP + p.rest_rows) * p.ld_dz);
     p.da_tn = tile_of(N, d_tiles * splits_of(dtype, d_tiles, (int)div_up(most, kStep)));
