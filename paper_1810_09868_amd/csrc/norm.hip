@@ -565,23 +565,27 @@ __global__ __launch_bounds__(256) void layer_norm_bwd_long_kernel(Rows r, const 
     e.store(part + (size_t)range * 2 * r.C + r.C + c, n);
 }
 
-// part [parts][2][C] added up in order: 16 columns to a workgroup, 64 ranges of parts, then these.
+// part [parts][2][C] added up in order: 16 columns to a workgroup at a time, 64 ranges of parts, then these.
+constexpr int kJoinBlocks = 1 << 16;     // (of 1024 threads: a launch has less than 2^32, rows up to 2^30 columns)
 __global__ __launch_bounds__(1024) void layer_norm_join_kernel(const float *__restrict__ part, int parts, int C, float *dgamma, float *dbeta)
 {
     __shared__ float sums[64][17];
     const int at = threadIdx.x & 15, slice = threadIdx.x >> 4;
-    const long col = (long)blockIdx.x * 16 + at, all = 2l * C;
-    float s = 0.f;
-    if (col < all)
-        for (int p = slice; p < parts; p += 64) s += part[(size_t)p * all + col];
-    sums[slice][at] = s;
-    __syncthreads();
-    // a wave's 64 lanes have a column's 64 ranges
-    const long mine = (long)blockIdx.x * 16 + (threadIdx.x >> 6);
-    s = team_sum<64>(sums[threadIdx.x & 63][threadIdx.x >> 6]);
-    if ((threadIdx.x & 63) || mine >= all) return;
-    float *to = mine < C ? dgamma : dbeta;
-    if (to) to[mine < C ? mine : mine - C] = s;
+    const long all = 2l * C;
+    for (long first = (long)blockIdx.x * 16; first < all; first += (long)gridDim.x * 16) {
+        const long col = first + at;
+        float s = 0.f;
+        if (col < all)
+            for (int p = slice; p < parts; p += 64) s += part[(size_t)p * all + col];
+        sums[slice][at] = s;
+        __syncthreads();
+        // a wave's 64 lanes have a column's 64 ranges
+        const long mine = first + (threadIdx.x >> 6);
+        s = team_sum<64>(sums[threadIdx.x & 63][threadIdx.x >> 6]);
+        float *to = mine < C ? dgamma : dbeta;
+        if (!(threadIdx.x & 63) && mine < all && to) to[mine < C ? mine : mine - C] = s;
+        __syncthreads();
+    }
 }
 
 // A thread has UNITS groups of eight columns, 256 apart, all loaded before the first block of numbers.  Memory bounds it where rows begin at whole 16
@@ -693,7 +697,7 @@ int backward_of(const Rows &r, int dtype, int g_dtype, const void *x, const void
             }
         });
     if (rc != VGG_OK || (rc = launch_status()) != VGG_OK || !part) return rc;
-    layer_norm_join_kernel<<<(int)((2l * r.C + 15) / 16), 1024, 0, s>>>(part, parts, r.C, dgamma, dbeta);
+    layer_norm_join_kernel<<<least((2l * r.C + 15) / 16, kJoinBlocks), 1024, 0, s>>>(part, parts, r.C, dgamma, dbeta);
     return launch_status();
 }
 
