@@ -154,10 +154,11 @@ __device__ __forceinline__ void load_columns(const float *p, int c, int n, float
     for (int k = 0; k < 8; ++k) v[k] = p && k < n ? e.get(k) : other;
 }
 
+// y may be x: a row's values are in registers before any of its places is written.
 // One read and one write of every value, which bounds it where rows are many (8192 x 25088 bf16: 157 us, 5.2 TB/s; 50001 x 333 fp32 in padded rows with dropout:
 // 29 us, 4.6 TB/s).  Few rows are one chain of a load, two sums and a store (1 x 4096 fp32: 3.1 us with the launch, 100 x 4096 bf16 with dropout 4.5).
 template <typename T, int LANES, int U>
-__global__ __launch_bounds__(kBlock<LANES>) void layer_norm_kernel(Rows r, const T *__restrict__ x, T *y)
+__global__ __launch_bounds__(kBlock<LANES>) void layer_norm_kernel(Rows r, const T *x, T *y)
 {
     constexpr int TEAMS = kBlock<LANES> / LANES, V = at_least_one(U);
     const int lane = threadIdx.x % LANES, team = TEAMS == 1 ? 0 : threadIdx.x / LANES;
@@ -217,9 +218,9 @@ __global__ __launch_bounds__(kBlock<LANES>) void layer_norm_kernel(Rows r, const
     }
 }
 
-// Rows of any length, met three times by a workgroup of 1024.
+// Rows of any length, met three times by a workgroup of 1024; where y is x, a thread writes what it alone reads.
 template <typename T>
-__global__ __launch_bounds__(1024) void layer_norm_long_kernel(Rows r, const T *__restrict__ x, T *y)
+__global__ __launch_bounds__(1024) void layer_norm_long_kernel(Rows r, const T *x, T *y)
 {
     __shared__ float2 place[32];
     int turn = 0;
@@ -329,7 +330,7 @@ constexpr int kFewRows = 256;
 // belong.  Two reads and a write of every value bound it (8192 x 25088 bf16: 268 us, 4.6 TB/s, and 20 to join its parts; 50001 x 333 fp32 39 and 7;
 // 100 x 4096 bf16, by columns, 5.0).  512 threads with 56 columns each hold the longest rows; 1024 with 28 have too few registers for a row and its next.
 template <typename T, typename G, int LANES, int U>
-__global__ __launch_bounds__(kBlock<LANES>) void layer_norm_bwd_kernel(Rows r, const T *__restrict__ x, const G *dy, G *dx, float *dgamma, float *dbeta,
+__global__ __launch_bounds__(kBlock<LANES>) void layer_norm_bwd_kernel(Rows r, const T *x, const G *dy, G *dx, float *dgamma, float *dbeta,
                                                                        float *part, int relu_mask, int row_blocks)
 {
     // teams of several waves: the waves' sums, then gamma, where U is 7 (the registers do not hold it); else what the teams have to add up
@@ -528,7 +529,7 @@ __global__ __launch_bounds__(1024) void layer_norm_bwd_sums_kernel(Rows r, const
 }
 // ... then 2048 columns of a range of rows to a workgroup.
 template <typename T, typename G>
-__global__ __launch_bounds__(256) void layer_norm_bwd_long_kernel(Rows r, const T *__restrict__ x, const G *dy, G *dx, const float *__restrict__ sums, float *part,
+__global__ __launch_bounds__(256) void layer_norm_bwd_long_kernel(Rows r, const T *x, const G *dy, G *dx, const float *__restrict__ sums, float *part,
                                                                   int relu_mask, int tiles)
 {
     const int tile = blockIdx.x % tiles, range = blockIdx.x / tiles, ranges = gridDim.x / tiles, c = tile * 2048 + threadIdx.x * 8;
