@@ -93,17 +93,22 @@ class DenseHead:
         self.scales: List[torch.Tensor] = []
         self.ws = _bytes(workspace_bytes(dtype, N, dims, group, self.top, norm, pieces))
 
-    def load(self, weights: Sequence[torch.Tensor], biases: Sequence[torch.Tensor]) -> None:
-        """Takes fp32 parameters; momentum starts from zero, layer norms from scale 1 and shift 0, dropout from step 0, and 4-bit
-        weights of earlier parameters are dropped."""
-        if [tuple(t.shape) for t in weights] != [tuple(w.shape) for w in self.w] or [tuple(t.shape) for t in biases] != [tuple(b.shape) for b in self.b]:
+    def load(self, weights: Sequence[torch.Tensor], biases: Sequence[torch.Tensor], gamma: Optional[Sequence[torch.Tensor]] = None,
+             beta: Optional[Sequence[torch.Tensor]] = None) -> None:
+        """Takes fp32 parameters; gamma and beta are the layer norms' scales and shifts, 1 and 0 where they are not given.  Momentum starts
+        from zero, dropout from step 0, and 4-bit weights of earlier parameters are dropped."""
+        shapes = lambda ts: [tuple(t.shape) for t in ts]  # noqa: E731
+        if shapes(weights) != shapes(self.w) or shapes(biases) != shapes(self.b):
             raise ValueError("a weight [out][in] and a bias [out] for each layer of %s" % self.dims)
+        if any(given is not None and shapes(given) != shapes(self.gamma) for given in (gamma, beta)):
+            raise ValueError("a scale and a shift [in] for each layer of %s%s" % (self.dims, "" if self.norm else ", of a head with layer norms"))
         for mine, given in zip(self.w + self.b, list(weights) + list(biases)):
             mine.copy_(given)
-        for t in self.momentum + self.beta + [self.rng[1:]]:
+        for own, given, start in ((self.gamma, gamma, 1.0), (self.beta, beta, 0.0)):
+            for l, t in enumerate(own):
+                t.fill_(start) if given is None else t.copy_(given[l])
+        for t in self.momentum + [self.rng[1:]]:
             t.zero_()
-        for t in self.gamma:
-            t.fill_(1.0)
         self.codes, self.scales = [], []
         self._refresh()
 
