@@ -440,8 +440,10 @@ int vgg_layer_norm_bwd(int dtype, int g_dtype, int N, int C, size_t ldx, const v
 /* ------------------------------------------------ losses over many classes */
 
 /* A dense layer over K classes and its softmax cross entropy, with no score
- * kept (short fp32 products, of at most 4096 rows, 1024 inputs and 2048 classes,
- * leave them in the workspace from one kernel to the next): z[n,k] = sum_i w[k,i] a[n,i] + bias[k],
+ * kept where there are many: short fp32 products (of at most 4096 rows, 1024
+ * inputs and 2048 classes) leave them in the workspace from one kernel to the
+ * next, and so do long contractions that are split because there are few scores,
+ * in one part for each of their ranges.  z[n,k] = sum_i w[k,i] a[n,i] + bias[k],
  *   loss[n] = log sum_k exp(z[n,k]) - z[n,y], y = labels[n]; 0 where y is not
  *             in [0,K);
  *   stats[n][2], or NULL: the row's largest score and the log of the sum of

@@ -1,7 +1,7 @@
-// A dense layer over many classes and its softmax cross entropy, without the scores [N][K] in memory.
+// A dense layer over many classes and its softmax cross entropy, without the scores [N][K] in memory (but where there are few and their contraction is split).
 //
 // z = a w^T + b.  Forward: every tile of scores leaves its rows' largest score m and E, the sum of the exponentials of the others above it;
-// joined over a row's tiles, loss = log(1 + E) - (z_label - m).  Backward, for a piece of the classes at a time: the scores again, from them
+// joined over a row's tiles, loss = log(1 + E) - (z_label - m).  Backward, for a piece of the classes at a time: the same scores again, bit for bit, from them
 // dz = g (softmax - 1[label]), and with it da += dz w, dw = dz^T a, db = sum_n dz.  E is kept without the largest's own 1, and the label's
 // dz is g expm1(log p), so that a label that is all but certain keeps its digits.
 //

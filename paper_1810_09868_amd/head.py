@@ -1,5 +1,5 @@
 """A classifier of dense layers: trained with orthogonalised updates, held in 4 bits, answering with log probabilities; with
-layer norm in front of its layers, dropout between them and a loss that keeps no scores, where they are asked for.
+layer norm in front of its layers, dropout between them and a loss that takes its scores in pieces, where they are asked for.
 
 Buffer management around binding's entry points, as model.Vgg19 around the whole network's (no arithmetic: all compute
 happens in libvgg_mi355x.so).  The layers are those of the network's classifier (dense, ReLU between) on features of any
@@ -49,7 +49,7 @@ class DenseHead:
     norm: every layer takes the layer norm of what comes to it, with a scale and a shift of its own, learned at bias_lr.
     dropout: the share of what leaves a hidden layer (norm: of its layer norm) that a training step drops, anew in each
     step, by `seed`.  pieces: a training step forms the classes' scores and their gradients in pieces (vgg_fc_xent), so that
-    nothing of [N][classes] is kept; answers have them all."""
+    nothing of [N][classes] is kept where that is much; answers have them all."""
 
     def __init__(self, dtype: int, N: int, dims: Sequence[int], lr: float = 0.02, mu: float = 0.95, weight_decay: float = 0.0,
                  bias_lr: float = 0.01, ns_steps: int = 5, group: int = 64, top: int = 5, update_dtype: int = B.F32, norm: bool = False,
